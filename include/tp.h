@@ -555,6 +555,74 @@ int tp_keep_best(const double *fitness, double *best, int32_t *stall,
 int tp_select(const double *fitness, float *params, int32_t N, int64_t P,
               int32_t keep, int32_t *rank, void *stream);
 
+/*
+ * A policy with memory: a gated linear recurrence over bars.  Channel d of
+ * sequence b (an env), pre-activations x, r, i of each step:
+ *   rho = 1/(1+exp(-r)), iota = 1/(1+exp(-i)),
+ *   a = exp(-8 softplus(lambda_d) rho),
+ *   h_t = a h_{t-1} + sqrt(1 - a^2) iota x,   y_t = h_t.
+ * Where done[t][b] is set the episode ends with step t (as for tp_gae): the
+ * state is 0 after it.  Sequence b has len[b] steps (clamped to 0..T); in the
+ * steps past them y and the gradients are 0, the state stays as it is, and
+ * what the inputs hold there does not matter.
+ * States, lambda and their gradients are fp32; x, r, i, y and their gradients
+ * are all fp32 or all bf16 (rounded once, to nearest even).
+ */
+typedef struct tp_recur {
+    int32_t T;             /* steps, >= 1                                    */
+    int32_t B;             /* sequences, >= 1                                */
+    int32_t D;             /* channels, >= 1                                 */
+    int32_t dtype;         /* of x, r, i, y and their gradients              */
+    const float *lambda;   /* [D] decay parameters                           */
+    const uint8_t *done;   /* [T][B] or NULL (no episode ends)               */
+    const int32_t *len;    /* [B] or NULL (all T steps)                      */
+} tp_recur;
+
+/* A [T][B][D] array: element (t, b, d) at p + t*st + b*sb + d elements, so
+ * that x, r and i may be parts of one product's rows.  Outputs must not
+ * overlap themselves or the inputs. */
+typedef struct tp_rows {
+    void *p;
+    int64_t st, sb;
+} tp_rows;
+
+/* Bytes of the states tp_recur_forward keeps for tp_recur_backward, and of
+ * the workspace either call needs (256-byte aligned; its contents do not
+ * matter between calls).  0 for bad sizes. */
+size_t tp_recur_saved_bytes(const tp_recur *cfg);
+size_t tp_recur_workspace_bytes(const tp_recur *cfg);
+
+/*
+ * tp_recur_forward -- y and the last states of whole sequences.
+ *   h0 [B][D] or NULL (zeros); y may have p = NULL (not stored); h_last
+ *   [B][D] or NULL, the state after the last step (0 where done is set on
+ *   it); saved or NULL (no gradients wanted).
+ */
+int tp_recur_forward(const tp_recur *cfg, const tp_rows *x, const tp_rows *r,
+                     const tp_rows *i, const float *h0, const tp_rows *y, float *h_last,
+                     float *saved, void *work, size_t work_bytes, void *stream);
+
+/*
+ * tp_recur_backward -- gradients of everything tp_recur_forward read, from
+ * dy and dh_last ([B][D] or NULL, zeros).  saved: what the forward call on
+ * the same inputs kept.
+ *   dx, dr, di as x, r, i; dlambda [D]; dh0 [B][D] or NULL.
+ * Sums over steps and sequences run in a fixed order.
+ */
+int tp_recur_backward(const tp_recur *cfg, const tp_rows *x, const tp_rows *r,
+                      const tp_rows *i, const float *saved, const tp_rows *dy,
+                      const float *dh_last, const tp_rows *dx, const tp_rows *dr,
+                      const tp_rows *di, float *dlambda, float *dh0, void *work,
+                      size_t work_bytes, void *stream);
+
+/*
+ * tp_recur_step -- one bar: h_out = the states after a step from h, y
+ * (or p = NULL) the same before episode ends clear them.  cfg->T must be 1
+ * and cfg->len NULL; done [B] or NULL; h, h_out [B][D], may be one buffer.
+ */
+int tp_recur_step(const tp_recur *cfg, const tp_rows *x, const tp_rows *r, const tp_rows *i,
+                  const float *h, float *h_out, const tp_rows *y, void *stream);
+
 /* Message for the last non-OK return on the calling thread ("" if none). */
 const char *tp_last_error(void);
 

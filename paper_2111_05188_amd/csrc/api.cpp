@@ -231,6 +231,85 @@ int check_critic(const tp_critic *c, CriticLayout *lay)
     return TP_OK;
 }
 
+// ---------------------------------------------------------------------------
+// gated linear recurrence
+// ---------------------------------------------------------------------------
+int check_recur(const tp_recur *c)
+{
+    if (!c) return fail(TP_EINVAL, "recurrence configuration is NULL");
+    if (c->T < 1 || c->B < 1 || c->D < 1)
+        return fail(TP_EINVAL, "recurrence T = %d, B = %d, D = %d must be >= 1", c->T, c->B, c->D);
+    if (c->dtype != TP_F32 && c->dtype != TP_BF16)
+        return fail(TP_EINVAL, "recurrence dtype %d", c->dtype);
+    if (!recur_fits(c->T, c->B, c->D))
+        return fail(TP_EUNSUPPORTED, "recurrence of T = %d, B = %d, D = %d exceeds the launch grid",
+                    c->T, c->B, c->D);
+    return TP_OK;
+}
+
+// One [T][B][D] array of the recurrence: strides to bytes.
+int check_rows(const tp_recur *c, const tp_rows *m, const char *name, bool needed, RecurRows *out)
+{
+    out->p = nullptr;
+    out->st = out->sb = 0;
+    if (!m || !m->p)
+        return needed ? fail(TP_EINVAL, "recurrence array %s is NULL", name) : TP_OK;
+    const int es = c->dtype == TP_BF16 ? 2 : 4;
+    if (!aligned(m->p, es)) return fail(TP_EINVAL, "recurrence array %s is misaligned", name);
+    const int64_t lim = (int64_t)1 << 40;
+    if ((c->T > 1 && (m->st < 0 || m->st > lim)) || (c->B > 1 && (m->sb < 0 || m->sb > lim)))
+        return fail(TP_EINVAL, "recurrence array %s: strides %lld, %lld", name, (long long)m->st,
+                    (long long)m->sb);
+    out->p = m->p;
+    // the stride of an axis of one is never followed
+    out->st = c->T > 1 ? m->st * es : 0;
+    out->sb = c->B > 1 ? m->sb * es : 0;
+    return TP_OK;
+}
+
+// An output: every element at an address of its own (rows of D, one axis
+// inside the other).
+int check_out_rows(const tp_recur *c, const tp_rows *m, const char *name)
+{
+    if (!m || !m->p) return TP_OK;
+    const int64_t D = c->D, st = m->st, sb = m->sb;
+    const bool t_ok = c->T == 1 || st >= D, b_ok = c->B == 1 || sb >= D;
+    const bool nest = c->T == 1 || c->B == 1 || st >= (c->B - 1) * sb + D ||
+                      sb >= (c->T - 1) * st + D;
+    if (!t_ok || !b_ok || !nest)
+        return fail(TP_EINVAL, "recurrence output %s: strides %lld, %lld let rows overlap", name,
+                    (long long)st, (long long)sb);
+    return TP_OK;
+}
+
+// what the whole-sequence calls share
+int recur_args(const tp_recur *c, const tp_rows *x, const tp_rows *r, const tp_rows *i, void *work,
+               size_t work_bytes, RecurArgs *a)
+{
+    int rc = check_recur(c);
+    if (rc != TP_OK) return rc;
+    if (!c->lambda || !aligned(c->lambda, 4))
+        return fail(TP_EINVAL, "recurrence lambda is NULL or misaligned");
+    if (c->len && !aligned(c->len, 4)) return fail(TP_EINVAL, "recurrence len is misaligned");
+    a->T = c->T;
+    a->B = c->B;
+    a->D = c->D;
+    a->bf16 = c->dtype == TP_BF16;
+    a->lam = c->lambda;
+    a->done = c->done;
+    a->len = c->len;
+    if ((rc = check_rows(c, x, "x", true, &a->x)) != TP_OK) return rc;
+    if ((rc = check_rows(c, r, "r", true, &a->r)) != TP_OK) return rc;
+    if ((rc = check_rows(c, i, "i", true, &a->i)) != TP_OK) return rc;
+    if (!work || !aligned(work, 256))
+        return fail(TP_EINVAL, "recurrence workspace is NULL or not 256-byte aligned");
+    const size_t need = recur_workspace_bytes(c->T, c->B, c->D);
+    if (work_bytes < need)
+        return fail(TP_EINVAL, "recurrence workspace of %zu bytes, %zu needed", work_bytes, need);
+    a->work = work;
+    return TP_OK;
+}
+
 }  // namespace
 
 // ---------------------------------------------------------------------------
@@ -825,6 +904,98 @@ int tp_select(const double *fitness, float *params, int32_t N, int64_t P, int32_
     if (keep < 1 || keep > N) return fail(TP_EINVAL, "keep = %d outside 1..N = %d", keep, N);
     hipError_t e = launch_select(fitness, params, N, P, keep, rank, (hipStream_t)stream);
     if (e != hipSuccess) return hip_fail(e, "select launch");
+    return ok();
+}
+
+size_t tp_recur_saved_bytes(const tp_recur *cfg)
+{
+    if (check_recur(cfg) != TP_OK) return 0;
+    ok();
+    return (size_t)((cfg->T + RECUR_CHUNK - 1) / RECUR_CHUNK) * cfg->B * cfg->D * sizeof(float);
+}
+
+size_t tp_recur_workspace_bytes(const tp_recur *cfg)
+{
+    if (check_recur(cfg) != TP_OK) return 0;
+    ok();
+    return recur_workspace_bytes(cfg->T, cfg->B, cfg->D);
+}
+
+int tp_recur_forward(const tp_recur *cfg, const tp_rows *x, const tp_rows *r, const tp_rows *i,
+                     const float *h0, const tp_rows *y, float *h_last, float *saved, void *work,
+                     size_t work_bytes, void *stream)
+{
+    RecurArgs a{};
+    int rc = recur_args(cfg, x, r, i, work, work_bytes, &a);
+    if (rc != TP_OK) return rc;
+    if ((rc = check_rows(cfg, y, "y", false, &a.y)) != TP_OK) return rc;
+    if ((rc = check_out_rows(cfg, y, "y")) != TP_OK) return rc;
+    if (!a.y.p && !h_last && !saved)
+        return fail(TP_EINVAL, "recurrence has no output: y, h_last and saved are NULL");
+    if (!aligned(h0, 4) || !aligned(h_last, 4) || !aligned(saved, 4))
+        return fail(TP_EINVAL, "recurrence states are misaligned");
+    a.h0 = h0;
+    a.h_last = h_last;
+    a.saved = saved;
+    hipError_t e = launch_recur(a, false, (hipStream_t)stream);
+    if (e != hipSuccess) return hip_fail(e, "recurrence launch");
+    return ok();
+}
+
+int tp_recur_backward(const tp_recur *cfg, const tp_rows *x, const tp_rows *r, const tp_rows *i,
+                      const float *saved, const tp_rows *dy, const float *dh_last,
+                      const tp_rows *dx, const tp_rows *dr, const tp_rows *di, float *dlambda,
+                      float *dh0, void *work, size_t work_bytes, void *stream)
+{
+    RecurArgs a{};
+    int rc = recur_args(cfg, x, r, i, work, work_bytes, &a);
+    if (rc != TP_OK) return rc;
+    if ((rc = check_rows(cfg, dy, "dy", true, &a.dy)) != TP_OK) return rc;
+    if ((rc = check_rows(cfg, dx, "dx", true, &a.dx)) != TP_OK) return rc;
+    if ((rc = check_rows(cfg, dr, "dr", true, &a.dr)) != TP_OK) return rc;
+    if ((rc = check_rows(cfg, di, "di", true, &a.di)) != TP_OK) return rc;
+    if ((rc = check_out_rows(cfg, dx, "dx")) != TP_OK) return rc;
+    if ((rc = check_out_rows(cfg, dr, "dr")) != TP_OK) return rc;
+    if ((rc = check_out_rows(cfg, di, "di")) != TP_OK) return rc;
+    if (!saved || !dlambda) return fail(TP_EINVAL, "recurrence saved or dlambda is NULL");
+    if (!aligned(saved, 4) || !aligned(dh_last, 4) || !aligned(dlambda, 4) || !aligned(dh0, 4))
+        return fail(TP_EINVAL, "recurrence states are misaligned");
+    a.saved = const_cast<float *>(saved);
+    a.dh_last = dh_last;
+    a.dlam = dlambda;
+    a.dh0 = dh0;
+    hipError_t e = launch_recur(a, true, (hipStream_t)stream);
+    if (e != hipSuccess) return hip_fail(e, "recurrence gradient launch");
+    return ok();
+}
+
+int tp_recur_step(const tp_recur *cfg, const tp_rows *x, const tp_rows *r, const tp_rows *i,
+                  const float *h, float *h_out, const tp_rows *y, void *stream)
+{
+    RecurArgs a{};
+    int rc = check_recur(cfg);
+    if (rc != TP_OK) return rc;
+    if (cfg->T != 1 || cfg->len)
+        return fail(TP_EINVAL, "recurrence step: T = %d must be 1 and len NULL", cfg->T);
+    if (!cfg->lambda || !aligned(cfg->lambda, 4))
+        return fail(TP_EINVAL, "recurrence lambda is NULL or misaligned");
+    if ((rc = check_rows(cfg, x, "x", true, &a.x)) != TP_OK) return rc;
+    if ((rc = check_rows(cfg, r, "r", true, &a.r)) != TP_OK) return rc;
+    if ((rc = check_rows(cfg, i, "i", true, &a.i)) != TP_OK) return rc;
+    if ((rc = check_rows(cfg, y, "y", false, &a.y)) != TP_OK) return rc;
+    if ((rc = check_out_rows(cfg, y, "y")) != TP_OK) return rc;
+    if (!h || !h_out || !aligned(h, 4) || !aligned(h_out, 4))
+        return fail(TP_EINVAL, "recurrence state is NULL or misaligned");
+    a.T = 1;
+    a.B = cfg->B;
+    a.D = cfg->D;
+    a.bf16 = cfg->dtype == TP_BF16;
+    a.lam = cfg->lambda;
+    a.done = cfg->done;
+    a.h0 = h;
+    a.h_last = h_out;
+    hipError_t e = launch_recur_step(a, (hipStream_t)stream);
+    if (e != hipSuccess) return hip_fail(e, "recurrence step launch");
     return ok();
 }
 

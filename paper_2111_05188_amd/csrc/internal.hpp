@@ -195,6 +195,39 @@ hipError_t launch_ppo_update(const PpoArgs &a, hipStream_t s);
 hipError_t launch_minibatch_rows(uint64_t seed, uint64_t counter, int n_updates, int B, int L,
                                  int E, int agent, int epa, int64_t *idx, hipStream_t s);
 
+// Gated linear recurrence: steps of a chunk (the states kept for the gradients
+// are those before each chunk), rows of a [T][B][D] array in bytes.
+constexpr int RECUR_CHUNK = 8;
+
+struct RecurRows {
+    void *p;
+    int64_t st, sb;            // bytes between steps and between sequences
+};
+
+struct RecurArgs {
+    int T, B, D;
+    bool bf16;
+    const float *lam;
+    const uint8_t *done;
+    const int32_t *len;
+    RecurRows x, r, i, y, dy, dx, dr, di;
+    const float *h0;           // the step's state in
+    float *h_last;             // the step's state out
+    float *saved;
+    const float *dh_last;
+    float *dlam, *dh0;
+    void *work;
+    // filled by the launcher
+    float2 *maps;
+    float *parts;
+    int units, blocks_d, seg_len;
+};
+
+size_t recur_workspace_bytes(int T, int B, int D);
+bool recur_fits(int T, int B, int D);
+hipError_t launch_recur(RecurArgs &a, bool backward, hipStream_t s);
+hipError_t launch_recur_step(RecurArgs &a, hipStream_t s);
+
 // Maximum LDS per workgroup on gfx950.
 constexpr size_t LDS_LIMIT = 160 * 1024;
 

@@ -78,6 +78,15 @@ class Traj(C.Structure):
                 ("mu_tap", C.c_void_p)]
 
 
+class Recur(C.Structure):
+    _fields_ = [("T", C.c_int32), ("B", C.c_int32), ("D", C.c_int32), ("dtype", C.c_int32),
+                ("lam", C.c_void_p), ("done", C.c_void_p), ("len", C.c_void_p)]
+
+
+class Rows(C.Structure):
+    _fields_ = [("p", C.c_void_p), ("st", C.c_int64), ("sb", C.c_int64)]
+
+
 EXPORTS = ("tp_env_reset", "tp_env_step", "tp_actor_packed_bytes",
            "tp_actor_pack", "tp_rollout", "tp_gae", "tp_critic_packed_bytes",
            "tp_critic_pack", "tp_critic_value", "tp_backtest_metrics",
@@ -88,6 +97,8 @@ EXPORTS = ("tp_env_reset", "tp_env_step", "tp_actor_packed_bytes",
            "tp_rollout_kernel",
            "tp_actor_release", "tp_critic_release", "tp_check_starts",
            "tp_backtest_metrics_noalloc",
+           "tp_recur_saved_bytes", "tp_recur_workspace_bytes", "tp_recur_forward",
+           "tp_recur_backward", "tp_recur_step",
            "tp_last_error", "tp_version")
 
 _lib = None
@@ -138,6 +149,13 @@ def load(path: str = LIB_PATH):
     L.tp_actor_release.argtypes = [vp]
     L.tp_critic_release.argtypes = [vp]
     L.tp_check_starts.argtypes = [vp, i32, i64, i32]
+    L.tp_recur_saved_bytes.restype = sz
+    L.tp_recur_saved_bytes.argtypes = [vp]
+    L.tp_recur_workspace_bytes.restype = sz
+    L.tp_recur_workspace_bytes.argtypes = [vp]
+    L.tp_recur_forward.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    L.tp_recur_backward.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    L.tp_recur_step.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp]
     L.tp_last_error.restype = C.c_char_p
     L.tp_version.restype = C.c_int
     for f in ("tp_env_reset", "tp_env_step", "tp_actor_pack", "tp_rollout", "tp_gae",
@@ -145,7 +163,8 @@ def load(path: str = LIB_PATH):
               "tp_ensemble_fuse", "tp_fitness", "tp_keep_best", "tp_select",
               "tp_ppo_update", "tp_ppo_update_agents", "tp_minibatch_rows",
               "tp_actor_release", "tp_critic_release", "tp_check_starts",
-              "tp_backtest_metrics_noalloc"):
+              "tp_backtest_metrics_noalloc", "tp_recur_forward", "tp_recur_backward",
+              "tp_recur_step"):
         getattr(L, f).restype = C.c_int
     _lib = L
     return L
@@ -616,3 +635,94 @@ def rollout_kernel(mkt: MarketT, actor: ActorT) -> int:
     if r < 0:
         _check(r)
     return r
+
+
+# --------------------------------------------------------------------------
+# gated linear recurrence
+# --------------------------------------------------------------------------
+
+class RecurT:
+    """Sequences of the gated linear recurrence (see tp_recur): lam [D] fp32,
+    T steps of B sequences, done [T][B] uint8 and lens [B] int32 optional."""
+
+    def __init__(self, lam: torch.Tensor, T: int, B: int, dtype: torch.dtype,
+                 done: torch.Tensor | None = None, lens: torch.Tensor | None = None):
+        assert lam.dim() == 1 and lam.dtype == torch.float32 and lam.is_contiguous()
+        assert dtype in (torch.float32, torch.bfloat16)
+        assert done is None or (done.shape == (T, B) and done.element_size() == 1
+                                and done.is_contiguous())
+        assert lens is None or (lens.shape == (B,) and lens.dtype == torch.int32
+                                and lens.is_contiguous())
+        self.lam, self.done, self.lens, self.dtype = lam, done, lens, dtype
+        self.T, self.B, self.D = T, B, lam.shape[0]
+        self.s = Recur(T, B, self.D, TP_BF16 if dtype == torch.bfloat16 else TP_F32, _ptr(lam),
+                       _ptr(done), _ptr(lens))
+
+    def _bytes(self, f) -> int:
+        nb = f(C.byref(self.s))
+        if nb == 0:
+            raise TPError(TP_EINVAL, last_error())
+        return nb
+
+    def workspace(self) -> torch.Tensor:
+        return torch.empty(self._bytes(load().tp_recur_workspace_bytes), dtype=torch.uint8,
+                           device=self.lam.device)
+
+    def saved(self) -> torch.Tensor:
+        """The states recur_forward keeps for recur_backward."""
+        return torch.empty(self._bytes(load().tp_recur_saved_bytes) // 4, dtype=torch.float32,
+                           device=self.lam.device)
+
+    def rows(self, t: torch.Tensor | None):
+        """A [T][B][D] tensor (any strides over steps and sequences)."""
+        if t is None:
+            return None
+        assert t.shape == (self.T, self.B, self.D) and t.dtype == self.dtype
+        assert self.D == 1 or t.stride(2) == 1
+        return C.byref(Rows(t.data_ptr(), t.stride(0), t.stride(1)))
+
+    def state(self, t: torch.Tensor | None):
+        if t is None:
+            return None
+        assert t.shape == (self.B, self.D) and t.dtype == torch.float32 and t.is_contiguous()
+        return t.data_ptr()
+
+
+def recur_forward(rc: RecurT, x, r, i, y, work, h0=None, h_last=None, saved=None, stream=None):
+    """y [T][B][D] (or None) and h_last [B][D] of x, r, i [T][B][D]; saved
+    (rc.saved()) keeps what recur_backward needs."""
+    assert saved is None or saved.numel() * 4 >= rc._bytes(load().tp_recur_saved_bytes)
+    _check(load().tp_recur_forward(C.byref(rc.s), rc.rows(x), rc.rows(r), rc.rows(i),
+                                   rc.state(h0), rc.rows(y), rc.state(h_last), _ptr(saved),
+                                   _ptr(work), work.numel(), _stream(stream)))
+
+
+def recur_backward(rc: RecurT, x, r, i, saved, dy, dx, dr, di, dlam, work, dh_last=None,
+                   dh0=None, stream=None):
+    """Gradients of recur_forward's inputs into dx, dr, di [T][B][D], dlam [D]
+    and dh0 [B][D]."""
+    assert saved.numel() * 4 >= rc._bytes(load().tp_recur_saved_bytes)
+    assert dlam.shape == (rc.D,) and dlam.dtype == torch.float32 and dlam.is_contiguous()
+    _check(load().tp_recur_backward(C.byref(rc.s), rc.rows(x), rc.rows(r), rc.rows(i),
+                                    _ptr(saved), rc.rows(dy), rc.state(dh_last), rc.rows(dx),
+                                    rc.rows(dr), rc.rows(di), _ptr(dlam), rc.state(dh0),
+                                    _ptr(work), work.numel(), _stream(stream)))
+
+
+def recur_step(x, r, i, lam, h, h_out, y=None, done=None, stream=None):
+    """One bar: h_out [B][D] fp32 (may be h) and y [B][D] from x, r, i [B][D]
+    and the states h; done [B] uint8 clears states after the step."""
+    B, D = h.shape
+    assert h.dtype == h_out.dtype == lam.dtype == torch.float32 and lam.shape == (D,)
+    assert h_out.shape == h.shape and h.is_contiguous() and h_out.is_contiguous()
+    assert lam.is_contiguous()
+    assert done is None or (done.shape == (B,) and done.element_size() == 1
+                            and done.is_contiguous())
+    s = Recur(1, B, D, _dtype_code(x), _ptr(lam), _ptr(done), None)
+
+    def rows(t):
+        assert t.shape == (B, D) and t.dtype == x.dtype and (D == 1 or t.stride(1) == 1)
+        return C.byref(Rows(t.data_ptr(), 0, t.stride(0)))
+
+    _check(load().tp_recur_step(C.byref(s), rows(x), rows(r), rows(i), _ptr(h), _ptr(h_out),
+                                None if y is None else rows(y), _stream(stream)))
