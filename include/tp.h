@@ -623,6 +623,58 @@ int tp_recur_backward(const tp_recur *cfg, const tp_rows *x, const tp_rows *r,
 int tp_recur_step(const tp_recur *cfg, const tp_rows *x, const tp_rows *r, const tp_rows *i,
                   const float *h, float *h_out, const tp_rows *y, void *stream);
 
+/*
+ * 4-bit matrices (the OCP microscaling format MXFP4): blocks of 32 elements
+ * along K share a scale 2^e; an element is one of 0, 1/2, 1, 3/2, 2, 3, 4, 6
+ * with a sign, times it.  e = floor(log2 of the block's largest magnitude) - 2,
+ * at least -127; elements round to nearest, ties to the even code, and the
+ * largest magnitudes saturate at 6.  A block with a NaN or an infinity is NaN.
+ * `data` holds the matrix in the order in which the products' matrix
+ * instructions read it (opaque; 256-byte aligned, tp_mx4_bytes of them).
+ */
+typedef struct tp_mx4 {
+    void *data;
+    int64_t rows, K;       /* 1 .. 2^29 each                                */
+} tp_mx4;
+
+typedef enum { TP_ACT_NONE = 0, TP_ACT_TANH = 1 } tp_act;
+
+/* Bytes of a 4-bit matrix (about rows * K * 17/32, rows rounded up to 32, K
+ * to 64); 0 for bad sizes. */
+size_t tp_mx4_bytes(int64_t rows, int64_t K);
+
+/*
+ * tp_mx4_quantize -- out = x in 4 bits.  Element (row, k) of x at
+ * x + row*row_stride + k*col_stride elements (dtype fp32 or bf16); one of the
+ * strides must be 1, so a transposed view works as well.
+ */
+int tp_mx4_quantize(const void *x, int32_t dtype, int64_t row_stride, int64_t col_stride,
+                    const tp_mx4 *out, void *stream);
+
+/* tp_mx4_dequantize -- the values of m into y [rows][ld], ld >= K (exact in
+ * fp32; in bf16 too, as far as its exponent reaches). */
+int tp_mx4_dequantize(const tp_mx4 *m, void *y, int32_t dtype, int64_t ld, void *stream);
+
+/* Bytes of the workspace tp_mx4_matmul and tp_mx4_linear need for these
+ * sizes (256-byte aligned); 0 for bad sizes. */
+size_t tp_mx4_workspace_bytes(int64_t M, int64_t N, int64_t K);
+
+/*
+ * tp_mx4_matmul -- y[m][n] = act(sum_k a[m][k] w[n][k] + bias[n]): a.rows = M,
+ * w.rows = N, a.K = w.K; sums in fp32 in a fixed order, rounded once to y's
+ * type.  bias [N] fp32 or NULL; y [M][ldy], ldy >= N.
+ */
+int tp_mx4_matmul(const tp_mx4 *a, const tp_mx4 *w, const float *bias, int32_t act, void *y,
+                  int32_t dtype, int64_t ldy, void *work, size_t work_bytes, void *stream);
+
+/*
+ * tp_mx4_linear -- a layer on 4-bit weights: the rows of x [M][ldx] (x_dtype,
+ * w.K elements each) go to 4 bits as by tp_mx4_quantize, then the product.
+ */
+int tp_mx4_linear(const void *x, int32_t x_dtype, int64_t M, int64_t ldx, const tp_mx4 *w,
+                  const float *bias, int32_t act, void *y, int32_t dtype, int64_t ldy, void *work,
+                  size_t work_bytes, void *stream);
+
 /* Message for the last non-OK return on the calling thread ("" if none). */
 const char *tp_last_error(void);
 

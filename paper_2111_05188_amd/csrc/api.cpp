@@ -310,6 +310,69 @@ int recur_args(const tp_recur *c, const tp_rows *x, const tp_rows *r, const tp_r
     return TP_OK;
 }
 
+// ---------------------------------------------------------------------------
+// 4-bit matrices
+// ---------------------------------------------------------------------------
+constexpr int64_t MX4_MOST = (int64_t)1 << 29;
+
+int check_mx4_size(int64_t rows, int64_t K, const char *name)
+{
+    if (rows < 1 || K < 1 || rows > MX4_MOST || K > MX4_MOST)
+        return fail(TP_EINVAL, "4-bit %s: %lld rows of %lld elements (1 .. 2^29 each)", name,
+                    (long long)rows, (long long)K);
+    const Mx4Layout L = mx4_layout(rows, K);
+    if (L.tiles * L.groups > 1 << 24)   // workgroups of 256 threads in a 32-bit grid
+        return fail(TP_EUNSUPPORTED, "4-bit %s: %lld x %lld exceeds the launch grid", name,
+                    (long long)rows, (long long)K);
+    return TP_OK;
+}
+
+int check_mx4(const tp_mx4 *m, const char *name)
+{
+    if (!m || !m->data) return fail(TP_EINVAL, "4-bit %s is NULL", name);
+    if (!aligned(m->data, 256)) return fail(TP_EINVAL, "4-bit %s is not 256-byte aligned", name);
+    return check_mx4_size(m->rows, m->K, name);
+}
+
+int check_matrix(const void *p, int dtype, int64_t ld, int64_t cols, const char *name)
+{
+    if (dtype != TP_F32 && dtype != TP_BF16) return fail(TP_EINVAL, "%s: dtype %d", name, dtype);
+    if (!p) return fail(TP_EINVAL, "%s is NULL", name);
+    if (!aligned(p, dtype == TP_BF16 ? 2 : 4)) return fail(TP_EINVAL, "%s is misaligned", name);
+    if (ld < cols || ld > (int64_t)1 << 40)
+        return fail(TP_EINVAL, "%s: pitch %lld of rows of %lld", name, (long long)ld,
+                    (long long)cols);
+    return TP_OK;
+}
+
+// a product's epilogue, output and workspace (a.la, a.lw are set)
+int mx4_product(Mx4Args &a, const float *bias, int32_t act, void *y, int32_t dtype, int64_t ldy,
+                void *work, size_t work_bytes, void *stream)
+{
+    const int64_t M = a.la.rows, N = a.lw.rows, K = a.la.K;
+    if (!aligned(bias, 4)) return fail(TP_EINVAL, "bias is misaligned");
+    if (act != TP_ACT_NONE && act != TP_ACT_TANH) return fail(TP_EINVAL, "activation %d", act);
+    int rc = check_matrix(y, dtype, ldy, N, "y");
+    if (rc != TP_OK) return rc;
+    if (((M + 31) / 32) * ((N + 31) / 32) > 1 << 24)
+        return fail(TP_EUNSUPPORTED, "a product of %lld x %lld exceeds the launch grid",
+                    (long long)M, (long long)N);
+    if (!work || !aligned(work, 256))
+        return fail(TP_EINVAL, "4-bit workspace is NULL or not 256-byte aligned");
+    const size_t need = mx4_workspace_bytes(M, N, K);
+    if (work_bytes < need)
+        return fail(TP_EINVAL, "4-bit workspace of %zu bytes, %zu needed", work_bytes, need);
+    a.bias = bias;
+    a.act = act;
+    a.y = y;
+    a.y_bf16 = dtype == TP_BF16;
+    a.ldy = ldy;
+    a.work = work;
+    hipError_t e = launch_mx4_product(a, (hipStream_t)stream);
+    if (e != hipSuccess) return hip_fail(e, "4-bit product launch");
+    return ok();
+}
+
 }  // namespace
 
 // ---------------------------------------------------------------------------
@@ -997,6 +1060,91 @@ int tp_recur_step(const tp_recur *cfg, const tp_rows *x, const tp_rows *r, const
     hipError_t e = launch_recur_step(a, (hipStream_t)stream);
     if (e != hipSuccess) return hip_fail(e, "recurrence step launch");
     return ok();
+}
+
+size_t tp_mx4_bytes(int64_t rows, int64_t K)
+{
+    if (check_mx4_size(rows, K, "matrix") != TP_OK) return 0;
+    ok();
+    return mx4_layout(rows, K).total;
+}
+
+int tp_mx4_quantize(const void *x, int32_t dtype, int64_t row_stride, int64_t col_stride,
+                    const tp_mx4 *out, void *stream)
+{
+    int rc = check_mx4(out, "output");
+    if (rc != TP_OK) return rc;
+    const int64_t rows = out->rows, K = out->K;
+    // the stride of an axis of one is never followed
+    if (K == 1) col_stride = 1;
+    else if (rows == 1) row_stride = 1;
+    const bool by_rows = col_stride == 1;
+    if (!by_rows && row_stride != 1)
+        return fail(TP_EUNSUPPORTED, "4-bit source: strides %lld, %lld, one of them must be 1",
+                    (long long)row_stride, (long long)col_stride);
+    // rows may repeat or lie on one another: the source is only read
+    const int64_t ld = by_rows ? row_stride : col_stride;
+    if (ld < 0 || ld > (int64_t)1 << 40)
+        return fail(TP_EINVAL, "4-bit source: stride %lld", (long long)ld);
+    if ((rc = check_matrix(x, dtype, 1, 1, "4-bit source")) != TP_OK) return rc;
+    hipError_t e = launch_mx4_quantize(x, dtype == TP_BF16, row_stride, col_stride,
+                                       mx4_layout(rows, K), out->data, (hipStream_t)stream);
+    if (e != hipSuccess) return hip_fail(e, "quantize launch");
+    return ok();
+}
+
+int tp_mx4_dequantize(const tp_mx4 *m, void *y, int32_t dtype, int64_t ld, void *stream)
+{
+    int rc = check_mx4(m, "matrix");
+    if (rc != TP_OK) return rc;
+    if ((rc = check_matrix(y, dtype, ld, m->K, "y")) != TP_OK) return rc;
+    hipError_t e = launch_mx4_dequantize(m->data, mx4_layout(m->rows, m->K), y, dtype == TP_BF16,
+                                         ld, (hipStream_t)stream);
+    if (e != hipSuccess) return hip_fail(e, "dequantize launch");
+    return ok();
+}
+
+size_t tp_mx4_workspace_bytes(int64_t M, int64_t N, int64_t K)
+{
+    if (check_mx4_size(M, K, "matrix") != TP_OK || check_mx4_size(N, K, "matrix") != TP_OK) return 0;
+    ok();
+    return mx4_workspace_bytes(M, N, K);
+}
+
+int tp_mx4_matmul(const tp_mx4 *a, const tp_mx4 *w, const float *bias, int32_t act, void *y,
+                  int32_t dtype, int64_t ldy, void *work, size_t work_bytes, void *stream)
+{
+    int rc = check_mx4(a, "a");
+    if (rc != TP_OK) return rc;
+    if ((rc = check_mx4(w, "w")) != TP_OK) return rc;
+    if (a->K != w->K)
+        return fail(TP_EINVAL, "a has %lld elements a row, w %lld", (long long)a->K,
+                    (long long)w->K);
+    Mx4Args p{};
+    p.a = (const uint8_t *)a->data;
+    p.w = (const uint8_t *)w->data;
+    p.la = mx4_layout(a->rows, a->K);
+    p.lw = mx4_layout(w->rows, w->K);
+    return mx4_product(p, bias, act, y, dtype, ldy, work, work_bytes, stream);
+}
+
+int tp_mx4_linear(const void *x, int32_t x_dtype, int64_t M, int64_t ldx, const tp_mx4 *w,
+                  const float *bias, int32_t act, void *y, int32_t dtype, int64_t ldy, void *work,
+                  size_t work_bytes, void *stream)
+{
+    int rc = check_mx4(w, "w");
+    if (rc != TP_OK) return rc;
+    if ((rc = check_mx4_size(M, w->K, "x")) != TP_OK) return rc;
+    if (M == 1) ldx = w->K;             // never followed
+    if ((rc = check_matrix(x, x_dtype, ldx, w->K, "x")) != TP_OK) return rc;
+    Mx4Args p{};
+    p.x = x;
+    p.x_bf16 = x_dtype == TP_BF16;
+    p.ldx = ldx;
+    p.w = (const uint8_t *)w->data;
+    p.la = mx4_layout(M, w->K);
+    p.lw = mx4_layout(w->rows, w->K);
+    return mx4_product(p, bias, act, y, dtype, ldy, work, work_bytes, stream);
 }
 
 int tp_gae(const float *reward, const float *value, const uint8_t *done, int32_t L, int32_t E,

@@ -159,6 +159,15 @@ __device__ __forceinline__ void wave_lds_fence()
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
 
+// Keeps an address in scalar registers (the compiler otherwise adds the lane's
+// offset first and steps one 64-bit vector address per row).
+template <class P>
+__device__ __forceinline__ P *scalar(P *p)
+{
+    asm("" : "+s"(p));
+    return p;
+}
+
 // Sum over the 64 lanes (same value returned to every lane).
 __device__ __forceinline__ double wave_sum(double v)
 {

@@ -228,6 +228,37 @@ bool recur_fits(int T, int B, int D);
 hipError_t launch_recur(RecurArgs &a, bool backward, hipStream_t s);
 hipError_t launch_recur_step(RecurArgs &a, hipStream_t s);
 
+// 4-bit matrices (mx4.hpp has the layout).
+struct Mx4Layout {
+    int64_t rows, K;
+    int64_t tiles, ksteps, groups;   // of 32 rows, 64 elements, 4 k-steps
+    int64_t off_scales;
+    size_t total;
+};
+
+Mx4Layout mx4_layout(int64_t rows, int64_t K);
+hipError_t launch_mx4_quantize(const void *x, bool bf16, int64_t row_stride, int64_t col_stride,
+                               const Mx4Layout &L, void *dst, hipStream_t s);
+hipError_t launch_mx4_dequantize(const void *src, const Mx4Layout &L, void *y, bool bf16,
+                                 int64_t ld, hipStream_t s);
+
+struct Mx4Args {
+    const uint8_t *a, *w;            // a is NULL where x is taken to 4 bits on the way
+    Mx4Layout la, lw;
+    const void *x;                   // rows [M][K] of pitch ldx
+    bool x_bf16;
+    int64_t ldx;
+    const float *bias;
+    int act;
+    void *y;
+    bool y_bf16;
+    int64_t ldy;
+    void *work;
+};
+
+size_t mx4_workspace_bytes(int64_t M, int64_t N, int64_t K);
+hipError_t launch_mx4_product(const Mx4Args &a, hipStream_t s);
+
 // Maximum LDS per workgroup on gfx950.
 constexpr size_t LDS_LIMIT = 160 * 1024;
 

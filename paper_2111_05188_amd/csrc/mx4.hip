@@ -1,0 +1,315 @@
+// Matrices to 4-bit blocks and back.  Both directions move what they have to
+// and compute little; they are bound by the memory.
+#include "mx4.hpp"
+
+namespace tpk {
+namespace {
+
+// ---------------------------------------------------------------------------
+// rows in memory: a wave takes 8 rows x 256 elements (4 k-steps).  Eight lanes
+// read a row's 64 elements of a k-step (bf16: 128 bytes), four lanes hold a
+// block and take its largest magnitude together, and each stores one dword of
+// codes: 8 rows x 16 bytes are neighbours in a fragment.
+// VEC: 16-byte loads (base, row pitch and K allow them up to the last block).
+// ---------------------------------------------------------------------------
+template <bool BF>
+__device__ __forceinline__ void load8(const void *row, int64_t k, float *v, uint32_t *w, bool vec,
+                                      int64_t K)
+{
+    if (vec && k + 8 <= K) {
+        if constexpr (BF) {
+            const uint4 q = *(const uint4 *)((const uint16_t *)row + k);
+            w[0] = q.x;
+            w[1] = q.y;
+            w[2] = q.z;
+            w[3] = q.w;
+        } else {
+            const float4 p = *(const float4 *)((const float *)row + k);
+            const float4 q = *(const float4 *)((const float *)row + k + 4);
+            v[0] = p.x;
+            v[1] = p.y;
+            v[2] = p.z;
+            v[3] = p.w;
+            v[4] = q.x;
+            v[5] = q.y;
+            v[6] = q.z;
+            v[7] = q.w;
+        }
+    } else if constexpr (BF) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const uint16_t *p = (const uint16_t *)row + k + 2 * e;
+            const uint32_t lo = k + 2 * e < K ? p[0] : 0, hi = k + 2 * e + 1 < K ? p[1] : 0;
+            w[e] = lo | hi << 16;
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = k + e < K ? ((const float *)row)[k + e] : 0.0f;
+    }
+}
+
+// the largest magnitude of eight values, as fp32 bits
+template <bool BF>
+__device__ __forceinline__ uint32_t top8(const float *v, const uint32_t *w)
+{
+    if constexpr (BF) {
+        uint32_t m = w[0] & 0x7FFF7FFFu;
+#pragma unroll
+        for (int e = 1; e < 4; ++e) m = max_u16(m, w[e] & 0x7FFF7FFFu);
+        const uint32_t hi = m >> 16, lo = m & 0xFFFFu;
+        return (hi > lo ? hi : lo) << 16;
+    } else {
+        uint32_t m = 0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const uint32_t b = __float_as_uint(v[e]) & 0x7FFFFFFFu;
+            m = b > m ? b : m;
+        }
+        return m;
+    }
+}
+
+__device__ __forceinline__ uint32_t max_of_four_lanes(uint32_t m)
+{
+    // quad_perm [1,0,3,2], then [2,3,0,1]
+    uint32_t o = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)m, 0xB1, 0xF, 0xF, true);
+    m = o > m ? o : m;
+    o = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)m, 0x4E, 0xF, 0xF, true);
+    return o > m ? o : m;
+}
+
+template <bool BF>
+__global__ __launch_bounds__(256) void mx4_quantize_rows_kernel(const void *x, int64_t ld,
+                                                                Mx4Layout L, uint8_t *dst,
+                                                                int vec)
+{
+    const int wv = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    const int64_t rt = blockIdx.x / (uint32_t)L.groups, g = blockIdx.x - rt * L.groups;
+    const int rr = 8 * wv + (lane >> 3), q = lane & 7;      // row of the tile, eighth of the k-step
+    const int64_t row = rt * 32 + rr;
+    const bool in = row < L.rows;
+    const char *src = (const char *)x + (in ? row : 0) * ld * (BF ? 2 : 4);
+    float v[4][8];
+    uint32_t w[4][4];
+#pragma unroll
+    for (int s = 0; s < 4; ++s) load8<BF>(src, (g * 4 + s) * 64 + q * 8, v[s], w[s], vec, in ? L.K : 0);
+    uint32_t scales = 0;
+    // lane of the fragment: row + 32 * half; its dword: eighth % 4
+    const int fl = rr + 32 * (q >> 2);
+#pragma unroll
+    for (int s = 0; s < 4; ++s) {
+        const int64_t ks = g * 4 + s;
+        const uint32_t top = max_of_four_lanes(top8<BF>(v[s], w[s]));
+        const bool empty = !in || ks * 64 + (q >> 2) * 32 >= L.K;   // no element at all
+        const uint32_t byte = empty ? 127u : scale_byte(top);
+        scales |= byte << (8 * s);
+        uint32_t code;
+        if constexpr (BF) code = codes_of_bf16(w[s], scale_value(byte));
+        else code = codes_of(v[s], scale_value(byte));
+        if (byte == 255) code = 0x22222222u;                        // ones of a NaN scale
+        if (ks < L.ksteps)
+            *(uint32_t *)(dst + ((rt * L.ksteps + ks) * 64 + fl) * 16 + (q & 3) * 4) = code;
+    }
+    if ((q & 3) == 0) *(uint32_t *)(dst + L.off_scales + ((rt * L.groups + g) * 64 + fl) * 4) = scales;
+}
+
+// ---------------------------------------------------------------------------
+// columns in memory (element (row, k) at row + k ld): a lane takes V rows and
+// walks down k, so a block needs no other lane; a wave has 64 V rows and one
+// group of 4 k-steps.
+// ---------------------------------------------------------------------------
+template <bool BF, int V>
+__global__ __launch_bounds__(256) void mx4_quantize_cols_kernel(const char *x, int64_t ld,
+                                                                Mx4Layout L, uint8_t *dst)
+{
+    constexpr int ES = BF ? 2 : 4;
+    const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    const uint32_t strips = (uint32_t)(L.tiles * 32 + 64 * V - 1) / (64 * V);
+    const uint32_t unit = blockIdx.x * 4 + wv, g = unit / strips;
+    if (g >= L.groups) return;
+    const uint32_t row0 = (unit - g * strips) * 64 * V + lane * V;
+    if (row0 >= L.tiles * 32) return;
+    // (V divides the number of rows: a lane's rows are all in or all out)
+    const bool in = row0 < L.rows;
+    const uint32_t off = (uint32_t)(in ? row0 : L.rows - V) * ES;
+    uint32_t scales[V][2];
+#pragma unroll
+    for (int e = 0; e < V; ++e) scales[e][0] = scales[e][1] = 0;
+#pragma unroll 1
+    for (int b = 0; b < 8; ++b) {
+        const int64_t k0 = (int64_t)g * 256 + b * 32;
+        float v[V][32];
+#pragma unroll
+        for (int j = 0; j < 32; ++j) {
+            const int64_t k = k0 + j < L.K ? k0 + j : L.K - 1;
+            const char *p = scalar(x + k * ld * ES) + (size_t)off;
+            if constexpr (BF && V == 2) {
+                const uint32_t w = *(const uint32_t *)p;
+                v[0][j] = __uint_as_float(w << 16);
+                v[1][j] = __uint_as_float(w & 0xFFFF0000u);
+            } else if constexpr (BF) {
+                v[0][j] = __uint_as_float((uint32_t) * (const uint16_t *)p << 16);
+            } else if constexpr (V == 2) {
+                const float2 w = *(const float2 *)p;
+                v[0][j] = w.x;
+                v[1][j] = w.y;
+            } else {
+                v[0][j] = *(const float *)p;
+            }
+        }
+        const int valid = !in || k0 >= L.K ? 0 : L.K - k0 < 32 ? (int)(L.K - k0) : 32;
+        const uint32_t ks = g * 4 + (b >> 1);
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+            const uint32_t row = row0 + e;
+            uint32_t top = 0;
+#pragma unroll
+            for (int j = 0; j < 32; ++j) {
+                v[e][j] = j < valid ? v[e][j] : 0.0f;
+                const uint32_t m = __float_as_uint(v[e][j]) & 0x7FFFFFFFu;
+                top = m > top ? m : top;
+            }
+            const uint32_t byte = valid == 0 ? 127u : scale_byte(top);
+            const float sc = scale_value(byte);
+            uint4 code;
+            code.x = codes_of(&v[e][0], sc);
+            code.y = codes_of(&v[e][8], sc);
+            code.z = codes_of(&v[e][16], sc);
+            code.w = codes_of(&v[e][24], sc);
+            if (byte == 255) code = make_uint4(0x22222222u, 0x22222222u, 0x22222222u, 0x22222222u);
+            scales[e][b & 1] |= byte << (8 * (b >> 1));
+            const uint32_t fl = (row & 31) + 32 * (b & 1);
+            if (ks < L.ksteps)
+                *(uint4 *)(dst + (((int64_t)(row >> 5) * L.ksteps + ks) * 64 + fl) * 16) = code;
+        }
+    }
+#pragma unroll
+    for (int e = 0; e < V; ++e)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const uint32_t row = row0 + e, fl = (row & 31) + 32 * h;
+            *(uint32_t *)(dst + L.off_scales +
+                          (((int64_t)(row >> 5) * L.groups + g) * 64 + fl) * 4) = scales[e][h];
+        }
+}
+
+// ---------------------------------------------------------------------------
+// back to rows: the places of mx4_quantize_rows_kernel
+// ---------------------------------------------------------------------------
+template <bool BF>
+__global__ __launch_bounds__(256) void mx4_dequantize_kernel(const uint8_t *src, Mx4Layout L,
+                                                             void *y, int64_t ld, int vec)
+{
+    const int wv = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    const int64_t rt = blockIdx.x / (uint32_t)L.groups, g = blockIdx.x - rt * L.groups;
+    const int rr = 8 * wv + (lane >> 3), q = lane & 7, fl = rr + 32 * (q >> 2);
+    const int64_t row = rt * 32 + rr;
+    if (row >= L.rows) return;
+    const uint32_t scales = *(const uint32_t *)(src + L.off_scales + ((rt * L.groups + g) * 64 + fl) * 4);
+#pragma unroll
+    for (int s = 0; s < 4; ++s) {
+        const int64_t ks = g * 4 + s, k = ks * 64 + q * 8;
+        if (k >= L.K) continue;
+        const uint32_t c = *(const uint32_t *)(src + ((rt * L.ksteps + ks) * 64 + fl) * 16 + (q & 3) * 4);
+        const float sc = scale_value(scales >> (8 * s) & 255u);
+        float v[8];
+        floatx2 p = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, 1.0f, 0);
+        v[0] = p[0];
+        v[1] = p[1];
+        p = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, 1.0f, 1);
+        v[2] = p[0];
+        v[3] = p[1];
+        p = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, 1.0f, 2);
+        v[4] = p[0];
+        v[5] = p[1];
+        p = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, 1.0f, 3);
+        v[6] = p[0];
+        v[7] = p[1];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] *= sc;
+        if constexpr (BF) {
+            __bf16 *out = (__bf16 *)y + row * ld + k;
+            __bf16 w[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) w[e] = to_bf16(v[e]);   // exact: two significant bits
+            if (vec && k + 8 <= L.K) {
+                __builtin_memcpy(__builtin_assume_aligned(out, 16), w, 16);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (k + e < L.K) out[e] = w[e];
+            }
+        } else {
+            float *out = (float *)y + row * ld + k;
+            if (vec && k + 8 <= L.K) {
+                *(float4 *)out = make_float4(v[0], v[1], v[2], v[3]);
+                *(float4 *)(out + 4) = make_float4(v[4], v[5], v[6], v[7]);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (k + e < L.K) out[e] = v[e];
+            }
+        }
+    }
+}
+
+bool vec16(const void *p, int64_t ld, int es) { return ((uintptr_t)p | (uint64_t)(ld * es)) % 16 == 0; }
+
+}  // namespace
+
+Mx4Layout mx4_layout(int64_t rows, int64_t K)
+{
+    Mx4Layout L;
+    L.rows = rows;
+    L.K = K;
+    L.tiles = (rows + 31) / 32;
+    L.ksteps = (K + 63) / 64;
+    L.groups = (L.ksteps + 3) / 4;
+    L.off_scales = L.tiles * L.ksteps * 1024;
+    L.total = (size_t)(L.off_scales + L.tiles * L.groups * 256);
+    return L;
+}
+
+hipError_t launch_mx4_quantize(const void *x, bool bf16, int64_t row_stride, int64_t col_stride,
+                               const Mx4Layout &L, void *dst, hipStream_t s)
+{
+    if (col_stride == 1) {
+        const dim3 grid((unsigned)(L.tiles * L.groups));
+        const int vec = vec16(x, row_stride, bf16 ? 2 : 4);
+        if (bf16)
+            hipLaunchKernelGGL(mx4_quantize_rows_kernel<true>, grid, dim3(256), 0, s, x, row_stride,
+                               L, (uint8_t *)dst, vec);
+        else
+            hipLaunchKernelGGL(mx4_quantize_rows_kernel<false>, grid, dim3(256), 0, s, x,
+                               row_stride, L, (uint8_t *)dst, vec);
+        return hipGetLastError();
+    }
+    // two rows a lane where every pair is aligned
+    const int es = bf16 ? 2 : 4;
+    const bool two = L.rows >= 128 && L.rows % 2 == 0 &&
+                     ((uintptr_t)x | (uint64_t)(col_stride * es)) % (2 * es) == 0;
+    const int64_t strips = (L.tiles * 32 + (two ? 127 : 63)) / (two ? 128 : 64);
+    const dim3 grid((unsigned)((strips * L.groups + 3) / 4));
+    void (*kernel)(const char *, int64_t, Mx4Layout, uint8_t *) =
+        bf16 ? (two ? mx4_quantize_cols_kernel<true, 2> : mx4_quantize_cols_kernel<true, 1>)
+             : (two ? mx4_quantize_cols_kernel<false, 2> : mx4_quantize_cols_kernel<false, 1>);
+    hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, (const char *)x, col_stride, L,
+                       (uint8_t *)dst);
+    return hipGetLastError();
+}
+
+hipError_t launch_mx4_dequantize(const void *src, const Mx4Layout &L, void *y, bool bf16,
+                                 int64_t ld, hipStream_t s)
+{
+    const dim3 grid((unsigned)(L.tiles * L.groups));
+    const int vec = vec16(y, ld, bf16 ? 2 : 4);
+    if (bf16)
+        hipLaunchKernelGGL(mx4_dequantize_kernel<true>, grid, dim3(256), 0, s, (const uint8_t *)src,
+                           L, y, ld, vec);
+    else
+        hipLaunchKernelGGL(mx4_dequantize_kernel<false>, grid, dim3(256), 0, s,
+                           (const uint8_t *)src, L, y, ld, vec);
+    return hipGetLastError();
+}
+
+}  // namespace tpk

@@ -240,14 +240,6 @@ __device__ __forceinline__ uint32_t done_bits(uint8_t flag, int nv)
     return (uint32_t)__ballot(flag != 0) & ((1u << nv) - 1u);
 }
 
-// keeps a row's address in scalar registers (the compiler otherwise adds the
-// lane's offset first and steps one 64-bit vector address per row)
-__device__ __forceinline__ char *scalar(char *p)
-{
-    asm("" : "+s"(p));
-    return p;
-}
-
 __device__ __forceinline__ char *row_at(const RecurRows &m, int b, int t)
 {
     return (char *)m.p + (m.st * t + m.sb * b);

@@ -22,6 +22,7 @@ LIB_PATH = os.environ.get("TP_LIB_PATH") or os.path.join(HERE, "libtp.so")
 
 TP_OK, TP_EINVAL, TP_ERANGE, TP_EUNSUPPORTED, TP_EHIP = 0, -1, -2, -3, -4
 TP_F32, TP_BF16 = 0, 1
+TP_ACT_NONE, TP_ACT_TANH = 0, 1
 _NAMES = {TP_EINVAL: "TP_EINVAL", TP_ERANGE: "TP_ERANGE",
           TP_EUNSUPPORTED: "TP_EUNSUPPORTED", TP_EHIP: "TP_EHIP"}
 
@@ -87,6 +88,10 @@ class Rows(C.Structure):
     _fields_ = [("p", C.c_void_p), ("st", C.c_int64), ("sb", C.c_int64)]
 
 
+class Mx4(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("rows", C.c_int64), ("K", C.c_int64)]
+
+
 EXPORTS = ("tp_env_reset", "tp_env_step", "tp_actor_packed_bytes",
            "tp_actor_pack", "tp_rollout", "tp_gae", "tp_critic_packed_bytes",
            "tp_critic_pack", "tp_critic_value", "tp_backtest_metrics",
@@ -98,7 +103,8 @@ EXPORTS = ("tp_env_reset", "tp_env_step", "tp_actor_packed_bytes",
            "tp_actor_release", "tp_critic_release", "tp_check_starts",
            "tp_backtest_metrics_noalloc",
            "tp_recur_saved_bytes", "tp_recur_workspace_bytes", "tp_recur_forward",
-           "tp_recur_backward", "tp_recur_step",
+           "tp_recur_backward", "tp_recur_step", "tp_mx4_bytes", "tp_mx4_quantize",
+           "tp_mx4_dequantize", "tp_mx4_workspace_bytes", "tp_mx4_matmul", "tp_mx4_linear",
            "tp_last_error", "tp_version")
 
 _lib = None
@@ -156,6 +162,14 @@ def load(path: str = LIB_PATH):
     L.tp_recur_forward.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
     L.tp_recur_backward.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
     L.tp_recur_step.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp]
+    L.tp_mx4_bytes.restype = sz
+    L.tp_mx4_bytes.argtypes = [i64, i64]
+    L.tp_mx4_workspace_bytes.restype = sz
+    L.tp_mx4_workspace_bytes.argtypes = [i64, i64, i64]
+    L.tp_mx4_quantize.argtypes = [vp, i32, i64, i64, vp, vp]
+    L.tp_mx4_dequantize.argtypes = [vp, vp, i32, i64, vp]
+    L.tp_mx4_matmul.argtypes = [vp, vp, vp, i32, vp, i32, i64, vp, sz, vp]
+    L.tp_mx4_linear.argtypes = [vp, i32, i64, i64, vp, vp, i32, vp, i32, i64, vp, sz, vp]
     L.tp_last_error.restype = C.c_char_p
     L.tp_version.restype = C.c_int
     for f in ("tp_env_reset", "tp_env_step", "tp_actor_pack", "tp_rollout", "tp_gae",
@@ -164,7 +178,8 @@ def load(path: str = LIB_PATH):
               "tp_ppo_update", "tp_ppo_update_agents", "tp_minibatch_rows",
               "tp_actor_release", "tp_critic_release", "tp_check_starts",
               "tp_backtest_metrics_noalloc", "tp_recur_forward", "tp_recur_backward",
-              "tp_recur_step"):
+              "tp_recur_step", "tp_mx4_quantize", "tp_mx4_dequantize", "tp_mx4_matmul",
+              "tp_mx4_linear"):
         getattr(L, f).restype = C.c_int
     _lib = L
     return L
@@ -726,3 +741,93 @@ def recur_step(x, r, i, lam, h, h_out, y=None, done=None, stream=None):
 
     _check(load().tp_recur_step(C.byref(s), rows(x), rows(r), rows(i), _ptr(h), _ptr(h_out),
                                 None if y is None else rows(y), _stream(stream)))
+
+
+# --------------------------------------------------------------------------
+# 4-bit matrices
+# --------------------------------------------------------------------------
+
+class Mx4T:
+    """A matrix [rows][K] in 4 bits (see tp_mx4); its bytes are opaque."""
+
+    def __init__(self, data: torch.Tensor, rows: int, K: int):
+        assert data.dtype == torch.uint8 and data.is_contiguous()
+        assert data.numel() >= mx4_bytes(rows, K)
+        self.data, self.rows, self.K = data, rows, K
+        self.s = Mx4(_ptr(data), rows, K)
+
+    @staticmethod
+    def empty(rows: int, K: int, device="cuda"):
+        return Mx4T(torch.empty(mx4_bytes(rows, K), dtype=torch.uint8, device=device), rows, K)
+
+
+def mx4_bytes(rows: int, K: int) -> int:
+    nb = load().tp_mx4_bytes(rows, K)
+    if nb == 0:
+        raise TPError(TP_EINVAL, last_error())
+    return nb
+
+
+def _matrix(t: torch.Tensor):
+    assert t.dim() == 2 and t.dtype in (torch.float32, torch.bfloat16)
+    return t.data_ptr(), _dtype_code(t)
+
+
+def mx4_quantize(x: torch.Tensor, out: Mx4T | None = None, stream=None) -> Mx4T:
+    """x [rows][K] (fp32 or bf16, one stride of 1: transposed views too) in 4
+    bits."""
+    p, dt = _matrix(x)
+    if out is None:
+        out = Mx4T.empty(x.shape[0], x.shape[1], x.device)
+    assert x.shape == (out.rows, out.K)
+    _check(load().tp_mx4_quantize(p, dt, x.stride(0), x.stride(1), C.byref(out.s),
+                                  _stream(stream)))
+    return out
+
+
+def mx4_dequantize(m: Mx4T, y: torch.Tensor, stream=None):
+    """The values of m into y [rows][K]."""
+    p, dt = _matrix(y)
+    assert y.shape == (m.rows, m.K) and (m.K == 1 or y.stride(1) == 1)
+    _check(load().tp_mx4_dequantize(C.byref(m.s), p, dt, _pitch(y), _stream(stream)))
+
+
+def _pitch(t: torch.Tensor) -> int:
+    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+
+
+def mx4_workspace(M: int, N: int, K: int, device="cuda") -> torch.Tensor:
+    nb = load().tp_mx4_workspace_bytes(M, N, K)
+    if nb == 0:
+        raise TPError(TP_EINVAL, last_error())
+    return torch.empty(nb, dtype=torch.uint8, device=device)
+
+
+def mx4_matmul(a: Mx4T, w: Mx4T, y: torch.Tensor, bias: torch.Tensor | None = None,
+               act: int = TP_ACT_NONE, work: torch.Tensor | None = None, stream=None):
+    """y [M][N] = act(a w^T + bias) of 4-bit a [M][K] and w [N][K]."""
+    if work is None:
+        work = mx4_workspace(a.rows, w.rows, a.K, y.device)
+    p, dt = _matrix(y)
+    assert y.shape == (a.rows, w.rows) and (w.rows == 1 or y.stride(1) == 1)
+    assert bias is None or (bias.shape == (w.rows,) and bias.dtype == torch.float32
+                            and bias.is_contiguous())
+    _check(load().tp_mx4_matmul(C.byref(a.s), C.byref(w.s), _ptr(bias), act, p, dt, _pitch(y),
+                                _ptr(work), work.numel(), _stream(stream)))
+
+
+def mx4_linear(x: torch.Tensor, w: Mx4T, y: torch.Tensor, bias: torch.Tensor | None = None,
+               act: int = TP_ACT_NONE, work: torch.Tensor | None = None, stream=None):
+    """y [M][N] = act(x4 w^T + bias): a layer on 4-bit weights w [N][K]; x4 is x
+    [M][K] in 4 bits."""
+    M = x.shape[0]
+    if work is None:
+        work = mx4_workspace(M, w.rows, w.K, y.device)
+    px, dx = _matrix(x)
+    p, dt = _matrix(y)
+    assert x.shape == (M, w.K) and (w.K == 1 or x.stride(1) == 1)
+    assert y.shape == (M, w.rows) and (w.rows == 1 or y.stride(1) == 1)
+    assert bias is None or (bias.shape == (w.rows,) and bias.dtype == torch.float32
+                            and bias.is_contiguous())
+    _check(load().tp_mx4_linear(px, dx, M, _pitch(x), C.byref(w.s), _ptr(bias), act, p, dt,
+                                _pitch(y), _ptr(work), work.numel(), _stream(stream)))
