@@ -1,0 +1,126 @@
+"""A policy's memory over bars: the stored observations of a rollout, or one bar of a live loop,
+through a product with 4-bit weights and a gated linear recurrence.
+
+  gates [T][B][3 D] = obs [T][B][S] W^T      tp.mx4_linear   (x, r, i side by side)
+  y, h              = recurrence(x, r, i)    tp.recur_forward, one bar: tp.recur_step
+
+and back: tp.recur_backward gives the gates' gradient and lambda's; W's is the product of the
+gates' gradient and the observations over all T B rows, both in 4 bits (tp.mx4_quantize of
+transposed views, tp.mx4_matmul).  The fp32 master of W is kept and taken to 4 bits again after an
+optimiser's step; the rounding to 4 bits counts as the identity in the gradient.
+
+obs and done are what tp.rollout stores (tp.TrajT.obs, .done).  Plumbing only (buffers and the
+order of calls); `python -m paper_2111_05188_amd.memory` trains a layer to remember.
+"""
+
+from __future__ import annotations
+
+import torch
+
+from . import tp
+
+
+class MemoryLayer:
+    """D channels over observations of S features.  W [3 D][S] fp32, lam [D] fp32."""
+
+    def __init__(self, W: torch.Tensor, lam: torch.Tensor, dtype=torch.bfloat16):
+        self.D, self.S = lam.shape[0], W.shape[1]
+        assert W.shape == (3 * self.D, self.S) and W.dtype == lam.dtype == torch.float32
+        self.W, self.lam, self.dtype = W, lam, dtype
+        self.w4 = tp.mx4_quantize(W)
+        self.rc = None
+
+    @staticmethod
+    def init(S: int, D: int, seed: int = 0, dtype=torch.bfloat16, device="cuda"):
+        """W ~ N(0, 1/S); memories of 10 to 1,000 bars at an open gate of one half."""
+        g = torch.Generator(device=device).manual_seed(seed)
+        W = torch.randn(3 * D, S, generator=g, device=device) * S ** -0.5
+        a = 1.0 - 10.0 ** -torch.linspace(1.0, 3.0, D, device=device)
+        return MemoryLayer(W, torch.log(torch.expm1(-torch.log(a) / 4.0)), dtype)
+
+    def parts(self, gates):
+        D = self.D
+        return gates[..., :D], gates[..., D:2 * D], gates[..., 2 * D:]
+
+    def _sequence(self, T: int, B: int, done, lens):
+        """Buffers of sequences of this size (kept while the size stays)."""
+        dev, D = self.lam.device, self.D
+        if self.rc is None or (self.rc.T, self.rc.B) != (T, B):
+            new = lambda *s, dt=self.dtype: torch.empty(s, dtype=dt, device=dev)  # noqa: E731
+            self.gates, self.y = new(T, B, 3 * D), new(T, B, D)
+            self.dgates, self.h_last = new(T, B, 3 * D), new(B, D, dt=torch.float32)
+            self.dlam, self.dh0 = new(D, dt=torch.float32), new(B, D, dt=torch.float32)
+            self.dW = new(3 * D, self.S, dt=torch.float32)
+            rc = tp.RecurT(self.lam, T, B, self.dtype)
+            self.work, self.saved = rc.workspace(), rc.saved()
+            self.work4 = tp.mx4_workspace(T * B, 3 * D, self.S, dev)
+            self.workW = tp.mx4_workspace(3 * D, self.S, T * B, dev)
+            self.dg4, self.obs4 = tp.Mx4T.empty(3 * D, T * B, dev), tp.Mx4T.empty(self.S, T * B, dev)
+        self.rc = tp.RecurT(self.lam, T, B, self.dtype, done=done, lens=lens)
+
+    def encode(self, obs, done=None, lens=None, h0=None, stream=None):
+        """y [T][B][D] and the last states [B][D] of stored observations [T][B][ld] (ld >= S;
+        rows follow one another); done [T][B] and lens [B] as tp.recur_forward."""
+        T, B, ld = obs.shape
+        self._sequence(T, B, done, lens)
+        self.rows = obs.reshape(T * B, ld)[:, :self.S]
+        tp.mx4_linear(self.rows, self.w4, self.gates.view(T * B, -1), work=self.work4,
+                      stream=stream)
+        tp.recur_forward(self.rc, *self.parts(self.gates), self.y, self.work, h0=h0,
+                         h_last=self.h_last, saved=self.saved, stream=stream)
+        return self.y, self.h_last
+
+    def gradients(self, dy, dh_last=None, stream=None):
+        """Gradients of the last encode's W, lambda and first states, from dy [T][B][D]."""
+        tp.recur_backward(self.rc, *self.parts(self.gates), self.saved, dy,
+                          *self.parts(self.dgates), self.dlam, self.work, dh_last=dh_last,
+                          dh0=self.dh0, stream=stream)
+        n = self.rc.T * self.rc.B
+        tp.mx4_quantize(self.dgates.view(n, -1).t(), self.dg4, stream=stream)
+        tp.mx4_quantize(self.rows.t(), self.obs4, stream=stream)
+        tp.mx4_matmul(self.dg4, self.obs4, self.dW, work=self.workW, stream=stream)
+        return self.dW, self.dlam, self.dh0
+
+    def refresh(self, stream=None):
+        """The weights in 4 bits again, after an optimiser has changed W."""
+        tp.mx4_quantize(self.W, self.w4, stream=stream)
+
+    def step(self, obs, h, done=None, stream=None):
+        """One bar: y [B][D] of observations [B][ld]; the states h [B][D] move on in place."""
+        B = obs.shape[0]
+        gates = torch.empty(B, 3 * self.D, dtype=self.dtype, device=obs.device)
+        y = torch.empty(B, self.D, dtype=self.dtype, device=obs.device)
+        if getattr(self, "work1", None) is None or self.work1[0] != B:
+            self.work1 = (B, tp.mx4_workspace(B, 3 * self.D, self.S, obs.device))
+        tp.mx4_linear(obs[:, :self.S], self.w4, gates, work=self.work1[1], stream=stream)
+        tp.recur_step(*self.parts(gates), self.lam, h, h, y, done=done, stream=stream)
+        return y
+
+
+def train_to_remember(T=96, B=64, S=31, D=64, steps=300, lr=0.02, seed=0):
+    """Teach a layer's first channel the mean of the last 20 bars of the first feature, over two
+    episodes a sequence.  The losses, as shares of the target's own mean square."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    layer = MemoryLayer.init(S, D, seed, torch.float32)
+    opt = torch.optim.Adam([layer.W, layer.lam], lr=lr)
+    obs = torch.randn(T, B, -(-S // 32) * 32, generator=g, device="cuda")
+    half = T // 2
+    done = torch.zeros(T, B, dtype=torch.uint8, device="cuda")
+    done[half - 1] = 1
+    want = torch.stack([obs[max(t - t % half, t - 19):t + 1, :, 0].sum(0)
+                        for t in range(T)]) / 20
+    dy, losses = torch.zeros(T, B, D, device="cuda"), []
+    for _ in range(steps):
+        y, _ = layer.encode(obs, done)
+        off = y[..., 0] - want
+        losses.append(float(off.square().sum() / want.square().sum()))
+        dy[..., 0] = off
+        layer.W.grad, layer.lam.grad, _ = layer.gradients(dy)
+        opt.step()
+        layer.refresh()
+    return losses
+
+
+if __name__ == "__main__":
+    seen = train_to_remember()
+    print(f"error {seen[0]:.3f} -> {seen[-1]:.3f} of the target's mean square in {len(seen)} updates")
