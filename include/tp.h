@@ -640,7 +640,7 @@ typedef struct tp_mx4 {
 typedef enum { TP_ACT_NONE = 0, TP_ACT_TANH = 1 } tp_act;
 
 /* Bytes of a 4-bit matrix (about rows * K * 17/32, rows rounded up to 32, K
- * to 64); 0 for bad sizes. */
+ * to 256); 0 for bad sizes. */
 size_t tp_mx4_bytes(int64_t rows, int64_t K);
 
 /*

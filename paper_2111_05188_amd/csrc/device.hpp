@@ -159,13 +159,34 @@ __device__ __forceinline__ void wave_lds_fence()
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
 
-// Keeps an address in scalar registers (the compiler otherwise adds the lane's
-// offset first and steps one 64-bit vector address per row).
-template <class P>
-__device__ __forceinline__ P *scalar(P *p)
+// Barrier of a workgroup that orders its LDS accesses alone: loads and stores
+// of global memory stay in flight across it.
+__device__ __forceinline__ void workgroup_lds_barrier()
 {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+
+// One access at a wave's base address plus a lane's offset in bytes.  The base
+// is kept in scalar registers: the compiler otherwise adds the lane's offset
+// first and steps a 64-bit vector address per access.
+#define TP_GLOBAL __attribute__((address_space(1)))
+
+template <class T>
+__device__ __forceinline__ T load_at(const void *base, uint32_t off)
+{
+    const TP_GLOBAL char *p = (const TP_GLOBAL char *)base;
     asm("" : "+s"(p));
-    return p;
+    return *(const TP_GLOBAL T *)(p + off);
+}
+
+template <class T>
+__device__ __forceinline__ void store_at(void *base, uint32_t off, T v)
+{
+    TP_GLOBAL char *p = (TP_GLOBAL char *)base;
+    asm("" : "+s"(p));
+    *(TP_GLOBAL T *)(p + off) = v;
 }
 
 // Sum over the 64 lanes (same value returned to every lane).

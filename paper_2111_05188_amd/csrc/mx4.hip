@@ -12,63 +12,6 @@ namespace {
 // codes: 8 rows x 16 bytes are neighbours in a fragment.
 // VEC: 16-byte loads (base, row pitch and K allow them up to the last block).
 // ---------------------------------------------------------------------------
-template <bool BF>
-__device__ __forceinline__ void load8(const void *row, int64_t k, float *v, uint32_t *w, bool vec,
-                                      int64_t K)
-{
-    if (vec && k + 8 <= K) {
-        if constexpr (BF) {
-            const uint4 q = *(const uint4 *)((const uint16_t *)row + k);
-            w[0] = q.x;
-            w[1] = q.y;
-            w[2] = q.z;
-            w[3] = q.w;
-        } else {
-            const float4 p = *(const float4 *)((const float *)row + k);
-            const float4 q = *(const float4 *)((const float *)row + k + 4);
-            v[0] = p.x;
-            v[1] = p.y;
-            v[2] = p.z;
-            v[3] = p.w;
-            v[4] = q.x;
-            v[5] = q.y;
-            v[6] = q.z;
-            v[7] = q.w;
-        }
-    } else if constexpr (BF) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const uint16_t *p = (const uint16_t *)row + k + 2 * e;
-            const uint32_t lo = k + 2 * e < K ? p[0] : 0, hi = k + 2 * e + 1 < K ? p[1] : 0;
-            w[e] = lo | hi << 16;
-        }
-    } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = k + e < K ? ((const float *)row)[k + e] : 0.0f;
-    }
-}
-
-// the largest magnitude of eight values, as fp32 bits
-template <bool BF>
-__device__ __forceinline__ uint32_t top8(const float *v, const uint32_t *w)
-{
-    if constexpr (BF) {
-        uint32_t m = w[0] & 0x7FFF7FFFu;
-#pragma unroll
-        for (int e = 1; e < 4; ++e) m = max_u16(m, w[e] & 0x7FFF7FFFu);
-        const uint32_t hi = m >> 16, lo = m & 0xFFFFu;
-        return (hi > lo ? hi : lo) << 16;
-    } else {
-        uint32_t m = 0;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const uint32_t b = __float_as_uint(v[e]) & 0x7FFFFFFFu;
-            m = b > m ? b : m;
-        }
-        return m;
-    }
-}
-
 __device__ __forceinline__ uint32_t max_of_four_lanes(uint32_t m)
 {
     // quad_perm [1,0,3,2], then [2,3,0,1]
@@ -107,8 +50,7 @@ __global__ __launch_bounds__(256) void mx4_quantize_rows_kernel(const void *x, i
         if constexpr (BF) code = codes_of_bf16(w[s], scale_value(byte));
         else code = codes_of(v[s], scale_value(byte));
         if (byte == 255) code = 0x22222222u;                        // ones of a NaN scale
-        if (ks < L.ksteps)
-            *(uint32_t *)(dst + ((rt * L.ksteps + ks) * 64 + fl) * 16 + (q & 3) * 4) = code;
+        *(uint32_t *)(dst + ((rt * L.ksteps + ks) * 64 + fl) * 16 + (q & 3) * 4) = code;
     }
     if ((q & 3) == 0) *(uint32_t *)(dst + L.off_scales + ((rt * L.groups + g) * 64 + fl) * 4) = scales;
 }
@@ -142,19 +84,19 @@ __global__ __launch_bounds__(256) void mx4_quantize_cols_kernel(const char *x, i
 #pragma unroll
         for (int j = 0; j < 32; ++j) {
             const int64_t k = k0 + j < L.K ? k0 + j : L.K - 1;
-            const char *p = scalar(x + k * ld * ES) + (size_t)off;
+            const char *p = x + k * ld * ES;
             if constexpr (BF && V == 2) {
-                const uint32_t w = *(const uint32_t *)p;
+                const uint32_t w = load_at<uint32_t>(p, off);
                 v[0][j] = __uint_as_float(w << 16);
                 v[1][j] = __uint_as_float(w & 0xFFFF0000u);
             } else if constexpr (BF) {
-                v[0][j] = __uint_as_float((uint32_t) * (const uint16_t *)p << 16);
+                v[0][j] = __uint_as_float((uint32_t)load_at<uint16_t>(p, off) << 16);
             } else if constexpr (V == 2) {
-                const float2 w = *(const float2 *)p;
-                v[0][j] = w.x;
-                v[1][j] = w.y;
+                const floatx2 w = load_at<floatx2>(p, off);
+                v[0][j] = w[0];
+                v[1][j] = w[1];
             } else {
-                v[0][j] = *(const float *)p;
+                v[0][j] = load_at<float>(p, off);
             }
         }
         const int valid = !in || k0 >= L.K ? 0 : L.K - k0 < 32 ? (int)(L.K - k0) : 32;
@@ -179,8 +121,7 @@ __global__ __launch_bounds__(256) void mx4_quantize_cols_kernel(const char *x, i
             if (byte == 255) code = make_uint4(0x22222222u, 0x22222222u, 0x22222222u, 0x22222222u);
             scales[e][b & 1] |= byte << (8 * (b >> 1));
             const uint32_t fl = (row & 31) + 32 * (b & 1);
-            if (ks < L.ksteps)
-                *(uint4 *)(dst + (((int64_t)(row >> 5) * L.ksteps + ks) * 64 + fl) * 16) = code;
+            *(uint4 *)(dst + (((int64_t)(row >> 5) * L.ksteps + ks) * 64 + fl) * 16) = code;
         }
     }
 #pragma unroll
@@ -263,8 +204,8 @@ Mx4Layout mx4_layout(int64_t rows, int64_t K)
     L.rows = rows;
     L.K = K;
     L.tiles = (rows + 31) / 32;
-    L.ksteps = (K + 63) / 64;
-    L.groups = (L.ksteps + 3) / 4;
+    L.groups = (K + 255) / 256;
+    L.ksteps = 4 * L.groups;
     L.off_scales = L.tiles * L.ksteps * 1024;
     L.total = (size_t)(L.off_scales + L.tiles * L.groups * 256);
     return L;

@@ -9,7 +9,8 @@
 //   scales [row tile][group of 4 k-steps][64 lanes][4 bytes]: byte s is the
 //          scale of lane l's block in k-step s of the group (2^(byte - 127)),
 //          so the instruction picks a k-step's scale by its byte select.
-// Rows and elements past the matrix are zeros of scale 1.
+// Rows and elements past the matrix are zeros of scale 1, up to whole tiles and
+// groups, so that no reader has a partial one.
 #pragma once
 
 #include "device.hpp"
@@ -18,6 +19,7 @@
 namespace tpk {
 
 typedef int intx4 __attribute__((ext_vector_type(4)));
+typedef uint32_t uintx4 __attribute__((ext_vector_type(4)));
 typedef int intx8 __attribute__((ext_vector_type(8)));
 typedef float floatx16 __attribute__((ext_vector_type(16)));
 typedef float floatx2 __attribute__((ext_vector_type(2)));
@@ -83,6 +85,65 @@ __device__ __forceinline__ uint32_t max_u16(uint32_t a, uint32_t b)
     x = __builtin_elementwise_max(x, y);
     __builtin_memcpy(&a, &x, 4);
     return a;
+}
+
+// Eight elements k .. k + 7 of a row of K, zeros past it: fp32 in v, bf16
+// pairs in w.  vec: rows are 16-byte aligned.
+template <bool BF>
+__device__ __forceinline__ void load8(const void *row, int64_t k, float *v, uint32_t *w, bool vec,
+                                      int64_t K)
+{
+    if (vec && k + 8 <= K) {
+        if constexpr (BF) {
+            const uint4 q = *(const uint4 *)((const uint16_t *)row + k);
+            w[0] = q.x;
+            w[1] = q.y;
+            w[2] = q.z;
+            w[3] = q.w;
+        } else {
+            const float4 p = *(const float4 *)((const float *)row + k);
+            const float4 q = *(const float4 *)((const float *)row + k + 4);
+            v[0] = p.x;
+            v[1] = p.y;
+            v[2] = p.z;
+            v[3] = p.w;
+            v[4] = q.x;
+            v[5] = q.y;
+            v[6] = q.z;
+            v[7] = q.w;
+        }
+    } else if constexpr (BF) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const uint16_t *p = (const uint16_t *)row + k + 2 * e;
+            const uint32_t lo = k + 2 * e < K ? p[0] : 0, hi = k + 2 * e + 1 < K ? p[1] : 0;
+            w[e] = lo | hi << 16;
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = k + e < K ? ((const float *)row)[k + e] : 0.0f;
+    }
+}
+
+// the largest magnitude of eight values, as fp32 bits
+template <bool BF>
+__device__ __forceinline__ uint32_t top8(const float *v, const uint32_t *w)
+{
+    if constexpr (BF) {
+        uint32_t m = w[0] & 0x7FFF7FFFu;
+#pragma unroll
+        for (int e = 1; e < 4; ++e) m = max_u16(m, w[e] & 0x7FFF7FFFu);
+        const uint32_t hi = m >> 16, lo = m & 0xFFFFu;
+        return (hi > lo ? hi : lo) << 16;
+    } else {
+        uint32_t m = 0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const uint32_t b = __float_as_uint(v[e]) & 0x7FFFFFFFu;
+            m = b > m ? b : m;
+        }
+        return m;
+    }
 }
 
 }  // namespace tpk

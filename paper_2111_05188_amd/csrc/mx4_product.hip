@@ -111,31 +111,30 @@ __global__ __launch_bounds__(256) void mx4_product_kernel(Mx4Args a, int nblocks
                      uint32_t (&hw)[TN]) {
 #pragma unroll
         for (int s = 0; s < 4; ++s) {
-            const int64_t ks = g * 4 + s < ksteps ? g * 4 + s : ksteps - 1;
+            const int64_t ks = g * 4 + s;
 #pragma unroll
             for (int i = 0; i < TM; ++i)
-                ga[s][i] = *(const intx4 *)(scalar(ca[i] + ks * 1024) + (size_t)(lane * 16u));
+                ga[s][i] = load_at<intx4>(ca[i] + ks * 1024, lane * 16u);
 #pragma unroll
             for (int j = 0; j < TN; ++j)
-                gw[s][j] = *(const intx4 *)(scalar(cw[j] + ks * 1024) + (size_t)(lane * 16u));
+                gw[s][j] = load_at<intx4>(cw[j] + ks * 1024, lane * 16u);
         }
 #pragma unroll
         for (int i = 0; i < TM; ++i)
-            ha[i] = *(const uint32_t *)(scalar(pa[i] + (int64_t)g * 256) + (size_t)(lane * 4u));
+            ha[i] = load_at<uint32_t>(pa[i] + (int64_t)g * 256, lane * 4u);
 #pragma unroll
         for (int j = 0; j < TN; ++j)
-            hw[j] = *(const uint32_t *)(scalar(pw[j] + (int64_t)g * 256) + (size_t)(lane * 4u));
+            hw[j] = load_at<uint32_t>(pw[j] + (int64_t)g * 256, lane * 4u);
     };
     fetch(g0, fa, fw, sa, sw);
     for (int g = g0; g < g1; ++g) {
         intx4 na[4][TM], nw[4][TN];
         uint32_t ma[TM], mw[TN];
         fetch(g + 1 < g1 ? g + 1 : g, na, nw, ma, mw);
-        const int left = ksteps - g * 4;
         Step<0>::run<TM, TN>(c, fa[0], sa, fw[0], sw);
-        if (left > 1) Step<1>::run<TM, TN>(c, fa[1], sa, fw[1], sw);
-        if (left > 2) Step<2>::run<TM, TN>(c, fa[2], sa, fw[2], sw);
-        if (left > 3) Step<3>::run<TM, TN>(c, fa[3], sa, fw[3], sw);
+        Step<1>::run<TM, TN>(c, fa[1], sa, fw[1], sw);
+        Step<2>::run<TM, TN>(c, fa[2], sa, fw[2], sw);
+        Step<3>::run<TM, TN>(c, fa[3], sa, fw[3], sw);
 #pragma unroll
         for (int s = 0; s < 4; ++s) {
 #pragma unroll
@@ -187,6 +186,347 @@ __global__ __launch_bounds__(256) void mx4_join_kernel(Mx4Args a, int parts)
     else finish4<false>(a, m, n, z, false);
 }
 
+// ---------------------------------------------------------------------------
+// K up to 1,024: a wave keeps its RT x 32 rows of A in registers for all of K
+// (a lane's part of a fragment is one block of 32, so rows of x go to 4 bits
+// there with no other lane's help), and W goes past it one tile of 32 columns
+// at a time, from LDS, where the workgroup's waves share it.  x is read once,
+// y written once.  From L1 instead of LDS a tile took 1.7 us against 1.3.
+// 65,536 x 1,001 bf16 rows times 1,536: 110 us, 22 of them for x at 6 TB/s,
+// the rest bound by LDS reads (13,100 a CU) with y's 201 MB behind them; 45 us
+// with 512 columns (4.5 TB/s).
+// SRC: x in fp32 (0), bf16 (1), or A in 4 bits (2).  KG groups of 4 k-steps.
+// ---------------------------------------------------------------------------
+enum { SRC_F32 = 0, SRC_BF16 = 1, SRC_FOUR = 2 };
+
+template <int S, int RT, int KS>
+__device__ __forceinline__ void mfma_row(floatx16 (&c)[RT], const intx4 &w, uint32_t scale,
+                                         const intx4 (&fa)[RT][KS], int ks,
+                                         const uint32_t (&sa)[RT][KS / 4], int g)
+{
+#pragma unroll
+    for (int i = 0; i < RT; ++i) c[i] = mfma_fp4<S>(w, scale, fa[i][ks], sa[i][g], c[i]);
+}
+
+// Rows of y from row m0 on as a buffer that ends with the matrix: stores past
+// it are dropped.  A wave reaches 64 rows, under 2^31 bytes.
+template <bool BF>
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t out_buffer(const Mx4Args &a, int64_t m0)
+{
+    constexpr int ES = BF ? 2 : 4;
+    const int64_t bytes = m0 < a.la.rows ? ((a.la.rows - 1 - m0) * a.ldy + a.lw.rows) * ES : 0;
+    return __builtin_amdgcn_make_buffer_rsrc((char *)a.y + m0 * a.ldy * ES, 0,
+                                             (int)(bytes < 0x7FFFFFFC ? bytes : 0x7FFFFFFC),
+                                             0x00027000);
+}
+
+// A wave's rows of y go out 256 bytes at a time: results of 64 (bf16: 128)
+// columns gather in the wave's part of the LDS, then each store writes four
+// whole pieces.  (Stores straight from the result's registers are 8 bytes of
+// 32 rows each, or 64 bytes of two rows: 65,536 x 1,536 in bf16 took 158 and
+// 124 us against 110.)
+constexpr int PIECE = 256, PIECE_PITCH = PIECE + 16;
+
+// results of tile `slot` of the piece: lane l has row l%32 of tile i, columns
+// 8 r + 4(l/32) .. +3 in registers 4 r .. 4 r + 3
+template <bool BF, int RT>
+__device__ __forceinline__ void gather_tile(char *lds, int slot, int lane, int act,
+                                            const floatx4 (&bias)[4], floatx16 (&c)[RT])
+{
+    constexpr int ES = BF ? 2 : 4;
+#pragma unroll
+    for (int i = 0; i < RT; ++i)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) c[i][e] += bias[e / 4][e % 4];
+    if (act == TP_ACT_TANH) {
+#pragma unroll
+        for (int i = 0; i < RT; ++i)
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+                c[i][e] = BF ? tanh_for_bf16(c[i][e]) : tanh_f32(c[i][e]);
+    }
+#pragma unroll
+    for (int i = 0; i < RT; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const float z[4] = {c[i][4 * r], c[i][4 * r + 1], c[i][4 * r + 2], c[i][4 * r + 3]};
+            char *at = lds + (32 * i + (lane & 31)) * PIECE_PITCH +
+                       (slot * 32 + 8 * r + 4 * (lane >> 5)) * ES;
+            if constexpr (BF) {
+                const bf16x4 w = {to_bf16(z[0]), to_bf16(z[1]), to_bf16(z[2]), to_bf16(z[3])};
+                *(bf16x4 *)at = w;
+            } else {
+                *(floatx4 *)at = floatx4{z[0], z[1], z[2], z[3]};
+            }
+        }
+}
+
+// The piece's rows to y from column n0 on, columns under n1.  EVEN: n1 is a
+// multiple of 16 bytes and y 4-byte aligned, so that a lane's 16 bytes are all
+// in or all out, and no branch stands around the stores: the compiler can count
+// them, and what waits for a later load need not wait for them.
+template <bool BF, int RT, bool EVEN>
+__device__ __forceinline__ void flush_piece(const char *lds, __amdgpu_buffer_rsrc_t out,
+                                            uint32_t pitch, int64_t n0, int64_t n1, int lane)
+{
+    constexpr int ES = BF ? 2 : 4, E = 16 / ES;     // elements of a lane
+    const int64_t n = n0 + (lane & 15) * E;
+    const char *from = lds + (lane >> 4) * PIECE_PITCH + (lane & 15) * 16;
+    const uint32_t to = (uint32_t)(lane >> 4) * pitch + (uint32_t)n * ES;
+    if constexpr (EVEN) {
+        // (an offset of 2^31 and more is outside every buffer)
+        const uint32_t at = n < n1 ? to : 0x80000000u;
+#pragma unroll
+        for (int k = 0; k < 8 * RT; ++k) {
+            const uintx4 v = *(const uintx4 *)(from + 4 * k * PIECE_PITCH);
+            __builtin_amdgcn_raw_buffer_store_b128(v, out, (int)(at + 4 * k * pitch), 0, 0);
+        }
+    } else if (n < n1) {
+#pragma unroll 1
+        for (int k = 0; k < 8 * RT; ++k)
+#pragma unroll
+            for (int e = 0; e < E; ++e)
+                if (n + e < n1) {
+                    const int at = (int)(to + 4 * k * pitch + e * ES);
+                    const char *v = from + 4 * k * PIECE_PITCH + e * ES;
+                    if constexpr (BF)
+                        __builtin_amdgcn_raw_buffer_store_b16(*(const uint16_t *)v, out, at, 0, 0);
+                    else
+                        __builtin_amdgcn_raw_buffer_store_b32(*(const uint32_t *)v, out, at, 0, 0);
+                }
+    }
+}
+
+// A block of 32 elements as loaded: bf16 in pairs, fp32
+template <bool BF>
+struct RawBlock {
+    uint32_t w[BF ? 16 : 32];
+};
+
+// Rows of x from row m0 on as a buffer that ends with the matrix: the hardware
+// returns zeros past it, so a row's last block needs no branch.
+template <bool BF>
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_buffer(const Mx4Args &a, int64_t m0)
+{
+    constexpr int ES = BF ? 2 : 4;
+    const int64_t bytes = m0 < a.la.rows ? ((a.la.rows - 1 - m0) * a.ldx + a.la.K) * ES : 0;
+    // whole dwords: the last one holds the last element
+    const int64_t most = bytes < 0xFFFFFFFC ? (bytes + 3) & ~(int64_t)3 : 0xFFFFFFFC;
+    return __builtin_amdgcn_make_buffer_rsrc((void *)((const char *)a.x + m0 * a.ldx * ES), 0,
+                                             (int)(uint32_t)most, 0x00027000);
+}
+
+// block at byte `off` of the buffer (16-byte aligned)
+template <bool BF>
+__device__ __forceinline__ void load_block(__amdgpu_buffer_rsrc_t rows, uint32_t off,
+                                           RawBlock<BF> &raw)
+{
+#pragma unroll
+    for (int q = 0; q < (BF ? 4 : 8); ++q) {
+        const uintx4 v = __builtin_amdgcn_raw_buffer_load_b128(rows, (int)(off + 16 * q), 0, 0);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) raw.w[4 * q + e] = v[e];
+    }
+}
+
+// zeros from element n of the block on
+template <bool BF>
+__device__ __forceinline__ void end_block(RawBlock<BF> &raw, int n)
+{
+#pragma unroll
+    for (int e = 0; e < (BF ? 16 : 32); ++e) {
+        if constexpr (BF) raw.w[e] = 2 * e >= n ? 0 : 2 * e + 1 >= n ? raw.w[e] & 0xFFFFu : raw.w[e];
+        else raw.w[e] = e >= n ? 0 : raw.w[e];
+    }
+}
+
+template <bool BF>
+__device__ __forceinline__ uint32_t block_to_fp4(const RawBlock<BF> &raw, bool any, intx4 &code)
+{
+    float v[4][8];
+    uint32_t w[4][4], top = 0;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        if constexpr (BF) __builtin_memcpy(w[q], &raw.w[4 * q], 16);
+        else __builtin_memcpy(v[q], &raw.w[8 * q], 32);
+        const uint32_t t = top8<BF>(v[q], w[q]);
+        top = t > top ? t : top;
+    }
+    const uint32_t byte = any ? scale_byte(top) : 127u;
+    const float sc = scale_value(byte);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        uint32_t c;
+        if constexpr (BF) c = codes_of_bf16(w[q], sc);
+        else c = codes_of(v[q], sc);
+        code[q] = (int)(byte == 255 ? 0x22222222u : c);
+    }
+    return byte;
+}
+
+template <int SRC, int KG, int RT, int NW, bool YBF, bool EVEN>
+__global__ __launch_bounds__(64 * NW, 2) void mx4_panel_kernel(Mx4Args a, int tiles_per)
+{
+    constexpr int KS = 4 * KG, SCALES = KS * 1024, BIAS = SCALES + KG * 256;  // a tile of W
+    constexpr int LOADS = KS / NW;                              // of 16 bytes a thread
+    __shared__ __attribute__((aligned(16))) char tiles[2][BIAS + 128];
+    __shared__ __attribute__((aligned(16))) char pieces[NW][RT * 32 * PIECE_PITCH];
+    const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    const int64_t mt0 = ((int64_t)blockIdx.x * NW + wv) * RT;   // (past A: reads zeros, stores nothing)
+    const int ntiles = (int)a.lw.tiles, nt0 = blockIdx.y * tiles_per;
+    const int nt1 = nt0 + tiles_per < ntiles ? nt0 + tiles_per : ntiles;
+    const uint8_t *pw = a.w + a.lw.off_scales;
+    // the workgroup's share of a tile on its way: registers, then LDS.  The
+    // tiles of a whole piece are under way, since a tile takes less time than
+    // W's latency; past the last tile they repeat it.
+    constexpr int SLOTS = PIECE / (32 * (YBF ? 2 : 4));     // tiles of a piece
+    struct Share {
+        intx4 code[LOADS];
+        uint32_t scale, bias;
+    };
+    // no bias: a buffer of nothing, which reads as zeros
+    const __amdgpu_buffer_rsrc_t biases = __builtin_amdgcn_make_buffer_rsrc(
+        (void *)a.bias, 0, a.bias ? (int)(a.lw.rows * 4) : 0, 0x00027000);
+    const int wg = wv < KG ? wv : KG - 1;
+    auto fetch_tile = [&](int t, Share &to) {
+        const int64_t nt = t < nt1 ? t : nt1 - 1;
+#pragma unroll
+        for (int k = 0; k < LOADS; ++k)
+            to.code[k] = load_at<intx4>(a.w + (nt * KS + k * NW + wv) * 1024, lane * 16u);
+        to.scale = load_at<uint32_t>(pw + (nt * KG + wg) * 256, lane * 4u);
+        to.bias = __builtin_amdgcn_raw_buffer_load_b32(biases, (int)nt * 128 + (lane & 31) * 4, 0, 0);
+    };
+    auto store_tile = [&](char *to, const Share &from) {
+#pragma unroll
+        for (int k = 0; k < LOADS; ++k)
+            *(intx4 *)(to + (k * NW + wv) * 1024 + lane * 16) = from.code[k];
+        *(uint32_t *)(to + SCALES + wg * 256 + lane * 4) = from.scale;
+        *(uint32_t *)(to + BIAS + (lane & 31) * 4) = from.bias;     // (the same from every wave)
+    };
+    // Whole pieces in an order that starts elsewhere for each workgroup, a
+    // partial one last: in step, all workgroups would write the same columns at
+    // a time, and with a pitch of many 256 bytes that is a few of the memory's
+    // channels.
+    const int whole = (nt1 - nt0) / SLOTS, turn = whole ? (int)(blockIdx.x % (uint32_t)whole) : 0;
+    auto piece_at = [&](int k) {
+        const int q = k + turn < whole ? k + turn : k + turn - whole;
+        return nt0 + (k < whole ? q : k) * SLOTS;
+    };
+    Share first, share[SLOTS];
+    fetch_tile(piece_at(0), first);
+
+    intx4 fa[RT][KS];
+    uint32_t sa[RT][KG];
+    if constexpr (SRC == SRC_FOUR) {
+#pragma unroll
+        for (int i = 0; i < RT; ++i) {
+            const int64_t t = mt0 + i < a.la.tiles ? mt0 + i : a.la.tiles - 1;
+#pragma unroll
+            for (int s = 0; s < KS; ++s) fa[i][s] = load_at<intx4>(a.a + (t * KS + s) * 1024, lane * 16u);
+#pragma unroll
+            for (int g = 0; g < KG; ++g)
+                sa[i][g] = load_at<uint32_t>(a.a + a.la.off_scales + (t * KG + g) * 256, lane * 4u);
+        }
+    } else {
+        // U k-steps' loads are in flight while the U before go to 4 bits
+        constexpr bool BF = SRC == SRC_BF16;
+        constexpr int U = BF ? 4 : 2, ES = BF ? 2 : 4;
+        const int K = (int)a.la.K, half = (lane >> 5) * 32;
+        const __amdgpu_buffer_rsrc_t rows = rows_buffer<BF>(a, mt0 * 32);
+        const uint32_t pitch = (uint32_t)a.ldx * ES, off = (lane & 31) * pitch + half * ES;
+        RawBlock<BF> raw[2][U];
+#pragma unroll
+        for (int i = 0; i < RT; ++i)
+#pragma unroll
+            for (int g = 0; g < KG; ++g) sa[i][g] = 0;
+        auto fetch = [&](int u, RawBlock<BF> (&to)[U]) {
+#pragma unroll
+            for (int s = 0; s < U; ++s) {
+                const int ks = u * U + s;
+                load_block<BF>(rows, off + ks / KS * 32 * pitch + ks % KS * 64 * ES, to[s]);
+            }
+        };
+        fetch(0, raw[0]);
+#pragma unroll
+        for (int u = 0; u < RT * KS / U; ++u) {
+            if (u + 1 < RT * KS / U) fetch(u + 1, raw[(u + 1) & 1]);
+#pragma unroll
+            for (int s = 0; s < U; ++s) {
+                const int ks = (u * U + s) % KS, i = (u * U + s) / KS, left = K - ks * 64 - half;
+                // (only the last group of k-steps can end inside)
+                if (ks >= KS - 4 && K < ks * 64 + 64) end_block<BF>(raw[u & 1][s], left);
+                sa[i][ks / 4] |= block_to_fp4<BF>(raw[u & 1][s], left > 0, fa[i][ks])
+                                 << (8 * (ks % 4));
+                // keeps the conversion here: the compiler otherwise moves it to
+                // the codes' use, and what all units loaded has to wait for it
+                asm volatile("" : "+v"(fa[i][ks]));
+            }
+        }
+    }
+    store_tile(tiles[0], first);
+#pragma unroll
+    for (int u = 0; u < SLOTS; ++u)
+        fetch_tile(u + 1 < SLOTS ? piece_at(0) + u + 1 : piece_at(1), share[u]);
+    const __amdgpu_buffer_rsrc_t out = out_buffer<YBF>(a, mt0 * 32);
+    const uint32_t pitch = (uint32_t)a.ldy * (YBF ? 2 : 4);
+    char *lds = pieces[wv];
+    auto tile_step = [&](int u, int later) {
+        char *tile = tiles[u & 1], *other = tiles[(u + 1) & 1];
+        // this tile is whole, and nobody reads the one before any more
+        workgroup_lds_barrier();
+        store_tile(other, share[u]);
+        fetch_tile(later, share[u]);
+        floatx16 c[RT] = {}, c2[RT] = {};       // even and odd k-steps: twice the chains
+        // a group's fragments are read while the group before is multiplied
+        intx4 fw[2][4];
+        uint32_t sw[2];
+        auto read_group = [&](int g) {
+#pragma unroll
+            for (int s = 0; s < 4; ++s)
+                fw[g & 1][s] = *(const intx4 *)(tile + (4 * g + s) * 1024 + lane * 16);
+            sw[g & 1] = *(const uint32_t *)(tile + SCALES + g * 256 + lane * 4);
+        };
+        read_group(0);
+#pragma unroll
+        for (int g = 0; g < KG; ++g) {
+            if (g + 1 < KG) read_group(g + 1);
+            __builtin_amdgcn_sched_barrier(0);
+            mfma_row<0, RT, KS>(c, fw[g & 1][0], sw[g & 1], fa, 4 * g, sa, g);
+            mfma_row<1, RT, KS>(c2, fw[g & 1][1], sw[g & 1], fa, 4 * g + 1, sa, g);
+            mfma_row<2, RT, KS>(c, fw[g & 1][2], sw[g & 1], fa, 4 * g + 2, sa, g);
+            mfma_row<3, RT, KS>(c2, fw[g & 1][3], sw[g & 1], fa, 4 * g + 3, sa, g);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+#pragma unroll
+        for (int i = 0; i < RT; ++i) c[i] += c2[i];
+        floatx4 bias[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+            bias[r] = *(const floatx4 *)(tile + BIAS + (8 * r + 4 * (lane >> 5)) * 4);
+        gather_tile<YBF, RT>(lds, u, lane, a.act, bias, c);
+    };
+    const int64_t N = a.lw.rows;
+    auto flush = [&](int t) {
+        const int64_t n0 = (int64_t)t * 32, n1 = (int64_t)(t + SLOTS < nt1 ? t + SLOTS : nt1) * 32;
+        wave_lds_fence();
+        flush_piece<YBF, RT, EVEN>(lds, out, pitch, n0, n1 < N ? n1 : N, lane);
+        wave_lds_fence();
+    };
+    for (int k = 0; k < whole; ++k) {
+        // the tile under way after a step is the one SLOTS + 1 further on
+        const int next = piece_at(k + 1), after = piece_at(k + 2);
+#pragma unroll
+        for (int u = 0; u < SLOTS; ++u) tile_step(u, u + 1 < SLOTS ? next + u + 1 : after);
+        flush(piece_at(k));
+    }
+    const int rest = nt1 - nt0 - whole * SLOTS;
+    if (rest == 0) return;
+#pragma unroll
+    for (int u = 0; u < SLOTS - 1; ++u)
+        if (u < rest) tile_step(u, nt1);
+    flush(nt0 + whole * SLOTS);
+}
+
 constexpr int TM = 4, TN = 2;
 
 struct Plan {
@@ -222,9 +562,49 @@ size_t mx4_workspace_bytes(int64_t M, int64_t N, int64_t K)
            (p.parts > 1 ? (size_t)p.parts * M * N * sizeof(float) : 0) + 256;
 }
 
+template <int SRC, int KG, int RT, int NW>
+void start_panel(const Mx4Args &a, hipStream_t s)
+{
+    const int64_t blocks = (a.la.tiles + NW * RT - 1) / (NW * RT), nt = a.lw.tiles;
+    int64_t parts = blocks < 256 ? (256 + blocks - 1) / blocks : 1;
+    if (parts > nt) parts = nt;
+    const int per = (int)((nt + parts - 1) / parts);
+    const dim3 grid((unsigned)blocks, (unsigned)((nt + per - 1) / per));
+    // 16 bytes of a row of y are all inside it, at addresses of whole dwords
+    const int es = a.y_bf16 ? 2 : 4;
+    const bool even = a.lw.rows * es % 16 == 0 && ((uintptr_t)a.y | (uint64_t)(a.ldy * es)) % 4 == 0;
+    void (*kernel)(Mx4Args, int) =
+        a.y_bf16 ? (even ? mx4_panel_kernel<SRC, KG, RT, NW, true, true>
+                         : mx4_panel_kernel<SRC, KG, RT, NW, true, false>)
+                 : (even ? mx4_panel_kernel<SRC, KG, RT, NW, false, true>
+                         : mx4_panel_kernel<SRC, KG, RT, NW, false, false>);
+    hipLaunchKernelGGL(kernel, grid, dim3(64 * NW), 0, s, a, per);
+}
+
+constexpr int PANEL_RT = 1, PANEL_NW = 4;
+
+template <int SRC>
+hipError_t launch_panel(const Mx4Args &a, hipStream_t s)
+{
+    switch (a.la.groups) {
+    case 1: start_panel<SRC, 1, PANEL_RT, PANEL_NW>(a, s); break;
+    case 2: start_panel<SRC, 2, PANEL_RT, PANEL_NW>(a, s); break;
+    case 3: start_panel<SRC, 3, PANEL_RT, PANEL_NW>(a, s); break;
+    default: start_panel<SRC, 4, PANEL_RT, PANEL_NW>(a, s);
+    }
+    return hipGetLastError();
+}
+
 hipError_t launch_mx4_product(const Mx4Args &in, hipStream_t s)
 {
     Mx4Args a = in;
+    const int es = a.x_bf16 ? 2 : 4;
+    // a wave's 64 rows within a buffer's 32-bit offsets
+    const bool panel = a.la.groups <= 4 && a.ldy * (a.y_bf16 ? 2 : 4) < (int64_t)1 << 25;
+    // rows of x in 16-byte pieces
+    if (panel && !a.a && ((uintptr_t)a.x | (uint64_t)(a.ldx * es)) % 16 == 0 &&
+        a.ldx * es < (int64_t)1 << 25)
+        return a.x_bf16 ? launch_panel<SRC_BF16>(a, s) : launch_panel<SRC_F32>(a, s);
     const Plan p = plan_of(a.la.rows, a.lw.rows, a.la.K);
     if (!a.a) {
         const hipError_t e = launch_mx4_quantize(a.x, a.x_bf16, a.ldx, 1, a.la, a.work, s);
@@ -232,6 +612,7 @@ hipError_t launch_mx4_product(const Mx4Args &in, hipStream_t s)
         a.a = (const uint8_t *)a.work;
         a.work = (char *)a.work + round256(a.la.total);
     }
+    if (panel) return launch_panel<SRC_FOUR>(a, s);
     hipLaunchKernelGGL((mx4_product_kernel<TM, TN>),
                        dim3((unsigned)(p.mblocks * p.nblocks), (unsigned)p.parts), dim3(256), 0, s,
                        a, p.nblocks, p.groups_per);

@@ -30,8 +30,9 @@ constexpr float RATE = 8.0f;
 template <int BYTES> struct RawOf;
 template <> struct RawOf<2> { typedef uint16_t type; };
 template <> struct RawOf<4> { typedef uint32_t type; };
-template <> struct RawOf<8> { typedef uint2 type; };
-template <> struct RawOf<16> { typedef uint4 type; };
+template <> struct RawOf<8> {
+    typedef uint32_t type __attribute__((ext_vector_type(2)));
+};
 
 template <bool BF, int V>
 using Raw = typename RawOf<(BF ? 2 : 4) * V>::type;
@@ -39,7 +40,7 @@ using Raw = typename RawOf<(BF ? 2 : 4) * V>::type;
 template <bool BF, int V>
 __device__ __forceinline__ Raw<BF, V> load_row(const void *row, uint32_t d)
 {
-    return *(const Raw<BF, V> *)((const char *)row + (size_t)(d * (BF ? 2u : 4u)));
+    return load_at<Raw<BF, V>>(row, d * (BF ? 2u : 4u));
 }
 
 template <bool BF, int V>
@@ -69,7 +70,7 @@ __device__ __forceinline__ void store_row(void *row, uint32_t d, const float *v)
     } else {
         __builtin_memcpy(&raw, v, sizeof raw);
     }
-    *(Raw<BF, V> *)((char *)row + (size_t)(d * (BF ? 2u : 4u))) = raw;
+    store_at(row, d * (BF ? 2u : 4u), raw);
 }
 
 template <int V>
@@ -250,14 +251,11 @@ template <bool BF, int V>
 __device__ __forceinline__ void load_chunk(const RecurRows &m, int b, int t, int T, uint32_t d,
                                            Raw<BF, V> *raw)
 {
-    if (t + C <= T) {
-        char *row = row_at(m, b, t);
+    const char *row = row_at(m, b, t < T ? t : T - 1);
 #pragma unroll
-        for (int k = 0; k < C; ++k) raw[k] = load_row<BF, V>(scalar(row + k * m.st), d);
-    } else {
-#pragma unroll
-        for (int k = 0; k < C; ++k)
-            raw[k] = load_row<BF, V>(scalar(row_at(m, b, t + k < T ? t + k : T - 1)), d);
+    for (int k = 0; k < C; ++k) {
+        raw[k] = load_row<BF, V>(row, d);
+        row += t + k + 1 < T ? m.st : 0;
     }
 }
 
@@ -389,7 +387,7 @@ __global__ __launch_bounds__(64 * W * GROUP<W>) void recur_fwd_kernel(RecurArgs 
                     y[e] = plain || k < nv ? h[e] : 0.0f;
                     if (!plain && (clear >> k & 1)) h[e] = 0.0f;
                 }
-                if (p.live && t + k < a.T) store_row<BF, V>(scalar(out + k * a.y.st), p.dc, y);
+                if (p.live && t + k < a.T) store_row<BF, V>(out + k * a.y.st, p.dc, y);
             }
             if constexpr (W == 1) {
 #pragma unroll
@@ -542,9 +540,9 @@ __global__ __launch_bounds__(64 * W * GROUP<W>) void recur_bwd_kernel(RecurArgs 
                 G[e] = fade<BF>(c[k][e], gg);
             }
             if (p.live && t + k < a.T) {
-                store_row<BF, V>(scalar(outx + k * a.dx.st), p.dc, dx);
-                store_row<BF, V>(scalar(outr + k * a.dr.st), p.dc, dr);
-                store_row<BF, V>(scalar(outi + k * a.di.st), p.dc, di);
+                store_row<BF, V>(outx + k * a.dx.st, p.dc, dx);
+                store_row<BF, V>(outr + k * a.dr.st, p.dc, dr);
+                store_row<BF, V>(outi + k * a.di.st, p.dc, di);
             }
         }
         if constexpr (W == 1) {

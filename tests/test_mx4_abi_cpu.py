@@ -14,10 +14,10 @@ def _refused(rc, text, code=tp.TP_EINVAL):
 
 
 def test_bytes():
-    # whole fragments of 32 x 64 codes and of 32 x 256 scales
-    assert tp.mx4_bytes(1, 1) == 1024 + 256
-    assert tp.mx4_bytes(32, 64) == 1024 + 256
-    assert tp.mx4_bytes(33, 257) == 2 * (5 * 1024 + 2 * 256)
+    # whole tiles of 32 rows and 256 elements
+    assert tp.mx4_bytes(1, 1) == 32 * 256 * 17 // 32
+    assert tp.mx4_bytes(32, 256) == 32 * 256 * 17 // 32
+    assert tp.mx4_bytes(33, 257) == 4 * 32 * 256 * 17 // 32
     assert tp.mx4_bytes(512, 1024) == 512 * 1024 * 17 // 32
     L = tp.load()
     for rows, K in ((0, 4), (4, 0), (-1, 4), (1 << 30, 4), (4, 1 << 30)):
