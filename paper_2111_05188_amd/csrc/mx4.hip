@@ -71,9 +71,10 @@ __global__ __launch_bounds__(256) void mx4_quantize_cols_kernel(const char *x, i
     if (g >= L.groups) return;
     const uint32_t row0 = (unit - g * strips) * 64 * V + lane * V;
     if (row0 >= L.tiles * 32) return;
-    // (V divides the number of rows: a lane's rows are all in or all out)
+    // A lane's V elements are one aligned word, so that the last one may be read
+    // with an element that is not the matrix's.
     const bool in = row0 < L.rows;
-    const uint32_t off = (uint32_t)(in ? row0 : L.rows - V) * ES;
+    const uint32_t off = (uint32_t)(in ? row0 : (L.rows - 1) / V * V) * ES;
     uint32_t scales[V][2];
 #pragma unroll
     for (int e = 0; e < V; ++e) scales[e][0] = scales[e][1] = 0;
@@ -99,11 +100,12 @@ __global__ __launch_bounds__(256) void mx4_quantize_cols_kernel(const char *x, i
                 v[0][j] = load_at<float>(p, off);
             }
         }
-        const int valid = !in || k0 >= L.K ? 0 : L.K - k0 < 32 ? (int)(L.K - k0) : 32;
+        const int steps = k0 >= L.K ? 0 : L.K - k0 < 32 ? (int)(L.K - k0) : 32;
         const uint32_t ks = g * 4 + (b >> 1);
 #pragma unroll
         for (int e = 0; e < V; ++e) {
             const uint32_t row = row0 + e;
+            const int valid = row < L.rows ? steps : 0;
             uint32_t top = 0;
 #pragma unroll
             for (int j = 0; j < 32; ++j) {
@@ -227,7 +229,7 @@ hipError_t launch_mx4_quantize(const void *x, bool bf16, int64_t row_stride, int
     }
     // two rows a lane where every pair is aligned
     const int es = bf16 ? 2 : 4;
-    const bool two = L.rows >= 128 && L.rows % 2 == 0 &&
+    const bool two = L.rows >= 128 &&
                      ((uintptr_t)x | (uint64_t)(col_stride * es)) % (2 * es) == 0;
     const int64_t strips = (L.tiles * 32 + (two ? 127 : 63)) / (two ? 128 : 64);
     const dim3 grid((unsigned)((strips * L.groups + 3) / 4));

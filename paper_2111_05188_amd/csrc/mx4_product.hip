@@ -47,141 +47,181 @@ __device__ __forceinline__ void finish4(const Mx4Args &a, int64_t m, int64_t n, 
     }
 }
 
-// a 32 x 32 result (register i: n = n0 + 8(i/4) + 4(lane/32) + i%4)
-__device__ __forceinline__ void finish_tile(const Mx4Args &a, int64_t m, int64_t n0, int lane,
-                                            const floatx16 &c, bool vec)
-{
-    if (m >= a.la.rows) return;
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-        float z[4] = {c[4 * r], c[4 * r + 1], c[4 * r + 2], c[4 * r + 3]};
-        const int64_t n = n0 + 8 * r + 4 * (lane >> 5);
-        if (a.y_bf16) finish4<true>(a, m, n, z, vec);
-        else finish4<false>(a, m, n, z, vec);
-    }
-}
-
-template <int S0>
-struct Step {
-    template <int TM, int TN>
-    static __device__ __forceinline__ void run(floatx16 (&c)[TM][TN], const intx4 (&fa)[TM],
-                                               const uint32_t (&sa)[TM], const intx4 (&fw)[TN],
-                                               const uint32_t (&sw)[TN])
-    {
-#pragma unroll
-        for (int i = 0; i < TM; ++i)
-#pragma unroll
-            for (int j = 0; j < TN; ++j)
-                c[i][j] = mfma_fp4<S0>(fw[j], sw[j], fa[i], sa[i], c[i][j]);
-    }
-};
-
 // ---------------------------------------------------------------------------
-// Any size: a wave has TM x TN tiles of 32 x 32, a workgroup 2 x 2 waves, and
-// each wave streams its fragments from L1 and L2, a group of k-steps ahead.
-// gridDim.y > 1: a part of K each, its sums in fp32 to the workspace.
+// Any size.  A workgroup of 2 x 2 waves has 8 x 8 tiles of 32 x 32, a wave 4 x 4
+// of them (256 registers of sums: each fragment read from LDS feeds four matrix
+// instructions).  Groups of four k-steps go through two LDS buffers: while one
+// is multiplied, the next lies in registers and is stored to the other.
+// More workgroups than blocks: a part of K each; its sums go to the workspace as the lanes
+// hold them, 1 KiB a store, and mx4_join_kernel adds the parts in order.
+// 1,536 x 1,001 over K = 65,536: XX us (YY of the 8.4 PFLOP/s that the
+// instruction reaches); fragments straight from L1, 4 x 2 tiles a wave, 125 us.
 // ---------------------------------------------------------------------------
-template <int TM, int TN>
-__global__ __launch_bounds__(256) void mx4_product_kernel(Mx4Args a, int nblocks, int groups_per)
+constexpr int WT = 4, BT = 2 * WT;                  // tiles of a wave, of a workgroup, a side
+constexpr int64_t BLOCK_FLOATS = (int64_t)BT * BT * 1024;
+
+__global__ __launch_bounds__(256, 1) void mx4_product_kernel(Mx4Args a, int nblocks, int blocks,
+                                                             int groups_per)
 {
+    constexpr int STAGE = 2 * BT * 4096;            // A's tiles, then W's: four k-steps of each
+    __shared__ __attribute__((aligned(16))) char stages[2 * STAGE];
     const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-    const int mb = blockIdx.x / nblocks, nb = blockIdx.x - mb * nblocks;
-    const int mt0 = (mb * 2 + (wv >> 1)) * TM, nt0 = (nb * 2 + (wv & 1)) * TN;
-    const int ksteps = (int)a.la.ksteps, groups = (int)a.la.groups;
-    const int g0 = blockIdx.y * groups_per;
-    const int g1 = g0 + groups_per < groups ? g0 + groups_per : groups;
-    const char *ca[TM], *cw[TN];
-    const char *pa[TM], *pw[TN];
-#pragma unroll
-    for (int i = 0; i < TM; ++i) {
-        const int64_t t = mt0 + i < a.la.tiles ? mt0 + i : a.la.tiles - 1;
-        ca[i] = (const char *)a.a + t * ksteps * 1024;
-        pa[i] = (const char *)a.a + a.la.off_scales + t * groups * 256;
-    }
-#pragma unroll
-    for (int j = 0; j < TN; ++j) {
-        const int64_t t = nt0 + j < a.lw.tiles ? nt0 + j : a.lw.tiles - 1;
-        cw[j] = (const char *)a.w + t * ksteps * 1024;
-        pw[j] = (const char *)a.w + a.lw.off_scales + t * groups * 256;
-    }
-    floatx16 c[TM][TN] = {};
-    intx4 fa[4][TM], fw[4][TN];
-    uint32_t sa[TM], sw[TN];
-    auto fetch = [&](int g, intx4 (&ga)[4][TM], intx4 (&gw)[4][TN], uint32_t (&ha)[TM],
-                     uint32_t (&hw)[TN]) {
-#pragma unroll
-        for (int s = 0; s < 4; ++s) {
-            const int64_t ks = g * 4 + s;
-#pragma unroll
-            for (int i = 0; i < TM; ++i)
-                ga[s][i] = load_at<intx4>(ca[i] + ks * 1024, lane * 16u);
-#pragma unroll
-            for (int j = 0; j < TN; ++j)
-                gw[s][j] = load_at<intx4>(cw[j] + ks * 1024, lane * 16u);
-        }
-#pragma unroll
-        for (int i = 0; i < TM; ++i)
-            ha[i] = load_at<uint32_t>(pa[i] + (int64_t)g * 256, lane * 4u);
-#pragma unroll
-        for (int j = 0; j < TN; ++j)
-            hw[j] = load_at<uint32_t>(pw[j] + (int64_t)g * 256, lane * 4u);
+    // Workgroups go to the eight XCDs in turn; here an XCD's share is neighbours,
+    // who read the same part of K of the same tiles, so that its L2 has them.
+    const uint32_t total = gridDim.x, xcd = blockIdx.x % 8, each = total / 8, more = total % 8;
+    const int at = (int)(xcd * each + (xcd < more ? xcd : more) + blockIdx.x / 8);
+    const int part = at / blocks, block = at - part * blocks;
+    const int mb = block / nblocks, nb = block - mb * nblocks;
+    const int wm = wv >> 1, wn = wv & 1;
+    const int64_t ksteps = a.la.ksteps, groups = a.la.groups;
+    const int g0 = part * groups_per;
+    const int g1 = g0 + groups_per < groups ? g0 + groups_per : (int)groups;
+    // tiles past the matrix repeat its last one
+    auto a_tile = [&](int i) {
+        const int64_t t = (int64_t)mb * BT + i;
+        return t < a.la.tiles ? t : a.la.tiles - 1;
     };
-    fetch(g0, fa, fw, sa, sw);
-    for (int g = g0; g < g1; ++g) {
-        intx4 na[4][TM], nw[4][TN];
-        uint32_t ma[TM], mw[TN];
-        fetch(g + 1 < g1 ? g + 1 : g, na, nw, ma, mw);
-        Step<0>::run<TM, TN>(c, fa[0], sa, fw[0], sw);
-        Step<1>::run<TM, TN>(c, fa[1], sa, fw[1], sw);
-        Step<2>::run<TM, TN>(c, fa[2], sa, fw[2], sw);
-        Step<3>::run<TM, TN>(c, fa[3], sa, fw[3], sw);
+    auto w_tile = [&](int j) {
+        const int64_t t = (int64_t)nb * BT + j;
+        return t < a.lw.tiles ? t : a.lw.tiles - 1;
+    };
+    // waves 0 and 1 bring A's tiles, 2 and 3 W's, four each
+    const uint8_t *from[4];
 #pragma unroll
-        for (int s = 0; s < 4; ++s) {
+    for (int t = 0; t < 4; ++t)
+        from[t] = wv < 2 ? a.a + a_tile(wv * 4 + t) * ksteps * 1024
+                         : a.w + w_tile(wv * 4 + t - BT) * ksteps * 1024;
+    const uint8_t *pa[WT], *pw[WT];
 #pragma unroll
-            for (int i = 0; i < TM; ++i) fa[s][i] = na[s][i];
-#pragma unroll
-            for (int j = 0; j < TN; ++j) fw[s][j] = nw[s][j];
-        }
-#pragma unroll
-        for (int i = 0; i < TM; ++i) sa[i] = ma[i];
-#pragma unroll
-        for (int j = 0; j < TN; ++j) sw[j] = mw[j];
+    for (int i = 0; i < WT; ++i) {
+        pa[i] = a.a + a.la.off_scales + a_tile(wm * WT + i) * groups * 256;
+        pw[i] = a.w + a.lw.off_scales + w_tile(wn * WT + i) * groups * 256;
     }
-    const int64_t M = a.la.rows, N = a.lw.rows;
-    const bool vec = ((uintptr_t)a.y | (uint64_t)(a.ldy * (a.y_bf16 ? 2 : 4))) %
-                         (a.y_bf16 ? 8 : 16) == 0;
+    intx4 share[16];
+    uint32_t na[WT], nw[WT];
+    auto fetch = [&](int g, int k) {
+        share[k] = load_at<intx4>(from[k / 4] + ((int64_t)g * 4 + k % 4) * 1024, lane * 16u);
+    };
+    auto fetch_scale = [&](int g, int k) {
+        if (k < WT) na[k] = load_at<uint32_t>(pa[k] + (int64_t)g * 256, lane * 4u);
+        else nw[k - WT] = load_at<uint32_t>(pw[k - WT] + (int64_t)g * 256, lane * 4u);
+    };
+    auto put = [&](char *to, int k) {
+        *(intx4 *)(to + (wv * 16 + k) * 1024 + lane * 16) = share[k];
+    };
+    floatx16 c[WT][WT] = {};
 #pragma unroll
-    for (int i = 0; i < TM; ++i)
+    for (int k = 0; k < 16; ++k) fetch(g0, k);
 #pragma unroll
-        for (int j = 0; j < TN; ++j) {
-            const int64_t m = (int64_t)(mt0 + i) * 32 + (lane & 31), n0 = (int64_t)(nt0 + j) * 32;
-            if (gridDim.y == 1) {
-                finish_tile(a, m, n0, lane, c[i][j], vec);
-            } else if (m < M) {
-                float *part = (float *)a.work + ((int64_t)blockIdx.y * M + m) * N;
+    for (int k = 0; k < 2 * WT; ++k) fetch_scale(g0, k);
 #pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    const int64_t n = n0 + 8 * (e / 4) + 4 * (lane >> 5) + e % 4;
-                    if (n < N) part[n] = c[i][j][e];
-                }
-            }
+    for (int k = 0; k < 16; ++k) {
+        put(stages, k);
+        fetch(g0 + 1 < g1 ? g0 + 1 : g0, k);
+    }
+    for (int g = g0; g < g1; ++g) {
+        const char *now = stages + ((g - g0) & 1) * STAGE;
+        char *other = stages + ((g - g0 + 1) & 1) * STAGE;
+        // (past the last group: the last one again)
+        const int next = g + 1 < g1 ? g + 1 : g1 - 1, later = g + 2 < g1 ? g + 2 : g1 - 1;
+        // this stage is whole, and nobody reads the one before any more
+        workgroup_lds_barrier();
+        uint32_t sa[WT], sw[WT];
+#pragma unroll
+        for (int i = 0; i < WT; ++i) {
+            sa[i] = na[i];
+            sw[i] = nw[i];
         }
+        intx4 fa[2][WT], fw[2][WT];
+        auto read = [&](int s, int k) {
+            if (k < WT)
+                fa[s & 1][k] = *(const intx4 *)(now + ((wm * WT + k) * 4 + s) * 1024 + lane * 16);
+            else
+                fw[s & 1][k - WT] = *(const intx4 *)(now + ((BT + wn * WT + k - WT) * 4 + s) * 1024 + lane * 16);
+        };
+#pragma unroll
+        for (int k = 0; k < 2 * WT; ++k) read(0, k);
+        // Between the matrix instructions, in this order: the next stage from
+        // registers to LDS and the one after into the registers just stored;
+        // the next k-step's fragments; the next group's scales.
+#pragma unroll
+        for (int q = 0; q < 4 * WT * WT; ++q) {
+            const int s = q / (WT * WT), i = q / WT % WT, j = q % WT, k = q % (WT * WT);
+            __builtin_amdgcn_sched_barrier(0);
+            if (s == 0) c[i][j] = mfma_fp4<0>(fw[0][j], sw[j], fa[0][i], sa[i], c[i][j]);
+            else if (s == 1) c[i][j] = mfma_fp4<1>(fw[1][j], sw[j], fa[1][i], sa[i], c[i][j]);
+            else if (s == 2) c[i][j] = mfma_fp4<2>(fw[0][j], sw[j], fa[0][i], sa[i], c[i][j]);
+            else c[i][j] = mfma_fp4<3>(fw[1][j], sw[j], fa[1][i], sa[i], c[i][j]);
+            if (s < 3 && k % 2 == 0) read(s + 1, k / 2);
+            if (s == 0) {
+                put(other, k);
+                fetch(later, k);
+            }
+            if (s == 1 && k % 2 == 1) fetch_scale(next, k / 2);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    }
+    if ((int)total == blocks) {
+        // a row of tiles at a time through the wave's part of the LDS, then in
+        // rows of 128 columns (a loop: unrolled, the epilogue of 256 registers
+        // is longer than the compiler keeps registers for)
+        constexpr int PITCH = (WT * 32 + 4) * 4;
+        char *rows = stages + wv * 32 * PITCH;
+        const bool vec = ((uintptr_t)a.y | (uint64_t)(a.ldy * (a.y_bf16 ? 2 : 4))) %
+                             (a.y_bf16 ? 8 : 16) == 0;
+        workgroup_lds_barrier();
+#pragma unroll
+        for (int i = 0; i < WT; ++i) {
+#pragma unroll
+            for (int j = 0; j < WT; ++j)
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    *(floatx4 *)(rows + (lane & 31) * PITCH + (j * 32 + 8 * r + 4 * (lane >> 5)) * 4) =
+                        floatx4{c[i][j][4 * r], c[i][j][4 * r + 1], c[i][j][4 * r + 2],
+                                c[i][j][4 * r + 3]};
+            wave_lds_fence();
+            const int64_t m0 = ((int64_t)mb * BT + wm * WT + i) * 32 + (lane >> 5);
+            const int64_t n = ((int64_t)nb * BT + wn * WT) * 32 + (lane & 31) * 4;
+#pragma unroll 1
+            for (int k = 0; k < 32; k += 2) {
+                const floatx4 v = *(const floatx4 *)(rows + (k + (lane >> 5)) * PITCH + (lane & 31) * 16);
+                float z[4] = {v[0], v[1], v[2], v[3]};
+                if (m0 + k >= a.la.rows) continue;
+                if (a.y_bf16) finish4<true>(a, m0 + k, n, z, vec);
+                else finish4<false>(a, m0 + k, n, z, vec);
+            }
+            wave_lds_fence();
+        }
+        return;
+    }
+    float *sums = (float *)a.work + (int64_t)at * BLOCK_FLOATS;
+#pragma unroll
+    for (int i = 0; i < WT; ++i)
+#pragma unroll
+        for (int j = 0; j < WT; ++j)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                store_at(sums + (((wv * WT + i) * WT + j) * 4 + r) * 256, lane * 16u,
+                         floatx4{c[i][j][4 * r], c[i][j][4 * r + 1], c[i][j][4 * r + 2],
+                                 c[i][j][4 * r + 3]});
 }
 
-// the parts of K in order
-__global__ __launch_bounds__(256) void mx4_join_kernel(Mx4Args a, int parts)
+// the parts of K in order: a thread has four neighbours of a row
+__global__ __launch_bounds__(256) void mx4_join_kernel(Mx4Args a, int nblocks, int blocks, int parts)
 {
-    const int64_t M = a.la.rows, N = a.lw.rows, n4 = (N + 3) / 4;
-    const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (at >= M * n4) return;
-    const int64_t m = at / n4, n = (at - m * n4) * 4;
-    float z[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-    for (int p = 0; p < parts; ++p) {
-        const float *part = (const float *)a.work + ((int64_t)p * M + m) * N + n;
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (n + e < N) z[e] += part[e];
-    }
+    const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;     // of a part's fours
+    const int block = (int)(at / (BLOCK_FLOATS / 4)), in = (int)(at % (BLOCK_FLOATS / 4));
+    const int lane = in & 63, r = in >> 6 & 3, j = in >> 8 & 3, i = in >> 10 & 3, wv = in >> 12;
+    const int mb = block / nblocks, nb = block - mb * nblocks;
+    const int64_t m = ((int64_t)mb * BT + (wv >> 1) * WT + i) * 32 + (lane & 31);
+    const int64_t n = ((int64_t)nb * BT + (wv & 1) * WT + j) * 32 + 8 * r + 4 * (lane >> 5);
+    if (m >= a.la.rows || n >= a.lw.rows) return;
+    const floatx4 *part = (const floatx4 *)a.work + at;
+    const int64_t stride = (int64_t)blocks * (BLOCK_FLOATS / 4);
+    floatx4 sum = {};
+#pragma unroll 8
+    for (int p = 0; p < parts; ++p) sum += part[p * stride];
+    float z[4] = {sum[0], sum[1], sum[2], sum[3]};
     if (a.y_bf16) finish4<true>(a, m, n, z, false);
     else finish4<false>(a, m, n, z, false);
 }
@@ -527,27 +567,32 @@ __global__ __launch_bounds__(64 * NW, 2) void mx4_panel_kernel(Mx4Args a, int ti
     flush(nt0 + whole * SLOTS);
 }
 
-constexpr int TM = 4, TN = 2;
-
 struct Plan {
     int mblocks, nblocks, parts, groups_per;
 };
 
-// Parts of K so that the workgroups fill the GPU once, each with at least
-// four groups of k-steps.
+// Parts of K so that the workgroups fill the GPU once; a part has at least
+// four groups of k-steps, and there are at most 64 (each is 256 KiB a workgroup
+// to store and to add).
 Plan plan_of(int64_t M, int64_t N, int64_t K)
 {
     Plan p;
-    const int64_t mt = (M + 31) / 32, nt = (N + 31) / 32, groups = (K + 255) / 256;
-    p.mblocks = (int)((mt + 2 * TM - 1) / (2 * TM));
-    p.nblocks = (int)((nt + 2 * TN - 1) / (2 * TN));
+    const int64_t groups = (K + 255) / 256;
+    p.mblocks = (int)((M + 32 * BT - 1) / (32 * BT));
+    p.nblocks = (int)((N + 32 * BT - 1) / (32 * BT));
     const int64_t blocks = (int64_t)p.mblocks * p.nblocks;
     int64_t parts = blocks < 256 ? 256 / blocks : 1;
+    if (parts > 64) parts = 64;
     if (parts > groups / 4) parts = groups / 4;
     if (parts < 1) parts = 1;
     p.groups_per = (int)((groups + parts - 1) / parts);
     p.parts = (int)((groups + p.groups_per - 1) / p.groups_per);
     return p;
+}
+
+size_t parts_bytes(const Plan &p)
+{
+    return p.parts > 1 ? (size_t)p.parts * p.mblocks * p.nblocks * BLOCK_FLOATS * sizeof(float) : 0;
 }
 
 size_t round256(size_t n) { return (n + 255) / 256 * 256; }
@@ -558,8 +603,7 @@ size_t round256(size_t n) { return (n + 255) / 256 * 256; }
 size_t mx4_workspace_bytes(int64_t M, int64_t N, int64_t K)
 {
     const Plan p = plan_of(M, N, K);
-    return round256(mx4_layout(M, K).total) +
-           (p.parts > 1 ? (size_t)p.parts * M * N * sizeof(float) : 0) + 256;
+    return round256(mx4_layout(M, K).total) + parts_bytes(p) + 256;
 }
 
 template <int SRC, int KG, int RT, int NW>
@@ -613,14 +657,13 @@ hipError_t launch_mx4_product(const Mx4Args &in, hipStream_t s)
         a.work = (char *)a.work + round256(a.la.total);
     }
     if (panel) return launch_panel<SRC_FOUR>(a, s);
-    hipLaunchKernelGGL((mx4_product_kernel<TM, TN>),
-                       dim3((unsigned)(p.mblocks * p.nblocks), (unsigned)p.parts), dim3(256), 0, s,
-                       a, p.nblocks, p.groups_per);
+    const int blocks = p.mblocks * p.nblocks;
+    hipLaunchKernelGGL(mx4_product_kernel, dim3((unsigned)(blocks * p.parts)), dim3(256), 0, s, a,
+                       p.nblocks, blocks, p.groups_per);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || p.parts == 1) return e;
-    const int64_t threads = a.la.rows * ((a.lw.rows + 3) / 4);
-    hipLaunchKernelGGL(mx4_join_kernel, dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, s, a,
-                       p.parts);
+    hipLaunchKernelGGL(mx4_join_kernel, dim3((unsigned)(blocks * (BLOCK_FLOATS / 4 / 256))),
+                       dim3(256), 0, s, a, p.nblocks, blocks, p.parts);
     return hipGetLastError();
 }
 
