@@ -321,7 +321,7 @@ int check_mx4_size(int64_t rows, int64_t K, const char *name)
         return fail(TP_EINVAL, "4-bit %s: %lld rows of %lld elements (1 .. 2^29 each)", name,
                     (long long)rows, (long long)K);
     const Mx4Layout L = mx4_layout(rows, K);
-    if (L.tiles * L.groups > 1 << 24)   // workgroups of 256 threads in a 32-bit grid
+    if (L.tiles * L.groups > 1 << 22)   // workgroups of 256 threads in a 32-bit grid
         return fail(TP_EUNSUPPORTED, "4-bit %s: %lld x %lld exceeds the launch grid", name,
                     (long long)rows, (long long)K);
     return TP_OK;

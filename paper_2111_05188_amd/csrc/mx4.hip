@@ -1,5 +1,7 @@
 // Matrices to 4-bit blocks and back.  Both directions move what they have to
 // and compute little; they are bound by the memory.
+#include <type_traits>
+
 #include "mx4.hpp"
 
 namespace tpk {
@@ -57,8 +59,9 @@ __global__ __launch_bounds__(256) void mx4_quantize_rows_kernel(const void *x, i
 
 // ---------------------------------------------------------------------------
 // columns in memory (element (row, k) at row + k ld): a lane takes V rows and
-// walks down k, so a block needs no other lane; a wave has 64 V rows and one
-// group of 4 k-steps.
+// walks down k, so a block needs no other lane; a wave has 64 V rows and the
+// blocks of one half (the first or second 32) of a group's 4 k-steps, whose
+// scales are one dword.
 // ---------------------------------------------------------------------------
 template <bool BF, int V>
 __global__ __launch_bounds__(256) void mx4_quantize_cols_kernel(const char *x, int64_t ld,
@@ -67,20 +70,18 @@ __global__ __launch_bounds__(256) void mx4_quantize_cols_kernel(const char *x, i
     constexpr int ES = BF ? 2 : 4;
     const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const uint32_t strips = (uint32_t)(L.tiles * 32 + 64 * V - 1) / (64 * V);
-    const uint32_t unit = blockIdx.x * 4 + wv, g = unit / strips;
+    const uint32_t unit = blockIdx.x * 4 + wv, gh = unit / strips, g = gh / 2, h = gh % 2;
     if (g >= L.groups) return;
-    const uint32_t row0 = (unit - g * strips) * 64 * V + lane * V;
+    const uint32_t row0 = (unit - gh * strips) * 64 * V + lane * V;
     if (row0 >= L.tiles * 32) return;
     // A lane's V elements are one aligned word, so that the last one may be read
     // with an element that is not the matrix's.
     const bool in = row0 < L.rows;
     const uint32_t off = (uint32_t)(in ? row0 : (L.rows - 1) / V * V) * ES;
-    uint32_t scales[V][2];
-#pragma unroll
-    for (int e = 0; e < V; ++e) scales[e][0] = scales[e][1] = 0;
+    uint32_t scales[V] = {};
 #pragma unroll 1
-    for (int b = 0; b < 8; ++b) {
-        const int64_t k0 = (int64_t)g * 256 + b * 32;
+    for (int s = 0; s < 4; ++s) {
+        const int64_t k0 = (int64_t)g * 256 + s * 64 + h * 32;
         float v[V][32];
 #pragma unroll
         for (int j = 0; j < 32; ++j) {
@@ -101,7 +102,7 @@ __global__ __launch_bounds__(256) void mx4_quantize_cols_kernel(const char *x, i
             }
         }
         const int steps = k0 >= L.K ? 0 : L.K - k0 < 32 ? (int)(L.K - k0) : 32;
-        const uint32_t ks = g * 4 + (b >> 1);
+        const uint32_t ks = g * 4 + s;
 #pragma unroll
         for (int e = 0; e < V; ++e) {
             const uint32_t row = row0 + e;
@@ -121,19 +122,17 @@ __global__ __launch_bounds__(256) void mx4_quantize_cols_kernel(const char *x, i
             code.z = codes_of(&v[e][16], sc);
             code.w = codes_of(&v[e][24], sc);
             if (byte == 255) code = make_uint4(0x22222222u, 0x22222222u, 0x22222222u, 0x22222222u);
-            scales[e][b & 1] |= byte << (8 * (b >> 1));
-            const uint32_t fl = (row & 31) + 32 * (b & 1);
+            scales[e] |= byte << (8 * s);
+            const uint32_t fl = (row & 31) + 32 * h;
             *(uint4 *)(dst + (((int64_t)(row >> 5) * L.ksteps + ks) * 64 + fl) * 16) = code;
         }
     }
 #pragma unroll
-    for (int e = 0; e < V; ++e)
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const uint32_t row = row0 + e, fl = (row & 31) + 32 * h;
-            *(uint32_t *)(dst + L.off_scales +
-                          (((int64_t)(row >> 5) * L.groups + g) * 64 + fl) * 4) = scales[e][h];
-        }
+    for (int e = 0; e < V; ++e) {
+        const uint32_t row = row0 + e, fl = (row & 31) + 32 * h;
+        *(uint32_t *)(dst + L.off_scales + (((int64_t)(row >> 5) * L.groups + g) * 64 + fl) * 4) =
+            scales[e];
+    }
 }
 
 // ---------------------------------------------------------------------------
@@ -141,7 +140,7 @@ __global__ __launch_bounds__(256) void mx4_quantize_cols_kernel(const char *x, i
 // ---------------------------------------------------------------------------
 template <bool BF>
 __global__ __launch_bounds__(256) void mx4_dequantize_kernel(const uint8_t *src, Mx4Layout L,
-                                                             void *y, int64_t ld, int vec)
+                                                             void *y, int64_t ld)
 {
     const int wv = threadIdx.x >> 6, lane = threadIdx.x & 63;
     const int64_t rt = blockIdx.x / (uint32_t)L.groups, g = blockIdx.x - rt * L.groups;
@@ -175,7 +174,7 @@ __global__ __launch_bounds__(256) void mx4_dequantize_kernel(const uint8_t *src,
             __bf16 w[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) w[e] = to_bf16(v[e]);   // exact: two significant bits
-            if (vec && k + 8 <= L.K) {
+            if (k + 8 <= L.K) {
                 __builtin_memcpy(__builtin_assume_aligned(out, 16), w, 16);
             } else {
 #pragma unroll
@@ -184,7 +183,7 @@ __global__ __launch_bounds__(256) void mx4_dequantize_kernel(const uint8_t *src,
             }
         } else {
             float *out = (float *)y + row * ld + k;
-            if (vec && k + 8 <= L.K) {
+            if (k + 8 <= L.K) {
                 *(float4 *)out = make_float4(v[0], v[1], v[2], v[3]);
                 *(float4 *)(out + 4) = make_float4(v[4], v[5], v[6], v[7]);
             } else {
@@ -192,6 +191,76 @@ __global__ __launch_bounds__(256) void mx4_dequantize_kernel(const uint8_t *src,
                 for (int e = 0; e < 8; ++e)
                     if (k + e < L.K) out[e] = v[e];
             }
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------
+// back to rows that are not 16-byte aligned: a lane writes one aligned piece of
+// 16 bytes, wherever that begins in the row, so its elements come from two
+// neighbouring dwords of codes and may have two scales.  A wave takes eight
+// rows, whose codes share cache lines.  (65,536 x 1,001 bf16 of pitch 1,001:
+// 115 us with an element a store, 53 so; 34 where pieces and rows agree.)
+// ---------------------------------------------------------------------------
+template <bool BF>
+__global__ __launch_bounds__(256) void mx4_dequantize_odd_kernel(const uint8_t *src, Mx4Layout L,
+                                                                 void *y, int64_t ld, int strips)
+{
+    constexpr int ES = BF ? 2 : 4, E = 16 / ES;
+    const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    const int64_t unit = (int64_t)blockIdx.x * 4 + wv, row8 = unit / strips;
+    const int64_t piece = (unit - row8 * strips) * 64 + lane;
+    if (row8 * 8 >= L.rows) return;
+    const int64_t rt = row8 / 4;
+    const int64_t left = L.rows - row8 * 8;
+    const int nrows = left < 8 ? (int)left : 8;
+#pragma unroll 4
+    for (int q = 0; q < nrows; ++q) {
+        const int64_t row = row8 * 8 + q;
+        char *base = (char *)y + row * ld * ES;
+        const int skew = (int)((uintptr_t)base % 16) / ES;      // elements of the piece before the row
+        const int64_t k0 = piece * E - skew;
+        if (k0 >= L.K) continue;
+        // code dwords k/8 of element k, from the one that holds the first
+        const int64_t ka = k0 < 0 ? 0 : k0, d0 = ka / 8;
+        const int64_t d1 = (d0 + 1) * 8 < L.K ? d0 + 1 : d0;
+        auto place = [&](int64_t d) {       // of dword d of the row
+            return ((rt * L.ksteps + (d >> 3)) * 64 + (row & 31) + 32 * (d >> 2 & 1)) * 16 + (d & 3) * 4;
+        };
+        auto scale_at = [&](int64_t d) {
+            const int64_t ks = d >> 3;
+            return (uint32_t)src[L.off_scales + ((rt * L.groups + (ks >> 2)) * 64 + (row & 31) +
+                                                 32 * (d >> 2 & 1)) * 4 + (ks & 3)];
+        };
+        const uint32_t c0 = *(const uint32_t *)(src + place(d0)), c1 = *(const uint32_t *)(src + place(d1));
+        const float s0 = scale_value(scale_at(d0)), s1 = scale_value(scale_at(d1));
+        // element e of the piece is nibble `first + e` of c0, c1
+        const int first = (int)(k0 - d0 * 8);                    // -7 .. 7
+        const uint64_t codes = (uint64_t)c1 << 32 | c0;
+        const uint32_t w = first < 0 ? (uint32_t)(codes << (-4 * first)) : (uint32_t)(codes >> (4 * first));
+        float v[8];
+        floatx2 p = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.0f, 0);
+        v[0] = p[0];
+        v[1] = p[1];
+        p = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.0f, 1);
+        v[2] = p[0];
+        v[3] = p[1];
+        p = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.0f, 2);
+        v[4] = p[0];
+        v[5] = p[1];
+        p = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.0f, 3);
+        v[6] = p[0];
+        v[7] = p[1];
+        typename std::conditional<BF, __bf16, float>::type out[E];
+#pragma unroll
+        for (int e = 0; e < E; ++e) out[e] = v[e] * (first + e < 8 ? s0 : s1);
+        auto *to = (typename std::conditional<BF, __bf16, float>::type *)(base + k0 * ES);
+        if (k0 >= 0 && k0 + E <= L.K) {
+            __builtin_memcpy(__builtin_assume_aligned(to, 16), out, 16);
+        } else {
+#pragma unroll
+            for (int e = 0; e < E; ++e)
+                if (k0 + e >= 0 && k0 + e < L.K) to[e] = out[e];
         }
     }
 }
@@ -227,12 +296,13 @@ hipError_t launch_mx4_quantize(const void *x, bool bf16, int64_t row_stride, int
                                row_stride, L, (uint8_t *)dst, vec);
         return hipGetLastError();
     }
-    // two rows a lane where every pair is aligned
+    // two rows a lane where every pair is aligned and eight waves a CU are left
+    // (1,536 x 11,011 fp32, 1,032 or 2,064 waves: 20 or 16 us)
     const int es = bf16 ? 2 : 4;
-    const bool two = L.rows >= 128 &&
+    const bool two = (L.rows + 127) / 128 * L.groups * 2 >= 2048 &&
                      ((uintptr_t)x | (uint64_t)(col_stride * es)) % (2 * es) == 0;
     const int64_t strips = (L.tiles * 32 + (two ? 127 : 63)) / (two ? 128 : 64);
-    const dim3 grid((unsigned)((strips * L.groups + 3) / 4));
+    const dim3 grid((unsigned)((strips * L.groups * 2 + 3) / 4));
     void (*kernel)(const char *, int64_t, Mx4Layout, uint8_t *) =
         bf16 ? (two ? mx4_quantize_cols_kernel<true, 2> : mx4_quantize_cols_kernel<true, 1>)
              : (two ? mx4_quantize_cols_kernel<false, 2> : mx4_quantize_cols_kernel<false, 1>);
@@ -244,14 +314,18 @@ hipError_t launch_mx4_quantize(const void *x, bool bf16, int64_t row_stride, int
 hipError_t launch_mx4_dequantize(const void *src, const Mx4Layout &L, void *y, bool bf16,
                                  int64_t ld, hipStream_t s)
 {
-    const dim3 grid((unsigned)(L.tiles * L.groups));
-    const int vec = vec16(y, ld, bf16 ? 2 : 4);
-    if (bf16)
-        hipLaunchKernelGGL(mx4_dequantize_kernel<true>, grid, dim3(256), 0, s, (const uint8_t *)src,
-                           L, y, ld, vec);
-    else
-        hipLaunchKernelGGL(mx4_dequantize_kernel<false>, grid, dim3(256), 0, s,
-                           (const uint8_t *)src, L, y, ld, vec);
+    if (!vec16(y, ld, bf16 ? 2 : 4)) {
+        // a row's pieces: one more where it begins inside the first
+        const int each = bf16 ? 8 : 4;
+        const int64_t strips = (L.K + 2 * each - 2) / each / 64 + 1, units = (L.rows + 7) / 8 * strips;
+        hipLaunchKernelGGL((bf16 ? mx4_dequantize_odd_kernel<true> : mx4_dequantize_odd_kernel<false>),
+                           dim3((unsigned)((units + 3) / 4)), dim3(256), 0, s, (const uint8_t *)src, L,
+                           y, ld, (int)strips);
+        return hipGetLastError();
+    }
+    hipLaunchKernelGGL((bf16 ? mx4_dequantize_kernel<true> : mx4_dequantize_kernel<false>),
+                       dim3((unsigned)(L.tiles * L.groups)), dim3(256), 0, s, (const uint8_t *)src, L,
+                       y, ld);
     return hipGetLastError();
 }
 
