@@ -11,6 +11,11 @@
 // carry.  S segments split a long sequence over workgroups the same way, with
 // the maps of all segments from a first launch.
 //
+// With many sequences the memory bounds it: 390 steps x 4,096 sequences x 512
+// channels in bf16 take 1.34 ms, 6.6 GB at 4.9 TB/s, and 3.9 ms with the
+// gradients (18.9 GB at 4.8: the gates are read again, and the states before
+// every chunk are kept instead of all of them).
+//
 // 1 - a^2 comes from a - 1 by a polynomial rather than from a: long memories
 // have a within 1e-4 of 1, and what fp32 leaves of 1 - a is what their states
 // are made of.
@@ -32,6 +37,9 @@ template <> struct RawOf<2> { typedef uint16_t type; };
 template <> struct RawOf<4> { typedef uint32_t type; };
 template <> struct RawOf<8> {
     typedef uint32_t type __attribute__((ext_vector_type(2)));
+};
+template <> struct RawOf<16> {
+    typedef uint32_t type __attribute__((ext_vector_type(4)));
 };
 
 template <bool BF, int V>
@@ -203,7 +211,7 @@ struct Place {
 template <int W> constexpr int GROUP = W == 1 ? 4 : 1;
 
 template <int V, int W>
-__device__ __forceinline__ bool place(const RecurArgs &a, Place<V, W> &p)
+__device__ __forceinline__ bool place(const RecurArgs &a, int segment, Place<V, W> &p)
 {
     const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int unit = blockIdx.x * GROUP<W> + (W == 1 ? wv : 0);
@@ -217,7 +225,7 @@ __device__ __forceinline__ bool place(const RecurArgs &a, Place<V, W> &p)
     int len = a.len ? a.len[p.b] : a.T;
     len = __builtin_amdgcn_readfirstlane(len);
     p.len = len < 0 ? 0 : len > a.T ? a.T : len;
-    p.t0 = blockIdx.y * a.seg_len;
+    p.t0 = segment * a.seg_len;
     p.t1 = a.T - p.t0 < a.seg_len ? a.T : p.t0 + a.seg_len;
     return true;
 }
@@ -268,6 +276,56 @@ __device__ __forceinline__ float join(float2 m, float c)
 
 __device__ __forceinline__ float join_p(float2 m, float P) { return m.x == 0.0f ? 0.0f : m.x * P; }
 
+// The maps of `n` segments after the states c, from segment `first` on, forward
+// or (BACK) backward.  Each wave reduces a share of them, sixteen loads in
+// flight; the shares go through LDS.
+template <int V, int W, bool BACK>
+__device__ __forceinline__ void join_segments(const float2 *maps, int64_t BD, int first, int n,
+                                              float2 (*lds)[W == 1 ? 1 : 64 * V], int w, int lane,
+                                              float (&c)[V])
+{
+    if (n <= 0) return;
+    const int per = (n + W - 1) / W, a0 = w * per, a1 = a0 + per < n ? a0 + per : n;
+    float P[V], H[V];
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+        P[e] = 1.0f;
+        H[e] = W == 1 ? c[e] : 0.0f;
+    }
+#pragma unroll 1
+    for (int k = a0; k < a1; k += 16) {
+        float2 m[16][V];
+#pragma unroll
+        for (int q = 0; q < 16; ++q) {
+            const int at = k + q < a1 ? k + q : a1 - 1;
+            const float2 *from = maps + (int64_t)(BACK ? first - at : first + at) * BD;
+#pragma unroll
+            for (int e = 0; e < V; ++e) m[q][e] = from[e];
+        }
+#pragma unroll
+        for (int q = 0; q < 16; ++q)
+            if (k + q < a1) {
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    H[e] = join(m[q][e], H[e]);
+                    P[e] = join_p(m[q][e], P[e]);
+                }
+            }
+    }
+    if constexpr (W > 1) {
+#pragma unroll
+        for (int e = 0; e < V; ++e) lds[w][lane * V + e] = make_float2(P[e], H[e]);
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < W; ++j)
+#pragma unroll
+            for (int e = 0; e < V; ++e) c[e] = join(lds[j][lane * V + e], c[e]);
+    } else {
+#pragma unroll
+        for (int e = 0; e < V; ++e) c[e] = H[e];
+    }
+}
+
 // ---------------------------------------------------------------------------
 // forward: states (SUMMARY = false), or a segment's map alone
 // ---------------------------------------------------------------------------
@@ -276,7 +334,7 @@ __global__ __launch_bounds__(64 * W * GROUP<W>) void recur_fwd_kernel(RecurArgs 
 {
     __shared__ float2 maps[W == 1 ? 1 : 2][W][W == 1 ? 1 : 64 * V];
     Place<V, W> p;
-    if (!place<V, W>(a, p)) return;
+    if (!place<V, W>(a, blockIdx.y, p)) return;
     float s[V], s2[V], carry[V], carryP[V];
     const int64_t bd = (int64_t)p.b * a.D + p.dc, BD = (int64_t)a.B * a.D;
 #pragma unroll
@@ -287,11 +345,8 @@ __global__ __launch_bounds__(64 * W * GROUP<W>) void recur_fwd_kernel(RecurArgs 
         carryP[e] = 1.0f;
     }
     if constexpr (!SUMMARY)
-        for (int j = 0; j < (int)blockIdx.y; ++j) {
-            const float2 *m = a.maps + j * BD + bd;
-#pragma unroll
-            for (int e = 0; e < V; ++e) carry[e] = join(m[e], carry[e]);
-        }
+        join_segments<V, W, false>(a.maps + bd, BD, 0, (int)blockIdx.y, maps[W == 1 ? 0 : 1], p.w,
+                                   p.lane, carry);
 
     Raw<BF, V> x[C], r[C], i[C];
     auto fetch = [&](int t) {
@@ -415,7 +470,7 @@ __global__ __launch_bounds__(64 * W * GROUP<W>) void recur_bwd_kernel(RecurArgs 
 {
     __shared__ float2 maps[W == 1 ? 1 : 2][W][W == 1 ? 1 : 64 * V];
     Place<V, W> p;
-    if (!place<V, W>(a, p)) return;
+    if (!place<V, W>(a, blockIdx.y, p)) return;
     float s[V], s2[V], carry[V], sum[V];
     const int64_t bd = (int64_t)p.b * a.D + p.dc, BD = (int64_t)a.B * a.D;
 #pragma unroll
@@ -425,11 +480,9 @@ __global__ __launch_bounds__(64 * W * GROUP<W>) void recur_bwd_kernel(RecurArgs 
         carry[e] = a.dh_last ? a.dh_last[bd + e] : 0.0f;
         sum[e] = 0.0f;
     }
-    for (int j = (int)gridDim.y - 1; j > (int)blockIdx.y; --j) {
-        const float2 *m = a.maps + j * BD + bd;
-#pragma unroll
-        for (int e = 0; e < V; ++e) carry[e] = join(m[e], carry[e]);
-    }
+    join_segments<V, W, true>(a.maps + bd, BD, (int)gridDim.y - 1,
+                              (int)(gridDim.y - 1 - blockIdx.y), maps[W == 1 ? 0 : 1], p.w, p.lane,
+                              carry);
     const int tiles = (p.t1 - p.t0 + W * C - 1) / (W * C);
     int t = p.t0 + (tiles - 1) * W * C + p.w * C, par = 0;
 
@@ -573,7 +626,8 @@ __global__ __launch_bounds__(64 * W * GROUP<W>) void recur_bwd_map_kernel(RecurA
 {
     __shared__ float2 maps[W == 1 ? 1 : 2][W][W == 1 ? 1 : 64 * V];
     Place<V, W> p;
-    if (!place<V, W>(a, p)) return;
+    const int segment = blockIdx.y + 1;
+    if (!place<V, W>(a, segment, p)) return;
     float s[V], s2[V], carry[V], carryP[V];
     const int64_t bd = (int64_t)p.b * a.D + p.dc, BD = (int64_t)a.B * a.D;
 #pragma unroll
@@ -653,7 +707,7 @@ __global__ __launch_bounds__(64 * W * GROUP<W>) void recur_bwd_map_kernel(RecurA
     if (!p.live || p.w != 0) return;
 #pragma unroll
     for (int e = 0; e < V; ++e)
-        a.maps[blockIdx.y * BD + bd + e] = make_float2(carryP[e], carry[e]);
+        a.maps[segment * BD + bd + e] = make_float2(carryP[e], carry[e]);
 }
 
 // dlambda_d = sigmoid(lambda) / softplus(lambda) * sum over rows of parts,
@@ -679,37 +733,44 @@ __global__ __launch_bounds__(1024) void recur_lambda_kernel(const float *parts, 
 }
 
 // ---------------------------------------------------------------------------
-// one step
+// one step: a wave has 64 V channels of `rows` sequences, so that lambda's
+// softplus, some hundred instructions, is taken once for all of them
 // ---------------------------------------------------------------------------
 template <bool BF, int V>
-__global__ __launch_bounds__(256) void recur_step_kernel(RecurArgs a)
+__global__ __launch_bounds__(256) void recur_step_kernel(RecurArgs a, int rows)
 {
     const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int unit = blockIdx.x * 4 + wv;
     if (unit >= a.units) return;
-    const int b = unit / a.blocks_d;
-    const int d = (unit - b * a.blocks_d) * 64 * V + (threadIdx.x & 63) * V;
+    const int set = unit / a.blocks_d, b0 = set * rows;
+    const int d = (unit - set * a.blocks_d) * 64 * V + (threadIdx.x & 63) * V;
     if (d >= a.D) return;
-    const bool clear = a.done && a.done[b] != 0;
-    float x[V], r[V], i[V], h[V];
-    unpack<BF, V>(load_row<BF, V>(row_at(a.x, b, 0), d), x);
-    unpack<BF, V>(load_row<BF, V>(row_at(a.r, b, 0), d), r);
-    unpack<BF, V>(load_row<BF, V>(row_at(a.i, b, 0), d), i);
-    const int64_t bd = (int64_t)b * a.D + d;
-    load_f32<V>(a.h0 + bd, h);
+    const int b1 = a.B - b0 < rows ? a.B : b0 + rows;
+    float s[V], s2[V];
 #pragma unroll
     for (int e = 0; e < V; ++e) {
-        const float s = RATE * softplus(a.lam[d + e]);
-        float c, u;
-        gate<BF>(x[e], r[e], i[e], s, s * LOG2E, c, u);
-        h[e] = advance<BF>(c, h[e], u);
+        s[e] = RATE * softplus(a.lam[d + e]);
+        s2[e] = s[e] * LOG2E;
     }
-    if (a.y.p) store_row<BF, V>(row_at(a.y, b, 0), d, h);
-    if (clear) {
+    typedef float state __attribute__((ext_vector_type(V)));
+    for (int b = b0; b < b1; ++b) {
+        float x[V], r[V], i[V], h[V];
+        unpack<BF, V>(load_row<BF, V>(row_at(a.x, b, 0), d), x);
+        unpack<BF, V>(load_row<BF, V>(row_at(a.r, b, 0), d), r);
+        unpack<BF, V>(load_row<BF, V>(row_at(a.i, b, 0), d), i);
+        const state was = load_at<state>(a.h0 + (int64_t)b * a.D, d * 4u);
+        const bool clear = a.done && a.done[b] != 0;
+        state now;
 #pragma unroll
-        for (int e = 0; e < V; ++e) h[e] = 0.0f;
+        for (int e = 0; e < V; ++e) {
+            float c, u;
+            gate<BF>(x[e], r[e], i[e], s[e], s2[e], c, u);
+            h[e] = advance<BF>(c, was[e], u);
+            now[e] = clear ? 0.0f : h[e];
+        }
+        if (a.y.p) store_row<BF, V>(row_at(a.y, b, 0), d, h);
+        store_at(a.h_last + (int64_t)b * a.D, d * 4u, now);
     }
-    store_f32<V>(a.h_last + bd, h);
 }
 
 bool rows_allow(const RecurRows &m, int V, int es)
@@ -731,7 +792,15 @@ struct Shape {
     int64_t units;
 };
 
-// V, W and S by how many waves a call has.
+// Two channels a lane, waves of a workgroup along time (W), segments (S), by
+// how many waves a call has.  Measured (bf16, us, T x B x D; forward):
+//   390 x 4,096 x 512 (32,768 units of one wave)   W = 1       1,340
+//   390 x 64 x 512    (512)     W = 1, 4, 16: 73, 34, 43;  W = 4, S = 2: 46
+//   2,520 x 16 x 256  (64)      W = 4, S = 1, 4, 16, 64: 135, 69, 44, 43; W = 16: 99
+//   24,570 x 1 x 512  (8)       W = 4, S = 16, 64, 128, 256: 151, 61, 53, 54
+//   256 x 64 x 64     (64)      W = 16: 14;  W = 4, S = 8: 14 in two launches
+// A wave's step takes about 60 instructions of four cycles, so few waves on few
+// CUs are slower than reading everything twice on all of them.
 Shape shape_of(int T, int B, int D, bool wide)
 {
     Shape s;
@@ -739,15 +808,18 @@ Shape shape_of(int T, int B, int D, bool wide)
     s.V = wide && D > 64 && units(2) >= 1024 ? 2 : 1;
     s.units = units(s.V);
     s.blocks_d = (D + 64 * s.V - 1) / (64 * s.V);
-    s.W = s.units >= 2048 || T <= C ? 1 : s.units >= 1024 || T <= 4 * C ? 4 : 16;
+    if (s.units >= 2048 || T <= C) s.W = 1;
+    else if (s.units >= 512 || T <= 4 * C || T > 2 * 16 * C) s.W = 4;
+    else s.W = 16;
     s.S = 1;
     const int tile = s.W * C;
-    const int64_t tiles = (T + tile - 1) / tile, waves = s.units * s.W;
-    if (waves < 1024 && tiles > 1) {
-        int64_t want = 1024 / waves;
-        if (want > 64) want = 64;
+    const int64_t tiles = ((int64_t)T + tile - 1) / tile, waves = s.units * s.W;
+    if (s.W == 4 && waves < 1024 && tiles > 1) {
+        int64_t want = 4096 / waves;
+        if (want > 256) want = 256;
         if (want > tiles) want = tiles;
-        s.S = (int)((tiles + (tiles + want - 1) / want - 1) / ((tiles + want - 1) / want));
+        const int64_t per = (tiles + want - 1) / want;
+        s.S = (int)((tiles + per - 1) / per);
     }
     s.seg_len = (int)((tiles + s.S - 1) / s.S) * tile;
     return s;
@@ -758,24 +830,26 @@ void start(RecurArgs &a, const Shape &sh, bool backward, hipStream_t s)
 {
     const dim3 grid((unsigned)((sh.units + GROUP<W> - 1) / GROUP<W>), (unsigned)sh.S);
     const int threads = 64 * W * GROUP<W>;
-    if (!backward) {
-        if (sh.S > 1)
-            hipLaunchKernelGGL((recur_fwd_kernel<BF, V, W, true>),
-                               dim3(grid.x, grid.y - 1), dim3(threads), 0, s, a);
-        hipLaunchKernelGGL((recur_fwd_kernel<BF, V, W, false>), grid, dim3(threads), 0, s, a);
-    } else {
-        if (sh.S > 1)
-            hipLaunchKernelGGL((recur_bwd_map_kernel<BF, V, W>), grid, dim3(threads), 0, s, a);
-        hipLaunchKernelGGL((recur_bwd_kernel<BF, V, W>), grid, dim3(threads), 0, s, a);
+    if constexpr (V == 1 && W == 4) {       // the only ones that split a sequence
+        if (sh.S > 1 && !backward)          // (nobody needs the last segment's map,
+            hipLaunchKernelGGL((recur_fwd_kernel<BF, V, W, true>), dim3(grid.x, grid.y - 1),
+                               dim3(threads), 0, s, a);
+        if (sh.S > 1 && backward)           // or, backward, the first one's)
+            hipLaunchKernelGGL((recur_bwd_map_kernel<BF, V, W>), dim3(grid.x, grid.y - 1),
+                               dim3(threads), 0, s, a);
     }
+    if (backward) hipLaunchKernelGGL((recur_bwd_kernel<BF, V, W>), grid, dim3(threads), 0, s, a);
+    else hipLaunchKernelGGL((recur_fwd_kernel<BF, V, W, false>), grid, dim3(threads), 0, s, a);
 }
 
-template <bool BF, int V>
-void start_w(RecurArgs &a, const Shape &sh, bool backward, hipStream_t s)
+template <bool BF>
+void start_shape(RecurArgs &a, const Shape &sh, bool backward, hipStream_t s)
 {
-    if (sh.W == 1) start<BF, V, 1>(a, sh, backward, s);
-    else if (sh.W == 4) start<BF, V, 4>(a, sh, backward, s);
-    else start<BF, V, 16>(a, sh, backward, s);
+    // (two channels a lane are for many units: never 16 waves of them)
+    if (sh.V == 2) sh.W == 1 ? start<BF, 2, 1>(a, sh, backward, s) : start<BF, 2, 4>(a, sh, backward, s);
+    else if (sh.W == 1) start<BF, 1, 1>(a, sh, backward, s);
+    else if (sh.W == 4) start<BF, 1, 4>(a, sh, backward, s);
+    else start<BF, 1, 16>(a, sh, backward, s);
 }
 
 }  // namespace
@@ -810,13 +884,8 @@ hipError_t launch_recur(RecurArgs &a, bool backward, hipStream_t s)
     const size_t bd = (size_t)a.B * a.D;
     a.maps = (float2 *)a.work;
     a.parts = (float *)((char *)a.work + (sh.S > 1 ? sh.S * bd * sizeof(float2) : 0));
-    if (a.bf16) {
-        if (sh.V == 2) start_w<true, 2>(a, sh, backward, s);
-        else start_w<true, 1>(a, sh, backward, s);
-    } else {
-        if (sh.V == 2) start_w<false, 2>(a, sh, backward, s);
-        else start_w<false, 1>(a, sh, backward, s);
-    }
+    if (a.bf16) start_shape<true>(a, sh, backward, s);
+    else start_shape<false>(a, sh, backward, s);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || !backward) return e;
     hipLaunchKernelGGL(recur_lambda_kernel, dim3((a.D + 15) / 16), dim3(1024), 0, s, a.parts,
@@ -826,17 +895,21 @@ hipError_t launch_recur(RecurArgs &a, bool backward, hipStream_t s)
 
 hipError_t launch_recur_step(RecurArgs &a, hipStream_t s)
 {
-    const int V = allows(a, 2) ? 2 : 1;
+    // four channels a lane where that leaves a wave's lanes full; the states too
+    // have to be aligned to a lane's
+    const auto fits = [&](int V) {
+        return allows(a, V) && ((uintptr_t)a.h0 | (uintptr_t)a.h_last) % (4 * V) == 0;
+    };
+    const int V = a.D >= 256 && fits(4) ? 4 : a.D >= 128 && fits(2) ? 2 : 1;
     a.blocks_d = (a.D + 64 * V - 1) / (64 * V);
-    a.units = a.B * a.blocks_d;
-    const dim3 grid((a.units + 3) / 4);
-    if (a.bf16) {
-        if (V == 2) hipLaunchKernelGGL((recur_step_kernel<true, 2>), grid, dim3(256), 0, s, a);
-        else hipLaunchKernelGGL((recur_step_kernel<true, 1>), grid, dim3(256), 0, s, a);
-    } else {
-        if (V == 2) hipLaunchKernelGGL((recur_step_kernel<false, 2>), grid, dim3(256), 0, s, a);
-        else hipLaunchKernelGGL((recur_step_kernel<false, 1>), grid, dim3(256), 0, s, a);
-    }
+    // sequences a wave: as many as leave 16 waves a CU, at most 16
+    const int64_t all = (int64_t)a.B * a.blocks_d;
+    const int rows = (int)(all < 8192 ? 1 : all > 16 * 4096 ? 16 : all / 4096);
+    a.units = (a.B + rows - 1) / rows * a.blocks_d;
+    void (*kernel)(RecurArgs, int) =
+        a.bf16 ? (V == 4 ? recur_step_kernel<true, 4> : V == 2 ? recur_step_kernel<true, 2> : recur_step_kernel<true, 1>)
+               : (V == 4 ? recur_step_kernel<false, 4> : V == 2 ? recur_step_kernel<false, 2> : recur_step_kernel<false, 1>);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)((a.units + 3) / 4)), dim3(256), 0, s, a, rows);
     return hipGetLastError();
 }
 
