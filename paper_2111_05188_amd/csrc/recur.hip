@@ -433,6 +433,7 @@ __global__ __launch_bounds__(64 * W * GROUP<W>) void recur_fwd_kernel(RecurArgs 
             if (a.saved && p.live && t < a.T)
                 store_f32<V>(a.saved + (int64_t)(t / C) * BD + bd, h);
             char *out = row_at(a.y, p.b, t);
+            const bool stored = p.live && a.y.p;
 #pragma unroll
             for (int k = 0; k < C; ++k) {
                 float y[V];
@@ -442,7 +443,7 @@ __global__ __launch_bounds__(64 * W * GROUP<W>) void recur_fwd_kernel(RecurArgs 
                     y[e] = plain || k < nv ? h[e] : 0.0f;
                     if (!plain && (clear >> k & 1)) h[e] = 0.0f;
                 }
-                if (p.live && t + k < a.T) store_row<BF, V>(out + k * a.y.st, p.dc, y);
+                if (stored && t + k < a.T) store_row<BF, V>(out + k * a.y.st, p.dc, y);
             }
             if constexpr (W == 1) {
 #pragma unroll
@@ -870,9 +871,9 @@ size_t recur_workspace_bytes(int T, int B, int D)
 
 bool recur_fits(int T, int B, int D)
 {
-    // step numbers past the last chunk in 32 bits; workgroups of 256 threads in
-    // a 32-bit grid
-    return T <= 1 << 30 && (int64_t)B * ((D + 63) / 64) <= (int64_t)1 << 25;
+    // step numbers past the last chunk and a row's bytes in 32 bits; workgroups
+    // of 256 threads in a 32-bit grid
+    return T <= 1 << 30 && D <= 1 << 24 && (int64_t)B * ((D + 63) / 64) <= (int64_t)1 << 25;
 }
 
 hipError_t launch_recur(RecurArgs &a, bool backward, hipStream_t s)

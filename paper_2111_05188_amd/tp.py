@@ -672,6 +672,7 @@ class RecurT:
         self.T, self.B, self.D = T, B, lam.shape[0]
         self.s = Recur(T, B, self.D, TP_BF16 if dtype == torch.bfloat16 else TP_F32, _ptr(lam),
                        _ptr(done), _ptr(lens))
+        self.saved_count = self._bytes(load().tp_recur_saved_bytes) // 4
 
     def _bytes(self, f) -> int:
         nb = f(C.byref(self.s))
@@ -685,62 +686,78 @@ class RecurT:
 
     def saved(self) -> torch.Tensor:
         """The states recur_forward keeps for recur_backward."""
-        return torch.empty(self._bytes(load().tp_recur_saved_bytes) // 4, dtype=torch.float32,
-                           device=self.lam.device)
+        return torch.empty(self.saved_count, dtype=torch.float32, device=self.lam.device)
 
-    def rows(self, t: torch.Tensor | None):
-        """A [T][B][D] tensor (any strides over steps and sequences)."""
-        if t is None:
-            return None
-        assert t.shape == (self.T, self.B, self.D) and t.dtype == self.dtype
-        assert self.D == 1 or t.stride(2) == 1
-        return C.byref(Rows(t.data_ptr(), t.stride(0), t.stride(1)))
+    def rows(self, *ts):
+        """tp_rows of [T][B][D] tensors (any strides over steps and sequences), side by side;
+        None: not there."""
+        shape, dtype, v = (self.T, self.B, self.D), self.dtype, []
+        for t in ts:
+            if t is None:
+                v += (0, 0, 0)
+                continue
+            st, sb, sd = t.stride()
+            assert t.shape == shape and t.dtype is dtype and (sd == 1 or self.D == 1)
+            v += (t.data_ptr(), st, sb)
+        return _rows(v)
 
     def state(self, t: torch.Tensor | None):
         if t is None:
             return None
-        assert t.shape == (self.B, self.D) and t.dtype == torch.float32 and t.is_contiguous()
+        assert t.shape == (self.B, self.D) and t.dtype is torch.float32 and t.is_contiguous()
         return t.data_ptr()
+
+
+def _rows(v):
+    """An array of tp_rows (pointer, two strides each) and the addresses of its elements."""
+    a = (C.c_int64 * len(v))(*v)
+    p = C.addressof(a)
+    return a, range(p, p + 8 * len(v), 24)
 
 
 def recur_forward(rc: RecurT, x, r, i, y, work, h0=None, h_last=None, saved=None, stream=None):
     """y [T][B][D] (or None) and h_last [B][D] of x, r, i [T][B][D]; saved
     (rc.saved()) keeps what recur_backward needs."""
-    assert saved is None or saved.numel() * 4 >= rc._bytes(load().tp_recur_saved_bytes)
-    _check(load().tp_recur_forward(C.byref(rc.s), rc.rows(x), rc.rows(r), rc.rows(i),
-                                   rc.state(h0), rc.rows(y), rc.state(h_last), _ptr(saved),
-                                   _ptr(work), work.numel(), _stream(stream)))
+    assert saved is None or saved.numel() >= rc.saved_count
+    keep, (px, pr, pi, py) = rc.rows(x, r, i, y)
+    _check(load().tp_recur_forward(C.byref(rc.s), px, pr, pi, rc.state(h0), py, rc.state(h_last),
+                                   _ptr(saved), work.data_ptr(), work.numel(), _stream(stream)))
 
 
 def recur_backward(rc: RecurT, x, r, i, saved, dy, dx, dr, di, dlam, work, dh_last=None,
                    dh0=None, stream=None):
     """Gradients of recur_forward's inputs into dx, dr, di [T][B][D], dlam [D]
     and dh0 [B][D]."""
-    assert saved.numel() * 4 >= rc._bytes(load().tp_recur_saved_bytes)
-    assert dlam.shape == (rc.D,) and dlam.dtype == torch.float32 and dlam.is_contiguous()
-    _check(load().tp_recur_backward(C.byref(rc.s), rc.rows(x), rc.rows(r), rc.rows(i),
-                                    _ptr(saved), rc.rows(dy), rc.state(dh_last), rc.rows(dx),
-                                    rc.rows(dr), rc.rows(di), _ptr(dlam), rc.state(dh0),
-                                    _ptr(work), work.numel(), _stream(stream)))
+    assert saved.numel() >= rc.saved_count
+    assert dlam.shape == (rc.D,) and dlam.dtype is torch.float32 and dlam.is_contiguous()
+    keep, (px, pr, pi, pdy, pdx, pdr, pdi) = rc.rows(x, r, i, dy, dx, dr, di)
+    _check(load().tp_recur_backward(C.byref(rc.s), px, pr, pi, saved.data_ptr(), pdy,
+                                    rc.state(dh_last), pdx, pdr, pdi, dlam.data_ptr(),
+                                    rc.state(dh0), work.data_ptr(), work.numel(),
+                                    _stream(stream)))
 
 
 def recur_step(x, r, i, lam, h, h_out, y=None, done=None, stream=None):
     """One bar: h_out [B][D] fp32 (may be h) and y [B][D] from x, r, i [B][D]
     and the states h; done [B] uint8 clears states after the step."""
-    B, D = h.shape
-    assert h.dtype == h_out.dtype == lam.dtype == torch.float32 and lam.shape == (D,)
-    assert h_out.shape == h.shape and h.is_contiguous() and h_out.is_contiguous()
-    assert lam.is_contiguous()
+    B, D = shape = h.shape
+    f32, dtype, v = torch.float32, x.dtype, []
+    assert h.dtype is f32 and h_out.dtype is f32 and lam.dtype is f32 and lam.shape == (D,)
+    assert h_out.shape == shape and h.is_contiguous() and h_out.is_contiguous()
+    assert lam.is_contiguous() and (dtype is f32 or dtype is torch.bfloat16)
     assert done is None or (done.shape == (B,) and done.element_size() == 1
                             and done.is_contiguous())
-    s = Recur(1, B, D, _dtype_code(x), _ptr(lam), _ptr(done), None)
-
-    def rows(t):
-        assert t.shape == (B, D) and t.dtype == x.dtype and (D == 1 or t.stride(1) == 1)
-        return C.byref(Rows(t.data_ptr(), 0, t.stride(0)))
-
-    _check(load().tp_recur_step(C.byref(s), rows(x), rows(r), rows(i), _ptr(h), _ptr(h_out),
-                                None if y is None else rows(y), _stream(stream)))
+    for t in (x, r, i, y):
+        if t is None:
+            v += (0, 0, 0)
+            continue
+        sb, sd = t.stride()
+        assert t.shape == shape and t.dtype is dtype and (sd == 1 or D == 1)
+        v += (t.data_ptr(), 0, sb)
+    keep, (px, pr, pi, py) = _rows(v)
+    s = Recur(1, B, D, TP_F32 if dtype is f32 else TP_BF16, lam.data_ptr(), _ptr(done), None)
+    _check(load().tp_recur_step(C.byref(s), px, pr, pi, h.data_ptr(), h_out.data_ptr(), py,
+                                _stream(stream)))
 
 
 # --------------------------------------------------------------------------

@@ -305,6 +305,18 @@ def test_step_equals_the_sequence_kernel():
     assert torch.equal(h, last)
 
 
+@pytest.mark.parametrize("T,B", [(40, 3), (300, 2), (20, 2100)])
+def test_only_the_last_states(T, B):
+    """y left out: the last states and what the gradients need are those of a call with it."""
+    c = Case(T, B, 66, torch.bfloat16, 0.05, True, seed=20)
+    saved, kept = c.rc.saved().zero_(), c.rc.saved().zero_()
+    y, last = c.forward(saved)
+    only = torch.empty_like(last)
+    tp.recur_forward(c.rc, *c.split(c.gates), None, c.work, h0=dev(c.h0), h_last=only, saved=kept)
+    torch.cuda.synchronize()
+    assert torch.equal(only, last) and torch.equal(kept, saved)
+
+
 def test_segments_continue():
     """A sequence in two calls, the state handed on, equals one call to rounding."""
     c = Case(200, 3, 64, torch.float32, 0.02, seed=15)

@@ -48,6 +48,7 @@ def test_sizes():
         _refused(_forward(_cfg(**bad)), "recurrence")
     assert L.tp_recur_workspace_bytes(None) == 0
     _refused(_forward(_cfg(B=1 << 30, D=64)), "grid", tp.TP_EUNSUPPORTED)
+    _refused(_forward(_cfg(B=1, D=(1 << 24) + 1)), "grid", tp.TP_EUNSUPPORTED)
     _refused(_forward(_cfg(T=(1 << 30) + 1, B=1, D=1)), "grid", tp.TP_EUNSUPPORTED)
 
 
