@@ -634,7 +634,7 @@ int tp_recur_step(const tp_recur *cfg, const tp_rows *x, const tp_rows *r, const
  */
 typedef struct tp_mx4 {
     void *data;
-    int64_t rows, K;       /* 1 .. 2^29 each                                */
+    int64_t rows, K;       /* 1 .. 2^27 each                                */
 } tp_mx4;
 
 typedef enum { TP_ACT_NONE = 0, TP_ACT_TANH = 1 } tp_act;

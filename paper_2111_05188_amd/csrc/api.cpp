@@ -313,12 +313,12 @@ int recur_args(const tp_recur *c, const tp_rows *x, const tp_rows *r, const tp_r
 // ---------------------------------------------------------------------------
 // 4-bit matrices
 // ---------------------------------------------------------------------------
-constexpr int64_t MX4_MOST = (int64_t)1 << 29;
+constexpr int64_t MX4_MOST = (int64_t)1 << 27;    // (a row tile's bytes in 32 bits)
 
 int check_mx4_size(int64_t rows, int64_t K, const char *name)
 {
     if (rows < 1 || K < 1 || rows > MX4_MOST || K > MX4_MOST)
-        return fail(TP_EINVAL, "4-bit %s: %lld rows of %lld elements (1 .. 2^29 each)", name,
+        return fail(TP_EINVAL, "4-bit %s: %lld rows of %lld elements (1 .. 2^27 each)", name,
                     (long long)rows, (long long)K);
     const Mx4Layout L = mx4_layout(rows, K);
     if (L.tiles * L.groups > 1 << 22)   // workgroups of 256 threads in a 32-bit grid

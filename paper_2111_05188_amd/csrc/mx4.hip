@@ -135,6 +135,23 @@ __global__ __launch_bounds__(256) void mx4_quantize_cols_kernel(const char *x, i
     }
 }
 
+// eight codes to values, before their scale
+__device__ __forceinline__ void values_of(uint32_t c, float *v)
+{
+    floatx2 p = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, 1.0f, 0);
+    v[0] = p[0];
+    v[1] = p[1];
+    p = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, 1.0f, 1);
+    v[2] = p[0];
+    v[3] = p[1];
+    p = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, 1.0f, 2);
+    v[4] = p[0];
+    v[5] = p[1];
+    p = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, 1.0f, 3);
+    v[6] = p[0];
+    v[7] = p[1];
+}
+
 // ---------------------------------------------------------------------------
 // back to rows: the places of mx4_quantize_rows_kernel
 // ---------------------------------------------------------------------------
@@ -155,18 +172,7 @@ __global__ __launch_bounds__(256) void mx4_dequantize_kernel(const uint8_t *src,
         const uint32_t c = *(const uint32_t *)(src + ((rt * L.ksteps + ks) * 64 + fl) * 16 + (q & 3) * 4);
         const float sc = scale_value(scales >> (8 * s) & 255u);
         float v[8];
-        floatx2 p = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, 1.0f, 0);
-        v[0] = p[0];
-        v[1] = p[1];
-        p = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, 1.0f, 1);
-        v[2] = p[0];
-        v[3] = p[1];
-        p = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, 1.0f, 2);
-        v[4] = p[0];
-        v[5] = p[1];
-        p = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, 1.0f, 3);
-        v[6] = p[0];
-        v[7] = p[1];
+        values_of(c, v);
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] *= sc;
         if constexpr (BF) {
@@ -195,72 +201,110 @@ __global__ __launch_bounds__(256) void mx4_dequantize_kernel(const uint8_t *src,
     }
 }
 
+// A row tile's codes and scales by row of the tile and dword of eight elements
+struct TileReader {
+    const uint8_t *codes, *scales;
+
+    __device__ __forceinline__ TileReader(const uint8_t *src, const Mx4Layout &L, int64_t rt)
+        : codes(src + rt * L.ksteps * 1024), scales(src + L.off_scales + rt * L.groups * 256)
+    {
+    }
+    __device__ __forceinline__ uint32_t code(uint32_t r, uint32_t d) const
+    {
+        return load_at<uint32_t>(codes, (d >> 3) * 1024 + (d >> 2 & 1) * 512 + r * 16 + (d & 3) * 4);
+    }
+    __device__ __forceinline__ float scale(uint32_t r, uint32_t d) const
+    {
+        return scale_value(load_at<uint8_t>(
+            scales, (d >> 5) * 256 + (d >> 2 & 1) * 128 + r * 4 + (d >> 3 & 3)));
+    }
+};
+
 // ---------------------------------------------------------------------------
-// back to rows that are not 16-byte aligned: a lane writes one aligned piece of
-// 16 bytes, wherever that begins in the row, so its elements come from two
-// neighbouring dwords of codes and may have two scales.  A wave takes eight
-// rows, whose codes share cache lines.  (65,536 x 1,001 bf16 of pitch 1,001:
-// 115 us with an element a store, 53 so; 34 where pieces and rows agree.)
+// back to rows that follow one another without being 16-byte aligned: eight
+// rows begin at a multiple of 16 bytes (if y does), so a workgroup takes eight,
+// whose codes share cache lines, and writes them in whole pieces of 16 bytes.
+// A piece's elements come from two neighbouring dwords of codes, which may have
+// two scales, and where it passes a row's end from the next row's first.
+// (65,536 x 1,001 bf16: 115 us with an element a store, 54 with pieces that end
+// at the rows' ends, 48 so; 34 where pieces and rows agree.)
+// ---------------------------------------------------------------------------
+template <bool BF>
+__global__ __launch_bounds__(256) void mx4_dequantize_flat_kernel(const uint8_t *src, Mx4Layout L,
+                                                                  void *y)
+{
+    typedef typename std::conditional<BF, __bf16, float>::type T;
+    constexpr uint32_t E = 16 / sizeof(T);
+    const uint32_t K = (uint32_t)L.K, r0 = (blockIdx.x & 3) * 8;
+    const int64_t row0 = (int64_t)blockIdx.x * 8, left = L.rows - row0;
+    const uint32_t nrows = left < 8 ? (uint32_t)left : 8;
+    const TileReader tile(src, L, blockIdx.x >> 2);
+    T *out = (T *)y + row0 * K;
+    for (uint32_t p = blockIdx.y * 256 + threadIdx.x; p * E < nrows * K; p += 256 * gridDim.y) {
+        const uint32_t q = p * E / K, k = p * E - q * K, r = r0 + q;
+        const uint32_t d0 = k / 8, d1 = (d0 + 1) * 8 < K ? d0 + 1 : d0, first = k % 8;
+        const uint64_t codes = (uint64_t)tile.code(r, d1) << 32 | tile.code(r, d0);
+        const float s0 = tile.scale(r, d0), s1 = tile.scale(r, d1);
+        uint32_t w = (uint32_t)(codes >> (4 * first));
+        const uint32_t here = K - k;                    // elements up to the row's end
+        float s2 = 0.0f;
+        if (here < E && q + 1 < nrows) {
+            w = (w & ((1u << (4 * here)) - 1)) | tile.code(r + 1, 0) << (4 * here);
+            s2 = tile.scale(r + 1, 0);
+        }
+        float v[8];
+        values_of(w, v);
+        T z[E];
+#pragma unroll
+        for (uint32_t e = 0; e < E; ++e) z[e] = (T)(v[e] * (e >= here ? s2 : first + e < 8 ? s0 : s1));
+        if (here >= E || q + 1 < nrows) {
+            __builtin_memcpy(__builtin_assume_aligned(out + p * E, 16), z, 16);
+        } else {
+#pragma unroll
+            for (uint32_t e = 0; e < E; ++e)
+                if (e < here) out[p * E + e] = z[e];
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------
+// back to rows of any pitch and alignment: the same a row at a time, its first
+// and last piece by elements; a wave takes eight rows
 // ---------------------------------------------------------------------------
 template <bool BF>
 __global__ __launch_bounds__(256) void mx4_dequantize_odd_kernel(const uint8_t *src, Mx4Layout L,
                                                                  void *y, int64_t ld, int strips)
 {
-    constexpr int ES = BF ? 2 : 4, E = 16 / ES;
+    typedef typename std::conditional<BF, __bf16, float>::type T;
+    constexpr int ES = sizeof(T), E = 16 / ES;
     const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-    const int64_t unit = (int64_t)blockIdx.x * 4 + wv, row8 = unit / strips;
-    const int64_t piece = (unit - row8 * strips) * 64 + lane;
-    if (row8 * 8 >= L.rows) return;
-    const int64_t rt = row8 / 4;
-    const int64_t left = L.rows - row8 * 8;
+    const uint32_t unit = blockIdx.x * 4 + wv, row8 = unit / (uint32_t)strips;
+    const int piece = (int)(unit - row8 * strips) * 64 + lane, K = (int)L.K;
+    const int64_t left = L.rows - (int64_t)row8 * 8;
+    if (left <= 0) return;
+    const TileReader tile(src, L, row8 / 4);
     const int nrows = left < 8 ? (int)left : 8;
-#pragma unroll 4
     for (int q = 0; q < nrows; ++q) {
-        const int64_t row = row8 * 8 + q;
-        char *base = (char *)y + row * ld * ES;
-        const int skew = (int)((uintptr_t)base % 16) / ES;      // elements of the piece before the row
-        const int64_t k0 = piece * E - skew;
-        if (k0 >= L.K) continue;
-        // code dwords k/8 of element k, from the one that holds the first
-        const int64_t ka = k0 < 0 ? 0 : k0, d0 = ka / 8;
-        const int64_t d1 = (d0 + 1) * 8 < L.K ? d0 + 1 : d0;
-        auto place = [&](int64_t d) {       // of dword d of the row
-            return ((rt * L.ksteps + (d >> 3)) * 64 + (row & 31) + 32 * (d >> 2 & 1)) * 16 + (d & 3) * 4;
-        };
-        auto scale_at = [&](int64_t d) {
-            const int64_t ks = d >> 3;
-            return (uint32_t)src[L.off_scales + ((rt * L.groups + (ks >> 2)) * 64 + (row & 31) +
-                                                 32 * (d >> 2 & 1)) * 4 + (ks & 3)];
-        };
-        const uint32_t c0 = *(const uint32_t *)(src + place(d0)), c1 = *(const uint32_t *)(src + place(d1));
-        const float s0 = scale_value(scale_at(d0)), s1 = scale_value(scale_at(d1));
-        // element e of the piece is nibble `first + e` of c0, c1
-        const int first = (int)(k0 - d0 * 8);                    // -7 .. 7
-        const uint64_t codes = (uint64_t)c1 << 32 | c0;
-        const uint32_t w = first < 0 ? (uint32_t)(codes << (-4 * first)) : (uint32_t)(codes >> (4 * first));
+        const uint32_t r = (row8 & 3) * 8 + q;
+        char *base = (char *)y + ((int64_t)row8 * 8 + q) * ld * ES;
+        const int k0 = piece * E - (int)((uintptr_t)base % 16) / ES;    // the piece's first element
+        if (k0 >= K) continue;
+        const int d0 = (k0 < 0 ? 0 : k0) / 8, d1 = (d0 + 1) * 8 < K ? d0 + 1 : d0;
+        const int first = k0 - d0 * 8;                                  // -7 .. 7
+        const uint64_t codes = (uint64_t)tile.code(r, d1) << 32 | tile.code(r, d0);
+        const float s0 = tile.scale(r, d0), s1 = tile.scale(r, d1);
         float v[8];
-        floatx2 p = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.0f, 0);
-        v[0] = p[0];
-        v[1] = p[1];
-        p = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.0f, 1);
-        v[2] = p[0];
-        v[3] = p[1];
-        p = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.0f, 2);
-        v[4] = p[0];
-        v[5] = p[1];
-        p = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.0f, 3);
-        v[6] = p[0];
-        v[7] = p[1];
-        typename std::conditional<BF, __bf16, float>::type out[E];
+        values_of(first < 0 ? (uint32_t)(codes << (-4 * first)) : (uint32_t)(codes >> (4 * first)), v);
+        T z[E];
 #pragma unroll
-        for (int e = 0; e < E; ++e) out[e] = v[e] * (first + e < 8 ? s0 : s1);
-        auto *to = (typename std::conditional<BF, __bf16, float>::type *)(base + k0 * ES);
-        if (k0 >= 0 && k0 + E <= L.K) {
-            __builtin_memcpy(__builtin_assume_aligned(to, 16), out, 16);
+        for (int e = 0; e < E; ++e) z[e] = (T)(v[e] * (first + e < 8 ? s0 : s1));
+        T *to = (T *)(base + (int64_t)k0 * ES);
+        if (k0 >= 0 && k0 + E <= K) {
+            __builtin_memcpy(__builtin_assume_aligned(to, 16), z, 16);
         } else {
 #pragma unroll
             for (int e = 0; e < E; ++e)
-                if (k0 + e >= 0 && k0 + e < L.K) to[e] = out[e];
+                if (k0 + e >= 0 && k0 + e < K) to[e] = z[e];
         }
     }
 }
@@ -314,6 +358,15 @@ hipError_t launch_mx4_quantize(const void *x, bool bf16, int64_t row_stride, int
 hipError_t launch_mx4_dequantize(const void *src, const Mx4Layout &L, void *y, bool bf16,
                                  int64_t ld, hipStream_t s)
 {
+    // (eight rows of under 2^32 elements, a piece in two rows at most)
+    if (!vec16(y, ld, bf16 ? 2 : 4) && ld == L.K && L.K >= 8 && (uintptr_t)y % 16 == 0) {
+        const int64_t pieces = 8 * L.K / (bf16 ? 8 : 4), most = (pieces + 511) / 512;
+        const int64_t parts = most < 65535 ? most : 65535;      // two pieces a thread
+        hipLaunchKernelGGL((bf16 ? mx4_dequantize_flat_kernel<true> : mx4_dequantize_flat_kernel<false>),
+                           dim3((unsigned)((L.rows + 7) / 8), (unsigned)parts), dim3(256), 0, s,
+                           (const uint8_t *)src, L, y);
+        return hipGetLastError();
+    }
     if (!vec16(y, ld, bf16 ? 2 : 4)) {
         // a row's pieces: one more where it begins inside the first
         const int each = bf16 ? 8 : 4;

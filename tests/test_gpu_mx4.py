@@ -68,6 +68,24 @@ def test_quantize(shape, layout, dtype):
 
 
 @pytest.mark.parametrize("dtype", BOTH)
+@pytest.mark.parametrize("shape", SHAPES + [(17, 8), (50, 9), (9, 2047), (100, 63)])
+def test_dequantize_to_rows_of_any_pitch(shape, dtype):
+    """Rows one after the other, rows of a pitch, rows that begin anywhere: the same values, and
+    nothing else is written."""
+    rows, K = shape
+    m = tp.mx4_quantize(matrix(rows, K, dtype, 7))
+    want = mx4.values(host(matrix(rows, K, dtype, 7)))
+    for pitch, begin in ((K, 0), (K, 1), (K + 1, 0), (K + 5, 3), (-(-K // 8) * 8, 0)):
+        flat = torch.full((rows * pitch + 16,), 7.0, dtype=dtype, device="cuda")
+        y = flat[begin:].as_strided((rows, K), (pitch, 1), begin)
+        tp.mx4_dequantize(m, y)
+        torch.cuda.synchronize()
+        assert np.array_equal(host(y), want), (pitch, begin)
+        y.fill_(7.0)
+        assert (flat == 7.0).all(), (pitch, begin)
+
+
+@pytest.mark.parametrize("dtype", BOTH)
 @pytest.mark.parametrize("layout", ["rows", "turned"])
 def test_ties_and_special_blocks(layout, dtype):
     x = np.zeros((40, 96), np.float32)

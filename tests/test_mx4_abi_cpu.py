@@ -24,7 +24,7 @@ def test_bytes():
         assert L.tp_mx4_bytes(rows, K) == 0 and "rows of" in tp.last_error()
         assert L.tp_mx4_workspace_bytes(rows, 4, K) == 0
     assert L.tp_mx4_workspace_bytes(4, 0, 4) == 0
-    assert L.tp_mx4_bytes(1 << 28, 1 << 28) == 0 and "grid" in tp.last_error()
+    assert L.tp_mx4_bytes(1 << 27, 1 << 27) == 0 and "grid" in tp.last_error()
     with pytest.raises(tp.TPError):
         tp.mx4_bytes(0, 1)
     assert L.tp_mx4_workspace_bytes(64, 100, 1001) >= tp.mx4_bytes(64, 1001)
@@ -65,8 +65,8 @@ def test_products_refuse():
     _refused(mm(work=None), "workspace")
     _refused(mm(work=X + 64), "workspace")
     _refused(mm(nb=0), "needed")
-    big = C.byref(tp.Mx4(X, 1 << 29, 64))
-    _refused(mm(a=big, w=big, ldy=1 << 29), "grid", tp.TP_EUNSUPPORTED)
+    big = C.byref(tp.Mx4(X, 1 << 27, 64))
+    _refused(mm(a=big, w=big, ldy=1 << 27), "grid", tp.TP_EUNSUPPORTED)
     lin = dict(x=X, xd=tp.TP_BF16, M=4, ldx=64, w=w, bias=None, act=0, y=X, dtype=tp.TP_F32, ldy=5,
                work=X, nb=1 << 30, s=None)
 
