@@ -2,5 +2,6 @@
 
 ``tp``      : Python binding of the C ABI in include/tp.h (libtp.so).
 ``problem`` : device-side setup of a workload (market, state, actor, store).
+``memory``  : a policy's memory over bars (4-bit product and gated recurrence).
 ``build``   : compiles libtp.so for gfx950.
 """
