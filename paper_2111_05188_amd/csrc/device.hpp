@@ -173,20 +173,23 @@ __device__ __forceinline__ void workgroup_lds_barrier()
 // first and steps a 64-bit vector address per access.
 #define TP_GLOBAL __attribute__((address_space(1)))
 
-template <class T>
+// ONCE: the access is not to displace what the caches hold.
+template <class T, bool ONCE = false>
 __device__ __forceinline__ T load_at(const void *base, uint32_t off)
 {
     const TP_GLOBAL char *p = (const TP_GLOBAL char *)base;
     asm("" : "+s"(p));
+    if constexpr (ONCE) return __builtin_nontemporal_load((const TP_GLOBAL T *)(p + off));
     return *(const TP_GLOBAL T *)(p + off);
 }
 
-template <class T>
+template <bool ONCE = false, class T>
 __device__ __forceinline__ void store_at(void *base, uint32_t off, T v)
 {
     TP_GLOBAL char *p = (TP_GLOBAL char *)base;
     asm("" : "+s"(p));
-    *(TP_GLOBAL T *)(p + off) = v;
+    if constexpr (ONCE) __builtin_nontemporal_store(v, (TP_GLOBAL T *)(p + off));
+    else *(TP_GLOBAL T *)(p + off) = v;
 }
 
 // Sum over the 64 lanes (same value returned to every lane).

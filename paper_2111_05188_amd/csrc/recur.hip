@@ -45,10 +45,10 @@ template <> struct RawOf<16> {
 template <bool BF, int V>
 using Raw = typename RawOf<(BF ? 2 : 4) * V>::type;
 
-template <bool BF, int V>
+template <bool BF, int V, bool ONCE = false>
 __device__ __forceinline__ Raw<BF, V> load_row(const void *row, uint32_t d)
 {
-    return load_at<Raw<BF, V>>(row, d * (BF ? 2u : 4u));
+    return load_at<Raw<BF, V>, ONCE>(row, d * (BF ? 2u : 4u));
 }
 
 template <bool BF, int V>
@@ -66,7 +66,7 @@ __device__ __forceinline__ void unpack(const Raw<BF, V> &raw, float *v)
 }
 
 // bf16: round to nearest even, the only rounding of an output
-template <bool BF, int V>
+template <bool BF, int V, bool ONCE = false>
 __device__ __forceinline__ void store_row(void *row, uint32_t d, const float *v)
 {
     Raw<BF, V> raw;
@@ -78,7 +78,7 @@ __device__ __forceinline__ void store_row(void *row, uint32_t d, const float *v)
     } else {
         __builtin_memcpy(&raw, v, sizeof raw);
     }
-    store_at(row, d * (BF ? 2u : 4u), raw);
+    store_at<ONCE>(row, d * (BF ? 2u : 4u), raw);
 }
 
 template <int V>
@@ -255,14 +255,14 @@ __device__ __forceinline__ char *row_at(const RecurRows &m, int b, int t)
 }
 
 // rows t .. t + C - 1 of sequence b, the last one of all again past T
-template <bool BF, int V>
+template <bool BF, int V, bool ONCE = false>
 __device__ __forceinline__ void load_chunk(const RecurRows &m, int b, int t, int T, uint32_t d,
                                            Raw<BF, V> *raw)
 {
     const char *row = row_at(m, b, t < T ? t : T - 1);
 #pragma unroll
     for (int k = 0; k < C; ++k) {
-        raw[k] = load_row<BF, V>(row, d);
+        raw[k] = load_row<BF, V, ONCE>(row, d);
         row += t + k + 1 < T ? m.st : 0;
     }
 }
@@ -329,7 +329,7 @@ __device__ __forceinline__ void join_segments(const float2 *maps, int64_t BD, in
 // ---------------------------------------------------------------------------
 // forward: states (SUMMARY = false), or a segment's map alone
 // ---------------------------------------------------------------------------
-template <bool BF, int V, int W, bool SUMMARY>
+template <bool BF, int V, int W, bool SUMMARY, bool ONCE>
 __global__ __launch_bounds__(64 * W * GROUP<W>) void recur_fwd_kernel(RecurArgs a)
 {
     __shared__ float2 maps[W == 1 ? 1 : 2][W][W == 1 ? 1 : 64 * V];
@@ -350,9 +350,9 @@ __global__ __launch_bounds__(64 * W * GROUP<W>) void recur_fwd_kernel(RecurArgs 
 
     Raw<BF, V> x[C], r[C], i[C];
     auto fetch = [&](int t) {
-        load_chunk<BF, V>(a.x, p.b, t, a.T, p.dc, x);
-        load_chunk<BF, V>(a.r, p.b, t, a.T, p.dc, r);
-        load_chunk<BF, V>(a.i, p.b, t, a.T, p.dc, i);
+        load_chunk<BF, V, ONCE>(a.x, p.b, t, a.T, p.dc, x);
+        load_chunk<BF, V, ONCE>(a.r, p.b, t, a.T, p.dc, r);
+        load_chunk<BF, V, ONCE>(a.i, p.b, t, a.T, p.dc, i);
     };
     int t = p.t0 + p.w * C, par = 0;
     fetch(t);
@@ -443,7 +443,7 @@ __global__ __launch_bounds__(64 * W * GROUP<W>) void recur_fwd_kernel(RecurArgs 
                     y[e] = plain || k < nv ? h[e] : 0.0f;
                     if (!plain && (clear >> k & 1)) h[e] = 0.0f;
                 }
-                if (stored && t + k < a.T) store_row<BF, V>(out + k * a.y.st, p.dc, y);
+                if (stored && t + k < a.T) store_row<BF, V, ONCE>(out + k * a.y.st, p.dc, y);
             }
             if constexpr (W == 1) {
 #pragma unroll
@@ -466,7 +466,7 @@ __global__ __launch_bounds__(64 * W * GROUP<W>) void recur_fwd_kernel(RecurArgs 
 // from the last step to the first.  The forward pass left the state before
 // every chunk, so a chunk's coefficients need no other chunk.
 // ---------------------------------------------------------------------------
-template <bool BF, int V, int W>
+template <bool BF, int V, int W, bool ONCE>
 __global__ __launch_bounds__(64 * W * GROUP<W>) void recur_bwd_kernel(RecurArgs a)
 {
     __shared__ float2 maps[W == 1 ? 1 : 2][W][W == 1 ? 1 : 64 * V];
@@ -490,10 +490,10 @@ __global__ __launch_bounds__(64 * W * GROUP<W>) void recur_bwd_kernel(RecurArgs 
     Raw<BF, V> x[C], r[C], i[C], dy[C];
     float hs[V];
     auto fetch = [&](int tc) {
-        load_chunk<BF, V>(a.x, p.b, tc, a.T, p.dc, x);
-        load_chunk<BF, V>(a.r, p.b, tc, a.T, p.dc, r);
-        load_chunk<BF, V>(a.i, p.b, tc, a.T, p.dc, i);
-        load_chunk<BF, V>(a.dy, p.b, tc, a.T, p.dc, dy);
+        load_chunk<BF, V, ONCE>(a.x, p.b, tc, a.T, p.dc, x);
+        load_chunk<BF, V, ONCE>(a.r, p.b, tc, a.T, p.dc, r);
+        load_chunk<BF, V, ONCE>(a.i, p.b, tc, a.T, p.dc, i);
+        load_chunk<BF, V, ONCE>(a.dy, p.b, tc, a.T, p.dc, dy);
         const int tt = tc < a.T ? tc : a.T - 1;
         load_f32<V>(a.saved + (int64_t)(tt / C) * BD + bd, hs);
     };
@@ -594,9 +594,9 @@ __global__ __launch_bounds__(64 * W * GROUP<W>) void recur_bwd_kernel(RecurArgs 
                 G[e] = fade<BF>(c[k][e], gg);
             }
             if (p.live && t + k < a.T) {
-                store_row<BF, V>(outx + k * a.dx.st, p.dc, dx);
-                store_row<BF, V>(outr + k * a.dr.st, p.dc, dr);
-                store_row<BF, V>(outi + k * a.di.st, p.dc, di);
+                store_row<BF, V, ONCE>(outx + k * a.dx.st, p.dc, dx);
+                store_row<BF, V, ONCE>(outr + k * a.dr.st, p.dc, dr);
+                store_row<BF, V, ONCE>(outi + k * a.di.st, p.dc, di);
             }
         }
         if constexpr (W == 1) {
@@ -747,7 +747,7 @@ __global__ __launch_bounds__(1024) void recur_lambda_kernel(const float *parts, 
 // one step: a wave has 64 V channels of `rows` sequences, so that lambda's
 // softplus, some hundred instructions, is taken once for all of them
 // ---------------------------------------------------------------------------
-template <bool BF, int V>
+template <bool BF, int V, bool ONCE>
 __global__ __launch_bounds__(256) void recur_step_kernel(RecurArgs a, int rows)
 {
     const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -766,10 +766,10 @@ __global__ __launch_bounds__(256) void recur_step_kernel(RecurArgs a, int rows)
     typedef float state __attribute__((ext_vector_type(V)));
     for (int b = b0; b < b1; ++b) {
         float x[V], r[V], i[V], h[V];
-        unpack<BF, V>(load_row<BF, V>(row_at(a.x, b, 0), d), x);
-        unpack<BF, V>(load_row<BF, V>(row_at(a.r, b, 0), d), r);
-        unpack<BF, V>(load_row<BF, V>(row_at(a.i, b, 0), d), i);
-        const state was = load_at<state>(a.h0 + (int64_t)b * a.D, d * 4u);
+        unpack<BF, V>(load_row<BF, V, ONCE>(row_at(a.x, b, 0), d), x);
+        unpack<BF, V>(load_row<BF, V, ONCE>(row_at(a.r, b, 0), d), r);
+        unpack<BF, V>(load_row<BF, V, ONCE>(row_at(a.i, b, 0), d), i);
+        const state was = load_at<state, ONCE>(a.h0 + (int64_t)b * a.D, d * 4u);
         const bool clear = a.done && a.done[b] != 0;
         state now;
 #pragma unroll
@@ -779,8 +779,8 @@ __global__ __launch_bounds__(256) void recur_step_kernel(RecurArgs a, int rows)
             h[e] = advance<BF>(c, was[e], u);
             now[e] = clear ? 0.0f : h[e];
         }
-        if (a.y.p) store_row<BF, V>(row_at(a.y, b, 0), d, h);
-        store_at(a.h_last + (int64_t)b * a.D, d * 4u, now);
+        if (a.y.p) store_row<BF, V, ONCE>(row_at(a.y, b, 0), d, h);
+        store_at<ONCE>(a.h_last + (int64_t)b * a.D, d * 4u, now);
     }
 }
 
@@ -836,28 +836,38 @@ Shape shape_of(int T, int B, int D, bool wide)
     return s;
 }
 
-template <bool BF, int V, int W>
+template <bool BF, int V, int W, bool ONCE = false>
 void start(RecurArgs &a, const Shape &sh, bool backward, hipStream_t s)
 {
     const dim3 grid((unsigned)((sh.units + GROUP<W> - 1) / GROUP<W>), (unsigned)sh.S);
     const int threads = 64 * W * GROUP<W>;
     if constexpr (V == 1 && W == 4) {       // the only ones that split a sequence
         if (sh.S > 1 && !backward)          // (nobody needs the last segment's map,
-            hipLaunchKernelGGL((recur_fwd_kernel<BF, V, W, true>), dim3(grid.x, grid.y - 1),
+            hipLaunchKernelGGL((recur_fwd_kernel<BF, V, W, true, false>), dim3(grid.x, grid.y - 1),
                                dim3(threads), 0, s, a);
         if (sh.S > 1 && backward)           // or, backward, the first one's)
             hipLaunchKernelGGL((recur_bwd_map_kernel<BF, V, W>), dim3(grid.x, grid.y - 1),
                                dim3(threads), 0, s, a);
     }
-    if (backward) hipLaunchKernelGGL((recur_bwd_kernel<BF, V, W>), grid, dim3(threads), 0, s, a);
-    else hipLaunchKernelGGL((recur_fwd_kernel<BF, V, W, false>), grid, dim3(threads), 0, s, a);
+    if (backward)
+        hipLaunchKernelGGL((recur_bwd_kernel<BF, V, W, ONCE>), grid, dim3(threads), 0, s, a);
+    else
+        hipLaunchKernelGGL((recur_fwd_kernel<BF, V, W, false, ONCE>), grid, dim3(threads), 0, s, a);
 }
+
+// Arrays of which the last-level cache (256 MB) holds only a part are read and
+// written past the caches: 252 x 1,024 x 256 fp32 forward 209 -> 187 us, backward
+// 378 -> 350; a step of 65,536 x 512 156 -> 141, but one of 65,536 x 64, which
+// the cache holds, 18 -> 23.
+bool once(double bytes) { return bytes > 256e6; }
 
 template <bool BF>
 void start_shape(RecurArgs &a, const Shape &sh, bool backward, hipStream_t s)
 {
     // (two channels a lane are for many units: never 16 waves of them)
-    if (sh.V == 2) sh.W == 1 ? start<BF, 2, 1>(a, sh, backward, s) : start<BF, 2, 4>(a, sh, backward, s);
+    const bool cold = once((double)a.T * a.B * a.D * (BF ? 2 : 4) * (backward ? 7 : 4));
+    if (sh.V == 2 && sh.W == 1) cold ? start<BF, 2, 1, true>(a, sh, backward, s) : start<BF, 2, 1>(a, sh, backward, s);
+    else if (sh.V == 2) start<BF, 2, 4>(a, sh, backward, s);
     else if (sh.W == 1) start<BF, 1, 1>(a, sh, backward, s);
     else if (sh.W == 4) start<BF, 1, 4>(a, sh, backward, s);
     else start<BF, 1, 16>(a, sh, backward, s);
@@ -917,9 +927,12 @@ hipError_t launch_recur_step(RecurArgs &a, hipStream_t s)
     const int64_t all = (int64_t)a.B * a.blocks_d;
     const int rows = (int)(all < 8192 ? 1 : all > 16 * 4096 ? 16 : all / 4096);
     a.units = (a.B + rows - 1) / rows * a.blocks_d;
+    const bool cold = once((double)a.B * a.D * (4 * (a.bf16 ? 2 : 4) + 8));
     void (*kernel)(RecurArgs, int) =
-        a.bf16 ? (V == 4 ? recur_step_kernel<true, 4> : V == 2 ? recur_step_kernel<true, 2> : recur_step_kernel<true, 1>)
-               : (V == 4 ? recur_step_kernel<false, 4> : V == 2 ? recur_step_kernel<false, 2> : recur_step_kernel<false, 1>);
+        a.bf16 ? (V == 4 ? (cold ? recur_step_kernel<true, 4, true> : recur_step_kernel<true, 4, false>)
+                  : V == 2 ? recur_step_kernel<true, 2, false> : recur_step_kernel<true, 1, false>)
+               : (V == 4 ? (cold ? recur_step_kernel<false, 4, true> : recur_step_kernel<false, 4, false>)
+                  : V == 2 ? recur_step_kernel<false, 2, false> : recur_step_kernel<false, 1, false>);
     hipLaunchKernelGGL(kernel, dim3((unsigned)((a.units + 3) / 4)), dim3(256), 0, s, a, rows);
     return hipGetLastError();
 }
