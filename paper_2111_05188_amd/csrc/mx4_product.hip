@@ -267,7 +267,9 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t out_buffer(const Mx4Args &a, i
 // whole pieces.  (Stores straight from the result's registers are 8 bytes of
 // 32 rows each, or 64 bytes of two rows: 65,536 x 1,536 in bf16 took 158 and
 // 124 us against 110.)
-constexpr int PIECE = 256, PIECE_PITCH = PIECE + 16;
+// They pass the L2 (the buffer's nt bit), which W's tiles then keep: 65,536
+// rows 113 -> 100 us, 4,096 rows 21 -> 19.
+constexpr int PIECE = 256, PIECE_PITCH = PIECE + 16, NT = 2;
 
 // results of tile `slot` of the piece: lane l has row l%32 of tile i, columns
 // 8 r + 4(l/32) .. +3 in registers 4 r .. 4 r + 3
@@ -321,7 +323,7 @@ __device__ __forceinline__ void flush_piece(const char *lds, __amdgpu_buffer_rsr
 #pragma unroll
         for (int k = 0; k < 8 * RT; ++k) {
             const uintx4 v = *(const uintx4 *)(from + 4 * k * PIECE_PITCH);
-            __builtin_amdgcn_raw_buffer_store_b128(v, out, (int)(at + 4 * k * pitch), 0, 0);
+            __builtin_amdgcn_raw_buffer_store_b128(v, out, (int)(at + 4 * k * pitch), 0, NT);
         }
     } else if (n < n1) {
 #pragma unroll 1

@@ -81,11 +81,24 @@ __device__ __forceinline__ void store_row(void *row, uint32_t d, const float *v)
     store_at<ONCE>(row, d * (BF ? 2u : 4u), raw);
 }
 
-template <int V>
-__device__ __forceinline__ void load_f32(const float *p, float *v)
+// V neighbouring fp32 states of a row of D (aligned to a dword each)
+template <int V, bool ONCE>
+__device__ __forceinline__ void load_states(const float *row, uint32_t d, float *v)
 {
+    typedef float F __attribute__((ext_vector_type(V), aligned(4)));
+    const F f = load_at<F, ONCE>(row, d * 4u);
 #pragma unroll
-    for (int e = 0; e < V; ++e) v[e] = p[e];
+    for (int e = 0; e < V; ++e) v[e] = f[e];
+}
+
+template <int V, bool ONCE>
+__device__ __forceinline__ void store_states(float *row, uint32_t d, const float *v)
+{
+    typedef float F __attribute__((ext_vector_type(V), aligned(4)));
+    F f;
+#pragma unroll
+    for (int e = 0; e < V; ++e) f[e] = v[e];
+    store_at<ONCE>(row, d * 4u, f);
 }
 
 template <int V>
@@ -431,7 +444,7 @@ __global__ __launch_bounds__(64 * W * GROUP<W>) void recur_fwd_kernel(RecurArgs 
         }
         if constexpr (!SUMMARY) {
             if (a.saved && p.live && t < a.T)
-                store_f32<V>(a.saved + (int64_t)(t / C) * BD + bd, h);
+                store_states<V, ONCE>(a.saved + (int64_t)(t / C) * BD + (int64_t)p.b * a.D, p.dc, h);
             char *out = row_at(a.y, p.b, t);
             const bool stored = p.live && a.y.p;
 #pragma unroll
@@ -495,7 +508,7 @@ __global__ __launch_bounds__(64 * W * GROUP<W>) void recur_bwd_kernel(RecurArgs 
         load_chunk<BF, V, ONCE>(a.i, p.b, tc, a.T, p.dc, i);
         load_chunk<BF, V, ONCE>(a.dy, p.b, tc, a.T, p.dc, dy);
         const int tt = tc < a.T ? tc : a.T - 1;
-        load_f32<V>(a.saved + (int64_t)(tt / C) * BD + bd, hs);
+        load_states<V, ONCE>(a.saved + (int64_t)(tt / C) * BD + (int64_t)p.b * a.D, p.dc, hs);
     };
     fetch(t);
     uint8_t flag = load_done(a, p.b, t, p.lane);
