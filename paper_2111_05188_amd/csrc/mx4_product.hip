@@ -234,9 +234,9 @@ __global__ __launch_bounds__(256) void mx4_join_kernel(Mx4Args a, int nblocks, i
 // there with no other lane's help), and W goes past it one tile of 32 columns
 // at a time, from LDS, where the workgroup's waves share it.  x is read once,
 // y written once.  From L1 instead of LDS a tile took 1.7 us against 1.3.
-// 65,536 x 1,001 bf16 rows times 1,536: 110 us, 22 of them for x at 6 TB/s,
-// the rest bound by LDS reads (13,100 a CU) with y's 201 MB behind them; 45 us
-// with 512 columns (4.5 TB/s).
+// 65,536 x 1,001 bf16 rows times 1,536: 91 us (2.2 PFLOP/s), 23 of them for x
+// at 6 TB/s; then y's 201 MB, LDS reads (13,100 a CU) and 25 us of matrix
+// instructions share the rest.
 // SRC: x in fp32 (0), bf16 (1), or A in 4 bits (2).  KG groups of 4 k-steps.
 // ---------------------------------------------------------------------------
 enum { SRC_F32 = 0, SRC_BF16 = 1, SRC_FOUR = 2 };

@@ -12,8 +12,8 @@
 // the maps of all segments from a first launch.
 //
 // With many sequences the memory bounds it: 390 steps x 4,096 sequences x 512
-// channels in bf16 take 1.34 ms, 6.6 GB at 4.9 TB/s, and 3.9 ms with the
-// gradients (18.9 GB at 4.8: the gates are read again, and the states before
+// channels in bf16 take 1.32 ms, 6.6 GB at 5.0 TB/s, and 3.8 ms with the
+// gradients (18.9 GB at 5.0: the gates are read again, and the states before
 // every chunk are kept instead of all of them).
 //
 // 1 - a^2 comes from a - 1 by a polynomial rather than from a: long memories
@@ -289,12 +289,15 @@ __device__ __forceinline__ float join(float2 m, float c)
 
 __device__ __forceinline__ float join_p(float2 m, float P) { return m.x == 0.0f ? 0.0f : m.x * P; }
 
+// the shapes that split a sequence over workgroups: calls of few waves
+template <int V, int W> constexpr bool SEGMENTS = V == 1 && W == 4;
+
 // The maps of `n` segments after the states c, from segment `first` on, forward
 // or (BACK) backward.  Each wave reduces a share of them, sixteen loads in
 // flight; the shares go through LDS.
 template <int V, int W, bool BACK>
 __device__ __forceinline__ void join_segments(const float2 *maps, int64_t BD, int first, int n,
-                                              float2 (*lds)[W == 1 ? 1 : 64 * V], int w, int lane,
+                                              float2 (*lds)[64 * V], int w, int lane,
                                               float (&c)[V])
 {
     if (n <= 0) return;
@@ -303,7 +306,7 @@ __device__ __forceinline__ void join_segments(const float2 *maps, int64_t BD, in
 #pragma unroll
     for (int e = 0; e < V; ++e) {
         P[e] = 1.0f;
-        H[e] = W == 1 ? c[e] : 0.0f;
+        H[e] = 0.0f;
     }
 #pragma unroll 1
     for (int k = a0; k < a1; k += 16) {
@@ -325,18 +328,13 @@ __device__ __forceinline__ void join_segments(const float2 *maps, int64_t BD, in
                 }
             }
     }
-    if constexpr (W > 1) {
 #pragma unroll
-        for (int e = 0; e < V; ++e) lds[w][lane * V + e] = make_float2(P[e], H[e]);
-        __syncthreads();
+    for (int e = 0; e < V; ++e) lds[w][lane * V + e] = make_float2(P[e], H[e]);
+    __syncthreads();
 #pragma unroll
-        for (int j = 0; j < W; ++j)
+    for (int j = 0; j < W; ++j)
 #pragma unroll
-            for (int e = 0; e < V; ++e) c[e] = join(lds[j][lane * V + e], c[e]);
-    } else {
-#pragma unroll
-        for (int e = 0; e < V; ++e) c[e] = H[e];
-    }
+        for (int e = 0; e < V; ++e) c[e] = join(lds[j][lane * V + e], c[e]);
 }
 
 // ---------------------------------------------------------------------------
@@ -357,9 +355,8 @@ __global__ __launch_bounds__(64 * W * GROUP<W>) void recur_fwd_kernel(RecurArgs 
         carry[e] = !SUMMARY && a.h0 ? a.h0[bd + e] : 0.0f;
         carryP[e] = 1.0f;
     }
-    if constexpr (!SUMMARY)
-        join_segments<V, W, false>(a.maps + bd, BD, 0, (int)blockIdx.y, maps[W == 1 ? 0 : 1], p.w,
-                                   p.lane, carry);
+    if constexpr (!SUMMARY && SEGMENTS<V, W>)
+        join_segments<V, W, false>(a.maps + bd, BD, 0, (int)blockIdx.y, maps[1], p.w, p.lane, carry);
 
     Raw<BF, V> x[C], r[C], i[C];
     auto fetch = [&](int t) {
@@ -399,7 +396,7 @@ __global__ __launch_bounds__(64 * W * GROUP<W>) void recur_fwd_kernel(RecurArgs 
                 }
         }
         float h[V];
-        if constexpr (W > 1 || SUMMARY) {
+        if constexpr (W > 1) {
             float P[V], H[V];
 #pragma unroll
             for (int e = 0; e < V; ++e) {
@@ -414,30 +411,22 @@ __global__ __launch_bounds__(64 * W * GROUP<W>) void recur_fwd_kernel(RecurArgs 
                     P[e] = fade<BF>(c[k][e], P[e]);
                     if (!plain && (clear >> k & 1)) H[e] = P[e] = 0.0f;
                 }
-            if constexpr (W > 1) {
 #pragma unroll
-                for (int e = 0; e < V; ++e)
-                    maps[par][p.w][p.lane * V + e] = make_float2(P[e], H[e]);
-                __syncthreads();
+            for (int e = 0; e < V; ++e)
+                maps[par][p.w][p.lane * V + e] = make_float2(P[e], H[e]);
+            __syncthreads();
 #pragma unroll
-                for (int e = 0; e < V; ++e) h[e] = carry[e];
+            for (int e = 0; e < V; ++e) h[e] = carry[e];
 #pragma unroll
-                for (int j = 0; j < W; ++j)
-#pragma unroll
-                    for (int e = 0; e < V; ++e) {
-                        if (j == p.w) h[e] = carry[e];
-                        const float2 m = maps[par][j][p.lane * V + e];
-                        carry[e] = join(m, carry[e]);
-                        if (SUMMARY) carryP[e] = join_p(m, carryP[e]);
-                    }
-                par ^= 1;
-            } else {
+            for (int j = 0; j < W; ++j)
 #pragma unroll
                 for (int e = 0; e < V; ++e) {
-                    carry[e] = join(make_float2(P[e], H[e]), carry[e]);
-                    carryP[e] = join_p(make_float2(P[e], H[e]), carryP[e]);
+                    if (j == p.w) h[e] = carry[e];
+                    const float2 m = maps[par][j][p.lane * V + e];
+                    carry[e] = join(m, carry[e]);
+                    if (SUMMARY) carryP[e] = join_p(m, carryP[e]);
                 }
-            }
+            par ^= 1;
         } else {
 #pragma unroll
             for (int e = 0; e < V; ++e) h[e] = carry[e];
@@ -494,9 +483,9 @@ __global__ __launch_bounds__(64 * W * GROUP<W>) void recur_bwd_kernel(RecurArgs 
         carry[e] = a.dh_last ? a.dh_last[bd + e] : 0.0f;
         sum[e] = 0.0f;
     }
-    join_segments<V, W, true>(a.maps + bd, BD, (int)gridDim.y - 1,
-                              (int)(gridDim.y - 1 - blockIdx.y), maps[W == 1 ? 0 : 1], p.w, p.lane,
-                              carry);
+    if constexpr (SEGMENTS<V, W>)
+        join_segments<V, W, true>(a.maps + bd, BD, (int)gridDim.y - 1,
+                                  (int)(gridDim.y - 1 - blockIdx.y), maps[1], p.w, p.lane, carry);
     const int tiles = (p.t1 - p.t0 + W * C - 1) / (W * C);
     int t = p.t0 + (tiles - 1) * W * C + p.w * C, par = 0;
 
@@ -638,7 +627,7 @@ __global__ __launch_bounds__(64 * W * GROUP<W>) void recur_bwd_kernel(RecurArgs 
 template <bool BF, int V, int W>
 __global__ __launch_bounds__(64 * W * GROUP<W>) void recur_bwd_map_kernel(RecurArgs a)
 {
-    __shared__ float2 maps[W == 1 ? 1 : 2][W][W == 1 ? 1 : 64 * V];
+    __shared__ float2 maps[2][W][64 * V];
     Place<V, W> p;
     const int segment = blockIdx.y + 1;
     if (!place<V, W>(a, segment, p)) return;
@@ -696,27 +685,18 @@ __global__ __launch_bounds__(64 * W * GROUP<W>) void recur_bwd_map_kernel(RecurA
                 H[e] = fade<BF>(c[k][e], gg);
                 P[e] = fade<BF>(c[k][e], P[e]);
             }
-        if constexpr (W > 1) {
 #pragma unroll
-            for (int e = 0; e < V; ++e)
-                maps[par][p.w][p.lane * V + e] = make_float2(P[e], H[e]);
-            __syncthreads();
+        for (int e = 0; e < V; ++e) maps[par][p.w][p.lane * V + e] = make_float2(P[e], H[e]);
+        __syncthreads();
 #pragma unroll
-            for (int j = W - 1; j >= 0; --j)
-#pragma unroll
-                for (int e = 0; e < V; ++e) {
-                    const float2 m = maps[par][j][p.lane * V + e];
-                    carry[e] = join(m, carry[e]);
-                    carryP[e] = join_p(m, carryP[e]);
-                }
-            par ^= 1;
-        } else {
+        for (int j = W - 1; j >= 0; --j)
 #pragma unroll
             for (int e = 0; e < V; ++e) {
-                carry[e] = join(make_float2(P[e], H[e]), carry[e]);
-                carryP[e] = join_p(make_float2(P[e], H[e]), carryP[e]);
+                const float2 m = maps[par][j][p.lane * V + e];
+                carry[e] = join(m, carry[e]);
+                carryP[e] = join_p(m, carryP[e]);
             }
-        }
+        par ^= 1;
     }
     if (!p.live || p.w != 0) return;
 #pragma unroll
@@ -733,7 +713,7 @@ __global__ __launch_bounds__(1024) void recur_lambda_kernel(const float *parts, 
     const int c = threadIdx.x & 15, rg = threadIdx.x >> 4, d = blockIdx.x * 16 + c;
     double s = 0.0;
     if (d < D) {
-        // (sixteen loads in flight: 4,096 rows of 512 33 us one at a time, 16 so)
+        // (sixteen loads in flight: 4,096 rows of 512 33 us one at a time, 11 so)
         int64_t k = rg;
         for (; k + 15 * 64 < rows; k += 16 * 64) {
             float v[16];
@@ -818,7 +798,7 @@ struct Shape {
 
 // Two channels a lane, waves of a workgroup along time (W), segments (S), by
 // how many waves a call has.  Measured (bf16, us, T x B x D; forward):
-//   390 x 4,096 x 512 (32,768 units of one wave)   W = 1       1,340
+//   390 x 4,096 x 512 (32,768 units of one wave)   W = 1       1,320
 //   390 x 64 x 512    (512)     W = 1, 4, 16: 73, 34, 43;  W = 4, S = 2: 46
 //   2,520 x 16 x 256  (64)      W = 4, S = 1, 4, 16, 64: 135, 69, 44, 43; W = 16: 99
 //   24,570 x 1 x 512  (8)       W = 4, S = 16, 64, 128, 256: 151, 61, 53, 54
@@ -854,7 +834,7 @@ void start(RecurArgs &a, const Shape &sh, bool backward, hipStream_t s)
 {
     const dim3 grid((unsigned)((sh.units + GROUP<W> - 1) / GROUP<W>), (unsigned)sh.S);
     const int threads = 64 * W * GROUP<W>;
-    if constexpr (V == 1 && W == 4) {       // the only ones that split a sequence
+    if constexpr (SEGMENTS<V, W>) {
         if (sh.S > 1 && !backward)          // (nobody needs the last segment's map,
             hipLaunchKernelGGL((recur_fwd_kernel<BF, V, W, true, false>), dim3(grid.x, grid.y - 1),
                                dim3(threads), 0, s, a);
