@@ -60,7 +60,8 @@ class MemoryLayer:
 
     def encode(self, obs, done=None, lens=None, h0=None, stream=None):
         """y [T][B][D] and the last states [B][D] of stored observations [T][B][ld] (ld >= S;
-        rows follow one another); done [T][B] and lens [B] as tp.recur_forward."""
+        rows follow one another); done [T][B] and lens [B] as tp.recur_forward.  Both are buffers
+        of the layer, which its next encode of this size writes again."""
         T, B, ld = obs.shape
         self._sequence(T, B, done, lens)
         self.rows = obs.reshape(T * B, ld)[:, :self.S]
@@ -71,7 +72,8 @@ class MemoryLayer:
         return self.y, self.h_last
 
     def gradients(self, dy, dh_last=None, stream=None):
-        """Gradients of the last encode's W, lambda and first states, from dy [T][B][D]."""
+        """Gradients of the last encode's W, lambda and first states, from dy [T][B][D] (buffers
+        of the layer)."""
         tp.recur_backward(self.rc, *self.parts(self.gates), self.saved, dy,
                           *self.parts(self.dgates), self.dlam, self.work, dh_last=dh_last,
                           dh0=self.dh0, stream=stream)
