@@ -280,14 +280,26 @@ __device__ __forceinline__ void load_chunk(const RecurRows &m, int b, int t, int
     }
 }
 
-// the map m after the state c.  A map with P = 0 has an episode's end in it:
-// whatever c is, NaN and infinity too, is forgotten.
+// A map h -> P h + H with an episode's end in it forgets whatever h is, NaN and
+// infinity too.  That has a mark of its own, a negative P: a product of decays
+// reaches 0 without one, and then a NaN has to stay, as it does step by step.
+// So that an infinity stays as well, P does not fall to 0.
+constexpr float FORGETS = -1.0f, LEAST = 0x1p-149f;
+
+// P of a chunk's map; ends: one of its steps ends an episode
+__device__ __forceinline__ float map_p(float P, bool ends) { return ends ? FORGETS : fmaxf(P, LEAST); }
+
+// the map m after the state c
 __device__ __forceinline__ float join(float2 m, float c)
 {
-    return m.x == 0.0f ? m.y : fmaf(m.x, c, m.y);
+    return m.x < 0.0f ? m.y : fmaf(m.x, c, m.y);
 }
 
-__device__ __forceinline__ float join_p(float2 m, float P) { return m.x == 0.0f ? 0.0f : m.x * P; }
+// and after the map P.  (A NaN among the decays is in H too, and stays there.)
+__device__ __forceinline__ float join_p(float2 m, float P)
+{
+    return map_p(m.x * P, m.x < 0.0f || P < 0.0f);
+}
 
 // the shapes that split a sequence over workgroups: calls of few waves
 template <int V, int W> constexpr bool SEGMENTS = V == 1 && W == 4;
@@ -409,11 +421,11 @@ __global__ __launch_bounds__(64 * W * GROUP<W>) void recur_fwd_kernel(RecurArgs 
                 for (int e = 0; e < V; ++e) {
                     H[e] = advance<BF>(c[k][e], H[e], u[k][e]);
                     P[e] = fade<BF>(c[k][e], P[e]);
-                    if (!plain && (clear >> k & 1)) H[e] = P[e] = 0.0f;
+                    if (!plain && (clear >> k & 1)) H[e] = 0.0f;
                 }
 #pragma unroll
             for (int e = 0; e < V; ++e)
-                maps[par][p.w][p.lane * V + e] = make_float2(P[e], H[e]);
+                maps[par][p.w][p.lane * V + e] = make_float2(map_p(P[e], clear != 0), H[e]);
             __syncthreads();
 #pragma unroll
             for (int e = 0; e < V; ++e) h[e] = carry[e];
@@ -554,14 +566,14 @@ __global__ __launch_bounds__(64 * W * GROUP<W>) void recur_bwd_kernel(RecurArgs 
             for (int k = C - 1; k >= 0; --k)
 #pragma unroll
                 for (int e = 0; e < V; ++e) {
-                    if (!plain && (clear >> k & 1)) H[e] = P[e] = 0.0f;
+                    if (!plain && (clear >> k & 1)) H[e] = 0.0f;
                     const float gg = g[k][e] + H[e];
                     H[e] = fade<BF>(c[k][e], gg);
                     P[e] = fade<BF>(c[k][e], P[e]);
                 }
 #pragma unroll
             for (int e = 0; e < V; ++e)
-                maps[par][p.w][p.lane * V + e] = make_float2(P[e], H[e]);
+                maps[par][p.w][p.lane * V + e] = make_float2(map_p(P[e], clear != 0), H[e]);
             __syncthreads();
 #pragma unroll
             for (int e = 0; e < V; ++e) G[e] = carry[e];
@@ -680,13 +692,14 @@ __global__ __launch_bounds__(64 * W * GROUP<W>) void recur_bwd_map_kernel(RecurA
         for (int k = C - 1; k >= 0; --k)
 #pragma unroll
             for (int e = 0; e < V; ++e) {
-                if (clear >> k & 1) H[e] = P[e] = 0.0f;
+                if (clear >> k & 1) H[e] = 0.0f;
                 const float gg = g[k][e] + H[e];
                 H[e] = fade<BF>(c[k][e], gg);
                 P[e] = fade<BF>(c[k][e], P[e]);
             }
 #pragma unroll
-        for (int e = 0; e < V; ++e) maps[par][p.w][p.lane * V + e] = make_float2(P[e], H[e]);
+        for (int e = 0; e < V; ++e)
+            maps[par][p.w][p.lane * V + e] = make_float2(map_p(P[e], clear != 0), H[e]);
         __syncthreads();
 #pragma unroll
         for (int j = W - 1; j >= 0; --j)

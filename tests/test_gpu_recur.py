@@ -218,6 +218,42 @@ def test_an_episodes_end_forgets_nan(T):
     assert torch.isnan(dlam[5]) and torch.isfinite(dlam[:5]).all()
 
 
+# one wave a sequence; four waves; sixteen; segments over workgroups
+SPLITS = [(40, 2100, 64), (40, 600, 64), (200, 2, 64), (6000, 1, 64)]
+
+
+def decaying(T, B, D, dtype, seed, top):
+    """Memories of a hundred bars to a fraction of one: products of decays underflow, over many
+    steps or within a few."""
+    c = Case(T, B, D, dtype, seed=seed)
+    c.lam = np.linspace(-6.0, top, D).astype(np.float32)
+    c.rc = tp.RecurT(dev(c.lam), T, B, dtype)
+    return c
+
+
+@pytest.mark.parametrize("dtype", BOTH)
+@pytest.mark.parametrize("T,B,D", SPLITS)
+def test_nan_stays_to_the_end(T, B, D, dtype):
+    """Without an episode's end a NaN state is NaN in every later step, however little of it a
+    finite state would have left, and a NaN gradient in every earlier one."""
+    say(f"[recur] nan stays {T, B, D} {dtype}")
+    c = decaying(T, B, D, dtype, 21, 4.0)
+    saved = c.rc.saved()
+    c.gates[5, 0, :D] = float("nan")
+    y, last = c.forward(saved)
+    torch.cuda.synchronize()
+    assert torch.isfinite(y[:5]).all() and torch.isnan(y[5:, 0]).all() and torch.isnan(last[0]).all()
+    assert torch.isfinite(y[:, 1:]).all() and torch.isfinite(last[1:]).all()
+    c.gates[5, 0, :D] = 0.5
+    c.dy[T - 6, 0] = float("nan")
+    c.forward(saved)
+    dlam, dh0 = c.backward(saved)
+    torch.cuda.synchronize()
+    assert torch.isnan(c.out[:T - 5, 0]).all() and torch.isfinite(c.out[T - 5:]).all()
+    assert torch.isnan(dh0[0]).all() and torch.isnan(dlam).all()
+    assert torch.isfinite(c.out[:, 1:]).all() and torch.isfinite(dh0[1:]).all()
+
+
 @pytest.mark.parametrize("dtype", BOTH)
 def test_extreme_gates(dtype):
     """Gates shut and open to the last bit, lambda far out: results stay finite and right."""
