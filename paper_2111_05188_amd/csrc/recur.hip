@@ -122,10 +122,12 @@ __device__ __forceinline__ float exp_neg(float x) { return __builtin_amdgcn_exp2
 // a = exp(L) and a - 1 of L = -s rho <= 0 (L2 = L log2 e): near 0 from L + L^2
 // q(L), q fitted for the least relative error of a - 1 (fp32 7e-8 with
 // rounding; for results that go to bf16 3e-7), else from the hardware exp2.
+// a is never 0, so that an infinite state stays one (adding the smallest normal
+// number changes nothing above 2^-101, and leaves a NaN one).
 template <bool BF>
 __device__ __forceinline__ bool decay(float L, float L2, float &a, float &am1)
 {
-    const float far = __builtin_amdgcn_exp2f(L2);
+    const float far = __builtin_amdgcn_exp2f(L2) + 0x1p-126f;
     float q;
     if constexpr (BF) {
         q = 0x1.362a9cp-5f;
@@ -152,17 +154,24 @@ template <bool BF>
 __device__ __forceinline__ float keep(bool is_near, float a, float am1)
 {
     if constexpr (BF) return a;
-    return is_near ? am1 : a < 1e-38f ? 1e-38f : a;
+    return is_near ? am1 : a;
 }
 
 template <bool BF> constexpr float KEEP_ONE = BF ? 1.0f : 0.0f;   // a = 1
+
+// (a - 1) h of an infinite h must not meet h: there the largest finite number
+// stands for it (and for a NaN, which the sum has all the same)
+__device__ __forceinline__ float finite(float h)
+{
+    return __builtin_amdgcn_fmed3f(h, -__FLT_MAX__, __FLT_MAX__);
+}
 
 // a h + u
 template <bool BF>
 __device__ __forceinline__ float advance(float c, float h, float u)
 {
     if constexpr (BF) return fmaf(c, h, u);
-    return fmaf(c, h, c > 0.0f ? u : h + u);
+    return fmaf(c, c > 0.0f ? h : finite(h), c > 0.0f ? u : h + u);
 }
 
 // a g
@@ -170,7 +179,15 @@ template <bool BF>
 __device__ __forceinline__ float fade(float c, float g)
 {
     if constexpr (BF) return c * g;
-    return fmaf(c, g, c > 0.0f ? 0.0f : g);
+    return fmaf(c, c > 0.0f ? g : finite(g), c > 0.0f ? 0.0f : g);
+}
+
+// a P of a product of decays P, which is never infinite
+template <bool BF>
+__device__ __forceinline__ float fade_p(float c, float P)
+{
+    if constexpr (BF) return c * P;
+    return fmaf(c, P, c > 0.0f ? 0.0f : P);
 }
 
 // h -> a h + u
@@ -420,7 +437,7 @@ __global__ __launch_bounds__(64 * W * GROUP<W>) void recur_fwd_kernel(RecurArgs 
 #pragma unroll
                 for (int e = 0; e < V; ++e) {
                     H[e] = advance<BF>(c[k][e], H[e], u[k][e]);
-                    P[e] = fade<BF>(c[k][e], P[e]);
+                    P[e] = fade_p<BF>(c[k][e], P[e]);
                     if (!plain && (clear >> k & 1)) H[e] = 0.0f;
                 }
 #pragma unroll
@@ -569,7 +586,7 @@ __global__ __launch_bounds__(64 * W * GROUP<W>) void recur_bwd_kernel(RecurArgs 
                     if (!plain && (clear >> k & 1)) H[e] = 0.0f;
                     const float gg = g[k][e] + H[e];
                     H[e] = fade<BF>(c[k][e], gg);
-                    P[e] = fade<BF>(c[k][e], P[e]);
+                    P[e] = fade_p<BF>(c[k][e], P[e]);
                 }
 #pragma unroll
             for (int e = 0; e < V; ++e)
@@ -695,7 +712,7 @@ __global__ __launch_bounds__(64 * W * GROUP<W>) void recur_bwd_map_kernel(RecurA
                 if (clear >> k & 1) H[e] = 0.0f;
                 const float gg = g[k][e] + H[e];
                 H[e] = fade<BF>(c[k][e], gg);
-                P[e] = fade<BF>(c[k][e], P[e]);
+                P[e] = fade_p<BF>(c[k][e], P[e]);
             }
 #pragma unroll
         for (int e = 0; e < V; ++e)

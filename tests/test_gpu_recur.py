@@ -255,6 +255,48 @@ def test_nan_stays_to_the_end(T, B, D, dtype):
 
 
 @pytest.mark.parametrize("dtype", BOTH)
+@pytest.mark.parametrize("T,B,D", SPLITS)
+def test_infinity_stays(T, B, D, dtype):
+    """An infinite state stays what it is under finite inputs, in steps past a sequence's end too,
+    and so does an infinite gradient: a is never 0."""
+    say(f"[recur] infinity stays {T, B, D} {dtype}")
+    c = decaying(T, B, D, dtype, 22, 20.0)
+    inf = float("inf")
+    lens = np.full(B, T, np.int32)
+    lens[-1] = T - 3 if B > 1 else T
+    c.rc = tp.RecurT(c.rc.lam, T, B, dtype, lens=dev(lens))
+    c.h0[0] = np.where(np.arange(D) % 2, inf, -inf)
+    if B > 1:
+        c.h0[-1] = inf
+    want = dev(c.h0)
+    saved = c.rc.saved()
+    y, last = c.forward(saved)
+    torch.cuda.synchronize()
+    assert torch.equal(y[:, 0].float(), want[0].expand(T, D)) and torch.equal(last[0], want[0])
+    if B > 1:
+        assert (y[:T - 3, -1] == inf).all() and (y[T - 3:, -1] == 0).all() and (last[-1] == inf).all()
+    assert torch.isfinite(y[:, 1:B - 1]).all()
+    c.h0[:] = 0.5
+    c.dh[0], c.dh[-1] = c.dh[-1], inf
+    c.forward(saved)
+    _, dh0 = c.backward(saved)
+    torch.cuda.synchronize()
+    assert (dh0[-1] == inf).all() and torch.isfinite(dh0[:B - 1]).all()
+    dx = c.split(c.out)[0]
+    assert (dx[:lens[-1], -1] == inf).all() and (dx[lens[-1]:, -1] == 0).all()
+
+
+def test_an_infinite_state_steps_to_itself():
+    for dtype in BOTH:
+        c = decaying(1, 3, 256, dtype, 23, 20.0)
+        h = torch.full((3, 256), float("-inf"), device="cuda")
+        y = torch.empty(3, 256, dtype=dtype, device="cuda")
+        tp.recur_step(*c.split(c.gates[0]), c.rc.lam, h, h, y)
+        torch.cuda.synchronize()
+        assert (h == float("-inf")).all() and (y == float("-inf")).all()
+
+
+@pytest.mark.parametrize("dtype", BOTH)
 def test_extreme_gates(dtype):
     """Gates shut and open to the last bit, lambda far out: results stay finite and right."""
     T, B = 40, 2
