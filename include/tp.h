@@ -596,7 +596,8 @@ size_t tp_recur_workspace_bytes(const tp_recur *cfg);
  * tp_recur_forward -- y and the last states of whole sequences.
  *   h0 [B][D] or NULL (zeros); y may have p = NULL (not stored); h_last
  *   [B][D] or NULL, the state after the last step (0 where done is set on
- *   it); saved or NULL (no gradients wanted).
+ *   it); saved or NULL (no gradients wanted).  h_last may be h0's buffer;
+ *   buffers that overlap otherwise are refused.
  */
 int tp_recur_forward(const tp_recur *cfg, const tp_rows *x, const tp_rows *r,
                      const tp_rows *i, const float *h0, const tp_rows *y, float *h_last,
@@ -606,7 +607,8 @@ int tp_recur_forward(const tp_recur *cfg, const tp_rows *x, const tp_rows *r,
  * tp_recur_backward -- gradients of everything tp_recur_forward read, from
  * dy and dh_last ([B][D] or NULL, zeros).  saved: what the forward call on
  * the same inputs kept.
- *   dx, dr, di as x, r, i; dlambda [D]; dh0 [B][D] or NULL.
+ *   dx, dr, di as x, r, i; dlambda [D]; dh0 [B][D] or NULL, may be dh_last's
+ *   buffer (as h_last h0's).
  * Sums over steps and sequences run in a fixed order.
  */
 int tp_recur_backward(const tp_recur *cfg, const tp_rows *x, const tp_rows *r,
@@ -618,7 +620,8 @@ int tp_recur_backward(const tp_recur *cfg, const tp_rows *x, const tp_rows *r,
 /*
  * tp_recur_step -- one bar: h_out = the states after a step from h, y
  * (or p = NULL) the same before episode ends clear them.  cfg->T must be 1
- * and cfg->len NULL; done [B] or NULL; h, h_out [B][D], may be one buffer.
+ * and cfg->len NULL; done [B] or NULL; h, h_out [B][D], may be one buffer but
+ * not overlap otherwise.
  */
 int tp_recur_step(const tp_recur *cfg, const tp_rows *x, const tp_rows *r, const tp_rows *i,
                   const float *h, float *h_out, const tp_rows *y, void *stream);

@@ -282,6 +282,15 @@ int check_out_rows(const tp_recur *c, const tp_rows *m, const char *name)
     return TP_OK;
 }
 
+// States in and out: one buffer or two, never a part of one another.
+int check_states(const tp_recur *c, const float *in, const float *out, const char *names)
+{
+    const uintptr_t a = (uintptr_t)in, b = (uintptr_t)out;
+    if (!a || !b || a == b || (a > b ? a - b : b - a) >= (size_t)c->B * c->D * sizeof(float))
+        return TP_OK;
+    return fail(TP_EINVAL, "recurrence states %s overlap without being one buffer", names);
+}
+
 // what the whole-sequence calls share
 int recur_args(const tp_recur *c, const tp_rows *x, const tp_rows *r, const tp_rows *i, void *work,
                size_t work_bytes, RecurArgs *a)
@@ -997,6 +1006,7 @@ int tp_recur_forward(const tp_recur *cfg, const tp_rows *x, const tp_rows *r, co
         return fail(TP_EINVAL, "recurrence has no output: y, h_last and saved are NULL");
     if (!aligned(h0, 4) || !aligned(h_last, 4) || !aligned(saved, 4))
         return fail(TP_EINVAL, "recurrence states are misaligned");
+    if ((rc = check_states(cfg, h0, h_last, "h0 and h_last")) != TP_OK) return rc;
     a.h0 = h0;
     a.h_last = h_last;
     a.saved = saved;
@@ -1023,6 +1033,7 @@ int tp_recur_backward(const tp_recur *cfg, const tp_rows *x, const tp_rows *r, c
     if (!saved || !dlambda) return fail(TP_EINVAL, "recurrence saved or dlambda is NULL");
     if (!aligned(saved, 4) || !aligned(dh_last, 4) || !aligned(dlambda, 4) || !aligned(dh0, 4))
         return fail(TP_EINVAL, "recurrence states are misaligned");
+    if ((rc = check_states(cfg, dh_last, dh0, "dh_last and dh0")) != TP_OK) return rc;
     a.saved = const_cast<float *>(saved);
     a.dh_last = dh_last;
     a.dlam = dlambda;
@@ -1049,6 +1060,7 @@ int tp_recur_step(const tp_recur *cfg, const tp_rows *x, const tp_rows *r, const
     if ((rc = check_out_rows(cfg, y, "y")) != TP_OK) return rc;
     if (!h || !h_out || !aligned(h, 4) || !aligned(h_out, 4))
         return fail(TP_EINVAL, "recurrence state is NULL or misaligned");
+    if ((rc = check_states(cfg, h, h_out, "h and h_out")) != TP_OK) return rc;
     a.T = 1;
     a.B = cfg->B;
     a.D = cfg->D;

@@ -381,7 +381,11 @@ __global__ __launch_bounds__(64 * W * GROUP<W>) void recur_fwd_kernel(RecurArgs 
     for (int e = 0; e < V; ++e) {
         s[e] = RATE * softplus(a.lam[p.dc + e]);
         s2[e] = s[e] * LOG2E;
-        carry[e] = !SUMMARY && a.h0 ? a.h0[bd + e] : 0.0f;
+        const bool copied = SEGMENTS<V, W> && gridDim.y > 1;
+        carry[e] = SUMMARY ? 0.0f
+                   : copied ? a.maps[(gridDim.y - 1) * BD + bd + e].y
+                   : a.h0   ? a.h0[bd + e]
+                            : 0.0f;
         carryP[e] = 1.0f;
     }
     if constexpr (!SUMMARY && SEGMENTS<V, W>)
@@ -485,8 +489,14 @@ __global__ __launch_bounds__(64 * W * GROUP<W>) void recur_fwd_kernel(RecurArgs 
     if (!p.live || p.w != 0) return;
     if constexpr (SUMMARY) {
 #pragma unroll
-        for (int e = 0; e < V; ++e)
+        for (int e = 0; e < V; ++e) {
             a.maps[blockIdx.y * BD + bd + e] = make_float2(carryP[e], carry[e]);
+            // Segments read the first states while the last one stores the last
+            // states, which may be the same buffer: they read a copy, kept where
+            // the last segment would have its map, which nobody needs.
+            if (blockIdx.y == 0)
+                a.maps[gridDim.y * BD + bd + e] = make_float2(0.0f, a.h0 ? a.h0[bd + e] : 0.0f);
+        }
     } else if (p.t1 == a.T && a.h_last) {
         store_f32<V>(a.h_last + bd, carry);
     }
@@ -509,7 +519,8 @@ __global__ __launch_bounds__(64 * W * GROUP<W>) void recur_bwd_kernel(RecurArgs 
     for (int e = 0; e < V; ++e) {
         s[e] = RATE * softplus(a.lam[p.dc + e]);
         s2[e] = s[e] * LOG2E;
-        carry[e] = a.dh_last ? a.dh_last[bd + e] : 0.0f;
+        const bool copied = SEGMENTS<V, W> && gridDim.y > 1;
+        carry[e] = copied ? a.maps[bd + e].y : a.dh_last ? a.dh_last[bd + e] : 0.0f;
         sum[e] = 0.0f;
     }
     if constexpr (SEGMENTS<V, W>)
@@ -730,8 +741,11 @@ __global__ __launch_bounds__(64 * W * GROUP<W>) void recur_bwd_map_kernel(RecurA
     }
     if (!p.live || p.w != 0) return;
 #pragma unroll
-    for (int e = 0; e < V; ++e)
+    for (int e = 0; e < V; ++e) {
         a.maps[segment * BD + bd + e] = make_float2(carryP[e], carry[e]);
+        // (a copy, as of the first states forward: dh0 may be its buffer)
+        if (segment == 1) a.maps[bd + e] = make_float2(0.0f, a.dh_last ? a.dh_last[bd + e] : 0.0f);
+    }
 }
 
 // dlambda_d = sigmoid(lambda) / softplus(lambda) * sum over rows of parts,

@@ -61,7 +61,8 @@ class MemoryLayer:
     def encode(self, obs, done=None, lens=None, h0=None, stream=None):
         """y [T][B][D] and the last states [B][D] of stored observations [T][B][ld] (ld >= S;
         rows follow one another); done [T][B] and lens [B] as tp.recur_forward.  Both are buffers
-        of the layer, which its next encode of this size writes again."""
+        of the layer, which its next encode of this size writes again; the last states may be
+        that call's h0."""
         T, B, ld = obs.shape
         self._sequence(T, B, done, lens)
         self.rows = obs.reshape(T * B, ld)[:, :self.S]

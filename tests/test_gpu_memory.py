@@ -84,3 +84,18 @@ def test_updates_reach_the_4_bit_weights():
     tp.mx4_dequantize(layer.w4, back)
     torch.cuda.synchronize()
     assert np.array_equal(host(back), mx4.values(host(layer.W)))
+
+
+@pytest.mark.parametrize("dtype,tol", [(torch.float32, 2e-5), (torch.bfloat16, 2e-5 + 2.0 ** -8)])
+def test_a_trajectory_in_parts(dtype, tol):
+    """The last states of one encode are the first of the next, as they were returned."""
+    layer = memory.MemoryLayer.init(31, 64, 5, dtype)
+    obs = torch.randn(1200, 2, 32, generator=torch.Generator("cuda").manual_seed(6), device="cuda")
+    y, last = (t.clone() for t in layer.encode(obs))
+    h, parts = None, []
+    for k in range(3):
+        out, h = layer.encode(obs[400 * k:400 * (k + 1)], h0=h)
+        parts.append(out.clone())
+    torch.cuda.synchronize()
+    rms_close(torch.cat(parts), host(y), tol)
+    rms_close(h, host(last), 2e-5)

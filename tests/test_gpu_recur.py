@@ -412,6 +412,26 @@ def test_segments_continue():
     close("h", host(h), host(last), 2e-5)
 
 
+@pytest.mark.parametrize("T,B,D", SPLITS + [(24570, 1, 512), (2520, 16, 128)])
+def test_states_in_place(T, B, D):
+    """h_last in h0's buffer and dh0 in dh_last's: the bits of buffers of their own."""
+    c = Case(T, B, D, torch.bfloat16, 0.01, seed=24)
+    saved = c.rc.saved()
+    y, last = c.forward(saved)
+    _, dh0 = c.backward(saved)
+    want = c.out.clone()
+    for _ in range(3):
+        h, g, z = dev(c.h0), dev(c.dh), torch.empty_like(y)
+        c.out.fill_(7.0)
+        dlam = torch.empty(D, device="cuda")
+        tp.recur_forward(c.rc, *c.split(c.gates), z, c.work, h0=h, h_last=h, saved=saved)
+        tp.recur_backward(c.rc, *c.split(c.gates), saved, c.dy, *c.split(c.out), dlam, c.work,
+                          dh_last=g, dh0=g)
+        torch.cuda.synchronize()
+        assert torch.equal(z, y) and torch.equal(h, last)
+        assert torch.equal(c.out, want) and torch.equal(g, dh0)
+
+
 def test_same_inputs_same_bits_and_streams():
     """Calls on a stream of their own; two runs give the same bits (sums in a fixed order)."""
     c = Case(300, 40, 96, torch.bfloat16, 0.02, True, seed=16)

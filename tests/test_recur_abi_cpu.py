@@ -95,3 +95,13 @@ def test_step_refuses():
     _refused(step(h_out=X + 2), "state")
     _refused(step(x=None), "x is NULL")
     _refused(step(y=_rows(c, sb=3)), "overlap")
+
+
+def test_states_that_overlap_in_part_are_refused():
+    c = _cfg()
+    _refused(_forward(c, h0=X, h_last=X + 4), "h0 and h_last")
+    _refused(_forward(c, h0=X + 4 * (3 * 8 - 1), h_last=X), "h0 and h_last")
+    _refused(_backward(c, dh_last=X, dh0=X + 4), "dh_last and dh0")
+    L, c = tp.load(), _cfg(T=1)
+    r = _rows(c)
+    _refused(L.tp_recur_step(C.byref(c), r, r, r, X, X + 32, r, None), "h and h_out")
