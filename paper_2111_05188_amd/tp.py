@@ -795,7 +795,8 @@ def mx4_quantize(x: torch.Tensor, out: Mx4T | None = None, stream=None) -> Mx4T:
     bits."""
     p, dt = _matrix(x)
     if out is None:
-        out = Mx4T.empty(x.shape[0], x.shape[1], x.device)
+        with torch.cuda.stream(stream):
+            out = Mx4T.empty(x.shape[0], x.shape[1], x.device)
     assert x.shape == (out.rows, out.K)
     _check(load().tp_mx4_quantize(p, dt, x.stride(0), x.stride(1), C.byref(out.s),
                                   _stream(stream)))
@@ -823,8 +824,9 @@ def mx4_workspace(M: int, N: int, K: int, device="cuda") -> torch.Tensor:
 def mx4_matmul(a: Mx4T, w: Mx4T, y: torch.Tensor, bias: torch.Tensor | None = None,
                act: int = TP_ACT_NONE, work: torch.Tensor | None = None, stream=None):
     """y [M][N] = act(a w^T + bias) of 4-bit a [M][K] and w [N][K]."""
-    if work is None:
-        work = mx4_workspace(a.rows, w.rows, a.K, y.device)
+    if work is None:                    # (the stream's memory: it is given back before the end)
+        with torch.cuda.stream(stream):
+            work = mx4_workspace(a.rows, w.rows, a.K, y.device)
     p, dt = _matrix(y)
     assert y.shape == (a.rows, w.rows) and (w.rows == 1 or y.stride(1) == 1)
     assert bias is None or (bias.shape == (w.rows,) and bias.dtype == torch.float32
@@ -839,7 +841,8 @@ def mx4_linear(x: torch.Tensor, w: Mx4T, y: torch.Tensor, bias: torch.Tensor | N
     [M][K] in 4 bits."""
     M = x.shape[0]
     if work is None:
-        work = mx4_workspace(M, w.rows, w.K, y.device)
+        with torch.cuda.stream(stream):
+            work = mx4_workspace(M, w.rows, w.K, y.device)
     px, dx = _matrix(x)
     p, dt = _matrix(y)
     assert x.shape == (M, w.K) and (w.K == 1 or x.stride(1) == 1)

@@ -283,6 +283,35 @@ def test_streams_and_graph_replays():
             assert torch.equal(p, t)
 
 
+def test_memory_of_a_call_on_another_stream():
+    """What a call on a stream allocates itself is not handed out again before it has run: the
+    current stream's next memory is filled with other bytes while the call waits for its turn."""
+    M, N, K = 500, 100, 1601
+    x, w = matrix(M, K, torch.float32, 20, "odd"), matrix(N, K, torch.float32, 21)
+    qa, qw = tp.mx4_quantize(x), tp.mx4_quantize(w)
+    want, back_x = torch.empty(M, N, device="cuda"), torch.empty(M, K, device="cuda")
+    tp.mx4_linear(x, qw, want)
+    tp.mx4_dequantize(qa, back_x)
+    torch.cuda.synchronize()
+    nb = tp.mx4_workspace(M, N, K).numel()
+    s = torch.cuda.Stream()
+    for call in (lambda y: tp.mx4_linear(x, qw, y, stream=s),
+                 lambda y: tp.mx4_matmul(qa, qw, y, stream=s),
+                 lambda y: tp.mx4_matmul(tp.mx4_quantize(x, stream=s), qw, y, stream=s)):
+        y = torch.empty(M, N, device="cuda")
+        torch.cuda.synchronize()
+        with torch.cuda.stream(s):
+            torch.cuda._sleep(50_000_000)
+        call(y)
+        assert not s.query()
+        others = [torch.full((n,), 0xEE, dtype=torch.uint8, device="cuda")
+                  for n in (nb, nb, tp.mx4_bytes(M, K))]
+        torch.cuda.current_stream().synchronize()
+        s.synchronize()
+        del others
+        assert torch.equal(y, want)
+
+
 def test_refusals():
     x = torch.zeros(4, 64, device="cuda")
     w = tp.mx4_quantize(torch.zeros(5, 64, device="cuda"))
