@@ -21,14 +21,18 @@ from . import tp
 
 
 class MemoryLayer:
-    """D channels over observations of S features.  W [3 D][S] fp32, lam [D] fp32."""
+    """D channels over observations of S features.  W [3 D][S] fp32, lam [D] fp32.
+
+    Calls may be on different streams (`stream`, else torch's current one): each waits for what
+    earlier calls have queued, since they share the layer's buffers."""
 
     def __init__(self, W: torch.Tensor, lam: torch.Tensor, dtype=torch.bfloat16):
         self.D, self.S = lam.shape[0], W.shape[1]
         assert W.shape == (3 * self.D, self.S) and W.dtype == lam.dtype == torch.float32
         self.W, self.lam, self.dtype = W, lam, dtype
         self.w4 = tp.mx4_quantize(W)
-        self.rc = None
+        self.rc = self.work1 = None
+        self.stream = torch.cuda.current_stream()
 
     @staticmethod
     def init(S: int, D: int, seed: int = 0, dtype=torch.bfloat16, device="cuda"):
@@ -37,6 +41,20 @@ class MemoryLayer:
         W = torch.randn(3 * D, S, generator=g, device=device) * S ** -0.5
         a = 1.0 - 10.0 ** -torch.linspace(1.0, 3.0, D, device=device)
         return MemoryLayer(W, torch.log(torch.expm1(-torch.log(a) / 4.0)), dtype)
+
+    def _turn(self):
+        """The current stream, after a change of streams: in order behind the last call's, and
+        known to the allocator as a user of the buffers, which other calls may give back."""
+        s, last = torch.cuda.current_stream(), self.stream
+        if s != last:
+            if not torch.cuda.is_current_stream_capturing():    # (a capture begins in order)
+                s.wait_stream(last)
+            for t in vars(self).values():
+                t = t.data if isinstance(t, tp.Mx4T) else t
+                if isinstance(t, torch.Tensor):
+                    t.record_stream(s)
+            self.stream = s
+        return s
 
     def parts(self, gates):
         D = self.D
@@ -64,39 +82,49 @@ class MemoryLayer:
         of the layer, which its next encode of this size writes again; the last states may be
         that call's h0."""
         T, B, ld = obs.shape
-        self._sequence(T, B, done, lens)
-        self.rows = obs.reshape(T * B, ld)[:, :self.S]
-        tp.mx4_linear(self.rows, self.w4, self.gates.view(T * B, -1), work=self.work4,
-                      stream=stream)
-        tp.recur_forward(self.rc, *self.parts(self.gates), self.y, self.work, h0=h0,
-                         h_last=self.h_last, saved=self.saved, stream=stream)
+        with torch.cuda.stream(stream):
+            for t in (obs, done, lens):         # (the layer keeps them for the gradients)
+                if stream is not None and t is not None:
+                    t.record_stream(stream)
+            stream = self._turn()
+            self._sequence(T, B, done, lens)
+            self.rows = obs.reshape(T * B, ld)[:, :self.S]
+            tp.mx4_linear(self.rows, self.w4, self.gates.view(T * B, -1), work=self.work4,
+                          stream=stream)
+            tp.recur_forward(self.rc, *self.parts(self.gates), self.y, self.work, h0=h0,
+                             h_last=self.h_last, saved=self.saved, stream=stream)
         return self.y, self.h_last
 
     def gradients(self, dy, dh_last=None, stream=None):
         """Gradients of the last encode's W, lambda and first states, from dy [T][B][D] (buffers
         of the layer)."""
-        tp.recur_backward(self.rc, *self.parts(self.gates), self.saved, dy,
-                          *self.parts(self.dgates), self.dlam, self.work, dh_last=dh_last,
-                          dh0=self.dh0, stream=stream)
         n = self.rc.T * self.rc.B
-        tp.mx4_quantize(self.dgates.view(n, -1).t(), self.dg4, stream=stream)
-        tp.mx4_quantize(self.rows.t(), self.obs4, stream=stream)
-        tp.mx4_matmul(self.dg4, self.obs4, self.dW, work=self.workW, stream=stream)
+        with torch.cuda.stream(stream):
+            stream = self._turn()
+            tp.recur_backward(self.rc, *self.parts(self.gates), self.saved, dy,
+                              *self.parts(self.dgates), self.dlam, self.work, dh_last=dh_last,
+                              dh0=self.dh0, stream=stream)
+            tp.mx4_quantize(self.dgates.view(n, -1).t(), self.dg4, stream=stream)
+            tp.mx4_quantize(self.rows.t(), self.obs4, stream=stream)
+            tp.mx4_matmul(self.dg4, self.obs4, self.dW, work=self.workW, stream=stream)
         return self.dW, self.dlam, self.dh0
 
     def refresh(self, stream=None):
         """The weights in 4 bits again, after an optimiser has changed W."""
-        tp.mx4_quantize(self.W, self.w4, stream=stream)
+        with torch.cuda.stream(stream):
+            tp.mx4_quantize(self.W, self.w4, stream=self._turn())
 
     def step(self, obs, h, done=None, stream=None):
         """One bar: y [B][D] of observations [B][ld]; the states h [B][D] move on in place."""
-        B = obs.shape[0]
-        gates = torch.empty(B, 3 * self.D, dtype=self.dtype, device=obs.device)
-        y = torch.empty(B, self.D, dtype=self.dtype, device=obs.device)
-        if getattr(self, "work1", None) is None or self.work1[0] != B:
-            self.work1 = (B, tp.mx4_workspace(B, 3 * self.D, self.S, obs.device))
-        tp.mx4_linear(obs[:, :self.S], self.w4, gates, work=self.work1[1], stream=stream)
-        tp.recur_step(*self.parts(gates), self.lam, h, h, y, done=done, stream=stream)
+        B, D = obs.shape[0], self.D
+        with torch.cuda.stream(stream):
+            stream = self._turn()
+            gates = torch.empty(B, 3 * D, dtype=self.dtype, device=obs.device)
+            y = torch.empty(B, D, dtype=self.dtype, device=obs.device)
+            if self.work1 is None or self.B1 != B:
+                self.B1, self.work1 = B, tp.mx4_workspace(B, 3 * D, self.S, obs.device)
+            tp.mx4_linear(obs[:, :self.S], self.w4, gates, work=self.work1, stream=stream)
+            tp.recur_step(*self.parts(gates), self.lam, h, h, y, done=done, stream=stream)
         return y
 
 

@@ -99,3 +99,102 @@ def test_a_trajectory_in_parts(dtype, tol):
     torch.cuda.synchronize()
     rms_close(torch.cat(parts), host(y), tol)
     rms_close(h, host(last), 2e-5)
+
+
+def clobber(stream, *sizes):
+    """The current stream's next memory of these sizes in bytes, filled with other bytes while
+    `stream` has its work before it."""
+    junk = [torch.full((n,), 0xEE, dtype=torch.uint8, device="cuda") for n in sizes for _ in range(2)]
+    torch.cuda.current_stream().synchronize()
+    assert not stream.query()
+    return junk
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_calls_on_a_stream_of_their_own(dtype):
+    """Calls on a stream that is busy, while the current stream goes on with its own work: the
+    layer's temporaries, copies and buffers of another size are in the order of the calls."""
+    S, D, T, B = 301, 64, 40, 30
+    g = torch.Generator("cuda").manual_seed(8)
+    obs = torch.randn(B, T, 320, generator=g, device="cuda").transpose(0, 1)    # not in one piece
+    dy = torch.randn(T, B, D, generator=g, device="cuda").to(dtype)
+    layer = memory.MemoryLayer.init(S, D, 7, dtype)
+    size = torch.empty(0, dtype=dtype).element_size()
+
+    def calls(stream):
+        h = torch.zeros(B, D, device="cuda")
+        layer.encode(obs)                       # buffers from before, of the current stream
+        torch.cuda.synchronize()
+        own = stream is not None
+        if own:
+            with torch.cuda.stream(stream):
+                torch.cuda._sleep(100_000_000)
+        out, kept = [], []
+        for t in range(3):
+            out.append(layer.step(obs[t], h, stream=stream))
+            if own:
+                kept += clobber(stream, 3 * B * D * size, B * D * size)
+        if own:
+            torch.cuda._sleep(1_000_000)        # the current stream is busy too
+        out += [*layer.encode(obs, stream=stream), *layer.gradients(dy, stream=stream)]
+        kept_sizes = [t.numel() * t.element_size() for t in
+                      (layer.gates, layer.dgates, layer.saved, layer.work, layer.workW,
+                       layer.dg4.data, layer.obs4.data, layer.work1)]
+        out += layer.encode(obs[:20], stream=stream)
+        out.append(layer.step(obs[0, :20], h[:20], stream=stream))
+        if own:
+            kept += clobber(stream, *kept_sizes)
+            stream.synchronize()
+        torch.cuda.synchronize()
+        return [t.clone() for t in (*out, h)]
+
+    want = calls(None)
+    for t, p in zip(want, calls(torch.cuda.Stream())):
+        assert torch.equal(t, p)
+
+
+def test_streams_take_turns():
+    """Calls of one layer on two streams without a wait between them run in their order."""
+    layer = memory.MemoryLayer.init(31, 64, 9, torch.float32)
+    obs = torch.randn(2, 50, 8, 32, generator=torch.Generator("cuda").manual_seed(10), device="cuda")
+    dy = torch.ones(50, 8, 64, device="cuda")
+    want = []
+    for o in obs:
+        layer.encode(o)
+        want.append([t.clone() for t in layer.gradients(dy)])
+    torch.cuda.synchronize()
+    a, b = torch.cuda.Stream(), torch.cuda.Stream()
+    with torch.cuda.stream(a):
+        torch.cuda._sleep(50_000_000)
+    layer.encode(obs[0], stream=a)
+    got = layer.gradients(dy, stream=b)
+    with torch.cuda.stream(b):
+        first = [t.clone() for t in got]
+    layer.encode(obs[1], stream=a)
+    second = layer.gradients(dy, stream=a)
+    torch.cuda.synchronize()
+    for p, q in zip(want, (first, second)):
+        for t, u in zip(p, q):
+            assert torch.equal(t, u)
+
+
+def test_step_in_a_graph():
+    """One bar captured and replayed on new observations, after steps outside the capture."""
+    layer = memory.MemoryLayer.init(31, 64, 11)
+    g = torch.Generator("cuda").manual_seed(12)
+    obs, h = torch.randn(8, 32, generator=g, device="cuda"), torch.zeros(8, 64, device="cuda")
+    layer.step(obs, h)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        y = layer.step(obs, h)
+    for _ in range(3):
+        obs.normal_(generator=g)
+        h.fill_(0.5)
+        want = layer.step(obs, h).clone()
+        state = h.clone()
+        h.fill_(0.5)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(y, want) and torch.equal(h, state)
