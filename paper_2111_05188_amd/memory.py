@@ -88,8 +88,8 @@ class MemoryLayer:
                     t.record_stream(stream)
             stream = self._turn()
             self._sequence(T, B, done, lens)
-            self.rows = obs.reshape(T * B, ld)[:, :self.S]
-            tp.mx4_linear(self.rows, self.w4, self.gates.view(T * B, -1), work=self.work4,
+            self.rows = obs.reshape(T * B, ld)
+            tp.mx4_linear(self.rows[:, :self.S], self.w4, self.gates.view(T * B, -1), work=self.work4,
                           stream=stream)
             tp.recur_forward(self.rc, *self.parts(self.gates), self.y, self.work, h0=h0,
                              h_last=self.h_last, saved=self.saved, stream=stream)
@@ -105,9 +105,18 @@ class MemoryLayer:
                               *self.parts(self.dgates), self.dlam, self.work, dh_last=dh_last,
                               dh0=self.dh0, stream=stream)
             tp.mx4_quantize(self.dgates.view(n, -1).t(), self.dg4, stream=stream)
-            tp.mx4_quantize(self.rows.t(), self.obs4, stream=stream)
+            tp.mx4_quantize(self._seen()[:, :self.S].t(), self.obs4, stream=stream)
             tp.mx4_matmul(self.dg4, self.obs4, self.dW, work=self.workW, stream=stream)
         return self.dW, self.dlam, self.dh0
+
+    def _seen(self):
+        """The rows that the sequences have.  What lies past their ends has no gradient, but would
+        share its blocks of 32 rows, and so their scale, with what has: zeros in its place."""
+        lens = self.rc.lens
+        if lens is None:
+            return self.rows
+        past = torch.arange(self.rc.T, device=lens.device)[:, None] >= lens
+        return self.rows.masked_fill(past.view(-1, 1), 0.0)
 
     def refresh(self, stream=None):
         """The weights in 4 bits again, after an optimiser has changed W."""

@@ -198,3 +198,31 @@ def test_step_in_a_graph():
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(y, want) and torch.equal(h, state)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("junk", [1e6, float("nan"), float("inf")])
+def test_nothing_past_a_sequences_end_matters(dtype, junk):
+    """Ragged lengths: whatever the observations hold past them, every result is that of zeros
+    there, and W's gradient the product over the rows that the sequences have."""
+    T, B, S, D = 37, 9, 70, 48
+    g = torch.Generator("cuda").manual_seed(13)
+    lens = torch.tensor([0, T, 1, 5, 36, 20, 31, 12, 17], dtype=torch.int32, device="cuda")
+    past = torch.arange(T, device="cuda")[:, None] >= lens
+    clean = torch.randn(T, B, 96, generator=g, device="cuda").to(dtype).masked_fill(past[..., None], 0.0)
+    dirty = clean.masked_fill(past[..., None], junk)
+    done = (torch.rand(T, B, generator=g, device="cuda") < 0.1).byte()
+    h0, dh = torch.randn(2, B, D, generator=g, device="cuda")
+    dy = torch.randn(T, B, D, generator=g, device="cuda").to(dtype)
+    layer, res = memory.MemoryLayer.init(S, D, 14, dtype), []
+    for obs in (clean, dirty):
+        out = [*layer.encode(obs, done, lens, h0), *layer.gradients(dy, dh)]
+        torch.cuda.synchronize()
+        res.append([t.clone() for t in (*out, layer.dgates)])
+    for p, q in zip(*res):
+        assert torch.isfinite(p).all() and torch.equal(p, q)
+    a = mx4.values(host(layer.dgates.reshape(T * B, -1)).T)
+    b = mx4.values(host(clean.reshape(T * B, -1)[:, :S]).T)
+    want, mass = mx4.product(a, b)
+    assert (np.abs(host(layer.dW) - want) <= (T * B / 64 + 8) * 2.0 ** -23 * mass).all()
+    assert (layer.dgates[past] == 0).all()
