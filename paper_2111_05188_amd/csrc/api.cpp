@@ -375,7 +375,7 @@ int mx4_product(Mx4Args &a, const float *bias, int32_t act, void *y, int32_t dty
     a.act = act;
     a.y = y;
     a.y_bf16 = dtype == TP_BF16;
-    a.ldy = ldy;
+    a.ldy = M == 1 ? N : ldy;           // never followed
     a.work = work;
     hipError_t e = launch_mx4_product(a, (hipStream_t)stream);
     if (e != hipSuccess) return hip_fail(e, "4-bit product launch");
@@ -1087,9 +1087,9 @@ int tp_mx4_quantize(const void *x, int32_t dtype, int64_t row_stride, int64_t co
     int rc = check_mx4(out, "output");
     if (rc != TP_OK) return rc;
     const int64_t rows = out->rows, K = out->K;
-    // the stride of an axis of one is never followed
+    // the stride of an axis of one is never followed (0: as aligned as the base)
     if (K == 1) col_stride = 1;
-    else if (rows == 1) row_stride = 1;
+    if (rows == 1) row_stride = col_stride == 1 ? 0 : 1;
     const bool by_rows = col_stride == 1;
     if (!by_rows && row_stride != 1)
         return fail(TP_EUNSUPPORTED, "4-bit source: strides %lld, %lld, one of them must be 1",
@@ -1147,7 +1147,8 @@ int tp_mx4_linear(const void *x, int32_t x_dtype, int64_t M, int64_t ldx, const 
     int rc = check_mx4(w, "w");
     if (rc != TP_OK) return rc;
     if ((rc = check_mx4_size(M, w->K, "x")) != TP_OK) return rc;
-    if (M == 1) ldx = w->K;             // never followed
+    // never followed; in whole 16 bytes, so that the row is as aligned as its base
+    if (M == 1) ldx = (w->K + 7) / 8 * 8;
     if ((rc = check_matrix(x, x_dtype, ldx, w->K, "x")) != TP_OK) return rc;
     Mx4Args p{};
     p.x = x;

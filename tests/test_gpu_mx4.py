@@ -224,6 +224,23 @@ def test_repeated_rows_and_one_row():
     assert torch.equal(y, z.expand(33, 40))
 
 
+@pytest.mark.parametrize("dtype", BOTH)
+@pytest.mark.parametrize("K", [1, 31, 301, 1001])
+def test_one_row_goes_to_4_bits_on_the_way(K, dtype):
+    """A row's pitch means nothing to a single one: with an aligned base, x of any length goes to 4
+    bits inside the product, so the workspace stays as it was."""
+    w = matrix(192, K, torch.float32, 22)
+    x, qw = matrix(1, K, dtype, 23), tp.mx4_quantize(w)
+    work = tp.mx4_workspace(1, 192, K).fill_(0xEE)
+    y, z = torch.empty(1, 192, device="cuda"), torch.empty(2, 192, device="cuda")
+    tp.mx4_linear(x, qw, y, work=work)
+    tp.mx4_linear(x.repeat(2, 1), qw, z)
+    torch.cuda.synchronize()
+    assert (work == 0xEE).all() and torch.equal(y, z[:1])
+    assert np.array_equal(back(tp.mx4_quantize(x)), mx4.values(host(x)))
+    check(host(y), mx4.values(host(x)), mx4.values(host(w)), None, None, torch.float32, K)
+
+
 def test_rows_past_four_gigabytes():
     """Source and output rows whose offsets pass 32 bits."""
     K, N, M = 64, 32, 9
