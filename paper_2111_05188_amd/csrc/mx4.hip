@@ -358,8 +358,10 @@ hipError_t launch_mx4_quantize(const void *x, bool bf16, int64_t row_stride, int
 hipError_t launch_mx4_dequantize(const void *src, const Mx4Layout &L, void *y, bool bf16,
                                  int64_t ld, hipStream_t s)
 {
-    // (eight rows of under 2^32 elements, a piece in two rows at most)
-    if (!vec16(y, ld, bf16 ? 2 : 4) && ld == L.K && L.K >= 8 && (uintptr_t)y % 16 == 0) {
+    // (eight rows of under 2^32 elements, a piece in two rows at most, under
+    // 2^32 threads)
+    if (!vec16(y, ld, bf16 ? 2 : 4) && ld == L.K && L.K >= 8 && (uintptr_t)y % 16 == 0 &&
+        L.rows <= 1 << 26) {
         const int64_t pieces = 8 * L.K / (bf16 ? 8 : 4), most = (pieces + 511) / 512;
         const int64_t parts = most < 65535 ? most : 65535;      // two pieces a thread
         hipLaunchKernelGGL((bf16 ? mx4_dequantize_flat_kernel<true> : mx4_dequantize_flat_kernel<false>),

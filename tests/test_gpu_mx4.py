@@ -258,6 +258,18 @@ def test_rows_past_four_gigabytes():
     assert torch.equal(out.contiguous(), y)
 
 
+def test_the_most_rows():
+    """2^27 rows of odd length, one after the other, and back."""
+    rows, K = 1 << 27, 9
+    one = matrix(1, K, torch.bfloat16, 24)
+    m = tp.mx4_quantize(one.expand(rows, K))
+    y = torch.full((rows, K), 7.0, dtype=torch.bfloat16, device="cuda")
+    tp.mx4_dequantize(m, y)
+    want = torch.from_numpy(mx4.values(host(one))).cuda().bfloat16()
+    torch.cuda.synchronize()
+    assert (y == want).all()
+
+
 def test_streams_and_graph_replays():
     """On a stream of its own, and captured in a HIP graph and replayed on new inputs."""
     M, N, K = 300, 100, 301
