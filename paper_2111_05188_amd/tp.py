@@ -701,11 +701,23 @@ class RecurT:
             v += (t.data_ptr(), st, sb)
         return _rows(v)
 
+    def kept(self, t: torch.Tensor | None):
+        if t is None:
+            return None
+        assert t.numel() >= self.saved_count and t.dtype is torch.float32 and t.is_contiguous()
+        return t.data_ptr()
+
     def state(self, t: torch.Tensor | None):
         if t is None:
             return None
         assert t.shape == (self.B, self.D) and t.dtype is torch.float32 and t.is_contiguous()
         return t.data_ptr()
+
+
+def _work(t):
+    """A workspace's address and bytes."""
+    assert t.is_contiguous()
+    return t.data_ptr(), t.numel() * t.element_size()
 
 
 def _rows(v):
@@ -718,23 +730,20 @@ def _rows(v):
 def recur_forward(rc: RecurT, x, r, i, y, work, h0=None, h_last=None, saved=None, stream=None):
     """y [T][B][D] (or None) and h_last [B][D] of x, r, i [T][B][D]; saved
     (rc.saved()) keeps what recur_backward needs."""
-    assert saved is None or saved.numel() >= rc.saved_count
     keep, (px, pr, pi, py) = rc.rows(x, r, i, y)
     _check(load().tp_recur_forward(C.byref(rc.s), px, pr, pi, rc.state(h0), py, rc.state(h_last),
-                                   _ptr(saved), work.data_ptr(), work.numel(), _stream(stream)))
+                                   rc.kept(saved), *_work(work), _stream(stream)))
 
 
 def recur_backward(rc: RecurT, x, r, i, saved, dy, dx, dr, di, dlam, work, dh_last=None,
                    dh0=None, stream=None):
     """Gradients of recur_forward's inputs into dx, dr, di [T][B][D], dlam [D]
     and dh0 [B][D]."""
-    assert saved.numel() >= rc.saved_count
     assert dlam.shape == (rc.D,) and dlam.dtype is torch.float32 and dlam.is_contiguous()
     keep, (px, pr, pi, pdy, pdx, pdr, pdi) = rc.rows(x, r, i, dy, dx, dr, di)
-    _check(load().tp_recur_backward(C.byref(rc.s), px, pr, pi, saved.data_ptr(), pdy,
+    _check(load().tp_recur_backward(C.byref(rc.s), px, pr, pi, rc.kept(saved), pdy,
                                     rc.state(dh_last), pdx, pdr, pdi, dlam.data_ptr(),
-                                    rc.state(dh0), work.data_ptr(), work.numel(),
-                                    _stream(stream)))
+                                    rc.state(dh0), *_work(work), _stream(stream)))
 
 
 def recur_step(x, r, i, lam, h, h_out, y=None, done=None, stream=None):
@@ -832,7 +841,7 @@ def mx4_matmul(a: Mx4T, w: Mx4T, y: torch.Tensor, bias: torch.Tensor | None = No
     assert bias is None or (bias.shape == (w.rows,) and bias.dtype == torch.float32
                             and bias.is_contiguous())
     _check(load().tp_mx4_matmul(C.byref(a.s), C.byref(w.s), _ptr(bias), act, p, dt, _pitch(y),
-                                _ptr(work), work.numel(), _stream(stream)))
+                                *_work(work), _stream(stream)))
 
 
 def mx4_linear(x: torch.Tensor, w: Mx4T, y: torch.Tensor, bias: torch.Tensor | None = None,
@@ -850,4 +859,4 @@ def mx4_linear(x: torch.Tensor, w: Mx4T, y: torch.Tensor, bias: torch.Tensor | N
     assert bias is None or (bias.shape == (w.rows,) and bias.dtype == torch.float32
                             and bias.is_contiguous())
     _check(load().tp_mx4_linear(px, dx, M, _pitch(x), C.byref(w.s), _ptr(bias), act, p, dt,
-                                _pitch(y), _ptr(work), work.numel(), _stream(stream)))
+                                _pitch(y), *_work(work), _stream(stream)))

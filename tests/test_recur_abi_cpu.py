@@ -2,6 +2,9 @@
 
 import ctypes as C
 
+import pytest
+import torch
+
 from paper_2111_05188_amd import tp
 
 X = 0x100000
@@ -105,3 +108,19 @@ def test_states_that_overlap_in_part_are_refused():
     L, c = tp.load(), _cfg(T=1)
     r = _rows(c)
     _refused(L.tp_recur_step(C.byref(c), r, r, r, X, X + 32, r, None), "h and h_out")
+
+
+def test_kept_states_of_another_type_or_without_memory_are_refused():
+    """As many elements, but fewer bytes than the kernels write."""
+    T, B, D = 40, 3, 8
+    rc = tp.RecurT(torch.zeros(D), T, B, torch.float32)
+    x, n = torch.zeros(T, B, D), rc.saved_count
+    work, dlam = rc.workspace(), torch.zeros(D)
+    for saved in (torch.zeros(n, dtype=torch.bfloat16), torch.zeros(n, dtype=torch.uint8),
+                  torch.zeros(1).expand(n), torch.zeros(n - 1)):
+        with pytest.raises(AssertionError):
+            tp.recur_forward(rc, x, x, x, x.clone(), work, saved=saved)
+        with pytest.raises(AssertionError):
+            tp.recur_backward(rc, x, x, x, saved, x, x, x, x, dlam, work)
+    with pytest.raises(AssertionError):
+        tp.recur_forward(rc, x, x, x, x.clone(), work[:1].expand(work.numel()))
