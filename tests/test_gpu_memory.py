@@ -226,3 +226,38 @@ def test_nothing_past_a_sequences_end_matters(dtype, junk):
     want, mass = mx4.product(a, b)
     assert (np.abs(host(layer.dW) - want) <= (T * B / 64 + 8) * 2.0 ** -23 * mass).all()
     assert (layer.dgates[past] == 0).all()
+
+
+@pytest.mark.parametrize("dtype,tol", [(torch.float32, 3e-5), (torch.bfloat16, 3e-5 + 2.0 ** -8)])
+def test_states_and_gradients_of_a_layer(dtype, tol):
+    """Both types, with first states, last states' gradients, episode ends and lengths: each part
+    against 64 bits on what the part before it stored."""
+    T, B, S, D = 60, 5, 301, 40
+    rng = np.random.default_rng(15)
+    dev = lambda v, dt: torch.from_numpy(np.asarray(v)).cuda().to(dt)  # noqa: E731
+    obs = dev(rng.normal(size=(T, B, 320)), dtype)
+    done, lens = (rng.random((T, B)) < 0.05).astype(np.uint8), np.array([60, 0, 7, 33, 59], np.int32)
+    h0, dh, dy = rng.normal(size=(B, D)), rng.normal(size=(B, D)), rng.normal(size=(T, B, D))
+    layer = memory.MemoryLayer.init(S, D, 16, dtype)
+    y, last = layer.encode(obs, dev(done, torch.uint8), dev(lens, torch.int32), dev(h0, torch.float32))
+    dy = dev(dy, dtype)
+    dW, dlam, dh0 = layer.gradients(dy, dev(dh, torch.float32))
+    torch.cuda.synchronize()
+    x, w = mx4.values(host(obs.reshape(T * B, -1)[:, :S])), mx4.values(host(layer.W))
+    want, mass = mx4.product(x, w)
+    off = np.abs(host(layer.gates).reshape(T * B, -1) - want)
+    assert (off <= (S / 64 + 8) * 2.0 ** -23 * mass +
+            (2.0 ** -8 * np.abs(want) if dtype == torch.bfloat16 else 0.0)).all()
+    parts, lam = [host(v) for v in layer.parts(layer.gates)], host(layer.lam)
+    h0, dh = h0.astype(np.float32).astype(np.float64), dh.astype(np.float32).astype(np.float64)
+    wy, wl = recur.forward(*parts, lam, h0, done, lens)
+    rms_close(y, wy, tol)
+    rms_close(last, wl, 3e-5)
+    dx, dr, di, wlam, wh0, mass = recur.backward(*parts, lam, host(dy), dh, h0, done, lens)
+    rms_close(layer.dgates, np.concatenate([dx, dr, di], axis=2), tol)
+    assert (np.abs(host(dlam) - wlam) <= 3e-5 * mass + 1e-16).all()
+    rms_close(dh0, wh0, 3e-5)
+    seen = (np.arange(T)[:, None] < lens).reshape(-1, 1)
+    want, mass = mx4.product(mx4.values(host(layer.dgates).reshape(T * B, -1).T),
+                             mx4.values(np.where(seen, host(obs).reshape(T * B, -1)[:, :S], 0.0).T))
+    assert (np.abs(host(dW) - want) <= (T * B / 64 + 8) * 2.0 ** -23 * mass).all()

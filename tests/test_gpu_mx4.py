@@ -164,6 +164,33 @@ def test_linear(shape, layout, xdtype, dtype):
           dtype, K)
 
 
+@pytest.mark.parametrize("dtype", BOTH)
+@pytest.mark.parametrize("xdtype", [torch.float32, torch.bfloat16, None])
+@pytest.mark.parametrize("M,N,K", [(33000, 1536, 1001), (33000, 1001, 301), (16400, 1100, 512),
+                                   (16400, 1536, 40)])
+def test_many_rows(M, N, K, xdtype, dtype):
+    """Rows enough that a workgroup passes many tiles of W: several pieces of y's columns, whole
+    and partial, from starting points of each workgroup's own.  Every row is one of 300, whose
+    results a small call gives; x in memory, or (None) in 4 bits."""
+    say(f"[mx4] many rows {M, N, K} {xdtype} {dtype}")
+    base, w = matrix(300, K, xdtype or torch.float32, 25), matrix(N, K, torch.float32, 26)
+    bias = torch.randn(N, generator=torch.Generator("cuda").manual_seed(27), device="cuda")
+    pick = torch.randint(0, 300, (M,), generator=torch.Generator("cuda").manual_seed(28),
+                         device="cuda")
+    x = torch.zeros(M, -(-K // 32) * 32, dtype=base.dtype, device="cuda")[:, :K]
+    x.copy_(base[pick])
+    qw, small = tp.mx4_quantize(w), torch.empty(300, N, dtype=dtype, device="cuda")
+    wide = torch.full((M, N + 8), 7.0, dtype=dtype, device="cuda")
+    for rows, y in ((base, small), (x, wide[:, :N])):
+        if xdtype is None:
+            tp.mx4_matmul(tp.mx4_quantize(rows), qw, y, bias=bias)
+        else:
+            tp.mx4_linear(rows, qw, y, bias=bias)
+    torch.cuda.synchronize()
+    check(host(small), mx4.values(host(base)), mx4.values(host(w)), host(bias), None, dtype, K)
+    assert torch.equal(wide[:, :N], small[pick]) and (wide[:, N:] == 7.0).all()
+
+
 @pytest.mark.parametrize("M,N,K", [(96, 64, 20000), (5, 7, 65537), (1, 1, 4097), (200, 1001, 3001)])
 def test_long_sums(M, N, K):
     """The long axis is split over workgroups and joined in a fixed order."""

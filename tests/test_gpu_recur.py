@@ -177,6 +177,13 @@ def test_many_sequences(shape, dtype):
                                                     shape[1] ** 0.5)).all()
 
 
+@pytest.mark.parametrize("shape,dtype", [((64, 2100, 130), torch.float32),
+                                         ((64, 2100, 256), torch.bfloat16)])
+def test_more_than_the_last_level_cache_holds(shape, dtype):
+    """Over 256 MB of two channels a lane and a wave a sequence: loads and stores past the caches."""
+    test_many_sequences(shape, dtype)
+
+
 @pytest.mark.parametrize("dtype", BOTH)
 @pytest.mark.parametrize("shape", [(33, 3, 66), (300, 2, 64), (20, 1100, 128)])
 def test_nothing_past_a_sequences_end_matters(shape, dtype):
@@ -369,6 +376,13 @@ def test_step_continues_a_sequence(B, D, dtype):
                                c.done[t:t + 1, pick])
         close("y", host(y)[pick], wy[0], TOL[dtype])
         close("h", host(h)[pick], wh, 2e-5)
+
+
+@pytest.mark.parametrize("dtype", BOTH)
+@pytest.mark.parametrize("B,D", [(1000, 130), (300, 192), (32768, 516)])
+def test_step_of_two_and_four_channels_a_lane(B, D, dtype):
+    """The widths below 256, and steps of more bytes than the last-level cache holds."""
+    test_step_continues_a_sequence(B, D, dtype)
 
 
 def test_step_equals_the_sequence_kernel():
