@@ -476,8 +476,9 @@ def backtest_metrics(v0: torch.Tensor, v: torch.Tensor, periods_per_year: float,
     T, E = v.shape
     if out is None:
         out = torch.empty(E, 5, dtype=torch.float64, device=v.device)
-    if work is None:
-        work = backtest_metrics_workspace(T, E, v.device)
+    if work is None:                    # (the stream's memory: it is given back before the end)
+        with torch.cuda.stream(stream):
+            work = backtest_metrics_workspace(T, E, v.device)
     _check(load().tp_backtest_metrics(_ptr(v0), _ptr(v), T, E, periods_per_year,
                                       risk_free, _ptr(out), _ptr(work), work.numel(),
                                       _stream(stream)))

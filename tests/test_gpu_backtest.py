@@ -129,3 +129,25 @@ def test_metrics_edge_cases():
     assert met[0, 2] == 0.0 and met[0, 3] == 0.0
     with pytest.raises(tp.TPError):
         tp.backtest_metrics(v0, v, 0.0)
+
+
+def test_workspace_of_a_call_on_another_stream():
+    """The call's own workspace is not handed out again before it has run: the current stream's
+    next memory is filled with other bytes while the call waits for its turn."""
+    T, E = 5000, 3
+    g = torch.Generator("cuda").manual_seed(3)
+    v = 1.0 + torch.rand(T, E, generator=g, device="cuda", dtype=torch.float64)
+    v0 = torch.ones(E, device="cuda", dtype=torch.float64)
+    want = tp.backtest_metrics(v0, v, 252.0, 0.02)
+    nb = tp.backtest_metrics_workspace(T, E).numel()
+    out, s = torch.empty_like(want), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(s):
+        torch.cuda._sleep(50_000_000)
+    tp.backtest_metrics(v0, v, 252.0, 0.02, out=out, stream=s)
+    junk = [torch.full((nb,), 0xEE, dtype=torch.uint8, device="cuda") for _ in range(2)]
+    torch.cuda.current_stream().synchronize()
+    assert not s.query()
+    s.synchronize()
+    del junk
+    assert torch.equal(out, want)
