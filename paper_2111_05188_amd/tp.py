@@ -715,12 +715,6 @@ class RecurT:
         return t.data_ptr()
 
 
-def _work(t):
-    """A workspace's address and bytes."""
-    assert t.is_contiguous()
-    return t.data_ptr(), t.numel() * t.element_size()
-
-
 def _rows(v):
     """An array of tp_rows (pointer, two strides each) and the addresses of its elements."""
     a = (C.c_int64 * len(v))(*v)
@@ -731,9 +725,10 @@ def _rows(v):
 def recur_forward(rc: RecurT, x, r, i, y, work, h0=None, h_last=None, saved=None, stream=None):
     """y [T][B][D] (or None) and h_last [B][D] of x, r, i [T][B][D]; saved
     (rc.saved()) keeps what recur_backward needs."""
+    assert work.is_contiguous()
     keep, (px, pr, pi, py) = rc.rows(x, r, i, y)
     _check(load().tp_recur_forward(C.byref(rc.s), px, pr, pi, rc.state(h0), py, rc.state(h_last),
-                                   rc.kept(saved), *_work(work), _stream(stream)))
+                                   rc.kept(saved), work.data_ptr(), work.numel(), _stream(stream)))
 
 
 def recur_backward(rc: RecurT, x, r, i, saved, dy, dx, dr, di, dlam, work, dh_last=None,
@@ -741,10 +736,12 @@ def recur_backward(rc: RecurT, x, r, i, saved, dy, dx, dr, di, dlam, work, dh_la
     """Gradients of recur_forward's inputs into dx, dr, di [T][B][D], dlam [D]
     and dh0 [B][D]."""
     assert dlam.shape == (rc.D,) and dlam.dtype is torch.float32 and dlam.is_contiguous()
+    assert work.is_contiguous()
     keep, (px, pr, pi, pdy, pdx, pdr, pdi) = rc.rows(x, r, i, dy, dx, dr, di)
     _check(load().tp_recur_backward(C.byref(rc.s), px, pr, pi, rc.kept(saved), pdy,
                                     rc.state(dh_last), pdx, pdr, pdi, dlam.data_ptr(),
-                                    rc.state(dh0), *_work(work), _stream(stream)))
+                                    rc.state(dh0), work.data_ptr(), work.numel(),
+                                    _stream(stream)))
 
 
 def recur_step(x, r, i, lam, h, h_out, y=None, done=None, stream=None):
@@ -839,10 +836,11 @@ def mx4_matmul(a: Mx4T, w: Mx4T, y: torch.Tensor, bias: torch.Tensor | None = No
             work = mx4_workspace(a.rows, w.rows, a.K, y.device)
     p, dt = _matrix(y)
     assert y.shape == (a.rows, w.rows) and (w.rows == 1 or y.stride(1) == 1)
+    assert work.is_contiguous()
     assert bias is None or (bias.shape == (w.rows,) and bias.dtype == torch.float32
                             and bias.is_contiguous())
     _check(load().tp_mx4_matmul(C.byref(a.s), C.byref(w.s), _ptr(bias), act, p, dt, _pitch(y),
-                                *_work(work), _stream(stream)))
+                                work.data_ptr(), work.numel(), _stream(stream)))
 
 
 def mx4_linear(x: torch.Tensor, w: Mx4T, y: torch.Tensor, bias: torch.Tensor | None = None,
@@ -857,7 +855,8 @@ def mx4_linear(x: torch.Tensor, w: Mx4T, y: torch.Tensor, bias: torch.Tensor | N
     p, dt = _matrix(y)
     assert x.shape == (M, w.K) and (w.K == 1 or x.stride(1) == 1)
     assert y.shape == (M, w.rows) and (w.rows == 1 or y.stride(1) == 1)
+    assert work.is_contiguous()
     assert bias is None or (bias.shape == (w.rows,) and bias.dtype == torch.float32
                             and bias.is_contiguous())
     _check(load().tp_mx4_linear(px, dx, M, _pitch(x), C.byref(w.s), _ptr(bias), act, p, dt,
-                                _pitch(y), *_work(work), _stream(stream)))
+                                _pitch(y), work.data_ptr(), work.numel(), _stream(stream)))
