@@ -227,7 +227,7 @@ struct TileReader {
 // A piece's elements come from two neighbouring dwords of codes, which may have
 // two scales, and where it passes a row's end from the next row's first.
 // (65,536 x 1,001 bf16: 115 us with an element a store, 54 with pieces that end
-// at the rows' ends, 48 so; 34 where pieces and rows agree.)
+// at the rows' ends, 45 so; 34 where pieces and rows agree.)
 // ---------------------------------------------------------------------------
 template <bool BF>
 __global__ __launch_bounds__(256) void mx4_dequantize_flat_kernel(const uint8_t *src, Mx4Layout L,

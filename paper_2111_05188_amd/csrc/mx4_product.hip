@@ -54,8 +54,8 @@ __device__ __forceinline__ void finish4(const Mx4Args &a, int64_t m, int64_t n, 
 // is multiplied, the next lies in registers and is stored to the other.
 // More workgroups than blocks: a part of K each; its sums go to the workspace as the lanes
 // hold them, 1 KiB a store, and mx4_join_kernel adds the parts in order.
-// 1,536 x 1,001 over K = 65,536: 64 us, 18 of them for launch and sums, then
-// 4.4 of the 8.4 PFLOP/s that the instruction reaches; with the copies in a row
+// 1,536 x 1,001 over K = 65,536: 67 us, 18 of them for launch and sums, then
+// 4.1 of the 8.4 PFLOP/s that the instruction reaches; with the copies in a row
 // before the matrix instructions 76 us, with fragments straight from L1 and 4 x
 // 2 tiles a wave 125 us.
 // ---------------------------------------------------------------------------
@@ -234,7 +234,7 @@ __global__ __launch_bounds__(256) void mx4_join_kernel(Mx4Args a, int nblocks, i
 // there with no other lane's help), and W goes past it one tile of 32 columns
 // at a time, from LDS, where the workgroup's waves share it.  x is read once,
 // y written once.  From L1 instead of LDS a tile took 1.7 us against 1.3.
-// 65,536 x 1,001 bf16 rows times 1,536: 91 us (2.2 PFLOP/s), 23 of them for x
+// 65,536 x 1,001 bf16 rows times 1,536: 90 us (2.2 PFLOP/s), 23 of them for x
 // at 6 TB/s; then y's 201 MB, LDS reads (13,100 a CU) and 25 us of matrix
 // instructions share the rest.
 // SRC: x in fp32 (0), bf16 (1), or A in 4 bits (2).  KG groups of 4 k-steps.
@@ -251,7 +251,7 @@ __device__ __forceinline__ void mfma_row(floatx16 (&c)[RT], const intx4 &w, uint
 }
 
 // Rows of y from row m0 on as a buffer that ends with the matrix: stores past
-// it are dropped.  A wave reaches 64 rows, under 2^31 bytes.
+// it are dropped.  A wave reaches RT x 32 rows, under 2^31 bytes.
 template <bool BF>
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t out_buffer(const Mx4Args &a, int64_t m0)
 {
@@ -647,11 +647,12 @@ hipError_t launch_mx4_product(const Mx4Args &in, hipStream_t s)
 {
     Mx4Args a = in;
     const int es = a.x_bf16 ? 2 : 4;
-    // a wave's 64 rows within a buffer's 32-bit offsets
-    const bool panel = a.la.groups <= 4 && a.ldy * (a.y_bf16 ? 2 : 4) < (int64_t)1 << 25;
+    // a wave's rows within 2^30 bytes: offsets from 2^31 on are outside its buffers
+    constexpr int64_t PITCH_END = ((int64_t)1 << 30) / (32 * PANEL_RT);
+    const bool panel = a.la.groups <= 4 && a.ldy * (a.y_bf16 ? 2 : 4) < PITCH_END;
     // rows of x in 16-byte pieces
     if (panel && !a.a && ((uintptr_t)a.x | (uint64_t)(a.ldx * es)) % 16 == 0 &&
-        a.ldx * es < (int64_t)1 << 25)
+        a.ldx * es < PITCH_END)
         return a.x_bf16 ? launch_panel<SRC_BF16>(a, s) : launch_panel<SRC_F32>(a, s);
     const Plan p = plan_of(a.la.rows, a.lw.rows, a.la.K);
     if (!a.a) {

@@ -13,7 +13,7 @@
 //
 // With many sequences the memory bounds it: 390 steps x 4,096 sequences x 512
 // channels in bf16 take 1.32 ms, 6.6 GB at 5.0 TB/s, and 3.8 ms with the
-// gradients (18.9 GB at 5.0: the gates are read again, and the states before
+// gradients (18.9 GB at 4.9: the gates are read again, and the states before
 // every chunk are kept instead of all of them).
 //
 // 1 - a^2 comes from a - 1 by a polynomial rather than from a: long memories

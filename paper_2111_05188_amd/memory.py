@@ -80,7 +80,8 @@ class MemoryLayer:
         """y [T][B][D] and the last states [B][D] of stored observations [T][B][ld] (ld >= S;
         rows follow one another); done [T][B] and lens [B] as tp.recur_forward.  Both are buffers
         of the layer, which its next encode of this size writes again; the last states may be
-        that call's h0."""
+        that call's h0.  gradients reads obs, done and lens again: until then they stay as they
+        are (a rollout into the same trajectory would change W's gradient)."""
         T, B, ld = obs.shape
         with torch.cuda.stream(stream):
             for t in (obs, done, lens):         # (the layer keeps them for the gradients)
@@ -97,7 +98,7 @@ class MemoryLayer:
 
     def gradients(self, dy, dh_last=None, stream=None):
         """Gradients of the last encode's W, lambda and first states, from dy [T][B][D] (buffers
-        of the layer)."""
+        of the layer), on the observations where they lie and with lam as it is."""
         n = self.rc.T * self.rc.B
         with torch.cuda.stream(stream):
             stream = self._turn()
