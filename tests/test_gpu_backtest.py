@@ -143,7 +143,7 @@ def test_workspace_of_a_call_on_another_stream():
     out, s = torch.empty_like(want), torch.cuda.Stream()
     torch.cuda.synchronize()
     with torch.cuda.stream(s):
-        torch.cuda._sleep(50_000_000)
+        torch.cuda._sleep(500_000_000)     # a fifth of a second
     tp.backtest_metrics(v0, v, 252.0, 0.02, out=out, stream=s)
     junk = [torch.full((nb,), 0xEE, dtype=torch.uint8, device="cuda") for _ in range(2)]
     torch.cuda.current_stream().synchronize()

@@ -128,7 +128,7 @@ def test_calls_on_a_stream_of_their_own(dtype):
         own = stream is not None
         if own:
             with torch.cuda.stream(stream):
-                torch.cuda._sleep(100_000_000)
+                torch.cuda._sleep(500_000_000)     # a fifth of a second
         out, kept = [], []
         for t in range(3):
             out.append(layer.step(obs[t], h, stream=stream))
@@ -165,7 +165,7 @@ def test_streams_take_turns():
     torch.cuda.synchronize()
     a, b = torch.cuda.Stream(), torch.cuda.Stream()
     with torch.cuda.stream(a):
-        torch.cuda._sleep(50_000_000)
+        torch.cuda._sleep(500_000_000)     # a fifth of a second
     layer.encode(obs[0], stream=a)
     got = layer.gradients(dy, stream=b)
     with torch.cuda.stream(b):

@@ -357,7 +357,7 @@ def test_memory_of_a_call_on_another_stream():
         y = torch.empty(M, N, device="cuda")
         torch.cuda.synchronize()
         with torch.cuda.stream(s):
-            torch.cuda._sleep(50_000_000)
+            torch.cuda._sleep(500_000_000)     # a fifth of a second
         call(y)
         assert not s.query()
         others = [torch.full((n,), 0xEE, dtype=torch.uint8, device="cuda")
