@@ -678,6 +678,185 @@ int tp_mx4_linear(const void *x, int32_t x_dtype, int64_t M, int64_t ldx, const 
                   const float *bias, int32_t act, void *y, int32_t dtype, int64_t ldy, void *work,
                   size_t work_bytes, void *stream);
 
+/*
+ * A policy of blocks with a matrix memory.  Three calls belong together: the
+ * gated delta rule (a block's memory), the norms around a block, and the policy
+ * loss that trains it on what tp_rollout and tp_gae store.
+ *
+ * Gated delta rule: head h of sequence b (an env) has a state S [dk][dv], 0 or h0
+ * at first.  Of each step's query q, key k [dk], value v [dv] and pre-activations
+ * r, b:
+ *   q^ = q / sqrt(q.q + 1e-6), k^ = k / sqrt(k.k + 1e-6),
+ *   g = -8 softplus(lambda_h) / (1 + exp(-r)),  beta = 1 / (1 + exp(-b)),
+ *   S' = exp(g) S,  u = beta (v - S'^T k^),  S = S' + k^ u^T,  y = S^T q^.
+ * Where done[t][b] is set the episode ends with step t (as for tp_gae): the state
+ * is 0 after it.  Sequence b has len[b] steps (clamped to 0..T); in the steps past
+ * them y and the gradients are 0, the state stays as it is, and what the inputs
+ * hold there does not matter.
+ * States, lambda and their gradients are fp32; q, k, v, r, b, y and their
+ * gradients are all fp32 or all bf16 (rounded once, to nearest even).  Sums are
+ * fp32; a bf16 call multiplies states and writes as two bf16 numbers each (2^-17
+ * of a value is lost).  q.q and k.k, and the states, have to be in fp32's range.
+ * A NaN or an infinity in a step reaches y and the states from that step on, to
+ * the episode's end, and the gradients that read them (r's up to 31 steps before).
+ */
+typedef struct tp_delta {
+    int32_t T;             /* steps, >= 1                                    */
+    int32_t B;             /* sequences, >= 1                                */
+    int32_t H;             /* heads, >= 1; B * H <= 2^23                     */
+    int32_t dk, dv;        /* channels of a head's keys and values, 1 .. 128 */
+    int32_t dtype;         /* of q, k, v, r, b, y and their gradients        */
+    const float *lambda;   /* [H] decay parameters                           */
+    const uint8_t *done;   /* [T][B] or NULL (no episode ends)               */
+    const int32_t *len;    /* [B] or NULL (all T steps)                      */
+} tp_delta;
+
+/* A [T][B][H][d] array (d = dk, dv, or 1 for r and b): element (t, b, h, i) at
+ * p + t*st + b*sb + h*sh + i elements, so that all of them may be parts of one
+ * product's rows.  Outputs must not overlap themselves or the inputs. */
+typedef struct tp_heads {
+    void *p;
+    int64_t st, sb, sh;
+} tp_heads;
+
+/* Bytes of the states tp_delta_forward keeps for tp_delta_backward, and of the
+ * workspace either call needs (256-byte aligned; its contents do not matter
+ * between calls).  0 for bad sizes. */
+size_t tp_delta_saved_bytes(const tp_delta *cfg);
+size_t tp_delta_workspace_bytes(const tp_delta *cfg);
+
+/*
+ * tp_delta_forward -- y and the last states of whole sequences.
+ *   h0 [B][H][dk][dv] or NULL (zeros); y may be NULL (not stored); h_last
+ *   [B][H][dk][dv] or NULL, the state after the last step (0 where done is set on
+ *   it); saved (16-byte aligned) or NULL (no gradients wanted).  h_last may be
+ *   h0's buffer; buffers that overlap otherwise are refused.
+ */
+int tp_delta_forward(const tp_delta *cfg, const tp_heads *q, const tp_heads *k,
+                     const tp_heads *v, const tp_heads *r, const tp_heads *b, const float *h0,
+                     const tp_heads *y, float *h_last, float *saved, void *work,
+                     size_t work_bytes, void *stream);
+
+/*
+ * tp_delta_backward -- gradients of everything tp_delta_forward read, from dy and
+ * dh_last ([B][H][dk][dv] or NULL, zeros).  saved: what the forward call on the
+ * same inputs kept.
+ *   dq, dk, dv, dr, db as q, k, v, r, b; dlambda [H]; dh0 [B][H][dk][dv] or NULL,
+ *   may be dh_last's buffer (as h_last h0's).
+ * Sums run in a fixed order.
+ */
+int tp_delta_backward(const tp_delta *cfg, const tp_heads *q, const tp_heads *k,
+                      const tp_heads *v, const tp_heads *r, const tp_heads *b,
+                      const float *saved, const tp_heads *dy, const float *dh_last,
+                      const tp_heads *dq, const tp_heads *dk, const tp_heads *dv,
+                      const tp_heads *dr, const tp_heads *db, float *dlambda, float *dh0,
+                      void *work, size_t work_bytes, void *stream);
+
+/*
+ * tp_delta_step -- one bar: h_out = the states after a step from h, y (or NULL)
+ * the step's outputs.  cfg->T must be 1 and cfg->len NULL; done [B] or NULL; h,
+ * h_out [B][H][dk][dv], may be one buffer but not overlap otherwise.
+ */
+int tp_delta_step(const tp_delta *cfg, const tp_heads *q, const tp_heads *k, const tp_heads *v,
+                  const tp_heads *r, const tp_heads *b, const float *h, float *h_out,
+                  const tp_heads *y, void *stream);
+
+/*
+ * Norms around a block of a residual stream.  Of each row's x (the stream), y (the
+ * block's output) and z (its gate's pre-activation):
+ *   f = y / rms(y) * w_post * z / (1 + exp(-z)),
+ *   X = x + scale * f,   n = X / rms(X) * w_pre,
+ * rms(v) = sqrt(mean v^2 + eps), y's over each of `groups` groups of neighbouring
+ * channels (heads).  y NULL: X = x; z NULL: no gate; w_post NULL: y as it is;
+ * scale NULL: 1; w_pre NULL: no n.  z, w_post and scale need y.
+ * Rows are all fp32 or all bf16; arithmetic and sums are fp32 (the weights'
+ * gradients' last sums fp64), each output is rounded once, n is taken from X
+ * before its rounding.
+ */
+typedef struct tp_norm {
+    int64_t rows;          /* >= 1, at most 2^40                             */
+    int32_t D;             /* channels, 1 .. 4096                            */
+    int32_t groups;        /* of y's norm; divides D                         */
+    int32_t dtype;         /* of the rows                                    */
+    float eps;             /* > 0                                            */
+    const float *w_post, *scale, *w_pre;    /* [D] each, or NULL             */
+} tp_norm;
+
+/* Rows [rows][D]: element (m, d) at p + m*ld + d elements, ld >= D.  NULL, or p =
+ * NULL: not there. */
+typedef struct tp_matrix {
+    void *p;
+    int64_t ld;
+} tp_matrix;
+
+/*
+ * tp_norm_forward -- x_out = X and n; one of them may be NULL.  x_out may be x
+ * (the same pointer and pitch).
+ */
+int tp_norm_forward(const tp_norm *cfg, const tp_matrix *x, const tp_matrix *y,
+                    const tp_matrix *z, const tp_matrix *x_out, const tp_matrix *n,
+                    void *stream);
+
+/* Bytes of the workspace tp_norm_backward needs (256-byte aligned); 0 for bad
+ * sizes. */
+size_t tp_norm_workspace_bytes(const tp_norm *cfg);
+
+/*
+ * tp_norm_backward -- gradients from dx_out and dn (either may be NULL, zeros; dn
+ * needs w_pre) and the forward call's inputs.  dx is needed, dy and dz where y and
+ * z are there; dw_post, dscale, dw_pre [D] or NULL.  dx may be dx_out (the same
+ * pointer and pitch).  Sums over rows run in a fixed order.
+ */
+int tp_norm_backward(const tp_norm *cfg, const tp_matrix *x, const tp_matrix *y,
+                     const tp_matrix *z, const tp_matrix *dx_out, const tp_matrix *dn,
+                     const tp_matrix *dx, const tp_matrix *dy, const tp_matrix *dz,
+                     float *dw_post, float *dscale, float *dw_pre, void *work,
+                     size_t work_bytes, void *stream);
+
+/*
+ * Clipped policy loss (PPO, Section 5.2; tp_ppo_update's L_clip and H) of a
+ * diagonal Gaussian policy whose means come from anywhere, with two clips and a
+ * KL term, over the rows (t, b) with t < len[b], N of them (len NULL: all):
+ *   logp = sum_i [-(a_i - mu_i)^2 / (2 sigma_i^2) - log_std_i] - (n/2) ln 2pi,
+ *   rho  = exp(logp - logp_old),
+ *   L = -mean min(rho A, clip(rho, 1 - clip_low, 1 + clip_high) A)
+ *       + kl_coef mean KL(ref || pi) - ent_coef H,
+ *   KL(ref || pi) = sum_i log(sigma_i / s_i) + (s_i^2 + (m_i - mu_i)^2) / (2 sigma_i^2) - 1/2,
+ * with m = mu_ref and s = exp(log_std_ref) (the policy that acted: a rollout's
+ * mu_tap).  What the other rows hold does not matter.  All up to the ratio is in
+ * 64 bits, so that no rounding moves a row over a clip.
+ */
+typedef struct tp_policy {
+    int32_t T, B;          /* rows [T][B], >= 1                              */
+    int32_t n;             /* actions, 1 .. 128                              */
+    int32_t dtype;         /* of mu and its gradient                         */
+    double clip_low, clip_high;  /* > 0, clip_low < 1                        */
+    double kl_coef;        /* >= 0; needs mu_ref and log_std_ref unless 0    */
+    double ent_coef;       /* >= 0                                           */
+    const float *log_std;  /* [n]                                            */
+    const float *log_std_ref;    /* [n], with mu_ref; or NULL                */
+    const int32_t *len;    /* [B] or NULL                                    */
+} tp_policy;
+
+/* Bytes of the workspace tp_policy_loss needs (256-byte aligned); 0 for bad
+ * sizes. */
+size_t tp_policy_workspace_bytes(const tp_policy *cfg);
+
+/*
+ * tp_policy_loss -- the loss and its gradient.
+ *   mu [T*B][ld_mu] (ld_mu >= n), action [T][B][n], logp, adv [T][B], mu_ref
+ *   [T][B][n] or NULL (no KL), fp32 but for mu;
+ *   stats [6] fp64: L, its first term, the mean KL, H, the fraction of rows with
+ *   rho outside the clips, N (0 rows: L = -ent_coef H, the means 0);
+ *   dmu [T*B][ld_dmu], 0 in the rows that no sequence has; dlog_std [n].
+ * Where rho A equals the clipped one the gradient is rho A's.  Sums run in a fixed
+ * order.
+ */
+int tp_policy_loss(const tp_policy *cfg, const void *mu, int64_t ld_mu, const float *action,
+                   const float *logp, const float *adv, const float *mu_ref, double *stats,
+                   void *dmu, int64_t ld_dmu, float *dlog_std, void *work, size_t work_bytes,
+                   void *stream);
+
 /* Message for the last non-OK return on the calling thread ("" if none). */
 const char *tp_last_error(void);
 

@@ -16,7 +16,8 @@ SOURCES = ["api.cpp", "rollout.hip", "rollout_rs.hip", "rollout_rs_i4.hip", "rol
            "rollout_four_bf16.hip", "rollout_four_bf16_n8.hip",
            "critic.hip", "metrics.hip", "evolution.hip", "learner.hip",
            "env_kernels.hip", "gae.hip", "pack.hip", "recur.hip",
-           "mx4.hip", "mx4_product.hip"]
+           "mx4.hip", "mx4_product.hip", "delta.hip", "delta_backward.hip",
+           "norm.hip", "policy.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",

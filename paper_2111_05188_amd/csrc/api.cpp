@@ -8,6 +8,7 @@
 #include <map>
 #include <mutex>
 #include <string>
+#include <utility>
 
 #include "internal.hpp"
 #include "tp.h"
@@ -316,6 +317,176 @@ int recur_args(const tp_recur *c, const tp_rows *x, const tp_rows *r, const tp_r
     if (work_bytes < need)
         return fail(TP_EINVAL, "recurrence workspace of %zu bytes, %zu needed", work_bytes, need);
     a->work = work;
+    return TP_OK;
+}
+
+// ---------------------------------------------------------------------------
+// gated delta rule
+// ---------------------------------------------------------------------------
+int check_delta(const tp_delta *c)
+{
+    if (!c) return fail(TP_EINVAL, "delta rule configuration is NULL");
+    if (c->T < 1 || c->B < 1 || c->H < 1 || c->dk < 1 || c->dv < 1)
+        return fail(TP_EINVAL, "delta rule T = %d, B = %d, H = %d, dk = %d, dv = %d must be >= 1", c->T, c->B,
+                    c->H, c->dk, c->dv);
+    if (c->dtype != TP_F32 && c->dtype != TP_BF16) return fail(TP_EINVAL, "delta rule dtype %d", c->dtype);
+    if (c->dk > DELTA_MAX_D || c->dv > DELTA_MAX_D)
+        return fail(TP_EUNSUPPORTED, "delta rule heads of %d and %d channels, at most %d", c->dk, c->dv,
+                    DELTA_MAX_D);
+    if (!delta_fits(c->T, c->B, c->H))
+        return fail(TP_EUNSUPPORTED, "delta rule of T = %d, B = %d, H = %d exceeds the launch grid", c->T, c->B,
+                    c->H);
+    return TP_OK;
+}
+
+// One [T][B][H][d] array of the delta rule: strides to bytes.  An output: every
+// element at an address of its own (the axes nest by their strides).
+int check_heads(const tp_delta *c, const tp_heads *m, int d, const char *name, bool needed, bool output,
+                DeltaRows *out)
+{
+    *out = DeltaRows{};
+    if (!m || !m->p) return needed ? fail(TP_EINVAL, "delta rule array %s is NULL", name) : TP_OK;
+    const int es = c->dtype == TP_BF16 ? 2 : 4;
+    if (!aligned(m->p, es)) return fail(TP_EINVAL, "delta rule array %s is misaligned", name);
+    const int64_t lim = (int64_t)1 << 40;
+    struct Axis {
+        int64_t n, stride;
+    } ax[3] = {{c->T, m->st}, {c->B, m->sb}, {c->H, m->sh}};
+    for (Axis &x : ax) {
+        if (x.n == 1) x.stride = 0;             // never followed
+        if (x.stride < 0 || x.stride > lim)
+            return fail(TP_EINVAL, "delta rule array %s: strides %lld, %lld, %lld", name, (long long)m->st,
+                        (long long)m->sb, (long long)m->sh);
+    }
+    out->p = m->p;
+    out->st = ax[0].stride * es;
+    out->sb = ax[1].stride * es;
+    out->sh = ax[2].stride * es;
+    out->vec = d * es % 16 == 0 && ((uintptr_t)m->p | out->st | out->sb | out->sh) % 16 == 0;
+    if (!output) return TP_OK;
+    for (int i = 0; i < 2; ++i)
+        for (int j = 0; j < 2; ++j)
+            if (ax[j].stride > ax[j + 1].stride) std::swap(ax[j], ax[j + 1]);
+    int64_t inner = d;
+    for (const Axis &x : ax) {
+        if (x.n == 1) continue;
+        if (x.stride < inner)
+            return fail(TP_EINVAL, "delta rule output %s: strides %lld, %lld, %lld let rows overlap", name,
+                        (long long)m->st, (long long)m->sb, (long long)m->sh);
+        inner += (x.n - 1) * x.stride;
+    }
+    return TP_OK;
+}
+
+int check_head_states(const tp_delta *c, const float *in, const float *out, const char *names)
+{
+    const uintptr_t a = (uintptr_t)in, b = (uintptr_t)out;
+    if (!aligned(in, 4) || !aligned(out, 4)) return fail(TP_EINVAL, "delta rule states are misaligned");
+    const size_t bytes = (size_t)c->B * c->H * c->dk * c->dv * sizeof(float);
+    if (!a || !b || a == b || (a > b ? a - b : b - a) >= bytes) return TP_OK;
+    return fail(TP_EINVAL, "delta rule states %s overlap without being one buffer", names);
+}
+
+// what all calls share
+int delta_args(const tp_delta *c, const tp_heads *q, const tp_heads *k, const tp_heads *v, const tp_heads *r,
+               const tp_heads *b, DeltaArgs *a)
+{
+    int rc = check_delta(c);
+    if (rc != TP_OK) return rc;
+    if (!c->lambda || !aligned(c->lambda, 4)) return fail(TP_EINVAL, "delta rule lambda is NULL or misaligned");
+    if (c->len && !aligned(c->len, 4)) return fail(TP_EINVAL, "delta rule len is misaligned");
+    a->T = c->T;
+    a->B = c->B;
+    a->H = c->H;
+    a->dk = c->dk;
+    a->dv = c->dv;
+    a->bf16 = c->dtype == TP_BF16;
+    a->lam = c->lambda;
+    a->done = c->done;
+    a->len = c->len;
+    if ((rc = check_heads(c, q, c->dk, "q", true, false, &a->q)) != TP_OK) return rc;
+    if ((rc = check_heads(c, k, c->dk, "k", true, false, &a->k)) != TP_OK) return rc;
+    if ((rc = check_heads(c, v, c->dv, "v", true, false, &a->v)) != TP_OK) return rc;
+    if ((rc = check_heads(c, r, 1, "r", true, false, &a->r)) != TP_OK) return rc;
+    return check_heads(c, b, 1, "b", true, false, &a->b);
+}
+
+int delta_work(const tp_delta *c, void *work, size_t work_bytes, DeltaArgs *a)
+{
+    if (!work || !aligned(work, 256))
+        return fail(TP_EINVAL, "delta rule workspace is NULL or not 256-byte aligned");
+    const size_t need = delta_workspace_bytes(c->T, c->B, c->H, c->dk, c->dv);
+    if (work_bytes < need)
+        return fail(TP_EINVAL, "delta rule workspace of %zu bytes, %zu needed", work_bytes, need);
+    a->work = work;
+    return TP_OK;
+}
+
+// ---------------------------------------------------------------------------
+// norms around a block, policy loss
+// ---------------------------------------------------------------------------
+int check_norm(const tp_norm *c)
+{
+    if (!c) return fail(TP_EINVAL, "norm configuration is NULL");
+    if (c->rows < 1 || c->rows > (int64_t)1 << 40 || c->D < 1)
+        return fail(TP_EINVAL, "norm of %lld rows of %d channels", (long long)c->rows, c->D);
+    if (c->D > NORM_MAX_D) return fail(TP_EUNSUPPORTED, "norm of %d channels, at most %d", c->D, NORM_MAX_D);
+    if (c->groups < 1 || c->D % c->groups)
+        return fail(TP_EINVAL, "norm: %d groups of %d channels", c->groups, c->D);
+    if (c->dtype != TP_F32 && c->dtype != TP_BF16) return fail(TP_EINVAL, "norm dtype %d", c->dtype);
+    if (!(c->eps > 0.0f)) return fail(TP_EINVAL, "norm eps = %g must be > 0", c->eps);
+    if (!aligned(c->w_post, 4) || !aligned(c->scale, 4) || !aligned(c->w_pre, 4))
+        return fail(TP_EINVAL, "norm weights are misaligned");
+    return TP_OK;
+}
+
+int check_norm_rows(const tp_norm *c, const tp_matrix *m, const char *name, bool needed, NormRows *out)
+{
+    *out = NormRows{};
+    if (!m || !m->p) return needed ? fail(TP_EINVAL, "norm rows %s are NULL", name) : TP_OK;
+    const int es = c->dtype == TP_BF16 ? 2 : 4;
+    if (!aligned(m->p, es)) return fail(TP_EINVAL, "norm rows %s are misaligned", name);
+    out->p = m->p;
+    if (c->rows == 1) return TP_OK;             // (the pitch is never followed)
+    if (m->ld < c->D || m->ld > (int64_t)1 << 40)
+        return fail(TP_EINVAL, "norm rows %s: ld = %lld", name, (long long)m->ld);
+    out->ld = m->ld * es;
+    return TP_OK;
+}
+
+// what both calls share
+int norm_args(const tp_norm *c, const tp_matrix *x, const tp_matrix *y, const tp_matrix *z, NormArgs *a)
+{
+    int rc = check_norm(c);
+    if (rc != TP_OK) return rc;
+    a->rows = c->rows;
+    a->D = c->D;
+    a->groups = c->groups;
+    a->bf16 = c->dtype == TP_BF16;
+    a->eps = c->eps;
+    a->w_post = c->w_post;
+    a->scale = c->scale;
+    a->w_pre = c->w_pre;
+    if ((rc = check_norm_rows(c, x, "x", true, &a->x)) != TP_OK) return rc;
+    if ((rc = check_norm_rows(c, y, "y", false, &a->y)) != TP_OK) return rc;
+    if ((rc = check_norm_rows(c, z, "z", false, &a->z)) != TP_OK) return rc;
+    if (!a->y.p && (a->z.p || c->w_post || c->scale))
+        return fail(TP_EINVAL, "norm: z, w_post and scale need y");
+    return TP_OK;
+}
+
+int check_policy(const tp_policy *c)
+{
+    if (!c) return fail(TP_EINVAL, "policy loss configuration is NULL");
+    if (c->T < 1 || c->B < 1 || c->n < 1)
+        return fail(TP_EINVAL, "policy loss T = %d, B = %d, n = %d must be >= 1", c->T, c->B, c->n);
+    if (c->n > POLICY_MAX_N)
+        return fail(TP_EUNSUPPORTED, "policy loss of %d actions, at most %d", c->n, POLICY_MAX_N);
+    if (c->dtype != TP_F32 && c->dtype != TP_BF16) return fail(TP_EINVAL, "policy loss dtype %d", c->dtype);
+    if (!(c->clip_low > 0.0 && c->clip_low < 1.0 && c->clip_high > 0.0 && std::isfinite(c->clip_high)))
+        return fail(TP_EINVAL, "policy loss clips %g, %g", c->clip_low, c->clip_high);
+    if (!(c->kl_coef >= 0.0 && std::isfinite(c->kl_coef) && c->ent_coef >= 0.0 && std::isfinite(c->ent_coef)))
+        return fail(TP_EINVAL, "policy loss coefficients %g, %g", c->kl_coef, c->ent_coef);
     return TP_OK;
 }
 
@@ -1071,6 +1242,209 @@ int tp_recur_step(const tp_recur *cfg, const tp_rows *x, const tp_rows *r, const
     a.h_last = h_out;
     hipError_t e = launch_recur_step(a, (hipStream_t)stream);
     if (e != hipSuccess) return hip_fail(e, "recurrence step launch");
+    return ok();
+}
+
+size_t tp_delta_saved_bytes(const tp_delta *cfg)
+{
+    if (check_delta(cfg) != TP_OK) return 0;
+    ok();
+    return delta_saved_bytes(cfg->T, cfg->B, cfg->H, cfg->dk, cfg->dv);
+}
+
+size_t tp_delta_workspace_bytes(const tp_delta *cfg)
+{
+    if (check_delta(cfg) != TP_OK) return 0;
+    ok();
+    return delta_workspace_bytes(cfg->T, cfg->B, cfg->H, cfg->dk, cfg->dv);
+}
+
+int tp_delta_forward(const tp_delta *cfg, const tp_heads *q, const tp_heads *k, const tp_heads *v,
+                     const tp_heads *r, const tp_heads *b, const float *h0, const tp_heads *y, float *h_last,
+                     float *saved, void *work, size_t work_bytes, void *stream)
+{
+    DeltaArgs a{};
+    int rc = delta_args(cfg, q, k, v, r, b, &a);
+    if (rc != TP_OK) return rc;
+    if ((rc = check_heads(cfg, y, cfg->dv, "y", false, true, &a.y)) != TP_OK) return rc;
+    if ((rc = delta_work(cfg, work, work_bytes, &a)) != TP_OK) return rc;
+    if (!a.y.p && !h_last && !saved)
+        return fail(TP_EINVAL, "delta rule has no output: y, h_last and saved are NULL");
+    if ((rc = check_head_states(cfg, h0, h_last, "h0 and h_last")) != TP_OK) return rc;
+    if (!aligned(saved, 16)) return fail(TP_EINVAL, "delta rule saved is not 16-byte aligned");
+    a.h0 = h0;
+    a.h_last = h_last;
+    a.saved = saved;
+    hipError_t e = launch_delta_forward(a, (hipStream_t)stream);
+    if (e != hipSuccess) return hip_fail(e, "delta rule launch");
+    return ok();
+}
+
+int tp_delta_backward(const tp_delta *cfg, const tp_heads *q, const tp_heads *k, const tp_heads *v,
+                      const tp_heads *r, const tp_heads *b, const float *saved, const tp_heads *dy,
+                      const float *dh_last, const tp_heads *dq, const tp_heads *dk, const tp_heads *dv,
+                      const tp_heads *dr, const tp_heads *db, float *dlambda, float *dh0, void *work,
+                      size_t work_bytes, void *stream)
+{
+    DeltaArgs a{};
+    int rc = delta_args(cfg, q, k, v, r, b, &a);
+    if (rc != TP_OK) return rc;
+    if ((rc = check_heads(cfg, dy, cfg->dv, "dy", true, false, &a.dy)) != TP_OK) return rc;
+    if ((rc = check_heads(cfg, dq, cfg->dk, "dq", true, true, &a.dq)) != TP_OK) return rc;
+    if ((rc = check_heads(cfg, dk, cfg->dk, "dk", true, true, &a.dkey)) != TP_OK) return rc;
+    if ((rc = check_heads(cfg, dv, cfg->dv, "dv", true, true, &a.dval)) != TP_OK) return rc;
+    if ((rc = check_heads(cfg, dr, 1, "dr", true, true, &a.dr)) != TP_OK) return rc;
+    if ((rc = check_heads(cfg, db, 1, "db", true, true, &a.db)) != TP_OK) return rc;
+    if ((rc = delta_work(cfg, work, work_bytes, &a)) != TP_OK) return rc;
+    if (!saved || !dlambda) return fail(TP_EINVAL, "delta rule saved or dlambda is NULL");
+    if (!aligned(saved, 16) || !aligned(dlambda, 4))
+        return fail(TP_EINVAL, "delta rule saved or dlambda is misaligned");
+    if ((rc = check_head_states(cfg, dh_last, dh0, "dh_last and dh0")) != TP_OK) return rc;
+    a.saved = const_cast<float *>(saved);
+    a.dh_last = dh_last;
+    a.dlam = dlambda;
+    a.dh0 = dh0;
+    hipError_t e = launch_delta_backward(a, (hipStream_t)stream);
+    if (e != hipSuccess) return hip_fail(e, "delta rule gradient launch");
+    return ok();
+}
+
+int tp_delta_step(const tp_delta *cfg, const tp_heads *q, const tp_heads *k, const tp_heads *v,
+                  const tp_heads *r, const tp_heads *b, const float *h, float *h_out, const tp_heads *y,
+                  void *stream)
+{
+    DeltaArgs a{};
+    int rc = delta_args(cfg, q, k, v, r, b, &a);
+    if (rc != TP_OK) return rc;
+    if (cfg->T != 1 || cfg->len)
+        return fail(TP_EINVAL, "delta rule step: T = %d must be 1 and len NULL", cfg->T);
+    if ((rc = check_heads(cfg, y, cfg->dv, "y", false, true, &a.y)) != TP_OK) return rc;
+    if (!h || !h_out) return fail(TP_EINVAL, "delta rule state is NULL");
+    if ((rc = check_head_states(cfg, h, h_out, "h and h_out")) != TP_OK) return rc;
+    a.h0 = h;
+    a.h_last = h_out;
+    hipError_t e = launch_delta_step(a, (hipStream_t)stream);
+    if (e != hipSuccess) return hip_fail(e, "delta rule step launch");
+    return ok();
+}
+
+int tp_norm_forward(const tp_norm *cfg, const tp_matrix *x, const tp_matrix *y, const tp_matrix *z,
+                    const tp_matrix *x_out, const tp_matrix *n, void *stream)
+{
+    NormArgs a{};
+    int rc = norm_args(cfg, x, y, z, &a);
+    if (rc != TP_OK) return rc;
+    if ((rc = check_norm_rows(cfg, x_out, "x_out", false, &a.x_out)) != TP_OK) return rc;
+    if ((rc = check_norm_rows(cfg, n, "n", false, &a.n)) != TP_OK) return rc;
+    if (!a.x_out.p && !a.n.p) return fail(TP_EINVAL, "norm has no output: x_out and n are NULL");
+    if (a.n.p && !cfg->w_pre) return fail(TP_EINVAL, "norm: n needs w_pre");
+    if (a.x_out.p == a.x.p && a.x_out.ld != a.x.ld)
+        return fail(TP_EINVAL, "norm: x_out is x with another pitch");
+    hipError_t e = launch_norm(a, false, (hipStream_t)stream);
+    if (e != hipSuccess) return hip_fail(e, "norm launch");
+    return ok();
+}
+
+size_t tp_norm_workspace_bytes(const tp_norm *cfg)
+{
+    if (check_norm(cfg) != TP_OK) return 0;
+    ok();
+    return norm_workspace_bytes(cfg->D);
+}
+
+int tp_norm_backward(const tp_norm *cfg, const tp_matrix *x, const tp_matrix *y, const tp_matrix *z,
+                     const tp_matrix *dx_out, const tp_matrix *dn, const tp_matrix *dx, const tp_matrix *dy,
+                     const tp_matrix *dz, float *dw_post, float *dscale, float *dw_pre, void *work,
+                     size_t work_bytes, void *stream)
+{
+    NormArgs a{};
+    int rc = norm_args(cfg, x, y, z, &a);
+    if (rc != TP_OK) return rc;
+    if ((rc = check_norm_rows(cfg, dx_out, "dx_out", false, &a.dx_out)) != TP_OK) return rc;
+    if ((rc = check_norm_rows(cfg, dn, "dn", false, &a.dn)) != TP_OK) return rc;
+    if ((rc = check_norm_rows(cfg, dx, "dx", true, &a.dx)) != TP_OK) return rc;
+    if ((rc = check_norm_rows(cfg, dy, "dy", a.y.p != nullptr, &a.dy)) != TP_OK) return rc;
+    if ((rc = check_norm_rows(cfg, dz, "dz", a.z.p != nullptr, &a.dz)) != TP_OK) return rc;
+    if ((a.dy.p && !a.y.p) || (a.dz.p && !a.z.p))
+        return fail(TP_EINVAL, "norm: dy and dz need y and z");
+    if (a.dn.p && !cfg->w_pre) return fail(TP_EINVAL, "norm: dn needs w_pre");
+    if ((dw_post && !cfg->w_post) || (dscale && !cfg->scale) || (dw_pre && !cfg->w_pre))
+        return fail(TP_EINVAL, "norm: a gradient of weights that are not there");
+    if (!aligned(dw_post, 4) || !aligned(dscale, 4) || !aligned(dw_pre, 4))
+        return fail(TP_EINVAL, "norm weights' gradients are misaligned");
+    if (a.dx_out.p == a.dx.p && a.dx_out.ld != a.dx.ld)
+        return fail(TP_EINVAL, "norm: dx is dx_out with another pitch");
+    if (!work || !aligned(work, 256))
+        return fail(TP_EINVAL, "norm workspace is NULL or not 256-byte aligned");
+    const size_t need = norm_workspace_bytes(cfg->D);
+    if (work_bytes < need) return fail(TP_EINVAL, "norm workspace of %zu bytes, %zu needed", work_bytes, need);
+    a.dw_post = dw_post;
+    a.dscale = dscale;
+    a.dw_pre = dw_pre;
+    a.parts = (float *)work;
+    hipError_t e = launch_norm(a, true, (hipStream_t)stream);
+    if (e != hipSuccess) return hip_fail(e, "norm gradient launch");
+    return ok();
+}
+
+size_t tp_policy_workspace_bytes(const tp_policy *cfg)
+{
+    if (check_policy(cfg) != TP_OK) return 0;
+    ok();
+    return policy_workspace_bytes(cfg->n);
+}
+
+int tp_policy_loss(const tp_policy *cfg, const void *mu, int64_t ld_mu, const float *action, const float *logp,
+                   const float *adv, const float *mu_ref, double *stats, void *dmu, int64_t ld_dmu,
+                   float *dlog_std, void *work, size_t work_bytes, void *stream)
+{
+    int rc = check_policy(cfg);
+    if (rc != TP_OK) return rc;
+    const int es = cfg->dtype == TP_BF16 ? 2 : 4;
+    if (!mu || !action || !logp || !adv || !cfg->log_std)
+        return fail(TP_EINVAL, "a policy loss input is NULL");
+    if (!stats || !dmu || !dlog_std) return fail(TP_EINVAL, "a policy loss output is NULL");
+    if (!aligned(mu, es) || !aligned(dmu, es) || !aligned(action, 4) || !aligned(logp, 4) || !aligned(adv, 4) ||
+        !aligned(mu_ref, 4) || !aligned(stats, 8) || !aligned(dlog_std, 4) || !aligned(cfg->log_std, 4) ||
+        !aligned(cfg->log_std_ref, 4) || !aligned(cfg->len, 4))
+        return fail(TP_EINVAL, "policy loss arrays are misaligned");
+    if (!mu_ref != !cfg->log_std_ref)
+        return fail(TP_EINVAL, "policy loss: mu_ref and log_std_ref come together");
+    if (cfg->kl_coef > 0.0 && !mu_ref) return fail(TP_EINVAL, "policy loss: kl_coef needs mu_ref");
+    const int64_t rows = (int64_t)cfg->T * cfg->B, lim = (int64_t)1 << 40;
+    if (rows == 1) ld_mu = ld_dmu = (cfg->n + 7) / 8 * 8;      // never followed
+    if (ld_mu < cfg->n || ld_mu > lim || ld_dmu < cfg->n || ld_dmu > lim)
+        return fail(TP_EINVAL, "policy loss: ld_mu = %lld, ld_dmu = %lld", (long long)ld_mu, (long long)ld_dmu);
+    if (!work || !aligned(work, 256))
+        return fail(TP_EINVAL, "policy loss workspace is NULL or not 256-byte aligned");
+    const size_t need = policy_workspace_bytes(cfg->n);
+    if (work_bytes < need)
+        return fail(TP_EINVAL, "policy loss workspace of %zu bytes, %zu needed", work_bytes, need);
+    PolicyArgs a{};
+    a.T = cfg->T;
+    a.B = cfg->B;
+    a.n = cfg->n;
+    a.bf16 = cfg->dtype == TP_BF16;
+    a.clip_low = cfg->clip_low;
+    a.clip_high = cfg->clip_high;
+    a.kl_coef = cfg->kl_coef;
+    a.ent_coef = cfg->ent_coef;
+    a.log_std = cfg->log_std;
+    a.log_std_ref = cfg->log_std_ref;
+    a.len = cfg->len;
+    a.mu = mu;
+    a.ld_mu = ld_mu;
+    a.action = action;
+    a.logp = logp;
+    a.adv = adv;
+    a.mu_ref = mu_ref;
+    a.stats = stats;
+    a.dmu = dmu;
+    a.ld_dmu = ld_dmu;
+    a.dlog_std = dlog_std;
+    a.work = work;
+    hipError_t e = launch_policy_loss(a, (hipStream_t)stream);
+    if (e != hipSuccess) return hip_fail(e, "policy loss launch");
     return ok();
 }
 

@@ -1,0 +1,402 @@
+// Gated delta rule over bars, shared device code.  A head's state S [dk][dv],
+// queries and keys of unit length (q^ = q rq, k^ = k rk, r = 1/sqrt(x.x + eps)),
+// a decay e^g, a write strength beta:
+//   S' = e^g S,  u = beta (v - S'^T k^),  S <- S' + k^ u^T,  y = S^T q^.
+//
+// Up to 16 steps, a piece, go through the matrix units at once.  With the decays
+// gamma_c from before the piece to step c, G[c][j] = gamma_c / gamma_j and S0
+// the state before it:
+//   L[c][j] = beta_c G[c][j] k^_c.k^_j  (j < c),     T = (I + L)^-1,
+//   R = beta (V - gamma K^ S0),  U = T R,
+//   Y = gamma Q^ S0 + P U,       P[c][j] = G[c][j] q^_c.k^_j  (j <= c),
+//   S1 = gamma_C S0 + sum_c (gamma_C / gamma_c) k^_c u_c^T.
+// A piece ends with an episode, so that neither its decays nor a NaN reach over
+// an episode's end; steps with a NaN or an infinity near them are pieces of one
+// step, so that nothing reaches the steps before.
+//
+// Products run on 16 x 16 tiles.  Lane l = 16 g + n of a wave holds rows 4g..4g+3
+// of column n of a result, and that is also what the second operand of a product
+// over those rows wants, so states and writes never leave the registers; the same
+// registers taken as the first operand stand for the transposed tile.  In bf16 an
+// operand that is not an input is three bf16 numbers that add up to it: states and
+// writes go through many products one after the other, and keep fp32's precision
+// so (with two numbers states were off by 4e-6, lambda's gradient by 3e-5).  A
+// product over 16 fills half of the instruction's 32; the other half takes another
+// of the numbers.
+#pragma once
+
+#include "device.hpp"
+#include "internal.hpp"
+
+namespace tpk {
+namespace {
+
+constexpr float DELTA_LOG2E = 1.44269504088896341f;
+
+// ---------------------------------------------------------------------------
+// operands of a product over 16: Raw an input's own values, Val any fp32 values
+// ---------------------------------------------------------------------------
+template <bool BF> struct Tile;
+
+template <> struct Tile<false> {
+    typedef float elem;
+    typedef floatx4 raw;
+    typedef floatx4 val;
+    static constexpr int PAD = 4;               // elements after a row in LDS
+    static __device__ __forceinline__ val split(floatx4 x) { return x; }
+    static __device__ __forceinline__ floatx4 wide(raw x) { return x; }
+    static __device__ __forceinline__ floatx4 mm(floatx4 a, floatx4 b, floatx4 c)
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[i], b[i], c, 0, 0, 0);
+        return c;
+    }
+    static __device__ __forceinline__ floatx4 mm2(val a0, val a1, val b0, val b1, floatx4 c)
+    {
+        return mm(a1, b1, mm(a0, b0, c));
+    }
+};
+
+template <> struct Tile<true> {
+    typedef __bf16 elem;
+    typedef bf16x4 raw;
+    struct val {
+        bf16x4 hi, mid, lo;
+    };
+    static constexpr int PAD = 8;
+    // the upper 8 bits of a significand, the next 8 and the last: nothing is lost
+    static __device__ __forceinline__ val split(floatx4 x)
+    {
+        val v;
+        uint32_t h[4], m[4], l[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            h[i] = __float_as_uint(x[i]);
+            const float r = x[i] - __uint_as_float(h[i] & 0xFFFF0000u);
+            m[i] = __float_as_uint(r);
+            l[i] = __float_as_uint(r - __uint_as_float(m[i] & 0xFFFF0000u));
+        }
+        v.hi = upper(h);
+        v.mid = upper(m);
+        v.lo = upper(l);
+        return v;
+    }
+    static __device__ __forceinline__ bf16x4 upper(const uint32_t *w)
+    {
+        const uint32_t p[2] = {__builtin_amdgcn_perm(w[1], w[0], 0x07060302u),
+                               __builtin_amdgcn_perm(w[3], w[2], 0x07060302u)};
+        bf16x4 v;
+        __builtin_memcpy(&v, p, sizeof v);
+        return v;
+    }
+    static __device__ __forceinline__ floatx4 wide(raw x) { return __builtin_convertvector(x, floatx4); }
+    static __device__ __forceinline__ bf16x8 join(bf16x4 a, bf16x4 b)
+    {
+        return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+    }
+    static __device__ __forceinline__ floatx4 go(bf16x8 a, bf16x8 b, floatx4 c)
+    {
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+    }
+    // (the least products first)
+    static __device__ __forceinline__ floatx4 mm(raw a, val b, floatx4 c)
+    {
+        const bf16x4 z = {};
+        c = go(join(a, z), join(b.lo, z), c);
+        return go(join(a, a), join(b.mid, b.hi), c);
+    }
+    static __device__ __forceinline__ floatx4 mm(val a, raw b, floatx4 c)
+    {
+        const bf16x4 z = {};
+        c = go(join(a.lo, z), join(b, z), c);
+        return go(join(a.mid, a.hi), join(b, b), c);
+    }
+    static __device__ __forceinline__ floatx4 mm(val a, val b, floatx4 c)
+    {
+        c = go(join(a.hi, a.lo), join(b.lo, b.hi), c);
+        c = go(join(a.mid, a.hi), join(b.mid, b.mid), c);
+        return go(join(a.mid, a.hi), join(b.hi, b.hi), c);
+    }
+    // products over 32
+    static __device__ __forceinline__ floatx4 mm2(raw a0, raw a1, val b0, val b1, floatx4 c)
+    {
+        c = go(join(a0, a1), join(b0.lo, b1.lo), c);
+        c = go(join(a0, a1), join(b0.mid, b1.mid), c);
+        return go(join(a0, a1), join(b0.hi, b1.hi), c);
+    }
+    static __device__ __forceinline__ floatx4 mm2(val a0, val a1, raw b0, raw b1, floatx4 c)
+    {
+        c = go(join(a0.lo, a1.lo), join(b0, b1), c);
+        c = go(join(a0.mid, a1.mid), join(b0, b1), c);
+        return go(join(a0.hi, a1.hi), join(b0, b1), c);
+    }
+    static __device__ __forceinline__ floatx4 mm2(raw a0, raw a1, raw b0, raw b1, floatx4 c)
+    {
+        return go(join(a0, a1), join(b0, b1), c);
+    }
+    static __device__ __forceinline__ floatx4 mm2(val a0, val a1, val b0, val b1, floatx4 c)
+    {
+        return mm(a1, b1, mm(a0, b0, c));
+    }
+};
+
+// ---------------------------------------------------------------------------
+// rows of inputs in LDS: [G rows][D + PAD], 16-byte parts moved by the threads
+// ---------------------------------------------------------------------------
+typedef uint32_t Part __attribute__((ext_vector_type(4)));
+
+template <bool BF, int D, int G>
+struct Rows {
+    typedef typename Tile<BF>::elem E;
+    static constexpr int NT = 4 * D;                        // threads: a wave for 16 columns
+    static constexpr int NW = D / 16;
+    static constexpr int LD = D + Tile<BF>::PAD;
+    static constexpr int PER = 16 / (int)sizeof(E);         // elements of a part
+    static constexpr int PARTS = D / PER;                   // of a row
+    static constexpr int N = G * PARTS / NT;                // parts of a thread
+    static_assert(G * PARTS % NT == 0 && N >= 1, "threads share the rows evenly");
+
+    // part i of this thread: its row and first column
+    static __device__ __forceinline__ int row(int i) { return ((int)threadIdx.x + i * NT) / PARTS; }
+    static __device__ __forceinline__ int col(int i) { return ((int)threadIdx.x + i * NT) % PARTS * PER; }
+
+    // rows t0.. of an array into registers; zeros past `count` rows and d columns
+    static __device__ __forceinline__ void fetch(const DeltaRows &m, const char *base, int64_t t0, int count,
+                                                 int d, Part *reg)
+    {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            Part p = {};
+            const int r = row(i), c = col(i);
+            if (r < count && c < d) {
+                const char *at = base + (t0 + r) * m.st + c * (int64_t)sizeof(E);
+                if (m.vec) {
+                    p = *(const Part *)at;
+                } else {
+                    E e[PER];
+#pragma unroll
+                    for (int j = 0; j < PER; ++j) e[j] = c + j < d ? ((const E *)at)[j] : (E)0.0f;
+                    __builtin_memcpy(&p, e, sizeof p);
+                }
+            }
+            reg[i] = p;
+        }
+    }
+
+    static __device__ __forceinline__ void put(E *lds, const Part *reg)
+    {
+#pragma unroll
+        for (int i = 0; i < N; ++i) *(Part *)(lds + row(i) * LD + col(i)) = reg[i];
+    }
+
+    // the rows' values as they lie in LDS, zeros from row `count` to row `all`
+    static __device__ __forceinline__ void store(const DeltaRows &m, char *base, int64_t t0, int count, int all,
+                                                 int d, const E *lds)
+    {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int r = row(i), c = col(i);
+            if (r >= all || c >= d) continue;
+            Part p = {};
+            if (r < count) p = *(const Part *)(lds + r * LD + c);
+            char *at = base + (t0 + r) * m.st + c * (int64_t)sizeof(E);
+            if (m.vec) {
+                *(Part *)at = p;
+            } else {
+                E e[PER];
+                __builtin_memcpy(e, &p, sizeof p);
+#pragma unroll
+                for (int j = 0; j < PER; ++j)
+                    if (c + j < d) ((E *)at)[j] = e[j];
+            }
+        }
+    }
+
+    // a NaN or an infinity among this thread's parts
+    static __device__ __forceinline__ bool odd(const Part *reg)
+    {
+        uint32_t bad = 0;
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if constexpr (BF) bad |= ((reg[i][j] & 0x7F807F80u) + 0x00800080u) & 0x80008000u;
+                else bad |= ((reg[i][j] & 0x7F800000u) + 0x00800000u) & 0x80000000u;
+            }
+        return bad != 0;
+    }
+};
+
+// rows s.. of a tile as the operand of a product over columns (k-tile kt)
+template <bool BF, int LD, class E>
+__device__ __forceinline__ typename Tile<BF>::raw along_row(const E *lds, int s, int kt, int lane)
+{
+    return *(const typename Tile<BF>::raw *)(lds + (s + (lane & 15)) * LD + 16 * kt + 4 * (lane >> 4));
+}
+
+// columns 16 ct.. of rows s.. as the operand of a product over the rows; rows
+// from `count` on are zero where MASK
+template <bool BF, int LD, bool MASK, class E>
+__device__ __forceinline__ typename Tile<BF>::raw along_col(const E *lds, int s, int count, int ct, int lane)
+{
+    typename Tile<BF>::raw v;
+    const int r = 4 * (lane >> 4);
+    const E *p = lds + (s + r) * LD + 16 * ct + (lane & 15);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const E e = p[i * LD];
+        v[i] = !MASK || r + i < count ? e : (E)0.0f;
+    }
+    return v;
+}
+
+// ---------------------------------------------------------------------------
+// a piece's decays and triangles (one wave)
+// ---------------------------------------------------------------------------
+
+// scalars of a piece's rows, and the decay over all of it
+struct PieceRows {
+    float fade[16];             // gamma_c
+    float rest[16];             // gamma_C / gamma_c
+    float beta[16];
+    float rq[16], rk[16];
+    float aq[16], ak[16], au[16];   // gamma rq, beta gamma rk, rest rk
+    float total;
+};
+
+struct GroupGates {             // of the steps of a group
+    float *g, *beta;
+};
+
+__device__ __forceinline__ float delta_softplus(float x)
+{
+    return (x > 0.0f ? x : 0.0f) + log1pf(expf(-fabsf(x))) + (x != x ? x : 0.0f);
+}
+
+__device__ __forceinline__ float delta_sigmoid(float x) { return 1.0f / (1.0f + expf(-x)); }
+
+__device__ __forceinline__ float delta_exp(float x) { return __builtin_amdgcn_exp2f(x * DELTA_LOG2E); }
+
+// Decays between the steps of a piece, in the layout of a result: down[i] =
+// G[4g+i][n] (rows after columns), up[i] = G[n][4g+i]; 0 elsewhere.  Sums of g
+// run in 64 bits, so that a closed gate does not blur the decays after it.
+__device__ __forceinline__ void piece_decays(const double *cum, int count, int lane, floatx4 &down, floatx4 &up)
+{
+    const int n = lane & 15, r = 4 * (lane >> 4);
+    const double cn = cum[n];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float e = (float)(cum[r + i] - cn);
+        down[i] = r + i >= n && r + i < count ? delta_exp(e) : 0.0f;
+        up[i] = r + i <= n && n < count ? delta_exp(-e) : 0.0f;
+    }
+}
+
+// Sums of the log-decays over a piece's steps, by its wave, in the wave's own LDS.
+__device__ __forceinline__ double piece_sums(const float *g, int count, int lane, double *cum)
+{
+    const int n = lane & 15;
+    double c = n < count ? (double)g[n] : 0.0;
+    c += dpp_f64<DPP_ROW_SHR + 1>(c);
+    c += dpp_f64<DPP_ROW_SHR + 2>(c);
+    c += dpp_f64<DPP_ROW_SHR + 4>(c);
+    c += dpp_f64<DPP_ROW_SHR + 8>(c);
+    if (lane < 16) cum[n] = c;
+    wave_lds_fence();
+    return c;
+}
+
+// K K^T and Q K^T tiles of a piece, the rows' lengths, and T in both layouts.
+// L is nilpotent; its inverse grows from blocks of 1, 2, 4, 8 on the diagonal:
+// T <- T - T L_off T with the part of L that joins two blocks, so no power of L
+// is formed whose entries cancel.
+template <bool BF, int D, int LD, bool BOTH, class E>
+__device__ __forceinline__ void piece_triangles(const E *q, const E *k, const float *g, const float *beta, int s,
+                                                int count, int lane, double *cum, PieceRows *rows,
+                                                floatx4 &Tt, floatx4 &Tn, floatx4 &Pt, floatx4 &Pn)
+{
+    constexpr float EPS = 1e-6f;
+    const int n = lane & 15, r = 4 * (lane >> 4);
+    floatx4 kk = {}, qq = {}, kq = {}, qk = {};
+#pragma unroll
+    for (int kt = 0; kt < D / 16; kt += 2) {
+        const auto a0 = along_row<BF, LD>(k, s, kt, lane), b0 = along_row<BF, LD>(q, s, kt, lane);
+        const auto a1 = along_row<BF, LD>(k, s, kt + 1, lane), b1 = along_row<BF, LD>(q, s, kt + 1, lane);
+        kk = Tile<BF>::mm2(a0, a1, a0, a1, kk);
+        qq = Tile<BF>::mm2(b0, b1, b0, b1, qq);
+        if constexpr (BOTH) qk = Tile<BF>::mm2(b0, b1, a0, a1, qk);
+        else kq = Tile<BF>::mm2(a0, a1, b0, b1, kq);
+    }
+    const double c = piece_sums(g + s, count, lane, cum);
+    const double all = cum[count - 1];
+    // lengths from the diagonals
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (r + i == n) {
+            rows->rk[n] = n < count ? rsqrtf(kk[i] + EPS) : 0.0f;
+            rows->rq[n] = n < count ? rsqrtf(qq[i] + EPS) : 0.0f;
+        }
+    if (lane < 16) {
+        const float fade = n < count ? delta_exp((float)c) : 0.0f;
+        const float rest = n < count ? delta_exp((float)(all - c)) : 0.0f;
+        const float be = n < count ? beta[s + n] : 0.0f;
+        rows->fade[n] = fade;
+        rows->rest[n] = rest;
+        rows->beta[n] = be;
+        if (n == 0) rows->total = delta_exp((float)all);
+    }
+    wave_lds_fence();
+    if (lane < 16) {
+        const float rk = rows->rk[n];
+        rows->aq[n] = rows->fade[n] * rows->rq[n];
+        rows->ak[n] = rows->beta[n] * rows->fade[n] * rk;
+        rows->au[n] = rows->rest[n] * rk;
+    }
+    floatx4 down, up;
+    piece_decays(cum, count, lane, down, up);
+    const float rkn = rows->rk[n], rqn = rows->rq[n], ben = rows->beta[n];
+    const floatx4 rkr = *(const floatx4 *)(rows->rk + r), rqr = *(const floatx4 *)(rows->rq + r);
+    const floatx4 ber = *(const floatx4 *)(rows->beta + r);
+    floatx4 Ln, Lt;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float x = kk[i] * rkr[i] * rkn;
+        Ln[i] = r + i > n && r + i < count ? x * ber[i] * down[i] : 0.0f;   // row r+i after column n
+        Lt[i] = r + i < n && n < count ? x * ben * up[i] : 0.0f;            // transposed
+        if constexpr (BOTH) Pn[i] = r + i >= n && r + i < count ? qk[i] * rqr[i] * rkn * down[i] : 0.0f;
+        else Pt[i] = r + i <= n && n < count ? kq[i] * rkr[i] * rqn * up[i] : 0.0f;
+        // blocks of two: I - L inside them
+        const float one = r + i == n ? 1.0f : 0.0f;
+        Tn[i] = (r + i) / 2 == n / 2 ? one - Ln[i] : 0.0f;
+        Tt[i] = (r + i) / 2 == n / 2 ? one - Lt[i] : 0.0f;
+    }
+#pragma unroll
+    for (int w = 2; w < 16; w *= 2) {
+        floatx4 off;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            off[i] = (r + i) / w != n / w && (r + i) / (2 * w) == n / (2 * w) ? -Lt[i] : 0.0f;
+        const floatx4 z = {};
+        const floatx4 Y = Tile<false>::mm(off, Tn, z);               // -L_off T
+        const floatx4 t = Tile<false>::mm(Y, Tt, Tt);                // T^T - (L_off T)^T T^T
+        if (BOTH || w < 8) Tn = Tile<false>::mm(Tt, Y, Tn);
+        Tt = t;
+    }
+}
+
+// The next piece from step s of a group of `count` steps: it ends with a whole
+// tile, an episode or the group.
+__device__ __forceinline__ int piece_end(int s, int count, uint64_t ends, bool single)
+{
+    int e = single ? s + 1 : s + 16;
+    if (e > count) e = count;
+    const uint64_t m = ends >> s;
+    if (m) {
+        const int d = s + __builtin_ctzll(m) + 1;
+        if (d < e) e = d;
+    }
+    return e;
+}
+
+}  // namespace
+}  // namespace tpk

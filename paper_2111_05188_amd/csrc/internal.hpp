@@ -228,6 +228,89 @@ bool recur_fits(int T, int B, int D);
 hipError_t launch_recur(RecurArgs &a, bool backward, hipStream_t s);
 hipError_t launch_recur_step(RecurArgs &a, hipStream_t s);
 
+// Gated delta rule: steps between the states kept for the gradients, rows of a
+// [T][B][H][d] array in bytes.
+constexpr int DELTA_GROUP = 32;
+constexpr int DELTA_MAX_D = 128;
+
+struct DeltaRows {
+    void *p;
+    int64_t st, sb, sh;        // bytes between steps, sequences and heads
+    bool vec;                  // every row starts at a multiple of 16 bytes and is whole parts
+};
+
+struct DeltaArgs {
+    int T, B, H, dk, dv;
+    bool bf16;
+    const float *lam;
+    const uint8_t *done;
+    const int32_t *len;
+    DeltaRows q, k, v, r, b, y, dy, dq, dkey, dval, dr, db;
+    const float *h0;           // the step's state in
+    float *h_last;             // the step's state out
+    float *saved;
+    const float *dh_last;
+    float *dlam, *dh0;
+    void *work;
+    double *parts;             // filled by the launcher
+};
+
+inline int delta_width(int dk, int dv)
+{
+    const int d = dk > dv ? dk : dv;
+    return d <= 32 ? 32 : d <= 64 ? 64 : 128;
+}
+size_t delta_saved_bytes(int T, int B, int H, int dk, int dv);
+size_t delta_workspace_bytes(int T, int B, int H, int dk, int dv);
+bool delta_fits(int T, int B, int H);
+hipError_t launch_delta_forward(DeltaArgs &a, hipStream_t s);
+hipError_t launch_delta_backward(DeltaArgs &a, hipStream_t s);
+hipError_t launch_delta_step(DeltaArgs &a, hipStream_t s);
+
+// Norms around a block: rows of pitch ld bytes (p NULL: not there).
+struct NormRows {
+    void *p;
+    int64_t ld;
+};
+
+struct NormArgs {
+    int64_t rows;
+    int D, groups;
+    bool bf16;
+    float eps;
+    const float *w_post, *scale, *w_pre;
+    NormRows x, y, z, x_out, n, dx_out, dn, dx, dy, dz;
+    float *dw_post, *dscale, *dw_pre;
+    float *parts;              // the workspace
+    int group, mode;           // filled by the launcher
+};
+
+constexpr int NORM_MAX_D = 4096;
+size_t norm_workspace_bytes(int D);
+hipError_t launch_norm(NormArgs &a, bool backward, hipStream_t s);
+
+// Clipped policy loss: strides in elements.
+struct PolicyArgs {
+    int T, B, n;
+    bool bf16;
+    double clip_low, clip_high, kl_coef, ent_coef;
+    const float *log_std, *log_std_ref;
+    const int32_t *len;
+    const void *mu;
+    int64_t ld_mu;
+    const float *action, *logp, *adv, *mu_ref;
+    double *stats;
+    void *dmu;
+    int64_t ld_dmu;
+    float *dlog_std;
+    void *work;
+    double *count, *parts;     // filled by the launcher
+};
+
+constexpr int POLICY_MAX_N = 128;
+size_t policy_workspace_bytes(int n);
+hipError_t launch_policy_loss(PolicyArgs &a, hipStream_t s);
+
 // 4-bit matrices (mx4.hpp has the layout).
 struct Mx4Layout {
     int64_t rows, K;

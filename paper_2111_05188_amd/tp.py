@@ -88,6 +88,33 @@ class Rows(C.Structure):
     _fields_ = [("p", C.c_void_p), ("st", C.c_int64), ("sb", C.c_int64)]
 
 
+class Delta(C.Structure):
+    _fields_ = [("T", C.c_int32), ("B", C.c_int32), ("H", C.c_int32), ("dk", C.c_int32),
+                ("dv", C.c_int32), ("dtype", C.c_int32), ("lam", C.c_void_p),
+                ("done", C.c_void_p), ("len", C.c_void_p)]
+
+
+class Heads(C.Structure):
+    _fields_ = [("p", C.c_void_p), ("st", C.c_int64), ("sb", C.c_int64), ("sh", C.c_int64)]
+
+
+class Norm(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("D", C.c_int32), ("groups", C.c_int32),
+                ("dtype", C.c_int32), ("eps", C.c_float), ("w_post", C.c_void_p),
+                ("scale", C.c_void_p), ("w_pre", C.c_void_p)]
+
+
+class Matrix(C.Structure):
+    _fields_ = [("p", C.c_void_p), ("ld", C.c_int64)]
+
+
+class Policy(C.Structure):
+    _fields_ = [("T", C.c_int32), ("B", C.c_int32), ("n", C.c_int32), ("dtype", C.c_int32),
+                ("clip_low", C.c_double), ("clip_high", C.c_double), ("kl_coef", C.c_double),
+                ("ent_coef", C.c_double), ("log_std", C.c_void_p), ("log_std_ref", C.c_void_p),
+                ("len", C.c_void_p)]
+
+
 class Mx4(C.Structure):
     _fields_ = [("data", C.c_void_p), ("rows", C.c_int64), ("K", C.c_int64)]
 
@@ -105,6 +132,9 @@ EXPORTS = ("tp_env_reset", "tp_env_step", "tp_actor_packed_bytes",
            "tp_recur_saved_bytes", "tp_recur_workspace_bytes", "tp_recur_forward",
            "tp_recur_backward", "tp_recur_step", "tp_mx4_bytes", "tp_mx4_quantize",
            "tp_mx4_dequantize", "tp_mx4_workspace_bytes", "tp_mx4_matmul", "tp_mx4_linear",
+           "tp_delta_saved_bytes", "tp_delta_workspace_bytes", "tp_delta_forward",
+           "tp_delta_backward", "tp_delta_step", "tp_norm_forward", "tp_norm_backward",
+           "tp_norm_workspace_bytes", "tp_policy_workspace_bytes", "tp_policy_loss",
            "tp_last_error", "tp_version")
 
 _lib = None
@@ -170,6 +200,16 @@ def load(path: str = LIB_PATH):
     L.tp_mx4_dequantize.argtypes = [vp, vp, i32, i64, vp]
     L.tp_mx4_matmul.argtypes = [vp, vp, vp, i32, vp, i32, i64, vp, sz, vp]
     L.tp_mx4_linear.argtypes = [vp, i32, i64, i64, vp, vp, i32, vp, i32, i64, vp, sz, vp]
+    for f in ("tp_delta_saved_bytes", "tp_delta_workspace_bytes", "tp_norm_workspace_bytes",
+              "tp_policy_workspace_bytes"):
+        getattr(L, f).restype = sz
+        getattr(L, f).argtypes = [vp]
+    L.tp_delta_forward.argtypes = [vp] * 11 + [sz, vp]
+    L.tp_delta_backward.argtypes = [vp] * 17 + [sz, vp]
+    L.tp_delta_step.argtypes = [vp] * 10
+    L.tp_norm_forward.argtypes = [vp] * 7
+    L.tp_norm_backward.argtypes = [vp] * 13 + [sz, vp]
+    L.tp_policy_loss.argtypes = [vp, vp, i64, vp, vp, vp, vp, vp, vp, i64, vp, vp, sz, vp]
     L.tp_last_error.restype = C.c_char_p
     L.tp_version.restype = C.c_int
     for f in ("tp_env_reset", "tp_env_step", "tp_actor_pack", "tp_rollout", "tp_gae",
@@ -179,7 +219,8 @@ def load(path: str = LIB_PATH):
               "tp_actor_release", "tp_critic_release", "tp_check_starts",
               "tp_backtest_metrics_noalloc", "tp_recur_forward", "tp_recur_backward",
               "tp_recur_step", "tp_mx4_quantize", "tp_mx4_dequantize", "tp_mx4_matmul",
-              "tp_mx4_linear"):
+              "tp_mx4_linear", "tp_delta_forward", "tp_delta_backward", "tp_delta_step",
+              "tp_norm_forward", "tp_norm_backward", "tp_policy_loss"):
         getattr(L, f).restype = C.c_int
     _lib = L
     return L
@@ -860,3 +901,253 @@ def mx4_linear(x: torch.Tensor, w: Mx4T, y: torch.Tensor, bias: torch.Tensor | N
                             and bias.is_contiguous())
     _check(load().tp_mx4_linear(px, dx, M, _pitch(x), C.byref(w.s), _ptr(bias), act, p, dt,
                                 _pitch(y), work.data_ptr(), work.numel(), _stream(stream)))
+
+
+# --------------------------------------------------------------------------
+# gated delta rule
+# --------------------------------------------------------------------------
+
+class DeltaT:
+    """Sequences of the gated delta rule (see tp_delta): lam [H] fp32, T steps of B sequences,
+    heads of dk key and dv value channels, done [T][B] uint8 and lens [B] int32 optional."""
+
+    def __init__(self, lam: torch.Tensor, T: int, B: int, dk: int, dv: int, dtype: torch.dtype,
+                 done: torch.Tensor | None = None, lens: torch.Tensor | None = None):
+        assert lam.dim() == 1 and lam.dtype == torch.float32 and lam.is_contiguous()
+        assert dtype in (torch.float32, torch.bfloat16)
+        assert done is None or (done.shape == (T, B) and done.element_size() == 1
+                                and done.is_contiguous())
+        assert lens is None or (lens.shape == (B,) and lens.dtype == torch.int32
+                                and lens.is_contiguous())
+        self.lam, self.done, self.lens, self.dtype = lam, done, lens, dtype
+        self.T, self.B, self.H, self.dk, self.dv = T, B, lam.shape[0], dk, dv
+        self.s = Delta(T, B, self.H, dk, dv, TP_BF16 if dtype == torch.bfloat16 else TP_F32,
+                       _ptr(lam), _ptr(done), _ptr(lens))
+        self.saved_count = _bytes(load().tp_delta_saved_bytes, self.s) // 4
+
+    def workspace(self) -> torch.Tensor:
+        return torch.empty(_bytes(load().tp_delta_workspace_bytes, self.s), dtype=torch.uint8,
+                           device=self.lam.device)
+
+    def saved(self) -> torch.Tensor:
+        """The states delta_forward keeps for delta_backward."""
+        return torch.empty(self.saved_count, dtype=torch.float32, device=self.lam.device)
+
+    def heads(self, *pairs):
+        """tp_heads of pairs (tensor, d): [T][B][H][d] tensors (any strides but the last), or
+        [T][B][H] where d is None; tensor None: not there."""
+        lead, dtype, v = (self.T, self.B, self.H), self.dtype, []
+        for t, d in pairs:
+            if t is None:
+                v += (0, 0, 0, 0)
+                continue
+            assert t.dtype is dtype
+            if d is None:
+                assert t.shape == lead
+                v += (t.data_ptr(), *t.stride())
+            else:
+                st, sb, sh, sd = t.stride()
+                assert t.shape == (*lead, d) and (sd == 1 or d == 1)
+                v += (t.data_ptr(), st, sb, sh)
+        return _heads(v)
+
+    def inputs(self, q, k, v, r, b):
+        return (q, self.dk), (k, self.dk), (v, self.dv), (r, None), (b, None)
+
+    def kept(self, t: torch.Tensor | None):
+        if t is None:
+            return None
+        assert t.numel() >= self.saved_count and t.dtype is torch.float32 and t.is_contiguous()
+        return t.data_ptr()
+
+    def state(self, t: torch.Tensor | None):
+        if t is None:
+            return None
+        assert t.shape == (self.B, self.H, self.dk, self.dv)
+        assert t.dtype is torch.float32 and t.is_contiguous()
+        return t.data_ptr()
+
+
+def _bytes(f, s) -> int:
+    nb = f(C.byref(s))
+    if nb == 0:
+        raise TPError(TP_EINVAL, last_error())
+    return nb
+
+
+def _heads(v):
+    """An array of tp_heads (pointer, three strides each) and the addresses of its elements."""
+    a = (C.c_int64 * len(v))(*v)
+    p = C.addressof(a)
+    return a, range(p, p + 8 * len(v), 32)
+
+
+def delta_forward(dc: DeltaT, q, k, v, r, b, y, work, h0=None, h_last=None, saved=None,
+                  stream=None):
+    """y [T][B][H][dv] (or None) and h_last [B][H][dk][dv] of q, k [T][B][H][dk], v
+    [T][B][H][dv], r, b [T][B][H]; saved (dc.saved()) keeps what delta_backward needs."""
+    assert work.is_contiguous()
+    keep, (pq, pk, pv, pr, pb, py) = dc.heads(*dc.inputs(q, k, v, r, b), (y, dc.dv))
+    _check(load().tp_delta_forward(C.byref(dc.s), pq, pk, pv, pr, pb, dc.state(h0), py,
+                                   dc.state(h_last), dc.kept(saved), work.data_ptr(),
+                                   work.numel(), _stream(stream)))
+
+
+def delta_backward(dc: DeltaT, q, k, v, r, b, saved, dy, dq, dk, dv, dr, db, dlam, work,
+                   dh_last=None, dh0=None, stream=None):
+    """Gradients of delta_forward's inputs into dq, dk, dv, dr, db (shaped as q, k, v, r, b),
+    dlam [H] and dh0 [B][H][dk][dv]."""
+    assert dlam.shape == (dc.H,) and dlam.dtype is torch.float32 and dlam.is_contiguous()
+    assert work.is_contiguous()
+    keep, p = dc.heads(*dc.inputs(q, k, v, r, b), (dy, dc.dv), *dc.inputs(dq, dk, dv, dr, db))
+    pq, pk, pv, pr, pb, pdy, pdq, pdk, pdv, pdr, pdb = p
+    _check(load().tp_delta_backward(C.byref(dc.s), pq, pk, pv, pr, pb, dc.kept(saved), pdy,
+                                    dc.state(dh_last), pdq, pdk, pdv, pdr, pdb, dlam.data_ptr(),
+                                    dc.state(dh0), work.data_ptr(), work.numel(),
+                                    _stream(stream)))
+
+
+def delta_step(q, k, v, r, b, lam, h, h_out, y=None, done=None, stream=None):
+    """One bar: h_out [B][H][dk][dv] fp32 (may be h) and y [B][H][dv] from q, k [B][H][dk], v
+    [B][H][dv], r, b [B][H] and the states h; done [B] uint8 clears states after the step."""
+    B, H, dk, dv = shape = h.shape
+    f32, dtype, p = torch.float32, q.dtype, []
+    assert h.dtype is f32 and h_out.dtype is f32 and lam.dtype is f32 and lam.shape == (H,)
+    assert h_out.shape == shape and h.is_contiguous() and h_out.is_contiguous()
+    assert lam.is_contiguous() and (dtype is f32 or dtype is torch.bfloat16)
+    assert done is None or (done.shape == (B,) and done.element_size() == 1
+                            and done.is_contiguous())
+    for t, d in ((q, dk), (k, dk), (v, dv), (y, dv)):
+        if t is None:
+            p += (0, 0, 0, 0)
+            continue
+        sb, sh, sd = t.stride()
+        assert t.shape == (B, H, d) and t.dtype is dtype and (sd == 1 or d == 1)
+        p += (t.data_ptr(), 0, sb, sh)
+    for t in (r, b):
+        assert t.shape == (B, H) and t.dtype is dtype
+        p += (t.data_ptr(), 0, *t.stride())
+    keep, (pq, pk, pv, py, pr, pb) = _heads(p)
+    s = Delta(1, B, H, dk, dv, TP_F32 if dtype is f32 else TP_BF16, lam.data_ptr(), _ptr(done),
+              None)
+    _check(load().tp_delta_step(C.byref(s), pq, pk, pv, pr, pb, h.data_ptr(), h_out.data_ptr(),
+                                py, _stream(stream)))
+
+
+# --------------------------------------------------------------------------
+# norms around a block
+# --------------------------------------------------------------------------
+
+class NormT:
+    """Norms around a block (see tp_norm): rows of D channels; w_pre, w_post, scale [D] fp32
+    optional; y's norm over `groups` groups of channels."""
+
+    def __init__(self, rows: int, D: int, dtype: torch.dtype, w_pre: torch.Tensor | None = None,
+                 w_post: torch.Tensor | None = None, scale: torch.Tensor | None = None,
+                 groups: int = 1, eps: float = 1e-6):
+        assert dtype in (torch.float32, torch.bfloat16)
+        self.M, self.D, self.dtype = rows, D, dtype
+        self.w_pre, self.w_post, self.scale = w_pre, w_post, scale
+        self.s = Norm(rows, D, groups, TP_BF16 if dtype == torch.bfloat16 else TP_F32, eps,
+                      self.weight(w_post), self.weight(scale), self.weight(w_pre))
+        self.work_bytes = _bytes(load().tp_norm_workspace_bytes, self.s)
+
+    def workspace(self, device="cuda") -> torch.Tensor:
+        """What norm_backward needs."""
+        return torch.empty(self.work_bytes, dtype=torch.uint8, device=device)
+
+    def weight(self, t: torch.Tensor | None):
+        if t is None:
+            return None
+        assert t.shape == (self.D,) and t.dtype is torch.float32 and t.is_contiguous()
+        return t.data_ptr()
+
+    def matrices(self, *ts):
+        """tp_matrix of [rows][D] tensors (rows of any pitch); None: not there."""
+        v, shape = [], (self.M, self.D)
+        for t in ts:
+            if t is None:
+                v += (0, 0)
+                continue
+            assert t.shape == shape and t.dtype is self.dtype and (t.stride(1) == 1 or self.D == 1)
+            v += (t.data_ptr(), t.stride(0))
+        a = (C.c_int64 * len(v))(*v)
+        p = C.addressof(a)
+        return a, range(p, p + 8 * len(v), 16)
+
+
+def norm_forward(nc: NormT, x, y, z, x_out, n, stream=None):
+    """x_out = x + scale f, f = normed y times silu(z), and n = normed x_out ([rows][D] each; y,
+    z, and one of the outputs may be None; x_out may be x)."""
+    keep, p = nc.matrices(x, y, z, x_out, n)
+    _check(load().tp_norm_forward(C.byref(nc.s), *p, _stream(stream)))
+
+
+def norm_backward(nc: NormT, x, y, z, dx_out, dn, dx, dy, dz, dw_post, dscale, dw_pre, work,
+                  stream=None):
+    """Gradients of norm_forward's inputs into dx (may be dx_out), dy, dz [rows][D] and dw_post,
+    dscale, dw_pre [D] (None where not there or not wanted)."""
+    assert work.is_contiguous()
+    keep, p = nc.matrices(x, y, z, dx_out, dn, dx, dy, dz)
+    _check(load().tp_norm_backward(C.byref(nc.s), *p, nc.weight(dw_post), nc.weight(dscale),
+                                   nc.weight(dw_pre), work.data_ptr(), work.numel(),
+                                   _stream(stream)))
+
+
+# --------------------------------------------------------------------------
+# clipped policy loss
+# --------------------------------------------------------------------------
+
+class PolicyT:
+    """The clipped policy loss with KL over rows [T][B] (see tp_policy): log_std [n] fp32, clip
+    one number or (low, high); log_std_ref [n] with mu_ref; lens [B] int32 optional."""
+
+    def __init__(self, log_std: torch.Tensor, T: int, B: int, dtype: torch.dtype, clip=0.25,
+                 kl_coef: float = 0.0, ent_coef: float = 0.02,
+                 log_std_ref: torch.Tensor | None = None, lens: torch.Tensor | None = None):
+        n, = log_std.shape
+        assert dtype in (torch.float32, torch.bfloat16)
+        for t in (log_std, log_std_ref):
+            assert t is None or (t.shape == (n,) and t.dtype == torch.float32
+                                 and t.is_contiguous())
+        assert lens is None or (lens.shape == (B,) and lens.dtype == torch.int32
+                                and lens.is_contiguous())
+        low, high = clip if isinstance(clip, tuple) else (clip, clip)
+        self.log_std, self.log_std_ref, self.lens, self.dtype = log_std, log_std_ref, lens, dtype
+        self.T, self.B, self.n = T, B, n
+        self.s = Policy(T, B, n, TP_BF16 if dtype == torch.bfloat16 else TP_F32, low, high,
+                        kl_coef, ent_coef, _ptr(log_std), _ptr(log_std_ref), _ptr(lens))
+        self.work_bytes = _bytes(load().tp_policy_workspace_bytes, self.s)
+
+    def workspace(self) -> torch.Tensor:
+        return torch.empty(self.work_bytes, dtype=torch.uint8, device=self.log_std.device)
+
+    def means(self, t: torch.Tensor) -> int:
+        """The pitch of [T][B][n] means, whose rows follow one another."""
+        T, B, n = t.shape
+        st, sb, sn = t.stride()
+        assert (T, B, n) == (self.T, self.B, self.n) and t.dtype is self.dtype
+        assert n == 1 or sn == 1
+        if B == 1:
+            return st if T > 1 else n
+        assert T == 1 or st == B * sb
+        return sb
+
+
+def policy_loss(pc: PolicyT, mu, action, logp, adv, work, stats, dmu, dlog_std, mu_ref=None,
+                stream=None):
+    """stats [6] fp64 (loss, its policy term, mean KL, entropy, clip fraction, rows), dmu [T][B][n]
+    and dlog_std [n] of means mu [T][B][n], with action, mu_ref [T][B][n], logp, adv [T][B] as
+    tp.rollout and tp.gae store them."""
+    lead, n = (pc.T, pc.B), pc.n
+    for t, shape in ((action, (*lead, n)), (logp, lead), (adv, lead), (dlog_std, (n,))):
+        assert t.shape == shape and t.dtype is torch.float32 and t.is_contiguous()
+    assert mu_ref is None or (mu_ref.shape == (*lead, n) and mu_ref.dtype is torch.float32
+                              and mu_ref.is_contiguous())
+    assert stats.shape == (6,) and stats.dtype is torch.float64 and stats.is_contiguous()
+    assert work.is_contiguous()
+    _check(load().tp_policy_loss(C.byref(pc.s), mu.data_ptr(), pc.means(mu), action.data_ptr(),
+                                 logp.data_ptr(), adv.data_ptr(), _ptr(mu_ref),
+                                 stats.data_ptr(), dmu.data_ptr(), pc.means(dmu),
+                                 dlog_std.data_ptr(), work.data_ptr(), work.numel(),
+                                 _stream(stream)))
