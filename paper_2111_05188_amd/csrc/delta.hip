@@ -11,11 +11,9 @@
 namespace tpk {
 namespace {
 
-// a sequence's gates of a group of steps
-__device__ __forceinline__ float delta_gate(const DeltaRows &m, const char *base, int64_t t, bool bf)
+__device__ __forceinline__ float delta_gate(const char *p, bool bf)
 {
-    const char *p = base + t * m.st;
-    return bf ? (float)*(const __bf16 *)p : *(const float *)p;
+    return bf ? (float)*(const TP_GLOBAL __bf16 *)p : *(const TP_GLOBAL float *)p;
 }
 
 // one piece on the state's columns of this wave
@@ -24,16 +22,17 @@ __device__ __forceinline__ void run_piece(const E *q, const E *k, E *v, int s, i
                                           const PieceRows &rows, const typename Tile<BF>::val &Tt,
                                           const typename Tile<BF>::val &Pt, int w, int lane, floatx4 *S)
 {
+    typedef Tile<BF> TL;
     constexpr int KT = D / 16;
     const int r = 4 * (lane >> 4);
     floatx4 ks = {}, qs = {};
 #pragma unroll
     for (int kt = 0; kt < KT; kt += 2) {
-        const auto x0 = Tile<BF>::split(S[kt]), x1 = Tile<BF>::split(S[kt + 1]);
-        ks = Tile<BF>::mm2(along_row<BF, LD>(k, s, kt, lane), along_row<BF, LD>(k, s, kt + 1, lane), x0, x1, ks);
-        qs = Tile<BF>::mm2(along_row<BF, LD>(q, s, kt, lane), along_row<BF, LD>(q, s, kt + 1, lane), x0, x1, qs);
+        const auto x0 = TL::split(S[kt]), x1 = TL::split(S[kt + 1]);
+        ks = TL::mm2(along_row<BF, LD>(k, s, kt, lane), along_row<BF, LD>(k, s, kt + 1, lane), x0, x1, ks);
+        qs = TL::mm2(along_row<BF, LD>(q, s, kt, lane), along_row<BF, LD>(q, s, kt + 1, lane), x0, x1, qs);
     }
-    const floatx4 vv = Tile<BF>::wide(along_col<BF, LD, MASK>(v, s, count, w, lane));
+    const floatx4 vv = TL::wide(along_col<BF, LD, MASK>(v, s, count, w, lane));
     const floatx4 be = *(const floatx4 *)(rows.beta + r), ak = *(const floatx4 *)(rows.ak + r);
     const floatx4 aq = *(const floatx4 *)(rows.aq + r), au = *(const floatx4 *)(rows.au + r);
     floatx4 R, U = {}, o;
@@ -42,8 +41,8 @@ __device__ __forceinline__ void run_piece(const E *q, const E *k, E *v, int s, i
         R[i] = !MASK || r + i < count ? be[i] * vv[i] - ak[i] * ks[i] : 0.0f;
         o[i] = aq[i] * qs[i];
     }
-    U = Tile<BF>::mm(Tt, Tile<BF>::split(R), U);
-    o = Tile<BF>::mm(Pt, Tile<BF>::split(U), o);
+    U = TL::mm(Tt, TL::split(R), U);
+    o = TL::mm(Pt, TL::split(U), o);
 #pragma unroll
     for (int i = 0; i < 4; ++i)
         if (!MASK || r + i < count) v[(s + r + i) * LD + 16 * w + (lane & 15)] = (E)o[i];
@@ -55,20 +54,20 @@ __device__ __forceinline__ void run_piece(const E *q, const E *k, E *v, int s, i
     floatx4 W;
 #pragma unroll
     for (int i = 0; i < 4; ++i) W[i] = !MASK || r + i < count ? U[i] * au[i] : 0.0f;
-    const auto x = Tile<BF>::split(W);
+    const auto x = TL::split(W);
 #pragma unroll
     for (int kt = 0; kt < KT; ++kt)
-        S[kt] = Tile<BF>::mm(along_col<BF, LD, MASK>(k, s, count, kt, lane), x, S[kt] * rows.total);
+        S[kt] = TL::mm(along_col<BF, LD, MASK>(k, s, count, kt, lane), x, S[kt] * rows.total);
 }
 
-template <bool BF, int D>
+template <bool BF, int D, int G>
 __global__ __launch_bounds__(4 * D, D == 128 ? 2 : 3) void delta_fwd_kernel(DeltaArgs a)
 {
-    constexpr int G = DELTA_GROUP, NP = G / 16, KT = D / 16;
+    constexpr int NP = G / 16, KT = D / 16;
     typedef Rows<BF, D, G> RW;
     typedef typename RW::E E;
     typedef typename Tile<BF>::val val;
-    constexpr int LD = RW::LD;
+    constexpr int LD = RW::LD, NW = RW::NW;
     __shared__ __attribute__((aligned(16))) E buf[(3 * G + 16) * LD];
     __shared__ val sT[NP][64], sP[NP][64];
     __shared__ __attribute__((aligned(16))) PieceRows rows[NP];
@@ -82,9 +81,6 @@ __global__ __launch_bounds__(4 * D, D == 128 ? 2 : 3) void delta_fwd_kernel(Delt
     int len = a.len ? a.len[b] : a.T;
     len = len < 0 ? 0 : len > a.T ? a.T : len;
     const float rate = -8.0f * delta_softplus(a.lam[h]);
-    auto base = [&](const DeltaRows &m) { return (char *)m.p + b * m.sb + h * m.sh; };
-    const char *pq = base(a.q), *pk = base(a.k), *pv = base(a.v), *pr = base(a.r), *pb = base(a.b);
-
     const int64_t st = ((int64_t)b * a.H + h) * a.dk * a.dv;
     const int col = 16 * w + n;
     floatx4 S[KT];
@@ -96,21 +92,34 @@ __global__ __launch_bounds__(4 * D, D == 128 ? 2 : 3) void delta_fwd_kernel(Delt
             S[kt][i] = a.h0 && row < a.dk && col < a.dv ? a.h0[st + (int64_t)row * a.dv + col] : 0.0f;
         }
 
+    const char *pq = RW::at(a.q, b, h, 0), *pk = RW::at(a.k, b, h, 0), *pv = RW::at(a.v, b, h, 0);
+    char *py = a.y.p ? RW::at(a.y, b, h, 0) : nullptr;
+    const char *pr = (char *)a.r.p + b * a.r.sb + h * a.r.sh + threadIdx.x * a.r.st;
+    const char *pb = (char *)a.b.p + b * a.b.sb + h * a.b.sh + threadIdx.x * a.b.st;
+    const uint8_t *pd = a.done ? a.done + (int64_t)lane * a.B + b : nullptr;
+    float *ps = a.saved ? a.saved + (int64_t)blockIdx.x * D * D + r4 * D + col : nullptr;
     Part fq[RW::N], fk[RW::N], fv[RW::N];
     float fr = 0.0f, fb = 0.0f;
     uint8_t fd = 0;
-    auto fetch = [&](int t0) {
-        const int count = len - t0 < G ? len - t0 : G;
-        RW::fetch(a.q, pq, t0, count, a.dk, fq);
-        RW::fetch(a.k, pk, t0, count, a.dk, fk);
-        RW::fetch(a.v, pv, t0, count, a.dv, fv);
+    auto fetch = [&](int count) {
+        RW::fetch(a.q, pq, count, a.dk, fq);
+        RW::fetch(a.k, pk, count, a.dk, fk);
+        RW::fetch(a.v, pv, count, a.dv, fv);
+        pq += G * a.q.st;
+        pk += G * a.k.st;
+        pv += G * a.v.st;
         if ((int)threadIdx.x < count) {
-            fr = delta_gate(a.r, pr, t0 + threadIdx.x, BF);
-            fb = delta_gate(a.b, pb, t0 + threadIdx.x, BF);
+            fr = delta_gate(pr, BF);
+            fb = delta_gate(pb, BF);
         }
-        fd = a.done && lane < count ? a.done[(int64_t)(t0 + lane) * a.B + b] : 0;
+        pr += G * a.r.st;
+        pb += G * a.b.st;
+        if (pd) {
+            fd = lane < count ? *(const TP_GLOBAL uint8_t *)pd : 0;
+            pd += G * (int64_t)a.B;
+        }
     };
-    fetch(0);
+    fetch(len < G ? len : G);
     if (threadIdx.x < 2) sodd[threadIdx.x] = 0;
     workgroup_lds_barrier();
     for (int t0 = 0, turn = 0; t0 < a.T; t0 += G, turn ^= 1) {
@@ -119,44 +128,43 @@ __global__ __launch_bounds__(4 * D, D == 128 ? 2 : 3) void delta_fwd_kernel(Delt
             RW::put(q, fq);
             RW::put(k, fk);
             RW::put(v, fv);
-            bool odd = RW::odd(fq) || RW::odd(fk) || RW::odd(fv);
+            float odd = RW::odd(fq) + RW::odd(fk) + RW::odd(fv);
             if ((int)threadIdx.x < count) {
-                const float g = rate * delta_sigmoid(fr), be = delta_sigmoid(fb);
+                const float g = rate * delta_sigmoid(fr);
                 sg[threadIdx.x] = g < -3e38f ? -3e38f : g;
-                sbeta[threadIdx.x] = be;
-                odd = odd || !(fabsf(fr) < 3e38f) || !(fabsf(fb) < 3e38f);
+                sbeta[threadIdx.x] = delta_sigmoid(fb);
+                odd += (fr + fb) * 0.0f;
             }
             const uint64_t ends = __ballot(lane < count && fd != 0);
-            if (odd) sodd[turn] = 1;
-            if (a.saved) {
-                float *to = a.saved + (((int64_t)(t0 / G) * a.B + b) * a.H + h) * D * D + col;
-#pragma unroll
-                for (int kt = 0; kt < KT; ++kt)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) to[(16 * kt + r4 + i) * D] = S[kt][i];
-            }
+            if (odd != odd) sodd[turn] = 1;
             workgroup_lds_barrier();
-            if (t0 + G < len) fetch(t0 + G);
+            if (t0 + G < len) fetch(len - t0 - G < G ? len - t0 - G : G);
             const bool single = __builtin_amdgcn_readfirstlane(sodd[turn]) != 0;
             if (threadIdx.x == 0) sodd[turn ^ 1] = 0;
             for (int s = 0; s < count;) {
-                int from = s, to = s;
-                for (int p = 0; p <= w && from < count; ++p) {
-                    to = piece_end(from, count, ends, single);
-                    if (p < w) from = to;
-                }
-                if (w < NP && from < count) {
+                for (int p = w; p < NP; p += NW) {
+                    int from = s;
+                    for (int j = 0; j < p && from < count; ++j) from = piece_end(from, count, ends, single);
+                    if (from >= count) break;
                     floatx4 Tt, Tn, Pt, Pn;
-                    piece_triangles<BF, D, LD, false>(q, k, sg, sbeta, from, to - from, lane, cum[w], &rows[w], Tt,
-                                                      Tn, Pt, Pn);
-                    sT[w][lane] = Tile<BF>::split(Tt);
-                    sP[w][lane] = Tile<BF>::split(Pt);
+                    piece_triangles<BF, D, LD, false>(q, k, sg, sbeta, from,
+                                                      piece_end(from, count, ends, single) - from, lane, cum[p],
+                                                      &rows[p], Tt, Tn, Pt, Pn);
+                    sT[p][lane] = Tile<BF>::split(Tt);
+                    sP[p][lane] = Tile<BF>::split(Pt);
                 }
                 workgroup_lds_barrier();
 #pragma unroll 1
                 for (int p = 0; p < NP && s < count; ++p) {
                     const int e = piece_end(s, count, ends, single);
                     const bool done = ends >> (e - 1) & 1;
+                    if (ps && s % DELTA_GROUP == 0) {
+#pragma unroll
+                        for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) ((TP_GLOBAL float *)ps)[(16 * kt + i) * D] = S[kt][i];
+                        ps += (int64_t)gridDim.x * D * D;
+                    }
                     if (e - s == 16)
                         run_piece<BF, D, LD, false>(q, k, v, s, 16, done, rows[p], sT[p][lane], sP[p][lane], w,
                                                     lane, S);
@@ -168,7 +176,10 @@ __global__ __launch_bounds__(4 * D, D == 128 ? 2 : 3) void delta_fwd_kernel(Delt
                 workgroup_lds_barrier();
             }
         }
-        if (a.y.p) RW::store(a.y, base(a.y), t0, count > 0 ? count : 0, all, a.dv, v);
+        if (py) {
+            RW::store(a.y, py, count > 0 ? count : 0, all, a.dv, v);
+            py += G * a.y.st;
+        }
     }
     if (a.h_last) {
 #pragma unroll
@@ -242,8 +253,8 @@ __global__ __launch_bounds__(256) void delta_step_kernel(DeltaArgs a)
         }
     }
     const float alpha = delta_exp(-8.0f * delta_softplus(a.lam[h]) *
-                                  delta_sigmoid(delta_gate(a.r, base(a.r), 0, BF)));
-    const float beta = delta_sigmoid(delta_gate(a.b, base(a.b), 0, BF));
+                                  delta_sigmoid(delta_gate(base(a.r), BF)));
+    const float beta = delta_sigmoid(delta_gate(base(a.b), BF));
     __syncthreads();
     floatx4 ks = {}, qs = {};
 #pragma unroll
@@ -304,9 +315,10 @@ __global__ __launch_bounds__(256) void delta_step_kernel(DeltaArgs a)
 template <bool BF>
 void start_forward(DeltaArgs &a, hipStream_t s)
 {
+    constexpr int G = BF ? 64 : 32;
     const int D = delta_width(a.dk, a.dv);
-    void (*kernel)(DeltaArgs) = D == 32 ? delta_fwd_kernel<BF, 32> : D == 64 ? delta_fwd_kernel<BF, 64>
-                                                                             : delta_fwd_kernel<BF, 128>;
+    void (*kernel)(DeltaArgs) = D == 32 ? delta_fwd_kernel<BF, 32, G> : D == 64 ? delta_fwd_kernel<BF, 64, G>
+                                                                                : delta_fwd_kernel<BF, 128, G>;
     hipLaunchKernelGGL(kernel, dim3((unsigned)(a.B * a.H)), dim3(4 * D), 0, s, a);
 }
 

@@ -21,8 +21,8 @@
 // operand that is not an input is three bf16 numbers that add up to it: states and
 // writes go through many products one after the other, and keep fp32's precision
 // so (with two numbers states were off by 4e-6, lambda's gradient by 3e-5).  A
-// product over 16 fills half of the instruction's 32; the other half takes another
-// of the numbers.
+// product over 16 fills half of the instruction's 32; where nothing else fits, the
+// half-rate product over 16 saves the copies that would fill it.
 #pragma once
 
 #include "device.hpp"
@@ -54,6 +54,11 @@ template <> struct Tile<false> {
     static __device__ __forceinline__ floatx4 mm2(val a0, val a1, val b0, val b1, floatx4 c)
     {
         return mm(a1, b1, mm(a0, b0, c));
+    }
+    static __device__ __forceinline__ floatx4 mm_out(val a, val b, floatx4 c) { return mm(a, b, c); }
+    static __device__ __forceinline__ floatx4 mm2_out(val a0, val a1, val b0, val b1, floatx4 c)
+    {
+        return mm2(a0, a1, b0, b1, c);
     }
 };
 
@@ -98,29 +103,43 @@ template <> struct Tile<true> {
     {
         return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
     }
+    // (half the rate of the products over 32, but no register is copied to fill one)
+    static __device__ __forceinline__ floatx4 go(bf16x4 a, bf16x4 b, floatx4 c)
+    {
+        typedef short s4 __attribute__((ext_vector_type(4)));
+        s4 x, y;
+        __builtin_memcpy(&x, &a, sizeof x);
+        __builtin_memcpy(&y, &b, sizeof y);
+        return __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(x, y, c, 0, 0, 0);
+    }
     // (the least products first)
     static __device__ __forceinline__ floatx4 mm(raw a, val b, floatx4 c)
     {
-        const bf16x4 z = {};
-        c = go(join(a, z), join(b.lo, z), c);
-        return go(join(a, a), join(b.mid, b.hi), c);
+        return go(a, b.hi, go(a, b.mid, go(a, b.lo, c)));
     }
     static __device__ __forceinline__ floatx4 mm(val a, raw b, floatx4 c)
     {
-        const bf16x4 z = {};
-        c = go(join(a.lo, z), join(b, z), c);
-        return go(join(a.mid, a.hi), join(b, b), c);
+        return go(a.hi, b, go(a.mid, b, go(a.lo, b, c)));
     }
     static __device__ __forceinline__ floatx4 mm(val a, val b, floatx4 c)
     {
-        c = go(join(a.hi, a.lo), join(b.lo, b.hi), c);
-        c = go(join(a.mid, a.hi), join(b.mid, b.mid), c);
-        return go(join(a.mid, a.hi), join(b.hi, b.hi), c);
+        c = go(a.lo, b.hi, go(a.hi, b.lo, c));
+        c = go(a.mid, b.hi, go(a.hi, b.mid, c));
+        return go(a.hi, b.hi, go(a.mid, b.mid, c));
+    }
+    // the same for results that are rounded to bf16 next: two numbers of each
+    static __device__ __forceinline__ floatx4 mm_out(val a, val b, floatx4 c)
+    {
+        return go(a.hi, b.hi, go(a.mid, b.hi, go(a.hi, b.mid, c)));
     }
     // products over 32
     static __device__ __forceinline__ floatx4 mm2(raw a0, raw a1, val b0, val b1, floatx4 c)
     {
         c = go(join(a0, a1), join(b0.lo, b1.lo), c);
+        return mm2_out(a0, a1, b0, b1, c);
+    }
+    static __device__ __forceinline__ floatx4 mm2_out(raw a0, raw a1, val b0, val b1, floatx4 c)
+    {
         c = go(join(a0, a1), join(b0.mid, b1.mid), c);
         return go(join(a0, a1), join(b0.hi, b1.hi), c);
     }
@@ -154,28 +173,34 @@ struct Rows {
     static constexpr int PER = 16 / (int)sizeof(E);         // elements of a part
     static constexpr int PARTS = D / PER;                   // of a row
     static constexpr int N = G * PARTS / NT;                // parts of a thread
-    static_assert(G * PARTS % NT == 0 && N >= 1, "threads share the rows evenly");
+    static_assert(G * PARTS % NT == 0 && N >= 1 && NT % PARTS == 0, "threads share the rows evenly");
 
-    // part i of this thread: its row and first column
-    static __device__ __forceinline__ int row(int i) { return ((int)threadIdx.x + i * NT) / PARTS; }
-    static __device__ __forceinline__ int col(int i) { return ((int)threadIdx.x + i * NT) % PARTS * PER; }
+    // this thread's first part: its row and first column; the others are NT / PARTS rows on
+    static __device__ __forceinline__ int row() { return (int)threadIdx.x / PARTS; }
+    static __device__ __forceinline__ int col() { return (int)threadIdx.x % PARTS * PER; }
 
-    // rows t0.. of an array into registers; zeros past `count` rows and d columns
-    static __device__ __forceinline__ void fetch(const DeltaRows &m, const char *base, int64_t t0, int count,
-                                                 int d, Part *reg)
+    // where this thread's first part of rows t0.. is, and the bytes to its next one
+    static __device__ __forceinline__ char *at(const DeltaRows &m, int64_t b, int h, int64_t t0)
+    {
+        return (char *)m.p + b * m.sb + h * m.sh + (t0 + row()) * m.st + col() * (int64_t)sizeof(E);
+    }
+    static __device__ __forceinline__ int64_t hop(const DeltaRows &m) { return NT / PARTS * m.st; }
+
+    // rows of an array into registers; zeros past `count` rows and d columns
+    static __device__ __forceinline__ void fetch(const DeltaRows &m, const char *at, int count, int d, Part *reg)
     {
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             Part p = {};
-            const int r = row(i), c = col(i);
+            const int r = row() + i * (NT / PARTS), c = col();
+            const char *from = at + i * hop(m);
             if (r < count && c < d) {
-                const char *at = base + (t0 + r) * m.st + c * (int64_t)sizeof(E);
                 if (m.vec) {
-                    p = *(const Part *)at;
+                    p = *(const TP_GLOBAL Part *)from;
                 } else {
                     E e[PER];
 #pragma unroll
-                    for (int j = 0; j < PER; ++j) e[j] = c + j < d ? ((const E *)at)[j] : (E)0.0f;
+                    for (int j = 0; j < PER; ++j) e[j] = c + j < d ? ((const TP_GLOBAL E *)from)[j] : (E)0.0f;
                     __builtin_memcpy(&p, e, sizeof p);
                 }
             }
@@ -186,44 +211,51 @@ struct Rows {
     static __device__ __forceinline__ void put(E *lds, const Part *reg)
     {
 #pragma unroll
-        for (int i = 0; i < N; ++i) *(Part *)(lds + row(i) * LD + col(i)) = reg[i];
+        for (int i = 0; i < N; ++i) *(Part *)(lds + (row() + i * (NT / PARTS)) * LD + col()) = reg[i];
     }
 
     // the rows' values as they lie in LDS, zeros from row `count` to row `all`
-    static __device__ __forceinline__ void store(const DeltaRows &m, char *base, int64_t t0, int count, int all,
-                                                 int d, const E *lds)
+    static __device__ __forceinline__ void store(const DeltaRows &m, char *at, int count, int all, int d,
+                                                 const E *lds)
     {
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            const int r = row(i), c = col(i);
+            const int r = row() + i * (NT / PARTS), c = col();
             if (r >= all || c >= d) continue;
             Part p = {};
             if (r < count) p = *(const Part *)(lds + r * LD + c);
-            char *at = base + (t0 + r) * m.st + c * (int64_t)sizeof(E);
+            char *to = at + i * hop(m);
             if (m.vec) {
-                *(Part *)at = p;
+                *(TP_GLOBAL Part *)to = p;
             } else {
                 E e[PER];
                 __builtin_memcpy(e, &p, sizeof p);
 #pragma unroll
                 for (int j = 0; j < PER; ++j)
-                    if (c + j < d) ((E *)at)[j] = e[j];
+                    if (c + j < d) ((TP_GLOBAL E *)to)[j] = e[j];
             }
         }
     }
 
-    // a NaN or an infinity among this thread's parts
-    static __device__ __forceinline__ bool odd(const Part *reg)
+    // NaN if a NaN or an infinity is among this thread's parts, else 0
+    static __device__ __forceinline__ float odd(const Part *reg)
     {
-        uint32_t bad = 0;
+        float x = 0.0f;
 #pragma unroll
         for (int i = 0; i < N; ++i)
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                if constexpr (BF) bad |= ((reg[i][j] & 0x7F807F80u) + 0x00800080u) & 0x80008000u;
-                else bad |= ((reg[i][j] & 0x7F800000u) + 0x00800000u) & 0x80000000u;
+                if constexpr (BF) {
+                    typedef __bf16 two __attribute__((ext_vector_type(2)));
+                    const uint32_t w = reg[i][j];
+                    two v, z = {};
+                    __builtin_memcpy(&v, &w, sizeof v);
+                    x = __builtin_amdgcn_fdot2_f32_bf16(v, z, x, false);
+                } else {
+                    x = fmaf(__uint_as_float(reg[i][j]), 0.0f, x);
+                }
             }
-        return bad != 0;
+        return x;
     }
 };
 
@@ -385,10 +417,12 @@ __device__ __forceinline__ void piece_triangles(const E *q, const E *k, const fl
 }
 
 // The next piece from step s of a group of `count` steps: it ends with a whole
-// tile, an episode or the group.
+// tile, an episode, the group or the steps that a kept state is for.
 __device__ __forceinline__ int piece_end(int s, int count, uint64_t ends, bool single)
 {
     int e = single ? s + 1 : s + 16;
+    const int mark = (s / DELTA_GROUP + 1) * DELTA_GROUP;
+    if (e > mark) e = mark;
     if (e > count) e = count;
     const uint64_t m = ends >> s;
     if (m) {

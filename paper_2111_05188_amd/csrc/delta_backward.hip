@@ -25,7 +25,7 @@ namespace {
 __device__ __forceinline__ float gate_at(const DeltaRows &m, const char *base, int64_t t, bool bf)
 {
     const char *p = base + t * m.st;
-    return bf ? (float)*(const __bf16 *)p : *(const float *)p;
+    return bf ? (float)*(const TP_GLOBAL __bf16 *)p : *(const TP_GLOBAL float *)p;
 }
 
 // Sum over the 16 lanes of a row group, in all of them.
@@ -349,10 +349,10 @@ __global__ __launch_bounds__(4 * D, 2) void delta_bwd_kernel(DeltaArgs a)
         const int count = len - t0 < G ? len - t0 : G, all = a.T - t0 < G ? a.T - t0 : G;
         if (count > 0) {
             Part fq[RW::N], fk[RW::N], fv[RW::N], fy[RW::N];
-            RW::fetch(a.q, base(a.q), t0, count, a.dk, fq);
-            RW::fetch(a.k, base(a.k), t0, count, a.dk, fk);
-            RW::fetch(a.v, base(a.v), t0, count, a.dv, fv);
-            RW::fetch(a.dy, base(a.dy), t0, count, a.dv, fy);
+            RW::fetch(a.q, RW::at(a.q, b, h, t0), count, a.dk, fq);
+            RW::fetch(a.k, RW::at(a.k, b, h, t0), count, a.dk, fk);
+            RW::fetch(a.v, RW::at(a.v, b, h, t0), count, a.dv, fv);
+            RW::fetch(a.dy, RW::at(a.dy, b, h, t0), count, a.dv, fy);
             const uint8_t fd = a.done && lane < count ? a.done[(int64_t)(t0 + lane) * a.B + b] : 0;
             const float *kept = a.saved + (((int64_t)grp * a.B + b) * a.H + h) * D * D;
             auto load_state = [&] {
@@ -364,7 +364,7 @@ __global__ __launch_bounds__(4 * D, 2) void delta_bwd_kernel(DeltaArgs a)
                 }
             };
             load_state();
-            bool odd = RW::odd(fq) || RW::odd(fk) || RW::odd(fv) || RW::odd(fy);
+            float odd = RW::odd(fq) + RW::odd(fk) + RW::odd(fv) + RW::odd(fy);
             workgroup_lds_barrier();                // (the group before is done with)
             if ((int)threadIdx.x < count) {
                 const float fr = gate_at(a.r, base(a.r), t0 + threadIdx.x, BF);
@@ -374,13 +374,13 @@ __global__ __launch_bounds__(4 * D, 2) void delta_bwd_kernel(DeltaArgs a)
                 sh.beta[threadIdx.x] = delta_sigmoid(fb);
                 sh.shut[threadIdx.x] = delta_sigmoid(-fr);
                 sh.idle[threadIdx.x] = delta_sigmoid(-fb);
-                odd = odd || !(fabsf(fr) < 3e38f) || !(fabsf(fb) < 3e38f);
+                odd += (fr + fb) * 0.0f;
             }
             RW::put(sh.q, fq);
             RW::put(sh.k, fk);
             RW::put(sh.v, fv);
             RW::put(sh.dy, fy);
-            if (odd) sh.odd[turn] = 1;
+            if (odd != odd) sh.odd[turn] = 1;
             const uint64_t ends = __ballot(lane < count && fd != 0);
             workgroup_lds_barrier();
             const bool single = __builtin_amdgcn_readfirstlane(sh.odd[turn]) != 0;
@@ -530,9 +530,9 @@ __global__ __launch_bounds__(4 * D, 2) void delta_bwd_kernel(DeltaArgs a)
             wave_lds_fence();
         }
         const int done_rows = count > 0 ? count : 0;
-        RW::store(a.dq, base(a.dq), t0, done_rows, all, a.dk, sh.q);
-        RW::store(a.dkey, base(a.dkey), t0, done_rows, all, a.dk, sh.k);
-        RW::store(a.dval, base(a.dval), t0, done_rows, all, a.dv, sh.v);
+        RW::store(a.dq, RW::at(a.dq, b, h, t0), done_rows, all, a.dk, sh.q);
+        RW::store(a.dkey, RW::at(a.dkey, b, h, t0), done_rows, all, a.dk, sh.k);
+        RW::store(a.dval, RW::at(a.dval, b, h, t0), done_rows, all, a.dv, sh.v);
         if (w == 0 && lane < all) {
             const float x = lane < done_rows ? sh.x[lane] : 0.0f, y = lane < done_rows ? sh.dbeta[lane] : 0.0f;
             char *pr = base(a.dr) + (t0 + lane) * a.dr.st, *pb = base(a.db) + (t0 + lane) * a.db.st;
