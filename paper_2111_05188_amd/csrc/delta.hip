@@ -6,15 +6,15 @@
 // the next group's loads are under way while one is worked on.  Each wave first
 // prepares one piece of the group (its triangles, which do not need the state),
 // then all waves run the pieces on their columns.
+//
+// Where few heads leave most CUs without work, a sequence is split into segments.
+// What a segment does to the state is linear: a first launch runs every segment on
+// no state, for what it adds, and without values on the unit states, for its map;
+// a second one takes each segment's first state from them, one product a segment.
 #include "delta.hpp"
 
 namespace tpk {
 namespace {
-
-__device__ __forceinline__ float delta_gate(const char *p, bool bf)
-{
-    return bf ? (float)*(const TP_GLOBAL __bf16 *)p : *(const TP_GLOBAL float *)p;
-}
 
 // one piece on the state's columns of this wave
 template <bool BF, int D, int LD, bool MASK, class E>
@@ -24,6 +24,7 @@ __device__ __forceinline__ void run_piece(const E *q, const E *k, E *v, int s, i
 {
     typedef Tile<BF> TL;
     constexpr int KT = D / 16;
+    lane = fresh(lane);
     const int r = 4 * (lane >> 4);
     floatx4 ks = {}, qs = {};
 #pragma unroll
@@ -60,7 +61,35 @@ __device__ __forceinline__ void run_piece(const E *q, const E *k, E *v, int s, i
         S[kt] = TL::mm(along_col<BF, LD, MASK>(k, s, count, kt, lane), x, S[kt] * rows.total);
 }
 
-template <bool BF, int D, int G>
+// what a piece does to the unit states (a value's columns are zero)
+template <bool BF, int D, int LD, bool MASK, class E>
+__device__ __forceinline__ void map_piece(const E *k, int s, int count, bool ends, const PieceRows &rows,
+                                          const typename Tile<BF>::val &Tt, int lane, floatx4 *S)
+{
+    typedef Tile<BF> TL;
+    constexpr int KT = D / 16;
+    lane = fresh(lane);
+    const int r = 4 * (lane >> 4);
+    floatx4 ks = {}, R, U = {}, W;
+#pragma unroll
+    for (int kt = 0; kt < KT; kt += 2)
+        ks = TL::mm2(along_row<BF, LD>(k, s, kt, lane), along_row<BF, LD>(k, s, kt + 1, lane), TL::split(S[kt]),
+                     TL::split(S[kt + 1]), ks);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) R[i] = !MASK || r + i < count ? -(rows.ak[r + i] * ks[i]) : 0.0f;
+    U = TL::mm(Tt, TL::split(R), U);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) W[i] = !MASK || r + i < count ? U[i] * rows.au[r + i] : 0.0f;
+    const auto x = TL::split(W);
+#pragma unroll
+    for (int kt = 0; kt < KT; ++kt) {
+        S[kt] = TL::mm(along_col<BF, LD, MASK>(k, s, count, kt, lane), x, S[kt] * rows.total);
+        if (ends) S[kt] = floatx4{};
+    }
+}
+
+// MAP: a segment's map and what it adds, instead of outputs
+template <bool BF, int D, int G, bool MAP>
 __global__ __launch_bounds__(4 * D, D == 128 ? 2 : 3) void delta_fwd_kernel(DeltaArgs a)
 {
     constexpr int NP = G / 16, KT = D / 16;
@@ -80,24 +109,38 @@ __global__ __launch_bounds__(4 * D, D == 128 ? 2 : 3) void delta_fwd_kernel(Delt
     const int n = lane & 15, r4 = 4 * (lane >> 4);
     int len = a.len ? a.len[b] : a.T;
     len = len < 0 ? 0 : len > a.T ? a.T : len;
+    // this segment's steps
+    const int begin = blockIdx.y * a.seg_len, end = a.T - begin < a.seg_len ? a.T : begin + a.seg_len;
+    len = len < end ? len : end;
     const float rate = -8.0f * delta_softplus(a.lam[h]);
     const int64_t st = ((int64_t)b * a.H + h) * a.dk * a.dv;
+    const int64_t part = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * D * D;
     const int col = 16 * w + n;
-    floatx4 S[KT];
+    floatx4 S[KT], M[MAP ? KT : 1];
 #pragma unroll
     for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int row = 16 * kt + r4 + i;
-            S[kt][i] = a.h0 && row < a.dk && col < a.dv ? a.h0[st + (int64_t)row * a.dv + col] : 0.0f;
+            if constexpr (MAP) {
+                S[kt][i] = 0.0f;
+                M[kt][i] = row == col ? 1.0f : 0.0f;
+            } else if (a.segments > 1) {
+                S[kt][i] = a.adds[part + row * D + col];
+            } else {
+                S[kt][i] = a.h0 && row < a.dk && col < a.dv ? a.h0[st + (int64_t)row * a.dv + col] : 0.0f;
+            }
         }
+    bool cut = false;
 
-    const char *pq = RW::at(a.q, b, h, 0), *pk = RW::at(a.k, b, h, 0), *pv = RW::at(a.v, b, h, 0);
-    char *py = a.y.p ? RW::at(a.y, b, h, 0) : nullptr;
-    const char *pr = (char *)a.r.p + b * a.r.sb + h * a.r.sh + threadIdx.x * a.r.st;
-    const char *pb = (char *)a.b.p + b * a.b.sb + h * a.b.sh + threadIdx.x * a.b.st;
-    const uint8_t *pd = a.done ? a.done + (int64_t)lane * a.B + b : nullptr;
-    float *ps = a.saved ? a.saved + (int64_t)blockIdx.x * D * D + r4 * D + col : nullptr;
+    const char *pq = RW::at(a.q, b, h, begin), *pk = RW::at(a.k, b, h, begin), *pv = RW::at(a.v, b, h, begin);
+    char *py = !MAP && a.y.p ? RW::at(a.y, b, h, begin) : nullptr;
+    const char *pr = (char *)a.r.p + b * a.r.sb + h * a.r.sh + (begin + (int64_t)threadIdx.x) * a.r.st;
+    const char *pb = (char *)a.b.p + b * a.b.sb + h * a.b.sh + (begin + (int64_t)threadIdx.x) * a.b.st;
+    const uint8_t *pd = a.done ? a.done + (int64_t)(begin + lane) * a.B + b : nullptr;
+    float *ps = !MAP && a.saved
+                    ? a.saved + ((int64_t)(begin / DELTA_GROUP) * gridDim.x + blockIdx.x) * D * D + r4 * D + col
+                    : nullptr;
     Part fq[RW::N], fk[RW::N], fv[RW::N];
     float fr = 0.0f, fb = 0.0f;
     uint8_t fd = 0;
@@ -119,11 +162,11 @@ __global__ __launch_bounds__(4 * D, D == 128 ? 2 : 3) void delta_fwd_kernel(Delt
             pd += G * (int64_t)a.B;
         }
     };
-    fetch(len < G ? len : G);
+    fetch(len - begin < G ? len - begin : G);
     if (threadIdx.x < 2) sodd[threadIdx.x] = 0;
     workgroup_lds_barrier();
-    for (int t0 = 0, turn = 0; t0 < a.T; t0 += G, turn ^= 1) {
-        const int count = len - t0 < G ? len - t0 : G, all = a.T - t0 < G ? a.T - t0 : G;
+    for (int t0 = begin, turn = 0; t0 < end; t0 += G, turn ^= 1) {
+        const int count = len - t0 < G ? len - t0 : G, all = end - t0 < G ? end - t0 : G;
         if (count > 0) {
             RW::put(q, fq);
             RW::put(k, fk);
@@ -165,7 +208,18 @@ __global__ __launch_bounds__(4 * D, D == 128 ? 2 : 3) void delta_fwd_kernel(Delt
                             for (int i = 0; i < 4; ++i) ((TP_GLOBAL float *)ps)[(16 * kt + i) * D] = S[kt][i];
                         ps += (int64_t)gridDim.x * D * D;
                     }
-                    if (e - s == 16)
+                    if constexpr (MAP) {
+                        cut = cut || done;
+                        if (e - s == 16) {
+                            run_piece<BF, D, LD, false>(q, k, v, s, 16, done, rows[p], sT[p][lane], sP[p][lane],
+                                                        w, lane, S);
+                            map_piece<BF, D, LD, false>(k, s, 16, done, rows[p], sT[p][lane], lane, M);
+                        } else {
+                            run_piece<BF, D, LD, true>(q, k, v, s, e - s, done, rows[p], sT[p][lane], sP[p][lane],
+                                                       w, lane, S);
+                            map_piece<BF, D, LD, true>(k, s, e - s, done, rows[p], sT[p][lane], lane, M);
+                        }
+                    } else if (e - s == 16)
                         run_piece<BF, D, LD, false>(q, k, v, s, 16, done, rows[p], sT[p][lane], sP[p][lane], w,
                                                     lane, S);
                     else
@@ -181,7 +235,17 @@ __global__ __launch_bounds__(4 * D, D == 128 ? 2 : 3) void delta_fwd_kernel(Delt
             py += G * a.y.st;
         }
     }
-    if (a.h_last) {
+    if constexpr (MAP) {
+#pragma unroll
+        for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int row = 16 * kt + r4 + i;
+                a.adds[part + row * D + col] = S[kt][i];
+                a.maps[part + row * D + col] = M[kt][i];
+            }
+        if (threadIdx.x == 0) a.cuts[blockIdx.y * gridDim.x + blockIdx.x] = cut;
+    } else if (a.h_last && end == a.T) {
 #pragma unroll
         for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
@@ -189,6 +253,61 @@ __global__ __launch_bounds__(4 * D, D == 128 ? 2 : 3) void delta_fwd_kernel(Delt
                 const int row = 16 * kt + r4 + i;
                 if (row < a.dk && col < a.dv) a.h_last[st + (int64_t)row * a.dv + col] = S[kt][i];
             }
+    }
+}
+
+// The first state of every segment, in the place of what the segment adds: a
+// workgroup has 16 columns of one head's states, wave w the rows 16w.., 16(w+4)..
+// of them; all waves read all rows of the state before from LDS.
+template <int D>
+__global__ __launch_bounds__(256) void delta_join_kernel(DeltaArgs a, bool backward)
+{
+    constexpr int KT = D / 16, MINE = (KT + 3) / 4;
+    __shared__ floatx4 state[2][KT][64];
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int n = lane & 15, r4 = 4 * (lane >> 4), col = blockIdx.y * 16 + n, heads = gridDim.x;
+    const int64_t st = (int64_t)blockIdx.x * a.dk * a.dv;
+    const float *first = backward ? a.dh_last : a.h0;
+    floatx4 S[MINE];
+#pragma unroll
+    for (int j = 0; j < MINE; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int row = 16 * (w + 4 * j) + r4 + i;
+            S[j][i] = first && row < a.dk && col < a.dv ? first[st + (int64_t)row * a.dv + col] : 0.0f;
+        }
+    for (int x = 0; x < a.segments; ++x) {
+        const int seg = backward ? a.segments - 1 - x : x;
+        const int64_t at = ((int64_t)seg * heads + blockIdx.x) * D * D;
+        const bool more = x + 1 < a.segments;
+        floatx4 add[MINE], map[MINE][KT];
+#pragma unroll
+        for (int j = 0; j < MINE; ++j) {
+            const int t = w + 4 * j;
+            if (t >= KT) continue;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                float *p = a.adds + at + (16 * t + r4 + i) * D + col;
+                add[j][i] = more ? *p : 0.0f;
+                *p = S[j][i];
+            }
+#pragma unroll
+            for (int kt = 0; kt < KT; ++kt)
+                map[j][kt] = more ? *(const floatx4 *)(a.maps + at + (16 * t + n) * D + 16 * kt + r4) : floatx4{};
+            state[x & 1][t][lane] = S[j];
+        }
+        if (!more) return;
+        const bool cut = a.cuts[seg * heads + blockIdx.x] != 0;
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < MINE; ++j) {
+            if (w + 4 * j >= KT) continue;
+            if (!cut)
+#pragma unroll
+                for (int kt = 0; kt < KT; ++kt)
+                    add[j] = Tile<false>::mm(map[j][kt], state[x & 1][kt][lane], add[j]);
+            S[j] = add[j];
+        }
     }
 }
 
@@ -312,14 +431,16 @@ __global__ __launch_bounds__(256) void delta_step_kernel(DeltaArgs a)
     }
 }
 
-template <bool BF>
+template <bool BF, int D>
 void start_forward(DeltaArgs &a, hipStream_t s)
 {
     constexpr int G = BF ? 64 : 32;
-    const int D = delta_width(a.dk, a.dv);
-    void (*kernel)(DeltaArgs) = D == 32 ? delta_fwd_kernel<BF, 32, G> : D == 64 ? delta_fwd_kernel<BF, 64, G>
-                                                                                : delta_fwd_kernel<BF, 128, G>;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)(a.B * a.H)), dim3(4 * D), 0, s, a);
+    const unsigned heads = (unsigned)(a.B * a.H);
+    if (a.segments > 1) {                   // (nobody needs the last segment's map)
+        hipLaunchKernelGGL((delta_fwd_kernel<BF, D, G, true>), dim3(heads, a.segments - 1), dim3(4 * D), 0, s, a);
+        launch_delta_join(a, false, s);
+    }
+    hipLaunchKernelGGL((delta_fwd_kernel<BF, D, G, false>), dim3(heads, a.segments), dim3(4 * D), 0, s, a);
 }
 
 template <bool BF, bool VEC>
@@ -345,13 +466,62 @@ size_t delta_saved_bytes(int T, int B, int H, int dk, int dv)
     return (size_t)((T + DELTA_GROUP - 1) / DELTA_GROUP) * B * H * D * D * sizeof(float);
 }
 
-size_t delta_workspace_bytes(int, int B, int H, int, int)
+static int delta_segments(int T, int B, int H, int &seg_len)
 {
-    return ((size_t)B * H * sizeof(double) + 255) / 256 * 256;
+    const int64_t heads = (int64_t)B * H, groups = ((int64_t)T + 63) / 64;
+    int64_t want = heads < 256 ? 512 / heads : 1;
+    if (want > 64) want = 64;
+    if (want > groups / 2) want = groups / 2;
+    if (want < 2) want = 1;
+    const int64_t per = (groups + want - 1) / want;
+    seg_len = (int)(per * 64);
+    return (int)((groups + per - 1) / per);
+}
+
+// lambda's parts, one a head and segment; the maps
+size_t delta_workspace_bytes(int T, int B, int H, int dk, int dv)
+{
+    int seg_len;
+    const size_t n = (size_t)delta_segments(T, B, H, seg_len) * B * H, D = delta_width(dk, dv);
+    const size_t parts = (n * sizeof(double) + 255) / 256 * 256;
+    if (n == (size_t)B * H) return parts;
+    return parts + (n * sizeof(int32_t) + 255) / 256 * 256 + 2 * n * D * D * sizeof(float);
+}
+
+void delta_carve(DeltaArgs &a)
+{
+    a.segments = delta_segments(a.T, a.B, a.H, a.seg_len);
+    const size_t n = (size_t)a.segments * a.B * a.H, D = delta_width(a.dk, a.dv);
+    char *p = (char *)a.work;
+    a.parts = (double *)p;
+    p += (n * sizeof(double) + 255) / 256 * 256;
+    a.cuts = (int32_t *)p;
+    p += (n * sizeof(int32_t) + 255) / 256 * 256;
+    a.maps = (float *)p;
+    a.adds = a.maps + n * D * D;
+}
+
+hipError_t launch_delta_join(const DeltaArgs &a, bool backward, hipStream_t s)
+{
+    const int D = delta_width(a.dk, a.dv);
+    void (*kernel)(DeltaArgs, bool) = D == 32 ? delta_join_kernel<32> : D == 64 ? delta_join_kernel<64>
+                                                                                : delta_join_kernel<128>;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(a.B * a.H), D / 16), dim3(256), 0, s, a, backward);
+    return hipGetLastError();
+}
+
+template <bool BF>
+static void start_forward(DeltaArgs &a, hipStream_t s)
+{
+    const int D = delta_width(a.dk, a.dv);
+    if (D == 32) start_forward<BF, 32>(a, s);
+    else if (D == 64) start_forward<BF, 64>(a, s);
+    else start_forward<BF, 128>(a, s);
 }
 
 hipError_t launch_delta_forward(DeltaArgs &a, hipStream_t s)
 {
+    delta_carve(a);
     if (a.bf16) start_forward<true>(a, s);
     else start_forward<false>(a, s);
     return hipGetLastError();

@@ -55,6 +55,11 @@ template <> struct Tile<false> {
     {
         return mm(a1, b1, mm(a0, b0, c));
     }
+    // what a result's gradient needs of a value, and that as one dword
+    typedef floatx4 pair;
+    static __device__ __forceinline__ pair part(floatx4 x) { return x; }
+    static __device__ __forceinline__ floatx4 pack(floatx4 x) { return x; }
+    static __device__ __forceinline__ pair unpack(floatx4 x) { return x; }
     static __device__ __forceinline__ floatx4 mm_out(val a, val b, floatx4 c) { return mm(a, b, c); }
     static __device__ __forceinline__ floatx4 mm2_out(val a0, val a1, val b0, val b1, floatx4 c)
     {
@@ -103,7 +108,9 @@ template <> struct Tile<true> {
     {
         return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
     }
-    // (half the rate of the products over 32, but no register is copied to fill one)
+    // Half the rate of the products over 32, but no register is copied to fill one.  One
+    // accumulator takes products of one kind only: a product over 32 right after one over
+    // 16 read it before it was there (y off by an ulp of bf16, not always the same ones).
     static __device__ __forceinline__ floatx4 go(bf16x4 a, bf16x4 b, floatx4 c)
     {
         typedef short s4 __attribute__((ext_vector_type(4)));
@@ -127,19 +134,63 @@ template <> struct Tile<true> {
         c = go(a.mid, b.hi, go(a.hi, b.mid, c));
         return go(a.hi, b.hi, go(a.mid, b.mid, c));
     }
-    // the same for results that are rounded to bf16 next: two numbers of each
-    static __device__ __forceinline__ floatx4 mm_out(val a, val b, floatx4 c)
+    // Results that are rounded to bf16 next and feed nothing else take two numbers of
+    // each operand, to nearest: 2^-17 of a value is lost.
+    struct pair {
+        bf16x4 hi, mid;
+    };
+    static __device__ __forceinline__ pair part(floatx4 x)
     {
-        return go(a.hi, b.hi, go(a.mid, b.hi, go(a.hi, b.mid, c)));
+        pair v;
+        v.hi = __builtin_convertvector(x, bf16x4);
+        v.mid = __builtin_convertvector(x - __builtin_convertvector(v.hi, floatx4), bf16x4);
+        return v;
+    }
+    // both in one dword
+    static __device__ __forceinline__ floatx4 pack(floatx4 x)
+    {
+        const pair v = part(x);
+        uint32_t h[2], m[2];
+        __builtin_memcpy(h, &v.hi, sizeof h);
+        __builtin_memcpy(m, &v.mid, sizeof m);
+        const floatx4 w = {__uint_as_float(__builtin_amdgcn_perm(h[0], m[0], 0x05040100u)),
+                           __uint_as_float(__builtin_amdgcn_perm(h[0], m[0], 0x07060302u)),
+                           __uint_as_float(__builtin_amdgcn_perm(h[1], m[1], 0x05040100u)),
+                           __uint_as_float(__builtin_amdgcn_perm(h[1], m[1], 0x07060302u))};
+        return w;
+    }
+    static __device__ __forceinline__ pair unpack(floatx4 x)
+    {
+        const uint32_t w[4] = {__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]),
+                               __float_as_uint(x[3])};
+        const uint32_t m[2] = {__builtin_amdgcn_perm(w[1], w[0], 0x05040100u),
+                               __builtin_amdgcn_perm(w[3], w[2], 0x05040100u)};
+        pair v;
+        v.hi = upper(w);
+        __builtin_memcpy(&v.mid, m, sizeof m);
+        return v;
+    }
+    static __device__ __forceinline__ floatx4 mm_out(pair a, raw b, floatx4 c) { return go(a.hi, b, go(a.mid, b, c)); }
+    static __device__ __forceinline__ floatx4 mm2_out(raw a0, raw a1, pair b0, pair b1, floatx4 c)
+    {
+        c = go(join(a0, a1), join(b0.mid, b1.mid), c);
+        return go(join(a0, a1), join(b0.hi, b1.hi), c);
+    }
+    static __device__ __forceinline__ floatx4 mm2_out(pair a0, pair a1, raw b0, raw b1, floatx4 c)
+    {
+        c = go(join(a0.mid, a1.mid), join(b0, b1), c);
+        return go(join(a0.hi, a1.hi), join(b0, b1), c);
+    }
+    static __device__ __forceinline__ floatx4 mm2_out(pair a0, pair a1, pair b0, pair b1, floatx4 c)
+    {
+        c = go(join(a0.hi, a1.hi), join(b0.mid, b1.mid), c);
+        c = go(join(a0.mid, a1.mid), join(b0.hi, b1.hi), c);
+        return go(join(a0.hi, a1.hi), join(b0.hi, b1.hi), c);
     }
     // products over 32
     static __device__ __forceinline__ floatx4 mm2(raw a0, raw a1, val b0, val b1, floatx4 c)
     {
         c = go(join(a0, a1), join(b0.lo, b1.lo), c);
-        return mm2_out(a0, a1, b0, b1, c);
-    }
-    static __device__ __forceinline__ floatx4 mm2_out(raw a0, raw a1, val b0, val b1, floatx4 c)
-    {
         c = go(join(a0, a1), join(b0.mid, b1.mid), c);
         return go(join(a0, a1), join(b0.hi, b1.hi), c);
     }
@@ -282,9 +333,23 @@ __device__ __forceinline__ typename Tile<BF>::raw along_col(const E *lds, int s,
     return v;
 }
 
+// The lane's number, as if it were not known yet: what is compared and computed from
+// it stays inside the loop.  Outside, the compiler keeps some hundred lane masks and
+// addresses alive, more than there are registers for.
+__device__ __forceinline__ int fresh(int lane)
+{
+    asm volatile("" : "+v"(lane));
+    return lane;
+}
+
 // ---------------------------------------------------------------------------
 // a piece's decays and triangles (one wave)
 // ---------------------------------------------------------------------------
+
+__device__ __forceinline__ float delta_gate(const char *p, bool bf)
+{
+    return bf ? (float)*(const TP_GLOBAL __bf16 *)p : *(const TP_GLOBAL float *)p;
+}
 
 // scalars of a piece's rows, and the decay over all of it
 struct PieceRows {
@@ -348,6 +413,7 @@ __device__ __forceinline__ void piece_triangles(const E *q, const E *k, const fl
                                                 floatx4 &Tt, floatx4 &Tn, floatx4 &Pt, floatx4 &Pn)
 {
     constexpr float EPS = 1e-6f;
+    lane = fresh(lane);
     const int n = lane & 15, r = 4 * (lane >> 4);
     floatx4 kk = {}, qq = {}, kq = {}, qk = {};
 #pragma unroll
@@ -357,7 +423,7 @@ __device__ __forceinline__ void piece_triangles(const E *q, const E *k, const fl
         kk = Tile<BF>::mm2(a0, a1, a0, a1, kk);
         qq = Tile<BF>::mm2(b0, b1, b0, b1, qq);
         if constexpr (BOTH) qk = Tile<BF>::mm2(b0, b1, a0, a1, qk);
-        else kq = Tile<BF>::mm2(a0, a1, b0, b1, kq);
+        kq = Tile<BF>::mm2(a0, a1, b0, b1, kq);
     }
     const double c = piece_sums(g + s, count, lane, cum);
     const double all = cum[count - 1];
@@ -396,7 +462,7 @@ __device__ __forceinline__ void piece_triangles(const E *q, const E *k, const fl
         Ln[i] = r + i > n && r + i < count ? x * ber[i] * down[i] : 0.0f;   // row r+i after column n
         Lt[i] = r + i < n && n < count ? x * ben * up[i] : 0.0f;            // transposed
         if constexpr (BOTH) Pn[i] = r + i >= n && r + i < count ? qk[i] * rqr[i] * rkn * down[i] : 0.0f;
-        else Pt[i] = r + i <= n && n < count ? kq[i] * rkr[i] * rqn * up[i] : 0.0f;
+        Pt[i] = r + i <= n && n < count ? kq[i] * rkr[i] * rqn * up[i] : 0.0f;
         // blocks of two: I - L inside them
         const float one = r + i == n ? 1.0f : 0.0f;
         Tn[i] = (r + i) / 2 == n / 2 ? one - Ln[i] : 0.0f;
@@ -414,6 +480,16 @@ __device__ __forceinline__ void piece_triangles(const E *q, const E *k, const fl
         if (BOTH || w < 8) Tn = Tile<false>::mm(Tt, Y, Tn);
         Tt = t;
     }
+}
+
+// Sum over the 16 lanes of a row group, in all of them (rotations within the row).
+__device__ __forceinline__ float row_sum(float x)
+{
+    x += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x128, 0xF, 0xF, false));
+    x += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x124, 0xF, 0xF, false));
+    x += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x122, 0xF, 0xF, false));
+    x += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x121, 0xF, 0xF, false));
+    return x;
 }
 
 // The next piece from step s of a group of `count` steps: it ends with a whole

@@ -11,177 +11,181 @@
 // episode's end, and <G, S> at the end of the group if the episode goes on: the
 // terms of P, L and the states that a decay does not touch cancel in x.
 //
-// A workgroup has one head of one sequence and goes through its groups from the
-// last to the first, each from the state kept before it.  Products over the
-// values' columns sum over what different waves hold, so every wave carries two
-// strips of the state and of its gradient: columns 16w.. of S and G, and columns
-// 16w.. of their transposes, for which the same rows of K, Q, U and dR change
-// places in the products.  Nothing is transposed and no state goes through LDS.
+// x = y.dy - v.dv as well, and that is how it is summed: both come from the columns
+// that a wave has, to fp32's precision, while dq^ and dk^ are only as good as bf16
+// outputs need.
+//
+// A workgroup has one head of one sequence (a segment of it, where few heads leave
+// CUs without work) and goes through its groups from the last to the first, each
+// from the state kept before it.  Wave w has columns 16w.. of the state and of its
+// gradient in registers, in fp32, and runs the pieces forward for U and back for dR
+// on them.  dq^ and dk^ sum over all values' columns; for those the states before
+// and the gradients after a piece go through LDS once, to waves that have columns
+// 16w.. of the keys.
 #include "delta.hpp"
 
 namespace tpk {
 namespace {
 
-__device__ __forceinline__ float gate_at(const DeltaRows &m, const char *base, int64_t t, bool bf)
-{
-    const char *p = base + t * m.st;
-    return bf ? (float)*(const TP_GLOBAL __bf16 *)p : *(const TP_GLOBAL float *)p;
-}
+template <bool BF, int D>
+struct Back {
+    static constexpr int G = DELTA_GROUP, KT = D / 16;
+    // pieces at a time: their states' two transposes stay in registers
+    static constexpr int NP = D == 128 ? 1 : 2;
+    // a transpose goes through LDS in parts of the values' columns where all of it
+    // does not fit beside the rows
+    static constexpr int TURNS = D == 128 && !BF ? 2 : 1, TC = D / TURNS;
+    typedef Rows<BF, D, G> RW;
+    typedef typename RW::E E;
+    typedef Tile<BF> TL;
+    typedef typename TL::val val;
+    typedef typename TL::pair pair;
+    static constexpr int LD = RW::LD, NW = RW::NW, TLD = TC + 4;
+    static constexpr int PLANES = BF ? 2 : 1;
+    struct Shared {
+        // rows read past a piece's end stay inside: what follows each array here
+        __attribute__((aligned(16))) E q[G * LD], k[G * LD], v[G * LD], dy[G * LD];
+        __attribute__((aligned(16))) E U[PLANES * G * LD], dR[PLANES * G * LD];
+        __attribute__((aligned(16))) float turn[D * TLD];
+        __attribute__((aligned(16))) val m[NP][4][64];      // T, T^T, P, P^T; then the products with K, Q, K
+        __attribute__((aligned(16))) PieceRows rows[NP];
+        double cum[NP][16];
+        float g[G], beta[G], shut[G], idle[G];              // 1 - sigmoid(r), 1 - beta
+        float x[G], dbeta[G];
+        float sums[NW][G];                                  // y.dy - v.dv of a wave's columns
+        float dots[NW][G][2];                               // q^.dq^, k^.dk^ of a wave's columns
+        float ends[NW];                                     // <G, S> of a wave's columns
+        int odd[2];
+    };
+    static_assert(16 * LD * sizeof(E) <= D * TLD * sizeof(float), "rows past dR's end");
+    static_assert(sizeof(Shared) <= LDS_LIMIT, "LDS");
 
-// Sum over the 16 lanes of a row group, in all of them.
-__device__ __forceinline__ float row_sum(float x)
-{
-#pragma unroll
-    for (int m = 1; m < 16; m <<= 1) x += __shfl_xor(x, m);
-    return x;
-}
-
-// fp32 rows [G][LD] in LDS as operands: three planes of bf16, or one of fp32.
-template <bool BF, int G, int LD>
-struct Values {
-    typedef typename Tile<BF>::elem E;
-    static constexpr int COUNT = (BF ? 3 : 1) * G * LD;     // elements
-
-    static __device__ __forceinline__ void put(E *lds, int row, int col, typename Tile<BF>::val x, int i)
+    // U and dR: two planes of bf16, or one of fp32
+    static __device__ __forceinline__ void put(E *lds, int row, int col, pair x, int i)
     {
         if constexpr (BF) {
             lds[row * LD + col] = x.hi[i];
             lds[(G + row) * LD + col] = x.mid[i];
-            lds[(2 * G + row) * LD + col] = x.lo[i];
         } else {
             lds[row * LD + col] = x[i];
         }
     }
-    static __device__ __forceinline__ typename Tile<BF>::val rows(const E *lds, int s, int kt, int lane)
+    static __device__ __forceinline__ pair get(const E *lds, int s, int kt, int lane)
     {
         if constexpr (BF) {
-            typename Tile<BF>::val x;
+            pair x;
             x.hi = along_row<BF, LD>(lds, s, kt, lane);
             x.mid = along_row<BF, LD>(lds + G * LD, s, kt, lane);
-            x.lo = along_row<BF, LD>(lds + 2 * G * LD, s, kt, lane);
             return x;
         } else {
             return along_row<BF, LD>(lds, s, kt, lane);
         }
     }
-    template <bool MASK>
-    static __device__ __forceinline__ typename Tile<BF>::val cols(const E *lds, int s, int count, int ct, int lane)
+
+    // Columns 16w.. (of the values) of a state to columns 16w.. of its transpose.
+    // The buffer is free when all waves call; it is again after their next barrier.
+    static __device__ __forceinline__ void transpose(Shared &sh, const floatx4 *S, int w, int lane, floatx4 *T)
     {
-        if constexpr (BF) {
-            typename Tile<BF>::val x;
-            x.hi = along_col<BF, LD, MASK>(lds, s, count, ct, lane);
-            x.mid = along_col<BF, LD, MASK>(lds + G * LD, s, count, ct, lane);
-            x.lo = along_col<BF, LD, MASK>(lds + 2 * G * LD, s, count, ct, lane);
-            return x;
-        } else {
-            return along_col<BF, LD, MASK>(lds, s, count, ct, lane);
+        lane = fresh(lane);
+        const int n = lane & 15, r = 4 * (lane >> 4);
+#pragma unroll
+        for (int p = 0; p < TURNS; ++p) {
+            if (p) workgroup_lds_barrier();
+            if (TURNS == 1 || w / (NW / TURNS) == p) {
+#pragma unroll
+                for (int kt = 0; kt < KT; ++kt) {
+                    const floatx4 x = TL::pack(S[kt]);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) sh.turn[(16 * kt + r + i) * TLD + 16 * w + n - p * TC] = x[i];
+                }
+            }
+            workgroup_lds_barrier();
+#pragma unroll
+            for (int vt = p * KT / TURNS; vt < (p + 1) * KT / TURNS; ++vt)
+                T[vt] = *(const floatx4 *)(sh.turn + (16 * w + n) * TLD + 16 * vt + r - p * TC);
         }
     }
-};
 
-template <bool BF, int D>
-struct Back {
-    static constexpr int G = DELTA_GROUP, NP = G / 16, KT = D / 16;
-    typedef Rows<BF, D, G> RW;
-    typedef typename RW::E E;
-    typedef Tile<BF> TL;
-    typedef typename TL::val val;
-    static constexpr int LD = RW::LD;
-    typedef Values<BF, G, LD> VL;
-    // rows read past a piece's end stay inside: what follows each array here
-    struct Shared {
-        __attribute__((aligned(16))) E q[G * LD], k[G * LD], v[G * LD], dy[G * LD];
-        __attribute__((aligned(16))) E U[VL::COUNT], dR[VL::COUNT], pad[16 * LD];
-        __attribute__((aligned(16))) val m[NP][3][64];      // T, T^T, P; then the products with K, Q, K
-        __attribute__((aligned(16))) PieceRows rows[NP];
-        double cum[NP][16];
-        float g[G], beta[G], shut[G], idle[G];              // 1 - sigmoid(r), 1 - beta
-        float x[G], dbeta[G];
-        float dots[RW::NW][G][2];                           // q^.dq^, k^.dk^ of a strip
-        float ends[RW::NW];                                 // <G, S> of a strip
-        int odd[2];
-    };
-
-    // the writes U of a piece, and the state after it, on columns 16w..
-    template <bool MASK>
-    static __device__ __forceinline__ void forward(Shared &sh, int s, int count, bool ends, int p, int w, int lane,
-                                                   floatx4 *S)
+    // The writes U of a piece (kept where OUT), and the state after it, on columns
+    // 16w..; x: its rows' parts of y.dy.
+    template <bool MASK, bool OUT>
+    static __device__ __forceinline__ floatx4 forward(Shared &sh, int s, int count, bool ends, int p, int w, int lane,
+                                                      floatx4 *S)
     {
+        lane = fresh(lane);
         const int r = 4 * (lane >> 4);
         const PieceRows &rows = sh.rows[p];
-        floatx4 ks = {}, U = {}, R, W;
+        floatx4 ks = {}, qs = {}, U = {}, R, W, x = {};
 #pragma unroll
-        for (int kt = 0; kt < KT; kt += 2)
-            ks = TL::mm2(along_row<BF, LD>(sh.k, s, kt, lane), along_row<BF, LD>(sh.k, s, kt + 1, lane),
-                         TL::split(S[kt]), TL::split(S[kt + 1]), ks);
+        for (int kt = 0; kt < KT; kt += 2) {
+            const val x0 = TL::split(S[kt]), x1 = TL::split(S[kt + 1]);
+            ks = TL::mm2(along_row<BF, LD>(sh.k, s, kt, lane), along_row<BF, LD>(sh.k, s, kt + 1, lane), x0, x1, ks);
+            if constexpr (OUT)
+                qs = TL::mm2(along_row<BF, LD>(sh.q, s, kt, lane), along_row<BF, LD>(sh.q, s, kt + 1, lane), x0, x1,
+                             qs);
+        }
         const floatx4 vv = TL::wide(along_col<BF, LD, MASK>(sh.v, s, count, w, lane));
+        const floatx4 be = *(const floatx4 *)(rows.beta + r), ak = *(const floatx4 *)(rows.ak + r);
+        const floatx4 aq = *(const floatx4 *)(rows.aq + r), au = *(const floatx4 *)(rows.au + r);
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            R[i] = !MASK || r + i < count ? rows.beta[r + i] * vv[i] - rows.ak[r + i] * ks[i] : 0.0f;
+        for (int i = 0; i < 4; ++i) R[i] = !MASK || r + i < count ? be[i] * vv[i] - ak[i] * ks[i] : 0.0f;
         U = TL::mm(sh.m[p][1][lane], TL::split(R), U);
-        const val u = TL::split(U);
+        if constexpr (OUT) {
+            const pair u = TL::part(U);
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (!MASK || r + i < count) VL::put(sh.U, s + r + i, 16 * w + (lane & 15), u, i);
+            for (int i = 0; i < 4; ++i)
+                if (!MASK || r + i < count) put(sh.U, s + r + i, 16 * w + (lane & 15), u, i);
+            floatx4 o;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) W[i] = !MASK || r + i < count ? U[i] * rows.au[r + i] : 0.0f;
-        const val x = TL::split(W);
+            for (int i = 0; i < 4; ++i) o[i] = aq[i] * qs[i];
+            o = TL::mm(sh.m[p][3][lane], TL::split(U), o);
+            const floatx4 dy = TL::wide(along_col<BF, LD, MASK>(sh.dy, s, count, w, lane));
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[i] = !MASK || r + i < count ? o[i] * dy[i] : 0.0f;
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) W[i] = !MASK || r + i < count ? U[i] * au[i] : 0.0f;
+        const val y = TL::split(W);
 #pragma unroll
         for (int kt = 0; kt < KT; ++kt) {
-            S[kt] = TL::mm(along_col<BF, LD, MASK>(sh.k, s, count, kt, lane), x, S[kt] * rows.total);
+            S[kt] = TL::mm(along_col<BF, LD, MASK>(sh.k, s, count, kt, lane), y, S[kt] * rows.total);
             if (ends) S[kt] = floatx4{};
         }
-    }
-
-    // the transposed state after a piece, on columns 16w.. (keys)
-    template <bool MASK>
-    static __device__ __forceinline__ void forward_turned(Shared &sh, int s, int count, bool ends, int p, int w,
-                                                          int lane, floatx4 *ST)
-    {
-        const int r = 4 * (lane >> 4);
-        const PieceRows &rows = sh.rows[p];
-        const floatx4 kc = TL::wide(along_col<BF, LD, MASK>(sh.k, s, count, w, lane));
-        floatx4 W;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) W[i] = kc[i] * rows.au[r + i];
-        const val x = TL::split(W);
-#pragma unroll
-        for (int vt = 0; vt < KT; ++vt) {
-            ST[vt] = TL::mm(VL::template cols<MASK>(sh.U, s, count, vt, lane), x, ST[vt] * rows.total);
-            if (ends) ST[vt] = floatx4{};
-        }
+        return x;
     }
 
     // dR and dV of a piece, and the gradient of the state before it
     template <bool MASK>
-    static __device__ __forceinline__ void backward(Shared &sh, int s, int count, bool ends, int p, int w, int lane,
-                                                    floatx4 *Gs)
+    static __device__ __forceinline__ void backward(Shared &sh, int s, int count, int p, int w, int lane, floatx4 *Gs,
+                                                    floatx4 x)
     {
+        lane = fresh(lane);
         const int r = 4 * (lane >> 4), col = 16 * w + (lane & 15);
         const PieceRows &rows = sh.rows[p];
-        floatx4 kg = {}, dR = {};
+        floatx4 kg = {}, dU, dR = {}, A, B;
 #pragma unroll
-        for (int kt = 0; kt < KT; kt += 2) {
-            if (ends) Gs[kt] = Gs[kt + 1] = floatx4{};
+        for (int kt = 0; kt < KT; kt += 2)
             kg = TL::mm2(along_row<BF, LD>(sh.k, s, kt, lane), along_row<BF, LD>(sh.k, s, kt + 1, lane),
                          TL::split(Gs[kt]), TL::split(Gs[kt + 1]), kg);
-        }
         const auto dyc = along_col<BF, LD, MASK>(sh.dy, s, count, w, lane);
-        floatx4 dU;
+        const floatx4 be = *(const floatx4 *)(rows.beta + r), ak = *(const floatx4 *)(rows.ak + r);
+        const floatx4 aq = *(const floatx4 *)(rows.aq + r), au = *(const floatx4 *)(rows.au + r);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) dU[i] = !MASK || r + i < count ? kg[i] * rows.au[r + i] : 0.0f;
+        for (int i = 0; i < 4; ++i) dU[i] = !MASK || r + i < count ? kg[i] * au[i] : 0.0f;
         dU = TL::mm(sh.m[p][2][lane], dyc, dU);
         dR = TL::mm(sh.m[p][0][lane], TL::split(dU), dR);
-        const val x = TL::split(dR);
+        const pair d = TL::part(dR);
         const floatx4 dyw = TL::wide(dyc);
-        floatx4 A, B;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            A[i] = dyw[i] * rows.aq[r + i];
-            B[i] = !MASK || r + i < count ? -(dR[i] * rows.ak[r + i]) : 0.0f;
+            A[i] = dyw[i] * aq[i];
+            B[i] = !MASK || r + i < count ? -(dR[i] * ak[i]) : 0.0f;
+            E *v = sh.v + (s + r + i) * LD + col;
+            const float dv = be[i] * dR[i], t = row_sum(x[i] - (float)*v * dv);
             if (!MASK || r + i < count) {
-                VL::put(sh.dR, s + r + i, col, x, i);
-                sh.v[(s + r + i) * LD + col] = (E)(rows.beta[r + i] * dR[i]);
+                put(sh.dR, s + r + i, col, d, i);
+                *v = (E)dv;
+                if ((lane & 15) == 0) sh.sums[w][s + r + i] = t;
             }
         }
         const val a = TL::split(A), b = TL::split(B);
@@ -195,18 +199,19 @@ struct Back {
     // the gradients of a piece's triangles, as first operands (one wave)
     static __device__ __forceinline__ void triangles(Shared &sh, int s, int count, int p, int lane)
     {
+        lane = fresh(lane);
         const int n = lane & 15, r = 4 * (lane >> 4);
         const PieceRows &rows = sh.rows[p];
         floatx4 yu = {}, uy = {}, ru = {}, ur = {};
 #pragma unroll
         for (int vt = 0; vt < KT; vt += 2) {
             const auto y = along_row<BF, LD>(sh.dy, s, vt, lane), y1 = along_row<BF, LD>(sh.dy, s, vt + 1, lane);
-            const val u = VL::rows(sh.U, s, vt, lane), d = VL::rows(sh.dR, s, vt, lane);
-            const val u1 = VL::rows(sh.U, s, vt + 1, lane), d1 = VL::rows(sh.dR, s, vt + 1, lane);
-            yu = TL::mm2(y, y1, u, u1, yu);
-            uy = TL::mm2(u, u1, y, y1, uy);
-            ru = TL::mm2(d, d1, u, u1, ru);
-            ur = TL::mm2(u, u1, d, d1, ur);
+            const pair u = get(sh.U, s, vt, lane), d = get(sh.dR, s, vt, lane);
+            const pair u1 = get(sh.U, s, vt + 1, lane), d1 = get(sh.dR, s, vt + 1, lane);
+            yu = TL::mm2_out(y, y1, u, u1, yu);
+            uy = TL::mm2_out(u, u1, y, y1, uy);
+            ru = TL::mm2_out(d, d1, u, u1, ru);
+            ur = TL::mm2_out(u, u1, d, d1, ur);
         }
         floatx4 down, up, mq, mk, mm;
         piece_decays(sh.cum[p], count, lane, down, up);
@@ -225,62 +230,47 @@ struct Back {
         sh.m[p][2][lane] = TL::split(mm);
     }
 
-    // dQ^ and dK^ as far as they read the state before a piece
-    template <bool MASK>
-    static __device__ __forceinline__ void early(Shared &sh, int s, int p, int lane, const floatx4 *ST, floatx4 &dq,
-                                                 floatx4 &dk)
+    // Rows of a piece times a transposed state, on columns 16w.. of the keys.
+    static __device__ __forceinline__ floatx4 times(const E *rows, int s, int lane, const floatx4 *T)
     {
-        const int r = 4 * (lane >> 4);
-        const PieceRows &rows = sh.rows[p];
-        floatx4 a = {}, b = {};
+        lane = fresh(lane);
+        floatx4 c = {};
 #pragma unroll
-        for (int vt = 0; vt < KT; vt += 2) {
-            const val x = TL::split(ST[vt]), x1 = TL::split(ST[vt + 1]);
-            a = TL::mm2(along_row<BF, LD>(sh.dy, s, vt, lane), along_row<BF, LD>(sh.dy, s, vt + 1, lane), x, x1, a);
-            b = TL::mm(VL::rows(sh.dR, s, vt, lane), x, b);
-            b = TL::mm(VL::rows(sh.dR, s, vt + 1, lane), x1, b);
-        }
+        for (int vt = 0; vt < KT; vt += 2)
+            c = TL::mm2_out(get(rows, s, vt, lane), get(rows, s, vt + 1, lane), TL::unpack(T[vt]),
+                            TL::unpack(T[vt + 1]), c);
+        return c;
+    }
+    static __device__ __forceinline__ floatx4 times_dy(const Shared &sh, int s, int lane, const floatx4 *T)
+    {
+        lane = fresh(lane);
+        floatx4 c = {};
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            dq[i] = a[i] * rows.fade[r + i];
-            dk[i] = -(b[i] * rows.beta[r + i] * rows.fade[r + i]);
-        }
+        for (int vt = 0; vt < KT; vt += 2)
+            c = TL::mm2_out(along_row<BF, LD>(sh.dy, s, vt, lane), along_row<BF, LD>(sh.dy, s, vt + 1, lane),
+                            TL::unpack(T[vt]), TL::unpack(T[vt + 1]), c);
+        return c;
     }
 
-    // the rest of them, and the transposed gradient of the state before the piece
+    // the triangles' part, and the products that the unit rows' gradients need
     template <bool MASK>
-    static __device__ __forceinline__ void late(Shared &sh, int s, int count, bool ends, int p, int w, int lane,
-                                                floatx4 *GT, floatx4 &dq, floatx4 &dk)
+    static __device__ __forceinline__ void add_triangles(Shared &sh, int s, int count, int p, int w, int lane,
+                                                         floatx4 &dq, floatx4 &dk)
     {
+        lane = fresh(lane);
         const int r = 4 * (lane >> 4);
         const PieceRows &rows = sh.rows[p];
         const auto qc = along_col<BF, LD, MASK>(sh.q, s, count, w, lane);
         const auto kc = along_col<BF, LD, MASK>(sh.k, s, count, w, lane);
         const floatx4 qw = TL::wide(qc), kw = TL::wide(kc);
-        floatx4 c = {}, A, B;
-#pragma unroll
-        for (int vt = 0; vt < KT; ++vt) {
-            if (ends) GT[vt] = floatx4{};
-            c = TL::mm(VL::rows(sh.U, s, vt, lane), TL::split(GT[vt]), c);
-        }
+        floatx4 a = {}, b = {};
+        a = TL::mm(sh.m[p][0][lane], kc, a);
+        b = TL::mm(sh.m[p][1][lane], qc, b);
+        b = TL::mm(sh.m[p][2][lane], kc, b);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            dk[i] += c[i] * rows.rest[r + i];
-            A[i] = qw[i] * rows.aq[r + i];
-            B[i] = -(kw[i] * rows.ak[r + i]);
-        }
-        dq = TL::mm(sh.m[p][0][lane], kc, dq);
-        dk = TL::mm(sh.m[p][1][lane], qc, dk);
-        dk = TL::mm(sh.m[p][2][lane], kc, dk);
-        const val a = TL::split(A), b = TL::split(B);
-#pragma unroll
-        for (int vt = 0; vt < KT; ++vt) {
-            GT[vt] = TL::mm(along_col<BF, LD, MASK>(sh.dy, s, count, vt, lane), a, GT[vt] * rows.total);
-            GT[vt] = TL::mm(VL::template cols<MASK>(sh.dR, s, count, vt, lane), b, GT[vt]);
-        }
-        // what the unit rows' gradients need: their products with the rows
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
+            dq[i] += a[i];
+            dk[i] += b[i];
             const float x = row_sum(dq[i] * qw[i] * rows.rq[r + i]);
             const float y = row_sum(dk[i] * kw[i] * rows.rk[r + i]);
             if ((lane & 15) == 0 && (!MASK || r + i < count)) {
@@ -295,6 +285,7 @@ struct Back {
     static __device__ __forceinline__ void finish(Shared &sh, int s, int count, int p, int w, int lane, floatx4 dq,
                                                   floatx4 dk)
     {
+        lane = fresh(lane);
         const int r = 4 * (lane >> 4), col = 16 * w + (lane & 15);
         const PieceRows &rows = sh.rows[p];
 #pragma unroll
@@ -302,7 +293,7 @@ struct Back {
             if (MASK && r + i >= count) continue;
             float x = 0.0f, y = 0.0f;
 #pragma unroll
-            for (int j = 0; j < RW::NW; ++j) {
+            for (int j = 0; j < NW; ++j) {
                 x += sh.dots[j][s + r + i][0];
                 y += sh.dots[j][s + r + i][1];
             }
@@ -310,43 +301,51 @@ struct Back {
             const float rq = rows.rq[r + i], rk = rows.rk[r + i];
             *q = (E)(rq * (dq[i] - (float)*q * rq * x));
             *k = (E)(rk * (dk[i] - (float)*k * rk * y));
-            if (w == 0 && (lane & 15) == 0) sh.x[s + r + i] = x + y - 2.0f * sh.dbeta[s + r + i];
         }
     }
 };
+
+template <class F>
+__device__ __forceinline__ void whole_or_part(int count, F f)
+{
+    if (count == 16) f(std::integral_constant<bool, false>{});
+    else f(std::integral_constant<bool, true>{});
+}
 
 template <bool BF, int D>
 __global__ __launch_bounds__(4 * D, 2) void delta_bwd_kernel(DeltaArgs a)
 {
     typedef Back<BF, D> BK;
     typedef typename BK::RW RW;
-    constexpr int G = BK::G, NP = BK::NP, KT = BK::KT, LD = BK::LD;
+    constexpr int G = BK::G, NP = BK::NP, KT = BK::KT, LD = BK::LD, NW = BK::NW;
     __shared__ typename BK::Shared sh;
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int b = blockIdx.x / a.H, h = blockIdx.x - b * a.H;
     const int n = lane & 15, r4 = 4 * (lane >> 4), col = 16 * w + n;
     int len = a.len ? a.len[b] : a.T;
     len = len < 0 ? 0 : len > a.T ? a.T : len;
+    const int begin = blockIdx.y * a.seg_len, end = a.T - begin < a.seg_len ? a.T : begin + a.seg_len;
+    len = len < end ? len : end;
     const float rate = -8.0f * delta_softplus(a.lam[h]);
-    auto base = [&](const DeltaRows &m) { return (char *)m.p + b * m.sb + h * m.sh; };
-    const int64_t st = ((int64_t)b * a.H + h) * a.dk * a.dv;
+    const int64_t st = (int64_t)blockIdx.x * a.dk * a.dv;
+    const int64_t part = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * D * D;
 
-    floatx4 S[KT], ST[KT], Gs[KT], GT[KT];
+    floatx4 Gs[KT];
 #pragma unroll
     for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int row = 16 * kt + r4 + i;
-            Gs[kt][i] = a.dh_last && row < a.dk && col < a.dv ? a.dh_last[st + (int64_t)row * a.dv + col] : 0.0f;
-            GT[kt][i] = a.dh_last && row < a.dv && col < a.dk ? a.dh_last[st + (int64_t)col * a.dv + row] : 0.0f;
+            if (a.segments > 1) Gs[kt][i] = a.adds[part + row * D + col];
+            else Gs[kt][i] = a.dh_last && row < a.dk && col < a.dv ? a.dh_last[st + (int64_t)row * a.dv + col] : 0.0f;
         }
     if (threadIdx.x < 2) sh.odd[threadIdx.x] = 0;
     double lam = 0.0;
 
-    const int last = (a.T - 1) / G;
-    for (int grp = last, turn = 0; grp >= 0; --grp, turn ^= 1) {
+    const int first = begin / G, last = (end - 1) / G;
+    for (int grp = last, turn = 0; grp >= first; --grp, turn ^= 1) {
         const int t0 = grp * G;
-        const int count = len - t0 < G ? len - t0 : G, all = a.T - t0 < G ? a.T - t0 : G;
+        const int count = len - t0 < G ? len - t0 : G, all = end - t0 < G ? end - t0 : G;
         if (count > 0) {
             Part fq[RW::N], fk[RW::N], fv[RW::N], fy[RW::N];
             RW::fetch(a.q, RW::at(a.q, b, h, t0), count, a.dk, fq);
@@ -354,21 +353,20 @@ __global__ __launch_bounds__(4 * D, 2) void delta_bwd_kernel(DeltaArgs a)
             RW::fetch(a.v, RW::at(a.v, b, h, t0), count, a.dv, fv);
             RW::fetch(a.dy, RW::at(a.dy, b, h, t0), count, a.dv, fy);
             const uint8_t fd = a.done && lane < count ? a.done[(int64_t)(t0 + lane) * a.B + b] : 0;
-            const float *kept = a.saved + (((int64_t)grp * a.B + b) * a.H + h) * D * D;
+            const float *kept = a.saved + ((int64_t)grp * gridDim.x + blockIdx.x) * D * D;
+            floatx4 S[KT], ST[NP][KT], GT[KT], dq[NP], dk[NP], xs[NP];
             auto load_state = [&] {
 #pragma unroll
-                for (int kt = 0; kt < KT; ++kt) {
+                for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) S[kt][i] = kept[(16 * kt + r4 + i) * D + col];
-                    ST[kt] = *(const floatx4 *)(kept + col * D + 16 * kt + r4);
-                }
             };
             load_state();
             float odd = RW::odd(fq) + RW::odd(fk) + RW::odd(fv) + RW::odd(fy);
             workgroup_lds_barrier();                // (the group before is done with)
             if ((int)threadIdx.x < count) {
-                const float fr = gate_at(a.r, base(a.r), t0 + threadIdx.x, BF);
-                const float fb = gate_at(a.b, base(a.b), t0 + threadIdx.x, BF);
+                const float fr = delta_gate((char *)a.r.p + b * a.r.sb + h * a.r.sh + (t0 + threadIdx.x) * a.r.st, BF);
+                const float fb = delta_gate((char *)a.b.p + b * a.b.sb + h * a.b.sh + (t0 + threadIdx.x) * a.b.st, BF);
                 const float g = rate * delta_sigmoid(fr);
                 sh.g[threadIdx.x] = g < -3e38f ? -3e38f : g;
                 sh.beta[threadIdx.x] = delta_sigmoid(fb);
@@ -386,10 +384,6 @@ __global__ __launch_bounds__(4 * D, 2) void delta_bwd_kernel(DeltaArgs a)
             const bool single = __builtin_amdgcn_readfirstlane(sh.odd[turn]) != 0;
             if (threadIdx.x == 0) sh.odd[turn ^ 1] = 0;
 
-            auto run = [&](int c, auto f) {
-                if (c == 16) f(std::integral_constant<bool, false>{});
-                else f(std::integral_constant<bool, true>{});
-            };
             // NP pieces from step s on: where the p-th starts
             auto piece = [&](int s, int p) {
                 while (p-- > 0 && s < count) s = piece_end(s, count, ends, single);
@@ -405,28 +399,24 @@ __global__ __launch_bounds__(4 * D, 2) void delta_bwd_kernel(DeltaArgs a)
                 sh.m[w][0][lane] = Tile<BF>::split(Tn);
                 sh.m[w][1][lane] = Tile<BF>::split(Tt);
                 sh.m[w][2][lane] = Tile<BF>::split(Pn);
+                sh.m[w][3][lane] = Tile<BF>::split(Pt);
             };
             int batches = 0;
             for (int s = 0; s < count; s = piece(s, NP)) ++batches;
+#pragma unroll 1
             for (int batch = batches - 1; batch >= 0; --batch) {
+                const int lane = fresh(threadIdx.x & 63), r4 = 4 * (lane >> 4);
                 // the state before this batch: from the kept one, over the batches before
                 // (more than one where episodes end)
                 if (batch != batches - 1) load_state();
                 int s = 0;
+#pragma unroll 1
                 for (int j = 0; j < batch; ++j) {
                     prepare(s);
                     workgroup_lds_barrier();
                     for (int p = 0, x = s; p < NP && x < count; ++p) {
                         const int e = piece_end(x, count, ends, single);
-                        const bool done = ends >> (e - 1) & 1;
-                        BK::template forward<true>(sh, x, e - x, done, p, w, lane, S);
-                        x = e;
-                    }
-                    workgroup_lds_barrier();
-                    for (int p = 0, x = s; p < NP && x < count; ++p) {
-                        const int e = piece_end(x, count, ends, single);
-                        const bool done = ends >> (e - 1) & 1;
-                        BK::template forward_turned<true>(sh, x, e - x, done, p, w, lane, ST);
+                        BK::template forward<true, false>(sh, x, e - x, ends >> (e - 1) & 1, p, w, lane, S);
                         x = e;
                     }
                     workgroup_lds_barrier();
@@ -437,15 +427,18 @@ __global__ __launch_bounds__(4 * D, 2) void delta_bwd_kernel(DeltaArgs a)
 #pragma unroll
                 for (int p = 0; p < NP; ++p)
                     at[p + 1] = at[p] < count ? piece_end(at[p], count, ends, single) : at[p];
+                auto done = [&](int p) { return (bool)(ends >> (at[p + 1] - 1) & 1); };
                 prepare(s);
-                workgroup_lds_barrier();
+                // forward: U, and dY S^T of the states before the pieces
 #pragma unroll
                 for (int p = 0; p < NP; ++p) {
                     const int c = at[p + 1] - at[p];
                     if (c == 0) continue;
-                    const bool done = ends >> (at[p + 1] - 1) & 1;
-                    run(c, [&](auto m) {
-                        BK::template forward<decltype(m)::value>(sh, at[p], c, done, p, w, lane, S);
+                    BK::transpose(sh, S, w, lane, ST[p]);
+                    dq[p] = BK::times_dy(sh, at[p], lane, ST[p]);
+                    workgroup_lds_barrier();
+                    whole_or_part(c, [&](auto m) {
+                        xs[p] = BK::template forward<decltype(m)::value, true>(sh, at[p], c, done(p), p, w, lane, S);
                     });
                 }
                 if (batch == batches - 1) {
@@ -461,40 +454,48 @@ __global__ __launch_bounds__(4 * D, 2) void delta_bwd_kernel(DeltaArgs a)
                     x += __shfl_xor(x, 32);
                     if (lane == 0) sh.ends[w] = x;
                 }
+                // back: dR, U G^T of the gradients after the pieces, dR S^T
+                auto rest = [&](int p) {
+                    const floatx4 c = BK::times(sh.dR, at[p], lane, ST[p]);
+                    const PieceRows &rows = sh.rows[p];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        dq[p][i] *= rows.fade[r4 + i];
+                        dk[p][i] = dk[p][i] * rows.rest[r4 + i] - c[i] * rows.beta[r4 + i] * rows.fade[r4 + i];
+                    }
+                };
 #pragma unroll
                 for (int p = NP - 1; p >= 0; --p) {
                     const int c = at[p + 1] - at[p];
                     if (c == 0) continue;
-                    const bool done = ends >> (at[p + 1] - 1) & 1;
-                    run(c, [&](auto m) {
-                        BK::template backward<decltype(m)::value>(sh, at[p], c, done, p, w, lane, Gs);
+                    dk[p] = floatx4{};
+                    if (done(p)) {
+                        workgroup_lds_barrier();
+#pragma unroll
+                        for (int kt = 0; kt < KT; ++kt) Gs[kt] = floatx4{};
+                    } else {
+                        BK::transpose(sh, Gs, w, lane, GT);
+                        dk[p] = BK::times(sh.U, at[p], lane, GT);
+                    }
+                    if (p + 1 < NP && at[p + 2 < NP ? p + 2 : NP] > at[p + 1]) rest(p + 1 < NP ? p + 1 : p);
+                    workgroup_lds_barrier();
+                    whole_or_part(c, [&](auto m) {
+                        BK::template backward<decltype(m)::value>(sh, at[p], c, p, w, lane, Gs, xs[p]);
                     });
                 }
                 workgroup_lds_barrier();
+                rest(0);
                 if (w < NP) {
                     const int from = piece(s, w), to = from < count ? piece_end(from, count, ends, single) : from;
                     if (to > from) BK::triangles(sh, from, to - from, w, lane);
                 }
                 workgroup_lds_barrier();
-                floatx4 dq[NP], dk[NP];
 #pragma unroll
                 for (int p = 0; p < NP; ++p) {
                     const int c = at[p + 1] - at[p];
                     if (c == 0) continue;
-                    const bool done = ends >> (at[p + 1] - 1) & 1;
-                    run(c, [&](auto m) {
-                        BK::template early<decltype(m)::value>(sh, at[p], p, lane, ST, dq[p], dk[p]);
-                        if (p + 1 < NP)
-                            BK::template forward_turned<decltype(m)::value>(sh, at[p], c, done, p, w, lane, ST);
-                    });
-                }
-#pragma unroll
-                for (int p = NP - 1; p >= 0; --p) {
-                    const int c = at[p + 1] - at[p];
-                    if (c == 0) continue;
-                    const bool done = ends >> (at[p + 1] - 1) & 1;
-                    run(c, [&](auto m) {
-                        BK::template late<decltype(m)::value>(sh, at[p], c, done, p, w, lane, GT, dq[p], dk[p]);
+                    whole_or_part(c, [&](auto m) {
+                        BK::template add_triangles<decltype(m)::value>(sh, at[p], c, p, w, lane, dq[p], dk[p]);
                     });
                 }
                 workgroup_lds_barrier();
@@ -502,7 +503,7 @@ __global__ __launch_bounds__(4 * D, 2) void delta_bwd_kernel(DeltaArgs a)
                 for (int p = 0; p < NP; ++p) {
                     const int c = at[p + 1] - at[p];
                     if (c == 0) continue;
-                    run(c, [&](auto m) {
+                    whole_or_part(c, [&](auto m) {
                         BK::template finish<decltype(m)::value>(sh, at[p], c, p, w, lane, dq[p], dk[p]);
                     });
                 }
@@ -512,11 +513,19 @@ __global__ __launch_bounds__(4 * D, 2) void delta_bwd_kernel(DeltaArgs a)
             if (w == 0) {
                 float acc = 0.0f, on = 0.0f;
 #pragma unroll
-                for (int j = 0; j < RW::NW; ++j) on += sh.ends[j];
+                for (int j = 0; j < NW; ++j) on += sh.ends[j];
+                if (lane < count) {
+                    float x = 0.0f;
+#pragma unroll
+                    for (int j = 0; j < NW; ++j) x += sh.sums[j][lane];
+                    sh.x[lane] = x;
+                }
+                wave_lds_fence();
                 // the last step of this step's episode within the group
                 const uint64_t m = lane < count ? ends >> lane : 0;
-                const int end = m ? lane + __builtin_ctzll(m) : count - 1;
-                for (int c = 0; c < count; ++c) acc += c >= lane && c <= end ? sh.x[c] : 0.0f;
+                const int stop = m ? lane + __builtin_ctzll(m) : count - 1;
+                for (int c = 0; c < count; ++c) acc += c >= lane && c <= stop ? sh.x[c] : 0.0f;
+                wave_lds_fence();
                 if (lane < count) {
                     if (!m) acc += on;
                     // the first step of an episode has no state to fade
@@ -529,27 +538,28 @@ __global__ __launch_bounds__(4 * D, 2) void delta_bwd_kernel(DeltaArgs a)
             }
             wave_lds_fence();
         }
-        const int done_rows = count > 0 ? count : 0;
-        RW::store(a.dq, RW::at(a.dq, b, h, t0), done_rows, all, a.dk, sh.q);
-        RW::store(a.dkey, RW::at(a.dkey, b, h, t0), done_rows, all, a.dk, sh.k);
-        RW::store(a.dval, RW::at(a.dval, b, h, t0), done_rows, all, a.dv, sh.v);
+        const int some = count > 0 ? count : 0;
+        RW::store(a.dq, RW::at(a.dq, b, h, t0), some, all, a.dk, sh.q);
+        RW::store(a.dkey, RW::at(a.dkey, b, h, t0), some, all, a.dk, sh.k);
+        RW::store(a.dval, RW::at(a.dval, b, h, t0), some, all, a.dv, sh.v);
         if (w == 0 && lane < all) {
-            const float x = lane < done_rows ? sh.x[lane] : 0.0f, y = lane < done_rows ? sh.dbeta[lane] : 0.0f;
-            char *pr = base(a.dr) + (t0 + lane) * a.dr.st, *pb = base(a.db) + (t0 + lane) * a.db.st;
+            const float x = lane < some ? sh.x[lane] : 0.0f, y = lane < some ? sh.dbeta[lane] : 0.0f;
+            char *pr = (char *)a.dr.p + b * a.dr.sb + h * a.dr.sh + (t0 + lane) * a.dr.st;
+            char *pb = (char *)a.db.p + b * a.db.sb + h * a.db.sh + (t0 + lane) * a.db.st;
             if constexpr (BF) {
-                *(__bf16 *)pr = (__bf16)x;
-                *(__bf16 *)pb = (__bf16)y;
+                *(TP_GLOBAL __bf16 *)pr = (__bf16)x;
+                *(TP_GLOBAL __bf16 *)pb = (__bf16)y;
             } else {
-                *(float *)pr = x;
-                *(float *)pb = y;
+                *(TP_GLOBAL float *)pr = x;
+                *(TP_GLOBAL float *)pb = y;
             }
         }
     }
     if (w == 0) {
         lam = wave_sum(lam);
-        if (lane == 0) a.parts[blockIdx.x] = lam;
+        if (lane == 0) a.parts[(int64_t)blockIdx.y * gridDim.x + blockIdx.x] = lam;
     }
-    if (a.dh0) {
+    if (a.dh0 && begin == 0) {
 #pragma unroll
         for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
@@ -558,6 +568,153 @@ __global__ __launch_bounds__(4 * D, 2) void delta_bwd_kernel(DeltaArgs a)
                 if (row < a.dk && col < a.dv) a.dh0[st + (int64_t)row * a.dv + col] = Gs[kt][i];
             }
     }
+}
+
+// What a segment makes of the states' gradient after it: the gradient before it is
+// map (gradient after) + add.  One pass back without states: dU, dR and G of the
+// formulas, with dY on no gradient (add) and without it on the unit ones (map).
+template <bool BF, int D>
+__global__ __launch_bounds__(4 * D, 2) void delta_bwd_map_kernel(DeltaArgs a)
+{
+    constexpr int G = DELTA_GROUP, NP = G / 16, KT = D / 16;
+    typedef Rows<BF, D, G> RW;
+    typedef Tile<BF> TL;
+    typedef typename RW::E E;
+    typedef typename TL::val val;
+    constexpr int LD = RW::LD;
+    __shared__ __attribute__((aligned(16))) E buf[(3 * G + 16) * LD];
+    __shared__ val sT[NP][64], sP[NP][64];
+    __shared__ __attribute__((aligned(16))) PieceRows rows[NP];
+    __shared__ double cum[NP][16];
+    __shared__ float sg[G], sbeta[G];
+    __shared__ int sodd[2];
+    E *q = buf, *k = q + G * LD, *dy = k + G * LD;
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int b = blockIdx.x / a.H, h = blockIdx.x - b * a.H, segment = blockIdx.y + 1;
+    const int n = lane & 15, r4 = 4 * (lane >> 4), col = 16 * w + n;
+    int len = a.len ? a.len[b] : a.T;
+    len = len < 0 ? 0 : len > a.T ? a.T : len;
+    const int begin = segment * a.seg_len, end = a.T - begin < a.seg_len ? a.T : begin + a.seg_len;
+    len = len < end ? len : end;
+    const float rate = -8.0f * delta_softplus(a.lam[h]);
+    floatx4 Gs[KT], M[KT];
+#pragma unroll
+    for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            Gs[kt][i] = 0.0f;
+            M[kt][i] = 16 * kt + r4 + i == col ? 1.0f : 0.0f;
+        }
+    if (threadIdx.x < 2) sodd[threadIdx.x] = 0;
+    bool cut = false;
+    Part fq[RW::N], fk[RW::N], fy[RW::N];
+    auto fetch = [&](int t0) {
+        const int count = len - t0 < G ? len - t0 : G;
+        RW::fetch(a.q, RW::at(a.q, b, h, t0), count, a.dk, fq);
+        RW::fetch(a.k, RW::at(a.k, b, h, t0), count, a.dk, fk);
+        RW::fetch(a.dy, RW::at(a.dy, b, h, t0), count, a.dv, fy);
+    };
+    const int first = begin / G;
+    int grp = (len - 1) / G;                // (len <= begin: no group)
+    if (len > begin) fetch(grp * G);
+    for (int turn = 0; len > begin && grp >= first; --grp, turn ^= 1) {
+        const int t0 = grp * G, count = len - t0 < G ? len - t0 : G;
+        float odd = RW::odd(fq) + RW::odd(fk) + RW::odd(fy);
+        const uint8_t fd = a.done && lane < count ? a.done[(int64_t)(t0 + lane) * a.B + b] : 0;
+        workgroup_lds_barrier();
+        if ((int)threadIdx.x < count) {
+            const float fr = delta_gate((char *)a.r.p + b * a.r.sb + h * a.r.sh + (t0 + threadIdx.x) * a.r.st, BF);
+            const float fb = delta_gate((char *)a.b.p + b * a.b.sb + h * a.b.sh + (t0 + threadIdx.x) * a.b.st, BF);
+            const float g = rate * delta_sigmoid(fr);
+            sg[threadIdx.x] = g < -3e38f ? -3e38f : g;
+            sbeta[threadIdx.x] = delta_sigmoid(fb);
+            odd += (fr + fb) * 0.0f;
+        }
+        RW::put(q, fq);
+        RW::put(k, fk);
+        RW::put(dy, fy);
+        if (odd != odd) sodd[turn] = 1;
+        const uint64_t ends = __ballot(lane < count && fd != 0);
+        cut = cut || ends != 0;
+        workgroup_lds_barrier();
+        if (grp > first) fetch(t0 - G);
+        const bool single = __builtin_amdgcn_readfirstlane(sodd[turn]) != 0;
+        if (threadIdx.x == 0) sodd[turn ^ 1] = 0;
+        auto piece = [&](int s, int p) {
+            while (p-- > 0 && s < count) s = piece_end(s, count, ends, single);
+            return s;
+        };
+        int batches = 0;
+        for (int s = 0; s < count; s = piece(s, NP)) ++batches;
+#pragma unroll 1
+        for (int batch = batches - 1; batch >= 0; --batch) {
+            const int s = piece(0, batch * NP);
+            for (int p = w; p < NP; p += RW::NW) {
+                const int from = piece(s, p);
+                if (from >= count) break;
+                floatx4 Tt, Tn, Pt, Pn;
+                piece_triangles<BF, D, LD, true>(q, k, sg, sbeta, from, piece_end(from, count, ends, single) - from,
+                                                 lane, cum[p], &rows[p], Tt, Tn, Pt, Pn);
+                sT[p][lane] = TL::split(Tn);
+                sP[p][lane] = TL::split(Pn);
+            }
+            workgroup_lds_barrier();
+#pragma unroll 1
+            for (int p = NP - 1; p >= 0; --p) {
+                const int from = piece(s, p);
+                if (from >= count) continue;
+                const int c = piece_end(from, count, ends, single) - from;
+                const bool done = ends >> (from + c - 1) & 1;
+                floatx4 kg = {}, km = {}, dU, dM, dR = {}, dN = {}, A, B, C;
+                if (done) {
+#pragma unroll
+                    for (int kt = 0; kt < KT; ++kt) Gs[kt] = M[kt] = floatx4{};
+                }
+#pragma unroll
+                for (int kt = 0; kt < KT; kt += 2) {
+                    const auto k0 = along_row<BF, LD>(k, from, kt, lane), k1 = along_row<BF, LD>(k, from, kt + 1, lane);
+                    kg = TL::mm2(k0, k1, TL::split(Gs[kt]), TL::split(Gs[kt + 1]), kg);
+                    km = TL::mm2(k0, k1, TL::split(M[kt]), TL::split(M[kt + 1]), km);
+                }
+                const auto dyc = along_col<BF, LD, true>(dy, from, c, w, lane);
+                const floatx4 dyw = TL::wide(dyc);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    dU[i] = r4 + i < c ? kg[i] * rows[p].au[r4 + i] : 0.0f;
+                    dM[i] = r4 + i < c ? km[i] * rows[p].au[r4 + i] : 0.0f;
+                }
+                dU = TL::mm(sP[p][lane], dyc, dU);
+                dR = TL::mm(sT[p][lane], TL::split(dU), dR);
+                dN = TL::mm(sT[p][lane], TL::split(dM), dN);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float ak = rows[p].ak[r4 + i];
+                    A[i] = dyw[i] * rows[p].aq[r4 + i];
+                    B[i] = r4 + i < c ? -(dR[i] * ak) : 0.0f;
+                    C[i] = r4 + i < c ? -(dN[i] * ak) : 0.0f;
+                }
+                const val x = TL::split(A), y = TL::split(B), z = TL::split(C);
+#pragma unroll
+                for (int kt = 0; kt < KT; ++kt) {
+                    const auto kc = along_col<BF, LD, true>(k, from, c, kt, lane);
+                    Gs[kt] = TL::mm(along_col<BF, LD, true>(q, from, c, kt, lane), x, Gs[kt] * rows[p].total);
+                    Gs[kt] = TL::mm(kc, y, Gs[kt]);
+                    M[kt] = TL::mm(kc, z, M[kt] * rows[p].total);
+                }
+            }
+            workgroup_lds_barrier();
+        }
+    }
+    const int64_t part = ((int64_t)segment * gridDim.x + blockIdx.x) * D * D;
+#pragma unroll
+    for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int row = 16 * kt + r4 + i;
+            a.adds[part + row * D + col] = Gs[kt][i];
+            a.maps[part + row * D + col] = M[kt][i];
+        }
+    if (threadIdx.x == 0) a.cuts[segment * gridDim.x + blockIdx.x] = cut;
 }
 
 // dlambda_h = sigmoid(lambda) / softplus(lambda) * sum over sequences of parts, in
@@ -581,25 +738,37 @@ __global__ __launch_bounds__(256) void delta_lambda_kernel(const double *parts, 
     dlam[h] = (float)(s * (l < -700.0 ? 1.0 : sg / sp));
 }
 
+template <bool BF, int D>
+void start_backward(DeltaArgs &a, hipStream_t s)
+{
+    const unsigned heads = (unsigned)(a.B * a.H);
+    if (a.segments > 1) {                   // (nobody needs the first segment's map)
+        hipLaunchKernelGGL((delta_bwd_map_kernel<BF, D>), dim3(heads, a.segments - 1), dim3(4 * D), 0, s, a);
+        launch_delta_join(a, true, s);
+    }
+    hipLaunchKernelGGL((delta_bwd_kernel<BF, D>), dim3(heads, a.segments), dim3(4 * D), 0, s, a);
+}
+
 template <bool BF>
 void start_backward(DeltaArgs &a, hipStream_t s)
 {
     const int D = delta_width(a.dk, a.dv);
-    void (*kernel)(DeltaArgs) = D == 32 ? delta_bwd_kernel<BF, 32> : D == 64 ? delta_bwd_kernel<BF, 64>
-                                                                             : delta_bwd_kernel<BF, 128>;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)(a.B * a.H)), dim3(4 * D), 0, s, a);
+    if (D == 32) start_backward<BF, 32>(a, s);
+    else if (D == 64) start_backward<BF, 64>(a, s);
+    else start_backward<BF, 128>(a, s);
 }
 
 }  // namespace
 
 hipError_t launch_delta_backward(DeltaArgs &a, hipStream_t s)
 {
-    a.parts = (double *)a.work;
+    delta_carve(a);
     if (a.bf16) start_backward<true>(a, s);
     else start_backward<false>(a, s);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(delta_lambda_kernel, dim3(a.H), dim3(256), 0, s, a.parts, a.B, a.H, a.lam, a.dlam);
+    hipLaunchKernelGGL(delta_lambda_kernel, dim3(a.H), dim3(256), 0, s, a.parts, a.B * a.segments, a.H, a.lam,
+                       a.dlam);
     return hipGetLastError();
 }
 

@@ -252,7 +252,12 @@ struct DeltaArgs {
     const float *dh_last;
     float *dlam, *dh0;
     void *work;
-    double *parts;             // filled by the launcher
+    // filled by the launcher: parts of lambda's gradient, segments along time and
+    // their maps (state after = map state before + add; cut: an episode ended inside)
+    double *parts;
+    int segments, seg_len;
+    float *maps, *adds;        // [segments][B H][width][width]; adds: then the first states
+    int32_t *cuts;             // [segments][B H]
 };
 
 inline int delta_width(int dk, int dv)
@@ -263,6 +268,10 @@ inline int delta_width(int dk, int dv)
 size_t delta_saved_bytes(int T, int B, int H, int dk, int dv);
 size_t delta_workspace_bytes(int T, int B, int H, int dk, int dv);
 bool delta_fits(int T, int B, int H);
+// segments of a call and the workspace's parts; the first states of the segments
+// from their maps (of the gradient: from the last segment to the first)
+void delta_carve(DeltaArgs &a);
+hipError_t launch_delta_join(const DeltaArgs &a, bool backward, hipStream_t s);
 hipError_t launch_delta_forward(DeltaArgs &a, hipStream_t s);
 hipError_t launch_delta_backward(DeltaArgs &a, hipStream_t s);
 hipError_t launch_delta_step(DeltaArgs &a, hipStream_t s);
