@@ -318,17 +318,27 @@ __device__ __forceinline__ typename Tile<BF>::raw along_row(const E *lds, int s,
 }
 
 // columns 16 ct.. of rows s.. as the operand of a product over the rows; rows
-// from `count` on are zero where MASK
+// from `count` on are zero where MASK.  In bf16 one transposing read: the 16 lanes
+// of a group ask for 4 rows of 16 in parts of 4, and each gets a column of them.
 template <bool BF, int LD, bool MASK, class E>
 __device__ __forceinline__ typename Tile<BF>::raw along_col(const E *lds, int s, int count, int ct, int lane)
 {
     typename Tile<BF>::raw v;
-    const int r = 4 * (lane >> 4);
-    const E *p = lds + (s + r) * LD + 16 * ct + (lane & 15);
+    const int n = lane & 15, r = 4 * (lane >> 4);
+    if constexpr (BF) {
+        typedef short s4 __attribute__((ext_vector_type(4)));
+        typedef __attribute__((address_space(3))) s4 *at;
+        const s4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+            (at)(lds + (s + r + (n >> 2)) * LD + 16 * ct + 4 * (n & 3)));
+        __builtin_memcpy(&v, &x, sizeof v);
+    } else {
+        const E *p = lds + (s + r) * LD + 16 * ct + n;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const E e = p[i * LD];
-        v[i] = !MASK || r + i < count ? e : (E)0.0f;
+        for (int i = 0; i < 4; ++i) v[i] = p[i * LD];
+    }
+    if constexpr (MASK) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = r + i < count ? v[i] : (E)0.0f;
     }
     return v;
 }
