@@ -198,6 +198,53 @@ __device__ __forceinline__ double wave_sum(double v)
     return lane_value(wave_inclusive_scan(v), WAVE - 1);
 }
 
+// Sum over W neighbouring lanes (a power of two up to 64), in all of them, without
+// LDS: swaps within quads, mirrors within 8 and 16 lanes, then whole rows of 16 and
+// halves of the wave change places.  Every lane adds the same pairs.
+template <int STEP>
+__device__ __forceinline__ uint32_t lane_partner(uint32_t x, uint32_t &own)
+{
+    if constexpr (STEP < 16) {
+        constexpr int CTRL = STEP == 1 ? 0xB1 : STEP == 2 ? 0x4E : STEP == 4 ? 0x141 : 0x140;
+        own = x;
+        return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xF, 0xF, false);
+    } else {
+        auto v = STEP == 16 ? __builtin_amdgcn_permlane16_swap(x, x, false, false)
+                            : __builtin_amdgcn_permlane32_swap(x, x, false, false);
+        own = v[0];
+        return v[1];
+    }
+}
+
+template <int STEP>
+__device__ __forceinline__ float lane_add(float x)
+{
+    uint32_t own;
+    const uint32_t other = lane_partner<STEP>(__float_as_uint(x), own);
+    return __uint_as_float(own) + __uint_as_float(other);
+}
+
+template <int STEP>
+__device__ __forceinline__ double lane_add(double x)
+{
+    uint32_t lo, hi;
+    const uint32_t olo = lane_partner<STEP>((uint32_t)__double2loint(x), lo);
+    const uint32_t ohi = lane_partner<STEP>((uint32_t)__double2hiint(x), hi);
+    return __hiloint2double((int)hi, (int)lo) + __hiloint2double((int)ohi, (int)olo);
+}
+
+template <int W, class T>
+__device__ __forceinline__ T lanes_sum(T x)
+{
+    if constexpr (W > 1) x = lane_add<1>(x);
+    if constexpr (W > 2) x = lane_add<2>(x);
+    if constexpr (W > 4) x = lane_add<4>(x);
+    if constexpr (W > 8) x = lane_add<8>(x);
+    if constexpr (W > 16) x = lane_add<16>(x);
+    if constexpr (W > 32) x = lane_add<32>(x);
+    return x;
+}
+
 // fp32 -> bf16, IEEE round to nearest even (v_cvt_pk_bf16_f32 on gfx950).
 __device__ __forceinline__ __bf16 to_bf16(float x) { return (__bf16)x; }
 

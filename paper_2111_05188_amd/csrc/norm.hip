@@ -57,9 +57,14 @@ __device__ __forceinline__ void store_vec(void *row, int c, int D, const float *
 }
 
 // Sum over `width` neighbouring lanes (a power of two up to 64), in all of them.
-__device__ __forceinline__ float lanes_sum(float x, int width)
+__device__ __forceinline__ float some_lanes_sum(float x, int width)
 {
-    for (int m = 1; m < width; m <<= 1) x += __shfl_xor(x, m);
+    if (width > 1) x = lane_add<1>(x);
+    if (width > 2) x = lane_add<2>(x);
+    if (width > 4) x = lane_add<4>(x);
+    if (width > 8) x = lane_add<8>(x);
+    if (width > 16) x = lane_add<16>(x);
+    if (width > 32) x = lane_add<32>(x);
     return x;
 }
 
@@ -67,9 +72,7 @@ __device__ __forceinline__ float lanes_sum(float x, int width)
 template <int LPR>
 __device__ __forceinline__ float row_total(float x, float *lds)
 {
-    constexpr int W = LPR < 64 ? LPR : 64;
-#pragma unroll
-    for (int m = 1; m < W; m <<= 1) x += __shfl_xor(x, m);
+    x = lanes_sum<(LPR < 64 ? LPR : 64)>(x);
     if constexpr (LPR > 64) {
         __syncthreads();
         if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = x;
@@ -90,7 +93,7 @@ __device__ __forceinline__ void group_sums(const NormArgs &a, int lane, float (*
             float t = 0.0f;
 #pragma unroll
             for (int e = 0; e < V; ++e) t += s[j][e];
-            t = lanes_sum(t, a.group / V);
+            t = some_lanes_sum(t, a.group / V);
 #pragma unroll
             for (int e = 0; e < V; ++e) s[j][e] = t;
         }

@@ -393,3 +393,9 @@ def test_loss_same_bits_graphs_and_streams(dtype):
                    mu_ref=c.t["mu_ref"], stream=s)
     s.synchronize()
     assert all(torch.equal(x, y) for x, y in zip(a, outs))
+
+
+def test_policy_loss_of_many_sequences():
+    """More sequences than a workgroup adds up lengths of; more rows than there are lanes."""
+    for T, B, n in ((2, 8191, 3), (2, 8193, 3), (3, 30000, 1)):
+        Loss(T, B, n, torch.float32, True, seed=B).check()
