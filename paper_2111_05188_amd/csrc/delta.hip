@@ -20,7 +20,7 @@ namespace {
 template <bool BF, int D, int LD, bool MASK, class E>
 __device__ __forceinline__ void run_piece(const E *q, const E *k, E *v, int s, int count, bool ends,
                                           const PieceRows &rows, const typename Tile<BF>::val &Tt,
-                                          const typename Tile<BF>::val &Pt, int w, int lane, floatx4 *S)
+                                          const typename Tile<BF>::pair &Pt, int w, int lane, floatx4 *S)
 {
     typedef Tile<BF> TL;
     constexpr int KT = D / 16;
@@ -43,7 +43,7 @@ __device__ __forceinline__ void run_piece(const E *q, const E *k, E *v, int s, i
         o[i] = aq[i] * qs[i];
     }
     U = TL::mm(Tt, TL::split(R), U);
-    o = TL::mm(Pt, TL::split(U), o);
+    o = TL::mm_out(Pt, TL::part(U), o);
 #pragma unroll
     for (int i = 0; i < 4; ++i)
         if (!MASK || r + i < count) v[(s + r + i) * LD + 16 * w + (lane & 15)] = (E)o[i];
@@ -95,10 +95,10 @@ __global__ __launch_bounds__(4 * D, D == 128 ? 2 : 3) void delta_fwd_kernel(Delt
     constexpr int NP = G / 16, KT = D / 16;
     typedef Rows<BF, D, G> RW;
     typedef typename RW::E E;
-    typedef typename Tile<BF>::val val;
     constexpr int LD = RW::LD, NW = RW::NW;
     __shared__ __attribute__((aligned(16))) E buf[(3 * G + 16) * LD];
-    __shared__ val sT[NP][64], sP[NP][64];
+    __shared__ typename Tile<BF>::val sT[NP][64];
+    __shared__ typename Tile<BF>::pair sP[NP][64];
     __shared__ __attribute__((aligned(16))) PieceRows rows[NP];
     __shared__ double cum[NP][16];
     __shared__ float sg[G], sbeta[G];
@@ -194,7 +194,7 @@ __global__ __launch_bounds__(4 * D, D == 128 ? 2 : 3) void delta_fwd_kernel(Delt
                                                       piece_end(from, count, ends, single) - from, lane, cum[p],
                                                       &rows[p], Tt, Tn, Pt, Pn);
                     sT[p][lane] = Tile<BF>::split(Tt);
-                    sP[p][lane] = Tile<BF>::split(Pt);
+                    sP[p][lane] = Tile<BF>::part(Pt);
                 }
                 workgroup_lds_barrier();
 #pragma unroll 1
@@ -276,38 +276,61 @@ __global__ __launch_bounds__(256) void delta_join_kernel(DeltaArgs a, bool backw
             const int row = 16 * (w + 4 * j) + r4 + i;
             S[j][i] = first && row < a.dk && col < a.dv ? first[st + (int64_t)row * a.dv + col] : 0.0f;
         }
-    for (int x = 0; x < a.segments; ++x) {
+    struct Segment {
+        floatx4 add[MINE], map[MINE][KT];
+        int cut;
+    };
+    auto fetch = [&](int x, Segment &g) {
         const int seg = backward ? a.segments - 1 - x : x;
         const int64_t at = ((int64_t)seg * heads + blockIdx.x) * D * D;
-        const bool more = x + 1 < a.segments;
-        floatx4 add[MINE], map[MINE][KT];
+        g.cut = a.cuts[seg * heads + blockIdx.x];
 #pragma unroll
         for (int j = 0; j < MINE; ++j) {
             const int t = w + 4 * j;
             if (t >= KT) continue;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                float *p = a.adds + at + (16 * t + r4 + i) * D + col;
-                add[j][i] = more ? *p : 0.0f;
-                *p = S[j][i];
-            }
+            for (int i = 0; i < 4; ++i) g.add[j][i] = a.adds[at + (16 * t + r4 + i) * D + col];
 #pragma unroll
             for (int kt = 0; kt < KT; ++kt)
-                map[j][kt] = more ? *(const floatx4 *)(a.maps + at + (16 * t + n) * D + 16 * kt + r4) : floatx4{};
+                g.map[j][kt] = *(const floatx4 *)(a.maps + at + (16 * t + n) * D + 16 * kt + r4);
+        }
+    };
+    // the state before segment x goes to its place; the one after it, with the loads of
+    // the next but one on their way
+    auto step = [&](int x, Segment &g) {
+        const int seg = backward ? a.segments - 1 - x : x;
+        const int64_t at = ((int64_t)seg * heads + blockIdx.x) * D * D;
+#pragma unroll
+        for (int j = 0; j < MINE; ++j) {
+            const int t = w + 4 * j;
+            if (t >= KT) continue;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) a.adds[at + (16 * t + r4 + i) * D + col] = S[j][i];
             state[x & 1][t][lane] = S[j];
         }
-        if (!more) return;
-        const bool cut = a.cuts[seg * heads + blockIdx.x] != 0;
-        __syncthreads();
+        if (x + 1 == a.segments) return;
+        workgroup_lds_barrier();
 #pragma unroll
         for (int j = 0; j < MINE; ++j) {
             if (w + 4 * j >= KT) continue;
-            if (!cut)
+            S[j] = g.add[j];
+            floatx4 half = {};              // (two chains of products)
+            if (g.cut == 0)
 #pragma unroll
-                for (int kt = 0; kt < KT; ++kt)
-                    add[j] = Tile<false>::mm(map[j][kt], state[x & 1][kt][lane], add[j]);
-            S[j] = add[j];
+                for (int kt = 0; kt < KT; kt += 2) {
+                    S[j] = Tile<false>::mm(g.map[j][kt], state[x & 1][kt][lane], S[j]);
+                    half = Tile<false>::mm(g.map[j][kt + 1], state[x & 1][kt + 1][lane], half);
+                }
+            S[j] += half;
         }
+        if (x + 3 < a.segments) fetch(x + 2, g);
+    };
+    Segment even, odd;
+    fetch(0, even);
+    if (a.segments > 2) fetch(1, odd);
+    for (int x = 0; x < a.segments; x += 2) {
+        step(x, even);
+        if (x + 1 < a.segments) step(x + 1, odd);
     }
 }
 

@@ -74,7 +74,9 @@ template <> struct Tile<true> {
         bf16x4 hi, mid, lo;
     };
     static constexpr int PAD = 8;
-    // the upper 8 bits of a significand, the next 8 and the last: nothing is lost
+    // The upper 8 bits of a significand, the next 8 and the last: nothing is lost.
+    // (Rounding to the nearest, with the conversion instruction, takes as many
+    // instructions and is slower: 390 x 4,096 x 4 x 64 forward 1.94 ms against 1.82.)
     static __device__ __forceinline__ val split(floatx4 x)
     {
         val v;
@@ -135,28 +137,35 @@ template <> struct Tile<true> {
         return go(a.hi, b.hi, go(a.mid, b.mid, c));
     }
     // Results that are rounded to bf16 next and feed nothing else take two numbers of
-    // each operand, to nearest: 2^-17 of a value is lost.
+    // each operand, the second to nearest: 2^-16 of a value is lost.
     struct pair {
         bf16x4 hi, mid;
     };
+    static __device__ __forceinline__ void two(floatx4 x, uint32_t *h, uint32_t *m)
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            h[i] = __float_as_uint(x[i]);
+            m[i] = __float_as_uint(x[i] - __uint_as_float(h[i] & 0xFFFF0000u)) + 0x8000u;
+        }
+    }
     static __device__ __forceinline__ pair part(floatx4 x)
     {
+        uint32_t h[4], m[4];
+        two(x, h, m);
         pair v;
-        v.hi = __builtin_convertvector(x, bf16x4);
-        v.mid = __builtin_convertvector(x - __builtin_convertvector(v.hi, floatx4), bf16x4);
+        v.hi = upper(h);
+        v.mid = upper(m);
         return v;
     }
     // both in one dword
     static __device__ __forceinline__ floatx4 pack(floatx4 x)
     {
-        const pair v = part(x);
-        uint32_t h[2], m[2];
-        __builtin_memcpy(h, &v.hi, sizeof h);
-        __builtin_memcpy(m, &v.mid, sizeof m);
-        const floatx4 w = {__uint_as_float(__builtin_amdgcn_perm(h[0], m[0], 0x05040100u)),
-                           __uint_as_float(__builtin_amdgcn_perm(h[0], m[0], 0x07060302u)),
-                           __uint_as_float(__builtin_amdgcn_perm(h[1], m[1], 0x05040100u)),
-                           __uint_as_float(__builtin_amdgcn_perm(h[1], m[1], 0x07060302u))};
+        uint32_t h[4], m[4];
+        two(x, h, m);
+        floatx4 w;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = __uint_as_float(__builtin_amdgcn_perm(h[i], m[i], 0x07060302u));
         return w;
     }
     static __device__ __forceinline__ pair unpack(floatx4 x)
@@ -171,6 +180,10 @@ template <> struct Tile<true> {
         return v;
     }
     static __device__ __forceinline__ floatx4 mm_out(pair a, raw b, floatx4 c) { return go(a.hi, b, go(a.mid, b, c)); }
+    static __device__ __forceinline__ floatx4 mm_out(pair a, pair b, floatx4 c)
+    {
+        return go(a.hi, b.hi, go(a.mid, b.hi, go(a.hi, b.mid, c)));
+    }
     static __device__ __forceinline__ floatx4 mm2_out(raw a0, raw a1, pair b0, pair b1, floatx4 c)
     {
         c = go(join(a0, a1), join(b0.mid, b1.mid), c);

@@ -225,9 +225,9 @@ struct Back {
                     : above ? -(ur[i] * up[i] * rows.beta[n] * rows.rk[r + i]) : 0.0f;
             if (r + i == n && n < count) sh.dbeta[s + n] = ru[i];
         }
-        sh.m[p][0][lane] = TL::split(mq);
-        sh.m[p][1][lane] = TL::split(mk);
-        sh.m[p][2][lane] = TL::split(mm);
+        *(pair *)&sh.m[p][0][lane] = TL::part(mq);
+        *(pair *)&sh.m[p][1][lane] = TL::part(mk);
+        *(pair *)&sh.m[p][2][lane] = TL::part(mm);
     }
 
     // Rows of a piece times a transposed state, on columns 16w.. of the keys.
@@ -264,9 +264,9 @@ struct Back {
         const auto kc = along_col<BF, LD, MASK>(sh.k, s, count, w, lane);
         const floatx4 qw = TL::wide(qc), kw = TL::wide(kc);
         floatx4 a = {}, b = {};
-        a = TL::mm(sh.m[p][0][lane], kc, a);
-        b = TL::mm(sh.m[p][1][lane], qc, b);
-        b = TL::mm(sh.m[p][2][lane], kc, b);
+        a = TL::mm_out(*(const pair *)&sh.m[p][0][lane], kc, a);
+        b = TL::mm_out(*(const pair *)&sh.m[p][1][lane], qc, b);
+        b = TL::mm_out(*(const pair *)&sh.m[p][2][lane], kc, b);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             dq[i] += a[i];
