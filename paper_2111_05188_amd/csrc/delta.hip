@@ -133,8 +133,9 @@ __global__ __launch_bounds__(4 * D, D == 128 ? 2 : 3) void delta_fwd_kernel(Delt
         }
     bool cut = false;
 
-    const char *pq = RW::at(a.q, b, h, begin), *pk = RW::at(a.k, b, h, begin), *pv = RW::at(a.v, b, h, begin);
-    char *py = !MAP && a.y.p ? RW::at(a.y, b, h, begin) : nullptr;
+    const int tid = threadIdx.x;
+    const char *pq = RW::at(a.q, b, h, begin, tid), *pk = RW::at(a.k, b, h, begin, tid), *pv = RW::at(a.v, b, h, begin, tid);
+    char *py = !MAP && a.y.p ? RW::at(a.y, b, h, begin, tid) : nullptr;
     const char *pr = (char *)a.r.p + b * a.r.sb + h * a.r.sh + (begin + (int64_t)threadIdx.x) * a.r.st;
     const char *pb = (char *)a.b.p + b * a.b.sb + h * a.b.sh + (begin + (int64_t)threadIdx.x) * a.b.st;
     const uint8_t *pd = a.done ? a.done + (int64_t)(begin + lane) * a.B + b : nullptr;
@@ -145,9 +146,9 @@ __global__ __launch_bounds__(4 * D, D == 128 ? 2 : 3) void delta_fwd_kernel(Delt
     float fr = 0.0f, fb = 0.0f;
     uint8_t fd = 0;
     auto fetch = [&](int count) {
-        RW::fetch(a.q, pq, count, a.dk, fq);
-        RW::fetch(a.k, pk, count, a.dk, fk);
-        RW::fetch(a.v, pv, count, a.dv, fv);
+        RW::fetch(a.q, pq, count, a.dk, tid, fq);
+        RW::fetch(a.k, pk, count, a.dk, tid, fk);
+        RW::fetch(a.v, pv, count, a.dv, tid, fv);
         pq += G * a.q.st;
         pk += G * a.k.st;
         pv += G * a.v.st;
@@ -168,9 +169,9 @@ __global__ __launch_bounds__(4 * D, D == 128 ? 2 : 3) void delta_fwd_kernel(Delt
     for (int t0 = begin, turn = 0; t0 < end; t0 += G, turn ^= 1) {
         const int count = len - t0 < G ? len - t0 : G, all = end - t0 < G ? end - t0 : G;
         if (count > 0) {
-            RW::put(q, fq);
-            RW::put(k, fk);
-            RW::put(v, fv);
+            RW::put(q, fq, tid);
+            RW::put(k, fk, tid);
+            RW::put(v, fv, tid);
             float odd = RW::odd(fq) + RW::odd(fk) + RW::odd(fv);
             if ((int)threadIdx.x < count) {
                 const float g = rate * delta_sigmoid(fr);
@@ -231,7 +232,7 @@ __global__ __launch_bounds__(4 * D, D == 128 ? 2 : 3) void delta_fwd_kernel(Delt
             }
         }
         if (py) {
-            RW::store(a.y, py, count > 0 ? count : 0, all, a.dv, v);
+            RW::store(a.y, py, count > 0 ? count : 0, all, a.dv, tid, v);
             py += G * a.y.st;
         }
     }

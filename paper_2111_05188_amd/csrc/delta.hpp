@@ -55,11 +55,9 @@ template <> struct Tile<false> {
     {
         return mm(a1, b1, mm(a0, b0, c));
     }
-    // what a result's gradient needs of a value, and that as one dword
+    // what the results that feed nothing else need of a value
     typedef floatx4 pair;
     static __device__ __forceinline__ pair part(floatx4 x) { return x; }
-    static __device__ __forceinline__ floatx4 pack(floatx4 x) { return x; }
-    static __device__ __forceinline__ pair unpack(floatx4 x) { return x; }
     static __device__ __forceinline__ floatx4 mm_out(val a, val b, floatx4 c) { return mm(a, b, c); }
     static __device__ __forceinline__ floatx4 mm2_out(val a0, val a1, val b0, val b1, floatx4 c)
     {
@@ -141,42 +139,17 @@ template <> struct Tile<true> {
     struct pair {
         bf16x4 hi, mid;
     };
-    static __device__ __forceinline__ void two(floatx4 x, uint32_t *h, uint32_t *m)
+    static __device__ __forceinline__ pair part(floatx4 x)
     {
+        uint32_t h[4], m[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             h[i] = __float_as_uint(x[i]);
             m[i] = __float_as_uint(x[i] - __uint_as_float(h[i] & 0xFFFF0000u)) + 0x8000u;
         }
-    }
-    static __device__ __forceinline__ pair part(floatx4 x)
-    {
-        uint32_t h[4], m[4];
-        two(x, h, m);
         pair v;
         v.hi = upper(h);
         v.mid = upper(m);
-        return v;
-    }
-    // both in one dword
-    static __device__ __forceinline__ floatx4 pack(floatx4 x)
-    {
-        uint32_t h[4], m[4];
-        two(x, h, m);
-        floatx4 w;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = __uint_as_float(__builtin_amdgcn_perm(h[i], m[i], 0x07060302u));
-        return w;
-    }
-    static __device__ __forceinline__ pair unpack(floatx4 x)
-    {
-        const uint32_t w[4] = {__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]),
-                               __float_as_uint(x[3])};
-        const uint32_t m[2] = {__builtin_amdgcn_perm(w[1], w[0], 0x05040100u),
-                               __builtin_amdgcn_perm(w[3], w[2], 0x05040100u)};
-        pair v;
-        v.hi = upper(w);
-        __builtin_memcpy(&v.mid, m, sizeof m);
         return v;
     }
     static __device__ __forceinline__ floatx4 mm_out(pair a, raw b, floatx4 c) { return go(a.hi, b, go(a.mid, b, c)); }
@@ -239,25 +212,27 @@ struct Rows {
     static constexpr int N = G * PARTS / NT;                // parts of a thread
     static_assert(G * PARTS % NT == 0 && N >= 1 && NT % PARTS == 0, "threads share the rows evenly");
 
-    // this thread's first part: its row and first column; the others are NT / PARTS rows on
-    static __device__ __forceinline__ int row() { return (int)threadIdx.x / PARTS; }
-    static __device__ __forceinline__ int col() { return (int)threadIdx.x % PARTS * PER; }
+    // a thread's first part: its row and first column; the others are HOP rows on
+    static constexpr int HOP = NT / PARTS;
+    static __device__ __forceinline__ int row(int tid) { return tid / PARTS; }
+    static __device__ __forceinline__ int col(int tid) { return tid % PARTS * PER; }
 
-    // where this thread's first part of rows t0.. is, and the bytes to its next one
-    static __device__ __forceinline__ char *at(const DeltaRows &m, int64_t b, int h, int64_t t0)
+    // where a thread's first part of rows t0.. is
+    static __device__ __forceinline__ char *at(const DeltaRows &m, int b, int h, int64_t t0, int tid)
     {
-        return (char *)m.p + b * m.sb + h * m.sh + (t0 + row()) * m.st + col() * (int64_t)sizeof(E);
+        return (char *)m.p + b * m.sb + h * m.sh + (t0 + row(tid)) * m.st + col(tid) * (int64_t)sizeof(E);
     }
-    static __device__ __forceinline__ int64_t hop(const DeltaRows &m) { return NT / PARTS * m.st; }
 
     // rows of an array into registers; zeros past `count` rows and d columns
-    static __device__ __forceinline__ void fetch(const DeltaRows &m, const char *at, int count, int d, Part *reg)
+    static __device__ __forceinline__ void fetch(const DeltaRows &m, const char *at, int count, int d, int tid,
+                                                 Part *reg)
     {
+        const int64_t hop = HOP * m.st;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             Part p = {};
-            const int r = row() + i * (NT / PARTS), c = col();
-            const char *from = at + i * hop(m);
+            const int r = row(tid) + i * HOP, c = col(tid);
+            const char *from = at + i * hop;
             if (r < count && c < d) {
                 if (m.vec) {
                     p = *(const TP_GLOBAL Part *)from;
@@ -272,23 +247,24 @@ struct Rows {
         }
     }
 
-    static __device__ __forceinline__ void put(E *lds, const Part *reg)
+    static __device__ __forceinline__ void put(E *lds, const Part *reg, int tid)
     {
 #pragma unroll
-        for (int i = 0; i < N; ++i) *(Part *)(lds + (row() + i * (NT / PARTS)) * LD + col()) = reg[i];
+        for (int i = 0; i < N; ++i) *(Part *)(lds + (row(tid) + i * HOP) * LD + col(tid)) = reg[i];
     }
 
     // the rows' values as they lie in LDS, zeros from row `count` to row `all`
-    static __device__ __forceinline__ void store(const DeltaRows &m, char *at, int count, int all, int d,
+    static __device__ __forceinline__ void store(const DeltaRows &m, char *at, int count, int all, int d, int tid,
                                                  const E *lds)
     {
+        const int64_t hop = HOP * m.st;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            const int r = row() + i * (NT / PARTS), c = col();
+            const int r = row(tid) + i * HOP, c = col(tid);
             if (r >= all || c >= d) continue;
             Part p = {};
             if (r < count) p = *(const Part *)(lds + r * LD + c);
-            char *to = at + i * hop(m);
+            char *to = at + i * hop;
             if (m.vec) {
                 *(TP_GLOBAL Part *)to = p;
             } else {
@@ -363,6 +339,16 @@ __device__ __forceinline__ int fresh(int lane)
 {
     asm volatile("" : "+v"(lane));
     return lane;
+}
+
+// The kernel's arguments, read anew: eleven arrays' pointers and strides are more than
+// the scalar registers hold, and what the compiler keeps of them in others, through
+// memory, waits for the loads under way.
+__device__ __forceinline__ const DeltaArgs &fresh_args()
+{
+    auto p = (const __attribute__((address_space(4))) char *)__builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(p));
+    return *(const DeltaArgs *)(const char *)p;
 }
 
 // ---------------------------------------------------------------------------

@@ -84,7 +84,7 @@ struct Back {
 
     // Columns 16w.. (of the values) of a state to columns 16w.. of its transpose.
     // The buffer is free when all waves call; it is again after their next barrier.
-    static __device__ __forceinline__ void transpose(Shared &sh, const floatx4 *S, int w, int lane, floatx4 *T)
+    static __device__ __forceinline__ void transpose(Shared &sh, const floatx4 *S, int w, int lane, pair *T)
     {
         lane = fresh(lane);
         const int n = lane & 15, r = 4 * (lane >> 4);
@@ -93,16 +93,14 @@ struct Back {
             if (p) workgroup_lds_barrier();
             if (TURNS == 1 || w / (NW / TURNS) == p) {
 #pragma unroll
-                for (int kt = 0; kt < KT; ++kt) {
-                    const floatx4 x = TL::pack(S[kt]);
+                for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) sh.turn[(16 * kt + r + i) * TLD + 16 * w + n - p * TC] = x[i];
-                }
+                    for (int i = 0; i < 4; ++i) sh.turn[(16 * kt + r + i) * TLD + 16 * w + n - p * TC] = S[kt][i];
             }
             workgroup_lds_barrier();
 #pragma unroll
             for (int vt = p * KT / TURNS; vt < (p + 1) * KT / TURNS; ++vt)
-                T[vt] = *(const floatx4 *)(sh.turn + (16 * w + n) * TLD + 16 * vt + r - p * TC);
+                T[vt] = TL::part(*(const floatx4 *)(sh.turn + (16 * w + n) * TLD + 16 * vt + r - p * TC));
         }
     }
 
@@ -231,24 +229,23 @@ struct Back {
     }
 
     // Rows of a piece times a transposed state, on columns 16w.. of the keys.
-    static __device__ __forceinline__ floatx4 times(const E *rows, int s, int lane, const floatx4 *T)
+    static __device__ __forceinline__ floatx4 times(const E *rows, int s, int lane, const pair *T)
     {
         lane = fresh(lane);
         floatx4 c = {};
 #pragma unroll
         for (int vt = 0; vt < KT; vt += 2)
-            c = TL::mm2_out(get(rows, s, vt, lane), get(rows, s, vt + 1, lane), TL::unpack(T[vt]),
-                            TL::unpack(T[vt + 1]), c);
+            c = TL::mm2_out(get(rows, s, vt, lane), get(rows, s, vt + 1, lane), T[vt], T[vt + 1], c);
         return c;
     }
-    static __device__ __forceinline__ floatx4 times_dy(const Shared &sh, int s, int lane, const floatx4 *T)
+    static __device__ __forceinline__ floatx4 times_dy(const Shared &sh, int s, int lane, const pair *T)
     {
         lane = fresh(lane);
         floatx4 c = {};
 #pragma unroll
         for (int vt = 0; vt < KT; vt += 2)
-            c = TL::mm2_out(along_row<BF, LD>(sh.dy, s, vt, lane), along_row<BF, LD>(sh.dy, s, vt + 1, lane),
-                            TL::unpack(T[vt]), TL::unpack(T[vt + 1]), c);
+            c = TL::mm2_out(along_row<BF, LD>(sh.dy, s, vt, lane), along_row<BF, LD>(sh.dy, s, vt + 1, lane), T[vt],
+                            T[vt + 1], c);
         return c;
     }
 
@@ -342,31 +339,48 @@ __global__ __launch_bounds__(4 * D, 2) void delta_bwd_kernel(DeltaArgs a)
     if (threadIdx.x < 2) sh.odd[threadIdx.x] = 0;
     double lam = 0.0;
 
+    // a group's rows, gates and kept state; the group before's are under way while one
+    // is finished
     const int first = begin / G, last = (end - 1) / G;
+    floatx4 S[KT];
+    Part fq[RW::N], fk[RW::N], fv[RW::N], fy[RW::N];
+    float fr = 0.0f, fb = 0.0f;
+    uint8_t fd = 0;
+    auto load_state = [&](int grp) {
+        const DeltaArgs &a = fresh_args();
+        const int lane = fresh(threadIdx.x & 63), r4 = 4 * (lane >> 4), col = 16 * w + (lane & 15);
+        const float *from = a.saved + (((int64_t)grp * gridDim.x + blockIdx.x) * D + r4) * D + col;
+#pragma unroll
+        for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) S[kt][i] = ((const TP_GLOBAL float *)from)[(16 * kt + i) * D];
+    };
+    auto fetch = [&](int grp) {
+        const DeltaArgs &a = fresh_args();
+        const int tid = fresh(threadIdx.x), lane = tid & 63;
+        const int t0 = grp * G, count = len - t0 < G ? len - t0 : G;
+        RW::fetch(a.q, RW::at(a.q, b, h, t0, tid), count, a.dk, tid, fq);
+        RW::fetch(a.k, RW::at(a.k, b, h, t0, tid), count, a.dk, tid, fk);
+        RW::fetch(a.v, RW::at(a.v, b, h, t0, tid), count, a.dv, tid, fv);
+        RW::fetch(a.dy, RW::at(a.dy, b, h, t0, tid), count, a.dv, tid, fy);
+        if ((int)threadIdx.x < count) {
+            fr = delta_gate((char *)a.r.p + b * a.r.sb + h * a.r.sh + (t0 + tid) * a.r.st, BF);
+            fb = delta_gate((char *)a.b.p + b * a.b.sb + h * a.b.sh + (t0 + tid) * a.b.st, BF);
+        }
+        fd = a.done && lane < count ? *(const TP_GLOBAL uint8_t *)(a.done + (int64_t)(t0 + lane) * a.B + b) : 0;
+        load_state(grp);
+    };
+    if (len > begin) fetch((len - 1) / G);
     for (int grp = last, turn = 0; grp >= first; --grp, turn ^= 1) {
         const int t0 = grp * G;
         const int count = len - t0 < G ? len - t0 : G, all = end - t0 < G ? end - t0 : G;
         if (count > 0) {
-            Part fq[RW::N], fk[RW::N], fv[RW::N], fy[RW::N];
-            RW::fetch(a.q, RW::at(a.q, b, h, t0), count, a.dk, fq);
-            RW::fetch(a.k, RW::at(a.k, b, h, t0), count, a.dk, fk);
-            RW::fetch(a.v, RW::at(a.v, b, h, t0), count, a.dv, fv);
-            RW::fetch(a.dy, RW::at(a.dy, b, h, t0), count, a.dv, fy);
-            const uint8_t fd = a.done && lane < count ? a.done[(int64_t)(t0 + lane) * a.B + b] : 0;
-            const float *kept = a.saved + ((int64_t)grp * gridDim.x + blockIdx.x) * D * D;
-            floatx4 S[KT], ST[NP][KT], GT[KT], dq[NP], dk[NP], xs[NP];
-            auto load_state = [&] {
-#pragma unroll
-                for (int kt = 0; kt < KT; ++kt)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) S[kt][i] = kept[(16 * kt + r4 + i) * D + col];
-            };
-            load_state();
+            typename BK::pair ST[NP][KT], GT[KT];
+            floatx4 dq[NP], dk[NP], xs[NP];
             float odd = RW::odd(fq) + RW::odd(fk) + RW::odd(fv) + RW::odd(fy);
             workgroup_lds_barrier();                // (the group before is done with)
+            const int tid = fresh(threadIdx.x);
             if ((int)threadIdx.x < count) {
-                const float fr = delta_gate((char *)a.r.p + b * a.r.sb + h * a.r.sh + (t0 + threadIdx.x) * a.r.st, BF);
-                const float fb = delta_gate((char *)a.b.p + b * a.b.sb + h * a.b.sh + (t0 + threadIdx.x) * a.b.st, BF);
                 const float g = rate * delta_sigmoid(fr);
                 sh.g[threadIdx.x] = g < -3e38f ? -3e38f : g;
                 sh.beta[threadIdx.x] = delta_sigmoid(fb);
@@ -374,10 +388,10 @@ __global__ __launch_bounds__(4 * D, 2) void delta_bwd_kernel(DeltaArgs a)
                 sh.idle[threadIdx.x] = delta_sigmoid(-fb);
                 odd += (fr + fb) * 0.0f;
             }
-            RW::put(sh.q, fq);
-            RW::put(sh.k, fk);
-            RW::put(sh.v, fv);
-            RW::put(sh.dy, fy);
+            RW::put(sh.q, fq, tid);
+            RW::put(sh.k, fk, tid);
+            RW::put(sh.v, fv, tid);
+            RW::put(sh.dy, fy, tid);
             if (odd != odd) sh.odd[turn] = 1;
             const uint64_t ends = __ballot(lane < count && fd != 0);
             workgroup_lds_barrier();
@@ -408,7 +422,7 @@ __global__ __launch_bounds__(4 * D, 2) void delta_bwd_kernel(DeltaArgs a)
                 const int lane = fresh(threadIdx.x & 63), r4 = 4 * (lane >> 4);
                 // the state before this batch: from the kept one, over the batches before
                 // (more than one where episodes end)
-                if (batch != batches - 1) load_state();
+                if (batch != batches - 1) load_state(grp);
                 int s = 0;
 #pragma unroll 1
                 for (int j = 0; j < batch; ++j) {
@@ -485,6 +499,7 @@ __global__ __launch_bounds__(4 * D, 2) void delta_bwd_kernel(DeltaArgs a)
                 }
                 workgroup_lds_barrier();
                 rest(0);
+                if (batch == 0 && grp > first) fetch(grp - 1);
                 if (w < NP) {
                     const int from = piece(s, w), to = from < count ? piece_end(from, count, ends, single) : from;
                     if (to > from) BK::triangles(sh, from, to - from, w, lane);
@@ -538,10 +553,12 @@ __global__ __launch_bounds__(4 * D, 2) void delta_bwd_kernel(DeltaArgs a)
             }
             wave_lds_fence();
         }
+        const DeltaArgs &a = fresh_args();
+        const int tid = fresh(threadIdx.x), lane = tid & 63;
         const int some = count > 0 ? count : 0;
-        RW::store(a.dq, RW::at(a.dq, b, h, t0), some, all, a.dk, sh.q);
-        RW::store(a.dkey, RW::at(a.dkey, b, h, t0), some, all, a.dk, sh.k);
-        RW::store(a.dval, RW::at(a.dval, b, h, t0), some, all, a.dv, sh.v);
+        RW::store(a.dq, RW::at(a.dq, b, h, t0, tid), some, all, a.dk, tid, sh.q);
+        RW::store(a.dkey, RW::at(a.dkey, b, h, t0, tid), some, all, a.dk, tid, sh.k);
+        RW::store(a.dval, RW::at(a.dval, b, h, t0, tid), some, all, a.dv, tid, sh.v);
         if (w == 0 && lane < all) {
             const float x = lane < some ? sh.x[lane] : 0.0f, y = lane < some ? sh.dbeta[lane] : 0.0f;
             char *pr = (char *)a.dr.p + b * a.dr.sb + h * a.dr.sh + (t0 + lane) * a.dr.st;
@@ -608,11 +625,12 @@ __global__ __launch_bounds__(4 * D, 2) void delta_bwd_map_kernel(DeltaArgs a)
     if (threadIdx.x < 2) sodd[threadIdx.x] = 0;
     bool cut = false;
     Part fq[RW::N], fk[RW::N], fy[RW::N];
+    const int tid = threadIdx.x;
     auto fetch = [&](int t0) {
         const int count = len - t0 < G ? len - t0 : G;
-        RW::fetch(a.q, RW::at(a.q, b, h, t0), count, a.dk, fq);
-        RW::fetch(a.k, RW::at(a.k, b, h, t0), count, a.dk, fk);
-        RW::fetch(a.dy, RW::at(a.dy, b, h, t0), count, a.dv, fy);
+        RW::fetch(a.q, RW::at(a.q, b, h, t0, tid), count, a.dk, tid, fq);
+        RW::fetch(a.k, RW::at(a.k, b, h, t0, tid), count, a.dk, tid, fk);
+        RW::fetch(a.dy, RW::at(a.dy, b, h, t0, tid), count, a.dv, tid, fy);
     };
     const int first = begin / G;
     int grp = (len - 1) / G;                // (len <= begin: no group)
@@ -630,9 +648,9 @@ __global__ __launch_bounds__(4 * D, 2) void delta_bwd_map_kernel(DeltaArgs a)
             sbeta[threadIdx.x] = delta_sigmoid(fb);
             odd += (fr + fb) * 0.0f;
         }
-        RW::put(q, fq);
-        RW::put(k, fk);
-        RW::put(dy, fy);
+        RW::put(q, fq, tid);
+        RW::put(k, fk, tid);
+        RW::put(dy, fy, tid);
         if (odd != odd) sodd[turn] = 1;
         const uint64_t ends = __ballot(lane < count && fd != 0);
         cut = cut || ends != 0;
