@@ -361,7 +361,7 @@ __device__ __forceinline__ float delta_gate(const char *p, bool bf)
 }
 
 // scalars of a piece's rows, and the decay over all of it
-struct PieceRows {
+struct __attribute__((aligned(16))) PieceRows {
     float fade[16];             // gamma_c
     float rest[16];             // gamma_C / gamma_c
     float beta[16];
@@ -412,11 +412,14 @@ __device__ __forceinline__ double piece_sums(const float *g, int count, int lane
     return c;
 }
 
-// K K^T and Q K^T tiles of a piece, the rows' lengths, and T in both layouts.
-// L is nilpotent; its inverse grows from blocks of 1, 2, 4, 8 on the diagonal:
-// T <- T - T L_off T with the part of L that joins two blocks, so no power of L
-// is formed whose entries cancel.
-template <bool BF, int D, int LD, bool BOTH, class E>
+// What one wave prepares of a piece; the rows' scalars come along.
+enum : int { WANT_T = 1, WANT_PT = 2, WANT_P = 4 };
+
+// K K^T and Q K^T tiles of a piece, the rows' lengths, T and P in both layouts (as
+// far as they are wanted).  L is nilpotent; its inverse grows from blocks of 1, 2, 4,
+// 8 on the diagonal: T <- T - T L_off T with the part of L that joins two blocks, so
+// no power of L is formed whose entries cancel.
+template <bool BF, int D, int LD, int WANT, bool BOTH, class E>
 __device__ __forceinline__ void piece_triangles(const E *q, const E *k, const float *g, const float *beta, int s,
                                                 int count, int lane, double *cum, PieceRows *rows,
                                                 floatx4 &Tt, floatx4 &Tn, floatx4 &Pt, floatx4 &Pn)
@@ -431,8 +434,8 @@ __device__ __forceinline__ void piece_triangles(const E *q, const E *k, const fl
         const auto a1 = along_row<BF, LD>(k, s, kt + 1, lane), b1 = along_row<BF, LD>(q, s, kt + 1, lane);
         kk = Tile<BF>::mm2(a0, a1, a0, a1, kk);
         qq = Tile<BF>::mm2(b0, b1, b0, b1, qq);
-        if constexpr (BOTH) qk = Tile<BF>::mm2(b0, b1, a0, a1, qk);
-        kq = Tile<BF>::mm2(a0, a1, b0, b1, kq);
+        if constexpr (WANT & WANT_P) qk = Tile<BF>::mm2(b0, b1, a0, a1, qk);
+        if constexpr (WANT & WANT_PT) kq = Tile<BF>::mm2(a0, a1, b0, b1, kq);
     }
     const double c = piece_sums(g + s, count, lane, cum);
     const double all = cum[count - 1];
@@ -443,51 +446,58 @@ __device__ __forceinline__ void piece_triangles(const E *q, const E *k, const fl
             rows->rk[n] = n < count ? rsqrtf(kk[i] + EPS) : 0.0f;
             rows->rq[n] = n < count ? rsqrtf(qq[i] + EPS) : 0.0f;
         }
-    if (lane < 16) {
-        const float fade = n < count ? delta_exp((float)c) : 0.0f;
-        const float rest = n < count ? delta_exp((float)(all - c)) : 0.0f;
-        const float be = n < count ? beta[s + n] : 0.0f;
-        rows->fade[n] = fade;
-        rows->rest[n] = rest;
-        rows->beta[n] = be;
-        if (n == 0) rows->total = delta_exp((float)all);
-    }
-    wave_lds_fence();
-    if (lane < 16) {
-        const float rk = rows->rk[n];
-        rows->aq[n] = rows->fade[n] * rows->rq[n];
-        rows->ak[n] = rows->beta[n] * rows->fade[n] * rk;
-        rows->au[n] = rows->rest[n] * rk;
-    }
     floatx4 down, up;
     piece_decays(cum, count, lane, down, up);
-    const float rkn = rows->rk[n], rqn = rows->rq[n], ben = rows->beta[n];
+    wave_lds_fence();
+    if constexpr (WANT & WANT_T) {
+        if (lane < 16) {
+            const float fade = n < count ? delta_exp((float)c) : 0.0f;
+            const float rest = n < count ? delta_exp((float)(all - c)) : 0.0f;
+            const float be = n < count ? beta[s + n] : 0.0f;
+            rows->fade[n] = fade;
+            rows->rest[n] = rest;
+            rows->beta[n] = be;
+            if (n == 0) rows->total = delta_exp((float)all);
+            const float rk = rows->rk[n];
+            rows->aq[n] = fade * rows->rq[n];
+            rows->ak[n] = be * fade * rk;
+            rows->au[n] = rest * rk;
+        }
+    }
+    wave_lds_fence();
+    const float rkn = rows->rk[n], rqn = rows->rq[n];
     const floatx4 rkr = *(const floatx4 *)(rows->rk + r), rqr = *(const floatx4 *)(rows->rq + r);
-    const floatx4 ber = *(const floatx4 *)(rows->beta + r);
-    floatx4 Ln, Lt;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const float x = kk[i] * rkr[i] * rkn;
-        Ln[i] = r + i > n && r + i < count ? x * ber[i] * down[i] : 0.0f;   // row r+i after column n
-        Lt[i] = r + i < n && n < count ? x * ben * up[i] : 0.0f;            // transposed
-        if constexpr (BOTH) Pn[i] = r + i >= n && r + i < count ? qk[i] * rqr[i] * rkn * down[i] : 0.0f;
-        Pt[i] = r + i <= n && n < count ? kq[i] * rkr[i] * rqn * up[i] : 0.0f;
-        // blocks of two: I - L inside them
-        const float one = r + i == n ? 1.0f : 0.0f;
-        Tn[i] = (r + i) / 2 == n / 2 ? one - Ln[i] : 0.0f;
-        Tt[i] = (r + i) / 2 == n / 2 ? one - Lt[i] : 0.0f;
+        if constexpr (WANT & WANT_P) Pn[i] = r + i >= n && r + i < count ? qk[i] * rqr[i] * rkn * down[i] : 0.0f;
+        if constexpr (WANT & WANT_PT) Pt[i] = r + i <= n && n < count ? kq[i] * rkr[i] * rqn * up[i] : 0.0f;
     }
+    if constexpr (WANT & WANT_T) {
+        const float ben = rows->beta[n];
+        const floatx4 ber = *(const floatx4 *)(rows->beta + r);
+        floatx4 Lt;
 #pragma unroll
-    for (int w = 2; w < 16; w *= 2) {
-        floatx4 off;
+        for (int i = 0; i < 4; ++i) {
+            const float x = kk[i] * rkr[i] * rkn;
+            const float Ln = r + i > n && r + i < count ? x * ber[i] * down[i] : 0.0f;  // row r+i after column n
+            Lt[i] = r + i < n && n < count ? x * ben * up[i] : 0.0f;                    // transposed
+            // blocks of two: I - L inside them
+            const float one = r + i == n ? 1.0f : 0.0f;
+            Tn[i] = (r + i) / 2 == n / 2 ? one - Ln : 0.0f;
+            Tt[i] = (r + i) / 2 == n / 2 ? one - Lt[i] : 0.0f;
+        }
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            off[i] = (r + i) / w != n / w && (r + i) / (2 * w) == n / (2 * w) ? -Lt[i] : 0.0f;
-        const floatx4 z = {};
-        const floatx4 Y = Tile<false>::mm(off, Tn, z);               // -L_off T
-        const floatx4 t = Tile<false>::mm(Y, Tt, Tt);                // T^T - (L_off T)^T T^T
-        if (BOTH || w < 8) Tn = Tile<false>::mm(Tt, Y, Tn);
-        Tt = t;
+        for (int w = 2; w < 16; w *= 2) {
+            floatx4 off;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                off[i] = (r + i) / w != n / w && (r + i) / (2 * w) == n / (2 * w) ? -Lt[i] : 0.0f;
+            const floatx4 z = {};
+            const floatx4 Y = Tile<false>::mm(off, Tn, z);          // -L_off T
+            const floatx4 t = Tile<false>::mm(Y, Tt, Tt);           // T^T - (L_off T)^T T^T
+            if (BOTH || w < 8) Tn = Tile<false>::mm(Tt, Y, Tn);
+            Tt = t;
+        }
     }
 }
 

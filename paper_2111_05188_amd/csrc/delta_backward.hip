@@ -49,15 +49,16 @@ struct Back {
         __attribute__((aligned(16))) float turn[D * TLD];
         __attribute__((aligned(16))) val m[NP][4][64];      // T, T^T, P, P^T; then the products with K, Q, K
         __attribute__((aligned(16))) PieceRows rows[NP];
-        double cum[NP][16];
+        // y.dy, v.dv, dR.u of the waves' columns
+        __attribute__((aligned(16))) float sums[G][3][NW];
+        double cum[2 * NP][16];
         float g[G], beta[G], shut[G], idle[G];              // 1 - sigmoid(r), 1 - beta
         float x[G], dbeta[G];
-        float sums[NW][G];                                  // y.dy - v.dv of a wave's columns
-        float dots[NW][G][2];                               // q^.dq^, k^.dk^ of a wave's columns
         float ends[NW];                                     // <G, S> of a wave's columns
         int odd[2];
     };
     static_assert(16 * LD * sizeof(E) <= D * TLD * sizeof(float), "rows past dR's end");
+    static_assert(sizeof(PieceRows) % 16 == 0 && NP * sizeof(PieceRows) <= sizeof(Shared::dR), "P's rows");
     static_assert(sizeof(Shared) <= LDS_LIMIT, "LDS");
 
     // U and dR: two planes of bf16, or one of fp32
@@ -104,8 +105,8 @@ struct Back {
         }
     }
 
-    // The writes U of a piece (kept where OUT), and the state after it, on columns
-    // 16w..; x: its rows' parts of y.dy.
+    // The writes U of a piece (kept where OUT, with the rows' parts of y.dy), and the
+    // state after it, on columns 16w...
     template <bool MASK, bool OUT>
     static __device__ __forceinline__ floatx4 forward(Shared &sh, int s, int count, bool ends, int p, int w, int lane,
                                                       floatx4 *S)
@@ -113,7 +114,7 @@ struct Back {
         lane = fresh(lane);
         const int r = 4 * (lane >> 4);
         const PieceRows &rows = sh.rows[p];
-        floatx4 ks = {}, qs = {}, U = {}, R, W, x = {};
+        floatx4 ks = {}, qs = {}, U = {}, R, W;
 #pragma unroll
         for (int kt = 0; kt < KT; kt += 2) {
             const val x0 = TL::split(S[kt]), x1 = TL::split(S[kt + 1]);
@@ -139,7 +140,10 @@ struct Back {
             o = TL::mm(sh.m[p][3][lane], TL::split(U), o);
             const floatx4 dy = TL::wide(along_col<BF, LD, MASK>(sh.dy, s, count, w, lane));
 #pragma unroll
-            for (int i = 0; i < 4; ++i) x[i] = !MASK || r + i < count ? o[i] * dy[i] : 0.0f;
+            for (int i = 0; i < 4; ++i) {
+                const float t = row_sum(o[i] * dy[i]);
+                if ((lane & 15) == 0 && (!MASK || r + i < count)) sh.sums[s + r + i][0][w] = t;
+            }
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i) W[i] = !MASK || r + i < count ? U[i] * au[i] : 0.0f;
@@ -149,13 +153,13 @@ struct Back {
             S[kt] = TL::mm(along_col<BF, LD, MASK>(sh.k, s, count, kt, lane), y, S[kt] * rows.total);
             if (ends) S[kt] = floatx4{};
         }
-        return x;
+        return U;
     }
 
     // dR and dV of a piece, and the gradient of the state before it
     template <bool MASK>
     static __device__ __forceinline__ void backward(Shared &sh, int s, int count, int p, int w, int lane, floatx4 *Gs,
-                                                    floatx4 x)
+                                                    floatx4 U)
     {
         lane = fresh(lane);
         const int r = 4 * (lane >> 4), col = 16 * w + (lane & 15);
@@ -179,11 +183,14 @@ struct Back {
             A[i] = dyw[i] * aq[i];
             B[i] = !MASK || r + i < count ? -(dR[i] * ak[i]) : 0.0f;
             E *v = sh.v + (s + r + i) * LD + col;
-            const float dv = be[i] * dR[i], t = row_sum(x[i] - (float)*v * dv);
+            const float dv = be[i] * dR[i], t = row_sum((float)*v * dv), u = row_sum(dR[i] * U[i]);
             if (!MASK || r + i < count) {
                 put(sh.dR, s + r + i, col, d, i);
                 *v = (E)dv;
-                if ((lane & 15) == 0) sh.sums[w][s + r + i] = t;
+                if ((lane & 15) == 0) {
+                    sh.sums[s + r + i][1][w] = t;
+                    sh.sums[s + r + i][2][w] = u;
+                }
             }
         }
         const val a = TL::split(A), b = TL::split(B);
@@ -194,38 +201,53 @@ struct Back {
         }
     }
 
-    // the gradients of a piece's triangles, as first operands (one wave)
-    static __device__ __forceinline__ void triangles(Shared &sh, int s, int count, int p, int lane)
+    // The gradients of a piece's triangles, as first operands: P's (half 0) and L's
+    // (half 1), a wave each.
+    static __device__ __forceinline__ void triangles(Shared &sh, int s, int count, int p, int half, int lane)
     {
         lane = fresh(lane);
         const int n = lane & 15, r = 4 * (lane >> 4);
         const PieceRows &rows = sh.rows[p];
-        floatx4 yu = {}, uy = {}, ru = {}, ur = {};
+        floatx4 a = {}, b = {}, down, up;
+        if (half == 0) {
 #pragma unroll
-        for (int vt = 0; vt < KT; vt += 2) {
-            const auto y = along_row<BF, LD>(sh.dy, s, vt, lane), y1 = along_row<BF, LD>(sh.dy, s, vt + 1, lane);
-            const pair u = get(sh.U, s, vt, lane), d = get(sh.dR, s, vt, lane);
-            const pair u1 = get(sh.U, s, vt + 1, lane), d1 = get(sh.dR, s, vt + 1, lane);
-            yu = TL::mm2_out(y, y1, u, u1, yu);
-            uy = TL::mm2_out(u, u1, y, y1, uy);
-            ru = TL::mm2_out(d, d1, u, u1, ru);
-            ur = TL::mm2_out(u, u1, d, d1, ur);
+            for (int vt = 0; vt < KT; vt += 2) {
+                const auto y = along_row<BF, LD>(sh.dy, s, vt, lane), y1 = along_row<BF, LD>(sh.dy, s, vt + 1, lane);
+                const pair u = get(sh.U, s, vt, lane), u1 = get(sh.U, s, vt + 1, lane);
+                a = TL::mm2_out(y, y1, u, u1, a);
+                b = TL::mm2_out(u, u1, y, y1, b);
+            }
+        } else {
+#pragma unroll
+            for (int vt = 0; vt < KT; vt += 2) {
+                const pair u = get(sh.U, s, vt, lane), d = get(sh.dR, s, vt, lane);
+                const pair u1 = get(sh.U, s, vt + 1, lane), d1 = get(sh.dR, s, vt + 1, lane);
+                a = TL::mm2_out(d, d1, u, u1, a);
+                b = TL::mm2_out(u, u1, d, d1, b);
+            }
         }
-        floatx4 down, up, mq, mk, mm;
         piece_decays(sh.cum[p], count, lane, down, up);
+        floatx4 x, y;
+        const floatx4 rk = *(const floatx4 *)(rows.rk + r), rq = *(const floatx4 *)(rows.rq + r);
+        const floatx4 be = *(const floatx4 *)(rows.beta + r);
+        const float ben = rows.beta[n];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const bool below = r + i >= n && r + i < count, above = r + i <= n && n < count;
-            mq[i] = above ? uy[i] * up[i] * rows.rk[r + i] : 0.0f;
-            mk[i] = below ? yu[i] * down[i] * rows.rq[r + i] : 0.0f;
-            mm[i] = r + i == n ? 0.0f
-                    : below ? -(ru[i] * down[i] * rows.beta[r + i] * rows.rk[r + i])
-                    : above ? -(ur[i] * up[i] * rows.beta[n] * rows.rk[r + i]) : 0.0f;
-            if (r + i == n && n < count) sh.dbeta[s + n] = ru[i];
+            if (half == 0) {
+                x[i] = above ? b[i] * up[i] * rk[i] : 0.0f;
+                y[i] = below ? a[i] * down[i] * rq[i] : 0.0f;
+            } else {
+                x[i] = r + i == n ? 0.0f
+                       : below ? -(a[i] * down[i] * be[i] * rk[i]) : above ? -(b[i] * up[i] * ben * rk[i]) : 0.0f;
+            }
         }
-        *(pair *)&sh.m[p][0][lane] = TL::part(mq);
-        *(pair *)&sh.m[p][1][lane] = TL::part(mk);
-        *(pair *)&sh.m[p][2][lane] = TL::part(mm);
+        if (half == 0) {
+            *(pair *)&sh.m[p][0][lane] = TL::part(x);
+            *(pair *)&sh.m[p][1][lane] = TL::part(y);
+        } else {
+            *(pair *)&sh.m[p][2][lane] = TL::part(x);
+        }
     }
 
     // Rows of a piece times a transposed state, on columns 16w.. of the keys.
@@ -249,13 +271,23 @@ struct Back {
         return c;
     }
 
-    // the triangles' part, and the products that the unit rows' gradients need
+    // sum of a row's parts of the waves
+    static __device__ __forceinline__ float total(const float *parts)
+    {
+        float x = 0.0f;
+#pragma unroll
+        for (int j = 0; j < NW; ++j) x += parts[j];
+        return x;
+    }
+
+    // The triangles' part, then x rq (dq^ - q^ (q^.dq^)) in place of q, and the same of
+    // k, with q^.dq^ = y.dy and k^.dk^ = 2 dR.u - v.dv.
     template <bool MASK>
-    static __device__ __forceinline__ void add_triangles(Shared &sh, int s, int count, int p, int w, int lane,
-                                                         floatx4 &dq, floatx4 &dk)
+    static __device__ __forceinline__ void finish(Shared &sh, int s, int count, int p, int w, int lane, floatx4 dq,
+                                                  floatx4 dk)
     {
         lane = fresh(lane);
-        const int r = 4 * (lane >> 4);
+        const int r = 4 * (lane >> 4), col = 16 * w + (lane & 15);
         const PieceRows &rows = sh.rows[p];
         const auto qc = along_col<BF, LD, MASK>(sh.q, s, count, w, lane);
         const auto kc = along_col<BF, LD, MASK>(sh.k, s, count, w, lane);
@@ -264,40 +296,14 @@ struct Back {
         a = TL::mm_out(*(const pair *)&sh.m[p][0][lane], kc, a);
         b = TL::mm_out(*(const pair *)&sh.m[p][1][lane], qc, b);
         b = TL::mm_out(*(const pair *)&sh.m[p][2][lane], kc, b);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            dq[i] += a[i];
-            dk[i] += b[i];
-            const float x = row_sum(dq[i] * qw[i] * rows.rq[r + i]);
-            const float y = row_sum(dk[i] * kw[i] * rows.rk[r + i]);
-            if ((lane & 15) == 0 && (!MASK || r + i < count)) {
-                sh.dots[w][s + r + i][0] = x;
-                sh.dots[w][s + r + i][1] = y;
-            }
-        }
-    }
-
-    // x rq (dq^ - q^ (q^.dq^)) in place of q, and the same of k
-    template <bool MASK>
-    static __device__ __forceinline__ void finish(Shared &sh, int s, int count, int p, int w, int lane, floatx4 dq,
-                                                  floatx4 dk)
-    {
-        lane = fresh(lane);
-        const int r = 4 * (lane >> 4), col = 16 * w + (lane & 15);
-        const PieceRows &rows = sh.rows[p];
+        const floatx4 rq = *(const floatx4 *)(rows.rq + r), rk = *(const floatx4 *)(rows.rk + r);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             if (MASK && r + i >= count) continue;
-            float x = 0.0f, y = 0.0f;
-#pragma unroll
-            for (int j = 0; j < NW; ++j) {
-                x += sh.dots[j][s + r + i][0];
-                y += sh.dots[j][s + r + i][1];
-            }
-            E *q = sh.q + (s + r + i) * LD + col, *k = sh.k + (s + r + i) * LD + col;
-            const float rq = rows.rq[r + i], rk = rows.rk[r + i];
-            *q = (E)(rq * (dq[i] - (float)*q * rq * x));
-            *k = (E)(rk * (dk[i] - (float)*k * rk * y));
+            const float (*t)[NW] = sh.sums[s + r + i];
+            const float yd = total(t[0]), kd = 2.0f * total(t[2]) - total(t[1]);
+            sh.q[(s + r + i) * LD + col] = (E)(rq[i] * (dq[i] + a[i] - qw[i] * rq[i] * yd));
+            sh.k[(s + r + i) * LD + col] = (E)(rk[i] * (dk[i] + b[i] - kw[i] * rk[i] * kd));
         }
     }
 };
@@ -342,7 +348,7 @@ __global__ __launch_bounds__(4 * D, 2) void delta_bwd_kernel(DeltaArgs a)
     // a group's rows, gates and kept state; the group before's are under way while one
     // is finished
     const int first = begin / G, last = (end - 1) / G;
-    floatx4 S[KT];
+    floatx4 S[KT], SK[D < 128 ? KT : 1];
     Part fq[RW::N], fk[RW::N], fv[RW::N], fy[RW::N];
     float fr = 0.0f, fb = 0.0f;
     uint8_t fd = 0;
@@ -354,6 +360,11 @@ __global__ __launch_bounds__(4 * D, 2) void delta_bwd_kernel(DeltaArgs a)
         for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
             for (int i = 0; i < 4; ++i) S[kt][i] = ((const TP_GLOBAL float *)from)[(16 * kt + i) * D];
+        if constexpr (D < 128) {
+            const float *turned = a.saved + (((int64_t)grp * gridDim.x + blockIdx.x) * D + col) * D + r4;
+#pragma unroll
+            for (int kt = 0; kt < KT; ++kt) SK[kt] = *(const TP_GLOBAL floatx4 *)(turned + 16 * kt);
+        }
     };
     auto fetch = [&](int grp) {
         const DeltaArgs &a = fresh_args();
@@ -376,7 +387,7 @@ __global__ __launch_bounds__(4 * D, 2) void delta_bwd_kernel(DeltaArgs a)
         const int count = len - t0 < G ? len - t0 : G, all = end - t0 < G ? end - t0 : G;
         if (count > 0) {
             typename BK::pair ST[NP][KT], GT[KT];
-            floatx4 dq[NP], dk[NP], xs[NP];
+            floatx4 dq[NP], dk[NP], U[NP];
             float odd = RW::odd(fq) + RW::odd(fk) + RW::odd(fv) + RW::odd(fy);
             workgroup_lds_barrier();                // (the group before is done with)
             const int tid = fresh(threadIdx.x);
@@ -403,17 +414,26 @@ __global__ __launch_bounds__(4 * D, 2) void delta_bwd_kernel(DeltaArgs a)
                 while (p-- > 0 && s < count) s = piece_end(s, count, ends, single);
                 return s;
             };
+            // T, then P of each piece, a wave each (P's has its rows where dR will be)
             auto prepare = [&](int s) {
-                if (w >= NP) return;
-                const int from = piece(s, w), to = from < count ? piece_end(from, count, ends, single) : from;
-                if (to == from) return;
-                floatx4 Tt, Tn, Pt, Pn;
-                piece_triangles<BF, D, LD, true>(sh.q, sh.k, sh.g, sh.beta, from, to - from, lane, sh.cum[w],
-                                                 &sh.rows[w], Tt, Tn, Pt, Pn);
-                sh.m[w][0][lane] = Tile<BF>::split(Tn);
-                sh.m[w][1][lane] = Tile<BF>::split(Tt);
-                sh.m[w][2][lane] = Tile<BF>::split(Pn);
-                sh.m[w][3][lane] = Tile<BF>::split(Pt);
+                for (int j = w; j < 2 * NP; j += NW) {
+                    const int p = j % NP, from = piece(s, p);
+                    if (from >= count) continue;
+                    const int c = piece_end(from, count, ends, single) - from;
+                    floatx4 Tt, Tn, Pt, Pn;
+                    if (j < NP) {
+                        piece_triangles<BF, D, LD, WANT_T, true>(sh.q, sh.k, sh.g, sh.beta, from, c, lane, sh.cum[j],
+                                                                 &sh.rows[j], Tt, Tn, Pt, Pn);
+                        sh.m[p][0][lane] = Tile<BF>::split(Tn);
+                        sh.m[p][1][lane] = Tile<BF>::split(Tt);
+                    } else {
+                        piece_triangles<BF, D, LD, WANT_P | WANT_PT, true>(sh.q, sh.k, sh.g, sh.beta, from, c, lane,
+                                                                           sh.cum[j], (PieceRows *)sh.dR + p, Tt, Tn,
+                                                                           Pt, Pn);
+                        sh.m[p][2][lane] = Tile<BF>::split(Pn);
+                        sh.m[p][3][lane] = Tile<BF>::split(Pt);
+                    }
+                }
             };
             int batches = 0;
             for (int s = 0; s < count; s = piece(s, NP)) ++batches;
@@ -448,11 +468,17 @@ __global__ __launch_bounds__(4 * D, 2) void delta_bwd_kernel(DeltaArgs a)
                 for (int p = 0; p < NP; ++p) {
                     const int c = at[p + 1] - at[p];
                     if (c == 0) continue;
-                    BK::transpose(sh, S, w, lane, ST[p]);
+                    // (the kept state's transpose comes from memory, where there is room for it)
+                    if (D < 128 && p == 0 && batch == 0) {
+#pragma unroll
+                        for (int kt = 0; kt < KT; ++kt) ST[p][kt] = Tile<BF>::part(SK[D < 128 ? kt : 0]);
+                    } else {
+                        BK::transpose(sh, S, w, lane, ST[p]);
+                    }
                     dq[p] = BK::times_dy(sh, at[p], lane, ST[p]);
                     workgroup_lds_barrier();
                     whole_or_part(c, [&](auto m) {
-                        xs[p] = BK::template forward<decltype(m)::value, true>(sh, at[p], c, done(p), p, w, lane, S);
+                        U[p] = BK::template forward<decltype(m)::value, true>(sh, at[p], c, done(p), p, w, lane, S);
                     });
                 }
                 if (batch == batches - 1) {
@@ -463,9 +489,7 @@ __global__ __launch_bounds__(4 * D, 2) void delta_bwd_kernel(DeltaArgs a)
                         for (int i = 0; i < 4; ++i) x += S[kt][i] * Gs[kt][i];
                     // (an episode that ends here leaves nothing to the next group)
                     if (ends >> (count - 1) & 1) x = 0.0f;
-                    x = row_sum(x);
-                    x += __shfl_xor(x, 16);
-                    x += __shfl_xor(x, 32);
+                    x = lanes_sum<64>(x);
                     if (lane == 0) sh.ends[w] = x;
                 }
                 // back: dR, U G^T of the gradients after the pieces, dR S^T
@@ -494,24 +518,16 @@ __global__ __launch_bounds__(4 * D, 2) void delta_bwd_kernel(DeltaArgs a)
                     if (p + 1 < NP && at[p + 2 < NP ? p + 2 : NP] > at[p + 1]) rest(p + 1 < NP ? p + 1 : p);
                     workgroup_lds_barrier();
                     whole_or_part(c, [&](auto m) {
-                        BK::template backward<decltype(m)::value>(sh, at[p], c, p, w, lane, Gs, xs[p]);
+                        BK::template backward<decltype(m)::value>(sh, at[p], c, p, w, lane, Gs, U[p]);
                     });
                 }
                 workgroup_lds_barrier();
                 rest(0);
                 if (batch == 0 && grp > first) fetch(grp - 1);
-                if (w < NP) {
-                    const int from = piece(s, w), to = from < count ? piece_end(from, count, ends, single) : from;
-                    if (to > from) BK::triangles(sh, from, to - from, w, lane);
-                }
-                workgroup_lds_barrier();
-#pragma unroll
-                for (int p = 0; p < NP; ++p) {
-                    const int c = at[p + 1] - at[p];
-                    if (c == 0) continue;
-                    whole_or_part(c, [&](auto m) {
-                        BK::template add_triangles<decltype(m)::value>(sh, at[p], c, p, w, lane, dq[p], dk[p]);
-                    });
+                for (int j = w; j < 2 * NP; j += NW) {
+                    const int from = piece(s, j % NP);
+                    if (from < count)
+                        BK::triangles(sh, from, piece_end(from, count, ends, single) - from, j % NP, j / NP, lane);
                 }
                 workgroup_lds_barrier();
 #pragma unroll
@@ -526,21 +542,26 @@ __global__ __launch_bounds__(4 * D, 2) void delta_bwd_kernel(DeltaArgs a)
             }
             // gates: lane t of the first wave has step t
             if (w == 0) {
-                float acc = 0.0f, on = 0.0f;
+                float on = 0.0f, x = 0.0f;
 #pragma unroll
                 for (int j = 0; j < NW; ++j) on += sh.ends[j];
                 if (lane < count) {
-                    float x = 0.0f;
-#pragma unroll
-                    for (int j = 0; j < NW; ++j) x += sh.sums[j][lane];
+                    const float (*t)[NW] = sh.sums[lane];
+                    x = BK::total(t[0]) - BK::total(t[1]);
                     sh.x[lane] = x;
+                    sh.dbeta[lane] = BK::total(t[2]) * sh.idle[lane];
                 }
                 wave_lds_fence();
                 // the last step of this step's episode within the group
                 const uint64_t m = lane < count ? ends >> lane : 0;
                 const int stop = m ? lane + __builtin_ctzll(m) : count - 1;
-                for (int c = 0; c < count; ++c) acc += c >= lane && c <= stop ? sh.x[c] : 0.0f;
-                wave_lds_fence();
+                float acc = 0.0f;
+                if (single) {               // (a NaN stays in its episode)
+                    for (int c = 0; c < count; ++c) acc += c >= lane && c <= stop ? sh.x[c] : 0.0f;
+                } else {                    // differences of sums from the first step, in 64 bits
+                    const double sum = wave_inclusive_scan((double)x);
+                    acc = (float)(__shfl(sum, stop) - sum + (double)x);
+                }
                 if (lane < count) {
                     if (!m) acc += on;
                     // the first step of an episode has no state to fade
@@ -548,7 +569,6 @@ __global__ __launch_bounds__(4 * D, 2) void delta_bwd_kernel(DeltaArgs a)
                     const float wg = acc * sh.g[lane];
                     lam += (double)wg;
                     sh.x[lane] = wg * sh.shut[lane];
-                    sh.dbeta[lane] = sh.dbeta[lane] * sh.idle[lane];
                 }
             }
             wave_lds_fence();
@@ -671,7 +691,7 @@ __global__ __launch_bounds__(4 * D, 2) void delta_bwd_map_kernel(DeltaArgs a)
                 const int from = piece(s, p);
                 if (from >= count) break;
                 floatx4 Tt, Tn, Pt, Pn;
-                piece_triangles<BF, D, LD, true>(q, k, sg, sbeta, from, piece_end(from, count, ends, single) - from,
+                piece_triangles<BF, D, LD, WANT_T | WANT_P, true>(q, k, sg, sbeta, from, piece_end(from, count, ends, single) - from,
                                                  lane, cum[p], &rows[p], Tt, Tn, Pt, Pn);
                 sT[p][lane] = TL::split(Tn);
                 sP[p][lane] = TL::split(Pn);
