@@ -192,7 +192,7 @@ __global__ __launch_bounds__(4 * D, D == 128 ? 2 : 3) void delta_fwd_kernel(Delt
                     if (from >= count) break;
                     floatx4 Tt, Tn, Pt, Pn;
                     piece_triangles<BF, D, LD, WANT_T | WANT_PT, false>(q, k, sg, sbeta, from,
-                                                      piece_end(from, count, ends, single) - from, lane, cum[p],
+                                                      piece_end(from, count, ends, single) - from, single, lane, cum[p],
                                                       &rows[p], Tt, Tn, Pt, Pn);
                     sT[p][lane] = Tile<BF>::split(Tt);
                     sP[p][lane] = Tile<BF>::part(Pt);

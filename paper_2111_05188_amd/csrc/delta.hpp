@@ -383,19 +383,17 @@ __device__ __forceinline__ float delta_sigmoid(float x) { return 1.0f / (1.0f + 
 
 __device__ __forceinline__ float delta_exp(float x) { return __builtin_amdgcn_exp2f(x * DELTA_LOG2E); }
 
-// Decays between the steps of a piece, in the layout of a result: down[i] =
-// G[4g+i][n] (rows after columns), up[i] = G[n][4g+i]; 0 elsewhere.  Sums of g
-// run in 64 bits, so that a closed gate does not blur the decays after it.
-__device__ __forceinline__ void piece_decays(const double *cum, int count, int lane, floatx4 &down, floatx4 &up)
+// Decays between the steps of a piece, in the layout of a result: fade[i] between
+// steps 4g+i and n, whichever is first.  Sums of g run in 64 bits, so that a closed
+// gate does not blur the decays after it.
+__device__ __forceinline__ floatx4 piece_decays(const double *cum, int lane)
 {
     const int n = lane & 15, r = 4 * (lane >> 4);
     const double cn = cum[n];
+    floatx4 fade;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const float e = (float)(cum[r + i] - cn);
-        down[i] = r + i >= n && r + i < count ? delta_exp(e) : 0.0f;
-        up[i] = r + i <= n && n < count ? delta_exp(-e) : 0.0f;
-    }
+    for (int i = 0; i < 4; ++i) fade[i] = delta_exp(-fabsf((float)(cum[r + i] - cn)));
+    return fade;
 }
 
 // Sums of the log-decays over a piece's steps, by its wave, in the wave's own LDS.
@@ -418,15 +416,16 @@ enum : int { WANT_T = 1, WANT_PT = 2, WANT_P = 4 };
 // K K^T and Q K^T tiles of a piece, the rows' lengths, T and P in both layouts (as
 // far as they are wanted).  L is nilpotent; its inverse grows from blocks of 1, 2, 4,
 // 8 on the diagonal: T <- T - T L_off T with the part of L that joins two blocks, so
-// no power of L is formed whose entries cancel.
+// no power of L is formed whose entries cancel.  Rows past the piece's end have
+// length 0 and no decay; one: they may hold a NaN, and only the first row counts.
 template <bool BF, int D, int LD, int WANT, bool BOTH, class E>
 __device__ __forceinline__ void piece_triangles(const E *q, const E *k, const float *g, const float *beta, int s,
-                                                int count, int lane, double *cum, PieceRows *rows,
+                                                int count, bool one, int lane, double *cum, PieceRows *rows,
                                                 floatx4 &Tt, floatx4 &Tn, floatx4 &Pt, floatx4 &Pn)
 {
     constexpr float EPS = 1e-6f;
     lane = fresh(lane);
-    const int n = lane & 15, r = 4 * (lane >> 4);
+    const int n = lane & 15, grp = lane >> 4, r = 4 * grp;
     floatx4 kk = {}, qq = {}, kq = {}, qk = {};
 #pragma unroll
     for (int kt = 0; kt < D / 16; kt += 2) {
@@ -437,67 +436,73 @@ __device__ __forceinline__ void piece_triangles(const E *q, const E *k, const fl
         if constexpr (WANT & WANT_P) qk = Tile<BF>::mm2(b0, b1, a0, a1, qk);
         if constexpr (WANT & WANT_PT) kq = Tile<BF>::mm2(a0, a1, b0, b1, kq);
     }
+    const float be = (WANT & WANT_T) && n < count ? beta[s + n] : 0.0f;
     const double c = piece_sums(g + s, count, lane, cum);
-    const double all = cum[count - 1];
-    // lengths from the diagonals
+    if (one) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-        if (r + i == n) {
-            rows->rk[n] = n < count ? rsqrtf(kk[i] + EPS) : 0.0f;
-            rows->rq[n] = n < count ? rsqrtf(qq[i] + EPS) : 0.0f;
-        }
-    floatx4 down, up;
-    piece_decays(cum, count, lane, down, up);
-    wave_lds_fence();
-    if constexpr (WANT & WANT_T) {
-        if (lane < 16) {
-            const float fade = n < count ? delta_exp((float)c) : 0.0f;
-            const float rest = n < count ? delta_exp((float)(all - c)) : 0.0f;
-            const float be = n < count ? beta[s + n] : 0.0f;
-            rows->fade[n] = fade;
-            rows->rest[n] = rest;
-            rows->beta[n] = be;
-            if (n == 0) rows->total = delta_exp((float)all);
-            const float rk = rows->rk[n];
-            rows->aq[n] = fade * rows->rq[n];
-            rows->ak[n] = be * fade * rk;
-            rows->au[n] = rest * rk;
+        for (int i = 0; i < 4; ++i) {
+            const bool it = r + i == 0 && n == 0;
+            kk[i] = it ? kk[i] : 0.0f;
+            qq[i] = it ? qq[i] : 0.0f;
+            kq[i] = it ? kq[i] : 0.0f;
+            qk[i] = it ? qk[i] : 0.0f;
         }
     }
+    // lengths from the diagonals: lane 16 (n/4) + n has row n's
+    if (grp == n >> 2) {
+        const float dk = n & 2 ? (n & 1 ? kk[3] : kk[2]) : (n & 1 ? kk[1] : kk[0]);
+        const float dq = n & 2 ? (n & 1 ? qq[3] : qq[2]) : (n & 1 ? qq[1] : qq[0]);
+        rows->rk[n] = n < count ? __builtin_amdgcn_rsqf(dk + EPS) : 0.0f;
+        rows->rq[n] = n < count ? __builtin_amdgcn_rsqf(dq + EPS) : 0.0f;
+        if constexpr (WANT & WANT_T) rows->beta[n] = be;
+    }
+    const floatx4 fade = piece_decays(cum, lane);
     wave_lds_fence();
     const float rkn = rows->rk[n], rqn = rows->rq[n];
     const floatx4 rkr = *(const floatx4 *)(rows->rk + r), rqr = *(const floatx4 *)(rows->rq + r);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        if constexpr (WANT & WANT_P) Pn[i] = r + i >= n && r + i < count ? qk[i] * rqr[i] * rkn * down[i] : 0.0f;
-        if constexpr (WANT & WANT_PT) Pt[i] = r + i <= n && n < count ? kq[i] * rkr[i] * rqn * up[i] : 0.0f;
-    }
     if constexpr (WANT & WANT_T) {
-        const float ben = rows->beta[n];
         const floatx4 ber = *(const floatx4 *)(rows->beta + r);
-        floatx4 Lt;
+        if (lane < 16) {
+            const double all = cum[15];
+            const float since = n < count ? delta_exp((float)c) : 0.0f;
+            const float rest = n < count ? delta_exp((float)(all - c)) : 0.0f;
+            rows->fade[n] = since;
+            rows->rest[n] = rest;
+            if (n == 0) rows->total = delta_exp((float)all);
+            rows->aq[n] = since * rqn;
+            rows->ak[n] = be * since * rkn;
+            rows->au[n] = rest * rkn;
+        }
+        const bool same4 = grp == n >> 2, same8 = grp >> 1 == n >> 3;
+        floatx4 Lt, off;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const float x = kk[i] * rkr[i] * rkn;
-            const float Ln = r + i > n && r + i < count ? x * ber[i] * down[i] : 0.0f;  // row r+i after column n
-            Lt[i] = r + i < n && n < count ? x * ben * up[i] : 0.0f;                    // transposed
+            const float x = kk[i] * rkr[i] * (rkn * fade[i]);
+            const float Ln = r + i > n ? x * ber[i] : 0.0f;     // row r+i after column n
+            Lt[i] = r + i < n ? x * be : 0.0f;                  // transposed
             // blocks of two: I - L inside them
-            const float one = r + i == n ? 1.0f : 0.0f;
-            Tn[i] = (r + i) / 2 == n / 2 ? one - Ln : 0.0f;
-            Tt[i] = (r + i) / 2 == n / 2 ? one - Lt[i] : 0.0f;
+            const float unit = r + i == n ? 1.0f : 0.0f;
+            const bool same2 = 2 * grp + i / 2 == n >> 1;
+            Tn[i] = same2 ? unit - Ln : 0.0f;
+            Tt[i] = same2 ? unit - Lt[i] : 0.0f;
+            off[i] = same4 && !same2 ? -Lt[i] : 0.0f;
         }
 #pragma unroll
         for (int w = 2; w < 16; w *= 2) {
-            floatx4 off;
+            if (w > 2)
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                off[i] = (r + i) / w != n / w && (r + i) / (2 * w) == n / (2 * w) ? -Lt[i] : 0.0f;
+                for (int i = 0; i < 4; ++i) off[i] = (w == 4 ? same8 && !same4 : !same8) ? -Lt[i] : 0.0f;
             const floatx4 z = {};
             const floatx4 Y = Tile<false>::mm(off, Tn, z);          // -L_off T
             const floatx4 t = Tile<false>::mm(Y, Tt, Tt);           // T^T - (L_off T)^T T^T
             if (BOTH || w < 8) Tn = Tile<false>::mm(Tt, Y, Tn);
             Tt = t;
         }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if constexpr (WANT & WANT_P) Pn[i] = r + i >= n ? qk[i] * rqr[i] * (rkn * fade[i]) : 0.0f;
+        if constexpr (WANT & WANT_PT) Pt[i] = r + i <= n ? kq[i] * rkr[i] * (rqn * fade[i]) : 0.0f;
     }
 }
 

@@ -40,11 +40,13 @@ struct Back {
     typedef Tile<BF> TL;
     typedef typename TL::val val;
     typedef typename TL::pair pair;
+    typedef typename TL::raw raw;
     static constexpr int LD = RW::LD, NW = RW::NW, TLD = TC + 4;
     static constexpr int PLANES = BF ? 2 : 1;
     struct Shared {
-        // rows read past a piece's end stay inside: what follows each array here
-        __attribute__((aligned(16))) E q[G * LD], k[G * LD], v[G * LD], dy[G * LD];
+        // Rows read past a piece's end stay inside, in what follows each array.  Where
+        // such rows are summed over (dy, q, k, times zeros) they are inputs again.
+        __attribute__((aligned(16))) E dy[G * LD], q[G * LD], k[G * LD], v[G * LD];
         __attribute__((aligned(16))) E U[PLANES * G * LD], dR[PLANES * G * LD];
         __attribute__((aligned(16))) float turn[D * TLD];
         __attribute__((aligned(16))) val m[NP][4][64];      // T, T^T, P, P^T; then the products with K, Q, K
@@ -105,100 +107,142 @@ struct Back {
         }
     }
 
+    // f(i) for the rows 4g + i that a piece has.  (ONE, here and below: a piece of one
+    // step, beside which there may be a NaN or an infinity.)
+    template <class F>
+    static __device__ __forceinline__ void each_row(int count, int r, F f)
+    {
+        if (count == 16) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) f(i);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (r + i < count) f(i);
+        }
+    }
+
     // The writes U of a piece (kept where OUT, with the rows' parts of y.dy), and the
     // state after it, on columns 16w...
-    template <bool MASK, bool OUT>
+    template <bool ONE, bool OUT>
     static __device__ __forceinline__ floatx4 forward(Shared &sh, int s, int count, bool ends, int p, int w, int lane,
                                                       floatx4 *S)
     {
         lane = fresh(lane);
         const int r = 4 * (lane >> 4);
         const PieceRows &rows = sh.rows[p];
+        // all that comes from LDS first: behind a write nothing is read ahead
+        raw kr[KT], qr[OUT ? KT : 1], kc[KT], dyc = {};
+        val P = {};
+#pragma unroll
+        for (int kt = 0; kt < KT; ++kt) {
+            kr[kt] = along_row<BF, LD>(sh.k, s, kt, lane);
+            if constexpr (OUT) qr[kt] = along_row<BF, LD>(sh.q, s, kt, lane);
+        }
+        const floatx4 vv = TL::wide(along_col<BF, LD, ONE>(sh.v, s, count, w, lane));
+        const floatx4 be = *(const floatx4 *)(rows.beta + r), ak = *(const floatx4 *)(rows.ak + r);
+        const floatx4 aq = *(const floatx4 *)(rows.aq + r), au = *(const floatx4 *)(rows.au + r);
+        const float total = rows.total;
+        const val Tt = sh.m[p][1][lane];
+        if constexpr (OUT) {
+            P = sh.m[p][3][lane];
+            dyc = along_col<BF, LD, ONE>(sh.dy, s, count, w, lane);
+        }
+#pragma unroll
+        for (int kt = 0; kt < KT; ++kt) kc[kt] = along_col<BF, LD, ONE>(sh.k, s, count, kt, lane);
         floatx4 ks = {}, qs = {}, U = {}, R, W;
 #pragma unroll
         for (int kt = 0; kt < KT; kt += 2) {
             const val x0 = TL::split(S[kt]), x1 = TL::split(S[kt + 1]);
-            ks = TL::mm2(along_row<BF, LD>(sh.k, s, kt, lane), along_row<BF, LD>(sh.k, s, kt + 1, lane), x0, x1, ks);
-            if constexpr (OUT)
-                qs = TL::mm2(along_row<BF, LD>(sh.q, s, kt, lane), along_row<BF, LD>(sh.q, s, kt + 1, lane), x0, x1,
-                             qs);
-        }
-        const floatx4 vv = TL::wide(along_col<BF, LD, MASK>(sh.v, s, count, w, lane));
-        const floatx4 be = *(const floatx4 *)(rows.beta + r), ak = *(const floatx4 *)(rows.ak + r);
-        const floatx4 aq = *(const floatx4 *)(rows.aq + r), au = *(const floatx4 *)(rows.au + r);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) R[i] = !MASK || r + i < count ? be[i] * vv[i] - ak[i] * ks[i] : 0.0f;
-        U = TL::mm(sh.m[p][1][lane], TL::split(R), U);
-        if constexpr (OUT) {
-            const pair u = TL::part(U);
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                if (!MASK || r + i < count) put(sh.U, s + r + i, 16 * w + (lane & 15), u, i);
-            floatx4 o;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) o[i] = aq[i] * qs[i];
-            o = TL::mm(sh.m[p][3][lane], TL::split(U), o);
-            const floatx4 dy = TL::wide(along_col<BF, LD, MASK>(sh.dy, s, count, w, lane));
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float t = row_sum(o[i] * dy[i]);
-                if ((lane & 15) == 0 && (!MASK || r + i < count)) sh.sums[s + r + i][0][w] = t;
-            }
+            ks = TL::mm2(kr[kt], kr[kt + 1], x0, x1, ks);
+            if constexpr (OUT) qs = TL::mm2(qr[kt], qr[kt + 1], x0, x1, qs);
         }
 #pragma unroll
-        for (int i = 0; i < 4; ++i) W[i] = !MASK || r + i < count ? U[i] * au[i] : 0.0f;
+        for (int i = 0; i < 4; ++i) R[i] = r + i < count ? be[i] * vv[i] - ak[i] * ks[i] : 0.0f;
+        U = TL::mm(Tt, TL::split(R), U);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) W[i] = r + i < count ? U[i] * au[i] : 0.0f;
         const val y = TL::split(W);
 #pragma unroll
         for (int kt = 0; kt < KT; ++kt) {
-            S[kt] = TL::mm(along_col<BF, LD, MASK>(sh.k, s, count, kt, lane), y, S[kt] * rows.total);
+            S[kt] = TL::mm(kc[kt], y, S[kt] * total);
             if (ends) S[kt] = floatx4{};
+        }
+        if constexpr (OUT) {
+            const pair u = TL::part(U);
+            floatx4 o, t;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) o[i] = aq[i] * qs[i];
+            o = TL::mm(P, TL::split(U), o);
+            const floatx4 dy = TL::wide(dyc);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) t[i] = row_sum(o[i] * dy[i]);
+            each_row(count, r, [&](int i) {
+                put(sh.U, s + r + i, 16 * w + (lane & 15), u, i);
+                if ((lane & 15) == 0) sh.sums[s + r + i][0][w] = t[i];
+            });
         }
         return U;
     }
 
     // dR and dV of a piece, and the gradient of the state before it
-    template <bool MASK>
+    template <bool ONE>
     static __device__ __forceinline__ void backward(Shared &sh, int s, int count, int p, int w, int lane, floatx4 *Gs,
                                                     floatx4 U)
     {
         lane = fresh(lane);
         const int r = 4 * (lane >> 4), col = 16 * w + (lane & 15);
         const PieceRows &rows = sh.rows[p];
+        raw kr[KT], kc[KT], qc[KT];
+#pragma unroll
+        for (int kt = 0; kt < KT; ++kt) kr[kt] = along_row<BF, LD>(sh.k, s, kt, lane);
+        const raw dyc = along_col<BF, LD, ONE>(sh.dy, s, count, w, lane);
+        const floatx4 vw = TL::wide(along_col<BF, LD, ONE>(sh.v, s, count, w, lane));
+        const floatx4 be = *(const floatx4 *)(rows.beta + r), ak = *(const floatx4 *)(rows.ak + r);
+        const floatx4 aq = *(const floatx4 *)(rows.aq + r), au = *(const floatx4 *)(rows.au + r);
+        const float total = rows.total;
+        const val Pn = sh.m[p][2][lane], Tn = sh.m[p][0][lane];
+#pragma unroll
+        for (int kt = 0; kt < KT; ++kt) {
+            qc[kt] = along_col<BF, LD, ONE>(sh.q, s, count, kt, lane);
+            kc[kt] = along_col<BF, LD, ONE>(sh.k, s, count, kt, lane);
+        }
         floatx4 kg = {}, dU, dR = {}, A, B;
 #pragma unroll
         for (int kt = 0; kt < KT; kt += 2)
-            kg = TL::mm2(along_row<BF, LD>(sh.k, s, kt, lane), along_row<BF, LD>(sh.k, s, kt + 1, lane),
-                         TL::split(Gs[kt]), TL::split(Gs[kt + 1]), kg);
-        const auto dyc = along_col<BF, LD, MASK>(sh.dy, s, count, w, lane);
-        const floatx4 be = *(const floatx4 *)(rows.beta + r), ak = *(const floatx4 *)(rows.ak + r);
-        const floatx4 aq = *(const floatx4 *)(rows.aq + r), au = *(const floatx4 *)(rows.au + r);
+            kg = TL::mm2(kr[kt], kr[kt + 1], TL::split(Gs[kt]), TL::split(Gs[kt + 1]), kg);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) dU[i] = !MASK || r + i < count ? kg[i] * au[i] : 0.0f;
-        dU = TL::mm(sh.m[p][2][lane], dyc, dU);
-        dR = TL::mm(sh.m[p][0][lane], TL::split(dU), dR);
-        const pair d = TL::part(dR);
+        for (int i = 0; i < 4; ++i) dU[i] = r + i < count ? kg[i] * au[i] : 0.0f;
+        dU = TL::mm(Pn, dyc, dU);
+        dR = TL::mm(Tn, TL::split(dU), dR);
         const floatx4 dyw = TL::wide(dyc);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             A[i] = dyw[i] * aq[i];
-            B[i] = !MASK || r + i < count ? -(dR[i] * ak[i]) : 0.0f;
-            E *v = sh.v + (s + r + i) * LD + col;
-            const float dv = be[i] * dR[i], t = row_sum((float)*v * dv), u = row_sum(dR[i] * U[i]);
-            if (!MASK || r + i < count) {
-                put(sh.dR, s + r + i, col, d, i);
-                *v = (E)dv;
-                if ((lane & 15) == 0) {
-                    sh.sums[s + r + i][1][w] = t;
-                    sh.sums[s + r + i][2][w] = u;
-                }
-            }
+            B[i] = r + i < count ? -(dR[i] * ak[i]) : 0.0f;
         }
         const val a = TL::split(A), b = TL::split(B);
 #pragma unroll
         for (int kt = 0; kt < KT; ++kt) {
-            Gs[kt] = TL::mm(along_col<BF, LD, MASK>(sh.q, s, count, kt, lane), a, Gs[kt] * rows.total);
-            Gs[kt] = TL::mm(along_col<BF, LD, MASK>(sh.k, s, count, kt, lane), b, Gs[kt]);
+            Gs[kt] = TL::mm(qc[kt], a, Gs[kt] * total);
+            Gs[kt] = TL::mm(kc[kt], b, Gs[kt]);
         }
+        const pair d = TL::part(dR);
+        floatx4 dv, t, u;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            dv[i] = be[i] * dR[i];
+            t[i] = row_sum(vw[i] * dv[i]);
+            u[i] = row_sum(dR[i] * U[i]);
+        }
+        each_row(count, r, [&](int i) {
+            put(sh.dR, s + r + i, col, d, i);
+            sh.v[(s + r + i) * LD + col] = (E)dv[i];
+            if ((lane & 15) == 0) {
+                sh.sums[s + r + i][1][w] = t[i];
+                sh.sums[s + r + i][2][w] = u[i];
+            }
+        });
     }
 
     // The gradients of a piece's triangles, as first operands: P's (half 0) and L's
@@ -208,7 +252,7 @@ struct Back {
         lane = fresh(lane);
         const int n = lane & 15, r = 4 * (lane >> 4);
         const PieceRows &rows = sh.rows[p];
-        floatx4 a = {}, b = {}, down, up;
+        floatx4 a = {}, b = {};
         if (half == 0) {
 #pragma unroll
             for (int vt = 0; vt < KT; vt += 2) {
@@ -226,7 +270,7 @@ struct Back {
                 b = TL::mm2_out(u, u1, d, d1, b);
             }
         }
-        piece_decays(sh.cum[p], count, lane, down, up);
+        const floatx4 fade = piece_decays(sh.cum[p], lane);
         floatx4 x, y;
         const floatx4 rk = *(const floatx4 *)(rows.rk + r), rq = *(const floatx4 *)(rows.rq + r);
         const floatx4 be = *(const floatx4 *)(rows.beta + r);
@@ -235,11 +279,11 @@ struct Back {
         for (int i = 0; i < 4; ++i) {
             const bool below = r + i >= n && r + i < count, above = r + i <= n && n < count;
             if (half == 0) {
-                x[i] = above ? b[i] * up[i] * rk[i] : 0.0f;
-                y[i] = below ? a[i] * down[i] * rq[i] : 0.0f;
+                x[i] = above ? b[i] * fade[i] * rk[i] : 0.0f;
+                y[i] = below ? a[i] * fade[i] * rq[i] : 0.0f;
             } else {
                 x[i] = r + i == n ? 0.0f
-                       : below ? -(a[i] * down[i] * be[i] * rk[i]) : above ? -(b[i] * up[i] * ben * rk[i]) : 0.0f;
+                       : below ? -(a[i] * fade[i] * be[i] * rk[i]) : above ? -(b[i] * fade[i] * ben * rk[i]) : 0.0f;
             }
         }
         if (half == 0) {
@@ -282,37 +326,40 @@ struct Back {
 
     // The triangles' part, then x rq (dq^ - q^ (q^.dq^)) in place of q, and the same of
     // k, with q^.dq^ = y.dy and k^.dk^ = 2 dR.u - v.dv.
-    template <bool MASK>
+    template <bool ONE>
     static __device__ __forceinline__ void finish(Shared &sh, int s, int count, int p, int w, int lane, floatx4 dq,
                                                   floatx4 dk)
     {
         lane = fresh(lane);
         const int r = 4 * (lane >> 4), col = 16 * w + (lane & 15);
         const PieceRows &rows = sh.rows[p];
-        const auto qc = along_col<BF, LD, MASK>(sh.q, s, count, w, lane);
-        const auto kc = along_col<BF, LD, MASK>(sh.k, s, count, w, lane);
+        const auto qc = along_col<BF, LD, ONE>(sh.q, s, count, w, lane);
+        const auto kc = along_col<BF, LD, ONE>(sh.k, s, count, w, lane);
         const floatx4 qw = TL::wide(qc), kw = TL::wide(kc);
         floatx4 a = {}, b = {};
         a = TL::mm_out(*(const pair *)&sh.m[p][0][lane], kc, a);
         b = TL::mm_out(*(const pair *)&sh.m[p][1][lane], qc, b);
         b = TL::mm_out(*(const pair *)&sh.m[p][2][lane], kc, b);
         const floatx4 rq = *(const floatx4 *)(rows.rq + r), rk = *(const floatx4 *)(rows.rk + r);
+        floatx4 yd, kd;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            if (MASK && r + i >= count) continue;
-            const float (*t)[NW] = sh.sums[s + r + i];
-            const float yd = total(t[0]), kd = 2.0f * total(t[2]) - total(t[1]);
-            sh.q[(s + r + i) * LD + col] = (E)(rq[i] * (dq[i] + a[i] - qw[i] * rq[i] * yd));
-            sh.k[(s + r + i) * LD + col] = (E)(rk[i] * (dk[i] + b[i] - kw[i] * rk[i] * kd));
+        for (int i = 0; i < 4; ++i) {           // (rows past the group's are not there)
+            const float (*t)[NW] = sh.sums[s + r + i < G ? s + r + i : G - 1];
+            yd[i] = total(t[0]);
+            kd[i] = 2.0f * total(t[2]) - total(t[1]);
         }
+        each_row(count, r, [&](int i) {
+            sh.q[(s + r + i) * LD + col] = (E)(rq[i] * (dq[i] + a[i] - qw[i] * rq[i] * yd[i]));
+            sh.k[(s + r + i) * LD + col] = (E)(rk[i] * (dk[i] + b[i] - kw[i] * rk[i] * kd[i]));
+        });
     }
 };
 
 template <class F>
-__device__ __forceinline__ void whole_or_part(int count, F f)
+__device__ __forceinline__ void pieces_of(bool one, F f)
 {
-    if (count == 16) f(std::integral_constant<bool, false>{});
-    else f(std::integral_constant<bool, true>{});
+    if (one) f(std::integral_constant<bool, true>{});
+    else f(std::integral_constant<bool, false>{});
 }
 
 template <bool BF, int D>
@@ -422,12 +469,12 @@ __global__ __launch_bounds__(4 * D, 2) void delta_bwd_kernel(DeltaArgs a)
                     const int c = piece_end(from, count, ends, single) - from;
                     floatx4 Tt, Tn, Pt, Pn;
                     if (j < NP) {
-                        piece_triangles<BF, D, LD, WANT_T, true>(sh.q, sh.k, sh.g, sh.beta, from, c, lane, sh.cum[j],
-                                                                 &sh.rows[j], Tt, Tn, Pt, Pn);
+                        piece_triangles<BF, D, LD, WANT_T, true>(sh.q, sh.k, sh.g, sh.beta, from, c, single, lane,
+                                                                sh.cum[j],                                                                 &sh.rows[j], Tt, Tn, Pt, Pn);
                         sh.m[p][0][lane] = Tile<BF>::split(Tn);
                         sh.m[p][1][lane] = Tile<BF>::split(Tt);
                     } else {
-                        piece_triangles<BF, D, LD, WANT_P | WANT_PT, true>(sh.q, sh.k, sh.g, sh.beta, from, c, lane,
+                        piece_triangles<BF, D, LD, WANT_P | WANT_PT, true>(sh.q, sh.k, sh.g, sh.beta, from, c, single, lane,
                                                                            sh.cum[j], (PieceRows *)sh.dR + p, Tt, Tn,
                                                                            Pt, Pn);
                         sh.m[p][2][lane] = Tile<BF>::split(Pn);
@@ -477,7 +524,7 @@ __global__ __launch_bounds__(4 * D, 2) void delta_bwd_kernel(DeltaArgs a)
                     }
                     dq[p] = BK::times_dy(sh, at[p], lane, ST[p]);
                     workgroup_lds_barrier();
-                    whole_or_part(c, [&](auto m) {
+                    pieces_of(single, [&](auto m) {
                         U[p] = BK::template forward<decltype(m)::value, true>(sh, at[p], c, done(p), p, w, lane, S);
                     });
                 }
@@ -517,7 +564,7 @@ __global__ __launch_bounds__(4 * D, 2) void delta_bwd_kernel(DeltaArgs a)
                     }
                     if (p + 1 < NP && at[p + 2 < NP ? p + 2 : NP] > at[p + 1]) rest(p + 1 < NP ? p + 1 : p);
                     workgroup_lds_barrier();
-                    whole_or_part(c, [&](auto m) {
+                    pieces_of(single, [&](auto m) {
                         BK::template backward<decltype(m)::value>(sh, at[p], c, p, w, lane, Gs, U[p]);
                     });
                 }
@@ -534,7 +581,7 @@ __global__ __launch_bounds__(4 * D, 2) void delta_bwd_kernel(DeltaArgs a)
                 for (int p = 0; p < NP; ++p) {
                     const int c = at[p + 1] - at[p];
                     if (c == 0) continue;
-                    whole_or_part(c, [&](auto m) {
+                    pieces_of(single, [&](auto m) {
                         BK::template finish<decltype(m)::value>(sh, at[p], c, p, w, lane, dq[p], dk[p]);
                     });
                 }
@@ -692,7 +739,7 @@ __global__ __launch_bounds__(4 * D, 2) void delta_bwd_map_kernel(DeltaArgs a)
                 if (from >= count) break;
                 floatx4 Tt, Tn, Pt, Pn;
                 piece_triangles<BF, D, LD, WANT_T | WANT_P, true>(q, k, sg, sbeta, from, piece_end(from, count, ends, single) - from,
-                                                 lane, cum[p], &rows[p], Tt, Tn, Pt, Pn);
+                                                 single, lane, cum[p], &rows[p], Tt, Tn, Pt, Pn);
                 sT[p][lane] = TL::split(Tn);
                 sP[p][lane] = TL::split(Pn);
             }
