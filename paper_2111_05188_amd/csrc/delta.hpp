@@ -43,6 +43,7 @@ template <> struct Tile<false> {
     typedef floatx4 raw;
     typedef floatx4 val;
     static constexpr int PAD = 4;               // elements after a row in LDS
+    template <bool NEAR = false>
     static __device__ __forceinline__ val split(floatx4 x) { return x; }
     static __device__ __forceinline__ floatx4 wide(raw x) { return x; }
     static __device__ __forceinline__ floatx4 mm(floatx4 a, floatx4 b, floatx4 c)
@@ -59,10 +60,15 @@ template <> struct Tile<false> {
     typedef floatx4 pair;
     static __device__ __forceinline__ pair part(floatx4 x) { return x; }
     static __device__ __forceinline__ floatx4 mm_out(val a, val b, floatx4 c) { return mm(a, b, c); }
-    static __device__ __forceinline__ floatx4 mm2_out(val a0, val a1, val b0, val b1, floatx4 c)
+    static __device__ __forceinline__ pair head(val x) { return x; }
+    static __device__ __forceinline__ raw eye(int lane)
     {
-        return mm2(a0, a1, b0, b1, c);
+        raw x;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = 4 * (lane >> 4) + i == (lane & 15) ? 1.0f : 0.0f;
+        return x;
     }
+    static __device__ __forceinline__ pair turned(pair x, raw eye) { return mm(x, eye, floatx4{}); }
 };
 
 template <> struct Tile<true> {
@@ -72,9 +78,11 @@ template <> struct Tile<true> {
         bf16x4 hi, mid, lo;
     };
     static constexpr int PAD = 8;
-    // The upper 8 bits of a significand, the next 8 and the last: nothing is lost.
+    // The upper 8 bits of a significand, the next 8 and the last: nothing is lost.  (NEAR:
+    // the second to nearest, where the first two are taken for a pair as well.)
     // (Rounding to the nearest, with the conversion instruction, takes as many
     // instructions and is slower: 390 x 4,096 x 4 x 64 forward 1.94 ms against 1.82.)
+    template <bool NEAR = false>
     static __device__ __forceinline__ val split(floatx4 x)
     {
         val v;
@@ -83,7 +91,7 @@ template <> struct Tile<true> {
         for (int i = 0; i < 4; ++i) {
             h[i] = __float_as_uint(x[i]);
             const float r = x[i] - __uint_as_float(h[i] & 0xFFFF0000u);
-            m[i] = __float_as_uint(r);
+            m[i] = __float_as_uint(r) + (NEAR ? 0x8000u : 0u);
             l[i] = __float_as_uint(r - __uint_as_float(m[i] & 0xFFFF0000u));
         }
         v.hi = upper(h);
@@ -157,21 +165,26 @@ template <> struct Tile<true> {
     {
         return go(a.hi, b.hi, go(a.mid, b.hi, go(a.hi, b.mid, c)));
     }
-    static __device__ __forceinline__ floatx4 mm2_out(raw a0, raw a1, pair b0, pair b1, floatx4 c)
+    static __device__ __forceinline__ floatx4 mm_out(raw a, pair b, floatx4 c) { return go(a, b.hi, go(a, b.mid, c)); }
+    static __device__ __forceinline__ pair head(val x) { return pair{x.hi, x.mid}; }
+    // The transposed tile: a product with the unit matrix, which loses nothing.
+    static __device__ __forceinline__ raw eye(int lane)
     {
-        c = go(join(a0, a1), join(b0.mid, b1.mid), c);
-        return go(join(a0, a1), join(b0.hi, b1.hi), c);
+        raw x;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = (__bf16)(4 * (lane >> 4) + i == (lane & 15) ? 1.0f : 0.0f);
+        return x;
     }
-    static __device__ __forceinline__ floatx4 mm2_out(pair a0, pair a1, raw b0, raw b1, floatx4 c)
+    static __device__ __forceinline__ pair turned(pair x, raw eye)
     {
-        c = go(join(a0.mid, a1.mid), join(b0, b1), c);
-        return go(join(a0.hi, a1.hi), join(b0, b1), c);
-    }
-    static __device__ __forceinline__ floatx4 mm2_out(pair a0, pair a1, pair b0, pair b1, floatx4 c)
-    {
-        c = go(join(a0.hi, a1.hi), join(b0.mid, b1.mid), c);
-        c = go(join(a0.mid, a1.mid), join(b0.hi, b1.hi), c);
-        return go(join(a0.hi, a1.hi), join(b0.hi, b1.hi), c);
+        const floatx4 h = go(x.hi, eye, floatx4{}), m = go(x.mid, eye, floatx4{});
+        uint32_t a[4], b[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            a[i] = __float_as_uint(h[i]);
+            b[i] = __float_as_uint(m[i]);
+        }
+        return pair{upper(a), upper(b)};
     }
     // products over 32
     static __device__ __forceinline__ floatx4 mm2(raw a0, raw a1, val b0, val b1, floatx4 c)

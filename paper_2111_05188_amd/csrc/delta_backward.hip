@@ -30,26 +30,25 @@ namespace {
 template <bool BF, int D>
 struct Back {
     static constexpr int G = DELTA_GROUP, KT = D / 16;
-    // pieces at a time: their states' two transposes stay in registers
+    // pieces at a time: the transposes of the states before them stay in registers
     static constexpr int NP = D == 128 ? 1 : 2;
-    // a transpose goes through LDS in parts of the values' columns where all of it
-    // does not fit beside the rows
-    static constexpr int TURNS = D == 128 && !BF ? 2 : 1, TC = D / TURNS;
+    // the waves' parts of dq^ and of dk^ go through LDS one after the other where it does
+    // not hold both beside the rows
+    static constexpr int TURNS = D == 128 || (!BF && D == 64) ? 2 : 1;
     typedef Rows<BF, D, G> RW;
     typedef typename RW::E E;
     typedef Tile<BF> TL;
     typedef typename TL::val val;
     typedef typename TL::pair pair;
     typedef typename TL::raw raw;
-    static constexpr int LD = RW::LD, NW = RW::NW, TLD = TC + 4;
-    static constexpr int PLANES = BF ? 2 : 1;
+    static constexpr int LD = RW::LD, NW = RW::NW;
+    static constexpr int HALF = KT + 1, TILES = 2 * HALF / TURNS;
     struct Shared {
         // Rows read past a piece's end stay inside, in what follows each array.  Where
         // such rows are summed over (dy, q, k, times zeros) they are inputs again.
         __attribute__((aligned(16))) E dy[G * LD], q[G * LD], k[G * LD], v[G * LD];
-        __attribute__((aligned(16))) E U[PLANES * G * LD], dR[PLANES * G * LD];
-        __attribute__((aligned(16))) float turn[D * TLD];
-        __attribute__((aligned(16))) val m[NP][4][64];      // T, T^T, P, P^T; then the products with K, Q, K
+        __attribute__((aligned(16))) floatx4 parts[TILES][NW][64];  // of the waves' columns
+        __attribute__((aligned(16))) val m[NP][4][64];      // T, T^T, P, P^T
         __attribute__((aligned(16))) PieceRows rows[NP];
         // y.dy, v.dv, dR.u of the waves' columns
         __attribute__((aligned(16))) float sums[G][3][NW];
@@ -59,53 +58,9 @@ struct Back {
         float ends[NW];                                     // <G, S> of a wave's columns
         int odd[2];
     };
-    static_assert(16 * LD * sizeof(E) <= D * TLD * sizeof(float), "rows past dR's end");
-    static_assert(sizeof(PieceRows) % 16 == 0 && NP * sizeof(PieceRows) <= sizeof(Shared::dR), "P's rows");
+    static_assert(16 * LD * sizeof(E) <= sizeof(Shared::parts), "rows past v's end");
+    static_assert(sizeof(PieceRows) % 16 == 0 && NP * sizeof(PieceRows) <= sizeof(Shared::parts), "P's rows");
     static_assert(sizeof(Shared) <= LDS_LIMIT, "LDS");
-
-    // U and dR: two planes of bf16, or one of fp32
-    static __device__ __forceinline__ void put(E *lds, int row, int col, pair x, int i)
-    {
-        if constexpr (BF) {
-            lds[row * LD + col] = x.hi[i];
-            lds[(G + row) * LD + col] = x.mid[i];
-        } else {
-            lds[row * LD + col] = x[i];
-        }
-    }
-    static __device__ __forceinline__ pair get(const E *lds, int s, int kt, int lane)
-    {
-        if constexpr (BF) {
-            pair x;
-            x.hi = along_row<BF, LD>(lds, s, kt, lane);
-            x.mid = along_row<BF, LD>(lds + G * LD, s, kt, lane);
-            return x;
-        } else {
-            return along_row<BF, LD>(lds, s, kt, lane);
-        }
-    }
-
-    // Columns 16w.. (of the values) of a state to columns 16w.. of its transpose.
-    // The buffer is free when all waves call; it is again after their next barrier.
-    static __device__ __forceinline__ void transpose(Shared &sh, const floatx4 *S, int w, int lane, pair *T)
-    {
-        lane = fresh(lane);
-        const int n = lane & 15, r = 4 * (lane >> 4);
-#pragma unroll
-        for (int p = 0; p < TURNS; ++p) {
-            if (p) workgroup_lds_barrier();
-            if (TURNS == 1 || w / (NW / TURNS) == p) {
-#pragma unroll
-                for (int kt = 0; kt < KT; ++kt)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) sh.turn[(16 * kt + r + i) * TLD + 16 * w + n - p * TC] = S[kt][i];
-            }
-            workgroup_lds_barrier();
-#pragma unroll
-            for (int vt = p * KT / TURNS; vt < (p + 1) * KT / TURNS; ++vt)
-                T[vt] = TL::part(*(const floatx4 *)(sh.turn + (16 * w + n) * TLD + 16 * vt + r - p * TC));
-        }
-    }
 
     // f(i) for the rows 4g + i that a piece has.  (ONE, here and below: a piece of one
     // step, beside which there may be a NaN or an infinity.)
@@ -122,11 +77,11 @@ struct Back {
         }
     }
 
-    // The writes U of a piece (kept where OUT, with the rows' parts of y.dy), and the
-    // state after it, on columns 16w...
+    // The writes U of a piece and the state after it, on columns 16w...  OUT: the rows'
+    // parts of y.dy too, and the transpose of the state before it.
     template <bool ONE, bool OUT>
     static __device__ __forceinline__ floatx4 forward(Shared &sh, int s, int count, bool ends, int p, int w, int lane,
-                                                      floatx4 *S)
+                                                      floatx4 *S, pair *ST)
     {
         lane = fresh(lane);
         const int r = 4 * (lane >> 4);
@@ -150,12 +105,17 @@ struct Back {
         }
 #pragma unroll
         for (int kt = 0; kt < KT; ++kt) kc[kt] = along_col<BF, LD, ONE>(sh.k, s, count, kt, lane);
+        const raw eye = TL::eye(lane);
         floatx4 ks = {}, qs = {}, U = {}, R, W;
 #pragma unroll
         for (int kt = 0; kt < KT; kt += 2) {
-            const val x0 = TL::split(S[kt]), x1 = TL::split(S[kt + 1]);
+            const val x0 = TL::template split<OUT>(S[kt]), x1 = TL::template split<OUT>(S[kt + 1]);
             ks = TL::mm2(kr[kt], kr[kt + 1], x0, x1, ks);
-            if constexpr (OUT) qs = TL::mm2(qr[kt], qr[kt + 1], x0, x1, qs);
+            if constexpr (OUT) {
+                qs = TL::mm2(qr[kt], qr[kt + 1], x0, x1, qs);
+                ST[kt] = TL::turned(TL::head(x0), eye);
+                ST[kt + 1] = TL::turned(TL::head(x1), eye);
+            }
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i) R[i] = r + i < count ? be[i] * vv[i] - ak[i] * ks[i] : 0.0f;
@@ -169,7 +129,6 @@ struct Back {
             if (ends) S[kt] = floatx4{};
         }
         if constexpr (OUT) {
-            const pair u = TL::part(U);
             floatx4 o, t;
 #pragma unroll
             for (int i = 0; i < 4; ++i) o[i] = aq[i] * qs[i];
@@ -178,24 +137,33 @@ struct Back {
 #pragma unroll
             for (int i = 0; i < 4; ++i) t[i] = row_sum(o[i] * dy[i]);
             each_row(count, r, [&](int i) {
-                put(sh.U, s + r + i, 16 * w + (lane & 15), u, i);
                 if ((lane & 15) == 0) sh.sums[s + r + i][0][w] = t[i];
             });
         }
         return U;
     }
 
-    // dR and dV of a piece, and the gradient of the state before it
+    // What the waves' columns give to the gradients of a piece's triangles and keys.
+    struct Mine {
+        raw dy;             // rows of dY, as first operand
+        pair U, dR;         // transposed, for either
+        floatx4 ak, au;
+    };
+
+    // dR and dV of a piece, and the gradient of the state before it; of the one after it
+    // the transpose.
     template <bool ONE>
-    static __device__ __forceinline__ void backward(Shared &sh, int s, int count, int p, int w, int lane, floatx4 *Gs,
-                                                    floatx4 U)
+    static __device__ __forceinline__ Mine backward(Shared &sh, int s, int count, int p, int w, int lane, floatx4 *Gs,
+                                                    floatx4 U, pair *GT)
     {
         lane = fresh(lane);
         const int r = 4 * (lane >> 4), col = 16 * w + (lane & 15);
         const PieceRows &rows = sh.rows[p];
+        Mine mine;
         raw kr[KT], kc[KT], qc[KT];
 #pragma unroll
         for (int kt = 0; kt < KT; ++kt) kr[kt] = along_row<BF, LD>(sh.k, s, kt, lane);
+        mine.dy = along_row<BF, LD>(sh.dy, s, w, lane);
         const raw dyc = along_col<BF, LD, ONE>(sh.dy, s, count, w, lane);
         const floatx4 vw = TL::wide(along_col<BF, LD, ONE>(sh.v, s, count, w, lane));
         const floatx4 be = *(const floatx4 *)(rows.beta + r), ak = *(const floatx4 *)(rows.ak + r);
@@ -207,10 +175,15 @@ struct Back {
             qc[kt] = along_col<BF, LD, ONE>(sh.q, s, count, kt, lane);
             kc[kt] = along_col<BF, LD, ONE>(sh.k, s, count, kt, lane);
         }
+        const raw eye = TL::eye(lane);
         floatx4 kg = {}, dU, dR = {}, A, B;
 #pragma unroll
-        for (int kt = 0; kt < KT; kt += 2)
-            kg = TL::mm2(kr[kt], kr[kt + 1], TL::split(Gs[kt]), TL::split(Gs[kt + 1]), kg);
+        for (int kt = 0; kt < KT; kt += 2) {
+            const val x0 = TL::template split<true>(Gs[kt]), x1 = TL::template split<true>(Gs[kt + 1]);
+            kg = TL::mm2(kr[kt], kr[kt + 1], x0, x1, kg);
+            GT[kt] = TL::turned(TL::head(x0), eye);
+            GT[kt + 1] = TL::turned(TL::head(x1), eye);
+        }
 #pragma unroll
         for (int i = 0; i < 4; ++i) dU[i] = r + i < count ? kg[i] * au[i] : 0.0f;
         dU = TL::mm(Pn, dyc, dU);
@@ -227,7 +200,6 @@ struct Back {
             Gs[kt] = TL::mm(qc[kt], a, Gs[kt] * total);
             Gs[kt] = TL::mm(kc[kt], b, Gs[kt]);
         }
-        const pair d = TL::part(dR);
         floatx4 dv, t, u;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -235,84 +207,51 @@ struct Back {
             t[i] = row_sum(vw[i] * dv[i]);
             u[i] = row_sum(dR[i] * U[i]);
         }
+        mine.U = TL::turned(TL::part(U), eye);
+        mine.dR = TL::turned(TL::part(dR), eye);
+        mine.ak = ak;
+        mine.au = au;
         each_row(count, r, [&](int i) {
-            put(sh.dR, s + r + i, col, d, i);
             sh.v[(s + r + i) * LD + col] = (E)dv[i];
             if ((lane & 15) == 0) {
                 sh.sums[s + r + i][1][w] = t[i];
                 sh.sums[s + r + i][2][w] = u[i];
             }
         });
+        return mine;
     }
 
-    // The gradients of a piece's triangles, as first operands: P's (half 0) and L's
-    // (half 1), a wave each.
-    static __device__ __forceinline__ void triangles(Shared &sh, int s, int count, int p, int half, int lane)
+    // A wave's part of dY S0^T for all keys, and of P's gradient (turn 0), or of
+    // rest rk U G1^T - beta gamma rk dR S0^T, and of L's (turn 1).
+    static __device__ __forceinline__ void give(Shared &sh, int turn, int w, int lane, const Mine &m, const pair *ST,
+                                                const pair *GT)
     {
         lane = fresh(lane);
-        const int n = lane & 15, r = 4 * (lane >> 4);
-        const PieceRows &rows = sh.rows[p];
-        floatx4 a = {}, b = {};
-        if (half == 0) {
+        const int first = TURNS == 1 ? turn * HALF : 0;
 #pragma unroll
-            for (int vt = 0; vt < KT; vt += 2) {
-                const auto y = along_row<BF, LD>(sh.dy, s, vt, lane), y1 = along_row<BF, LD>(sh.dy, s, vt + 1, lane);
-                const pair u = get(sh.U, s, vt, lane), u1 = get(sh.U, s, vt + 1, lane);
-                a = TL::mm2_out(y, y1, u, u1, a);
-                b = TL::mm2_out(u, u1, y, y1, b);
-            }
-        } else {
-#pragma unroll
-            for (int vt = 0; vt < KT; vt += 2) {
-                const pair u = get(sh.U, s, vt, lane), d = get(sh.dR, s, vt, lane);
-                const pair u1 = get(sh.U, s, vt + 1, lane), d1 = get(sh.dR, s, vt + 1, lane);
-                a = TL::mm2_out(d, d1, u, u1, a);
-                b = TL::mm2_out(u, u1, d, d1, b);
-            }
-        }
-        const floatx4 fade = piece_decays(sh.cum[p], lane);
-        floatx4 x, y;
-        const floatx4 rk = *(const floatx4 *)(rows.rk + r), rq = *(const floatx4 *)(rows.rq + r);
-        const floatx4 be = *(const floatx4 *)(rows.beta + r);
-        const float ben = rows.beta[n];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const bool below = r + i >= n && r + i < count, above = r + i <= n && n < count;
-            if (half == 0) {
-                x[i] = above ? b[i] * fade[i] * rk[i] : 0.0f;
-                y[i] = below ? a[i] * fade[i] * rq[i] : 0.0f;
+        for (int kt = 0; kt < KT; ++kt) {
+            floatx4 x = {}, y = {};
+            if (turn == 0) {
+                x = TL::mm_out(m.dy, ST[kt], x);
             } else {
-                x[i] = r + i == n ? 0.0f
-                       : below ? -(a[i] * fade[i] * be[i] * rk[i]) : above ? -(b[i] * fade[i] * ben * rk[i]) : 0.0f;
+                x = TL::mm_out(m.U, GT[kt], x);
+                y = TL::mm_out(m.dR, ST[kt], y);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) x[i] = m.au[i] * x[i] - m.ak[i] * y[i];
             }
+            sh.parts[first + kt][w][lane] = x;
         }
-        if (half == 0) {
-            *(pair *)&sh.m[p][0][lane] = TL::part(x);
-            *(pair *)&sh.m[p][1][lane] = TL::part(y);
-        } else {
-            *(pair *)&sh.m[p][2][lane] = TL::part(x);
-        }
+        floatx4 z = {};
+        sh.parts[first + KT][w][lane] = turn == 0 ? TL::mm_out(m.dy, m.U, z) : TL::mm_out(m.dR, m.U, z);
     }
 
-    // Rows of a piece times a transposed state, on columns 16w.. of the keys.
-    static __device__ __forceinline__ floatx4 times(const E *rows, int s, int lane, const pair *T)
+    // the sum of all waves' parts of a tile
+    static __device__ __forceinline__ floatx4 take(const Shared &sh, int tile, int lane)
     {
-        lane = fresh(lane);
-        floatx4 c = {};
+        floatx4 x = sh.parts[tile][0][lane];
 #pragma unroll
-        for (int vt = 0; vt < KT; vt += 2)
-            c = TL::mm2_out(get(rows, s, vt, lane), get(rows, s, vt + 1, lane), T[vt], T[vt + 1], c);
-        return c;
-    }
-    static __device__ __forceinline__ floatx4 times_dy(const Shared &sh, int s, int lane, const pair *T)
-    {
-        lane = fresh(lane);
-        floatx4 c = {};
-#pragma unroll
-        for (int vt = 0; vt < KT; vt += 2)
-            c = TL::mm2_out(along_row<BF, LD>(sh.dy, s, vt, lane), along_row<BF, LD>(sh.dy, s, vt + 1, lane), T[vt],
-                            T[vt + 1], c);
-        return c;
+        for (int j = 1; j < NW; ++j) x += sh.parts[tile][j][lane];
+        return x;
     }
 
     // sum of a row's parts of the waves
@@ -324,33 +263,60 @@ struct Back {
         return x;
     }
 
-    // The triangles' part, then x rq (dq^ - q^ (q^.dq^)) in place of q, and the same of
-    // k, with q^.dq^ = y.dy and k^.dk^ = 2 dR.u - v.dv.
-    template <bool ONE>
-    static __device__ __forceinline__ void finish(Shared &sh, int s, int count, int p, int w, int lane, floatx4 dq,
-                                                  floatx4 dk)
+    // What is summed of a piece: its keys' columns 16w.. (rows' lengths are in them or
+    // come with the decays) and a triangle's gradient, scaled by both rows' lengths.
+    struct Sums {
+        floatx4 dq, dk, M, E;
+    };
+    static __device__ __forceinline__ void collect(const Shared &sh, int turn, int w, int lane, Sums &t)
     {
         lane = fresh(lane);
-        const int r = 4 * (lane >> 4), col = 16 * w + (lane & 15);
+        const int first = TURNS == 1 ? turn * HALF : 0;
+        (turn == 0 ? t.dq : t.dk) = take(sh, first + w, lane);
+        (turn == 0 ? t.M : t.E) = take(sh, first + KT, lane);
+    }
+
+    // rq (dq^ - q^ (q^.dq^)) in place of q, and the same of k, with q^.dq^ = y.dy and
+    // k^.dk^ = 2 dR.u - v.dv.
+    template <bool ONE>
+    static __device__ __forceinline__ void finish(Shared &sh, int s, int count, int p, int w, int lane, Sums &t)
+    {
+        lane = fresh(lane);
+        const int n = lane & 15, r = 4 * (lane >> 4), col = 16 * w + n;
         const PieceRows &rows = sh.rows[p];
-        const auto qc = along_col<BF, LD, ONE>(sh.q, s, count, w, lane);
-        const auto kc = along_col<BF, LD, ONE>(sh.k, s, count, w, lane);
-        const floatx4 qw = TL::wide(qc), kw = TL::wide(kc);
-        floatx4 a = {}, b = {};
-        a = TL::mm_out(*(const pair *)&sh.m[p][0][lane], kc, a);
-        b = TL::mm_out(*(const pair *)&sh.m[p][1][lane], qc, b);
-        b = TL::mm_out(*(const pair *)&sh.m[p][2][lane], kc, b);
+        const raw qc = along_col<BF, LD, ONE>(sh.q, s, count, w, lane);
+        const raw kc = along_col<BF, LD, ONE>(sh.k, s, count, w, lane);
         const floatx4 rq = *(const floatx4 *)(rows.rq + r), rk = *(const floatx4 *)(rows.rk + r);
+        const floatx4 be = *(const floatx4 *)(rows.beta + r), aq = *(const floatx4 *)(rows.aq + r);
+        const float rkn = rows.rk[n];
         floatx4 yd, kd;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {           // (rows past the group's are not there)
-            const float (*t)[NW] = sh.sums[s + r + i < G ? s + r + i : G - 1];
-            yd[i] = total(t[0]);
-            kd[i] = 2.0f * total(t[2]) - total(t[1]);
+            const float (*x)[NW] = sh.sums[s + r + i < G ? s + r + i : G - 1];
+            yd[i] = total(x[0]);
+            kd[i] = 2.0f * total(x[2]) - total(x[1]);
         }
+        const floatx4 fade = piece_decays(sh.cum[p], lane);
+        floatx4 M, L;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float f = fade[i] * rkn;
+            M[i] = r + i >= n && r + i < count ? t.M[i] * f * rq[i] : 0.0f;
+            L[i] = r + i > n && r + i < count ? -(t.E[i] * f * be[i] * rk[i]) : 0.0f;
+        }
+        const raw eye = TL::eye(lane);
+        const pair m = TL::part(M), l = TL::part(L);
+        floatx4 a, b = t.dk;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) a[i] = aq[i] * t.dq[i];
+        b = TL::mm_out(m, qc, b);
+        b = TL::mm_out(l, kc, b);
+        a = TL::mm_out(TL::turned(m, eye), kc, a);
+        b = TL::mm_out(TL::turned(l, eye), kc, b);
+        const floatx4 qw = TL::wide(qc), kw = TL::wide(kc);
         each_row(count, r, [&](int i) {
-            sh.q[(s + r + i) * LD + col] = (E)(rq[i] * (dq[i] + a[i] - qw[i] * rq[i] * yd[i]));
-            sh.k[(s + r + i) * LD + col] = (E)(rk[i] * (dk[i] + b[i] - kw[i] * rk[i] * kd[i]));
+            sh.q[(s + r + i) * LD + col] = (E)(a[i] - qw[i] * rq[i] * rq[i] * yd[i]);
+            sh.k[(s + r + i) * LD + col] = (E)(b[i] - kw[i] * rk[i] * rk[i] * kd[i]);
         });
     }
 };
@@ -395,7 +361,7 @@ __global__ __launch_bounds__(4 * D, 2) void delta_bwd_kernel(DeltaArgs a)
     // a group's rows, gates and kept state; the group before's are under way while one
     // is finished
     const int first = begin / G, last = (end - 1) / G;
-    floatx4 S[KT], SK[D < 128 ? KT : 1];
+    floatx4 S[KT];
     Part fq[RW::N], fk[RW::N], fv[RW::N], fy[RW::N];
     float fr = 0.0f, fb = 0.0f;
     uint8_t fd = 0;
@@ -407,11 +373,6 @@ __global__ __launch_bounds__(4 * D, 2) void delta_bwd_kernel(DeltaArgs a)
         for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
             for (int i = 0; i < 4; ++i) S[kt][i] = ((const TP_GLOBAL float *)from)[(16 * kt + i) * D];
-        if constexpr (D < 128) {
-            const float *turned = a.saved + (((int64_t)grp * gridDim.x + blockIdx.x) * D + col) * D + r4;
-#pragma unroll
-            for (int kt = 0; kt < KT; ++kt) SK[kt] = *(const TP_GLOBAL floatx4 *)(turned + 16 * kt);
-        }
     };
     auto fetch = [&](int grp) {
         const DeltaArgs &a = fresh_args();
@@ -434,7 +395,7 @@ __global__ __launch_bounds__(4 * D, 2) void delta_bwd_kernel(DeltaArgs a)
         const int count = len - t0 < G ? len - t0 : G, all = end - t0 < G ? end - t0 : G;
         if (count > 0) {
             typename BK::pair ST[NP][KT], GT[KT];
-            floatx4 dq[NP], dk[NP], U[NP];
+            floatx4 U[NP];
             float odd = RW::odd(fq) + RW::odd(fk) + RW::odd(fv) + RW::odd(fy);
             workgroup_lds_barrier();                // (the group before is done with)
             const int tid = fresh(threadIdx.x);
@@ -461,7 +422,7 @@ __global__ __launch_bounds__(4 * D, 2) void delta_bwd_kernel(DeltaArgs a)
                 while (p-- > 0 && s < count) s = piece_end(s, count, ends, single);
                 return s;
             };
-            // T, then P of each piece, a wave each (P's has its rows where dR will be)
+            // T, then P of each piece, a wave each (P's has its rows where the parts will be)
             auto prepare = [&](int s) {
                 for (int j = w; j < 2 * NP; j += NW) {
                     const int p = j % NP, from = piece(s, p);
@@ -475,7 +436,7 @@ __global__ __launch_bounds__(4 * D, 2) void delta_bwd_kernel(DeltaArgs a)
                         sh.m[p][1][lane] = Tile<BF>::split(Tt);
                     } else {
                         piece_triangles<BF, D, LD, WANT_P | WANT_PT, true>(sh.q, sh.k, sh.g, sh.beta, from, c, single, lane,
-                                                                           sh.cum[j], (PieceRows *)sh.dR + p, Tt, Tn,
+                                                                           sh.cum[j], (PieceRows *)sh.parts + p, Tt, Tn,
                                                                            Pt, Pn);
                         sh.m[p][2][lane] = Tile<BF>::split(Pn);
                         sh.m[p][3][lane] = Tile<BF>::split(Pt);
@@ -486,7 +447,7 @@ __global__ __launch_bounds__(4 * D, 2) void delta_bwd_kernel(DeltaArgs a)
             for (int s = 0; s < count; s = piece(s, NP)) ++batches;
 #pragma unroll 1
             for (int batch = batches - 1; batch >= 0; --batch) {
-                const int lane = fresh(threadIdx.x & 63), r4 = 4 * (lane >> 4);
+                const int lane = fresh(threadIdx.x & 63);
                 // the state before this batch: from the kept one, over the batches before
                 // (more than one where episodes end)
                 if (batch != batches - 1) load_state(grp);
@@ -497,7 +458,8 @@ __global__ __launch_bounds__(4 * D, 2) void delta_bwd_kernel(DeltaArgs a)
                     workgroup_lds_barrier();
                     for (int p = 0, x = s; p < NP && x < count; ++p) {
                         const int e = piece_end(x, count, ends, single);
-                        BK::template forward<true, false>(sh, x, e - x, ends >> (e - 1) & 1, p, w, lane, S);
+                        BK::template forward<true, false>(sh, x, e - x, ends >> (e - 1) & 1, p, w, lane, S,
+                                                         (typename BK::pair *)nullptr);
                         x = e;
                     }
                     workgroup_lds_barrier();
@@ -510,22 +472,14 @@ __global__ __launch_bounds__(4 * D, 2) void delta_bwd_kernel(DeltaArgs a)
                     at[p + 1] = at[p] < count ? piece_end(at[p], count, ends, single) : at[p];
                 auto done = [&](int p) { return (bool)(ends >> (at[p + 1] - 1) & 1); };
                 prepare(s);
-                // forward: U, and dY S^T of the states before the pieces
+                workgroup_lds_barrier();
 #pragma unroll
                 for (int p = 0; p < NP; ++p) {
                     const int c = at[p + 1] - at[p];
                     if (c == 0) continue;
-                    // (the kept state's transpose comes from memory, where there is room for it)
-                    if (D < 128 && p == 0 && batch == 0) {
-#pragma unroll
-                        for (int kt = 0; kt < KT; ++kt) ST[p][kt] = Tile<BF>::part(SK[D < 128 ? kt : 0]);
-                    } else {
-                        BK::transpose(sh, S, w, lane, ST[p]);
-                    }
-                    dq[p] = BK::times_dy(sh, at[p], lane, ST[p]);
-                    workgroup_lds_barrier();
                     pieces_of(single, [&](auto m) {
-                        U[p] = BK::template forward<decltype(m)::value, true>(sh, at[p], c, done(p), p, w, lane, S);
+                        U[p] = BK::template forward<decltype(m)::value, true>(sh, at[p], c, done(p), p, w, lane, S,
+                                                                              ST[p]);
                     });
                 }
                 if (batch == batches - 1) {
@@ -539,50 +493,33 @@ __global__ __launch_bounds__(4 * D, 2) void delta_bwd_kernel(DeltaArgs a)
                     x = lanes_sum<64>(x);
                     if (lane == 0) sh.ends[w] = x;
                 }
-                // back: dR, U G^T of the gradients after the pieces, dR S^T
-                auto rest = [&](int p) {
-                    const floatx4 c = BK::times(sh.dR, at[p], lane, ST[p]);
-                    const PieceRows &rows = sh.rows[p];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        dq[p][i] *= rows.fade[r4 + i];
-                        dk[p][i] = dk[p][i] * rows.rest[r4 + i] - c[i] * rows.beta[r4 + i] * rows.fade[r4 + i];
-                    }
-                };
 #pragma unroll
                 for (int p = NP - 1; p >= 0; --p) {
                     const int c = at[p + 1] - at[p];
                     if (c == 0) continue;
-                    dk[p] = floatx4{};
                     if (done(p)) {
-                        workgroup_lds_barrier();
 #pragma unroll
                         for (int kt = 0; kt < KT; ++kt) Gs[kt] = floatx4{};
-                    } else {
-                        BK::transpose(sh, Gs, w, lane, GT);
-                        dk[p] = BK::times(sh.U, at[p], lane, GT);
                     }
-                    if (p + 1 < NP && at[p + 2 < NP ? p + 2 : NP] > at[p + 1]) rest(p + 1 < NP ? p + 1 : p);
-                    workgroup_lds_barrier();
+                    typename BK::Mine mine;
                     pieces_of(single, [&](auto m) {
-                        BK::template backward<decltype(m)::value>(sh, at[p], c, p, w, lane, Gs, U[p]);
+                        mine = BK::template backward<decltype(m)::value>(sh, at[p], c, p, w, lane, Gs, U[p], GT);
                     });
-                }
-                workgroup_lds_barrier();
-                rest(0);
-                if (batch == 0 && grp > first) fetch(grp - 1);
-                for (int j = w; j < 2 * NP; j += NW) {
-                    const int from = piece(s, j % NP);
-                    if (from < count)
-                        BK::triangles(sh, from, piece_end(from, count, ends, single) - from, j % NP, j / NP, lane);
-                }
-                workgroup_lds_barrier();
+                    // the waves' parts to the waves that have the keys' columns
+                    typename BK::Sums t;
+                    if (p + 1 < NP) workgroup_lds_barrier();
 #pragma unroll
-                for (int p = 0; p < NP; ++p) {
-                    const int c = at[p + 1] - at[p];
-                    if (c == 0) continue;
+                    for (int x = 0; x < 2; ++x) {
+                        BK::give(sh, x, w, lane, mine, ST[p], GT);
+                        if (x == 0 && BK::TURNS == 1) continue;
+                        if (x == 1 && p == 0 && batch == 0 && grp > first) fetch(grp - 1);
+                        workgroup_lds_barrier();
+                        if (BK::TURNS == 1) BK::collect(sh, 0, w, lane, t);
+                        BK::collect(sh, x, w, lane, t);
+                        if (x == 0) workgroup_lds_barrier();
+                    }
                     pieces_of(single, [&](auto m) {
-                        BK::template finish<decltype(m)::value>(sh, at[p], c, p, w, lane, dq[p], dk[p]);
+                        BK::template finish<decltype(m)::value>(sh, at[p], c, p, w, lane, t);
                     });
                 }
                 workgroup_lds_barrier();
