@@ -19,8 +19,8 @@ namespace {
 // one piece on the state's columns of this wave
 template <bool BF, int D, int LD, bool MASK, class E>
 __device__ __forceinline__ void run_piece(const E *q, const E *k, E *v, int s, int count, bool ends,
-                                          const PieceRows &rows, const typename Tile<BF>::val &Tt,
-                                          const typename Tile<BF>::pair &Pt, int w, int lane, floatx4 *S)
+                                          const PieceRows &rows, const floatx4 &Tt, const floatx4 &Pt, int w,
+                                          int lane, floatx4 *S)
 {
     typedef Tile<BF> TL;
     constexpr int KT = D / 16;
@@ -42,8 +42,8 @@ __device__ __forceinline__ void run_piece(const E *q, const E *k, E *v, int s, i
         R[i] = !MASK || r + i < count ? be[i] * vv[i] - ak[i] * ks[i] : 0.0f;
         o[i] = aq[i] * qs[i];
     }
-    U = TL::mm(Tt, TL::split(R), U);
-    o = TL::mm_out(Pt, TL::part(U), o);
+    U = Tile<false>::mm(Tt, R, U);
+    o = Tile<false>::mm(Pt, U, o);
 #pragma unroll
     for (int i = 0; i < 4; ++i)
         if (!MASK || r + i < count) v[(s + r + i) * LD + 16 * w + (lane & 15)] = (E)o[i];
@@ -64,7 +64,7 @@ __device__ __forceinline__ void run_piece(const E *q, const E *k, E *v, int s, i
 // what a piece does to the unit states (a value's columns are zero)
 template <bool BF, int D, int LD, bool MASK, class E>
 __device__ __forceinline__ void map_piece(const E *k, int s, int count, bool ends, const PieceRows &rows,
-                                          const typename Tile<BF>::val &Tt, int lane, floatx4 *S)
+                                          const floatx4 &Tt, int lane, floatx4 *S)
 {
     typedef Tile<BF> TL;
     constexpr int KT = D / 16;
@@ -77,7 +77,7 @@ __device__ __forceinline__ void map_piece(const E *k, int s, int count, bool end
                      TL::split(S[kt + 1]), ks);
 #pragma unroll
     for (int i = 0; i < 4; ++i) R[i] = !MASK || r + i < count ? -(rows.ak[r + i] * ks[i]) : 0.0f;
-    U = TL::mm(Tt, TL::split(R), U);
+    U = Tile<false>::mm(Tt, R, U);
 #pragma unroll
     for (int i = 0; i < 4; ++i) W[i] = !MASK || r + i < count ? U[i] * rows.au[r + i] : 0.0f;
     const auto x = TL::split(W);
@@ -97,8 +97,7 @@ __global__ __launch_bounds__(4 * D, D == 128 ? 2 : 3) void delta_fwd_kernel(Delt
     typedef typename RW::E E;
     constexpr int LD = RW::LD, NW = RW::NW;
     __shared__ __attribute__((aligned(16))) E buf[(3 * G + 16) * LD];
-    __shared__ typename Tile<BF>::val sT[NP][64];
-    __shared__ typename Tile<BF>::pair sP[NP][64];
+    __shared__ floatx4 sT[NP][64], sP[NP][64];
     __shared__ __attribute__((aligned(16))) PieceRows rows[NP];
     __shared__ double cum[NP][16];
     __shared__ float sg[G], sbeta[G];
@@ -194,8 +193,8 @@ __global__ __launch_bounds__(4 * D, D == 128 ? 2 : 3) void delta_fwd_kernel(Delt
                     piece_triangles<BF, D, LD, WANT_T | WANT_PT, false>(q, k, sg, sbeta, from,
                                                       piece_end(from, count, ends, single) - from, single, lane, cum[p],
                                                       &rows[p], Tt, Tn, Pt, Pn);
-                    sT[p][lane] = Tile<BF>::split(Tt);
-                    sP[p][lane] = Tile<BF>::part(Pt);
+                    sT[p][lane] = Tt;
+                    sP[p][lane] = Pt;
                 }
                 workgroup_lds_barrier();
 #pragma unroll 1

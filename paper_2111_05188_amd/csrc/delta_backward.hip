@@ -48,7 +48,8 @@ struct Back {
         // such rows are summed over (dy, q, k, times zeros) they are inputs again.
         __attribute__((aligned(16))) E dy[G * LD], q[G * LD], k[G * LD], v[G * LD];
         __attribute__((aligned(16))) floatx4 parts[TILES][NW][64];  // of the waves' columns
-        __attribute__((aligned(16))) val m[NP][4][64];      // T, T^T, P, P^T
+        __attribute__((aligned(16))) floatx4 m[NP][3][64];  // T, T^T, P^T
+        __attribute__((aligned(16))) val P[NP][64];
         __attribute__((aligned(16))) PieceRows rows[NP];
         // y.dy, v.dv, dR.u of the waves' columns
         __attribute__((aligned(16))) float sums[G][3][NW];
@@ -88,7 +89,7 @@ struct Back {
         const PieceRows &rows = sh.rows[p];
         // all that comes from LDS first: behind a write nothing is read ahead
         raw kr[KT], qr[OUT ? KT : 1], kc[KT], dyc = {};
-        val P = {};
+        floatx4 P = {};
 #pragma unroll
         for (int kt = 0; kt < KT; ++kt) {
             kr[kt] = along_row<BF, LD>(sh.k, s, kt, lane);
@@ -98,9 +99,9 @@ struct Back {
         const floatx4 be = *(const floatx4 *)(rows.beta + r), ak = *(const floatx4 *)(rows.ak + r);
         const floatx4 aq = *(const floatx4 *)(rows.aq + r), au = *(const floatx4 *)(rows.au + r);
         const float total = rows.total;
-        const val Tt = sh.m[p][1][lane];
+        const floatx4 Tt = sh.m[p][1][lane];
         if constexpr (OUT) {
-            P = sh.m[p][3][lane];
+            P = sh.m[p][2][lane];
             dyc = along_col<BF, LD, ONE>(sh.dy, s, count, w, lane);
         }
 #pragma unroll
@@ -119,7 +120,7 @@ struct Back {
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i) R[i] = r + i < count ? be[i] * vv[i] - ak[i] * ks[i] : 0.0f;
-        U = TL::mm(Tt, TL::split(R), U);
+        U = Tile<false>::mm(Tt, R, U);
 #pragma unroll
         for (int i = 0; i < 4; ++i) W[i] = r + i < count ? U[i] * au[i] : 0.0f;
         const val y = TL::split(W);
@@ -132,7 +133,7 @@ struct Back {
             floatx4 o, t;
 #pragma unroll
             for (int i = 0; i < 4; ++i) o[i] = aq[i] * qs[i];
-            o = TL::mm(P, TL::split(U), o);
+            o = Tile<false>::mm(P, U, o);
             const floatx4 dy = TL::wide(dyc);
 #pragma unroll
             for (int i = 0; i < 4; ++i) t[i] = row_sum(o[i] * dy[i]);
@@ -169,7 +170,8 @@ struct Back {
         const floatx4 be = *(const floatx4 *)(rows.beta + r), ak = *(const floatx4 *)(rows.ak + r);
         const floatx4 aq = *(const floatx4 *)(rows.aq + r), au = *(const floatx4 *)(rows.au + r);
         const float total = rows.total;
-        const val Pn = sh.m[p][2][lane], Tn = sh.m[p][0][lane];
+        const val Pn = sh.P[p][lane];
+        const floatx4 Tn = sh.m[p][0][lane];
 #pragma unroll
         for (int kt = 0; kt < KT; ++kt) {
             qc[kt] = along_col<BF, LD, ONE>(sh.q, s, count, kt, lane);
@@ -187,7 +189,7 @@ struct Back {
 #pragma unroll
         for (int i = 0; i < 4; ++i) dU[i] = r + i < count ? kg[i] * au[i] : 0.0f;
         dU = TL::mm(Pn, dyc, dU);
-        dR = TL::mm(Tn, TL::split(dU), dR);
+        dR = Tile<false>::mm(Tn, dU, dR);
         const floatx4 dyw = TL::wide(dyc);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -432,14 +434,14 @@ __global__ __launch_bounds__(4 * D, 2) void delta_bwd_kernel(DeltaArgs a)
                     if (j < NP) {
                         piece_triangles<BF, D, LD, WANT_T, true>(sh.q, sh.k, sh.g, sh.beta, from, c, single, lane,
                                                                 sh.cum[j],                                                                 &sh.rows[j], Tt, Tn, Pt, Pn);
-                        sh.m[p][0][lane] = Tile<BF>::split(Tn);
-                        sh.m[p][1][lane] = Tile<BF>::split(Tt);
+                        sh.m[p][0][lane] = Tn;
+                        sh.m[p][1][lane] = Tt;
                     } else {
                         piece_triangles<BF, D, LD, WANT_P | WANT_PT, true>(sh.q, sh.k, sh.g, sh.beta, from, c, single, lane,
                                                                            sh.cum[j], (PieceRows *)sh.parts + p, Tt, Tn,
                                                                            Pt, Pn);
-                        sh.m[p][2][lane] = Tile<BF>::split(Pn);
-                        sh.m[p][3][lane] = Tile<BF>::split(Pt);
+                        sh.P[p][lane] = Tile<BF>::split(Pn);
+                        sh.m[p][2][lane] = Pt;
                     }
                 }
             };
