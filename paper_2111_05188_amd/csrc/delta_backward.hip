@@ -63,24 +63,27 @@ struct Back {
     static_assert(sizeof(PieceRows) % 16 == 0 && NP * sizeof(PieceRows) <= sizeof(Shared::parts), "P's rows");
     static_assert(sizeof(Shared) <= LDS_LIMIT, "LDS");
 
-    // f(i) for the rows 4g + i that a piece has.  (ONE, here and below: a piece of one
-    // step, beside which there may be a NaN or an infinity.)
-    template <class F>
+    // f(i) for the rows 4g + i that a piece has.  (PART, here and below: a piece of fewer
+    // steps than 16; beside one of one step there may be a NaN or an infinity.)
+    template <bool PART, class F>
     static __device__ __forceinline__ void each_row(int count, int r, F f)
     {
-        if (count == 16) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) f(i);
-        } else {
+        for (int i = 0; i < 4; ++i)
+            if (!PART || r + i < count) f(i);
+    }
+
+    // (a branch: as many selects would run for every piece)
+    static __device__ __forceinline__ void clear(floatx4 *S)
+    {
+        asm volatile("");
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                if (r + i < count) f(i);
-        }
+        for (int kt = 0; kt < KT; ++kt) S[kt] = floatx4{};
     }
 
     // The writes U of a piece and the state after it, on columns 16w...  OUT: the rows'
     // parts of y.dy too, and the transpose of the state before it.
-    template <bool ONE, bool OUT>
+    template <bool PART, bool OUT>
     static __device__ __forceinline__ floatx4 forward(Shared &sh, int s, int count, bool ends, int p, int w, int lane,
                                                       floatx4 *S, pair *ST)
     {
@@ -95,17 +98,17 @@ struct Back {
             kr[kt] = along_row<BF, LD>(sh.k, s, kt, lane);
             if constexpr (OUT) qr[kt] = along_row<BF, LD>(sh.q, s, kt, lane);
         }
-        const floatx4 vv = TL::wide(along_col<BF, LD, ONE>(sh.v, s, count, w, lane));
+        const floatx4 vv = TL::wide(along_col<BF, LD, PART>(sh.v, s, count, w, lane));
         const floatx4 be = *(const floatx4 *)(rows.beta + r), ak = *(const floatx4 *)(rows.ak + r);
         const floatx4 aq = *(const floatx4 *)(rows.aq + r), au = *(const floatx4 *)(rows.au + r);
         const float total = rows.total;
         const floatx4 Tt = sh.m[p][1][lane];
         if constexpr (OUT) {
             P = sh.m[p][2][lane];
-            dyc = along_col<BF, LD, ONE>(sh.dy, s, count, w, lane);
+            dyc = along_col<BF, LD, PART>(sh.dy, s, count, w, lane);
         }
 #pragma unroll
-        for (int kt = 0; kt < KT; ++kt) kc[kt] = along_col<BF, LD, ONE>(sh.k, s, count, kt, lane);
+        for (int kt = 0; kt < KT; ++kt) kc[kt] = along_col<BF, LD, PART>(sh.k, s, count, kt, lane);
         const raw eye = TL::eye(lane);
         floatx4 ks = {}, qs = {}, U = {}, R, W;
 #pragma unroll
@@ -119,16 +122,14 @@ struct Back {
             }
         }
 #pragma unroll
-        for (int i = 0; i < 4; ++i) R[i] = r + i < count ? be[i] * vv[i] - ak[i] * ks[i] : 0.0f;
+        for (int i = 0; i < 4; ++i) R[i] = !PART || r + i < count ? be[i] * vv[i] - ak[i] * ks[i] : 0.0f;
         U = Tile<false>::mm(Tt, R, U);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) W[i] = r + i < count ? U[i] * au[i] : 0.0f;
+        for (int i = 0; i < 4; ++i) W[i] = !PART || r + i < count ? U[i] * au[i] : 0.0f;
         const val y = TL::split(W);
 #pragma unroll
-        for (int kt = 0; kt < KT; ++kt) {
-            S[kt] = TL::mm(kc[kt], y, S[kt] * total);
-            if (ends) S[kt] = floatx4{};
-        }
+        for (int kt = 0; kt < KT; ++kt) S[kt] = TL::mm(kc[kt], y, S[kt] * total);
+        if (ends) clear(S);
         if constexpr (OUT) {
             floatx4 o, t;
 #pragma unroll
@@ -137,7 +138,7 @@ struct Back {
             const floatx4 dy = TL::wide(dyc);
 #pragma unroll
             for (int i = 0; i < 4; ++i) t[i] = row_sum(o[i] * dy[i]);
-            each_row(count, r, [&](int i) {
+            each_row<PART>(count, r, [&](int i) {
                 if ((lane & 15) == 0) sh.sums[s + r + i][0][w] = t[i];
             });
         }
@@ -153,7 +154,7 @@ struct Back {
 
     // dR and dV of a piece, and the gradient of the state before it; of the one after it
     // the transpose.
-    template <bool ONE>
+    template <bool PART>
     static __device__ __forceinline__ Mine backward(Shared &sh, int s, int count, int p, int w, int lane, floatx4 *Gs,
                                                     floatx4 U, pair *GT)
     {
@@ -165,8 +166,8 @@ struct Back {
 #pragma unroll
         for (int kt = 0; kt < KT; ++kt) kr[kt] = along_row<BF, LD>(sh.k, s, kt, lane);
         mine.dy = along_row<BF, LD>(sh.dy, s, w, lane);
-        const raw dyc = along_col<BF, LD, ONE>(sh.dy, s, count, w, lane);
-        const floatx4 vw = TL::wide(along_col<BF, LD, ONE>(sh.v, s, count, w, lane));
+        const raw dyc = along_col<BF, LD, PART>(sh.dy, s, count, w, lane);
+        const floatx4 vw = TL::wide(along_col<BF, LD, PART>(sh.v, s, count, w, lane));
         const floatx4 be = *(const floatx4 *)(rows.beta + r), ak = *(const floatx4 *)(rows.ak + r);
         const floatx4 aq = *(const floatx4 *)(rows.aq + r), au = *(const floatx4 *)(rows.au + r);
         const float total = rows.total;
@@ -174,8 +175,8 @@ struct Back {
         const floatx4 Tn = sh.m[p][0][lane];
 #pragma unroll
         for (int kt = 0; kt < KT; ++kt) {
-            qc[kt] = along_col<BF, LD, ONE>(sh.q, s, count, kt, lane);
-            kc[kt] = along_col<BF, LD, ONE>(sh.k, s, count, kt, lane);
+            qc[kt] = along_col<BF, LD, PART>(sh.q, s, count, kt, lane);
+            kc[kt] = along_col<BF, LD, PART>(sh.k, s, count, kt, lane);
         }
         const raw eye = TL::eye(lane);
         floatx4 kg = {}, dU, dR = {}, A, B;
@@ -187,14 +188,14 @@ struct Back {
             GT[kt + 1] = TL::turned(TL::head(x1), eye);
         }
 #pragma unroll
-        for (int i = 0; i < 4; ++i) dU[i] = r + i < count ? kg[i] * au[i] : 0.0f;
+        for (int i = 0; i < 4; ++i) dU[i] = !PART || r + i < count ? kg[i] * au[i] : 0.0f;
         dU = TL::mm(Pn, dyc, dU);
         dR = Tile<false>::mm(Tn, dU, dR);
         const floatx4 dyw = TL::wide(dyc);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             A[i] = dyw[i] * aq[i];
-            B[i] = r + i < count ? -(dR[i] * ak[i]) : 0.0f;
+            B[i] = !PART || r + i < count ? -(dR[i] * ak[i]) : 0.0f;
         }
         const val a = TL::split(A), b = TL::split(B);
 #pragma unroll
@@ -213,7 +214,7 @@ struct Back {
         mine.dR = TL::turned(TL::part(dR), eye);
         mine.ak = ak;
         mine.au = au;
-        each_row(count, r, [&](int i) {
+        each_row<PART>(count, r, [&](int i) {
             sh.v[(s + r + i) * LD + col] = (E)dv[i];
             if ((lane & 15) == 0) {
                 sh.sums[s + r + i][1][w] = t[i];
@@ -280,14 +281,14 @@ struct Back {
 
     // rq (dq^ - q^ (q^.dq^)) in place of q, and the same of k, with q^.dq^ = y.dy and
     // k^.dk^ = 2 dR.u - v.dv.
-    template <bool ONE>
+    template <bool PART>
     static __device__ __forceinline__ void finish(Shared &sh, int s, int count, int p, int w, int lane, Sums &t)
     {
         lane = fresh(lane);
         const int n = lane & 15, r = 4 * (lane >> 4), col = 16 * w + n;
         const PieceRows &rows = sh.rows[p];
-        const raw qc = along_col<BF, LD, ONE>(sh.q, s, count, w, lane);
-        const raw kc = along_col<BF, LD, ONE>(sh.k, s, count, w, lane);
+        const raw qc = along_col<BF, LD, PART>(sh.q, s, count, w, lane);
+        const raw kc = along_col<BF, LD, PART>(sh.k, s, count, w, lane);
         const floatx4 rq = *(const floatx4 *)(rows.rq + r), rk = *(const floatx4 *)(rows.rk + r);
         const floatx4 be = *(const floatx4 *)(rows.beta + r), aq = *(const floatx4 *)(rows.aq + r);
         const float rkn = rows.rk[n];
@@ -303,8 +304,8 @@ struct Back {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const float f = fade[i] * rkn;
-            M[i] = r + i >= n && r + i < count ? t.M[i] * f * rq[i] : 0.0f;
-            L[i] = r + i > n && r + i < count ? -(t.E[i] * f * be[i] * rk[i]) : 0.0f;
+            M[i] = r + i >= n && (!PART || r + i < count) ? t.M[i] * f * rq[i] : 0.0f;
+            L[i] = r + i > n && (!PART || r + i < count) ? -(t.E[i] * f * be[i] * rk[i]) : 0.0f;
         }
         const raw eye = TL::eye(lane);
         const pair m = TL::part(M), l = TL::part(L);
@@ -316,7 +317,7 @@ struct Back {
         a = TL::mm_out(TL::turned(m, eye), kc, a);
         b = TL::mm_out(TL::turned(l, eye), kc, b);
         const floatx4 qw = TL::wide(qc), kw = TL::wide(kc);
-        each_row(count, r, [&](int i) {
+        each_row<PART>(count, r, [&](int i) {
             sh.q[(s + r + i) * LD + col] = (E)(a[i] - qw[i] * rq[i] * rq[i] * yd[i]);
             sh.k[(s + r + i) * LD + col] = (E)(b[i] - kw[i] * rk[i] * rk[i] * kd[i]);
         });
@@ -324,9 +325,9 @@ struct Back {
 };
 
 template <class F>
-__device__ __forceinline__ void pieces_of(bool one, F f)
+__device__ __forceinline__ void pieces_of(int count, F f)
 {
-    if (one) f(std::integral_constant<bool, true>{});
+    if (count < 16) f(std::integral_constant<bool, true>{});
     else f(std::integral_constant<bool, false>{});
 }
 
@@ -479,7 +480,7 @@ __global__ __launch_bounds__(4 * D, 2) void delta_bwd_kernel(DeltaArgs a)
                 for (int p = 0; p < NP; ++p) {
                     const int c = at[p + 1] - at[p];
                     if (c == 0) continue;
-                    pieces_of(single, [&](auto m) {
+                    pieces_of(c, [&](auto m) {
                         U[p] = BK::template forward<decltype(m)::value, true>(sh, at[p], c, done(p), p, w, lane, S,
                                                                               ST[p]);
                     });
@@ -499,12 +500,9 @@ __global__ __launch_bounds__(4 * D, 2) void delta_bwd_kernel(DeltaArgs a)
                 for (int p = NP - 1; p >= 0; --p) {
                     const int c = at[p + 1] - at[p];
                     if (c == 0) continue;
-                    if (done(p)) {
-#pragma unroll
-                        for (int kt = 0; kt < KT; ++kt) Gs[kt] = floatx4{};
-                    }
+                    if (done(p)) BK::clear(Gs);
                     typename BK::Mine mine;
-                    pieces_of(single, [&](auto m) {
+                    pieces_of(c, [&](auto m) {
                         mine = BK::template backward<decltype(m)::value>(sh, at[p], c, p, w, lane, Gs, U[p], GT);
                     });
                     // the waves' parts to the waves that have the keys' columns
@@ -520,7 +518,7 @@ __global__ __launch_bounds__(4 * D, 2) void delta_bwd_kernel(DeltaArgs a)
                         BK::collect(sh, x, w, lane, t);
                         if (x == 0) workgroup_lds_barrier();
                     }
-                    pieces_of(single, [&](auto m) {
+                    pieces_of(c, [&](auto m) {
                         BK::template finish<decltype(m)::value>(sh, at[p], c, p, w, lane, t);
                     });
                 }
