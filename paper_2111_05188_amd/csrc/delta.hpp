@@ -69,6 +69,8 @@ template <> struct Tile<false> {
         return x;
     }
     static __device__ __forceinline__ pair turned(pair x, raw eye) { return mm(x, eye, floatx4{}); }
+    // of two tiles whose values are never in the same place (the others are zeros)
+    static __device__ __forceinline__ pair either(pair a, pair b) { return a + b; }
 };
 
 template <> struct Tile<true> {
@@ -185,6 +187,16 @@ template <> struct Tile<true> {
             b[i] = __float_as_uint(m[i]);
         }
         return pair{upper(a), upper(b)};
+    }
+    static __device__ __forceinline__ pair either(pair a, pair b)
+    {
+        uint64_t x[2], y[2];
+        __builtin_memcpy(x, &a, sizeof a);
+        __builtin_memcpy(y, &b, sizeof b);
+        x[0] |= y[0];
+        x[1] |= y[1];
+        __builtin_memcpy(&a, x, sizeof a);
+        return a;
     }
     // products over 32
     static __device__ __forceinline__ floatx4 mm2(raw a0, raw a1, val b0, val b1, floatx4 c)

@@ -60,6 +60,7 @@ struct Back {
         int odd[2];
     };
     static_assert(16 * LD * sizeof(E) <= sizeof(Shared::parts), "rows past v's end");
+    static_assert(sizeof(pair) == sizeof(floatx4), "triangles' gradients");
     static_assert(sizeof(PieceRows) % 16 == 0 && NP * sizeof(PieceRows) <= sizeof(Shared::parts), "P's rows");
     static_assert(sizeof(Shared) <= LDS_LIMIT, "LDS");
 
@@ -266,32 +267,63 @@ struct Back {
         return x;
     }
 
-    // What is summed of a piece: its keys' columns 16w.. (rows' lengths are in them or
-    // come with the decays) and a triangle's gradient, scaled by both rows' lengths.
-    struct Sums {
-        floatx4 dq, dk, M, E;
-    };
-    static __device__ __forceinline__ void collect(const Shared &sh, int turn, int w, int lane, Sums &t)
+    // The gradient of a piece's triangle P (turn 0) or L (turn 1), scaled by both rows'
+    // lengths, by one wave: as it is and transposed, or, L's, the sum of both.  They take the
+    // place of T and P.
+    template <bool PART>
+    static __device__ __forceinline__ void triangle(Shared &sh, int count, int p, int turn, int lane)
     {
         lane = fresh(lane);
-        const int first = TURNS == 1 ? turn * HALF : 0;
-        (turn == 0 ? t.dq : t.dk) = take(sh, first + w, lane);
-        (turn == 0 ? t.M : t.E) = take(sh, first + KT, lane);
+        const int n = lane & 15, r = 4 * (lane >> 4);
+        const PieceRows &rows = sh.rows[p];
+        const floatx4 sum = take(sh, TURNS == 1 ? turn * HALF + KT : KT, lane);
+        const floatx4 rq = *(const floatx4 *)(rows.rq + r), rk = *(const floatx4 *)(rows.rk + r);
+        const floatx4 be = *(const floatx4 *)(rows.beta + r);
+        const float rkn = rows.rk[n];
+        const floatx4 fade = piece_decays(sh.cum[p], lane);
+        floatx4 x;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float f = turn == 0 ? rq[i] : -(be[i] * rk[i]);
+            const bool in = turn == 0 ? r + i >= n : r + i > n;
+            x[i] = in && (!PART || r + i < count) ? sum[i] * (fade[i] * rkn) * f : 0.0f;
+        }
+        const pair d = TL::part(x), t = TL::turned(d, TL::eye(lane));
+        if (turn == 0) {
+            *(pair *)&sh.m[p][0][lane] = d;
+            *(pair *)&sh.m[p][1][lane] = t;
+        } else {
+            *(pair *)&sh.m[p][2][lane] = TL::either(d, t);
+        }
+    }
+
+    // What is summed of a piece on its keys' columns 16w..
+    struct Sums {
+        floatx4 dq, dk;
+    };
+    template <bool PART>
+    static __device__ __forceinline__ void collect(Shared &sh, int count, int p, int turn, int w, int lane, Sums &t)
+    {
+        lane = fresh(lane);
+        (turn == 0 ? t.dq : t.dk) = take(sh, TURNS == 1 ? turn * HALF + w : w, lane);
+        if (w == (2 * p + turn) % NW) triangle<PART>(sh, count, p, turn, lane);
     }
 
     // rq (dq^ - q^ (q^.dq^)) in place of q, and the same of k, with q^.dq^ = y.dy and
     // k^.dk^ = 2 dR.u - v.dv.
     template <bool PART>
-    static __device__ __forceinline__ void finish(Shared &sh, int s, int count, int p, int w, int lane, Sums &t)
+    static __device__ __forceinline__ void finish(Shared &sh, int s, int count, int p, int w, int lane,
+                                                  const Sums &t)
     {
         lane = fresh(lane);
-        const int n = lane & 15, r = 4 * (lane >> 4), col = 16 * w + n;
+        const int r = 4 * (lane >> 4), col = 16 * w + (lane & 15);
         const PieceRows &rows = sh.rows[p];
         const raw qc = along_col<BF, LD, PART>(sh.q, s, count, w, lane);
         const raw kc = along_col<BF, LD, PART>(sh.k, s, count, w, lane);
         const floatx4 rq = *(const floatx4 *)(rows.rq + r), rk = *(const floatx4 *)(rows.rk + r);
-        const floatx4 be = *(const floatx4 *)(rows.beta + r), aq = *(const floatx4 *)(rows.aq + r);
-        const float rkn = rows.rk[n];
+        const floatx4 aq = *(const floatx4 *)(rows.aq + r);
+        const pair m = *(const pair *)&sh.m[p][0][lane], mt = *(const pair *)&sh.m[p][1][lane];
+        const pair l = *(const pair *)&sh.m[p][2][lane];
         floatx4 yd, kd;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {           // (rows past the group's are not there)
@@ -299,23 +331,12 @@ struct Back {
             yd[i] = total(x[0]);
             kd[i] = 2.0f * total(x[2]) - total(x[1]);
         }
-        const floatx4 fade = piece_decays(sh.cum[p], lane);
-        floatx4 M, L;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float f = fade[i] * rkn;
-            M[i] = r + i >= n && (!PART || r + i < count) ? t.M[i] * f * rq[i] : 0.0f;
-            L[i] = r + i > n && (!PART || r + i < count) ? -(t.E[i] * f * be[i] * rk[i]) : 0.0f;
-        }
-        const raw eye = TL::eye(lane);
-        const pair m = TL::part(M), l = TL::part(L);
         floatx4 a, b = t.dk;
 #pragma unroll
         for (int i = 0; i < 4; ++i) a[i] = aq[i] * t.dq[i];
         b = TL::mm_out(m, qc, b);
         b = TL::mm_out(l, kc, b);
-        a = TL::mm_out(TL::turned(m, eye), kc, a);
-        b = TL::mm_out(TL::turned(l, eye), kc, b);
+        a = TL::mm_out(mt, kc, a);
         const floatx4 qw = TL::wide(qc), kw = TL::wide(kc);
         each_row<PART>(count, r, [&](int i) {
             sh.q[(s + r + i) * LD + col] = (E)(a[i] - qw[i] * rq[i] * rq[i] * yd[i]);
@@ -496,6 +517,7 @@ __global__ __launch_bounds__(4 * D, 2) void delta_bwd_kernel(DeltaArgs a)
                     x = lanes_sum<64>(x);
                     if (lane == 0) sh.ends[w] = x;
                 }
+                typename BK::Sums t[NP];
 #pragma unroll
                 for (int p = NP - 1; p >= 0; --p) {
                     const int c = at[p + 1] - at[p];
@@ -506,7 +528,6 @@ __global__ __launch_bounds__(4 * D, 2) void delta_bwd_kernel(DeltaArgs a)
                         mine = BK::template backward<decltype(m)::value>(sh, at[p], c, p, w, lane, Gs, U[p], GT);
                     });
                     // the waves' parts to the waves that have the keys' columns
-                    typename BK::Sums t;
                     if (p + 1 < NP) workgroup_lds_barrier();
 #pragma unroll
                     for (int x = 0; x < 2; ++x) {
@@ -514,12 +535,20 @@ __global__ __launch_bounds__(4 * D, 2) void delta_bwd_kernel(DeltaArgs a)
                         if (x == 0 && BK::TURNS == 1) continue;
                         if (x == 1 && p == 0 && batch == 0 && grp > first) fetch(grp - 1);
                         workgroup_lds_barrier();
-                        if (BK::TURNS == 1) BK::collect(sh, 0, w, lane, t);
-                        BK::collect(sh, x, w, lane, t);
+                        pieces_of(c, [&](auto m) {
+                            if (BK::TURNS == 1) BK::template collect<decltype(m)::value>(sh, c, p, 0, w, lane, t[p]);
+                            BK::template collect<decltype(m)::value>(sh, c, p, x, w, lane, t[p]);
+                        });
                         if (x == 0) workgroup_lds_barrier();
                     }
+                }
+                workgroup_lds_barrier();
+#pragma unroll
+                for (int p = 0; p < NP; ++p) {
+                    const int c = at[p + 1] - at[p];
+                    if (c == 0) continue;
                     pieces_of(c, [&](auto m) {
-                        BK::template finish<decltype(m)::value>(sh, at[p], c, p, w, lane, t);
+                        BK::template finish<decltype(m)::value>(sh, at[p], c, p, w, lane, t[p]);
                     });
                 }
                 workgroup_lds_barrier();
