@@ -16,8 +16,8 @@
 namespace tpk {
 namespace {
 
-// one piece on the state's columns of this wave
-template <bool BF, int D, int LD, bool MASK, class E>
+// one piece on the state's columns of this wave; OUT: its outputs, in place of v
+template <bool BF, int D, int LD, bool MASK, bool OUT, class E>
 __device__ __forceinline__ void run_piece(const E *q, const E *k, E *v, int s, int count, bool ends,
                                           const PieceRows &rows, const floatx4 &Tt, const floatx4 &Pt, int w,
                                           int lane, floatx4 *S)
@@ -31,7 +31,8 @@ __device__ __forceinline__ void run_piece(const E *q, const E *k, E *v, int s, i
     for (int kt = 0; kt < KT; kt += 2) {
         const auto x0 = TL::split(S[kt]), x1 = TL::split(S[kt + 1]);
         ks = TL::mm2(along_row<BF, LD>(k, s, kt, lane), along_row<BF, LD>(k, s, kt + 1, lane), x0, x1, ks);
-        qs = TL::mm2(along_row<BF, LD>(q, s, kt, lane), along_row<BF, LD>(q, s, kt + 1, lane), x0, x1, qs);
+        if constexpr (OUT)
+            qs = TL::mm2(along_row<BF, LD>(q, s, kt, lane), along_row<BF, LD>(q, s, kt + 1, lane), x0, x1, qs);
     }
     const floatx4 vv = TL::wide(along_col<BF, LD, MASK>(v, s, count, w, lane));
     const floatx4 be = *(const floatx4 *)(rows.beta + r), ak = *(const floatx4 *)(rows.ak + r);
@@ -43,10 +44,12 @@ __device__ __forceinline__ void run_piece(const E *q, const E *k, E *v, int s, i
         o[i] = aq[i] * qs[i];
     }
     U = Tile<false>::mm(Tt, R, U);
-    o = Tile<false>::mm(Pt, U, o);
+    if constexpr (OUT) {
+        o = Tile<false>::mm(Pt, U, o);
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-        if (!MASK || r + i < count) v[(s + r + i) * LD + 16 * w + (lane & 15)] = (E)o[i];
+        for (int i = 0; i < 4; ++i)
+            if (!MASK || r + i < count) v[(s + r + i) * LD + 16 * w + (lane & 15)] = (E)o[i];
+    }
     if (ends) {
 #pragma unroll
         for (int kt = 0; kt < KT; ++kt) S[kt] = floatx4{};
@@ -145,7 +148,7 @@ __global__ __launch_bounds__(4 * D, D == 128 ? 2 : 3) void delta_fwd_kernel(Delt
     float fr = 0.0f, fb = 0.0f;
     uint8_t fd = 0;
     auto fetch = [&](int count) {
-        RW::fetch(a.q, pq, count, a.dk, tid, fq);
+        if constexpr (!MAP) RW::fetch(a.q, pq, count, a.dk, tid, fq);
         RW::fetch(a.k, pk, count, a.dk, tid, fk);
         RW::fetch(a.v, pv, count, a.dv, tid, fv);
         pq += G * a.q.st;
@@ -168,10 +171,10 @@ __global__ __launch_bounds__(4 * D, D == 128 ? 2 : 3) void delta_fwd_kernel(Delt
     for (int t0 = begin, turn = 0; t0 < end; t0 += G, turn ^= 1) {
         const int count = len - t0 < G ? len - t0 : G, all = end - t0 < G ? end - t0 : G;
         if (count > 0) {
-            RW::put(q, fq, tid);
+            if constexpr (!MAP) RW::put(q, fq, tid);
             RW::put(k, fk, tid);
             RW::put(v, fv, tid);
-            float odd = RW::odd(fq) + RW::odd(fk) + RW::odd(fv);
+            float odd = (MAP ? 0.0f : RW::odd(fq)) + RW::odd(fk) + RW::odd(fv);
             if ((int)threadIdx.x < count) {
                 const float g = rate * delta_sigmoid(fr);
                 sg[threadIdx.x] = g < -3e38f ? -3e38f : g;
@@ -190,11 +193,11 @@ __global__ __launch_bounds__(4 * D, D == 128 ? 2 : 3) void delta_fwd_kernel(Delt
                     for (int j = 0; j < p && from < count; ++j) from = piece_end(from, count, ends, single);
                     if (from >= count) break;
                     floatx4 Tt, Tn, Pt, Pn;
-                    piece_triangles<BF, D, LD, WANT_T | WANT_PT, false>(q, k, sg, sbeta, from,
-                                                      piece_end(from, count, ends, single) - from, single, lane, cum[p],
+                    piece_triangles<BF, D, LD, MAP ? WANT_T : WANT_T | WANT_PT, false>(MAP ? k : q, k, sg, sbeta, from,
+                                                      piece_end(from, count, ends, single) - from, lane, cum[p],
                                                       &rows[p], Tt, Tn, Pt, Pn);
                     sT[p][lane] = Tt;
-                    sP[p][lane] = Pt;
+                    if constexpr (!MAP) sP[p][lane] = Pt;
                 }
                 workgroup_lds_barrier();
 #pragma unroll 1
@@ -211,19 +214,19 @@ __global__ __launch_bounds__(4 * D, D == 128 ? 2 : 3) void delta_fwd_kernel(Delt
                     if constexpr (MAP) {
                         cut = cut || done;
                         if (e - s == 16) {
-                            run_piece<BF, D, LD, false>(q, k, v, s, 16, done, rows[p], sT[p][lane], sP[p][lane],
+                            run_piece<BF, D, LD, false, !MAP>(q, k, v, s, 16, done, rows[p], sT[p][lane], sP[p][lane],
                                                         w, lane, S);
                             map_piece<BF, D, LD, false>(k, s, 16, done, rows[p], sT[p][lane], lane, M);
                         } else {
-                            run_piece<BF, D, LD, true>(q, k, v, s, e - s, done, rows[p], sT[p][lane], sP[p][lane],
+                            run_piece<BF, D, LD, true, !MAP>(q, k, v, s, e - s, done, rows[p], sT[p][lane], sP[p][lane],
                                                        w, lane, S);
                             map_piece<BF, D, LD, true>(k, s, e - s, done, rows[p], sT[p][lane], lane, M);
                         }
                     } else if (e - s == 16)
-                        run_piece<BF, D, LD, false>(q, k, v, s, 16, done, rows[p], sT[p][lane], sP[p][lane], w,
+                        run_piece<BF, D, LD, false, !MAP>(q, k, v, s, 16, done, rows[p], sT[p][lane], sP[p][lane], w,
                                                     lane, S);
                     else
-                        run_piece<BF, D, LD, true>(q, k, v, s, e - s, done, rows[p], sT[p][lane], sP[p][lane], w,
+                        run_piece<BF, D, LD, true, !MAP>(q, k, v, s, e - s, done, rows[p], sT[p][lane], sP[p][lane], w,
                                                    lane, S);
                     s = e;
                 }
@@ -256,59 +259,88 @@ __global__ __launch_bounds__(4 * D, D == 128 ? 2 : 3) void delta_fwd_kernel(Delt
     }
 }
 
-// The first state of every segment, in the place of what the segment adds: a
-// workgroup has 16 columns of one head's states, wave w the rows 16w.., 16(w+4)..
-// of them; all waves read all rows of the state before from LDS.
-template <int D>
-__global__ __launch_bounds__(256) void delta_join_kernel(DeltaArgs a, bool backward)
+// The state after a run of segments, or before every one of them.  In the order of
+// their positions (backward: from the last segment on) they are split into blocks of
+// `per`.  FOLD: a block's own map and what it adds, from its segments' (columns of the
+// unit states, then of no state).  Else the first state of every segment, in the place of
+// what it adds, from `first`, or from each block's in `starts`.
+struct DeltaJoin {
+    const float *maps;
+    float *adds;
+    const int32_t *cuts;
+    int n, per;
+    bool backward;
+    const float *first, *starts;
+    int dk, dv;
+    float *block_maps, *block_adds;
+    int32_t *block_cuts;
+};
+
+// A workgroup has 16 columns of one head's states, wave w the rows 16w.., 16(w+4).. of
+// them; all waves read all rows of the state before from LDS.
+template <int D, bool FOLD>
+__global__ __launch_bounds__(256) void delta_join_kernel(DeltaJoin a)
 {
     constexpr int KT = D / 16, MINE = (KT + 3) / 4;
     __shared__ floatx4 state[2][KT][64];
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int n = lane & 15, r4 = 4 * (lane >> 4), col = blockIdx.y * 16 + n, heads = gridDim.x;
+    const int n = lane & 15, r4 = 4 * (lane >> 4), heads = gridDim.x;
+    const bool unit = FOLD && blockIdx.y < KT;
+    const int col = (FOLD && !unit ? blockIdx.y - KT : blockIdx.y) * 16 + n;
+    const int from = blockIdx.z * a.per, count = a.n - from < a.per ? a.n - from : a.per;
+    const int64_t block = ((int64_t)blockIdx.z * heads + blockIdx.x) * D * D;
     const int64_t st = (int64_t)blockIdx.x * a.dk * a.dv;
-    const float *first = backward ? a.dh_last : a.h0;
     floatx4 S[MINE];
 #pragma unroll
     for (int j = 0; j < MINE; ++j)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int row = 16 * (w + 4 * j) + r4 + i;
-            S[j][i] = first && row < a.dk && col < a.dv ? first[st + (int64_t)row * a.dv + col] : 0.0f;
+            if constexpr (FOLD) S[j][i] = unit && row == col ? 1.0f : 0.0f;
+            else if (a.starts) S[j][i] = row < D ? a.starts[block + row * D + col] : 0.0f;
+            else S[j][i] = a.first && row < a.dk && col < a.dv ? a.first[st + (int64_t)row * a.dv + col] : 0.0f;
         }
+    // products: of all segments but, where nothing follows, the last
+    const int steps = FOLD ? count : count - 1;
     struct Segment {
         floatx4 add[MINE], map[MINE][KT];
         int cut;
     };
+    auto place = [&](int x) {
+        const int seg = a.backward ? a.n - 1 - from - x : from + x;
+        return (int64_t)seg * heads + blockIdx.x;
+    };
     auto fetch = [&](int x, Segment &g) {
-        const int seg = backward ? a.segments - 1 - x : x;
-        const int64_t at = ((int64_t)seg * heads + blockIdx.x) * D * D;
-        g.cut = a.cuts[seg * heads + blockIdx.x];
+        const int64_t at = place(x) * D * D;
+        g.cut = a.cuts[place(x)];
 #pragma unroll
         for (int j = 0; j < MINE; ++j) {
             const int t = w + 4 * j;
             if (t >= KT) continue;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) g.add[j][i] = a.adds[at + (16 * t + r4 + i) * D + col];
+            for (int i = 0; i < 4; ++i) g.add[j][i] = unit ? 0.0f : a.adds[at + (16 * t + r4 + i) * D + col];
 #pragma unroll
             for (int kt = 0; kt < KT; ++kt)
                 g.map[j][kt] = *(const floatx4 *)(a.maps + at + (16 * t + n) * D + 16 * kt + r4);
         }
     };
+    bool cut = false;
     // the state before segment x goes to its place; the one after it, with the loads of
     // the next but one on their way
     auto step = [&](int x, Segment &g) {
-        const int seg = backward ? a.segments - 1 - x : x;
-        const int64_t at = ((int64_t)seg * heads + blockIdx.x) * D * D;
+        const int64_t at = place(x) * D * D;
 #pragma unroll
         for (int j = 0; j < MINE; ++j) {
             const int t = w + 4 * j;
             if (t >= KT) continue;
+            if constexpr (!FOLD) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) a.adds[at + (16 * t + r4 + i) * D + col] = S[j][i];
+                for (int i = 0; i < 4; ++i) a.adds[at + (16 * t + r4 + i) * D + col] = S[j][i];
+            }
             state[x & 1][t][lane] = S[j];
         }
-        if (x + 1 == a.segments) return;
+        if (x >= steps) return;
+        cut = cut || g.cut != 0;
         workgroup_lds_barrier();
 #pragma unroll
         for (int j = 0; j < MINE; ++j) {
@@ -323,14 +355,25 @@ __global__ __launch_bounds__(256) void delta_join_kernel(DeltaArgs a, bool backw
                 }
             S[j] += half;
         }
-        if (x + 3 < a.segments) fetch(x + 2, g);
+        if (x + 2 < steps) fetch(x + 2, g);
     };
     Segment even, odd;
-    fetch(0, even);
-    if (a.segments > 2) fetch(1, odd);
-    for (int x = 0; x < a.segments; x += 2) {
+    if (steps > 0) fetch(0, even);
+    if (steps > 1) fetch(1, odd);
+    for (int x = 0; x < count; x += 2) {
         step(x, even);
-        if (x + 1 < a.segments) step(x + 1, odd);
+        if (x + 1 < count) step(x + 1, odd);
+    }
+    if constexpr (FOLD) {
+        float *to = (unit ? a.block_maps : a.block_adds) + block;
+#pragma unroll
+        for (int j = 0; j < MINE; ++j) {
+            const int t = w + 4 * j;
+            if (t >= KT) continue;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) to[(16 * t + r4 + i) * D + col] = S[j][i];
+        }
+        if (blockIdx.y == 0 && threadIdx.x == 0) a.block_cuts[(int64_t)blockIdx.z * heads + blockIdx.x] = cut;
     }
 }
 
@@ -501,14 +544,28 @@ static int delta_segments(int T, int B, int H, int &seg_len)
     return (int)((groups + per - 1) / per);
 }
 
-// lambda's parts, one a head and segment; the maps
+// blocks of segments (1: the join takes them one after the other), and of how many
+static int delta_blocks(int segments, int &per)
+{
+    per = segments;
+    if (segments <= 24) return 1;
+    per = 1;
+    while (per * per < segments) ++per;
+    return (segments + per - 1) / per;
+}
+
+static size_t delta_round(size_t bytes) { return (bytes + 255) / 256 * 256; }
+
+// lambda's parts, one a head and segment; the maps of segments, and of blocks of them
 size_t delta_workspace_bytes(int T, int B, int H, int dk, int dv)
 {
-    int seg_len;
-    const size_t n = (size_t)delta_segments(T, B, H, seg_len) * B * H, D = delta_width(dk, dv);
-    const size_t parts = (n * sizeof(double) + 255) / 256 * 256;
-    if (n == (size_t)B * H) return parts;
-    return parts + (n * sizeof(int32_t) + 255) / 256 * 256 + 2 * n * D * D * sizeof(float);
+    int seg_len, per;
+    const int segments = delta_segments(T, B, H, seg_len), blocks = delta_blocks(segments, per);
+    const size_t heads = (size_t)B * H, D = delta_width(dk, dv), state = 2 * D * D * sizeof(float);
+    size_t bytes = delta_round(segments * heads * sizeof(double));
+    if (segments > 1) bytes += delta_round(segments * heads * sizeof(int32_t)) + segments * heads * state;
+    if (blocks > 1) bytes += delta_round(blocks * heads * sizeof(int32_t)) + blocks * heads * state;
+    return bytes;
 }
 
 void delta_carve(DeltaArgs &a)
@@ -517,19 +574,52 @@ void delta_carve(DeltaArgs &a)
     const size_t n = (size_t)a.segments * a.B * a.H, D = delta_width(a.dk, a.dv);
     char *p = (char *)a.work;
     a.parts = (double *)p;
-    p += (n * sizeof(double) + 255) / 256 * 256;
+    p += delta_round(n * sizeof(double));
     a.cuts = (int32_t *)p;
-    p += (n * sizeof(int32_t) + 255) / 256 * 256;
+    p += delta_round(n * sizeof(int32_t));
     a.maps = (float *)p;
     a.adds = a.maps + n * D * D;
+}
+
+template <int D>
+static void start_join(const DeltaArgs &a, bool backward, hipStream_t s)
+{
+    const unsigned heads = (unsigned)(a.B * a.H);
+    DeltaJoin j = {};
+    j.maps = a.maps;
+    j.adds = a.adds;
+    j.cuts = a.cuts;
+    j.n = a.segments;
+    j.backward = backward;
+    j.first = backward ? a.dh_last : a.h0;
+    j.dk = a.dk;
+    j.dv = a.dv;
+    const unsigned blocks = delta_blocks(a.segments, j.per);
+    if (blocks > 1) {
+        const size_t n = (size_t)blocks * heads;
+        char *p = (char *)(a.adds + (size_t)a.segments * heads * D * D);
+        j.block_cuts = (int32_t *)p;
+        j.block_maps = (float *)(p + delta_round(n * sizeof(int32_t)));
+        j.block_adds = j.block_maps + n * D * D;
+        hipLaunchKernelGGL((delta_join_kernel<D, true>), dim3(heads, D / 8, blocks - 1), dim3(256), 0, s, j);
+        DeltaJoin o = j;
+        o.maps = j.block_maps;
+        o.adds = j.block_adds;
+        o.cuts = j.block_cuts;
+        o.n = o.per = blocks;
+        o.backward = false;
+        hipLaunchKernelGGL((delta_join_kernel<D, false>), dim3(heads, D / 16), dim3(256), 0, s, o);
+        j.starts = j.block_adds;
+    }
+    hipLaunchKernelGGL((delta_join_kernel<D, false>), dim3(heads, D / 16, blocks), dim3(256), 0, s, j);
 }
 
 hipError_t launch_delta_join(const DeltaArgs &a, bool backward, hipStream_t s)
 {
     const int D = delta_width(a.dk, a.dv);
-    void (*kernel)(DeltaArgs, bool) = D == 32 ? delta_join_kernel<32> : D == 64 ? delta_join_kernel<64>
-                                                                                : delta_join_kernel<128>;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)(a.B * a.H), D / 16), dim3(256), 0, s, a, backward);
+    if (D == 32) start_join<32>(a, backward, s);
+    else if (D == 64) start_join<64>(a, backward, s);
+    else start_join<128>(a, backward, s);
     return hipGetLastError();
 }
 

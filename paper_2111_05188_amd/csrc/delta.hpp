@@ -442,10 +442,10 @@ enum : int { WANT_T = 1, WANT_PT = 2, WANT_P = 4 };
 // far as they are wanted).  L is nilpotent; its inverse grows from blocks of 1, 2, 4,
 // 8 on the diagonal: T <- T - T L_off T with the part of L that joins two blocks, so
 // no power of L is formed whose entries cancel.  Rows past the piece's end have
-// length 0 and no decay; one: they may hold a NaN, and only the first row counts.
+// length 0 and no decay, whatever LDS holds there: an output or a gradient may be a NaN.
 template <bool BF, int D, int LD, int WANT, bool BOTH, class E>
 __device__ __forceinline__ void piece_triangles(const E *q, const E *k, const float *g, const float *beta, int s,
-                                                int count, bool one, int lane, double *cum, PieceRows *rows,
+                                                int count, int lane, double *cum, PieceRows *rows,
                                                 floatx4 &Tt, floatx4 &Tn, floatx4 &Pt, floatx4 &Pn)
 {
     constexpr float EPS = 1e-6f;
@@ -463,10 +463,10 @@ __device__ __forceinline__ void piece_triangles(const E *q, const E *k, const fl
     }
     const float be = (WANT & WANT_T) && n < count ? beta[s + n] : 0.0f;
     const double c = piece_sums(g + s, count, lane, cum);
-    if (one) {
+    if (count < 16) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const bool it = r + i == 0 && n == 0;
+            const bool it = r + i < count && n < count;
             kk[i] = it ? kk[i] : 0.0f;
             qq[i] = it ? qq[i] : 0.0f;
             kq[i] = it ? kq[i] : 0.0f;

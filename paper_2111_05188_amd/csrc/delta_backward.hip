@@ -454,12 +454,12 @@ __global__ __launch_bounds__(4 * D, 2) void delta_bwd_kernel(DeltaArgs a)
                     const int c = piece_end(from, count, ends, single) - from;
                     floatx4 Tt, Tn, Pt, Pn;
                     if (j < NP) {
-                        piece_triangles<BF, D, LD, WANT_T, true>(sh.q, sh.k, sh.g, sh.beta, from, c, single, lane,
-                                                                sh.cum[j],                                                                 &sh.rows[j], Tt, Tn, Pt, Pn);
+                        piece_triangles<BF, D, LD, WANT_T, true>(sh.q, sh.k, sh.g, sh.beta, from, c, lane, sh.cum[j],
+                                                                 &sh.rows[j], Tt, Tn, Pt, Pn);
                         sh.m[p][0][lane] = Tn;
                         sh.m[p][1][lane] = Tt;
                     } else {
-                        piece_triangles<BF, D, LD, WANT_P | WANT_PT, true>(sh.q, sh.k, sh.g, sh.beta, from, c, single, lane,
+                        piece_triangles<BF, D, LD, WANT_P | WANT_PT, true>(sh.q, sh.k, sh.g, sh.beta, from, c, lane,
                                                                            sh.cum[j], (PieceRows *)sh.parts + p, Tt, Tn,
                                                                            Pt, Pn);
                         sh.P[p][lane] = Tile<BF>::split(Pn);
@@ -569,7 +569,8 @@ __global__ __launch_bounds__(4 * D, 2) void delta_bwd_kernel(DeltaArgs a)
                 const uint64_t m = lane < count ? ends >> lane : 0;
                 const int stop = m ? lane + __builtin_ctzll(m) : count - 1;
                 float acc = 0.0f;
-                if (single) {               // (a NaN stays in its episode)
+                // (a NaN or an infinity, from a state or a gradient too, stays in its episode)
+                if (__ballot(lane < count && !(fabsf(x) <= 3.4e38f))) {
                     for (int c = 0; c < count; ++c) acc += c >= lane && c <= stop ? sh.x[c] : 0.0f;
                 } else {                    // differences of sums from the first step, in 64 bits
                     const double sum = wave_inclusive_scan((double)x);
@@ -704,8 +705,9 @@ __global__ __launch_bounds__(4 * D, 2) void delta_bwd_map_kernel(DeltaArgs a)
                 const int from = piece(s, p);
                 if (from >= count) break;
                 floatx4 Tt, Tn, Pt, Pn;
-                piece_triangles<BF, D, LD, WANT_T | WANT_P, true>(q, k, sg, sbeta, from, piece_end(from, count, ends, single) - from,
-                                                 single, lane, cum[p], &rows[p], Tt, Tn, Pt, Pn);
+                piece_triangles<BF, D, LD, WANT_T | WANT_P, true>(q, k, sg, sbeta, from,
+                                                                  piece_end(from, count, ends, single) - from, lane,
+                                                                  cum[p], &rows[p], Tt, Tn, Pt, Pn);
                 sT[p][lane] = TL::split(Tn);
                 sP[p][lane] = TL::split(Pn);
             }

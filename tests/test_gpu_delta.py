@@ -176,6 +176,75 @@ def test_few_long_sequences(shape, dtype, done, ragged):
 
 
 @pytest.mark.parametrize("dtype", BOTH)
+@pytest.mark.parametrize("shape", [(3205, 1, 1, 32, 32), (4400, 2, 2, 16, 64), (3700, 1, 1, 128, 96)])
+@pytest.mark.parametrize("done,ragged", [(0.0, False), (0.001, True)])
+def test_very_long_sequences(shape, dtype, done, ragged):
+    """So many segments that their states are joined over blocks of them."""
+    say(f"[delta] very long {shape} {dtype}")
+    Case(*shape, dtype, done, ragged, seed=6).check()
+
+
+@pytest.mark.parametrize("dtype", BOTH)
+def test_a_bad_number_far_before_an_episodes_end(dtype):
+    """It stays in its episode, over segments and blocks of them; the states may be one buffer."""
+    T = 3800
+    c = Case(T, 1, 2, 32, 32, dtype, seed=15)
+    c.done = np.zeros((T, 1), np.uint8)
+    c.done[3000] = 1
+    c.setup()
+    y0, h0 = c.forward()
+    c.parts(c.rows)[2][500, 0, 1, 3] = float("nan")
+    y, state = torch.full_like(y0, 7.0), dev(c.h0)
+    tp.delta_forward(c.dc, *c.parts(c.rows), y, c.work, h0=state, h_last=state)
+    torch.cuda.synchronize()
+    y0, y, h0, h = host(y0), host(y), host(h0), host(state)
+    same = np.ones(y.shape, bool)
+    same[500:3001, 0, 1] = False
+    close("y", y[same], y0[same], 2 * TOL[dtype])
+    close("h_last", h, h0, 4e-5)
+    assert np.isnan(y[500:3001, 0, 1, 3]).all() and np.isfinite(y[500:3001, 0, 1, :3]).all()
+
+
+@pytest.mark.parametrize("dtype", BOTH)
+@pytest.mark.parametrize("T", [90, 900])
+def test_bad_states_stay_in_their_episodes(T, dtype):
+    """A NaN in the first states reaches the first episode, one in the last states' gradient the
+    last one: not the others', whose steps share groups and pieces of them."""
+    c = Case(T, 1, 2, 64, 48, dtype, seed=16)
+    ends = [T - 50, T - 30, T - 27, T - 3]
+    c.done = np.zeros((T, 1), np.uint8)
+    c.done[ends] = 1
+    c.setup()
+
+    def run():
+        saved = c.dc.saved()
+        y, last = c.forward(saved)
+        c.out.fill_(7.0)
+        _, dh0 = c.backward(saved)
+        torch.cuda.synchronize()
+        return [host(x) for x in (y, *c.parts(c.out), last, dh0)]
+
+    fine = run()
+    assert all(np.isfinite(x).all() for x in fine)
+    tol = 2 * TOL[dtype]
+    c.h0[0, 1, 5, 3], keep = np.nan, c.h0[0, 1, 5, 3]
+    got = run()
+    for name, x, y in zip(("y", "dq", "dk", "dv", "dr", "db"), got, fine):
+        close(name + " after", x[ends[0] + 1:], y[ends[0] + 1:], tol)
+        close(name + " of the other head", x[:, :, 0], y[:, :, 0], tol)
+    close("h_last", got[6], fine[6], tol)
+    assert np.isnan(got[0][:ends[0] + 1, 0, 1, 3]).all()
+    c.h0[0, 1, 5, 3] = keep
+    c.dh[0, 1, 5, 3] = np.nan
+    got = run()
+    for name, x, y in zip(("y", "dq", "dk", "dv", "dr", "db"), got, fine):
+        close(name + " before", x[:ends[-1] + 1], y[:ends[-1] + 1], tol)
+        close(name + " of the other head", x[:, :, 0], y[:, :, 0], tol)
+    close("dh0", got[7], fine[7], tol)
+    assert np.isnan(got[2][ends[-1] + 1:, 0, 1]).any()
+
+
+@pytest.mark.parametrize("dtype", BOTH)
 @pytest.mark.parametrize("done", [1.0, 0.5])
 @pytest.mark.parametrize("T", [1, 40, 75])
 def test_episodes_of_one_and_few_steps(T, done, dtype):
