@@ -429,10 +429,16 @@ void start_norm(NormArgs &a, bool backward, hipStream_t s)
         else start_norm<BF, V, 256, 4>(a, backward, s);
         return;
     }
+    // Element by element: 16-byte loads of rows that start anywhere, with the row's last
+    // vector ending with it, took 1.46 ms where this takes 0.93 (258,048 rows of 301 in fp32,
+    // with gradients; with registers for 512 channels in place of 320, 0.98).
     const int D = a.D;
     if (D <= 64) start_norm<BF, 1, 64, 1>(a, backward, s);
     else if (D <= 128) start_norm<BF, 1, 64, 2>(a, backward, s);
+    else if (D <= 192) start_norm<BF, 1, 64, 3>(a, backward, s);
     else if (D <= 256) start_norm<BF, 1, 64, 4>(a, backward, s);
+    else if (D <= 320) start_norm<BF, 1, 64, 5>(a, backward, s);
+    else if (D <= 384) start_norm<BF, 1, 64, 6>(a, backward, s);
     else if (D <= 512) start_norm<BF, 1, 64, 8>(a, backward, s);
     else if (D <= 1024) start_norm<BF, 1, 256, 4>(a, backward, s);
     else if (D <= 2048) start_norm<BF, 1, 256, 8>(a, backward, s);

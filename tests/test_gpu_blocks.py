@@ -98,6 +98,14 @@ def test_norms_and_gradients(size, dtype):
 
 
 @pytest.mark.parametrize("dtype", BOTH)
+@pytest.mark.parametrize("D,groups", [(129, 3), (191, 1), (193, 1), (255, 5), (257, 1), (319, 11), (321, 3),
+                                      (383, 1), (385, 7), (511, 7), (513, 27), (1025, 5), (2049, 3)])
+def test_rows_of_odd_lengths(D, groups, dtype):
+    """On both sides of what a lane's registers hold."""
+    Norm(13, D, groups, dtype, seed=D).check()
+
+
+@pytest.mark.parametrize("dtype", BOTH)
 @pytest.mark.parametrize("parts", [("x", "w_pre"), ("x",), ("x", "y"), ("x", "y", "z"),
                                    ("x", "y", "w_post"), ("x", "y", "scale", "w_pre"),
                                    ("x", "y", "z", "w_post", "w_pre")])
