@@ -16,8 +16,8 @@
 // What a segment does to the state is linear: a first launch runs every segment on
 // no state, for what it adds, and without values on the unit states, for its map;
 // then each segment's first state comes from them, one product a segment, or, for many,
-// over blocks of them.  24,570 steps of 4 heads of 128 in bf16: 285 us (6.6 ms
-// without segments), of which maps 107, join 100, outputs 93; each of the three
+// over blocks of them.  24,570 steps of 4 heads of 128 in bf16: 275 us (6.6 ms
+// without segments), of which maps 106, join 86, outputs 92; each of the three
 // is a chain, of six groups of 64 steps or of eight segments' maps at a time.
 #include "delta.hpp"
 
@@ -284,12 +284,12 @@ struct DeltaJoin {
     int32_t *block_cuts;
 };
 
-// A workgroup has 16 columns of one head's states, wave w the rows 16w.., 16(w+4).. of
+// A workgroup has 16 columns of one head's states, wave w the rows 16w.. of
 // them; all waves read all rows of the state before from LDS.
 template <int D, bool FOLD>
-__global__ __launch_bounds__(256) void delta_join_kernel(DeltaJoin a)
+__global__ __launch_bounds__(4 * D) void delta_join_kernel(DeltaJoin a)
 {
-    constexpr int KT = D / 16, MINE = (KT + 3) / 4;
+    constexpr int KT = D / 16;
     __shared__ floatx4 state[2][KT][64];
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int n = lane & 15, r4 = 4 * (lane >> 4), heads = gridDim.x;
@@ -298,20 +298,18 @@ __global__ __launch_bounds__(256) void delta_join_kernel(DeltaJoin a)
     const int from = blockIdx.z * a.per, count = a.n - from < a.per ? a.n - from : a.per;
     const int64_t block = ((int64_t)blockIdx.z * heads + blockIdx.x) * D * D;
     const int64_t st = (int64_t)blockIdx.x * a.dk * a.dv;
-    floatx4 S[MINE];
+    floatx4 S;
 #pragma unroll
-    for (int j = 0; j < MINE; ++j)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int row = 16 * (w + 4 * j) + r4 + i;
-            if constexpr (FOLD) S[j][i] = unit && row == col ? 1.0f : 0.0f;
-            else if (a.starts) S[j][i] = row < D ? a.starts[block + row * D + col] : 0.0f;
-            else S[j][i] = a.first && row < a.dk && col < a.dv ? a.first[st + (int64_t)row * a.dv + col] : 0.0f;
-        }
+    for (int i = 0; i < 4; ++i) {
+        const int row = 16 * w + r4 + i;
+        if constexpr (FOLD) S[i] = unit && row == col ? 1.0f : 0.0f;
+        else if (a.starts) S[i] = a.starts[block + row * D + col];
+        else S[i] = a.first && row < a.dk && col < a.dv ? a.first[st + (int64_t)row * a.dv + col] : 0.0f;
+    }
     // products: of all segments but, where nothing follows, the last
     const int steps = FOLD ? count : count - 1;
     struct Segment {
-        floatx4 add[MINE], map[MINE][KT];
+        floatx4 add, map[KT];
         int cut;
     };
     auto place = [&](int x) {
@@ -322,47 +320,33 @@ __global__ __launch_bounds__(256) void delta_join_kernel(DeltaJoin a)
         const int64_t at = place(x) * D * D;
         g.cut = a.cuts[place(x)];
 #pragma unroll
-        for (int j = 0; j < MINE; ++j) {
-            const int t = w + 4 * j;
-            if (t >= KT) continue;
+        for (int i = 0; i < 4; ++i) g.add[i] = unit ? 0.0f : a.adds[at + (16 * w + r4 + i) * D + col];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) g.add[j][i] = unit ? 0.0f : a.adds[at + (16 * t + r4 + i) * D + col];
-#pragma unroll
-            for (int kt = 0; kt < KT; ++kt)
-                g.map[j][kt] = *(const floatx4 *)(a.maps + at + (16 * t + n) * D + 16 * kt + r4);
-        }
+        for (int kt = 0; kt < KT; ++kt)
+            g.map[kt] = *(const floatx4 *)(a.maps + at + (16 * w + n) * D + 16 * kt + r4);
     };
     bool cut = false;
     // the state before segment x goes to its place; the one after it, with the loads of
     // the next but one on their way
     auto step = [&](int x, Segment &g) {
         const int64_t at = place(x) * D * D;
+        if constexpr (!FOLD) {
 #pragma unroll
-        for (int j = 0; j < MINE; ++j) {
-            const int t = w + 4 * j;
-            if (t >= KT) continue;
-            if constexpr (!FOLD) {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) a.adds[at + (16 * t + r4 + i) * D + col] = S[j][i];
-            }
-            state[x & 1][t][lane] = S[j];
+            for (int i = 0; i < 4; ++i) a.adds[at + (16 * w + r4 + i) * D + col] = S[i];
         }
+        state[x & 1][w][lane] = S;
         if (x >= steps) return;
         cut = cut || g.cut != 0;
         workgroup_lds_barrier();
+        S = g.add;
+        floatx4 half = {};                  // (two chains of products)
+        if (g.cut == 0)
 #pragma unroll
-        for (int j = 0; j < MINE; ++j) {
-            if (w + 4 * j >= KT) continue;
-            S[j] = g.add[j];
-            floatx4 half = {};              // (two chains of products)
-            if (g.cut == 0)
-#pragma unroll
-                for (int kt = 0; kt < KT; kt += 2) {
-                    S[j] = Tile<false>::mm(g.map[j][kt], state[x & 1][kt][lane], S[j]);
-                    half = Tile<false>::mm(g.map[j][kt + 1], state[x & 1][kt + 1][lane], half);
-                }
-            S[j] += half;
-        }
+            for (int kt = 0; kt < KT; kt += 2) {
+                S = Tile<false>::mm(g.map[kt], state[x & 1][kt][lane], S);
+                half = Tile<false>::mm(g.map[kt + 1], state[x & 1][kt + 1][lane], half);
+            }
+        S += half;
         if (x + 2 < steps) fetch(x + 2, g);
     };
     Segment even, odd;
@@ -375,12 +359,7 @@ __global__ __launch_bounds__(256) void delta_join_kernel(DeltaJoin a)
     if constexpr (FOLD) {
         float *to = (unit ? a.block_maps : a.block_adds) + block;
 #pragma unroll
-        for (int j = 0; j < MINE; ++j) {
-            const int t = w + 4 * j;
-            if (t >= KT) continue;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) to[(16 * t + r4 + i) * D + col] = S[j][i];
-        }
+        for (int i = 0; i < 4; ++i) to[(16 * w + r4 + i) * D + col] = S[i];
         if (blockIdx.y == 0 && threadIdx.x == 0) a.block_cuts[(int64_t)blockIdx.z * heads + blockIdx.x] = cut;
     }
 }
@@ -610,26 +589,25 @@ static void start_join(const DeltaArgs &a, bool backward, hipStream_t s)
         j.block_cuts = (int32_t *)p;
         j.block_maps = (float *)(p + delta_round(n * sizeof(int32_t)));
         j.block_adds = j.block_maps + n * D * D;
-        hipLaunchKernelGGL((delta_join_kernel<D, true>), dim3(heads, D / 8, blocks - 1), dim3(256), 0, s, j);
+        hipLaunchKernelGGL((delta_join_kernel<D, true>), dim3(heads, D / 8, blocks - 1), dim3(4 * D), 0, s, j);
         DeltaJoin o = j;
         o.maps = j.block_maps;
         o.adds = j.block_adds;
         o.cuts = j.block_cuts;
         o.n = o.per = blocks;
         o.backward = false;
-        hipLaunchKernelGGL((delta_join_kernel<D, false>), dim3(heads, D / 16), dim3(256), 0, s, o);
+        hipLaunchKernelGGL((delta_join_kernel<D, false>), dim3(heads, D / 16), dim3(4 * D), 0, s, o);
         j.starts = j.block_adds;
     }
-    hipLaunchKernelGGL((delta_join_kernel<D, false>), dim3(heads, D / 16, blocks), dim3(256), 0, s, j);
+    hipLaunchKernelGGL((delta_join_kernel<D, false>), dim3(heads, D / 16, blocks), dim3(4 * D), 0, s, j);
 }
 
-hipError_t launch_delta_join(const DeltaArgs &a, bool backward, hipStream_t s)
+void launch_delta_join(const DeltaArgs &a, bool backward, hipStream_t s)
 {
     const int D = delta_width(a.dk, a.dv);
     if (D == 32) start_join<32>(a, backward, s);
     else if (D == 64) start_join<64>(a, backward, s);
     else start_join<128>(a, backward, s);
-    return hipGetLastError();
 }
 
 template <bool BF>

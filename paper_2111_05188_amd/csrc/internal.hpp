@@ -271,7 +271,7 @@ bool delta_fits(int T, int B, int H);
 // segments of a call and the workspace's parts; the first states of the segments
 // from their maps (of the gradient: from the last segment to the first)
 void delta_carve(DeltaArgs &a);
-hipError_t launch_delta_join(const DeltaArgs &a, bool backward, hipStream_t s);
+void launch_delta_join(const DeltaArgs &a, bool backward, hipStream_t s);
 hipError_t launch_delta_forward(DeltaArgs &a, hipStream_t s);
 hipError_t launch_delta_backward(DeltaArgs &a, hipStream_t s);
 hipError_t launch_delta_step(DeltaArgs &a, hipStream_t s);
