@@ -705,7 +705,7 @@ int tp_mx4_linear(const void *x, int32_t x_dtype, int64_t M, int64_t ldx, const 
 typedef struct tp_delta {
     int32_t T;             /* steps, >= 1                                    */
     int32_t B;             /* sequences, >= 1                                */
-    int32_t H;             /* heads, >= 1; B * H <= 2^23                     */
+    int32_t H;             /* heads, >= 1; B * H < 2^23                      */
     int32_t dk, dv;        /* channels of a head's keys and values, 1 .. 128 */
     int32_t dtype;         /* of q, k, v, r, b, y and their gradients        */
     const float *lambda;   /* [H] decay parameters                           */

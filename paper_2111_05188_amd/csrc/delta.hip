@@ -201,7 +201,7 @@ __global__ __launch_bounds__(4 * D, D == 128 ? 2 : 3) void delta_fwd_kernel(Delt
                     for (int j = 0; j < p && from < count; ++j) from = piece_end(from, count, ends, single);
                     if (from >= count) break;
                     floatx4 Tt, Tn, Pt, Pn;
-                    piece_triangles<BF, D, LD, MAP ? WANT_T : WANT_T | WANT_PT, false>(MAP ? k : q, k, sg, sbeta, from,
+                    piece_triangles<BF, D, LD, WANT_ROWS | (MAP ? WANT_T : WANT_T | WANT_PT), false>(MAP ? k : q, k, sg, sbeta, from,
                                                       piece_end(from, count, ends, single) - from, lane, cum[p],
                                                       &rows[p], Tt, Tn, Pt, Pn);
                     sT[p][lane] = Tt;
@@ -510,8 +510,8 @@ void start_step(DeltaArgs &a, hipStream_t s)
 
 bool delta_fits(int T, int B, int H)
 {
-    // steps past the last group and the heads of all sequences in 32 bits
-    return T <= 1 << 30 && (int64_t)B * H <= (int64_t)1 << 23;
+    // steps past the last group, and the threads of all sequences' heads, in 32 bits
+    return T <= 1 << 30 && (int64_t)B * H < (int64_t)1 << 23;
 }
 
 size_t delta_saved_bytes(int T, int B, int H, int dk, int dv)

@@ -387,11 +387,9 @@ __device__ __forceinline__ float delta_gate(const char *p, bool bf)
 
 // scalars of a piece's rows, and the decay over all of it
 struct __attribute__((aligned(16))) PieceRows {
-    float fade[16];             // gamma_c
-    float rest[16];             // gamma_C / gamma_c
     float beta[16];
     float rq[16], rk[16];
-    float aq[16], ak[16], au[16];   // gamma rq, beta gamma rk, rest rk
+    float aq[16], ak[16], au[16];   // gamma rq, beta gamma rk, (gamma_C / gamma) rk
     float total;
 };
 
@@ -435,8 +433,9 @@ __device__ __forceinline__ double piece_sums(const float *g, int count, int lane
     return c;
 }
 
-// What one wave prepares of a piece; the rows' scalars come along.
-enum : int { WANT_T = 1, WANT_PT = 2, WANT_P = 4 };
+// What one wave prepares of a piece.  (`rows` has the rows' scalars with WANT_ROWS, else
+// it is the wave's own while it works.)
+enum : int { WANT_T = 1, WANT_PT = 2, WANT_P = 4, WANT_ROWS = 8 };
 
 // K K^T and Q K^T tiles of a piece, the rows' lengths, T and P in both layouts (as
 // far as they are wanted).  L is nilpotent; its inverse grows from blocks of 1, 2, 4,
@@ -450,18 +449,19 @@ __device__ __forceinline__ void piece_triangles(const E *q, const E *k, const fl
 {
     constexpr float EPS = 1e-6f;
     lane = fresh(lane);
+    constexpr bool Q = (WANT & (WANT_P | WANT_PT | WANT_ROWS)) != 0, B = (WANT & (WANT_T | WANT_ROWS)) != 0;
     const int n = lane & 15, grp = lane >> 4, r = 4 * grp;
     floatx4 kk = {}, qq = {}, kq = {}, qk = {};
 #pragma unroll
     for (int kt = 0; kt < D / 16; kt += 2) {
-        const auto a0 = along_row<BF, LD>(k, s, kt, lane), b0 = along_row<BF, LD>(q, s, kt, lane);
-        const auto a1 = along_row<BF, LD>(k, s, kt + 1, lane), b1 = along_row<BF, LD>(q, s, kt + 1, lane);
+        const auto a0 = along_row<BF, LD>(k, s, kt, lane), b0 = along_row<BF, LD>(Q ? q : k, s, kt, lane);
+        const auto a1 = along_row<BF, LD>(k, s, kt + 1, lane), b1 = along_row<BF, LD>(Q ? q : k, s, kt + 1, lane);
         kk = Tile<BF>::mm2(a0, a1, a0, a1, kk);
-        qq = Tile<BF>::mm2(b0, b1, b0, b1, qq);
+        if constexpr (Q) qq = Tile<BF>::mm2(b0, b1, b0, b1, qq);
         if constexpr (WANT & WANT_P) qk = Tile<BF>::mm2(b0, b1, a0, a1, qk);
         if constexpr (WANT & WANT_PT) kq = Tile<BF>::mm2(a0, a1, b0, b1, kq);
     }
-    const float be = (WANT & WANT_T) && n < count ? beta[s + n] : 0.0f;
+    const float be = B && n < count ? beta[s + n] : 0.0f;
     const double c = piece_sums(g + s, count, lane, cum);
     if (count < 16) {
 #pragma unroll
@@ -478,26 +478,26 @@ __device__ __forceinline__ void piece_triangles(const E *q, const E *k, const fl
         const float dk = n & 2 ? (n & 1 ? kk[3] : kk[2]) : (n & 1 ? kk[1] : kk[0]);
         const float dq = n & 2 ? (n & 1 ? qq[3] : qq[2]) : (n & 1 ? qq[1] : qq[0]);
         rows->rk[n] = n < count ? __builtin_amdgcn_rsqf(dk + EPS) : 0.0f;
-        rows->rq[n] = n < count ? __builtin_amdgcn_rsqf(dq + EPS) : 0.0f;
-        if constexpr (WANT & WANT_T) rows->beta[n] = be;
+        if constexpr (Q) rows->rq[n] = n < count ? __builtin_amdgcn_rsqf(dq + EPS) : 0.0f;
+        if constexpr (B) rows->beta[n] = be;
     }
     const floatx4 fade = piece_decays(cum, lane);
     wave_lds_fence();
     const float rkn = rows->rk[n], rqn = rows->rq[n];
     const floatx4 rkr = *(const floatx4 *)(rows->rk + r), rqr = *(const floatx4 *)(rows->rq + r);
-    if constexpr (WANT & WANT_T) {
-        const floatx4 ber = *(const floatx4 *)(rows->beta + r);
+    if constexpr (WANT & WANT_ROWS) {
         if (lane < 16) {
             const double all = cum[15];
             const float since = n < count ? delta_exp((float)c) : 0.0f;
             const float rest = n < count ? delta_exp((float)(all - c)) : 0.0f;
-            rows->fade[n] = since;
-            rows->rest[n] = rest;
             if (n == 0) rows->total = delta_exp((float)all);
             rows->aq[n] = since * rqn;
             rows->ak[n] = be * since * rkn;
             rows->au[n] = rest * rkn;
         }
+    }
+    if constexpr (WANT & WANT_T) {
+        const floatx4 ber = *(const floatx4 *)(rows->beta + r);
         const bool same4 = grp == n >> 2, same8 = grp >> 1 == n >> 3;
         floatx4 Lt, off;
 #pragma unroll

@@ -68,7 +68,7 @@ struct Back {
     };
     static_assert(16 * LD * sizeof(E) <= sizeof(Shared::parts), "rows past v's end");
     static_assert(sizeof(pair) == sizeof(floatx4), "triangles' gradients");
-    static_assert(sizeof(PieceRows) % 16 == 0 && NP * sizeof(PieceRows) <= sizeof(Shared::parts), "P's rows");
+    static_assert(sizeof(PieceRows) % 16 == 0 && NP * sizeof(PieceRows) <= sizeof(Shared::parts), "T's rows");
     static_assert(sizeof(Shared) <= LDS_LIMIT, "LDS");
 
     // f(i) for the rows 4g + i that a piece has.  (PART, here and below: a piece of fewer
@@ -453,7 +453,7 @@ __global__ __launch_bounds__(4 * D, 2) void delta_bwd_kernel(DeltaArgs a)
                 while (p-- > 0 && s < count) s = piece_end(s, count, ends, single);
                 return s;
             };
-            // T, then P of each piece, a wave each (P's has its rows where the parts will be)
+            // T, then P of each piece, a wave each (T's has its rows where the parts will be)
             auto prepare = [&](int s) {
                 for (int j = w; j < 2 * NP; j += NW) {
                     const int p = j % NP, from = piece(s, p);
@@ -462,13 +462,12 @@ __global__ __launch_bounds__(4 * D, 2) void delta_bwd_kernel(DeltaArgs a)
                     floatx4 Tt, Tn, Pt, Pn;
                     if (j < NP) {
                         piece_triangles<BF, D, LD, WANT_T, true>(sh.q, sh.k, sh.g, sh.beta, from, c, lane, sh.cum[j],
-                                                                 &sh.rows[j], Tt, Tn, Pt, Pn);
+                                                                 (PieceRows *)sh.parts + p, Tt, Tn, Pt, Pn);
                         sh.m[p][0][lane] = Tn;
                         sh.m[p][1][lane] = Tt;
                     } else {
-                        piece_triangles<BF, D, LD, WANT_P | WANT_PT, true>(sh.q, sh.k, sh.g, sh.beta, from, c, lane,
-                                                                           sh.cum[j], (PieceRows *)sh.parts + p, Tt, Tn,
-                                                                           Pt, Pn);
+                        piece_triangles<BF, D, LD, WANT_ROWS | WANT_P | WANT_PT, true>(
+                            sh.q, sh.k, sh.g, sh.beta, from, c, lane, sh.cum[j], &sh.rows[p], Tt, Tn, Pt, Pn);
                         sh.P[p][lane] = Tile<BF>::split(Pn);
                         sh.m[p][2][lane] = Pt;
                     }
@@ -712,7 +711,7 @@ __global__ __launch_bounds__(4 * D, 2) void delta_bwd_map_kernel(DeltaArgs a)
                 const int from = piece(s, p);
                 if (from >= count) break;
                 floatx4 Tt, Tn, Pt, Pn;
-                piece_triangles<BF, D, LD, WANT_T | WANT_P, true>(q, k, sg, sbeta, from,
+                piece_triangles<BF, D, LD, WANT_ROWS | WANT_T | WANT_P, true>(q, k, sg, sbeta, from,
                                                                   piece_end(from, count, ends, single) - from, lane,
                                                                   cum[p], &rows[p], Tt, Tn, Pt, Pn);
                 sT[p][lane] = TL::split(Tn);
