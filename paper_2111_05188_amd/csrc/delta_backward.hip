@@ -63,6 +63,7 @@ struct Back {
         double cum[2 * NP][16];
         float g[G], beta[G], shut[G], idle[G];              // 1 - sigmoid(r), 1 - beta
         float x[G], dbeta[G];
+        __attribute__((aligned(16))) float along[NP][2][16];    // q^.dq^, k^.dk^
         float ends[NW];                                     // <G, S> of a wave's columns
         int odd[2];
     };
@@ -304,20 +305,31 @@ struct Back {
         }
     }
 
+    // q^.dq^ = y.dy (turn 0) or k^.dk^ = 2 dR.u - v.dv of a piece's rows
+    static __device__ __forceinline__ void lengths(Shared &sh, int s, int count, int p, int turn, int lane)
+    {
+        if (lane >= count) return;
+        const float (*x)[NW] = sh.sums[s + lane];
+        sh.along[p][turn][lane] = turn == 0 ? total(x[0]) : 2.0f * total(x[2]) - total(x[1]);
+    }
+
     // What is summed of a piece on its keys' columns 16w..
     struct Sums {
         floatx4 dq, dk;
     };
     template <bool PART>
-    static __device__ __forceinline__ void collect(Shared &sh, int count, int p, int turn, int w, int lane, Sums &t)
+    static __device__ __forceinline__ void collect(Shared &sh, int s, int count, int p, int turn, int w, int lane,
+                                                   Sums &t)
     {
         lane = fresh(lane);
         (turn == 0 ? t.dq : t.dk) = take(sh, TURNS == 1 ? turn * HALF + w : w, lane);
-        if (w == (2 * p + turn) % NW) triangle<PART>(sh, count, p, turn, lane);
+        if (w == (2 * p + turn) % NW) {
+            lengths(sh, s, count, p, turn, lane);
+            triangle<PART>(sh, count, p, turn, lane);
+        }
     }
 
-    // rq (dq^ - q^ (q^.dq^)) in place of q, and the same of k, with q^.dq^ = y.dy and
-    // k^.dk^ = 2 dR.u - v.dv.
+    // rq (dq^ - q^ (q^.dq^)) in place of q, and the same of k.
     template <bool PART>
     static __device__ __forceinline__ void finish(Shared &sh, int s, int count, int p, int w, int lane,
                                                   const Sums &t)
@@ -331,13 +343,7 @@ struct Back {
         const floatx4 aq = *(const floatx4 *)(rows.aq + r);
         const pair m = *(const pair *)&sh.m[p][0][lane], mt = *(const pair *)&sh.m[p][1][lane];
         const pair l = *(const pair *)&sh.m[p][2][lane];
-        floatx4 yd, kd;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {           // (rows past the group's are not there)
-            const float (*x)[NW] = sh.sums[s + r + i < G ? s + r + i : G - 1];
-            yd[i] = total(x[0]);
-            kd[i] = 2.0f * total(x[2]) - total(x[1]);
-        }
+        const floatx4 yd = *(const floatx4 *)(sh.along[p][0] + r), kd = *(const floatx4 *)(sh.along[p][1] + r);
         floatx4 a, b = t.dk;
 #pragma unroll
         for (int i = 0; i < 4; ++i) a[i] = aq[i] * t.dq[i];
@@ -542,8 +548,8 @@ __global__ __launch_bounds__(4 * D, 2) void delta_bwd_kernel(DeltaArgs a)
                         if (x == 1 && p == 0 && batch == 0 && grp > first) fetch(grp - 1);
                         workgroup_lds_barrier();
                         pieces_of(c, [&](auto m) {
-                            if (BK::TURNS == 1) BK::template collect<decltype(m)::value>(sh, c, p, 0, w, lane, t[p]);
-                            BK::template collect<decltype(m)::value>(sh, c, p, x, w, lane, t[p]);
+                            if (BK::TURNS == 1) BK::template collect<decltype(m)::value>(sh, at[p], c, p, 0, w, lane, t[p]);
+                            BK::template collect<decltype(m)::value>(sh, at[p], c, p, x, w, lane, t[p]);
                         });
                         if (x == 0) workgroup_lds_barrier();
                     }
