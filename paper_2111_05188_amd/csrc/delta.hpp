@@ -531,14 +531,22 @@ __device__ __forceinline__ void piece_triangles(const E *q, const E *k, const fl
     }
 }
 
-// Sum over the 16 lanes of a row group, in all of them (rotations within the row).
-__device__ __forceinline__ float row_sum(float x)
+template <int CTRL>
+__device__ __forceinline__ float dpp(float x)
 {
-    x += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x128, 0xF, 0xF, false));
-    x += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x124, 0xF, 0xF, false));
-    x += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x122, 0xF, 0xF, false));
-    x += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x121, 0xF, 0xF, false));
-    return x;
+    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), CTRL, 0xF, 0xF, false));
+}
+
+// Sums over the 16 lanes of a row group: lane n gets that of x[n % 4].  (Lanes swap halves
+// of what they have, so that the four sums go on in one register.)
+__device__ __forceinline__ float row_sums(floatx4 x, int lane)
+{
+    const bool odd = lane & 1, upper = lane & 2;
+    const float a = (odd ? x[1] : x[0]) + dpp<0xB1>(odd ? x[0] : x[1]);
+    const float b = (odd ? x[3] : x[2]) + dpp<0xB1>(odd ? x[2] : x[3]);
+    float c = (upper ? b : a) + dpp<0x4E>(upper ? a : b);
+    c += dpp<0x124>(c);
+    return c + dpp<0x128>(c);
 }
 
 // The next piece from step s of a group of `count` steps: it ends with a whole

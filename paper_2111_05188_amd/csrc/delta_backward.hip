@@ -146,10 +146,9 @@ struct Back {
             o = Tile<false>::mm(P, U, o);
             const floatx4 dy = TL::wide(dyc);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) t[i] = row_sum(o[i] * dy[i]);
-            each_row<PART>(count, r, [&](int i) {
-                if ((lane & 15) == 0) sh.sums[s + r + i][0][w] = t[i];
-            });
+            for (int i = 0; i < 4; ++i) t[i] = o[i] * dy[i];
+            const float sum = row_sums(t, lane);
+            if ((lane & 15) < 4 && (!PART || r + (lane & 3) < count)) sh.sums[s + r + (lane & 3)][0][w] = sum;
         }
         return U;
     }
@@ -216,20 +215,21 @@ struct Back {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             dv[i] = be[i] * dR[i];
-            t[i] = row_sum(vw[i] * dv[i]);
-            u[i] = row_sum(dR[i] * U[i]);
+            t[i] = vw[i] * dv[i];
+            u[i] = dR[i] * U[i];
         }
+        const float vd = row_sums(t, lane), ru = row_sums(u, lane);
         mine.U = TL::turned(TL::part(U), eye);
         mine.dR = TL::turned(TL::part(dR), eye);
         mine.ak = ak;
         mine.au = au;
         each_row<PART>(count, r, [&](int i) {
             sh.v[(s + r + i) * LD + col] = (E)dv[i];
-            if ((lane & 15) == 0) {
-                sh.sums[s + r + i][1][w] = t[i];
-                sh.sums[s + r + i][2][w] = u[i];
-            }
         });
+        if ((lane & 15) < 4 && (!PART || r + (lane & 3) < count)) {
+            sh.sums[s + r + (lane & 3)][1][w] = vd;
+            sh.sums[s + r + (lane & 3)][2][w] = ru;
+        }
         return mine;
     }
 
