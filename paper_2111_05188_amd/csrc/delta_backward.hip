@@ -419,9 +419,9 @@ __global__ __launch_bounds__(4 * D, 2) void delta_bwd_kernel(DeltaArgs a)
         RW::fetch(a.k, RW::at(a.k, b, h, t0, tid), count, a.dk, tid, fk);
         RW::fetch(a.v, RW::at(a.v, b, h, t0, tid), count, a.dv, tid, fv);
         RW::fetch(a.dy, RW::at(a.dy, b, h, t0, tid), count, a.dv, tid, fy);
-        if ((int)threadIdx.x < count) {
-            fr = delta_gate((char *)a.r.p + b * a.r.sb + h * a.r.sh + (t0 + tid) * a.r.st, BF);
-            fb = delta_gate((char *)a.b.p + b * a.b.sb + h * a.b.sh + (t0 + tid) * a.b.st, BF);
+        if (lane < count) {                     // (every wave: each takes some of the gates)
+            fr = delta_gate((char *)a.r.p + b * a.r.sb + h * a.r.sh + (t0 + lane) * a.r.st, BF);
+            fb = delta_gate((char *)a.b.p + b * a.b.sb + h * a.b.sh + (t0 + lane) * a.b.st, BF);
         }
         fd = a.done && lane < count ? *(const TP_GLOBAL uint8_t *)(a.done + (int64_t)(t0 + lane) * a.B + b) : 0;
         load_state(grp);
@@ -436,12 +436,14 @@ __global__ __launch_bounds__(4 * D, 2) void delta_bwd_kernel(DeltaArgs a)
             float odd = RW::odd(fq) + RW::odd(fk) + RW::odd(fv) + RW::odd(fy);
             workgroup_lds_barrier();                // (the group before is done with)
             const int tid = fresh(threadIdx.x);
-            if ((int)threadIdx.x < count) {
-                const float g = rate * delta_sigmoid(fr);
-                sh.g[threadIdx.x] = g < -3e38f ? -3e38f : g;
-                sh.beta[threadIdx.x] = delta_sigmoid(fb);
-                sh.shut[threadIdx.x] = delta_sigmoid(-fr);
-                sh.idle[threadIdx.x] = delta_sigmoid(-fb);
+            if (lane < count) {
+                if (w == 0) {
+                    const float g = rate * delta_sigmoid(fr);
+                    sh.g[lane] = g < -3e38f ? -3e38f : g;
+                }
+                if (w == 1) sh.beta[lane] = delta_sigmoid(fb);
+                if (w == 2 % NW) sh.shut[lane] = delta_sigmoid(-fr);
+                if (w == 3 % NW) sh.idle[lane] = delta_sigmoid(-fb);
                 odd += (fr + fb) * 0.0f;
             }
             RW::put(sh.q, fq, tid);

@@ -136,3 +136,9 @@ def test_the_binding_checks_shapes_and_types():
         tp.delta_step(q[0], q[0], v[0], r[0], r[0], torch.zeros(H + 1), h, h)
     with pytest.raises(tp.TPError):
         tp.DeltaT(torch.zeros(H), T, B, 129, dv, torch.float32)
+
+
+def test_the_launch_grid_is_not_overrun():
+    """2^23 heads of 128 channels would be 2^32 threads."""
+    for B, H in ((1 << 23, 1), (1 << 20, 8)):
+        _refused(_forward(_cfg(T=1, B=B, H=H)), "grid", tp.TP_EUNSUPPORTED)
