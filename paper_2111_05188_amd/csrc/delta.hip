@@ -7,16 +7,16 @@
 // prepares one piece of the group (its triangles, which do not need the state),
 // then all waves run the pieces on their columns.
 //
-// 390 steps of 4,096 sequences of 4 heads of 64 in bf16: 1.71 ms, 3.8 GB at 2.2 TB/s.
+// 390 steps of 4,096 sequences of 4 heads of 64 in bf16: 1.70 ms, 3.8 GB at 2.3 TB/s.
 // Vector instructions bound it (61% of the time, the matrix units another 28%), above
 // all the splits of the state into three bf16 numbers, once a piece.  Three workgroups a
-// CU; four (128 registers) or groups of 32 steps gain nothing (1.69 - 1.94 ms).
+// CU; four (128 registers) or groups of 32 steps gain nothing (1.69 - 1.94 ms), nor do gates shared out over the waves (1.76).
 //
 // Where few heads leave most CUs without work, a sequence is split into segments.
 // What a segment does to the state is linear: a first launch runs every segment on
 // no state, for what it adds, and without values on the unit states, for its map;
 // then each segment's first state comes from them, one product a segment, or, for many,
-// over blocks of them.  24,570 steps of 4 heads of 128 in bf16: 275 us (6.6 ms
+// over blocks of them.  24,570 steps of 4 heads of 128 in bf16: 270 us (6.6 ms
 // without segments), of which maps 106, join 86, outputs 92; each of the three
 // is a chain, of six groups of 64 steps or of eight segments' maps at a time.
 #include "delta.hpp"

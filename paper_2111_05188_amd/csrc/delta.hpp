@@ -22,7 +22,9 @@
 // writes go through many products one after the other, and keep fp32's precision
 // so (with two numbers states were off by 4e-6, lambda's gradient by 3e-5).  A
 // product over 16 fills half of the instruction's 32; where nothing else fits, the
-// half-rate product over 16 saves the copies that would fill it.
+// half-rate product over 16 saves the copies that would fill it.  T's and P's products
+// with what is no input run in fp32: as many cycles as those of three numbers by three,
+// and nothing to split.
 #pragma once
 
 #include "device.hpp"
@@ -138,12 +140,6 @@ template <> struct Tile<true> {
     {
         return go(a.hi, b, go(a.mid, b, go(a.lo, b, c)));
     }
-    static __device__ __forceinline__ floatx4 mm(val a, val b, floatx4 c)
-    {
-        c = go(a.lo, b.hi, go(a.hi, b.lo, c));
-        c = go(a.mid, b.hi, go(a.hi, b.mid, c));
-        return go(a.hi, b.hi, go(a.mid, b.mid, c));
-    }
     // Results that are rounded to bf16 next and feed nothing else take two numbers of
     // each operand, the second to nearest: 2^-16 of a value is lost.
     struct pair {
@@ -205,19 +201,9 @@ template <> struct Tile<true> {
         c = go(join(a0, a1), join(b0.mid, b1.mid), c);
         return go(join(a0, a1), join(b0.hi, b1.hi), c);
     }
-    static __device__ __forceinline__ floatx4 mm2(val a0, val a1, raw b0, raw b1, floatx4 c)
-    {
-        c = go(join(a0.lo, a1.lo), join(b0, b1), c);
-        c = go(join(a0.mid, a1.mid), join(b0, b1), c);
-        return go(join(a0.hi, a1.hi), join(b0, b1), c);
-    }
     static __device__ __forceinline__ floatx4 mm2(raw a0, raw a1, raw b0, raw b1, floatx4 c)
     {
         return go(join(a0, a1), join(b0, b1), c);
-    }
-    static __device__ __forceinline__ floatx4 mm2(val a0, val a1, val b0, val b1, floatx4 c)
-    {
-        return mm(a1, b1, mm(a0, b0, c));
     }
 };
 
@@ -391,10 +377,6 @@ struct __attribute__((aligned(16))) PieceRows {
     float rq[16], rk[16];
     float aq[16], ak[16], au[16];   // gamma rq, beta gamma rk, (gamma_C / gamma) rk
     float total;
-};
-
-struct GroupGates {             // of the steps of a group
-    float *g, *beta;
 };
 
 __device__ __forceinline__ float delta_softplus(float x)

@@ -21,14 +21,14 @@
 // wave multiplies its own, with its states transposed in registers (a product with the
 // unit matrix), and the parts meet in LDS, at waves that have columns 16w.. of the keys.
 // (States and gradients transposed through LDS, and whole sums in each wave, took six
-// barriers more: 4.90 ms where the below takes 4.59.)
+// barriers more: 4.90 ms where this took 4.76.)
 //
-// 390 steps of 2,048 sequences of 4 heads of 64 in bf16 take 4.59 ms with the forward
+// 390 steps of 2,048 sequences of 4 heads of 64 in bf16 take 4.34 ms with the forward
 // call, where the bytes (3.8 GB) take 0.8 at the rate of a copy.  A group of 32 steps
-// is 37,000 cycles of a workgroup, two of which a CU holds (72 KiB of LDS and 250
-// registers each); one alone still takes 32,000: what bounds it is the chain of products
+// is some 34,000 cycles of a workgroup, two of which a CU holds (71 KiB of LDS and 252
+// registers each); one alone is hardly faster: what bounds it is the chain of products
 // and splits of a wave, with the vector units at work 60% of the time and the matrix
-// units 26%.  Three workgroups (52 KiB, 168 registers) spill: 5.19 ms.
+// units 26%.  Three workgroups (51 KiB, 168 registers) spill: 5.19 ms against 4.74.
 #include "delta.hpp"
 
 namespace tpk {
@@ -648,7 +648,8 @@ __global__ __launch_bounds__(4 * D, 2) void delta_bwd_map_kernel(DeltaArgs a)
     typedef typename TL::val val;
     constexpr int LD = RW::LD;
     __shared__ __attribute__((aligned(16))) E buf[(3 * G + 16) * LD];
-    __shared__ val sT[NP][64], sP[NP][64];
+    __shared__ floatx4 sT[NP][64];
+    __shared__ val sP[NP][64];
     __shared__ __attribute__((aligned(16))) PieceRows rows[NP];
     __shared__ double cum[NP][16];
     __shared__ float sg[G], sbeta[G];
@@ -722,7 +723,7 @@ __global__ __launch_bounds__(4 * D, 2) void delta_bwd_map_kernel(DeltaArgs a)
                 piece_triangles<BF, D, LD, WANT_ROWS | WANT_T | WANT_P, true>(q, k, sg, sbeta, from,
                                                                   piece_end(from, count, ends, single) - from, lane,
                                                                   cum[p], &rows[p], Tt, Tn, Pt, Pn);
-                sT[p][lane] = TL::split(Tn);
+                sT[p][lane] = Tn;
                 sP[p][lane] = TL::split(Pn);
             }
             workgroup_lds_barrier();
@@ -751,8 +752,8 @@ __global__ __launch_bounds__(4 * D, 2) void delta_bwd_map_kernel(DeltaArgs a)
                     dM[i] = r4 + i < c ? km[i] * rows[p].au[r4 + i] : 0.0f;
                 }
                 dU = TL::mm(sP[p][lane], dyc, dU);
-                dR = TL::mm(sT[p][lane], TL::split(dU), dR);
-                dN = TL::mm(sT[p][lane], TL::split(dM), dN);
+                dR = Tile<false>::mm(sT[p][lane], dU, dR);
+                dN = Tile<false>::mm(sT[p][lane], dM, dN);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const float ak = rows[p].ak[r4 + i];
