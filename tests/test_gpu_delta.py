@@ -489,3 +489,88 @@ def test_refusals_on_the_gpu():
         tp.delta_forward(c.dc, *c.parts(c.rows), c.dy, c.work[:8])
     with pytest.raises(tp.TPError):
         tp.delta_forward(c.dc, *c.parts(c.rows), None, c.work)
+
+
+@pytest.mark.parametrize("dtype", BOTH)
+@pytest.mark.parametrize("what", range(6))
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+@pytest.mark.parametrize("T", [90, 800])
+def test_a_bad_numbers_gradients_stay_in_its_episode(what, bad, T, dtype):
+    """In an input or (5) dy: the gradients of other episodes, heads and sequences, and the first
+    states' of the others, are as without it."""
+    c = Case(T, 2, 2, 64, 64, dtype, seed=17)
+    first, last = T - 70, T - 30
+    c.done = np.zeros((T, 2), np.uint8)
+    c.done[[first, last], 0] = 1
+    c.setup()
+
+    def run():
+        saved = c.dc.saved()
+        c.forward(saved)
+        c.out.fill_(7.0)
+        dlam, dh0 = c.backward(saved)
+        torch.cuda.synchronize()
+        return [host(x) for x in (*c.parts(c.out), dh0, dlam)]
+
+    fine = run()
+    x = (*c.parts(c.rows), c.dy)[what]
+    x[T - 49, 0, 1] = bad
+    got = run()
+    for name, a, b in zip(("dq", "dk", "dv", "dr", "db"), got, fine):
+        same = np.ones(a.shape, bool)
+        same[first + 1:last + 1, 0, 1] = False
+        close(name, a[same], b[same], 2 * TOL[dtype])
+    close("dh0", got[5], fine[5], 4e-5)
+    close("dlam", got[6][:1], fine[6][:1], 4e-5)
+    if what in (0, 1, 2, 5):
+        assert not np.isfinite(got[1][first + 1:last + 1, 0, 1]).all()
+
+
+def test_two_calls_at_once_and_a_graph_of_many_segments():
+    cases = [Case(2000, 1, 2, 64, 64, torch.bfloat16, 0.002, seed=18),
+             Case(3600, 1, 1, 32, 64, torch.float32, 0.001, seed=19)]
+
+    def run(c, o):
+        tp.delta_forward(c.dc, *c.parts(c.rows), o["y"], c.work, h0=o["h0"], h_last=o["last"],
+                         saved=o["saved"])
+        tp.delta_backward(c.dc, *c.parts(c.rows), o["saved"], c.dy, *c.parts(c.out), o["dlam"], c.work,
+                          dh_last=o["dh"], dh0=o["dh0"])
+
+    outs, want = [], []
+    for c in cases:
+        h0 = dev(c.h0)
+        o = dict(y=torch.empty(c.T, c.B, c.H, c.dv, dtype=c.dtype, device="cuda"), h0=h0,
+                 last=torch.empty_like(h0), saved=c.dc.saved(), dh=dev(c.dh), dh0=torch.empty_like(h0),
+                 dlam=torch.empty(c.H, device="cuda"))
+        run(c, o)
+        outs.append(o)
+        want.append([o[k].clone() for k in ("y", "last", "dlam", "dh0")] + [c.out.clone()])
+    torch.cuda.synchronize()
+
+    def check(c, o, w):
+        got = [o[k] for k in ("y", "last", "dlam", "dh0")] + [c.out]
+        assert all(torch.equal(a, b) for a, b in zip(got, w))
+
+    streams = [torch.cuda.Stream() for _ in cases]
+    for _ in range(3):
+        for c, o, s in zip(cases, outs, streams):
+            c.out.zero_()
+            o["y"].zero_()
+            s.wait_stream(torch.cuda.current_stream())
+            with torch.cuda.stream(s):
+                run(c, o)
+        torch.cuda.synchronize()
+        for c, o, w in zip(cases, outs, want):
+            check(c, o, w)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        for c, o in zip(cases, outs):
+            run(c, o)
+    for _ in range(3):
+        for c, o in zip(cases, outs):
+            c.out.zero_()
+            o["y"].zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        for c, o, w in zip(cases, outs, want):
+            check(c, o, w)
