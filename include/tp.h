@@ -695,9 +695,9 @@ int tp_mx4_linear(const void *x, int32_t x_dtype, int64_t M, int64_t ldx, const 
  * hold there does not matter.
  * States, lambda and their gradients are fp32; q, k, v, r, b, y and their
  * gradients are all fp32 or all bf16 (rounded once, to nearest even).  Sums are
- * fp32; a bf16 call multiplies states, writes and their gradients as three bf16
- * numbers each, which lose nothing, and what only outputs in bf16 read as two (2^-16
- * of a value is lost).  q.q and k.k, and the states, have to be in fp32's range.
+ * fp32; a bf16 call multiplies states, writes and their gradients in fp32 or as three
+ * bf16 numbers each, which lose nothing.  q.q and k.k, and the states, have to be in
+ * fp32's range.
  * A NaN or an infinity in a step reaches y and the states from that step on, to
  * the episode's end, and the gradients that read them (r's up to 31 steps before);
  * one in h0 the first episode, one in dh_last the last.

@@ -45,7 +45,6 @@ template <> struct Tile<false> {
     typedef floatx4 raw;
     typedef floatx4 val;
     static constexpr int PAD = 4;               // elements after a row in LDS
-    template <bool NEAR = false>
     static __device__ __forceinline__ val split(floatx4 x) { return x; }
     static __device__ __forceinline__ floatx4 wide(raw x) { return x; }
     static __device__ __forceinline__ floatx4 mm(floatx4 a, floatx4 b, floatx4 c)
@@ -58,11 +57,7 @@ template <> struct Tile<false> {
     {
         return mm(a1, b1, mm(a0, b0, c));
     }
-    // what the results that feed nothing else need of a value
-    typedef floatx4 pair;
-    static __device__ __forceinline__ pair part(floatx4 x) { return x; }
-    static __device__ __forceinline__ floatx4 mm_out(val a, val b, floatx4 c) { return mm(a, b, c); }
-    static __device__ __forceinline__ pair head(val x) { return x; }
+    // The transposed tile: a product with the unit matrix, which loses nothing.
     static __device__ __forceinline__ raw eye(int lane)
     {
         raw x;
@@ -70,9 +65,7 @@ template <> struct Tile<false> {
         for (int i = 0; i < 4; ++i) x[i] = 4 * (lane >> 4) + i == (lane & 15) ? 1.0f : 0.0f;
         return x;
     }
-    static __device__ __forceinline__ pair turned(pair x, raw eye) { return mm(x, eye, floatx4{}); }
-    // of two tiles whose values are never in the same place (the others are zeros)
-    static __device__ __forceinline__ pair either(pair a, pair b) { return a + b; }
+    static __device__ __forceinline__ floatx4 turned(val x, raw eye) { return mm(x, eye, floatx4{}); }
 };
 
 template <> struct Tile<true> {
@@ -82,11 +75,9 @@ template <> struct Tile<true> {
         bf16x4 hi, mid, lo;
     };
     static constexpr int PAD = 8;
-    // The upper 8 bits of a significand, the next 8 and the last: nothing is lost.  (NEAR:
-    // the second to nearest, where the first two are taken for a pair as well.)
+    // The upper 8 bits of a significand, the next 8 and the last: nothing is lost.
     // (Rounding to the nearest, with the conversion instruction, takes as many
     // instructions and is slower: 390 x 4,096 x 4 x 64 forward 1.94 ms against 1.82.)
-    template <bool NEAR = false>
     static __device__ __forceinline__ val split(floatx4 x)
     {
         val v;
@@ -95,7 +86,7 @@ template <> struct Tile<true> {
         for (int i = 0; i < 4; ++i) {
             h[i] = __float_as_uint(x[i]);
             const float r = x[i] - __uint_as_float(h[i] & 0xFFFF0000u);
-            m[i] = __float_as_uint(r) + (NEAR ? 0x8000u : 0u);
+            m[i] = __float_as_uint(r);
             l[i] = __float_as_uint(r - __uint_as_float(m[i] & 0xFFFF0000u));
         }
         v.hi = upper(h);
@@ -140,32 +131,6 @@ template <> struct Tile<true> {
     {
         return go(a.hi, b, go(a.mid, b, go(a.lo, b, c)));
     }
-    // Results that are rounded to bf16 next and feed nothing else take two numbers of
-    // each operand, the second to nearest: 2^-16 of a value is lost.
-    struct pair {
-        bf16x4 hi, mid;
-    };
-    static __device__ __forceinline__ pair part(floatx4 x)
-    {
-        uint32_t h[4], m[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            h[i] = __float_as_uint(x[i]);
-            m[i] = __float_as_uint(x[i] - __uint_as_float(h[i] & 0xFFFF0000u)) + 0x8000u;
-        }
-        pair v;
-        v.hi = upper(h);
-        v.mid = upper(m);
-        return v;
-    }
-    static __device__ __forceinline__ floatx4 mm_out(pair a, raw b, floatx4 c) { return go(a.hi, b, go(a.mid, b, c)); }
-    static __device__ __forceinline__ floatx4 mm_out(pair a, pair b, floatx4 c)
-    {
-        return go(a.hi, b.hi, go(a.mid, b.hi, go(a.hi, b.mid, c)));
-    }
-    static __device__ __forceinline__ floatx4 mm_out(raw a, pair b, floatx4 c) { return go(a, b.hi, go(a, b.mid, c)); }
-    static __device__ __forceinline__ pair head(val x) { return pair{x.hi, x.mid}; }
-    // The transposed tile: a product with the unit matrix, which loses nothing.
     static __device__ __forceinline__ raw eye(int lane)
     {
         raw x;
@@ -173,26 +138,9 @@ template <> struct Tile<true> {
         for (int i = 0; i < 4; ++i) x[i] = (__bf16)(4 * (lane >> 4) + i == (lane & 15) ? 1.0f : 0.0f);
         return x;
     }
-    static __device__ __forceinline__ pair turned(pair x, raw eye)
+    static __device__ __forceinline__ floatx4 turned(val x, raw eye)
     {
-        const floatx4 h = go(x.hi, eye, floatx4{}), m = go(x.mid, eye, floatx4{});
-        uint32_t a[4], b[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            a[i] = __float_as_uint(h[i]);
-            b[i] = __float_as_uint(m[i]);
-        }
-        return pair{upper(a), upper(b)};
-    }
-    static __device__ __forceinline__ pair either(pair a, pair b)
-    {
-        uint64_t x[2], y[2];
-        __builtin_memcpy(x, &a, sizeof a);
-        __builtin_memcpy(y, &b, sizeof b);
-        x[0] |= y[0];
-        x[1] |= y[1];
-        __builtin_memcpy(&a, x, sizeof a);
-        return a;
+        return go(x.hi, eye, go(x.mid, eye, go(x.lo, eye, floatx4{})));
     }
     // products over 32
     static __device__ __forceinline__ floatx4 mm2(raw a0, raw a1, val b0, val b1, floatx4 c)

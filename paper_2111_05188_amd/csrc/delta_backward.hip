@@ -46,8 +46,8 @@ struct Back {
     typedef typename RW::E E;
     typedef Tile<BF> TL;
     typedef typename TL::val val;
-    typedef typename TL::pair pair;
     typedef typename TL::raw raw;
+    typedef Tile<false> F;
     static constexpr int LD = RW::LD, NW = RW::NW;
     static constexpr int HALF = KT + 1, TILES = 2 * HALF / TURNS;
     struct Shared {
@@ -68,7 +68,6 @@ struct Back {
         int odd[2];
     };
     static_assert(16 * LD * sizeof(E) <= sizeof(Shared::parts), "rows past v's end");
-    static_assert(sizeof(pair) == sizeof(floatx4), "triangles' gradients");
     static_assert(sizeof(PieceRows) % 16 == 0 && NP * sizeof(PieceRows) <= sizeof(Shared::parts), "T's rows");
     static_assert(sizeof(Shared) <= LDS_LIMIT, "LDS");
 
@@ -94,7 +93,7 @@ struct Back {
     // parts of y.dy too, and the transpose of the state before it.
     template <bool PART, bool OUT>
     static __device__ __forceinline__ floatx4 forward(Shared &sh, int s, int count, bool ends, int p, int w, int lane,
-                                                      floatx4 *S, pair *ST)
+                                                      floatx4 *S, floatx4 *ST)
     {
         lane = fresh(lane);
         const int r = 4 * (lane >> 4);
@@ -122,12 +121,12 @@ struct Back {
         floatx4 ks = {}, qs = {}, U = {}, R, W;
 #pragma unroll
         for (int kt = 0; kt < KT; kt += 2) {
-            const val x0 = TL::template split<OUT>(S[kt]), x1 = TL::template split<OUT>(S[kt + 1]);
+            const val x0 = TL::split(S[kt]), x1 = TL::split(S[kt + 1]);
             ks = TL::mm2(kr[kt], kr[kt + 1], x0, x1, ks);
             if constexpr (OUT) {
                 qs = TL::mm2(qr[kt], qr[kt + 1], x0, x1, qs);
-                ST[kt] = TL::turned(TL::head(x0), eye);
-                ST[kt + 1] = TL::turned(TL::head(x1), eye);
+                ST[kt] = TL::turned(x0, eye);
+                ST[kt + 1] = TL::turned(x1, eye);
             }
         }
 #pragma unroll
@@ -155,8 +154,8 @@ struct Back {
 
     // What the waves' columns give to the gradients of a piece's triangles and keys.
     struct Mine {
-        raw dy;             // rows of dY, as first operand
-        pair U, dR;         // transposed, for either
+        floatx4 dy;         // rows of dY, as first operand
+        floatx4 U, dR;      // transposed, for either
         floatx4 ak, au;
     };
 
@@ -164,7 +163,7 @@ struct Back {
     // the transpose.
     template <bool PART>
     static __device__ __forceinline__ Mine backward(Shared &sh, int s, int count, int p, int w, int lane, floatx4 *Gs,
-                                                    floatx4 U, pair *GT)
+                                                    floatx4 U, floatx4 *GT)
     {
         lane = fresh(lane);
         const int r = 4 * (lane >> 4), col = 16 * w + (lane & 15);
@@ -173,7 +172,7 @@ struct Back {
         raw kr[KT], kc[KT], qc[KT];
 #pragma unroll
         for (int kt = 0; kt < KT; ++kt) kr[kt] = along_row<BF, LD>(sh.k, s, kt, lane);
-        mine.dy = along_row<BF, LD>(sh.dy, s, w, lane);
+        mine.dy = TL::wide(along_row<BF, LD>(sh.dy, s, w, lane));
         const raw dyc = along_col<BF, LD, PART>(sh.dy, s, count, w, lane);
         const floatx4 vw = TL::wide(along_col<BF, LD, PART>(sh.v, s, count, w, lane));
         const floatx4 be = *(const floatx4 *)(rows.beta + r), ak = *(const floatx4 *)(rows.ak + r);
@@ -190,10 +189,10 @@ struct Back {
         floatx4 kg = {}, dU, dR = {}, A, B;
 #pragma unroll
         for (int kt = 0; kt < KT; kt += 2) {
-            const val x0 = TL::template split<true>(Gs[kt]), x1 = TL::template split<true>(Gs[kt + 1]);
+            const val x0 = TL::split(Gs[kt]), x1 = TL::split(Gs[kt + 1]);
             kg = TL::mm2(kr[kt], kr[kt + 1], x0, x1, kg);
-            GT[kt] = TL::turned(TL::head(x0), eye);
-            GT[kt + 1] = TL::turned(TL::head(x1), eye);
+            GT[kt] = TL::turned(x0, eye);
+            GT[kt + 1] = TL::turned(x1, eye);
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i) dU[i] = !PART || r + i < count ? kg[i] * au[i] : 0.0f;
@@ -219,8 +218,9 @@ struct Back {
             u[i] = dR[i] * U[i];
         }
         const float vd = row_sums(t, lane), ru = row_sums(u, lane);
-        mine.U = TL::turned(TL::part(U), eye);
-        mine.dR = TL::turned(TL::part(dR), eye);
+        const floatx4 one = TL::wide(eye);
+        mine.U = F::turned(U, one);
+        mine.dR = F::turned(dR, one);
         mine.ak = ak;
         mine.au = au;
         each_row<PART>(count, r, [&](int i) {
@@ -235,8 +235,8 @@ struct Back {
 
     // A wave's part of dY S0^T for all keys, and of P's gradient (turn 0), or of
     // rest rk U G1^T - beta gamma rk dR S0^T, and of L's (turn 1).
-    static __device__ __forceinline__ void give(Shared &sh, int turn, int w, int lane, const Mine &m, const pair *ST,
-                                                const pair *GT)
+    static __device__ __forceinline__ void give(Shared &sh, int turn, int w, int lane, const Mine &m,
+                                                const floatx4 *ST, const floatx4 *GT)
     {
         lane = fresh(lane);
         const int first = TURNS == 1 ? turn * HALF : 0;
@@ -244,17 +244,17 @@ struct Back {
         for (int kt = 0; kt < KT; ++kt) {
             floatx4 x = {}, y = {};
             if (turn == 0) {
-                x = TL::mm_out(m.dy, ST[kt], x);
+                x = F::mm(m.dy, ST[kt], x);
             } else {
-                x = TL::mm_out(m.U, GT[kt], x);
-                y = TL::mm_out(m.dR, ST[kt], y);
+                x = F::mm(m.U, GT[kt], x);
+                y = F::mm(m.dR, ST[kt], y);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) x[i] = m.au[i] * x[i] - m.ak[i] * y[i];
             }
             sh.parts[first + kt][w][lane] = x;
         }
         floatx4 z = {};
-        sh.parts[first + KT][w][lane] = turn == 0 ? TL::mm_out(m.dy, m.U, z) : TL::mm_out(m.dR, m.U, z);
+        sh.parts[first + KT][w][lane] = F::mm(turn == 0 ? m.dy : m.dR, m.U, z);
     }
 
     // the sum of all waves' parts of a tile
@@ -296,12 +296,12 @@ struct Back {
             const bool in = turn == 0 ? r + i >= n : r + i > n;
             x[i] = in && (!PART || r + i < count) ? sum[i] * (fade[i] * rkn) * f : 0.0f;
         }
-        const pair d = TL::part(x), t = TL::turned(d, TL::eye(lane));
+        const floatx4 t = F::turned(x, F::eye(lane));
         if (turn == 0) {
-            *(pair *)&sh.m[p][0][lane] = d;
-            *(pair *)&sh.m[p][1][lane] = t;
+            sh.m[p][0][lane] = x;
+            sh.m[p][1][lane] = t;
         } else {
-            *(pair *)&sh.m[p][2][lane] = TL::either(d, t);
+            sh.m[p][2][lane] = x + t;       // (no place has both)
         }
     }
 
@@ -341,16 +341,15 @@ struct Back {
         const raw kc = along_col<BF, LD, PART>(sh.k, s, count, w, lane);
         const floatx4 rq = *(const floatx4 *)(rows.rq + r), rk = *(const floatx4 *)(rows.rk + r);
         const floatx4 aq = *(const floatx4 *)(rows.aq + r);
-        const pair m = *(const pair *)&sh.m[p][0][lane], mt = *(const pair *)&sh.m[p][1][lane];
-        const pair l = *(const pair *)&sh.m[p][2][lane];
+        const floatx4 m = sh.m[p][0][lane], mt = sh.m[p][1][lane], l = sh.m[p][2][lane];
         const floatx4 yd = *(const floatx4 *)(sh.along[p][0] + r), kd = *(const floatx4 *)(sh.along[p][1] + r);
         floatx4 a, b = t.dk;
 #pragma unroll
         for (int i = 0; i < 4; ++i) a[i] = aq[i] * t.dq[i];
-        b = TL::mm_out(m, qc, b);
-        b = TL::mm_out(l, kc, b);
-        a = TL::mm_out(mt, kc, a);
         const floatx4 qw = TL::wide(qc), kw = TL::wide(kc);
+        b = F::mm(m, qw, b);
+        b = F::mm(l, kw, b);
+        a = F::mm(mt, kw, a);
         each_row<PART>(count, r, [&](int i) {
             sh.q[(s + r + i) * LD + col] = (E)(a[i] - qw[i] * rq[i] * rq[i] * yd[i]);
             sh.k[(s + r + i) * LD + col] = (E)(b[i] - kw[i] * rk[i] * rk[i] * kd[i]);
@@ -431,7 +430,7 @@ __global__ __launch_bounds__(4 * D, 2) void delta_bwd_kernel(DeltaArgs a)
         const int t0 = grp * G;
         const int count = len - t0 < G ? len - t0 : G, all = end - t0 < G ? end - t0 : G;
         if (count > 0) {
-            typename BK::pair ST[NP][KT], GT[KT];
+            floatx4 ST[NP][KT], GT[KT];
             floatx4 U[NP];
             float odd = RW::odd(fq) + RW::odd(fk) + RW::odd(fv) + RW::odd(fy);
             workgroup_lds_barrier();                // (the group before is done with)
@@ -497,7 +496,7 @@ __global__ __launch_bounds__(4 * D, 2) void delta_bwd_kernel(DeltaArgs a)
                     for (int p = 0, x = s; p < NP && x < count; ++p) {
                         const int e = piece_end(x, count, ends, single);
                         BK::template forward<true, false>(sh, x, e - x, ends >> (e - 1) & 1, p, w, lane, S,
-                                                         (typename BK::pair *)nullptr);
+                                                         (floatx4 *)nullptr);
                         x = e;
                     }
                     workgroup_lds_barrier();
