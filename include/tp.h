@@ -699,8 +699,8 @@ int tp_mx4_linear(const void *x, int32_t x_dtype, int64_t M, int64_t ldx, const 
  * bf16 numbers each, which lose nothing.  q.q and k.k, and the states, have to be in
  * fp32's range.
  * A NaN or an infinity in a step reaches y and the states from that step on, to
- * the episode's end, and the gradients that read them (r's up to 31 steps before);
- * one in h0 the first episode, one in dh_last the last.
+ * the episode's end, and the gradients that read them; one in h0 the first episode,
+ * one in dh_last the last.
  */
 typedef struct tp_delta {
     int32_t T;             /* steps, >= 1                                    */

@@ -10,7 +10,7 @@ import numpy as np
 from .recur import sigmoid, softplus
 
 EPS = 1e-6
-AHEAD = 32          # steps that one sum of the decays' gradients runs over on the GPU
+AHEAD = 32          # steps that dr_mass adds up
 
 
 def _unit(x):
@@ -56,7 +56,10 @@ def forward(q, k, v, r, b, lam, h0=None, done=None, lens=None, states=None):
 def backward(q, k, v, r, b, lam, dy, dh_last=None, h0=None, done=None, lens=None):
     """Gradients of sum(y dy) + sum(h_last dh_last): dq, dk, dv, dr, db, dlam, dh0; and what the
     roundings of dr [T][B][H] and dlam [H] scale with, the lengths of the vectors whose products
-    add up to them, and of dq and dk, the gradients of the unit rows over the rows' lengths."""
+    add up to them, and of dq and dk, the gradients of the unit rows over the rows' lengths.
+    dr_across [T][B][H], dlam_across [H]: the same of dr and dlam, with only what passes a step's decay:
+    |e^g S| |D| / sqrt(d) of e^g S and its gradient D, whose product the gradient of g is (roundings of
+    single elements, in states of rank one at least)."""
     T, B, H, dk = q.shape
     states = []
     forward(q, k, v, r, b, lam, h0, done, lens, states)
@@ -64,7 +67,7 @@ def backward(q, k, v, r, b, lam, dy, dh_last=None, h0=None, done=None, lens=None
     dq, dk_, dv, dr, db = (np.zeros_like(x) for x in (q, k, v, r, b))
     dlam, w = np.zeros(H), np.zeros(r.shape)
     sizes = dict(dq_size=np.ones(r.shape + (1,)), dk_size=np.ones(r.shape + (1,)))
-    size, shut = np.zeros(r.shape), np.zeros(r.shape)
+    size, shut, across, past = (np.zeros(r.shape) for _ in range(4))
     norm = lambda x: np.sqrt((x * x).sum(-1))  # noqa: E731
     for t in reversed(range(T)):
         live, ends = _gates(t, B, done, lens)
@@ -88,6 +91,8 @@ def backward(q, k, v, r, b, lam, dy, dh_last=None, h0=None, done=None, lens=None
         dr[t][m] = (dg * g * rest)[m]
         db[t][m] = ((du * e).sum(-1) * beta * less)[m]
         shut[t][m] = (-g * rest)[m]
+        past[t][m] = (-g * np.sqrt((D1 * D1).sum((-2, -1)) * (S1 * S1).sum((-2, -1)) / min(dk, v.shape[3])))[m]
+        across[t][m] = (past[t] * rest)[m]
         size[t][m] = (norm(dqn) + norm(dkn) + 2.0 * norm(du) * norm(u)
                       + np.sqrt((G * G).sum((-2, -1)) * (S2 * S2).sum((-2, -1))))[m]
         dlam += w[t].sum(0)
@@ -98,4 +103,5 @@ def backward(q, k, v, r, b, lam, dy, dh_last=None, h0=None, done=None, lens=None
         ahead[t] = size[t:t + AHEAD].sum(0)
     mass = (ahead * -8.0 * softplus(lam) * -sigmoid(r)).sum((0, 1)) * kappa
     return dict(dq=dq, dk=dk_, dv=dv, dr=dr, db=db, dlam=kappa * dlam, dh0=G,
-                dr_mass=ahead * shut, dlam_mass=mass, **sizes)
+                dr_mass=ahead * shut, dlam_mass=mass, dr_across=across,
+                dlam_across=kappa * np.sqrt((past * past).sum((0, 1))), **sizes)

@@ -47,6 +47,7 @@ template <> struct Tile<false> {
     static constexpr int PAD = 4;               // elements after a row in LDS
     static __device__ __forceinline__ val split(floatx4 x) { return x; }
     static __device__ __forceinline__ floatx4 wide(raw x) { return x; }
+    static __device__ __forceinline__ floatx4 whole(val x) { return x; }
     static __device__ __forceinline__ floatx4 mm(floatx4 a, floatx4 b, floatx4 c)
     {
 #pragma unroll
@@ -103,6 +104,7 @@ template <> struct Tile<true> {
         return v;
     }
     static __device__ __forceinline__ floatx4 wide(raw x) { return __builtin_convertvector(x, floatx4); }
+    static __device__ __forceinline__ floatx4 whole(const val &x) { return wide(x.hi) + (wide(x.mid) + wide(x.lo)); }
     static __device__ __forceinline__ bf16x8 join(bf16x4 a, bf16x4 b)
     {
         return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
@@ -365,7 +367,8 @@ __device__ __forceinline__ double piece_sums(const float *g, int count, int lane
 
 // What one wave prepares of a piece.  (`rows` has the rows' scalars with WANT_ROWS, else
 // it is the wave's own while it works.)
-enum : int { WANT_T = 1, WANT_PT = 2, WANT_P = 4, WANT_ROWS = 8 };
+// WANT_L: L, with T, in Pn's place.
+enum : int { WANT_T = 1, WANT_PT = 2, WANT_P = 4, WANT_ROWS = 8, WANT_L = 16 };
 
 // K K^T and Q K^T tiles of a piece, the rows' lengths, T and P in both layouts (as
 // far as they are wanted).  L is nilpotent; its inverse grows from blocks of 1, 2, 4,
@@ -435,6 +438,7 @@ __device__ __forceinline__ void piece_triangles(const E *q, const E *k, const fl
             const float x = kk[i] * rkr[i] * (rkn * fade[i]);
             const float Ln = r + i > n ? x * ber[i] : 0.0f;     // row r+i after column n
             Lt[i] = r + i < n ? x * be : 0.0f;                  // transposed
+            if constexpr (WANT & WANT_L) Pn[i] = Ln;
             // blocks of two: I - L inside them
             const float unit = r + i == n ? 1.0f : 0.0f;
             const bool same2 = 2 * grp + i / 2 == n >> 1;

@@ -5,12 +5,15 @@
 //   M = (dY U^T) o G (lower),  E = -(dR U^T) o beta G (below the diagonal),
 //   dQ^ = gamma dY S0^T + M K^,
 //   dK^ = -beta gamma dR S0^T + (gamma_C/gamma) U G1^T + M^T Q^ + (E + E^T) K^.
-// The pre-activation of beta gets (dR.u)(1 - beta).  The log-decay of a step
-// multiplies what every later step of its episode reads, so its gradient is the
-// sum of x_c = q^_c.dq^_c + k^_c.dk^_c - 2 dR_c.u_c over the steps from it to the
-// episode's end, and <G, S> at the end of the group if the episode goes on: the
-// terms of P, L and the states that a decay does not touch cancel in x.  It is summed
-// as x = y.dy - v.dv, the same, which come from the columns that a wave has.
+// The pre-activation of beta gets (dR.u)(1 - beta).  The log-decay g_t of a step is in
+// what passes from before the step to it or after it, and its gradient is all of that:
+//   sum over c >= t > j of (dY U^T)[c][j] P[c][j] - (dR U^T)[c][j] L[c][j]
+//   + sum over c >= t of gamma_c (S0^T q^_c).dy_c - beta_c gamma_c (S0^T k^_c).dR_c
+//   + sum over j < t of (gamma_C/gamma_j) (G1^T k^_j).u_j  +  gamma_C <G1, S0>.
+// Every term has the step's decay as a factor, so the sum is as good as the products
+// however strong the decay.  (Summing y.dy - v.dv from the step to the episode's end is
+// the same but for rounding: terms that the decay does not touch cancel there, and at
+// decays of e^-24 a step 5% of lambda's gradient was lost, at e^-40 up to 75%.)
 //
 // A workgroup has one head of one sequence (a segment of it, where few heads leave
 // CUs without work) and goes through its groups from the last to the first, each
@@ -25,7 +28,7 @@
 // (States and gradients transposed through LDS, and whole sums in each wave, took six
 // barriers more: 4.90 ms where this took 4.76.)
 //
-// 390 steps of 2,048 sequences of 4 heads of 64 in bf16 take 5.00 ms with the forward
+// 390 steps of 2,048 sequences of 4 heads of 64 in bf16 take 5.20 ms with the forward
 // call, where the bytes (3.8 GB) take 0.8 at the rate of a copy.  A group of 32 steps
 // is some 34,000 cycles of a workgroup, two of which a CU holds (71 KiB of LDS and 252
 // registers each); one alone is hardly faster: what bounds it is the chain of products
@@ -60,13 +63,16 @@ struct Back {
         __attribute__((aligned(16))) floatx4 m[NP][3][64];  // T, T^T, P^T
         __attribute__((aligned(16))) val P[NP][64];
         __attribute__((aligned(16))) PieceRows rows[NP];
-        // y.dy, v.dv, dR.u of the waves' columns
-        __attribute__((aligned(16))) float sums[G][3][NW];
+        __attribute__((aligned(16))) floatx4 L[NP][64];
+        // y.dy, v.dv, dR.u of the waves' columns; and what of them passes a step's decay
+        // from or to a state: gamma S0^T q^.dy, beta gamma S0^T k^.dR, rest G1^T k^.u
+        __attribute__((aligned(16))) float sums[G][6][NW];
         double cum[2 * NP][16];
         float g[G], beta[G], shut[G], idle[G];              // 1 - sigmoid(r), 1 - beta
-        float x[G], dbeta[G];
+        float dr[G], dbeta[G];
         __attribute__((aligned(16))) float along[NP][2][16];    // q^.dq^, k^.dk^
-        float ends[NW];                                     // <G, S> of a wave's columns
+        float ends[NP][NW];                                 // gamma_C <G1, S0> of a wave's columns
+        float decay[G][3];                                  // parts of the gradients of g
         int odd[2];
     };
     static_assert(16 * LD * sizeof(E) <= sizeof(Shared::parts), "rows past v's end");
@@ -91,10 +97,14 @@ struct Back {
         for (int kt = 0; kt < KT; ++kt) S[kt] = floatx4{};
     }
 
-    // The writes U of a piece and the state after it, on columns 16w...  OUT: the rows'
-    // parts of y.dy too, and the transpose of the state before it.
+    // The writes U of a piece, the state after it, on columns 16w.., and what the state
+    // before it takes from R.  OUT: the rows' parts of y.dy too, and the transpose of the
+    // state before it.
+    struct Writes {
+        floatx4 U, S0;
+    };
     template <bool PART, bool OUT>
-    static __device__ __forceinline__ floatx4 forward(Shared &sh, int s, int count, bool ends, int p, int w, int lane,
+    static __device__ __forceinline__ Writes forward(Shared &sh, int s, int count, bool ends, int p, int w, int lane,
                                                       floatx4 *S, floatx4 *ST)
     {
         lane = fresh(lane);
@@ -120,7 +130,7 @@ struct Back {
 #pragma unroll
         for (int kt = 0; kt < KT; ++kt) kc[kt] = along_col<BF, LD, PART>(sh.k, s, count, kt, lane);
         const raw eye = TL::eye(lane);
-        floatx4 ks = {}, qs = {}, U = {}, R, W;
+        floatx4 ks = {}, qs = {}, U = {}, R, W, from;
 #pragma unroll
         for (int kt = 0; kt < KT; kt += 2) {
             const val x0 = TL::split(S[kt]), x1 = TL::split(S[kt + 1]);
@@ -132,7 +142,10 @@ struct Back {
             }
         }
 #pragma unroll
-        for (int i = 0; i < 4; ++i) R[i] = !PART || r + i < count ? be[i] * vv[i] - ak[i] * ks[i] : 0.0f;
+        for (int i = 0; i < 4; ++i) {
+            from[i] = ak[i] * ks[i];
+            R[i] = !PART || r + i < count ? be[i] * vv[i] - from[i] : 0.0f;
+        }
         U = Tile<false>::mm(Tt, R, U);
 #pragma unroll
         for (int i = 0; i < 4; ++i) W[i] = !PART || r + i < count ? U[i] * au[i] : 0.0f;
@@ -141,17 +154,23 @@ struct Back {
         for (int kt = 0; kt < KT; ++kt) S[kt] = TL::mm(kc[kt], y, S[kt] * total);
         if (ends) clear(S);
         if constexpr (OUT) {
-            floatx4 o, t;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) o[i] = aq[i] * qs[i];
-            o = Tile<false>::mm(P, U, o);
             const floatx4 dy = TL::wide(dyc);
+            floatx4 o, t, u;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                o[i] = aq[i] * qs[i];
+                u[i] = o[i] * dy[i];
+            }
+            o = Tile<false>::mm(P, U, o);
 #pragma unroll
             for (int i = 0; i < 4; ++i) t[i] = o[i] * dy[i];
-            const float sum = row_sums(t, lane);
-            if ((lane & 15) < 4 && (!PART || r + (lane & 3) < count)) sh.sums[s + r + (lane & 3)][0][w] = sum;
+            const float yd = row_sums(t, lane), qd = row_sums(u, lane);
+            if ((lane & 15) < 4 && (!PART || r + (lane & 3) < count)) {
+                sh.sums[s + r + (lane & 3)][0][w] = yd;
+                sh.sums[s + r + (lane & 3)][3][w] = qd;
+            }
         }
-        return U;
+        return Writes{U, from};
     }
 
     // What the waves' columns give to the gradients of a piece's triangles and keys.
@@ -165,8 +184,9 @@ struct Back {
     // the transpose.
     template <bool PART>
     static __device__ __forceinline__ Mine backward(Shared &sh, int s, int count, int p, int w, int lane, floatx4 *Gs,
-                                                    floatx4 U, floatx4 *GT)
+                                                    const Writes &x, const floatx4 *ST, floatx4 *GT)
     {
+        const floatx4 U = x.U;
         lane = fresh(lane);
         const int r = 4 * (lane >> 4), col = 16 * w + (lane & 15);
         const PieceRows &rows = sh.rows[p];
@@ -212,14 +232,24 @@ struct Back {
             Gs[kt] = TL::mm(qc[kt], a, Gs[kt] * total);
             Gs[kt] = TL::mm(kc[kt], b, Gs[kt]);
         }
-        floatx4 dv, t, u;
+        floatx4 dv, t, u, f, g;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             dv[i] = be[i] * dR[i];
             t[i] = vw[i] * dv[i];
             u[i] = dR[i] * U[i];
+            f[i] = dR[i] * x.S0[i];
+            g[i] = U[i] * (kg[i] * au[i]);
         }
         const float vd = row_sums(t, lane), ru = row_sums(u, lane);
+        const float rs = row_sums(f, lane), ug = row_sums(g, lane);
+        float e = 0.0f;
+#pragma unroll
+        for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) e += ST[kt][i] * GT[kt][i];
+        e = lanes_sum<64>(e);
+        if (lane == 0) sh.ends[p][w] = e * total;
         const floatx4 one = TL::wide(eye);
         mine.U = F::turned(U, one);
         mine.dR = F::turned(dR, one);
@@ -231,6 +261,8 @@ struct Back {
         if ((lane & 15) < 4 && (!PART || r + (lane & 3) < count)) {
             sh.sums[s + r + (lane & 3)][1][w] = vd;
             sh.sums[s + r + (lane & 3)][2][w] = ru;
+            sh.sums[s + r + (lane & 3)][4][w] = rs;
+            sh.sums[s + r + (lane & 3)][5][w] = ug;
         }
         return mine;
     }
@@ -279,9 +311,10 @@ struct Back {
 
     // The gradient of a piece's triangle P (turn 0) or L (turn 1), scaled by both rows'
     // lengths, by one wave: as it is and transposed, or, L's, the sum of both.  They take the
-    // place of T and P.
+    // place of T and P.  And what of it passes each step's decay: the products with the
+    // triangle itself, over the rows from the step on and the columns before it.
     template <bool PART>
-    static __device__ __forceinline__ void triangle(Shared &sh, int count, int p, int turn, int lane)
+    static __device__ __forceinline__ void triangle(Shared &sh, int s, int count, int p, int turn, int lane)
     {
         lane = fresh(lane);
         const int n = lane & 15, r = 4 * (lane >> 4);
@@ -291,13 +324,21 @@ struct Back {
         const floatx4 be = *(const floatx4 *)(rows.beta + r);
         const float rkn = rows.rk[n];
         const floatx4 fade = piece_decays(sh.cum[p], lane);
-        floatx4 x;
+        const floatx4 own = turn == 0 ? TL::whole(sh.P[p][lane]) : sh.L[p][lane];
+        floatx4 x, N, from, C = {};
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const float f = turn == 0 ? rq[i] : -(be[i] * rk[i]);
-            const bool in = turn == 0 ? r + i >= n : r + i > n;
-            x[i] = in && (!PART || r + i < count) ? sum[i] * (fade[i] * rkn) * f : 0.0f;
+            const bool in = turn == 0 ? r + i >= n : r + i > n, has = !PART || r + i < count;
+            x[i] = in && has ? sum[i] * (fade[i] * rkn) * f : 0.0f;
+            N[i] = r + i > n && has ? sum[i] * own[i] : 0.0f;
+            from[i] = r + i >= n ? 1.0f : 0.0f;
         }
+        C = F::mm(from, N, C);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) C[i] = r + i > n ? C[i] : 0.0f;
+        const float c = row_sums(C, lane);
+        if (n < 4 && (!PART || r + n < count)) sh.decay[s + r + n][turn] = turn == 0 ? c : -c;
         const floatx4 t = F::turned(x, F::eye(lane));
         if (turn == 0) {
             sh.m[p][0][lane] = x;
@@ -315,6 +356,25 @@ struct Back {
         sh.along[p][turn][lane] = turn == 0 ? total(x[0]) : 2.0f * total(x[2]) - total(x[1]);
     }
 
+    // What passes each step's decay from or to a piece's first and last state.
+    static __device__ __forceinline__ void states(Shared &sh, int s, int count, int p, int lane)
+    {
+        const int n = lane & 15;
+        const float (*x)[NW] = sh.sums[s + (n < count ? n : 0)];
+        float in = n < count ? total(x[3]) - total(x[4]) : 0.0f;        // of the steps from this one on
+        float out = n < count ? total(x[5]) : 0.0f;                     // of the ones before it
+        in += dpp<DPP_ROW_SHL + 1>(in);
+        in += dpp<DPP_ROW_SHL + 2>(in);
+        in += dpp<DPP_ROW_SHL + 4>(in);
+        in += dpp<DPP_ROW_SHL + 8>(in);
+        out = dpp<DPP_ROW_SHR + 1>(out);
+        out += dpp<DPP_ROW_SHR + 1>(out);
+        out += dpp<DPP_ROW_SHR + 2>(out);
+        out += dpp<DPP_ROW_SHR + 4>(out);
+        out += dpp<DPP_ROW_SHR + 8>(out);
+        if (lane < count) sh.decay[s + lane][2] = in + out + total(sh.ends[p]);
+    }
+
     // What is summed of a piece on its keys' columns 16w..
     struct Sums {
         floatx4 dq, dk;
@@ -327,7 +387,8 @@ struct Back {
         (turn == 0 ? t.dq : t.dk) = take(sh, TURNS == 1 ? turn * HALF + w : w, lane);
         if (w == (2 * p + turn) % NW) {
             lengths(sh, s, count, p, turn, lane);
-            triangle<PART>(sh, count, p, turn, lane);
+            triangle<PART>(sh, s, count, p, turn, lane);
+            if (turn == 1) states(sh, s, count, p, lane);
         }
     }
 
@@ -433,7 +494,7 @@ __global__ __launch_bounds__(4 * D, 2) void delta_bwd_kernel(DeltaArgs a)
         const int count = len - t0 < G ? len - t0 : G, all = end - t0 < G ? end - t0 : G;
         if (count > 0) {
             floatx4 ST[NP][KT], GT[KT];
-            floatx4 U[NP];
+            typename BK::Writes X[NP];
             float odd = RW::odd(fq) + RW::odd(fk) + RW::odd(fv) + RW::odd(fy);
             workgroup_lds_barrier();                // (the group before is done with)
             const int tid = fresh(threadIdx.x);
@@ -470,10 +531,11 @@ __global__ __launch_bounds__(4 * D, 2) void delta_bwd_kernel(DeltaArgs a)
                     const int c = piece_end(from, count, ends, single) - from;
                     floatx4 Tt, Tn, Pt, Pn;
                     if (j < NP) {
-                        piece_triangles<BF, D, LD, WANT_T, true>(sh.q, sh.k, sh.g, sh.beta, from, c, lane, sh.cum[j],
+                        piece_triangles<BF, D, LD, WANT_T | WANT_L, true>(sh.q, sh.k, sh.g, sh.beta, from, c, lane, sh.cum[j],
                                                                  (PieceRows *)sh.parts + p, Tt, Tn, Pt, Pn);
                         sh.m[p][0][lane] = Tn;
                         sh.m[p][1][lane] = Tt;
+                        sh.L[p][lane] = Pn;
                     } else {
                         piece_triangles<BF, D, LD, WANT_ROWS | WANT_P | WANT_PT, true>(
                             sh.q, sh.k, sh.g, sh.beta, from, c, lane, sh.cum[j], &sh.rows[p], Tt, Tn, Pt, Pn);
@@ -517,20 +579,9 @@ __global__ __launch_bounds__(4 * D, 2) void delta_bwd_kernel(DeltaArgs a)
                     const int c = at[p + 1] - at[p];
                     if (c == 0) continue;
                     pieces_of(c, [&](auto m) {
-                        U[p] = BK::template forward<decltype(m)::value, true>(sh, at[p], c, done(p), p, w, lane, S,
+                        X[p] = BK::template forward<decltype(m)::value, true>(sh, at[p], c, done(p), p, w, lane, S,
                                                                               ST[p]);
                     });
-                }
-                if (batch == batches - 1) {
-                    float x = 0.0f;
-#pragma unroll
-                    for (int kt = 0; kt < KT; ++kt)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) x += S[kt][i] * Gs[kt][i];
-                    // (an episode that ends here leaves nothing to the next group)
-                    if (ends >> (count - 1) & 1) x = 0.0f;
-                    x = lanes_sum<64>(x);
-                    if (lane == 0) sh.ends[w] = x;
                 }
                 typename BK::Sums t[NP];
 #pragma unroll
@@ -540,7 +591,8 @@ __global__ __launch_bounds__(4 * D, 2) void delta_bwd_kernel(DeltaArgs a)
                     if (done(p)) BK::clear(Gs);
                     typename BK::Mine mine;
                     pieces_of(c, [&](auto m) {
-                        mine = BK::template backward<decltype(m)::value>(sh, at[p], c, p, w, lane, Gs, U[p], GT);
+                        mine = BK::template backward<decltype(m)::value>(sh, at[p], c, p, w, lane, Gs, X[p], ST[p],
+                                                                            GT);
                     });
                     // the waves' parts to the waves that have the keys' columns
                     if (p + 1 < NP) workgroup_lds_barrier();
@@ -569,36 +621,11 @@ __global__ __launch_bounds__(4 * D, 2) void delta_bwd_kernel(DeltaArgs a)
                 workgroup_lds_barrier();
             }
             // gates: lane t of the first wave has step t
-            if (w == 0) {
-                float on = 0.0f, x = 0.0f;
-#pragma unroll
-                for (int j = 0; j < NW; ++j) on += sh.ends[j];
-                if (lane < count) {
-                    const float (*t)[NW] = sh.sums[lane];
-                    x = BK::total(t[0]) - BK::total(t[1]);
-                    sh.x[lane] = x;
-                    sh.dbeta[lane] = BK::total(t[2]) * sh.idle[lane];
-                }
-                wave_lds_fence();
-                // the last step of this step's episode within the group
-                const uint64_t m = lane < count ? ends >> lane : 0;
-                const int stop = m ? lane + __builtin_ctzll(m) : count - 1;
-                float acc = 0.0f;
-                // (a NaN or an infinity, from a state or a gradient too, stays in its episode)
-                if (__ballot(lane < count && !(fabsf(x) <= 3.4e38f))) {
-                    for (int c = 0; c < count; ++c) acc += c >= lane && c <= stop ? sh.x[c] : 0.0f;
-                } else {                    // differences of sums from the first step, in 64 bits
-                    const double sum = wave_inclusive_scan((double)x);
-                    acc = (float)(__shfl(sum, stop) - sum + (double)x);
-                }
-                if (lane < count) {
-                    if (!m) acc += on;
-                    // the first step of an episode has no state to fade
-                    if (lane > 0 && (ends >> (lane - 1) & 1)) acc = 0.0f;
-                    const float wg = acc * sh.g[lane];
-                    lam += (double)wg;
-                    sh.x[lane] = wg * sh.shut[lane];
-                }
+            if (w == 0 && lane < count) {
+                const float wg = (sh.decay[lane][0] + sh.decay[lane][1] + sh.decay[lane][2]) * sh.g[lane];
+                lam += (double)wg;
+                sh.dr[lane] = wg * sh.shut[lane];
+                sh.dbeta[lane] = BK::total(sh.sums[lane][2]) * sh.idle[lane];
             }
             wave_lds_fence();
         }
@@ -609,7 +636,7 @@ __global__ __launch_bounds__(4 * D, 2) void delta_bwd_kernel(DeltaArgs a)
         RW::store(a.dkey, RW::at(a.dkey, b, h, t0, tid), some, all, a.dk, tid, sh.k);
         RW::store(a.dval, RW::at(a.dval, b, h, t0, tid), some, all, a.dv, tid, sh.v);
         if (w == 0 && lane < all) {
-            const float x = lane < some ? sh.x[lane] : 0.0f, y = lane < some ? sh.dbeta[lane] : 0.0f;
+            const float x = lane < some ? sh.dr[lane] : 0.0f, y = lane < some ? sh.dbeta[lane] : 0.0f;
             char *pr = (char *)a.dr.p + b * a.dr.sb + h * a.dr.sh + (t0 + lane) * a.dr.st;
             char *pb = (char *)a.db.p + b * a.db.sb + h * a.db.sh + (t0 + lane) * a.db.st;
             if constexpr (BF) {

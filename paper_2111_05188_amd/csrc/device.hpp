@@ -108,7 +108,7 @@ __device__ __forceinline__ void box_muller_hw(float u0, float u1, float &z0, flo
 // row totals into the following rows.  A lane whose DPP source does not
 // exist (or whose row is masked off) receives 0.
 // ---------------------------------------------------------------------------
-enum : int { DPP_ROW_SHR = 0x110, DPP_ROW_BCAST15 = 0x142, DPP_ROW_BCAST31 = 0x143 };
+enum : int { DPP_ROW_SHL = 0x100, DPP_ROW_SHR = 0x110, DPP_ROW_BCAST15 = 0x142, DPP_ROW_BCAST31 = 0x143 };
 
 template <int CTRL, int ROWS = 0xF>
 __device__ __forceinline__ double dpp_f64(double x)
