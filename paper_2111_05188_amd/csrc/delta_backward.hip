@@ -184,7 +184,7 @@ struct Back {
     // the transpose.
     template <bool PART>
     static __device__ __forceinline__ Mine backward(Shared &sh, int s, int count, int p, int w, int lane, floatx4 *Gs,
-                                                    const Writes &x, const floatx4 *ST, floatx4 *GT)
+                                                    const Writes &x, floatx4 *GT)
     {
         const floatx4 U = x.U;
         lane = fresh(lane);
@@ -243,13 +243,6 @@ struct Back {
         }
         const float vd = row_sums(t, lane), ru = row_sums(u, lane);
         const float rs = row_sums(f, lane), ug = row_sums(g, lane);
-        float e = 0.0f;
-#pragma unroll
-        for (int kt = 0; kt < KT; ++kt)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) e += ST[kt][i] * GT[kt][i];
-        e = lanes_sum<64>(e);
-        if (lane == 0) sh.ends[p][w] = e * total;
         const floatx4 one = TL::wide(eye);
         mine.U = F::turned(U, one);
         mine.dR = F::turned(dR, one);
@@ -269,23 +262,30 @@ struct Back {
 
     // A wave's part of dY S0^T for all keys, and of P's gradient (turn 0), or of
     // rest rk U G1^T - beta gamma rk dR S0^T, and of L's (turn 1).
-    static __device__ __forceinline__ void give(Shared &sh, int turn, int w, int lane, const Mine &m,
+    static __device__ __forceinline__ void give(Shared &sh, int p, int turn, int w, int lane, const Mine &m,
                                                 const floatx4 *ST, const floatx4 *GT)
     {
         lane = fresh(lane);
         const int first = TURNS == 1 ? turn * HALF : 0;
+        float e = 0.0f;
 #pragma unroll
         for (int kt = 0; kt < KT; ++kt) {
             floatx4 x = {}, y = {};
             if (turn == 0) {
                 x = F::mm(m.dy, ST[kt], x);
             } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) e += ST[kt][i] * GT[kt][i];
                 x = F::mm(m.U, GT[kt], x);
                 y = F::mm(m.dR, ST[kt], y);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) x[i] = m.au[i] * x[i] - m.ak[i] * y[i];
             }
             sh.parts[first + kt][w][lane] = x;
+        }
+        if (turn == 1) {
+            e = lanes_sum<64>(e);
+            if (lane == 0) sh.ends[p][w] = e * sh.rows[p].total;
         }
         floatx4 z = {};
         sh.parts[first + KT][w][lane] = F::mm(turn == 0 ? m.dy : m.dR, m.U, z);
@@ -591,14 +591,13 @@ __global__ __launch_bounds__(4 * D, 2) void delta_bwd_kernel(DeltaArgs a)
                     if (done(p)) BK::clear(Gs);
                     typename BK::Mine mine;
                     pieces_of(c, [&](auto m) {
-                        mine = BK::template backward<decltype(m)::value>(sh, at[p], c, p, w, lane, Gs, X[p], ST[p],
-                                                                            GT);
+                        mine = BK::template backward<decltype(m)::value>(sh, at[p], c, p, w, lane, Gs, X[p], GT);
                     });
                     // the waves' parts to the waves that have the keys' columns
                     if (p + 1 < NP) workgroup_lds_barrier();
 #pragma unroll
                     for (int x = 0; x < 2; ++x) {
-                        BK::give(sh, x, w, lane, mine, ST[p], GT);
+                        BK::give(sh, p, x, w, lane, mine, ST[p], GT);
                         if (x == 0 && BK::TURNS == 1) continue;
                         if (x == 1 && p == 0 && batch == 0 && grp > first) fetch(grp - 1);
                         workgroup_lds_barrier();
