@@ -851,8 +851,8 @@ size_t tp_policy_workspace_bytes(const tp_policy *cfg);
  *   stats [6] fp64: L, its first term, the mean KL, H, the fraction of rows with
  *   rho outside the clips, N (0 rows: L = -ent_coef H, the means 0);
  *   dmu [T*B][ld_dmu], 0 in the rows that no sequence has; dlog_std [n].
- * Where rho A equals the clipped one the gradient is rho A's.  Sums run in a fixed
- * order.
+ * Where rho A equals the clipped one the gradient is rho A's.  A NaN in what a row
+ * that counts reads reaches L, the row's dmu and dlog_std.  Sums run in a fixed order.
  */
 int tp_policy_loss(const tp_policy *cfg, const void *mu, int64_t ld_mu, const float *action,
                    const float *logp, const float *adv, const float *mu_ref, double *stats,

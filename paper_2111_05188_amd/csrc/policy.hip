@@ -159,7 +159,8 @@ __global__ __launch_bounds__(256) void policy_kernel(PolicyArgs a)
             const double ratio = exp(-0.5 * q - ls_sum - old);
             const double clipped = ratio < lo ? lo : ratio > hi ? hi : ratio;
             const double s1 = ratio * A, s2 = clipped * A;
-            const bool open = s1 <= s2;
+            // (a NaN that the row brought goes on to the gradient, infinity times no advantage does not)
+            const bool open = s1 <= s2 || ratio != ratio || A != A;
             w = open ? -s1 * share : 0.0;
             if (lane == 0) {
                 sum_s += open ? s1 : s2;
