@@ -771,8 +771,8 @@ int tp_delta_step(const tp_delta *cfg, const tp_heads *q, const tp_heads *k, con
  * rms(v) = sqrt(mean v^2 + eps), y's over each of `groups` groups of neighbouring
  * channels (heads).  y NULL: X = x; z NULL: no gate; w_post NULL: y as it is;
  * scale NULL: 1; w_pre NULL: no n.  z, w_post and scale need y.
- * Rows are all fp32 or all bf16; arithmetic and sums are fp32 (the weights'
- * gradients' last sums fp64), each output is rounded once, n is taken from X
+ * Rows are all fp32 or all bf16; arithmetic and a row's sums are fp32 (the
+ * weights' gradients' sums over more than 32 rows fp64), each output is rounded once, n is taken from X
  * before its rounding.
  */
 typedef struct tp_norm {

@@ -1381,7 +1381,7 @@ int tp_norm_backward(const tp_norm *cfg, const tp_matrix *x, const tp_matrix *y,
     a.dw_post = dw_post;
     a.dscale = dscale;
     a.dw_pre = dw_pre;
-    a.parts = (float *)work;
+    a.parts = (double *)work;
     hipError_t e = launch_norm(a, true, (hipStream_t)stream);
     if (e != hipSuccess) return hip_fail(e, "norm gradient launch");
     return ok();

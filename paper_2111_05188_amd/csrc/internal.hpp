@@ -290,7 +290,7 @@ struct NormArgs {
     const float *w_post, *scale, *w_pre;
     NormRows x, y, z, x_out, n, dx_out, dn, dx, dy, dz;
     float *dw_post, *dscale, *dw_pre;
-    float *parts;              // the workspace
+    double *parts;             // the workspace
     int group, mode;           // filled by the launcher
 };
 

@@ -7,8 +7,8 @@
 // vectors of V elements each, and go from row to row with the weights in
 // registers.  All arithmetic is fp32; every output is rounded once (n is taken from
 // X before its rounding).  One pass: forward three arrays in and two out, backward
-// five in and three out, with the weights' gradients summed per lane, joined per
-// workgroup and then, in 64 bits and a fixed order, over the workgroups.
+// five in and three out, with the weights' gradients summed per lane in fp32 over 32
+// rows at most, and in 64 bits and a fixed order over a workgroup's and over all.
 //
 // Memory bounds it: 1,597,440 rows of 256 in bf16 forward 864 us (4.7 TB/s, the rate of a
 // copy); 258,048 odd rows of 301 in fp32 forward 390 us (4.0 TB/s) and back 542
@@ -20,6 +20,7 @@ namespace tpk {
 namespace {
 
 constexpr int NORM_BLOCKS = 1024;           // workgroups, and parts of the weights' gradients
+constexpr int NORM_ROWS = 32;               // rows that a lane adds up in fp32
 
 template <bool BF, int V>
 struct Vec {
@@ -249,149 +250,152 @@ __global__ __launch_bounds__(256) void norm_bwd_kernel(NormArgs a)
     constexpr int RPB = 256 / LPR, C = LPR * NV * V;
     const int lane = threadIdx.x % LPR, slot = threadIdx.x / LPR;
     float wp[NV][V], sc[NV][V], wq[NV][V];
-    float gp[NV][V] = {}, gs[NV][V] = {}, gq[NV][V] = {};
     load_weights<V, LPR, NV>(a.w_post, lane, a.D, wp);
     load_weights<V, LPR, NV>(a.scale, lane, a.D, sc);
     load_weights<V, LPR, NV>(a.w_pre, lane, a.D, wq);
     const float inv_group = 1.0f / (float)a.group, inv_D = 1.0f / (float)a.D;
-    for (int64_t r0 = (int64_t)blockIdx.x * RPB; r0 < a.rows; r0 += (int64_t)gridDim.x * RPB) {
-        const int64_t r = r0 + slot;
-        const bool live = r < a.rows;
-        float X[NV][V], y[NV][V], z[NV][V], ry[NV][V], dX[NV][V], dn[NV][V];
-#pragma unroll
-        for (int j = 0; j < NV; ++j) {
-            const int c = (j * LPR + lane) * V;
-            load_vec<BF, V>(live ? row_of(a.x, r) : nullptr, c, a.D, X[j]);
-            load_vec<BF, V>(live ? row_of(a.y, r) : nullptr, c, a.D, y[j]);
-            load_vec<BF, V>(live ? row_of(a.z, r) : nullptr, c, a.D, z[j]);
-            load_vec<BF, V>(live ? row_of(a.dx_out, r) : nullptr, c, a.D, dX[j]);
-            load_vec<BF, V>(live ? row_of(a.dn, r) : nullptr, c, a.D, dn[j]);
-        }
-        if (a.y.p && a.w_post) {
-#pragma unroll
-            for (int j = 0; j < NV; ++j)
-#pragma unroll
-                for (int e = 0; e < V; ++e) ry[j][e] = y[j][e] * y[j][e];
-            group_sums<V, LPR, NV>(a, lane, ry, lds);
-#pragma unroll
-            for (int j = 0; j < NV; ++j)
-#pragma unroll
-                for (int e = 0; e < V; ++e) {
-                    ry[j][e] = rsqrtf(ry[j][e] * inv_group + a.eps);
-                    y[j][e] = y[j][e] * ry[j][e];                       // yn
-                }
-        }
-        if (a.y.p) {
-#pragma unroll
-            for (int j = 0; j < NV; ++j)
-#pragma unroll
-                for (int e = 0; e < V; ++e) {
-                    float f = y[j][e] * (a.w_post ? wp[j][e] : 1.0f);
-                    if (a.z.p) f = f * (z[j][e] * norm_sigmoid(z[j][e]));
-                    X[j][e] = X[j][e] + sc[j][e] * f;
-                }
-        }
-        if (a.dn.p) {
-            float t = 0.0f, u = 0.0f;
-#pragma unroll
-            for (int j = 0; j < NV; ++j)
-#pragma unroll
-                for (int e = 0; e < V; ++e) {
-                    t += X[j][e] * X[j][e];
-                    u += X[j][e] * (dn[j][e] * wq[j][e]);
-                }
-            t = row_total<LPR>(t, lds);
-            u = row_total<LPR>(u, lds);
-            const float rx = rsqrtf(t * inv_D + a.eps), m = u * rx * inv_D;
-#pragma unroll
-            for (int j = 0; j < NV; ++j)
-#pragma unroll
-                for (int e = 0; e < V; ++e) {
-                    const float xn = X[j][e] * rx;
-                    dX[j][e] += rx * (dn[j][e] * wq[j][e] - xn * m);
-                    gq[j][e] += dn[j][e] * xn;
-                }
-        }
-        if (live)
-#pragma unroll
-            for (int j = 0; j < NV; ++j)
-                store_vec<BF, V>((void *)row_of(a.dx, r), (j * LPR + lane) * V, a.D, dX[j]);
-        if (!a.y.p) continue;
-        float s[NV][V];
-#pragma unroll
-        for (int j = 0; j < NV; ++j) {
-            float dz[V];
-#pragma unroll
-            for (int e = 0; e < V; ++e) {
-                const float w = a.w_post ? wp[j][e] : 1.0f, yn = y[j][e];
-                float g = 1.0f, slope = 0.0f;
-                if (a.z.p) {
-                    const float sg = norm_sigmoid(z[j][e]);
-                    g = z[j][e] * sg;
-                    slope = sg * (1.0f + z[j][e] * (1.0f - sg));
-                }
-                gs[j][e] += dX[j][e] * (yn * w * g);
-                const float df = dX[j][e] * sc[j][e];
-                gp[j][e] += df * (yn * g);
-                dz[e] = df * (yn * w) * slope;
-                dX[j][e] = df * w * g;                                  // d
-                s[j][e] = dX[j][e] * yn;
-            }
-            if (live && a.dz.p) store_vec<BF, V>((void *)row_of(a.dz, r), (j * LPR + lane) * V, a.D, dz);
-        }
-        if (a.w_post) {
-            group_sums<V, LPR, NV>(a, lane, s, lds);
-#pragma unroll
-            for (int j = 0; j < NV; ++j)
-#pragma unroll
-                for (int e = 0; e < V; ++e)
-                    dX[j][e] = ry[j][e] * (dX[j][e] - y[j][e] * (s[j][e] * inv_group));
-        }
-        if (live)
-#pragma unroll
-            for (int j = 0; j < NV; ++j)
-                store_vec<BF, V>((void *)row_of(a.dy, r), (j * LPR + lane) * V, a.D, dX[j]);
-    }
-    // this workgroup's part of the weights' gradients: [3][D] of it
+    // this workgroup's part of the weights' gradients, [3][D]: the lanes' sums go there
     __shared__ float join[RPB > 1 ? RPB * C : 1];
-    float *part = a.parts + (int64_t)blockIdx.x * 3 * a.D;
+    double *part = a.parts + (int64_t)blockIdx.x * 3 * a.D;
+    int64_t r0 = (int64_t)blockIdx.x * RPB;
+    for (bool more = false; r0 < a.rows; more = true) {
+        float gp[NV][V] = {}, gs[NV][V] = {}, gq[NV][V] = {};
+        for (int turn = 0; turn < NORM_ROWS && r0 < a.rows; ++turn, r0 += (int64_t)gridDim.x * RPB) {
+            const int64_t r = r0 + slot;
+            const bool live = r < a.rows;
+            float X[NV][V], y[NV][V], z[NV][V], ry[NV][V], dX[NV][V], dn[NV][V];
 #pragma unroll
-    for (int k = 0; k < 3; ++k) {
-        float (*g)[V] = k == 0 ? gp : k == 1 ? gs : gq;
-        if constexpr (RPB > 1) {
-            __syncthreads();
-#pragma unroll
-            for (int j = 0; j < NV; ++j)
-#pragma unroll
-                for (int e = 0; e < V; ++e) join[slot * C + (j * LPR + lane) * V + e] = g[j][e];
-            __syncthreads();
-            for (int c = threadIdx.x; c < a.D; c += 256) {
-                float t = 0.0f;
-#pragma unroll
-                for (int q = 0; q < RPB; ++q) t += join[q * C + c];
-                part[k * a.D + c] = t;
+            for (int j = 0; j < NV; ++j) {
+                const int c = (j * LPR + lane) * V;
+                load_vec<BF, V>(live ? row_of(a.x, r) : nullptr, c, a.D, X[j]);
+                load_vec<BF, V>(live ? row_of(a.y, r) : nullptr, c, a.D, y[j]);
+                load_vec<BF, V>(live ? row_of(a.z, r) : nullptr, c, a.D, z[j]);
+                load_vec<BF, V>(live ? row_of(a.dx_out, r) : nullptr, c, a.D, dX[j]);
+                load_vec<BF, V>(live ? row_of(a.dn, r) : nullptr, c, a.D, dn[j]);
             }
-        } else {
+            if (a.y.p && a.w_post) {
 #pragma unroll
-            for (int j = 0; j < NV; ++j)
+                for (int j = 0; j < NV; ++j)
+#pragma unroll
+                    for (int e = 0; e < V; ++e) ry[j][e] = y[j][e] * y[j][e];
+                group_sums<V, LPR, NV>(a, lane, ry, lds);
+#pragma unroll
+                for (int j = 0; j < NV; ++j)
+#pragma unroll
+                    for (int e = 0; e < V; ++e) {
+                        ry[j][e] = rsqrtf(ry[j][e] * inv_group + a.eps);
+                        y[j][e] = y[j][e] * ry[j][e];                       // yn
+                    }
+            }
+            if (a.y.p) {
+#pragma unroll
+                for (int j = 0; j < NV; ++j)
+#pragma unroll
+                    for (int e = 0; e < V; ++e) {
+                        float f = y[j][e] * (a.w_post ? wp[j][e] : 1.0f);
+                        if (a.z.p) f = f * (z[j][e] * norm_sigmoid(z[j][e]));
+                        X[j][e] = X[j][e] + sc[j][e] * f;
+                    }
+            }
+            if (a.dn.p) {
+                float t = 0.0f, u = 0.0f;
+#pragma unroll
+                for (int j = 0; j < NV; ++j)
+#pragma unroll
+                    for (int e = 0; e < V; ++e) {
+                        t += X[j][e] * X[j][e];
+                        u += X[j][e] * (dn[j][e] * wq[j][e]);
+                    }
+                t = row_total<LPR>(t, lds);
+                u = row_total<LPR>(u, lds);
+                const float rx = rsqrtf(t * inv_D + a.eps), m = u * rx * inv_D;
+#pragma unroll
+                for (int j = 0; j < NV; ++j)
+#pragma unroll
+                    for (int e = 0; e < V; ++e) {
+                        const float xn = X[j][e] * rx;
+                        dX[j][e] += rx * (dn[j][e] * wq[j][e] - xn * m);
+                        gq[j][e] += dn[j][e] * xn;
+                    }
+            }
+            if (live)
+#pragma unroll
+                for (int j = 0; j < NV; ++j)
+                    store_vec<BF, V>((void *)row_of(a.dx, r), (j * LPR + lane) * V, a.D, dX[j]);
+            if (!a.y.p) continue;
+            float s[NV][V];
+#pragma unroll
+            for (int j = 0; j < NV; ++j) {
+                float dz[V];
 #pragma unroll
                 for (int e = 0; e < V; ++e) {
-                    const int c = (j * LPR + lane) * V + e;
-                    if (c < a.D) part[k * a.D + c] = g[j][e];
+                    const float w = a.w_post ? wp[j][e] : 1.0f, yn = y[j][e];
+                    float g = 1.0f, slope = 0.0f;
+                    if (a.z.p) {
+                        const float sg = norm_sigmoid(z[j][e]);
+                        g = z[j][e] * sg;
+                        slope = sg * (1.0f + z[j][e] * (1.0f - sg));
+                    }
+                    gs[j][e] += dX[j][e] * (yn * w * g);
+                    const float df = dX[j][e] * sc[j][e];
+                    gp[j][e] += df * (yn * g);
+                    dz[e] = df * (yn * w) * slope;
+                    dX[j][e] = df * w * g;                                  // d
+                    s[j][e] = dX[j][e] * yn;
                 }
+                if (live && a.dz.p) store_vec<BF, V>((void *)row_of(a.dz, r), (j * LPR + lane) * V, a.D, dz);
+            }
+            if (a.w_post) {
+                group_sums<V, LPR, NV>(a, lane, s, lds);
+#pragma unroll
+                for (int j = 0; j < NV; ++j)
+#pragma unroll
+                    for (int e = 0; e < V; ++e)
+                        dX[j][e] = ry[j][e] * (dX[j][e] - y[j][e] * (s[j][e] * inv_group));
+            }
+            if (live)
+#pragma unroll
+                for (int j = 0; j < NV; ++j)
+                    store_vec<BF, V>((void *)row_of(a.dy, r), (j * LPR + lane) * V, a.D, dX[j]);
+        }
+#pragma unroll
+        for (int k = 0; k < 3; ++k) {
+            float (*g)[V] = k == 0 ? gp : k == 1 ? gs : gq;
+            if constexpr (RPB > 1) {
+                __syncthreads();
+#pragma unroll
+                for (int j = 0; j < NV; ++j)
+#pragma unroll
+                    for (int e = 0; e < V; ++e) join[slot * C + (j * LPR + lane) * V + e] = g[j][e];
+                __syncthreads();
+                for (int c = threadIdx.x; c < a.D; c += 256) {
+                    double t = more ? part[k * a.D + c] : 0.0;
+#pragma unroll
+                    for (int q = 0; q < RPB; ++q) t += (double)join[q * C + c];
+                    part[k * a.D + c] = t;
+                }
+            } else {
+#pragma unroll
+                for (int j = 0; j < NV; ++j)
+#pragma unroll
+                    for (int e = 0; e < V; ++e) {
+                        const int c = (j * LPR + lane) * V + e;
+                        if (c < a.D) part[k * a.D + c] = (more ? part[k * a.D + c] : 0.0) + (double)g[j][e];
+                    }
+            }
         }
     }
 }
 
 // sums of the workgroups' parts, 16 channels a workgroup, 16 rows at a time
-__global__ __launch_bounds__(256) void norm_join_kernel(const float *parts, int blocks, int D, float *w0, float *w1,
+__global__ __launch_bounds__(256) void norm_join_kernel(const double *parts, int blocks, int D, float *w0, float *w1,
                                                         float *w2)
 {
     __shared__ double red[16][17];
     const int c = threadIdx.x & 15, q = threadIdx.x >> 4, d = blockIdx.x * 16 + c;
     double s = 0.0;
     if (d < 3 * D)
-        for (int k = q; k < blocks; k += 16) s += (double)parts[(int64_t)k * 3 * D + d];
+        for (int k = q; k < blocks; k += 16) s += parts[(int64_t)k * 3 * D + d];
     red[q][c] = s;
     __syncthreads();
     if (q != 0 || d >= 3 * D) return;
@@ -404,7 +408,6 @@ __global__ __launch_bounds__(256) void norm_join_kernel(const float *parts, int 
 template <bool BF, int V, int LPR, int NV>
 void start_norm(NormArgs &a, bool backward, hipStream_t s)
 {
-    // rows and all its gradients of a workgroup in LDS: at most 64 KiB
     constexpr int RPB = 256 / LPR;
     const int64_t want = (a.rows + RPB - 1) / RPB;
     const int blocks = (int)(want < NORM_BLOCKS * (backward ? 1 : 2) ? want : NORM_BLOCKS * (backward ? 1 : 2));
@@ -461,7 +464,7 @@ void start_norm(NormArgs &a, bool backward, hipStream_t s)
 
 size_t norm_workspace_bytes(int D)
 {
-    return ((size_t)NORM_BLOCKS * 3 * D * sizeof(float) + 255) / 256 * 256;
+    return ((size_t)NORM_BLOCKS * 3 * D * sizeof(double) + 255) / 256 * 256;
 }
 
 hipError_t launch_norm(NormArgs &a, bool backward, hipStream_t s)

@@ -58,3 +58,29 @@ def test_gates_far_from_zero(D):
     want = blocks.norm_backward(**c.exact(), dx_out=host(c.t["dx_out"]))
     err = np.abs(host(new[3]) - want["dz"]) / (want["dz_size"] + 1e-36)
     assert err.max() <= 23 * 2.0 ** -24, err.max() * 2 ** 24
+
+
+@pytest.mark.parametrize("dtype", BOTH)
+@pytest.mark.parametrize("M,D", [(1 << 20, 513), (1 << 24, 8)])
+def test_weights_gradients_of_many_rows(M, D, dtype):
+    """Of rows all alike, as many times one's, whatever their number.  Half steps of 2^-24 in a row's
+    terms: x (of ones) squared and added up none, their mean, root and product with x 4, with dn 1, f's
+    5 more; sums of 32 of them 32 in fp32 at most, 2^-24 each of the largest partial sum: 42 in all, of
+    which equal terms' sums, that round alike, may use up any number; 64-bit sums of the rest none.  The
+    result's own rounding 1."""
+    g = torch.Generator("cuda").manual_seed(D)
+    rows = lambda v: v.to(dtype).expand(M, D).contiguous()  # noqa: E731
+    vec = lambda: torch.rand(D, generator=g, device="cuda") + 0.5  # noqa: E731
+    x, y, dn, dx_out = torch.ones(D, device="cuda"), torch.zeros(D, device="cuda"), vec(), vec()
+    y[::2] = 1.0
+    w_pre, w_post, scale = vec(), vec(), vec()
+    nc = tp.NormT(M, D, dtype, w_pre=w_pre, w_post=w_post, scale=scale)
+    out = [torch.empty(M, D, dtype=dtype, device="cuda") for _ in range(2)]
+    dw = [torch.empty(D, device="cuda") for _ in range(3)]
+    tp.norm_backward(nc, rows(x), rows(y), None, rows(dx_out), rows(dn), *out, None, *dw, nc.workspace())
+    one = lambda v: host(v.to(dtype))[None]  # noqa: E731
+    want = blocks.norm_backward(one(x), one(y), w_post=host(w_post), scale=host(scale), w_pre=host(w_pre),
+                                dx_out=one(dx_out), dn=one(dn))
+    for got, k in zip(dw, ("dw_post", "dscale", "dw_pre")):
+        err = np.abs(host(got) - M * want[k]) / (M * want[k + "_size"] + 1e-30)
+        assert err.max() <= 43 * 2.0 ** -24, (k, err.max() * 2 ** 24)
