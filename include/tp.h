@@ -792,8 +792,9 @@ typedef struct tp_matrix {
 } tp_matrix;
 
 /*
- * tp_norm_forward -- x_out = X and n; one of them may be NULL.  x_out may be x
- * (the same pointer and pitch).
+ * tp_norm_forward -- x_out = X and n; one of them may be NULL.  An output may be
+ * an input (the same pointer and pitch: x_out x, say); one that overlaps an array
+ * otherwise is refused.
  */
 int tp_norm_forward(const tp_norm *cfg, const tp_matrix *x, const tp_matrix *y,
                     const tp_matrix *z, const tp_matrix *x_out, const tp_matrix *n,
@@ -806,8 +807,9 @@ size_t tp_norm_workspace_bytes(const tp_norm *cfg);
 /*
  * tp_norm_backward -- gradients from dx_out and dn (either may be NULL, zeros; dn
  * needs w_pre) and the forward call's inputs.  dx is needed, dy and dz where y and
- * z are there; dw_post, dscale, dw_pre [D] or NULL.  dx may be dx_out (the same
- * pointer and pitch).  Sums over rows run in a fixed order.
+ * z are there; dw_post, dscale, dw_pre [D] or NULL.  An output may be an input (the same
+ * pointer and pitch: dx dx_out, dy y, say); one that overlaps an array, or the
+ * workspace, otherwise is refused.  Sums over rows run in a fixed order.
  */
 int tp_norm_backward(const tp_norm *cfg, const tp_matrix *x, const tp_matrix *y,
                      const tp_matrix *z, const tp_matrix *dx_out, const tp_matrix *dn,

@@ -454,6 +454,58 @@ int check_norm_rows(const tp_norm *c, const tp_matrix *m, const char *name, bool
     return TP_OK;
 }
 
+// Memory of a norm's array: rows of `width` bytes, `ld` apart.
+struct NormArea {
+    const char *name;
+    uintptr_t p;
+    int64_t rows, ld, width;
+};
+
+// Whether some row of a shares a byte with one of b.  Of unlike pitches the first 4,096 rows
+// that may meet are looked at.
+bool norm_overlap(NormArea a, NormArea b)
+{
+    if (a.p > b.p) std::swap(a, b);
+    const uint64_t d = b.p - a.p, last = (uint64_t)(a.rows - 1) * a.ld;
+    if (d >= last + a.width) return false;
+    // b's row at byte `off` of a's: the row of a that begins at or before it, and the next
+    const auto meet = [&](uint64_t off) {
+        const uint64_t j = a.rows == 1 ? 0 : off / a.ld, rem = off - j * a.ld;
+        return (j < (uint64_t)a.rows && rem < (uint64_t)a.width) ||
+               (j + 1 < (uint64_t)a.rows && a.ld - rem < (uint64_t)b.width);
+    };
+    if (a.rows == b.rows && a.ld == b.ld) return meet(d);       // (the other rows lie alike)
+    for (int64_t i = 0; i < b.rows && i < 4096; ++i) {
+        const uint64_t off = d + (uint64_t)i * b.ld;
+        if (off >= last + a.width) break;
+        if (meet(off)) return true;
+    }
+    return false;
+}
+
+// Outputs (the first `outputs` of n) are arrays of their own, or an input's rows in place.
+int check_norm_overlap(const NormArea *area, int outputs, int n)
+{
+    for (int i = 0; i < outputs; ++i)
+        for (int j = i + 1; j < n; ++j) {
+            const NormArea &a = area[i], &b = area[j];
+            if (!a.p || !b.p || !norm_overlap(a, b)) continue;
+            if (j >= outputs && a.p == b.p && a.ld == b.ld && a.rows == b.rows && a.width == b.width) continue;
+            return fail(TP_EINVAL, "norm: %s overlaps %s", a.name, b.name);
+        }
+    return TP_OK;
+}
+
+NormArea norm_rows_area(const tp_norm *c, const char *name, const NormRows &m)
+{
+    return {name, (uintptr_t)m.p, c->rows, m.ld, (int64_t)c->D * (c->dtype == TP_BF16 ? 2 : 4)};
+}
+
+NormArea norm_weight_area(const tp_norm *c, const char *name, const float *w)
+{
+    return {name, (uintptr_t)w, 1, 0, (int64_t)c->D * 4};
+}
+
 // what both calls share
 int norm_args(const tp_norm *c, const tp_matrix *x, const tp_matrix *y, const tp_matrix *z, NormArgs *a)
 {
@@ -1340,6 +1392,11 @@ int tp_norm_forward(const tp_norm *cfg, const tp_matrix *x, const tp_matrix *y, 
     if (a.n.p && !cfg->w_pre) return fail(TP_EINVAL, "norm: n needs w_pre");
     if (a.x_out.p == a.x.p && a.x_out.ld != a.x.ld)
         return fail(TP_EINVAL, "norm: x_out is x with another pitch");
+    const NormArea area[] = {norm_rows_area(cfg, "x_out", a.x_out), norm_rows_area(cfg, "n", a.n),
+                             norm_rows_area(cfg, "x", a.x), norm_rows_area(cfg, "y", a.y),
+                             norm_rows_area(cfg, "z", a.z), norm_weight_area(cfg, "w_post", cfg->w_post),
+                             norm_weight_area(cfg, "scale", cfg->scale), norm_weight_area(cfg, "w_pre", cfg->w_pre)};
+    if ((rc = check_norm_overlap(area, 2, 8)) != TP_OK) return rc;
     hipError_t e = launch_norm(a, false, (hipStream_t)stream);
     if (e != hipSuccess) return hip_fail(e, "norm launch");
     return ok();
@@ -1378,6 +1435,15 @@ int tp_norm_backward(const tp_norm *cfg, const tp_matrix *x, const tp_matrix *y,
         return fail(TP_EINVAL, "norm workspace is NULL or not 256-byte aligned");
     const size_t need = norm_workspace_bytes(cfg->D);
     if (work_bytes < need) return fail(TP_EINVAL, "norm workspace of %zu bytes, %zu needed", work_bytes, need);
+    const NormArea area[] = {norm_rows_area(cfg, "dx", a.dx), norm_rows_area(cfg, "dy", a.dy),
+                             norm_rows_area(cfg, "dz", a.dz), norm_weight_area(cfg, "dw_post", dw_post),
+                             norm_weight_area(cfg, "dscale", dscale), norm_weight_area(cfg, "dw_pre", dw_pre),
+                             {"the workspace", (uintptr_t)work, 1, 0, (int64_t)need},
+                             norm_rows_area(cfg, "x", a.x), norm_rows_area(cfg, "y", a.y),
+                             norm_rows_area(cfg, "z", a.z), norm_rows_area(cfg, "dx_out", a.dx_out),
+                             norm_rows_area(cfg, "dn", a.dn), norm_weight_area(cfg, "w_post", cfg->w_post),
+                             norm_weight_area(cfg, "scale", cfg->scale), norm_weight_area(cfg, "w_pre", cfg->w_pre)};
+    if ((rc = check_norm_overlap(area, 7, 15)) != TP_OK) return rc;
     a.dw_post = dw_post;
     a.dscale = dscale;
     a.dw_pre = dw_pre;

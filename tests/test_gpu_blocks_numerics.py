@@ -84,3 +84,32 @@ def test_weights_gradients_of_many_rows(M, D, dtype):
     for got, k in zip(dw, ("dw_post", "dscale", "dw_pre")):
         err = np.abs(host(got) - M * want[k]) / (M * want[k + "_size"] + 1e-30)
         assert err.max() <= 43 * 2.0 ** -24, (k, err.max() * 2 ** 24)
+
+
+@pytest.mark.parametrize("dtype", BOTH)
+@pytest.mark.parametrize("D", [128, 301])
+def test_outputs_in_the_inputs_places_and_between_their_rows(D, dtype):
+    """An output in any input's buffer, and arrays side by side in one buffer's rows, whole or with other
+    pitches one after the other."""
+    c = Norm(300, D, 1, dtype, seed=7)
+    X, n = c.forward()
+    want = c.backward()
+    t = {k: v.clone() for k, v in c.t.items()}
+    tp.norm_forward(c.nc, t["x"], t["y"], t["z"], t["z"], t["y"])
+    assert torch.equal(t["z"], X) and torch.equal(t["y"], n)
+    t = {k: v.clone() for k, v in c.t.items()}
+    dw = [torch.empty(D, device="cuda") for _ in range(3)]
+    tp.norm_backward(c.nc, t["x"], t["y"], t["z"], t["dx_out"], t["dn"], t["dn"], t["y"], t["z"], *dw,
+                     c.nc.workspace())
+    assert all(torch.equal(t[a], want[b]) for a, b in (("dn", "dx"), ("y", "dy"), ("z", "dz")))
+    assert all(torch.equal(a, want[b]) for a, b in zip(dw, ("dw_post", "dscale", "dw_pre")))
+    wide = torch.empty(300, 5 * D, dtype=dtype, device="cuda")
+    part = [wide[:, i * D:(i + 1) * D] for i in range(5)]
+    for p, k in zip(part, "xyz"):
+        p.copy_(c.t[k])
+    tp.norm_forward(c.nc, *part)
+    assert torch.equal(part[3], X) and torch.equal(part[4], n)
+    flat = torch.empty(300 * 3 * D, dtype=dtype, device="cuda")
+    a, b = flat[:300 * D].view(300, D), flat[300 * D:].view(300, 2 * D)[:, D:]
+    tp.norm_forward(c.nc, c.t["x"], c.t["y"], c.t["z"], a, b)
+    assert torch.equal(a, X) and torch.equal(b, n)
