@@ -34,7 +34,7 @@ __device__ __forceinline__ void run_piece(const E *q, const E *k, E *v, int s, i
     constexpr int KT = D / 16;
     lane = fresh(lane);
     const int r = 4 * (lane >> 4);
-    floatx4 ks = {}, qs = {};
+    typename TL::sum2 ks, qs;
 #pragma unroll
     for (int kt = 0; kt < KT; kt += 2) {
         const auto x0 = TL::split(S[kt]), x1 = TL::split(S[kt + 1]);
@@ -45,15 +45,15 @@ __device__ __forceinline__ void run_piece(const E *q, const E *k, E *v, int s, i
     const floatx4 vv = TL::wide(along_col<BF, LD, MASK>(v, s, count, w, lane));
     const floatx4 be = *(const floatx4 *)(rows.beta + r), ak = *(const floatx4 *)(rows.ak + r);
     const floatx4 aq = *(const floatx4 *)(rows.aq + r), au = *(const floatx4 *)(rows.au + r);
-    floatx4 R, U = {}, o;
+    floatx4 R, o;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         R[i] = !MASK || r + i < count ? be[i] * vv[i] - ak[i] * ks[i] : 0.0f;
         o[i] = aq[i] * qs[i];
     }
-    U = Tile<false>::mm(Tt, R, U);
+    const floatx4 U = Tile<false>::mm(Tt, R, {}).v;
     if constexpr (OUT) {
-        o = Tile<false>::mm(Pt, U, o);
+        o = Tile<false>::mm(Pt, U, {o}).v;
 #pragma unroll
         for (int i = 0; i < 4; ++i)
             if (!MASK || r + i < count) v[(s + r + i) * LD + 16 * w + (lane & 15)] = (E)o[i];
@@ -69,7 +69,7 @@ __device__ __forceinline__ void run_piece(const E *q, const E *k, E *v, int s, i
     const auto x = TL::split(W);
 #pragma unroll
     for (int kt = 0; kt < KT; ++kt)
-        S[kt] = TL::mm(along_col<BF, LD, MASK>(k, s, count, kt, lane), x, S[kt] * rows.total);
+        S[kt] = TL::mm(along_col<BF, LD, MASK>(k, s, count, kt, lane), x, {S[kt] * rows.total}).v;
 }
 
 // what a piece does to the unit states (a value's columns are zero)
@@ -81,20 +81,21 @@ __device__ __forceinline__ void map_piece(const E *k, int s, int count, bool end
     constexpr int KT = D / 16;
     lane = fresh(lane);
     const int r = 4 * (lane >> 4);
-    floatx4 ks = {}, R, U = {}, W;
+    typename TL::sum2 ks;
+    floatx4 R, W;
 #pragma unroll
     for (int kt = 0; kt < KT; kt += 2)
         ks = TL::mm2(along_row<BF, LD>(k, s, kt, lane), along_row<BF, LD>(k, s, kt + 1, lane), TL::split(S[kt]),
                      TL::split(S[kt + 1]), ks);
 #pragma unroll
     for (int i = 0; i < 4; ++i) R[i] = !MASK || r + i < count ? -(rows.ak[r + i] * ks[i]) : 0.0f;
-    U = Tile<false>::mm(Tt, R, U);
+    const floatx4 U = Tile<false>::mm(Tt, R, {}).v;
 #pragma unroll
     for (int i = 0; i < 4; ++i) W[i] = !MASK || r + i < count ? U[i] * rows.au[r + i] : 0.0f;
     const auto x = TL::split(W);
 #pragma unroll
     for (int kt = 0; kt < KT; ++kt) {
-        S[kt] = TL::mm(along_col<BF, LD, MASK>(k, s, count, kt, lane), x, S[kt] * rows.total);
+        S[kt] = TL::mm(along_col<BF, LD, MASK>(k, s, count, kt, lane), x, {S[kt] * rows.total}).v;
         if (ends) S[kt] = floatx4{};
     }
 }
@@ -338,15 +339,14 @@ __global__ __launch_bounds__(4 * D) void delta_join_kernel(DeltaJoin a)
         if (x >= steps) return;
         cut = cut || g.cut != 0;
         workgroup_lds_barrier();
-        S = g.add;
-        floatx4 half = {};                  // (two chains of products)
+        Sum<4> one{g.add}, half;            // (two chains of products)
         if (g.cut == 0)
 #pragma unroll
             for (int kt = 0; kt < KT; kt += 2) {
-                S = Tile<false>::mm(g.map[kt], state[x & 1][kt][lane], S);
+                one = Tile<false>::mm(g.map[kt], state[x & 1][kt][lane], one);
                 half = Tile<false>::mm(g.map[kt + 1], state[x & 1][kt + 1][lane], half);
             }
-        S += half;
+        S = one.v + half.v;
         if (x + 2 < steps) fetch(x + 2, g);
     };
     Segment even, odd;

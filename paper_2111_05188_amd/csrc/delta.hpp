@@ -40,6 +40,16 @@ constexpr float DELTA_LOG2E = 1.44269504088896341f;
 // ---------------------------------------------------------------------------
 template <bool BF> struct Tile;
 
+// An accumulator of products over K.  It takes products of one kind only, and starts from
+// zeros or a value that vector instructions made: hipcc puts no wait between two products
+// on one accumulator, whatever their kinds (its listing has them back to back), and of unlike
+// kinds the second read it before the first had written it (a product over 32 after one over
+// 16: y off by an ulp of bf16, not always the same ones).
+template <int K> struct Sum {
+    floatx4 v = {};
+    __device__ __forceinline__ float operator[](int i) const { return v[i]; }
+};
+
 template <> struct Tile<false> {
     typedef float elem;
     typedef floatx4 raw;
@@ -48,13 +58,14 @@ template <> struct Tile<false> {
     static __device__ __forceinline__ val split(floatx4 x) { return x; }
     static __device__ __forceinline__ floatx4 wide(raw x) { return x; }
     static __device__ __forceinline__ floatx4 whole(val x) { return x; }
-    static __device__ __forceinline__ floatx4 mm(floatx4 a, floatx4 b, floatx4 c)
+    typedef Sum<4> sum, sum2;                   // of products over 16 and over 32
+    static __device__ __forceinline__ sum mm(floatx4 a, floatx4 b, sum c)
     {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[i], b[i], c, 0, 0, 0);
+        for (int i = 0; i < 4; ++i) c.v = __builtin_amdgcn_mfma_f32_16x16x4f32(a[i], b[i], c.v, 0, 0, 0);
         return c;
     }
-    static __device__ __forceinline__ floatx4 mm2(val a0, val a1, val b0, val b1, floatx4 c)
+    static __device__ __forceinline__ sum2 mm2(val a0, val a1, val b0, val b1, sum2 c)
     {
         return mm(a1, b1, mm(a0, b0, c));
     }
@@ -66,7 +77,7 @@ template <> struct Tile<false> {
         for (int i = 0; i < 4; ++i) x[i] = 4 * (lane >> 4) + i == (lane & 15) ? 1.0f : 0.0f;
         return x;
     }
-    static __device__ __forceinline__ floatx4 turned(val x, raw eye) { return mm(x, eye, floatx4{}); }
+    static __device__ __forceinline__ floatx4 turned(val x, raw eye) { return mm(x, eye, {}).v; }
 };
 
 template <> struct Tile<true> {
@@ -109,27 +120,27 @@ template <> struct Tile<true> {
     {
         return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
     }
-    static __device__ __forceinline__ floatx4 go(bf16x8 a, bf16x8 b, floatx4 c)
+    typedef Sum<16> sum;
+    typedef Sum<32> sum2;
+    static __device__ __forceinline__ sum2 go(bf16x8 a, bf16x8 b, sum2 c)
     {
-        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+        return {__builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c.v, 0, 0, 0)};
     }
-    // Half the rate of the products over 32, but no register is copied to fill one.  One
-    // accumulator takes products of one kind only: a product over 32 right after one over
-    // 16 read it before it was there (y off by an ulp of bf16, not always the same ones).
-    static __device__ __forceinline__ floatx4 go(bf16x4 a, bf16x4 b, floatx4 c)
+    // Half the rate of the products over 32, but no register is copied to fill one.
+    static __device__ __forceinline__ sum go(bf16x4 a, bf16x4 b, sum c)
     {
         typedef short s4 __attribute__((ext_vector_type(4)));
         s4 x, y;
         __builtin_memcpy(&x, &a, sizeof x);
         __builtin_memcpy(&y, &b, sizeof y);
-        return __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(x, y, c, 0, 0, 0);
+        return {__builtin_amdgcn_mfma_f32_16x16x16bf16_1k(x, y, c.v, 0, 0, 0)};
     }
     // (the least products first)
-    static __device__ __forceinline__ floatx4 mm(raw a, val b, floatx4 c)
+    static __device__ __forceinline__ sum mm(raw a, val b, sum c)
     {
         return go(a, b.hi, go(a, b.mid, go(a, b.lo, c)));
     }
-    static __device__ __forceinline__ floatx4 mm(val a, raw b, floatx4 c)
+    static __device__ __forceinline__ sum mm(val a, raw b, sum c)
     {
         return go(a.hi, b, go(a.mid, b, go(a.lo, b, c)));
     }
@@ -142,16 +153,16 @@ template <> struct Tile<true> {
     }
     static __device__ __forceinline__ floatx4 turned(val x, raw eye)
     {
-        return go(x.hi, eye, go(x.mid, eye, go(x.lo, eye, floatx4{})));
+        return go(x.hi, eye, go(x.mid, eye, go(x.lo, eye, {}))).v;
     }
     // products over 32
-    static __device__ __forceinline__ floatx4 mm2(raw a0, raw a1, val b0, val b1, floatx4 c)
+    static __device__ __forceinline__ sum2 mm2(raw a0, raw a1, val b0, val b1, sum2 c)
     {
         c = go(join(a0, a1), join(b0.lo, b1.lo), c);
         c = go(join(a0, a1), join(b0.mid, b1.mid), c);
         return go(join(a0, a1), join(b0.hi, b1.hi), c);
     }
-    static __device__ __forceinline__ floatx4 mm2(raw a0, raw a1, raw b0, raw b1, floatx4 c)
+    static __device__ __forceinline__ sum2 mm2(raw a0, raw a1, raw b0, raw b1, sum2 c)
     {
         return go(join(a0, a1), join(b0, b1), c);
     }
@@ -384,7 +395,7 @@ __device__ __forceinline__ void piece_triangles(const E *q, const E *k, const fl
     lane = fresh(lane);
     constexpr bool Q = (WANT & (WANT_P | WANT_PT | WANT_ROWS)) != 0, B = (WANT & (WANT_T | WANT_ROWS)) != 0;
     const int n = lane & 15, grp = lane >> 4, r = 4 * grp;
-    floatx4 kk = {}, qq = {}, kq = {}, qk = {};
+    typename Tile<BF>::sum2 kk, qq, kq, qk;
 #pragma unroll
     for (int kt = 0; kt < D / 16; kt += 2) {
         const auto a0 = along_row<BF, LD>(k, s, kt, lane), b0 = along_row<BF, LD>(Q ? q : k, s, kt, lane);
@@ -400,10 +411,10 @@ __device__ __forceinline__ void piece_triangles(const E *q, const E *k, const fl
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const bool it = r + i < count && n < count;
-            kk[i] = it ? kk[i] : 0.0f;
-            qq[i] = it ? qq[i] : 0.0f;
-            kq[i] = it ? kq[i] : 0.0f;
-            qk[i] = it ? qk[i] : 0.0f;
+            kk.v[i] = it ? kk[i] : 0.0f;
+            qq.v[i] = it ? qq[i] : 0.0f;
+            kq.v[i] = it ? kq[i] : 0.0f;
+            qk.v[i] = it ? qk[i] : 0.0f;
         }
     }
     // lengths from the diagonals: lane 16 (n/4) + n has row n's
@@ -451,10 +462,9 @@ __device__ __forceinline__ void piece_triangles(const E *q, const E *k, const fl
             if (w > 2)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) off[i] = (w == 4 ? same8 && !same4 : !same8) ? -Lt[i] : 0.0f;
-            const floatx4 z = {};
-            const floatx4 Y = Tile<false>::mm(off, Tn, z);          // -L_off T
-            const floatx4 t = Tile<false>::mm(Y, Tt, Tt);           // T^T - (L_off T)^T T^T
-            if (BOTH || w < 8) Tn = Tile<false>::mm(Tt, Y, Tn);
+            const floatx4 Y = Tile<false>::mm(off, Tn, {}).v;       // -L_off T
+            const floatx4 t = Tile<false>::mm(Y, Tt, {Tt}).v;       // T^T - (L_off T)^T T^T
+            if (BOTH || w < 8) Tn = Tile<false>::mm(Tt, Y, {Tn}).v;
             Tt = t;
         }
     }

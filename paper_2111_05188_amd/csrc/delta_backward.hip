@@ -130,7 +130,8 @@ struct Back {
 #pragma unroll
         for (int kt = 0; kt < KT; ++kt) kc[kt] = along_col<BF, LD, PART>(sh.k, s, count, kt, lane);
         const raw eye = TL::eye(lane);
-        floatx4 ks = {}, qs = {}, U = {}, R, W, from;
+        typename TL::sum2 ks, qs;
+        floatx4 R, W, from;
 #pragma unroll
         for (int kt = 0; kt < KT; kt += 2) {
             const val x0 = TL::split(S[kt]), x1 = TL::split(S[kt + 1]);
@@ -146,12 +147,12 @@ struct Back {
             from[i] = ak[i] * ks[i];
             R[i] = !PART || r + i < count ? be[i] * vv[i] - from[i] : 0.0f;
         }
-        U = Tile<false>::mm(Tt, R, U);
+        const floatx4 U = F::mm(Tt, R, {}).v;
 #pragma unroll
         for (int i = 0; i < 4; ++i) W[i] = !PART || r + i < count ? U[i] * au[i] : 0.0f;
         const val y = TL::split(W);
 #pragma unroll
-        for (int kt = 0; kt < KT; ++kt) S[kt] = TL::mm(kc[kt], y, S[kt] * total);
+        for (int kt = 0; kt < KT; ++kt) S[kt] = TL::mm(kc[kt], y, {S[kt] * total}).v;
         if (ends) clear(S);
         if constexpr (OUT) {
             const floatx4 dy = TL::wide(dyc);
@@ -161,7 +162,7 @@ struct Back {
                 o[i] = aq[i] * qs[i];
                 u[i] = o[i] * dy[i];
             }
-            o = Tile<false>::mm(P, U, o);
+            o = F::mm(P, U, {o}).v;
 #pragma unroll
             for (int i = 0; i < 4; ++i) t[i] = o[i] * dy[i];
             const float yd = row_sums(t, lane), qd = row_sums(u, lane);
@@ -208,7 +209,8 @@ struct Back {
             kc[kt] = along_col<BF, LD, PART>(sh.k, s, count, kt, lane);
         }
         const raw eye = TL::eye(lane);
-        floatx4 kg = {}, dU, dR = {}, A, B;
+        typename TL::sum2 kg;
+        floatx4 dU, A, B;
 #pragma unroll
         for (int kt = 0; kt < KT; kt += 2) {
             const val x0 = TL::split(Gs[kt]), x1 = TL::split(Gs[kt + 1]);
@@ -218,8 +220,8 @@ struct Back {
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i) dU[i] = !PART || r + i < count ? kg[i] * au[i] : 0.0f;
-        dU = TL::mm(Pn, dyc, dU);
-        dR = Tile<false>::mm(Tn, dU, dR);
+        dU = TL::mm(Pn, dyc, {dU}).v;
+        const floatx4 dR = F::mm(Tn, dU, {}).v;
         const floatx4 dyw = TL::wide(dyc);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -228,10 +230,7 @@ struct Back {
         }
         const val a = TL::split(A), b = TL::split(B);
 #pragma unroll
-        for (int kt = 0; kt < KT; ++kt) {
-            Gs[kt] = TL::mm(qc[kt], a, Gs[kt] * total);
-            Gs[kt] = TL::mm(kc[kt], b, Gs[kt]);
-        }
+        for (int kt = 0; kt < KT; ++kt) Gs[kt] = TL::mm(kc[kt], b, TL::mm(qc[kt], a, {Gs[kt] * total})).v;
         floatx4 dv, t, u, f, g;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -270,14 +269,14 @@ struct Back {
         float e = 0.0f;
 #pragma unroll
         for (int kt = 0; kt < KT; ++kt) {
-            floatx4 x = {}, y = {};
+            floatx4 x;
             if (turn == 0) {
-                x = F::mm(m.dy, ST[kt], x);
+                x = F::mm(m.dy, ST[kt], {}).v;
             } else {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) e += ST[kt][i] * GT[kt][i];
-                x = F::mm(m.U, GT[kt], x);
-                y = F::mm(m.dR, ST[kt], y);
+                x = F::mm(m.U, GT[kt], {}).v;
+                const floatx4 y = F::mm(m.dR, ST[kt], {}).v;
 #pragma unroll
                 for (int i = 0; i < 4; ++i) x[i] = m.au[i] * x[i] - m.ak[i] * y[i];
             }
@@ -287,8 +286,7 @@ struct Back {
             e = lanes_sum<64>(e);
             if (lane == 0) sh.ends[p][w] = e * sh.rows[p].total;
         }
-        floatx4 z = {};
-        sh.parts[first + KT][w][lane] = F::mm(turn == 0 ? m.dy : m.dR, m.U, z);
+        sh.parts[first + KT][w][lane] = F::mm(turn == 0 ? m.dy : m.dR, m.U, {}).v;
     }
 
     // the sum of all waves' parts of a tile
@@ -325,7 +323,7 @@ struct Back {
         const float rkn = rows.rk[n];
         const floatx4 fade = piece_decays(sh.cum[p], lane);
         const floatx4 own = turn == 0 ? TL::whole(sh.P[p][lane]) : sh.L[p][lane];
-        floatx4 x, N, from, C = {};
+        floatx4 x, N, from;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const float f = turn == 0 ? rq[i] : -(be[i] * rk[i]);
@@ -334,7 +332,7 @@ struct Back {
             N[i] = r + i > n && has ? sum[i] * own[i] : 0.0f;
             from[i] = r + i >= n ? 1.0f : 0.0f;
         }
-        C = F::mm(from, N, C);
+        floatx4 C = F::mm(from, N, {}).v;
 #pragma unroll
         for (int i = 0; i < 4; ++i) C[i] = r + i > n ? C[i] : 0.0f;
         const float c = row_sums(C, lane);
@@ -410,9 +408,8 @@ struct Back {
 #pragma unroll
         for (int i = 0; i < 4; ++i) a[i] = aq[i] * t.dq[i];
         const floatx4 qw = TL::wide(qc), kw = TL::wide(kc);
-        b = F::mm(m, qw, b);
-        b = F::mm(l, kw, b);
-        a = F::mm(mt, kw, a);
+        b = F::mm(l, kw, F::mm(m, qw, {b})).v;
+        a = F::mm(mt, kw, {a}).v;
         each_row<PART>(count, r, [&](int i) {
             sh.q[(s + r + i) * LD + col] = (E)(a[i] - qw[i] * rq[i] * rq[i] * yd[i]);
             sh.k[(s + r + i) * LD + col] = (E)(b[i] - kw[i] * rk[i] * rk[i] * kd[i]);
@@ -760,7 +757,8 @@ __global__ __launch_bounds__(4 * D, 2) void delta_bwd_map_kernel(DeltaArgs a)
                 if (from >= count) continue;
                 const int c = piece_end(from, count, ends, single) - from;
                 const bool done = ends >> (from + c - 1) & 1;
-                floatx4 kg = {}, km = {}, dU, dM, dR = {}, dN = {}, A, B, C;
+                typename TL::sum2 kg, km;
+                floatx4 dU, dM, A, B, C;
                 if (done) {
 #pragma unroll
                     for (int kt = 0; kt < KT; ++kt) Gs[kt] = M[kt] = floatx4{};
@@ -778,9 +776,9 @@ __global__ __launch_bounds__(4 * D, 2) void delta_bwd_map_kernel(DeltaArgs a)
                     dU[i] = r4 + i < c ? kg[i] * rows[p].au[r4 + i] : 0.0f;
                     dM[i] = r4 + i < c ? km[i] * rows[p].au[r4 + i] : 0.0f;
                 }
-                dU = TL::mm(sP[p][lane], dyc, dU);
-                dR = Tile<false>::mm(sT[p][lane], dU, dR);
-                dN = Tile<false>::mm(sT[p][lane], dM, dN);
+                dU = TL::mm(sP[p][lane], dyc, {dU}).v;
+                const floatx4 dR = Tile<false>::mm(sT[p][lane], dU, {}).v;
+                const floatx4 dN = Tile<false>::mm(sT[p][lane], dM, {}).v;
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const float ak = rows[p].ak[r4 + i];
@@ -792,9 +790,9 @@ __global__ __launch_bounds__(4 * D, 2) void delta_bwd_map_kernel(DeltaArgs a)
 #pragma unroll
                 for (int kt = 0; kt < KT; ++kt) {
                     const auto kc = along_col<BF, LD, true>(k, from, c, kt, lane);
-                    Gs[kt] = TL::mm(along_col<BF, LD, true>(q, from, c, kt, lane), x, Gs[kt] * rows[p].total);
-                    Gs[kt] = TL::mm(kc, y, Gs[kt]);
-                    M[kt] = TL::mm(kc, z, M[kt] * rows[p].total);
+                    const auto qc = along_col<BF, LD, true>(q, from, c, kt, lane);
+                    Gs[kt] = TL::mm(kc, y, TL::mm(qc, x, {Gs[kt] * rows[p].total})).v;
+                    M[kt] = TL::mm(kc, z, {M[kt] * rows[p].total}).v;
                 }
             }
             workgroup_lds_barrier();
