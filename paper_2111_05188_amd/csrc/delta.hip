@@ -8,7 +8,7 @@
 // then all waves run the pieces on their columns.
 //
 // 390 steps of 4,096 sequences of 4 heads of 64 in bf16: 1.70 ms, 3.8 GB at 2.3 TB/s.
-// Vector instructions bound it (61% of the time, the matrix units another 28%), above
+// Vector instructions (62% of the time) and the matrix units (40%) bound it, above
 // all the splits of the state into three bf16 numbers, once a piece.  Three workgroups a
 // CU; four (128 registers) or groups of 32 steps gain nothing (1.69 - 1.94 ms), nor do gates shared out over the waves (1.76).
 //

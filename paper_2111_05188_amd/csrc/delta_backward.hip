@@ -30,10 +30,18 @@
 //
 // 390 steps of 2,048 sequences of 4 heads of 64 in bf16 take 5.20 ms with the forward
 // call, where the bytes (3.8 GB) take 0.8 at the rate of a copy.  A group of 32 steps
-// is some 34,000 cycles of a workgroup, two of which a CU holds (71 KiB of LDS and 252
-// registers each); one alone is hardly faster: what bounds it is the chain of products
-// and splits of a wave, with the vector units at work 60% of the time and the matrix
-// units 26%.  Three workgroups (51 KiB, 168 registers) spill: 5.19 ms against 4.74.
+// is some 46,000 cycles of a workgroup, two of which a CU holds (75 KiB of LDS and 251
+// registers each): what bounds it is the chain of products and splits of a wave, with
+// the vector units at work 46% of the time and the matrix units 41% (2,600 vector
+// instructions and 380 products a wave and group; fp32, 26% and 47%).  Three workgroups
+// (51 KiB, 168 registers) spilled: 5.19 ms against 4.74 then.  The fp32 products as three
+// bf16 products over 32 of operands of three numbers: 5.22 ms, heads of 128 6.03 against
+// 4.93 (390 x 512), more registers and splits.
+//
+// Where a group has more than NP pieces (episodes that end in it, or a NaN or an infinity,
+// which makes each step a piece), each batch of NP starts from the kept state over the ones
+// before it: with an end at one step in 16, 390 x 512 x 4 x 64 in bf16 take 2.5 ms with the
+// forward call where they take 1.4 without any, at one in 4 6.8, at every step 38.
 #include "delta.hpp"
 
 namespace tpk {

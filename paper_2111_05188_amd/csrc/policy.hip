@@ -15,8 +15,9 @@
 // Everything up to the ratio is in 64 bits: a rounding of 2^-24 in sums of some
 // hundred would put a few of a million rows on the other side of the clip, with a
 // gradient of theirs there or not.  The arithmetic hides behind the rows' loads:
-// 1,597,440 rows of 100, bf16, 450 us (4.3 TB/s); 258,048 of 30, fp32, 40 us (3.1 TB/s), of
-// which the join of the workgroups' sums takes 6.
+// 1,597,440 rows of 100, bf16, 453 us (4.3 TB/s); 258,048 of 30, fp32, half of them past their
+// sequences' ends, 41 us (1.9 TB/s of what is read and written), of which the join of the
+// workgroups' sums takes 6.
 // LPR lanes have a row.
 #include "device.hpp"
 #include "internal.hpp"
@@ -24,8 +25,8 @@
 namespace tpk {
 namespace {
 
-// Workgroups, and parts of the sums.  1,597,440 rows of 100: 533 us with 1,024, 474
-// with 2,048; 258,048 rows of 30, which each have few of: 40 and 44.
+// Workgroups, and parts of the sums.  1,597,440 rows of 100: 533 us with 1,024, 453
+// with 2,048; 258,048 rows of 30, which each have few of: 41 and 48.
 constexpr int POLICY_BLOCKS = 2048, POLICY_FEW = 1024;
 // up to so many sequences every workgroup adds up the lengths by itself
 constexpr int POLICY_LENS = 8192;
